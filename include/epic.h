@@ -308,6 +308,103 @@ epic_status epic_fallback_commit(const epic_grammar* g, const epic_lexer_table* 
 epic_status epic_extract_witness(const epic_grammar* g, const epic_lexer_table* t, const int32_t* d_x, int32_t B,
                                  int32_t n, int32_t* d_terms, int32_t cap, int32_t* d_len, void* cuda_stream);
 
+/*
+ * ---- Between the model and the checks: rows of logits ----
+ *
+ * The calls above take candidate tokens with confidences; the calls below make
+ * them from a masked diffusion LM's logits, and bring the answer back into
+ * training.  They need no grammar and no lexer table, hold no workspace,
+ * allocate nothing and are asynchronous on `cuda_stream`; they may be captured
+ * in a CUDA graph and may overlap on different streams.
+ *
+ * d_logits is [B][n][V]: element v of position i of sequence b is at
+ * b * stride_b + i * stride_n + v, strides in elements (>= 0, any value: the
+ * positions of a padded vocabulary, a transposed batch).  A row of V elements
+ * may start at any multiple of the element size.  Arithmetic is in 32 bits
+ * whatever the type.  d_pos [B][k] picks the positions; NULL takes the first
+ * k <= n.  A position outside 0..n-1 counts as a row of no tokens.
+ */
+enum { EPIC_F32 = 0, EPIC_F16 = 1, EPIC_BF16 = 2 }; /* the element type of logits */
+
+/*
+ * The candidates of Alg. 1: the K tokens with the largest logits of every
+ * proposed position, largest first (ties: lowest token id; -0 equals +0), and
+ * their softmax probabilities at temperature T = d_temperature[b] (NULL: 1)
+ * over the whole row.  Outputs d_cand [B][k][K] int32 and d_conf [B][k][K]
+ * float32, as epic_validate_batch and epic_pick_candidates take them.  A token
+ * whose logit is -inf or NaN is no candidate; where fewer than K are left the
+ * rest are -1 with confidence 0 (no validity bit of theirs is ever 1).
+ * T = 0 gives confidences 1, 0, 0, ...; a T below 0 or NaN gives no candidates.
+ * +inf logits share all probability.  Errors: EPIC_ERR_INVALID_ARG (NULL
+ * pointers, sizes < 0, a bad dtype, d_logits not aligned to its elements, k > n
+ * without d_pos), EPIC_ERR_CAPACITY when K > 256.
+ */
+epic_status epic_propose_topk(const void* d_logits, int32_t dtype, int32_t B, int32_t n, int32_t V, int64_t stride_b,
+                              int64_t stride_n, const int32_t* d_pos, int32_t k, const float* d_temperature,
+                              int32_t K, int32_t* d_cand, float* d_conf, void* cuda_stream);
+
+/*
+ * Draws instead of ranks: S tokens of every proposed position, one for each
+ * given number d_u [B][k][S] of [0, 1].  Each sequence has its own rules, [B]
+ * or NULL (off): temperature T (1), top-k (<= 0: off), top-p (>= 1: off), min-p
+ * (<= 0: off).  With c = log2(e) / T and m the row's largest logit, a token
+ * weighs w = 2^((z - m) c), each operation rounded to 32 bits, in whole units
+ * q = rint(2^30 w).  In the order of epic_propose_topk, kept are the first top-k
+ * tokens; of these the ones before which less than floor(rint(2^24 top-p) Q / 2^24)
+ * of their mass Q lies; of these the ones with w >= min-p; always the first.  With
+ * Q the kept mass, the token is the first in order of ids whose kept mass up to and
+ * with it exceeds floor(floor(2^24 u) Q / 2^24).  Sums are whole numbers, so a
+ * draw depends on its row, rules and number only.  (u has 24 bits of use, and
+ * tokens less likely than 2^-31 of the likeliest are not drawn.)
+ * Outputs d_tok [B][k][S] int32 and d_prob [B][k][S] float32, the token's
+ * probability among the kept ones: candidates and confidences with K = S.
+ * T = 0 takes the likeliest token.  A row of no tokens (all -inf or NaN), a T
+ * below 0 or NaN, a NaN rule, or a number outside [0, 1] gives -1 and 0.
+ * Errors as epic_propose_topk.
+ */
+epic_status epic_sample_tokens(const void* d_logits, int32_t dtype, int32_t B, int32_t n, int32_t V, int64_t stride_b,
+                               int64_t stride_n, const int32_t* d_pos, int32_t k, const float* d_temperature,
+                               const int32_t* d_top_k, const float* d_top_p, const float* d_min_p, const float* d_u,
+                               int32_t S, int32_t* d_tok, float* d_prob, void* cuda_stream);
+
+/*
+ * Distillation of a student's logits [B][n][V] from a teacher's top entries:
+ * token ids d_ids [B][n][K] with logits or log-probabilities d_vals [B][n][K]
+ * float32.  An entry counts when its id is in 0..V-1, its value is not -inf and,
+ * with d_valid [B][n][K] (epic_validate_batch's bits of the teacher's
+ * candidates, or NULL), its bit is 1.  Per row, with p = softmax(vals / tau)
+ * over the entries that count and lse = logsumexp(z / tau) over the row,
+ *   loss    = w tau^2 sum_k p_k (log p_k - (z[id_k] / tau - lse))
+ *   grad_j  = w tau g (softmax(z / tau)_j - sum over entries of token j of p)
+ * with w = d_weight[b][i] (NULL: 1) and g the gradient that comes down.  A row
+ * without entries that count and a row of weight 0 (whose logits are not read)
+ * have loss and gradient 0.  A token of probability 0 under the student that
+ * the teacher wants gives loss +inf and a finite gradient; NaN or +inf logits
+ * give NaN.  Entries of one token add up.
+ * epic_distill_forward: d_loss and d_lse [B][n] float32 (d_lse is for the
+ * backward call; 0 where the row was not read).
+ * epic_distill_backward: d_grad, of the logits' type, [B][n][V] with its own
+ * strides in elements, from d_lse and g = d_grad_loss [B][n].
+ * epic_distill_step: loss and gradient in one call with g = 1, reading the
+ * logits once.
+ * d_grad must not overlap d_logits; rows of d_grad must not overlap each other.
+ * Errors: EPIC_ERR_INVALID_ARG as epic_propose_topk, and for tau not in
+ * (0, 3e38]; EPIC_ERR_CAPACITY when K > 1024.
+ */
+epic_status epic_distill_forward(const void* d_logits, int32_t dtype, int32_t B, int32_t n, int32_t V,
+                                 int64_t stride_b, int64_t stride_n, const int32_t* d_ids, const float* d_vals,
+                                 const uint8_t* d_valid, int32_t K, float tau, const float* d_weight, float* d_loss,
+                                 float* d_lse, void* cuda_stream);
+epic_status epic_distill_backward(const void* d_logits, int32_t dtype, int32_t B, int32_t n, int32_t V,
+                                  int64_t stride_b, int64_t stride_n, const int32_t* d_ids, const float* d_vals,
+                                  const uint8_t* d_valid, int32_t K, float tau, const float* d_weight,
+                                  const float* d_lse, const float* d_grad_loss, void* d_grad, int64_t grad_stride_b,
+                                  int64_t grad_stride_n, void* cuda_stream);
+epic_status epic_distill_step(const void* d_logits, int32_t dtype, int32_t B, int32_t n, int32_t V, int64_t stride_b,
+                              int64_t stride_n, const int32_t* d_ids, const float* d_vals, const uint8_t* d_valid,
+                              int32_t K, float tau, const float* d_weight, float* d_loss, void* d_grad,
+                              int64_t grad_stride_b, int64_t grad_stride_n, void* cuda_stream);
+
 /* Device counters accumulated since the object was created (or reset). */
 typedef struct {
   uint64_t checks;           /* single-candidate validity checks run           */

@@ -18,10 +18,12 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 # translation units, compiled in parallel and linked into one library
 _SRC = [os.path.join(_HERE, 'csrc', f) for f in
         ('epic.cu', 'kernels_walk.cu', 'kernels_cta.cu', 'kernels_select.cu', 'region_forward.cu', 'region_good.cu',
-         'region_check.cu', 'peak.cu', 'witness.cu', 'grammar.cpp')]
+         'region_check.cu', 'peak.cu', 'witness.cu', 'logits_pick.cu', 'logits_distill.cu', 'logit_launch.cpp',
+         'grammar.cpp')]
 _DEPS = _SRC + [os.path.join(_HERE, 'csrc', f) for f in
                 ('grammar.h', 'device.cuh', 'walk.cuh', 'cover.cuh', 'warpwalk.cuh', 'packs.cuh',
-                 'seqpack.cuh', 'launch.h', 'region.cuh', 'gscols.cuh', 'rows.cuh', 'skeleton.cuh')] + \
+                 'seqpack.cuh', 'launch.h', 'region.cuh', 'gscols.cuh', 'rows.cuh', 'skeleton.cuh',
+                 'logit_rows.cuh', 'logit_launch.h')] + \
     [os.path.join(_HERE, '..', 'include', 'epic.h'), os.path.join(_HERE, '..', 'include', 'epic_measure.h')]
 LIB_PATH = os.path.join(_HERE, '_build', 'libepic.so')
 ARCH_FLAGS = ['-gencode', 'arch=compute_103a,code=sm_103a']
@@ -91,6 +93,8 @@ EXPORTS = ('epic_grammar_create', 'epic_grammar_destroy', 'epic_grammar_lexer_st
            'epic_validate_batch', 'epic_validate_batch_noalloc',
            'epic_pick_candidates', 'epic_select_compatible_subset', 'epic_commit', 'epic_fallback_commit',
            'epic_extract_witness',
+           'epic_propose_topk', 'epic_sample_tokens', 'epic_distill_forward', 'epic_distill_backward',
+           'epic_distill_step',
            'epic_get_stats', 'epic_status_string', 'epic_measure_int_peak', 'epic_last_kernel_times')
 
 
@@ -118,6 +122,14 @@ def load(path: str | None = None):
     lib.epic_commit.argtypes = [vp, i32, i32, vp, i32, vp, vp, vp]
     lib.epic_fallback_commit.argtypes = [vp, vp, vp, i32, i32, vp, i32, vp, vp, i32, vp, vp, vp, vp, vp]
     lib.epic_extract_witness.argtypes = [vp, vp, vp, i32, i32, vp, i32, vp, vp]
+    i64, f32 = C.c_int64, C.c_float
+    rows = [vp, i32, i32, i32, i32, i64, i64]  # logits, dtype, B, n, V and their strides
+    lib.epic_propose_topk.argtypes = rows + [vp, i32, vp, i32, vp, vp, vp]
+    lib.epic_sample_tokens.argtypes = rows + [vp, i32, vp, vp, vp, vp, vp, i32, vp, vp, vp]
+    target = [vp, vp, vp, i32, f32, vp]  # ids, vals, valid, K, tau, weight
+    lib.epic_distill_forward.argtypes = rows + target + [vp, vp, vp]
+    lib.epic_distill_backward.argtypes = rows + target + [vp, vp, vp, i64, i64, vp]
+    lib.epic_distill_step.argtypes = rows + target + [vp, vp, i64, i64, vp]
     lib.epic_get_stats.argtypes = [vp, C.POINTER(_Stats), C.c_size_t, C.c_int]
     lib.epic_measure_int_peak.argtypes = [C.POINTER(C.c_double), C.POINTER(C.c_double), vp]
     lib.epic_measure_int_peak.restype = C.c_int
@@ -349,3 +361,111 @@ def extract_witness(g: Grammar, t: LexTable, x, terms, lengths, stream=None):
     B, n = x.shape
     _check(load().epic_extract_witness(g.h, t.h, _ptr(x), B, n, _ptr(terms), terms.shape[1], _ptr(lengths),
                                        _stream(stream)), 'epic_extract_witness')
+
+
+# ---------------------------------------------------------------- rows of logits
+
+def _rows(logits):
+    """(address, dtype, B, n, V, strides) of logits [B][n][V]; the last dimension has unit stride, the others any."""
+    import torch
+    code = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}.get(logits.dtype)
+    if code is None:
+        raise ValueError('expected float32, float16 or bfloat16 logits, got %s' % logits.dtype)
+    if not logits.is_cuda:
+        raise ValueError('expected a CUDA tensor')
+    if logits.dim() != 3:
+        raise ValueError('expected logits [B][n][V]')
+    B, n, V = logits.shape
+    sb, sn, sv = logits.stride()
+    if sv != 1 and V > 1:
+        raise ValueError('expected logits with unit stride along the vocabulary')
+    return logits.data_ptr(), code, B, n, V, sb, sn
+
+
+def _arg(t, shape, dtype, name):
+    """Device pointer of a contiguous tensor of that shape and type (None stays None)."""
+    if t is None:
+        return None
+    if t.shape != shape or t.dtype != dtype:
+        raise ValueError('%s: expected %s of shape %s, got %s of shape %s' % (name, dtype, tuple(shape), t.dtype,
+                                                                             tuple(t.shape)))
+    return _ptr(t)
+
+
+def propose_topk(logits, cand, conf, pos=None, temperature=None, stream=None):
+    """epic_propose_topk: the K most likely tokens of each proposed position
+    of logits [B][n][V] and their softmax probabilities, into cand [B][k][K]
+    int32 and conf [B][k][K] float32.  pos [B][k] int32 (None: the first k);
+    temperature [B] float32 (None: 1)."""
+    import torch
+    rows = _rows(logits)
+    B, k, K = cand.shape
+    _check(load().epic_propose_topk(
+        *rows, _arg(pos, (B, k), torch.int32, 'pos'), k, _arg(temperature, rows[2:3], torch.float32, 'temperature'), K,
+        _arg(cand, (rows[2], k, K), torch.int32, 'cand'), _arg(conf, (B, k, K), torch.float32, 'conf'),
+        _stream(stream)), 'epic_propose_topk')
+
+
+def sample_tokens(logits, u, tok, prob, pos=None, temperature=None, top_k=None, top_p=None, min_p=None, stream=None):
+    """epic_sample_tokens: a token of each proposed position of logits
+    [B][n][V] for every given number u [B][k][S] float32 of [0, 1], into tok
+    [B][k][S] int32 and prob [B][k][S] float32.  The rules are [B] tensors
+    (float32, top_k int32) or None (off)."""
+    import torch
+    rows = _rows(logits)
+    B = rows[2:3]
+    shape = (rows[2],) + tuple(u.shape[1:])
+    k, S = shape[1:]
+    f32, i32 = torch.float32, torch.int32
+    _check(load().epic_sample_tokens(
+        *rows, _arg(pos, shape[:2], i32, 'pos'), k, _arg(temperature, B, f32, 'temperature'),
+        _arg(top_k, B, i32, 'top_k'), _arg(top_p, B, f32, 'top_p'), _arg(min_p, B, f32, 'min_p'),
+        _arg(u, shape, f32, 'u'), S, _arg(tok, shape, i32, 'tok'), _arg(prob, shape, f32, 'prob'),
+        _stream(stream)), 'epic_sample_tokens')
+
+
+def _targets(rows, ids, vals, tau, weight, valid):
+    import torch
+    shape = tuple(rows[2:4]) + (ids.shape[-1],)
+    return (_arg(ids, shape, torch.int32, 'ids'), _arg(vals, shape, torch.float32, 'vals'),
+            _arg(valid, shape, torch.uint8, 'valid'), shape[2], tau,
+            _arg(weight, shape[:2], torch.float32, 'weight'))
+
+
+def _gradient(logits, grad):
+    rows = _rows(grad)
+    if grad.shape != logits.shape or grad.dtype != logits.dtype:
+        raise ValueError('grad: expected %s of shape %s' % (logits.dtype, tuple(logits.shape)))
+    return rows[0], rows[5], rows[6]
+
+
+def distill_forward(logits, ids, vals, loss, lse, tau=1.0, weight=None, valid=None, stream=None):
+    """epic_distill_forward: loss and lse [B][n] float32 of student logits
+    [B][n][V] against a teacher's entries ids [B][n][K] int32, vals [B][n][K]
+    float32; weight [B][n] float32, valid [B][n][K] uint8 (None: all count)."""
+    import torch
+    rows = _rows(logits)
+    _check(load().epic_distill_forward(
+        *rows, *_targets(rows, ids, vals, tau, weight, valid), _arg(loss, rows[2:4], torch.float32, 'loss'),
+        _arg(lse, rows[2:4], torch.float32, 'lse'), _stream(stream)), 'epic_distill_forward')
+
+
+def distill_backward(logits, ids, vals, lse, grad_loss, grad, tau=1.0, weight=None, valid=None, stream=None):
+    """epic_distill_backward: grad [B][n][V], of the logits' type, from the
+    forward call's lse and the gradient grad_loss [B][n] of its loss."""
+    import torch
+    rows = _rows(logits)
+    _check(load().epic_distill_backward(
+        *rows, *_targets(rows, ids, vals, tau, weight, valid), _arg(lse, rows[2:4], torch.float32, 'lse'),
+        _arg(grad_loss, rows[2:4], torch.float32, 'grad_loss'), *_gradient(logits, grad), _stream(stream)),
+        'epic_distill_backward')
+
+
+def distill_step(logits, ids, vals, loss, grad, tau=1.0, weight=None, valid=None, stream=None):
+    """epic_distill_step: loss [B][n] and its gradient [B][n][V] in one call,
+    for a training loop whose row weights are known before the loss."""
+    import torch
+    rows = _rows(logits)
+    _check(load().epic_distill_step(
+        *rows, *_targets(rows, ids, vals, tau, weight, valid), _arg(loss, rows[2:4], torch.float32, 'loss'),
+        *_gradient(logits, grad), _stream(stream)), 'epic_distill_step')
