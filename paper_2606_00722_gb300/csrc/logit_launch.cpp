@@ -9,6 +9,7 @@ namespace epic {
 constexpr size_t kSlice = 64 << 10;
 constexpr size_t kSliceMax = 192 << 10;
 constexpr int kClusterMax = 8;
+constexpr size_t kSmemDefault = 16 << 10;  // with the kernels' own arrays within the 48 KB that need no asking
 
 RowShape row_shape(long long rows, int V, int size) {
   const long long E = 16 / size;
@@ -38,7 +39,7 @@ epic_status check_rows(const void* logits, int dtype, int B, int n, int V, int64
 
 epic_status launch_rows(const void* kernel, const RowShape& p, long long rows, void* args, cudaStream_t st) {
   if (rows > 0x7fffffffll / p.ctas) return EPIC_ERR_CAPACITY;
-  if (p.smem > (32 << 10) &&
+  if (p.smem > kSmemDefault &&
       cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)p.smem) != cudaSuccess) {
     cudaGetLastError();
     return EPIC_ERR_CUDA;

@@ -120,7 +120,8 @@ struct Slice {
   int head;           // elements between row16 and the row
   int c0, n;          // first chunk and number of chunks
   int V;
-  int wlo, whi;  // this warp's chunks of the slice
+  int wper;      // chunks of a warp: warp w has those from w * wper on
+  int wlo, whi;  // this warp's
   bool staged;
 
   // index of a chunk's first element (negative in a row's first chunk)
@@ -162,23 +163,93 @@ struct Slice {
     buf = shared;
     staged = a.staged;
     const int warps = blockDim.x / 32, w = threadIdx.x / 32;
-    const int wper = (((n + warps - 1) / warps) + 31) & ~31;
+    wper = (n + warps - 1) / warps;
     wlo = min(w * wper, n);
     whi = min(wlo + wper, n);
-    if (!staged) return;
+  }
+
+  // f(c) for each chunk of this thread as it arrives in shared memory: all loads are issued first, in four groups
+  template <typename F>
+  __device__ __forceinline__ void stage(F f) const {
     const int lane = threadIdx.x % 32;
-    for (int c = wlo + lane; c < whi; c += 32) {
-      const long long i0 = first(c);
-      if (i0 >= 0 && i0 + E <= V) {
-        const uint32_t dst = (uint32_t)__cvta_generic_to_shared(buf + c);
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(row16 + (size_t)(c0 + c) * 16)
-                     : "memory");
+    if (!staged) {
+      for (int c = wlo + lane; c < whi; c += 32) f(from_global(c));
+      return;
+    }
+    const int quarter = (((whi - wlo + 31) / 32 + 3) / 4) * 32;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int end = min(wlo + (g + 1) * quarter, whi);
+      for (int c = wlo + g * quarter + lane; c < end; c += 32) {
+        const long long i0 = first(c);
+        if (i0 >= 0 && i0 + E <= V) {
+          const uint32_t dst = (uint32_t)__cvta_generic_to_shared(buf + c);
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(row16 + (size_t)(c0 + c) * 16)
+                       : "memory");
+        } else {
+          buf[c] = from_global(c);
+        }
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      if (g == 0) asm volatile("cp.async.wait_group 3;" ::: "memory");
+      if (g == 1) asm volatile("cp.async.wait_group 2;" ::: "memory");
+      if (g == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
+      if (g == 3) asm volatile("cp.async.wait_group 0;" ::: "memory");
+      const int end = min(wlo + (g + 1) * quarter, whi);
+      for (int c = wlo + g * quarter + lane; c < end; c += 32) f(buf[c]);
+    }
+  }
+};
+
+// Running maximum of a thread's chunks, two 16-bit elements an instruction; kNan: NaN if any element is, else NaN is
+// left out.
+template <typename T, bool kNan>
+struct ChunkMax {
+  float f;
+  uint32_t h;
+  __device__ ChunkMax() {
+    f = -CUDART_INF_F;
+    h = std::is_same_v<T, __nv_bfloat16> ? 0xff80ff80u : 0xfc00fc00u;  // -inf twice
+  }
+  __device__ __forceinline__ static uint32_t max2(uint32_t a, uint32_t b) {
+    if constexpr (std::is_same_v<T, __nv_bfloat16>) {
+      if constexpr (kNan) {
+        asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(a) : "r"(a), "r"(b));
       } else {
-        buf[c] = from_global(c);
+        asm("max.bf16x2 %0, %1, %2;" : "=r"(a) : "r"(a), "r"(b));
+      }
+    } else {
+      if constexpr (kNan) {
+        asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(a) : "r"(a), "r"(b));
+      } else {
+        asm("max.f16x2 %0, %1, %2;" : "=r"(a) : "r"(a), "r"(b));
       }
     }
-    asm volatile("cp.async.commit_group;" ::: "memory");
-    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    return a;
+  }
+  __device__ __forceinline__ static float max1(float a, float b) {
+    if constexpr (kNan) {
+      asm("max.NaN.f32 %0, %1, %2;" : "=f"(a) : "f"(a), "f"(b));
+      return a;
+    }
+    return fmaxf(a, b);
+  }
+  __device__ __forceinline__ void add(const uint4& c) {
+    if constexpr (sizeof(T) == 4) {
+      f = max1(f, max1(max1(__uint_as_float(c.x), __uint_as_float(c.y)),
+                       max1(__uint_as_float(c.z), __uint_as_float(c.w))));
+    } else {
+      h = max2(h, max2(max2(c.x, c.y), max2(c.z, c.w)));
+    }
+  }
+  __device__ __forceinline__ float value() const {
+    if constexpr (sizeof(T) == 4) return f;
+    T v[2];
+    memcpy(v, &h, 4);
+    return max1(to_float<T>(v[0]), to_float<T>(v[1]));
   }
 };
 

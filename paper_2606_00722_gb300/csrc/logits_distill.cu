@@ -182,13 +182,9 @@ __global__ void __launch_bounds__(kRowThreads) k_distill(DistillArgs a) {
   }
   s.open(row_address<T>(a.rows, r), a.rows.V, a.rows, rank, staged);
   const float c2 = kLog2e / a.tau;
-  float m = -CUDART_INF_F;
-  for (int c = s.wlo + (int)(threadIdx.x % 32); c < s.whi; c += 32) {
-    float f[E];
-    unpack<T>(s.chunk(c), f);
-#pragma unroll
-    for (int e = 0; e < E; ++e) m = max_nan(m, f[e]);
-  }
+  ChunkMax<T, true> top;
+  s.stage([&](const uint4& c) { top.add(c); });
+  float m = top.value();
   m = block_reduce(m, MaxNan(), t.red, &t.value);
   float sum = 0.0f;
   if (m != -CUDART_INF_F)
