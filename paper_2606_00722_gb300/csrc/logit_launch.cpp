@@ -4,23 +4,22 @@
 
 namespace epic {
 
-// Bytes of a row that one CTA stages, and the most that it may: slices of this size leave room for three CTAs on an SM,
-// so that one row's loads run under another's passes.
-constexpr size_t kSlice = 64 << 10;
-constexpr size_t kSliceMax = 192 << 10;
 constexpr int kClusterMax = 8;
-constexpr size_t kSmemDefault = 16 << 10;  // with the kernels' own arrays within the 48 KB that need no asking
+constexpr int kThreadsMax = 512;
 
+// One CTA a row where the rows fill the GPU (two CTAs an SM).  Fewer rows are cut over clusters of up to eight CTAs,
+// down to a batch of 128 chunks a warp.
 RowShape row_shape(long long rows, int V, int size) {
   const long long E = 16 / size;
-  const long long chunks = V ? (V + E - 1 + E - 1) / E : 0;  // wherever the row starts in its first chunk
+  const long long chunks = V ? (V + E - 2) / E + 1 : 0;  // wherever the row starts in its first chunk
+  const long long full = 2 * 152;
   RowShape p = {};
   p.ctas = 1;
-  while (p.ctas < kClusterMax && (chunks + p.ctas - 1) / p.ctas * 16 > (long long)kSlice) p.ctas *= 2;
+  while (p.ctas < kClusterMax &&
+         (chunks * E > (long long)p.ctas * kSliceElems || (rows * p.ctas * 2 <= full && chunks > p.ctas * 2048)))
+    p.ctas *= 2;
   p.per = (int)((chunks + p.ctas - 1) / p.ctas);
-  p.staged = (size_t)p.per * 16 <= kSliceMax;
-  p.smem = p.staged ? (size_t)p.per * 16 : 0;
-  p.threads = std::min(256, std::max(64, (p.per + 31) / 32 * 32));
+  p.threads = (int)std::min<long long>(kThreadsMax, std::max<long long>(64, (p.per + 127) / 128 * 32));
   return p;
 }
 
@@ -29,6 +28,7 @@ epic_status check_rows(const void* logits, int dtype, int B, int n, int V, int64
   if (dtype != EPIC_F32 && dtype != EPIC_F16 && dtype != EPIC_BF16) return EPIC_ERR_INVALID_ARG;
   if (B < 0 || n < 0 || V < 0 || k < 0 || stride_b < 0 || stride_n < 0) return EPIC_ERR_INVALID_ARG;
   if (!pos && k > n) return EPIC_ERR_INVALID_ARG;
+  if (V > 0x7fffffff - 4096) return EPIC_ERR_CAPACITY;  // element indices and what lies past a row's end fit 32 bits
   if ((long long)B * k == 0) return EPIC_OK;
   if (n > 0 && V > 0) {
     if (!logits) return EPIC_ERR_INVALID_ARG;
@@ -39,15 +39,9 @@ epic_status check_rows(const void* logits, int dtype, int B, int n, int V, int64
 
 epic_status launch_rows(const void* kernel, const RowShape& p, long long rows, void* args, cudaStream_t st) {
   if (rows > 0x7fffffffll / p.ctas) return EPIC_ERR_CAPACITY;
-  if (p.smem > kSmemDefault &&
-      cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)p.smem) != cudaSuccess) {
-    cudaGetLastError();
-    return EPIC_ERR_CUDA;
-  }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(rows * p.ctas));
   cfg.blockDim = dim3(p.threads);
-  cfg.dynamicSmemBytes = p.smem;
   cfg.stream = st;
   cudaLaunchAttribute at = {};
   at.id = cudaLaunchAttributeClusterDimension;

@@ -8,12 +8,13 @@
 
 namespace epic {
 
+// Most elements of a slice whose masses, in parts of 15 and 16 bits, a histogram's 32-bit bins can add up.
+constexpr int kSliceElems = 131000;
+
 struct RowShape {
   int ctas;     // CTAs of a row: one cluster
   int threads;  // of a CTA
   int per;      // chunks of 16 bytes per CTA
-  int staged;   // whether a CTA's chunks fit in shared memory
-  size_t smem;  // dynamic shared memory of a CTA
 };
 
 // A row of V elements of `size` bytes, `rows` of them in the call.

@@ -1,14 +1,18 @@
-// Rows of logits on chip: what the kernels between a model's output and the
-// constraint work share.
+// Rows of logits: what the kernels between a model's output and the constraint
+// work share.
 //
-// A row of V logits belongs to a cluster of CTAs.  It is cut into chunks of 16
-// bytes from the aligned address at or below its first element; each CTA of
-// the cluster owns a run of chunks, staged once in its shared memory, so every
-// further pass over the row costs no memory traffic.  Rows that do not fit the
-// cluster's shared memory are read from global memory in every pass instead.
-// Within a CTA a warp owns a contiguous run of chunks and reads it 32 chunks at
-// a time, so sums by warp are sums in index order, and a thread reads in every
-// pass the chunks that it staged itself: staging needs no barrier.
+// A row of V logits belongs to a cluster of CTAs (one CTA where there are rows
+// enough).  It is cut into chunks of 16 bytes from the aligned address at or
+// below its first element; a CTA owns a run of chunks (its slice), a warp of it
+// a run of those, and reads 128 of them at a time, four a lane.  So sums by warp
+// and by batch are sums in index order, and a lane meets the same chunks in
+// every pass.  Nothing is staged: the first pass comes from memory, later ones
+// from the L2 cache, which holds the rows in flight (two CTAs of 512 threads an
+// SM are 304 rows, 77 MB at 126,000 tokens of 16 bits).  Slices staged in shared
+// memory were slower: an SM then holds three of 63 KB, each for the 10 us of
+// two cluster barriers and its passes, where 4 us would keep memory busy (the
+// 32 best of 1,024 x 126,000: 111 us staged in clusters of four, 99 us from L2
+// with a CTA a row, everything else alike).
 //
 // The order of a row: value descending, ties by index ascending, as one 64-bit
 // key (larger comes first).  NaN and -inf are not in the order.
@@ -29,8 +33,9 @@ namespace cg = cooperative_groups;
 
 typedef unsigned long long u64;
 
-constexpr int kRowThreads = 256;              // most threads of a row CTA
+constexpr int kRowThreads = 512;  // most threads of a row CTA
 constexpr int kRowWarps = kRowThreads / 32;
+constexpr int kRowCluster = 8;  // most CTAs of a row (the portable limit of a cluster)
 constexpr float kLog2e = 1.4426950408889634f;
 
 __device__ __forceinline__ float exp2_32(float x) {
@@ -45,8 +50,7 @@ struct RowArgs {
   long long stride_b, stride_n;  // in elements
   const int32_t* pos;            // [B][k] or NULL
   int n, k, V;
-  int per;     // chunks per CTA
-  int staged;  // the slices fit in shared memory
+  int per;  // chunks per CTA
 };
 
 template <typename T>
@@ -111,98 +115,106 @@ __device__ __forceinline__ uint4 pack(const float (&f)[ElemOf<T>::E]) {
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+constexpr int kBatch = 128;  // chunks that a warp reads at a time
+
+template <typename T>
+__device__ __forceinline__ uint4 empty_chunk() {  // all -inf
+  const uint32_t x = sizeof(T) == 4 ? 0xff800000u : std::is_same_v<T, __nv_bfloat16> ? 0xff80ff80u : 0xfc00fc00u;
+  return make_uint4(x, x, x, x);
+}
+
 // One CTA's part of a row.
 template <typename T>
 struct Slice {
   static constexpr int E = ElemOf<T>::E;
   const char* row16;  // the row's address, rounded down to 16 bytes
-  uint4* buf;         // staged chunks
   int head;           // elements between row16 and the row
   int c0, n;          // first chunk and number of chunks
   int V;
   int wper;      // chunks of a warp: warp w has those from w * wper on
   int wlo, whi;  // this warp's
-  bool staged;
+  int flo, fhi;  // the chunks whose 16 bytes are all of this row
 
   // index of a chunk's first element (negative in a row's first chunk)
-  __device__ __forceinline__ long long first(int c) const { return (long long)(c0 + c) * E - head; }
+  __device__ __forceinline__ int first(int c) const { return (c0 + c) * E - head; }
 
-  __device__ uint4 from_global(int c) const {
-    const long long i0 = first(c);
-    const char* p = row16 + (size_t)(c0 + c) * 16;
-    if (i0 >= 0 && i0 + E <= V) return __ldg(reinterpret_cast<const uint4*>(p));
+  __device__ __forceinline__ const char* address(int c) const { return row16 + (size_t)(c0 + c) * 16; }
+
+  // a chunk of the slice; -inf for what is outside the row
+  __device__ uint4 chunk(int c) const {
+    if (c >= flo && c < fhi) return __ldg(reinterpret_cast<const uint4*>(address(c)));
+    const T* p = reinterpret_cast<const T*>(address(c));
+    const int i0 = first(c);
     float f[E];
 #pragma unroll
-    for (int e = 0; e < E; ++e)
-      f[e] = i0 + e >= 0 && i0 + e < V ? to_float<T>(reinterpret_cast<const T*>(p)[e]) : -CUDART_INF_F;
+    for (int e = 0; e < E; ++e) f[e] = i0 + e >= 0 && i0 + e < V ? to_float<T>(p[e]) : -CUDART_INF_F;
     return pack<T>(f);
   }
 
-  __device__ __forceinline__ uint4 chunk(int c) const { return staged ? buf[c] : from_global(c); }
-
-  // the row of an element already known to be in the slice
-  __device__ float at(int idx) const {
-    const int c = (idx + head) / E - c0;
-    return staged ? to_float<T>(reinterpret_cast<const T*>(buf + c)[(idx + head) % E])
-                  : to_float<T>(reinterpret_cast<const T*>(row16)[idx + head]);
-  }
+  // the value of an element of the row
+  __device__ float at(int idx) const { return to_float<T>(reinterpret_cast<const T*>(row16)[(size_t)head + idx]); }
 
   // first and past-the-end index of the elements in the slice
-  __device__ __forceinline__ int lo() const { return (int)max(first(0), 0ll); }
-  __device__ __forceinline__ int hi() const { return (int)min(max(first(n), 0ll), (long long)V); }
+  __device__ __forceinline__ int lo() const { return max(first(0), 0); }
+  __device__ __forceinline__ int hi() const { return min(max(first(n), 0), V); }
 
   // the slice of the row at `addr` (NULL: a row of no elements) for CTA `rank` of the cluster
-  __device__ void open(const void* addr, int V_, const RowArgs& a, int rank, uint4* shared) {
-    V = addr ? V_ : 0;
+  __device__ void open(const void* addr, const RowArgs& a, int rank) {
+    V = addr ? a.V : 0;
     const uintptr_t p = reinterpret_cast<uintptr_t>(addr);
     row16 = reinterpret_cast<const char*>(p & ~(uintptr_t)15);
     head = (int)(p & 15) / (int)sizeof(T);
-    const long long total = V ? ((long long)head + V + E - 1) / E : 0;
+    const int total = V ? (head + V - 1) / E + 1 : 0;
     c0 = rank * a.per;
-    n = (int)min(max(total - c0, 0ll), (long long)a.per);
-    buf = shared;
-    staged = a.staged;
+    n = min(max(total - c0, 0), a.per);
     const int warps = blockDim.x / 32, w = threadIdx.x / 32;
     wper = (n + warps - 1) / warps;
     wlo = min(w * wper, n);
     whi = min(wlo + wper, n);
+    // the row's first and last chunk may have elements of other rows
+    flo = c0 == 0 && head > 0 ? 1 : 0;
+    fhi = c0 + n == total && (head + V) % E != 0 ? n - 1 : n;
   }
 
-  // f(c) for each chunk of this thread as it arrives in shared memory: all loads are issued first, in four groups
+  // f(v, c) for this warp's batches: v are this lane's chunks c, c + 32, c + 64 and c + 96, of -inf past the warp's end
   template <typename F>
-  __device__ __forceinline__ void stage(F f) const {
-    const int lane = threadIdx.x % 32;
-    if (!staged) {
-      for (int c = wlo + lane; c < whi; c += 32) f(from_global(c));
-      return;
-    }
-    const int quarter = (((whi - wlo + 31) / 32 + 3) / 4) * 32;
+  __device__ __forceinline__ void sweep(F f) const {
+    for (int base = wlo; base < whi; base += kBatch) {
+      const int c = base + (int)(threadIdx.x % 32);
+      uint4 v[4];
+      if (base >= flo && base + kBatch <= min(fhi, whi)) {
+        const uint4* p = reinterpret_cast<const uint4*>(address(c));
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const int end = min(wlo + (g + 1) * quarter, whi);
-      for (int c = wlo + g * quarter + lane; c < end; c += 32) {
-        const long long i0 = first(c);
-        if (i0 >= 0 && i0 + E <= V) {
-          const uint32_t dst = (uint32_t)__cvta_generic_to_shared(buf + c);
-          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(row16 + (size_t)(c0 + c) * 16)
-                       : "memory");
-        } else {
-          buf[c] = from_global(c);
-        }
+        for (int i = 0; i < 4; ++i) v[i] = __ldg(p + 32 * i);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = c + 32 * i < whi ? chunk(c + 32 * i) : empty_chunk<T>();
       }
-      asm volatile("cp.async.commit_group;" ::: "memory");
-    }
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      if (g == 0) asm volatile("cp.async.wait_group 3;" ::: "memory");
-      if (g == 1) asm volatile("cp.async.wait_group 2;" ::: "memory");
-      if (g == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
-      if (g == 3) asm volatile("cp.async.wait_group 0;" ::: "memory");
-      const int end = min(wlo + (g + 1) * quarter, whi);
-      for (int c = wlo + g * quarter + lane; c < end; c += 32) f(buf[c]);
+      f(v, c);
     }
   }
 };
+
+// Two 32-bit operations in one instruction, each rounded as the single one.
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 y;
+  asm("{.reg .b64 a, b, y; mov.b64 a, {%2, %3}; mov.b64 b, {%4, %5}; add.rn.f32x2 y, a, b; mov.b64 {%0, %1}, y;}"
+      : "=f"(y.x), "=f"(y.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return y;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 y;
+  asm("{.reg .b64 a, b, y; mov.b64 a, {%2, %3}; mov.b64 b, {%4, %5}; mul.rn.f32x2 y, a, b; mov.b64 {%0, %1}, y;}"
+      : "=f"(y.x), "=f"(y.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return y;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 y;
+  asm("{.reg .b64 a, b, c, y; mov.b64 a, {%2, %3}; mov.b64 b, {%4, %5}; mov.b64 c, {%6, %7}; "
+      "fma.rn.f32x2 y, a, b, c; mov.b64 {%0, %1}, y;}"
+      : "=f"(y.x), "=f"(y.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return y;
+}
 
 // Running maximum of a thread's chunks, two 16-bit elements an instruction; kNan: NaN if any element is, else NaN is
 // left out.
@@ -212,7 +224,7 @@ struct ChunkMax {
   uint32_t h;
   __device__ ChunkMax() {
     f = -CUDART_INF_F;
-    h = std::is_same_v<T, __nv_bfloat16> ? 0xff80ff80u : 0xfc00fc00u;  // -inf twice
+    h = empty_chunk<T>().x;
   }
   __device__ __forceinline__ static uint32_t max2(uint32_t a, uint32_t b) {
     if constexpr (std::is_same_v<T, __nv_bfloat16>) {
@@ -245,6 +257,10 @@ struct ChunkMax {
       h = max2(h, max2(max2(c.x, c.y), max2(c.z, c.w)));
     }
   }
+  __device__ __forceinline__ void add(const uint4 (&v)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) add(v[i]);
+  }
   __device__ __forceinline__ float value() const {
     if constexpr (sizeof(T) == 4) return f;
     T v[2];
@@ -254,7 +270,7 @@ struct ChunkMax {
 };
 
 template <typename T>
-__device__ __forceinline__ const void* row_address(const RowArgs& a, long long r) {
+__device__ __forceinline__ const T* row_address(const RowArgs& a, long long r) {
   const long long b = r / a.k;
   const int j = (int)(r - b * a.k);
   const int i = a.pos ? a.pos[r] : j;

@@ -7,9 +7,9 @@
 // A row with no entry that counts, or with w = 0, has loss and gradient 0.
 // Sums are held in 32 bits; the gradient is rounded once, to the logits' type.
 //
-// The forward pass and the one that also writes the gradient stage the row in a
-// cluster's shared memory (one read of the logits, one write of the gradient);
-// the backward pass has the row's logsumexp and streams.
+// Each row is read from memory once: for the loss in one pass with a running
+// maximum, for loss and gradient with a second pass from the caches.  The
+// backward pass has the row's logsumexp and reads the row once again.
 #include "../../include/epic.h"
 #include "logit_launch.h"
 #include "logit_rows.cuh"
@@ -39,44 +39,28 @@ struct Targets {
   float p[kMaxTargets];
   float lp[kMaxTargets];
   int id[kMaxTargets];  // -1: does not count
-  float red[kRowWarps];
-  float value;
+  int any;
+  float warp_m[kRowWarps], warp_s[kRowWarps];
+  float m, s;  // of the CTA
 };
 
 // larger of two, NaN if either is
-__device__ __forceinline__ float max_nan(float a, float b) {
-  float y;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
-  return y;
+__device__ __forceinline__ float max_nan(float a, float b) { return ChunkMax<float, true>::max1(a, b); }
+
+__device__ __forceinline__ float warp_add(float x) {
+  for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(~0u, x, o);
+  return x;
 }
-
-struct MaxNan {
-  __device__ float operator()(float a, float b) const { return max_nan(a, b); }
-};
-struct Add {
-  __device__ float operator()(float a, float b) const { return a + b; }
-};
-
-// one value from all threads, in a fixed order; every thread gets it
-template <typename Op>
-__device__ float block_reduce(float x, Op op, float* red, float* value) {
-  for (int o = 16; o; o >>= 1) x = op(x, __shfl_xor_sync(~0u, x, o));
-  if (threadIdx.x % 32 == 0) red[threadIdx.x / 32] = x;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int w = 1; w < (int)blockDim.x / 32; ++w) x = op(x, red[w]);
-    *value = x;
-  }
-  __syncthreads();
-  x = *value;
-  __syncthreads();
+__device__ __forceinline__ float warp_max_nan(float x) {
+  for (int o = 16; o; o >>= 1) x = max_nan(x, __shfl_xor_sync(~0u, x, o));
   return x;
 }
 
-// p and log p of the row's entries; false when none counts
-__device__ bool teacher(const DistillArgs& a, long long r, Targets& t) {
+// One warp: p and log p of the row's entries, and whether any counts.
+__device__ void teacher(const DistillArgs& a, long long r, Targets& t) {
+  const int lane = threadIdx.x % 32;
   float m = -CUDART_INF_F;
-  for (int k = threadIdx.x; k < a.K; k += blockDim.x) {
+  for (int k = lane; k < a.K; k += 32) {
     const long long o = r * a.K + k;
     const int id = a.ids[o];
     const float v = a.vals[o];
@@ -85,45 +69,100 @@ __device__ bool teacher(const DistillArgs& a, long long r, Targets& t) {
     t.lp[k] = v / a.tau;
     if (counts) m = max_nan(m, t.lp[k]);
   }
-  m = block_reduce(m, MaxNan(), t.red, &t.value);
-  if (m == -CUDART_INF_F) return false;
+  m = warp_max_nan(m);
+  if (lane == 0) t.any = m != -CUDART_INF_F;
   float sum = 0.0f;
-  for (int k = threadIdx.x; k < a.K; k += blockDim.x) {
+  for (int k = lane; k < a.K; k += 32) {
     t.lp[k] -= m;
     t.p[k] = t.id[k] >= 0 ? expf(t.lp[k]) : 0.0f;
     sum += t.p[k];
   }
-  sum = block_reduce(sum, Add(), t.red, &t.value);
+  sum = warp_add(sum);
   const float log_sum = logf(sum);
-  for (int k = threadIdx.x; k < a.K; k += blockDim.x) {
+  for (int k = lane; k < a.K; k += 32) {
     t.p[k] /= sum;
     t.lp[k] -= log_sum;
   }
-  __syncthreads();
-  return true;
 }
 
-// The slice's part of a gradient row: q(z) is the student's probability of a logit, the target's share is taken off
-// where the slice has it.
-template <typename T, typename Q>
-__device__ void write_gradient(const Slice<T>& s, T* grad, float coef, const Targets& t, int K, Q q) {
-  constexpr int E = ElemOf<T>::E;
-  const bool same = (reinterpret_cast<uintptr_t>(grad) & 15) == (uintptr_t)s.head * sizeof(T);
-  for (int c = s.wlo + (int)(threadIdx.x % 32); c < s.whi; c += 32) {
-    float f[E];
-    unpack<T>(s.chunk(c), f);
-    const long long i0 = s.first(c);
+// A chunk of the row at a distance of `by` bytes (0..15) past the start of `a`, b being the chunk after a.
+__device__ __forceinline__ uint4 shifted(const uint4& a, const uint4& b, int by) {
+  uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+  if (by & 8)
 #pragma unroll
-    for (int e = 0; e < E; ++e) f[e] = coef * q(f[e]);
-    if (same && i0 >= 0 && i0 + E <= s.V) {
+    for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
+  if (by & 4)
+#pragma unroll
+    for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
+  const int bits = 8 * (by & 3);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], bits);
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// The slice's elements of a gradient row, g(z) each.  The chunks are the gradient's: where its row starts elsewhere in
+// 16 bytes than the logits' row does, two chunks of logits are read for one of gradient.
+template <typename T, typename G>
+__device__ void write_row(const Slice<T>& s, T* grad, G g) {
+  constexpr int E = ElemOf<T>::E;
+  const int lo = s.lo(), hi = s.hi();
+  const int ghead = (int)(reinterpret_cast<uintptr_t>(grad) & 15) / (int)sizeof(T);
+  const auto put = [&](const uint4& v, int i0) {  // elements i0 .. i0 + E - 1
+    float f[E];
+    unpack<T>(v, f);
+#pragma unroll
+    for (int e = 0; e < E; ++e) f[e] = g(f[e]);
+    if (i0 >= lo && i0 + E <= hi) {
       *reinterpret_cast<uint4*>(grad + i0) = pack<T>(f);
     } else {
 #pragma unroll
       for (int e = 0; e < E; ++e)
-        if (i0 + e >= 0 && i0 + e < s.V) grad[i0 + e] = from_float<T>(f[e]);
+        if (i0 + e >= lo && i0 + e < hi) grad[i0 + e] = from_float<T>(f[e]);
+    }
+  };
+  if (ghead == s.head) {
+    s.sweep([&](const uint4 (&v)[4], int c) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (c + 32 * i < s.whi) put(v[i], s.first(c + 32 * i));
+    });
+    return;
+  }
+  if (lo >= hi) return;
+  // gradient chunk j starts `by` bytes into the chunk of logits at or before its first element
+  const int ahead = s.head - ghead, by = ((ahead + E) % E) * (int)sizeof(T), back = ahead < 0 ? 1 : 0;
+  for (int j = (lo + ghead) / E + (int)threadIdx.x; j <= (hi - 1 + ghead) / E; j += blockDim.x) {
+    const int c = j - back - s.c0;  // of the slice; a neighbour's elements are not put
+    uint4 a = empty_chunk<T>(), b = a;
+    if (c >= 0 && c < s.n) a = s.chunk(c);
+    if (c + 1 >= 0 && c + 1 < s.n) b = s.chunk(c + 1);
+    put(shifted(a, b, by), j * E - ghead);
+  }
+}
+
+template <typename T>
+__device__ void write_zeros(const Slice<T>& s, T* grad) {
+  constexpr int E = ElemOf<T>::E;
+  const int lo = s.lo(), hi = s.hi();
+  const int ghead = (int)(reinterpret_cast<uintptr_t>(grad) & 15) / (int)sizeof(T);
+  if (lo >= hi) return;
+  for (int j = (lo + ghead) / E + (int)threadIdx.x; j <= (hi - 1 + ghead) / E; j += blockDim.x) {
+    const int i0 = j * E - ghead;
+    if (i0 >= lo && i0 + E <= hi) {
+      *reinterpret_cast<uint4*>(grad + i0) = make_uint4(0, 0, 0, 0);
+    } else {
+      for (int e = 0; e < E; ++e)
+        if (i0 + e >= lo && i0 + e < hi) grad[i0 + e] = from_float<T>(0.0f);
     }
   }
-  __syncthreads();  // the targets' elements are written again, by whichever thread has them
+}
+
+// coef (q(z) - the target's share) over the slice.  The few elements that have a share are written again, each by a
+// thread of its own, after a barrier.
+template <typename T, typename Q>
+__device__ void write_gradient(const Slice<T>& s, T* grad, float coef, const Targets& t, int K, Q q) {
+  write_row(s, grad, [=](float z) { return coef * q(z); });
+  __syncthreads();
   const int lo = s.lo(), hi = s.hi();
   for (int k = threadIdx.x; k < K; k += blockDim.x) {
     const int id = t.id[k];
@@ -136,116 +175,131 @@ __device__ void write_gradient(const Slice<T>& s, T* grad, float coef, const Tar
 }
 
 template <typename T>
-__device__ void write_zeros(const Slice<T>& s, T* grad) {
-  constexpr int E = ElemOf<T>::E;
-  const bool same = (reinterpret_cast<uintptr_t>(grad) & 15) == (uintptr_t)s.head * sizeof(T);
-  for (int c = s.wlo + (int)(threadIdx.x % 32); c < s.whi; c += 32) {
-    const long long i0 = s.first(c);
-    if (same && i0 >= 0 && i0 + E <= s.V) {
-      *reinterpret_cast<uint4*>(grad + i0) = make_uint4(0, 0, 0, 0);
-    } else {
-      for (int e = 0; e < E; ++e)
-        if (i0 + e >= 0 && i0 + e < s.V) grad[i0 + e] = from_float<T>(0.0f);
-    }
-  }
-}
-
-template <typename T>
 __device__ __forceinline__ T* gradient_row(const DistillArgs& a, long long r) {
   const long long b = r / a.rows.k;
   return static_cast<T*>(a.grad) + b * a.gstride_b + (r - b * a.rows.k) * a.gstride_n;
 }
 
-// loss, and with a.grad the gradient: one cluster a row
+// Loss, and with a.grad the gradient: one cluster a row.  One pass keeps each lane's maximum so far and the sum of
+// exponentials relative to it; the gradient's pass reads the row again, from the caches.
 template <typename T>
-__global__ void __launch_bounds__(kRowThreads) k_distill(DistillArgs a) {
-  extern __shared__ uint4 staged[];
+__global__ void __launch_bounds__(kRowThreads, 2) k_distill(DistillArgs a) {
   __shared__ Targets t;
-  __shared__ float cta_m, cta_s;
   auto cluster = cg::this_cluster();
   constexpr int E = ElemOf<T>::E;
   const unsigned ctas = cluster.num_blocks(), rank = cluster.block_rank();
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, warps = blockDim.x / 32;
   const long long r = blockIdx.x / ctas;
   const float weight = a.weight ? a.weight[r] : 1.0f;
+  const T* logits = row_address<T>(a.rows, r);
   T* grad = a.grad ? gradient_row<T>(a, r) : nullptr;
   Slice<T> s;
-  const bool skip = weight == 0.0f || !teacher(a, r, t);  // the same in all CTAs of the row
-  if (skip) {
-    a.rows.staged = 0;
-    s.open(row_address<T>(a.rows, r), a.rows.V, a.rows, rank, staged);
+  s.open(logits, a.rows, rank);
+  if (weight == 0.0f) {  // the same in all CTAs of the row
     if (rank == 0 && threadIdx.x == 0) {
       a.loss[r] = 0.0f;
-      if (a.lse) a.lse[r] = 0.0f;
+      if (a.lse) a.lse[r] = CUDART_INF_F;
     }
     if (grad) write_zeros(s, grad);
     return;
   }
-  s.open(row_address<T>(a.rows, r), a.rows.V, a.rows, rank, staged);
+  if (warp == warps - 1) teacher(a, r, t);
   const float c2 = kLog2e / a.tau;
-  ChunkMax<T, true> top;
-  s.stage([&](const uint4& c) { top.add(c); });
-  float m = top.value();
-  m = block_reduce(m, MaxNan(), t.red, &t.value);
-  float sum = 0.0f;
-  if (m != -CUDART_INF_F)
-    for (int c = s.wlo + (int)(threadIdx.x % 32); c < s.whi; c += 32) {
-      float f[E];
-      unpack<T>(s.chunk(c), f);
+  float top = -CUDART_INF_F;
+  float2 sums = make_float2(0.0f, 0.0f);
+  const float2 by = make_float2(c2, c2);
+  s.sweep([&](const uint4 (&v)[4], int) {
+    ChunkMax<T, true> batch;
+    batch.add(v);
+    const float x = batch.value();
+    if (!(x <= top)) {  // larger, or NaN: the sums are NaN from then on
+      const float less = exp2_32((top - x) * c2);
+      sums.x *= less;
+      sums.y *= less;
+      top = x;
+    }
+    if (top == -CUDART_INF_F) return;
+    const float2 off = make_float2(-top, -top);
 #pragma unroll
-      for (int e = 0; e < E; ++e) sum += exp2_32((f[e] - m) * c2);
+    for (int i = 0; i < 4; ++i) {
+      float z[E];
+      unpack<T>(v[i], z);
+#pragma unroll
+      for (int e = 0; e < E; e += 2) {
+        const float2 y = mul2(add2(make_float2(z[e], z[e + 1]), off), by);
+        sums = add2(sums, make_float2(exp2_32(y.x), exp2_32(y.y)));
+      }
     }
-  sum = block_reduce(sum, Add(), t.red, &t.value);
-  if (threadIdx.x == 0) {
-    cta_m = m;
-    cta_s = sum;
+  });
+  // lanes, warps, CTAs; a part without elements has maximum -inf and sum 0
+  const auto part = [&](float sum, float of, float m) { return of == -CUDART_INF_F ? 0.0f : sum * exp2_32((of - m) * c2); };
+  float m = warp_max_nan(top);
+  float sum = warp_add(part(sums.x + sums.y, top, m));
+  if (lane == 0) {
+    t.warp_m[warp] = m;
+    t.warp_s[warp] = sum;
   }
-  cluster.sync();
-  m = -CUDART_INF_F;
-  for (unsigned i = 0; i < ctas; ++i) m = max_nan(m, *cluster.map_shared_rank(&cta_m, i));
-  sum = 0.0f;
-  for (unsigned i = 0; i < ctas; ++i) {
-    const float mi = *cluster.map_shared_rank(&cta_m, i);
-    if (mi != -CUDART_INF_F) sum += *cluster.map_shared_rank(&cta_s, i) * exp2_32((mi - m) * c2);
-  }
-  const float log_sum = m == -CUDART_INF_F ? -CUDART_INF_F : logf(sum);
-  if (rank == 0) {
-    float loss = 0.0f;
-    for (int k = threadIdx.x; k < a.K; k += blockDim.x) {
-      const float p = t.p[k];
-      if (t.id[k] < 0 || p == 0.0f) continue;
-      const float z = to_float<T>(static_cast<const T*>(row_address<T>(a.rows, r))[t.id[k]]);
-      const float lq = z == -CUDART_INF_F ? z : (z - m) / a.tau - log_sum;
-      loss += p * (t.lp[k] - lq);
-    }
-    loss = block_reduce(loss, Add(), t.red, &t.value);
+  __syncthreads();
+  m = warp_max_nan(lane < warps ? t.warp_m[lane] : -CUDART_INF_F);
+  sum = warp_add(lane < warps ? part(t.warp_s[lane], t.warp_m[lane], m) : 0.0f);
+  if (ctas > 1) {
     if (threadIdx.x == 0) {
-      a.loss[r] = weight * a.tau * a.tau * loss;
-      if (a.lse) a.lse[r] = m == -CUDART_INF_F ? m : m / a.tau + log_sum;
+      t.m = m;
+      t.s = sum;
+    }
+    cluster.sync();
+    float of = -CUDART_INF_F, x = 0.0f;
+    if (lane < (int)ctas) {
+      of = *cluster.map_shared_rank(&t.m, lane);
+      x = *cluster.map_shared_rank(&t.s, lane);
+    }
+    m = warp_max_nan(of);
+    sum = warp_add(part(x, of, m));
+  }
+  const bool any = t.any;
+  const float log_sum = m == -CUDART_INF_F ? -CUDART_INF_F : logf(sum);
+  if (rank == 0 && warp == 0) {
+    float loss = 0.0f;
+    if (any)
+      for (int k = lane; k < a.K; k += 32) {
+        const float p = t.p[k];
+        if (t.id[k] < 0 || p == 0.0f) continue;
+        const float z = to_float<T>(logits[t.id[k]]);
+        const float lq = z == -CUDART_INF_F ? z : (z - m) / a.tau - log_sum;
+        loss += p * (t.lp[k] - lq);
+      }
+    loss = warp_add(loss);
+    if (lane == 0) {
+      a.loss[r] = any ? weight * a.tau * a.tau * loss : 0.0f;
+      if (a.lse) a.lse[r] = !any ? CUDART_INF_F : m == -CUDART_INF_F ? m : m / a.tau + log_sum;
     }
   }
   if (grad) {
     const float scale = m == -CUDART_INF_F ? 0.0f : 1.0f / sum, at = m == -CUDART_INF_F ? 0.0f : m;
-    write_gradient(s, grad, weight * a.tau, t, a.K,
-                   [=](float z) { return exp2_32((z - at) * c2) * scale; });
+    if (any)
+      write_gradient(s, grad, weight * a.tau, t, a.K, [=](float z) { return exp2_32((z - at) * c2) * scale; });
+    else
+      write_zeros(s, grad);
   }
-  cluster.sync();  // no CTA leaves while its shared memory is read
+  if (ctas > 1) cluster.sync();  // no CTA leaves while its shared memory is read
 }
 
 // the gradient from the row's logsumexp: a CTA per slice, nothing shared between them
 template <typename T>
-__global__ void __launch_bounds__(kRowThreads) k_distill_backward(DistillArgs a, int parts) {
+__global__ void __launch_bounds__(kRowThreads, 2) k_distill_backward(DistillArgs a, int parts) {
   __shared__ Targets t;
   const long long r = blockIdx.x / parts;
-  const float weight = a.weight ? a.weight[r] : 1.0f;
-  const float coef = weight == 0.0f ? 0.0f : weight * a.tau * a.up[r];
+  const float weight = a.weight ? a.weight[r] : 1.0f, lse = a.lse_in[r];
+  const float coef = weight == 0.0f || lse == CUDART_INF_F ? 0.0f : weight * a.tau * a.up[r];
   T* grad = gradient_row<T>(a, r);
   Slice<T> s;
-  s.open(row_address<T>(a.rows, r), a.rows.V, a.rows, (int)(blockIdx.x % parts), nullptr);
-  if (coef == 0.0f || !teacher(a, r, t)) {
+  s.open(row_address<T>(a.rows, r), a.rows, (int)(blockIdx.x % parts));
+  if (coef == 0.0f) {
     write_zeros(s, grad);
     return;
   }
-  const float inv = 1.0f / a.tau, lse = a.lse_in[r];
+  if (threadIdx.x / 32 == blockDim.x / 32 - 1) teacher(a, r, t);
+  const float inv = 1.0f / a.tau;
   write_gradient(s, grad, coef, t, a.K, [=](float z) {
     return z == -CUDART_INF_F ? 0.0f : exp2_32(fmaf(z, inv, -lse) * kLog2e);
   });
@@ -253,18 +307,12 @@ __global__ void __launch_bounds__(kRowThreads) k_distill_backward(DistillArgs a,
 
 template <typename T>
 epic_status launch_distill(DistillArgs& a, long long rows, cudaStream_t st) {
-  if (a.lse_in) {
-    const RowShape p = row_shape(rows, a.rows.V, sizeof(T));
-    a.rows.per = p.per;
-    a.rows.staged = 0;
-    if (rows > 0x7fffffffll / p.ctas) return EPIC_ERR_CAPACITY;
-    k_distill_backward<T><<<(unsigned)(rows * p.ctas), p.threads, 0, st>>>(a, p.ctas);
-    return cudaGetLastError() == cudaSuccess ? EPIC_OK : EPIC_ERR_CUDA;
-  }
   const RowShape p = row_shape(rows, a.rows.V, sizeof(T));
   a.rows.per = p.per;
-  a.rows.staged = p.staged;
-  return launch_rows((const void*)k_distill<T>, p, rows, &a, st);
+  if (!a.lse_in) return launch_rows((const void*)k_distill<T>, p, rows, &a, st);
+  if (rows > 0x7fffffffll / p.ctas) return EPIC_ERR_CAPACITY;
+  k_distill_backward<T><<<(unsigned)(rows * p.ctas), p.threads, 0, st>>>(a, p.ctas);
+  return cudaGetLastError() == cudaSuccess ? EPIC_OK : EPIC_ERR_CUDA;
 }
 
 epic_status distill(DistillArgs& a, const void* logits, int dtype, int B, int n, int V, int64_t sb, int64_t sn,
@@ -278,7 +326,7 @@ epic_status distill(DistillArgs& a, const void* logits, int dtype, int B, int n,
   if (rows == 0) return EPIC_OK;
   if (a.K > 0 && (!a.ids || !a.vals)) return EPIC_ERR_INVALID_ARG;
   if (a.grad && (uintptr_t)a.grad % (dtype == EPIC_F32 ? 4 : 2)) return EPIC_ERR_INVALID_ARG;
-  a.rows = {logits, sb, sn, nullptr, n, n, V, 0, 0};
+  a.rows = {logits, sb, sn, nullptr, n, n, V, 0};
   cudaStream_t st = (cudaStream_t)stream;
   switch (dtype) {
     case EPIC_F32: return launch_distill<float>(a, rows, st);

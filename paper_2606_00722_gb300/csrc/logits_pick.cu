@@ -22,11 +22,16 @@
 namespace epic {
 namespace {
 
-constexpr int kListMax = 1024;  // most keys collected for ranking
+constexpr int kListMax = 512;   // most keys collected for ranking
 constexpr int kMaxK = 256;      // most candidates of a position, and the longest top-k list
-constexpr int kBins = 1024;     // of a threshold's histogram
-constexpr float kBinSpan = 32.0f;        // in powers of two below the maximum; lighter tokens weigh nothing
-constexpr float kGrid = 1073741824.0f;   // 2^30: the weights' grid
+constexpr int kBins = 2048;     // of a threshold's histogram
+constexpr int kGroups = kBins / 32;
+constexpr int kParts = 32;      // masses kept of a warp's chunks
+constexpr int kTops = 2 * kMaxK + kRowWarps * kRowCluster;
+constexpr float kBinsPerUnit = kBins / 32;  // bins to a power of two; past 2^-32 of the maximum weights are 0
+constexpr float kGrid = 1073741824.0f;      // 2^30: the weights' grid
+constexpr float kMagic = 12582912.0f;       // 1.5 * 2^23: x + kMagic holds rint(x) in its low bits, |x| < 2^22
+constexpr uint32_t kMagicBits = 0x4b400000u;
 
 struct PickArgs {
   RowArgs rows;
@@ -43,10 +48,11 @@ struct PickArgs {
   float* prob;
 };
 
-// a bin's mass is low + 2^16 high: parts of 16 and 14 bits of each element's, which 65,536 elements of a slice cannot
-// make overflow 32 bits (larger slices go by radix selection)
+// a bin's mass is low + 2^15 high: parts of 15 and 16 bits of each element's mass, whose sums over a slice of at most
+// kSliceElems elements fit 32 bits
 struct Histogram {
   uint32_t low[kBins], high[kBins];
+  u64 group[kGroups];
 };
 
 struct TopList {  // a sampler's top-k list, in order
@@ -56,19 +62,24 @@ struct TopList {  // a sampler's top-k list, in order
   uint32_t kept[kMaxK];
 };
 
+struct Tops {  // largest lane maxima (value keys): of this CTA's warps, and of all of the row's
+  uint32_t mine[kTops], all[kTops];
+};
+
 struct PickShared {
   union {
     Histogram bins;
     u64 radix[2][256];
     TopList top;
+    Tops tops;
   };
   u64 list[kListMax];
-  u64 coarse[kBins / 32];
-  u64 warp_q[kRowWarps];
-  u64 cta_q;
+  u64 parts[kRowWarps][kParts];  // kept masses by runs of batches
+  u64 warp_q[kRowWarps];         // and by warp
   u64 found, before;
-  float warp_f[kRowWarps], warp_t[kRowWarps];
-  float cta_f, cta_t, cta_s;
+  uint32_t row_top, row_floor;  // value keys
+  float warp_sum[kRowWarps];
+  float sums[kRowCluster];  // in the first CTA
   int count;
 };
 
@@ -79,6 +90,12 @@ struct Weigher {
     if (m == CUDART_INF_F) return z == m ? 1.0f : 0.0f;
     return exp2_32(__fmul_rn(__fsub_rn(z, m), c));
   }
+  // exponents of two elements
+  __device__ __forceinline__ float2 exponents(float a, float b) const {
+    return mul2(add2(make_float2(a, b), make_float2(-m, -m)), make_float2(c, c));
+  }
+  // Whether all elements up to `top` weigh less than 2^-8, so that their masses are below 2^22.  False for NaN.
+  __device__ __forceinline__ bool light(float top) const { return __fmul_rn(__fsub_rn(top, m), c) < -8.01f; }
 };
 
 __device__ __forceinline__ uint32_t grid_mass(float w) { return __float2uint_rn(w * kGrid); }
@@ -101,6 +118,13 @@ __device__ __forceinline__ u64 warp_scan(u64 x) {
   return x;
 }
 
+// Which tokens are kept: keys from floor_key on, with a weight of at least min_p.
+struct Kept {
+  u64 floor_key;
+  float min_p;
+  __device__ __forceinline__ bool all() const { return floor_key == 0 && !(min_p > 0.0f); }
+};
+
 template <typename T>
 struct Row {
   Slice<T> s;
@@ -111,78 +135,86 @@ struct Row {
 
   __device__ Row(PickShared& shared) : cluster(cg::this_cluster()), sh(shared), parity(0) {}
 
-  // f(value, index) for the elements of this warp's chunks
+  // f(value, index) for the elements of this warp's chunks (and -inf past their end)
   template <typename F>
   __device__ __forceinline__ void each(F f) const {
-    for (int c = s.wlo + (int)(threadIdx.x % 32); c < s.whi; c += 32) {
-      float z[E];
-      unpack<T>(s.chunk(c), z);
-      const long long i0 = s.first(c);
+    s.sweep([&](const uint4 (&v)[4], int c) {
 #pragma unroll
-      for (int e = 0; e < E; ++e) f(z[e], i0 + e);
-    }
+      for (int i = 0; i < 4; ++i) {
+        float z[E];
+        unpack<T>(v[i], z);
+        const int i0 = s.first(c + 32 * i);
+#pragma unroll
+        for (int e = 0; e < E; ++e) f(z[e], i0 + e);
+      }
+    });
   }
 
-  // Stages the row.  Returns its maximum, NaN left out (-inf for a row without elements), and a floor that at least K
-  // of its elements reach: the lowest over the row's warps of the j-th largest of the lanes' maxima, j times the number
-  // of warps being at least K.  (-inf where that says nothing: K or fewer lanes have elements.)
-  __device__ float open_top(int K, float* floor) {
-    ChunkMax<T, false> top;
-    s.stage([&](const uint4& c) { top.add(c); });
-    float m = top.value();
-    const int warps = blockDim.x / 32, w = threadIdx.x / 32;
-    uint32_t key = value_key(m), jth = 0;
-    const int j = (K + warps * (int)cluster.num_blocks() - 1) / (warps * (int)cluster.num_blocks());
-    if (j <= 32)
-      for (int i = 0; i < j; ++i) {
-        jth = __reduce_max_sync(~0u, key);
-        if (__ffs(__ballot_sync(~0u, key == jth)) - 1 == (int)(threadIdx.x % 32)) key = 0;
-      }
-    for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, o));
-    if (threadIdx.x % 32 == 0) {
-      sh.warp_f[w] = m;
-      sh.warp_t[w] = jth ? key_value(jth) : -CUDART_INF_F;
+  // The row's maximum from the lanes' (NaN left out, -inf for a row without elements).  For K > 0 *floor is a value
+  // that at least K elements reach (or -inf): the K-th largest of the largest j lane maxima of every warp, where j gives
+  // twice K of them.  About 1.4 K elements of a row in random order reach it; the lowest of the warps' j-th, which needs
+  // no ranking, lets ten times K through at one lane maximum a warp.
+  __device__ float top_of(float lane_top, int K, float* floor) {
+    const int warps = blockDim.x / 32, w = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int all = warps * (int)cluster.num_blocks();
+    const int j = K > 0 ? min((2 * K + all - 1) / all, 32) : 1;
+    uint32_t key = value_key(lane_top);
+    for (int i = 0; i < j; ++i) {
+      const uint32_t x = __reduce_max_sync(~0u, key);
+      if (lane == 0) sh.tops.mine[w * j + i] = x;
+      if (__ffs(__ballot_sync(~0u, key == x)) - 1 == lane) key = 0;
     }
-    if (threadIdx.x == 0) sh.count = 0;
-    __syncthreads();
     if (threadIdx.x == 0) {
-      float t = sh.warp_t[0];
-      for (int i = 1; i < warps; ++i) {
-        m = fmaxf(m, sh.warp_f[i]);
-        t = fminf(t, sh.warp_t[i]);
-      }
-      sh.cta_f = m;
-      sh.cta_t = t;
+      sh.count = 0;
+      sh.row_floor = 0;
     }
     cluster.sync();
-    m = -CUDART_INF_F;
-    float t = CUDART_INF_F;
-    for (unsigned r = 0; r < cluster.num_blocks(); ++r) {
-      m = fmaxf(m, *cluster.map_shared_rank(&sh.cta_f, r));
-      t = fminf(t, *cluster.map_shared_rank(&sh.cta_t, r));
+    const int n = all * j, per = warps * j;
+    if (K == 0) {  // every warp looks at all warps of the row
+      uint32_t m = 0;
+      for (int i = lane; i < n; i += 32) m = max(m, *cluster.map_shared_rank(&sh.tops.mine[i % per], i / per));
+      m = __reduce_max_sync(~0u, m);
+      cluster.sync();  // the tops' memory is free
+      return key_value(m);
     }
-    *floor = t;
-    return m;
+    for (int i = threadIdx.x; i < n; i += blockDim.x)
+      sh.tops.all[i] = *cluster.map_shared_rank(&sh.tops.mine[i % per], i / per);
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += blockDim.x) {
+      const uint32_t x = sh.tops.all[i];
+      int above = 0;
+      for (int o = 0; o < n; ++o) above += sh.tops.all[o] > x || (sh.tops.all[o] == x && o < i);
+      if (above == 0) sh.row_top = x;
+      if (above == K - 1) sh.row_floor = x;
+    }
+    __syncthreads();
+    *floor = sh.row_floor ? key_value(sh.row_floor) : -CUDART_INF_F;
+    return key_value(sh.row_top);
   }
 
-  // keys of elements >= floor to the first CTA's list (past its end they are only counted)
-  __device__ void collect(float floor) {
+  __device__ float lane_maximum() const {
+    ChunkMax<T, false> top;
+    s.sweep([&](const uint4 (&v)[4], int) { top.add(v); });
+    return top.value();
+  }
+
+  // Keys of elements >= floor to the first CTA's list (past its end they are only counted).  A lane whose maximum
+  // reaches the floor has such elements; its chunks are looked at by the whole warp.
+  __device__ void collect(float floor, float lane_top) {
     int* count = cluster.map_shared_rank(&sh.count, 0);
     u64* list = cluster.map_shared_rank(sh.list, 0);
-    for (int c = s.wlo + (int)(threadIdx.x % 32); c < s.whi; c += 32) {
-      const uint4 v = s.chunk(c);
-      ChunkMax<T, false> top;
-      top.add(v);
-      if (!(top.value() >= floor)) continue;
-      float z[E];
-      unpack<T>(v, z);
-      const long long i0 = s.first(c);
+    const int lane = threadIdx.x % 32;
+    for (uint32_t who = __ballot_sync(~0u, lane_top >= floor && lane_top > -CUDART_INF_F); who; who &= who - 1) {
+      for (int c = s.wlo + __ffs(who) - 1 + 32 * lane; c < s.whi; c += 32 * 32) {
+        float z[E];
+        unpack<T>(s.chunk(c), z);
 #pragma unroll
-      for (int e = 0; e < E; ++e)
-        if (z[e] >= floor && z[e] > -CUDART_INF_F) {
-          const int at = atomicAdd(count, 1);
-          if (at < kListMax) list[at] = order_key(z[e], (int)(i0 + e));
-        }
+        for (int e = 0; e < E; ++e)
+          if (z[e] >= floor && z[e] > -CUDART_INF_F) {
+            const int at = atomicAdd(count, 1);
+            if (at < kListMax) list[at] = order_key(z[e], s.first(c) + e);
+          }
+      }
     }
   }
 
@@ -195,8 +227,8 @@ struct Row {
     cluster.sync();
     int* count = cluster.map_shared_rank(&sh.count, 0);
     u64* list = cluster.map_shared_rank(sh.list, 0);
-    each([&](float z, long long i) {
-      if (z > -CUDART_INF_F && order_key(z, (int)i) >= floor_key) list[atomicAdd(count, 1)] = order_key(z, (int)i);
+    each([&](float z, int i) {
+      if (in_range(z, i, floor_key)) list[atomicAdd(count, 1)] = order_key(z, i);
     });
     cluster.sync();
   }
@@ -213,83 +245,245 @@ struct Row {
     }
   }
 
-  // ---- thresholds
+  // ---- masses
 
-  __device__ __forceinline__ bool in_range(float z, long long i, u64 floor_key) const {
-    return z > -CUDART_INF_F && order_key(z, (int)i) >= floor_key;
+  __device__ __forceinline__ bool in_range(float z, int i, u64 floor_key) const {
+    return z > -CUDART_INF_F && order_key(z, i) >= floor_key;
   }
+
+  __device__ __forceinline__ uint32_t kept_mass(float z, int i, const Weigher& weigh, const Kept& kept) const {
+    if (!in_range(z, i, kept.floor_key)) return 0;
+    const float w = weigh(z);
+    return w >= kept.min_p ? grid_mass(w) : 0;
+  }
+
+  __device__ __forceinline__ u64 chunk_mass(const uint4& v, int c, const Weigher& weigh, const Kept& kept) const {
+    float z[E];
+    unpack<T>(v, z);
+    const int i0 = s.first(c);
+    u64 q = 0;
+#pragma unroll
+    for (int e = 0; e < E; ++e) q += kept_mass(z[e], i0 + e, weigh, kept);
+    return q;
+  }
+
+  // A lane's kept mass of a batch.  Where all tokens are kept and all weigh below 2^-8 the conversions are additions
+  // (the conversion instruction shares its pipe, a quarter of a warp an SM cycle, with the exponential) and 32 masses
+  // fit 32 bits.
+  __device__ __forceinline__ u64 batch_mass(const uint4 (&v)[4], int c, const Weigher& weigh, const Kept& kept) const {
+    if (kept.all()) {
+      ChunkMax<T, true> top;
+      top.add(v);
+      if (weigh.light(top.value())) {
+        uint32_t q = 0u - 4u * E * kMagicBits;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float z[E];
+          unpack<T>(v[i], z);
+#pragma unroll
+          for (int e = 0; e < E; e += 2) {
+            const float2 y = weigh.exponents(z[e], z[e + 1]);
+            const float2 x = fma2(make_float2(exp2_32(y.x), exp2_32(y.y)), make_float2(kGrid, kGrid),
+                                  make_float2(kMagic, kMagic));
+            q += __float_as_uint(x.x) + __float_as_uint(x.y);
+          }
+        }
+        return q;
+      }
+    }
+    u64 q = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) q += chunk_mass(v[i], c + 32 * i, weigh, kept);
+    return q;
+  }
+
+  // a part is 2^shift batches
+  __device__ __forceinline__ int part_shift() const {
+    int shift = 0;
+    while ((s.wper + kBatch - 1) / kBatch > kParts << shift) ++shift;
+    return shift;
+  }
+
+  // warp sums of a batch's masses (below 2^35 a lane) into its part
+  __device__ __forceinline__ void add_part(u64 q, int c, int shift, u64& total) {
+    const uint32_t low = __reduce_add_sync(~0u, (uint32_t)q & 0xffffffu);
+    const uint32_t high = __reduce_add_sync(~0u, (uint32_t)(q >> 24));
+    if (threadIdx.x % 32 == 0 && (low | high)) {
+      const u64 x = low + ((u64)high << 24);
+      sh.parts[threadIdx.x / 32][((c - s.wlo) / kBatch) >> shift] += x;
+      total += x;
+    }
+  }
+
+  __device__ void clear_parts() {
+    for (int i = threadIdx.x % 32; i < kParts; i += 32) sh.parts[threadIdx.x / 32][i] = 0;
+    __syncwarp();
+  }
+
+  // masses of the row's kept tokens, by part and by warp
+  __device__ void masses(const Weigher& weigh, const Kept& kept) {
+    const int shift = part_shift();
+    clear_parts();
+    u64 total = 0;
+    s.sweep([&](const uint4 (&v)[4], int c) { add_part(batch_mass(v, c, weigh, kept), c, shift, total); });
+    if (threadIdx.x % 32 == 0) sh.warp_q[threadIdx.x / 32] = total;
+  }
+
+  // After a cluster barrier: the row's kept mass, the CTA's own and that of the CTAs ahead of it.  Every warp for itself.
+  __device__ u64 all_mass(u64* mine, u64* ahead) const {
+    const int warps = blockDim.x / 32, all = warps * (int)cluster.num_blocks();
+    const int rank = (int)cluster.block_rank();
+    u64 total = 0, own = 0, before = 0;
+    for (int i = threadIdx.x % 32; i < all; i += 32) {
+      const int r = i / warps;
+      const u64 x = *cluster.map_shared_rank(&sh.warp_q[i - r * warps], r);
+      total += x;
+      if (r < rank) before += x;
+      if (r == rank) own += x;
+    }
+    *mine = warp_sum(own);
+    *ahead = warp_sum(before);
+    return warp_sum(total);
+  }
+
+  // ---- thresholds
 
   // The key of the element, among keys >= floor, at which the running total of the order passes the target: with kMass
   // totals are masses and the target floor(arg all / 2^24) - 1, else they are counts and it is arg (or the last).
-  // All ones for a row without elements.  One histogram over evenly spaced exponents finds the bin, whose few elements
-  // the first CTA ranks; rows of many equal values go by radix selection.
+  // All ones for a row without elements.  A histogram over evenly spaced exponents finds the bin; where it has more
+  // elements than a list, a second one cuts it again; the first CTA ranks the bin's elements.  Rows of many equal
+  // values go by radix selection.
+  // With min_p >= 0 the masses of the kept tokens (from the threshold on, of at least min_p) are left by part and by warp
+  // as masses() leaves them, a cluster barrier included.
   template <bool kMass>
-  __device__ u64 select(const Weigher& weigh, u64 floor_key, u64 arg) {
-    if ((long long)s.n * E > 65536) return radix_select<kMass>(weigh, floor_key, arg);
-    for (int i = threadIdx.x; i < kBins; i += blockDim.x) sh.bins.low[i] = sh.bins.high[i] = 0;
-    if (threadIdx.x == 0) sh.count = 0;
-    __syncthreads();
-    const float scale = weigh.c * (kBins / kBinSpan);
-    const auto bin_of = [&](float z) { return min(__float2uint_rz((weigh.m - z) * scale), (uint32_t)kBins - 1); };
-    each([&](float z, long long i) {
-      if (!in_range(z, i, floor_key)) return;
-      const uint32_t b = bin_of(z);
-      if (kMass) {
-        const uint32_t q = grid_mass(weigh(z));
-        if (q & 0xffffu) atomicAdd(&sh.bins.low[b], q & 0xffffu);
-        if (q >> 16) atomicAdd(&sh.bins.high[b], q >> 16);
-      } else {
-        atomicAdd(&sh.bins.low[b], 1u);
-      }
-    });
-    __syncthreads();
-    const int lane = threadIdx.x % 32, warps = blockDim.x / 32;
-    for (int g = threadIdx.x / 32; g < kBins / 32; g += warps) {
-      const u64 x = warp_sum(sh.bins.low[32 * g + lane] + ((u64)sh.bins.high[32 * g + lane] << 16));
-      if (lane == 0) sh.coarse[g] = x;
-    }
-    cluster.sync();
-    if (threadIdx.x < 32) {  // every CTA finds the bin for itself
-      static_assert(kBins / 32 == 32, "a lane for each group of bins");
-      u64 x = 0;
-      for (unsigned r = 0; r < cluster.num_blocks(); ++r) x += *cluster.map_shared_rank(&sh.coarse[lane], r);
-      u64 upto = warp_scan(x);
-      const u64 all = __shfl_sync(~0u, upto, 31);
-      const u64 t = kMass ? share24(arg, all) - 1 : min(arg, all - 1);
-      const int g = min(__popc(__ballot_sync(~0u, upto <= t)), 31);
-      const u64 ahead = __shfl_sync(~0u, upto - x, g);
-      x = 0;
-      for (unsigned r = 0; r < cluster.num_blocks(); ++r) {
-        const Histogram* h = cluster.map_shared_rank(&sh.bins, r);
-        x += h->low[32 * g + lane] + ((u64)h->high[32 * g + lane] << 16);
-      }
-      upto = ahead + warp_scan(x);
-      const int l = min(__popc(__ballot_sync(~0u, upto <= t)), 31);
-      const u64 before = __shfl_sync(~0u, upto - x, l);
-      if (lane == 0) {
-        sh.found = all ? (u64)(32 * g + l) : ~0ull;
-        sh.before = t - before;  // the target within the bin
-      }
-    }
-    __syncthreads();
-    if (sh.found == ~0ull) {
-      cluster.sync();
-      return ~0ull;
-    }
-    const uint32_t bin = (uint32_t)sh.found;
-    const u64 t = sh.before;
+  __device__ u64 select(const Weigher& weigh, u64 floor_key, u64 arg, float min_p) {
+    const int lane = threadIdx.x % 32, warps = blockDim.x / 32, warp = threadIdx.x / 32;
     int* count = cluster.map_shared_rank(&sh.count, 0);
     u64* list = cluster.map_shared_rank(sh.list, 0);
-    each([&](float z, long long i) {
-      if (bin_of(z) == bin && in_range(z, i, floor_key)) {
-        const int at = atomicAdd(count, 1);
-        if (at < kListMax) list[at] = order_key(z, (int)i);
+    const bool keep = min_p >= 0.0f;
+    const int shift = part_shift();
+    u64 t = 0;
+    uint32_t outer = 0;  // the bin of the first level
+    int n = kListMax + 1;
+    const bool fits = (long long)per_cta * E <= kSliceElems && weigh.m < CUDART_INF_F;
+    for (int level = 0; level < 2 && fits; ++level) {
+      // the cluster's CTAs have left the memory of the bins and the count behind: a barrier is above
+      for (int i = threadIdx.x; i < kBins; i += blockDim.x) sh.bins.low[i] = sh.bins.high[i] = 0;
+      if (threadIdx.x == 0) sh.count = 0;
+      __syncthreads();
+      // Bins go down the order, by exponent; in the second level those outside the first's bin are below 0 or kBins.
+      const auto bin_of = [&](float y) -> int {
+        const float x = fminf(y * -kBinsPerUnit, (float)(kBins - 1));
+        const int b = (int)(__float_as_uint(x + kMagic) - kMagicBits);
+        if (level == 0) return b;
+        if (b != (int)outer) return b < (int)outer ? -1 : kBins;
+        return (int)fminf((x - ((float)outer - 0.5f)) * kBins, (float)(kBins - 1));
+      };
+      const auto exponent = [&](float z) { return __fmul_rn(__fsub_rn(z, weigh.m), weigh.c); };
+      each([&](float z, int i) {
+        const float y = exponent(z);
+        if (kMass) {
+          const uint32_t q = grid_mass(exp2_32(y));
+          if (q == 0 || (floor_key && order_key(z, i) < floor_key)) return;
+          const int b = bin_of(y);
+          if (b < 0 || b >= kBins) return;
+          atomicAdd(&sh.bins.low[b], q & 0x7fffu);
+          if (q >> 15) atomicAdd(&sh.bins.high[b], q >> 15);
+        } else {
+          if (!in_range(z, i, floor_key)) return;
+          const int b = bin_of(y);
+          if (b >= 0 && b < kBins) atomicAdd(&sh.bins.low[b], 1u);
+        }
+      });
+      __syncthreads();
+      for (int g = warp; g < kGroups; g += warps) {
+        const u64 x = warp_sum(sh.bins.low[32 * g + lane] + ((u64)sh.bins.high[32 * g + lane] << 15));
+        if (lane == 0) sh.bins.group[g] = x;
       }
-    });
-    cluster.sync();
-    const int n = *count;
-    if (n > kListMax) return radix_select<kMass>(weigh, floor_key, arg);
-    if (cluster.block_rank() == 0)
+      cluster.sync();
+      if (warp == 0) {  // every CTA finds the bin for itself
+        static_assert(kGroups == 64, "two groups of bins a lane");
+        u64 x0 = 0, x1 = 0;
+        for (unsigned r = 0; r < cluster.num_blocks(); ++r) {
+          const Histogram* h = cluster.map_shared_rank(&sh.bins, r);
+          x0 += h->group[2 * lane];
+          x1 += h->group[2 * lane + 1];
+        }
+        u64 upto = warp_scan(x0 + x1);
+        const u64 all = __shfl_sync(~0u, upto, 31);
+        if (level == 0) t = kMass ? share24(arg, all) - 1 : min(arg, all - 1);
+        int g = min(__popc(__ballot_sync(~0u, upto <= t)), 31);
+        u64 ahead = __shfl_sync(~0u, upto - x0 - x1, g);
+        const u64 half = __shfl_sync(~0u, x0, g);
+        g *= 2;
+        if (ahead + half <= t) {
+          ahead += half;
+          ++g;
+        }
+        u64 x = 0;
+        for (unsigned r = 0; r < cluster.num_blocks(); ++r) {
+          const Histogram* h = cluster.map_shared_rank(&sh.bins, r);
+          x += h->low[32 * g + lane] + ((u64)h->high[32 * g + lane] << 15);
+        }
+        upto = ahead + warp_scan(x);
+        const int l = min(__popc(__ballot_sync(~0u, upto <= t)), 31);
+        const u64 before = __shfl_sync(~0u, upto - x, l);
+        if (lane == 0) {
+          sh.found = all ? (u64)(32 * g + l) : ~0ull;
+          sh.before = t - before;  // the target within the bin
+        }
+      }
+      __syncthreads();
+      if (sh.found == ~0ull) {
+        if (lane == 0) sh.warp_q[warp] = 0;
+        cluster.sync();
+        return ~0ull;
+      }
+      const int bin = (int)sh.found;
+      t = sh.before;
+      // the bin's elements to the list; the mass of what is kept for sure to the parts
+      u64 total = 0;
+      if (keep) clear_parts();
+      s.sweep([&](const uint4 (&v)[4], int c) {
+        u64 sum = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float z[E];
+          unpack<T>(v[i], z);
+          const int i0 = s.first(c + 32 * i);
+#pragma unroll
+          for (int e = 0; e < E; ++e) {
+            const float y = exponent(z[e]);
+            const int b = bin_of(y);
+            if (b > bin || !(z[e] > -CUDART_INF_F)) continue;
+            if (floor_key && order_key(z[e], i0 + e) < floor_key) continue;
+            if (b == bin) {
+              const int at = atomicAdd(count, 1);
+              if (at < kListMax) list[at] = order_key(z[e], i0 + e);
+            } else if (keep) {
+              const float w = exp2_32(y);
+              if (w >= min_p) sum += grid_mass(w);
+            }
+          }
+        }
+        if (keep) add_part(sum, c, shift, total);
+      });
+      if (keep && lane == 0) sh.warp_q[warp] = total;
+      cluster.sync();
+      n = *count;
+      if (n <= kListMax) break;
+      outer = (uint32_t)bin;
+      cluster.sync();  // all have seen the count
+    }
+    if (n > kListMax) {
+      const u64 key = radix_select<kMass>(weigh, floor_key, arg);
+      if (keep) {
+        masses(weigh, Kept{max(key, 1ull), min_p});
+        cluster.sync();
+      }
+      return key;
+    }
+    if (cluster.block_rank() == 0) {
       for (int i = threadIdx.x; i < n; i += blockDim.x) {
         const u64 key = sh.list[i];
         u64 ahead = 0;
@@ -298,10 +492,33 @@ struct Row {
         const u64 own = kMass ? grid_mass(weigh(order_value(key))) : 1u;
         if (ahead <= t && t < ahead + own) sh.found = key;
       }
+      __syncthreads();
+      if (keep)
+        for (int i = threadIdx.x; i < n; i += blockDim.x) {
+          const u64 key = sh.list[i];
+          const float w = weigh(order_value(key));
+          if (key < sh.found || !(w >= min_p)) continue;
+          // the element's CTA, warp and part: head is the same in all CTAs, the warps' shares are not
+          const int c = (order_index(key) + s.head) / E, r = c / per_cta, at = c - r * per_cta;
+          const int there = (slice_chunks(r) + warps - 1) / warps, w_at = at / there;
+          int sh_there = 0;
+          while ((there + kBatch - 1) / kBatch > kParts << sh_there) ++sh_there;
+          const u64 q = grid_mass(w);
+          atomicAdd(cluster.map_shared_rank(&sh.parts[w_at][((at - w_at * there) / kBatch) >> sh_there], r), q);
+          atomicAdd(cluster.map_shared_rank(&sh.warp_q[w_at], r), q);
+        }
+    }
     cluster.sync();
     const u64 key = *cluster.map_shared_rank(&sh.found, 0);
-    cluster.sync();
+    if (!keep) cluster.sync();  // found and the list may be written again
     return key;
+  }
+
+  int per_cta;
+  // chunks of CTA r's slice
+  __device__ int slice_chunks(int r) const {
+    const int total = s.V ? (s.head + s.V - 1) / E + 1 : 0;
+    return min(max(total - r * per_cta, 0), per_cta);
   }
 
   // The same by eight bits of the keys at a time.
@@ -317,8 +534,8 @@ struct Row {
       u64* hist = sh.radix[parity];
       for (int i = threadIdx.x; i < 256; i += blockDim.x) hist[i] = 0;
       __syncthreads();
-      each([&](float z, long long i) {
-        const u64 key = order_key(z, (int)i);
+      each([&](float z, int i) {
+        const u64 key = order_key(z, i);
         if (z > -CUDART_INF_F && key >= floor_key && (shift == 56 || (key ^ prefix) >> (shift + 8) == 0)) {
           const u64 add = kMass ? (u64)grid_mass(weigh(z)) : 1ull;
           if (add) atomicAdd(&hist[(key >> shift) & 255], add);
@@ -357,67 +574,23 @@ struct Row {
     return prefix;
   }
 
-  // ---- masses and draws
-
-  __device__ __forceinline__ uint32_t kept_mass(float z, long long i, const Weigher& weigh, u64 floor_key,
-                                                float min_p) const {
-    if (!in_range(z, i, floor_key)) return 0;
-    const float w = weigh(z);
-    return w >= min_p ? grid_mass(w) : 0;
-  }
-
-  __device__ __forceinline__ u64 chunk_mass(int c, const Weigher& weigh, u64 floor_key, float min_p) const {
-    float z[E];
-    unpack<T>(s.chunk(c), z);
-    u64 q = 0;
-    if (floor_key == 0 && !(min_p > 0.0f) && weigh.m != CUDART_INF_F) {
-      // every token is kept; NaN weighs 0 by the conversion
-#pragma unroll
-      for (int e = 0; e < E; ++e) q += grid_mass(exp2_32(__fmul_rn(__fsub_rn(z[e], weigh.m), weigh.c)));
-      return q;
-    }
-    const long long i0 = s.first(c);
-#pragma unroll
-    for (int e = 0; e < E; ++e) q += kept_mass(z[e], i0 + e, weigh, floor_key, min_p);
-    return q;
-  }
-
-  // Mass of the row's kept keys; *mine is the CTA's part, *ahead that of the CTAs before it, sh.warp_q the warps'.
-  __device__ u64 mass(const Weigher& weigh, u64 floor_key, float min_p, u64* mine, u64* ahead) {
-    u64 q = 0;
-    for (int c = s.wlo + (int)(threadIdx.x % 32); c < s.whi; c += 32) q += chunk_mass(c, weigh, floor_key, min_p);
-    q = warp_sum(q);
-    if (threadIdx.x % 32 == 0) sh.warp_q[threadIdx.x / 32] = q;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      q = 0;
-      for (int w = 0; w < (int)blockDim.x / 32; ++w) q += sh.warp_q[w];
-      sh.cta_q = q;
-    }
-    cluster.sync();
-    u64 all = 0;
-    *ahead = *mine = 0;
-    for (unsigned r = 0; r < cluster.num_blocks(); ++r) {
-      const u64 x = *cluster.map_shared_rank(&sh.cta_q, r);
-      if (r == cluster.block_rank()) {
-        *ahead = all;
-        *mine = x;
-      }
-      all += x;
-    }
-    return all;
-  }
+  // ---- draws
 
   // one warp: the token of the slice whose kept mass covers t (counted from the slice's start)
-  __device__ void draw(u64 t, const Weigher& weigh, u64 floor_key, float min_p, u64 all, int32_t* tok,
-                       float* prob) const {
+  __device__ void draw(u64 t, const Weigher& weigh, const Kept& kept, u64 all, int32_t* tok, float* prob) const {
     const int lane = threadIdx.x % 32, warps = blockDim.x / 32;
     int w = 0;
     while (w < warps - 1 && t >= sh.warp_q[w]) t -= sh.warp_q[w++];
-    for (int c0 = w * s.wper; c0 < s.n; c0 += 32) {
+    const u64 part = sh.parts[w][lane];
+    const u64 parts = warp_scan(part);
+    const int p = min(__popc(__ballot_sync(~0u, parts <= t)), kParts - 1);
+    t -= __shfl_sync(~0u, parts - part, p);
+    for (int c0 = w * s.wper + ((p << part_shift()) * kBatch); c0 < s.n; c0 += 32) {
       // lanes past the warp's last chunk look into the next one's: the answer is never there
       const int c = c0 + lane;
-      const u64 q = c < s.n ? chunk_mass(c, weigh, floor_key, min_p) : 0;
+      uint4 v = empty_chunk<T>();
+      if (c < s.n) v = s.chunk(c);
+      const u64 q = chunk_mass(v, c, weigh, kept);
       const u64 upto = warp_scan(q);
       const u64 total = __shfl_sync(~0u, upto, 31);
       if (t >= total) {
@@ -427,16 +600,20 @@ struct Row {
       if (t >= upto - q && t < upto) {
         t -= upto - q;
         float z[E];
-        unpack<T>(s.chunk(c), z);
+        unpack<T>(v, z);
+        float hit = 0.0f;
+        int at = -1;
+#pragma unroll
         for (int e = 0; e < E; ++e) {
-          const uint32_t x = kept_mass(z[e], s.first(c) + e, weigh, floor_key, min_p);
-          if (t < x) {
-            *tok = (int32_t)(s.first(c) + e);
-            *prob = weigh(z[e]) * kGrid / (float)all;
-            break;
+          const uint32_t x = kept_mass(z[e], s.first(c) + e, weigh, kept);
+          if (at < 0 && t < x) {
+            at = e;
+            hit = z[e];
           }
-          t -= x;
+          t -= at < 0 ? x : 0;
         }
+        *tok = s.first(c) + at;
+        *prob = weigh(hit) * kGrid / (float)all;
       }
       break;
     }
@@ -490,82 +667,89 @@ struct Row {
   }
 };
 
-// sum of the row's weights over a CTA's warps: `total` is the sum in order of warps, in every thread of the CTA
-__device__ __forceinline__ float cta_sum(float x, PickShared& sh) {
-  for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(~0u, x, o);
-  if (threadIdx.x % 32 == 0) sh.warp_t[threadIdx.x / 32] = x;
-  __syncthreads();
-  x = 0.0f;
-  for (int w = 0; w < (int)blockDim.x / 32; ++w) x += sh.warp_t[w];
-  return x;
-}
-
 template <typename T>
-__global__ void __launch_bounds__(kRowThreads) k_propose(PickArgs a) {
-  extern __shared__ uint4 staged[];
+__global__ void __launch_bounds__(kRowThreads, 2) k_propose(PickArgs a) {
   __shared__ PickShared sh;
   Row<T> row(sh);
   constexpr int E = ElemOf<T>::E;
   const unsigned ctas = row.cluster.num_blocks(), rank = row.cluster.block_rank();
   const long long r = blockIdx.x / ctas;
   const float T_ = a.temperature ? a.temperature[r / a.rows.k] : 1.0f;
-  const void* addr = T_ >= 0.0f ? row_address<T>(a.rows, r) : nullptr;
-  row.s.open(addr, a.rows.V, a.rows, rank, staged);
+  row.s.open(T_ >= 0.0f ? row_address<T>(a.rows, r) : nullptr, a.rows, rank);
   Weigher weigh;
-  float floor;
-  weigh.m = row.open_top(a.K, &floor);
   weigh.c = fminf(__fdiv_rn(kLog2e, T_), CUDART_MAX_NORMAL_F);
-  row.collect(floor);
-  // The sum of the weights, each with its exponent in one fused step: what the rounding of m c adds is common to all
-  // and leaves with the division.  NaN and infinities make that sum NaN; it is then taken again with care.
-  const float mc = weigh.m * weigh.c;
-  float sum = 0.0f;
-  for (int c = row.s.wlo + (int)(threadIdx.x % 32); c < row.s.whi; c += 32) {
-    float z[E];
-    unpack<T>(row.s.chunk(c), z);
-#pragma unroll
-    for (int e = 0; e < E; ++e) sum += exp2_32(fmaf(z[e], weigh.c, -mc));
-  }
-  sum = cta_sum(sum, sh);
-  if (threadIdx.x == 0) sh.cta_s = sum;
-  row.cluster.sync();
-  sum = 0.0f;
-  for (unsigned i = 0; i < ctas; ++i) sum += *row.cluster.map_shared_rank(&sh.cta_s, i);
-  const bool fused = sum == sum;  // the same in all CTAs
-  if (!fused) {
-    sum = 0.0f;
-    row.each([&](float z, long long) {
-      const float w = weigh(z);
-      sum += w > 0.0f ? w : 0.0f;
-    });
-    row.cluster.sync();
-    sum = cta_sum(sum, sh);
-    if (threadIdx.x == 0) sh.cta_s = sum;
-    row.cluster.sync();
-    sum = 0.0f;
-    for (unsigned i = 0; i < ctas; ++i) sum += *row.cluster.map_shared_rank(&sh.cta_s, i);
-  }
-  row.settle(a.K);
-  if (rank == 0) {
-    int32_t* cand = a.cand + r * a.K;
-    float* conf = a.conf + r * a.K;
-    for (int i = sh.count + threadIdx.x; i < a.K; i += blockDim.x) {
-      cand[i] = -1;
-      conf[i] = 0.0f;
+  // one pass: each lane's maximum so far and the sum of its weights relative to it
+  float top = -CUDART_INF_F;
+  float2 sums = make_float2(0.0f, 0.0f);
+  row.s.sweep([&](const uint4 (&v)[4], int) {
+    ChunkMax<T, false> batch;
+    batch.add(v);
+    const float x = batch.value();
+    if (x > top) {
+      const float by = exp2_32((top - x) * weigh.c);
+      sums.x *= by;
+      sums.y *= by;
+      top = x;
     }
-    row.ranked([&](int at, u64 key) {
-      if (at >= a.K) return;
-      const float z = order_value(key);
-      cand[at] = order_index(key);
-      conf[at] = T_ == 0.0f ? (at == 0 ? 1.0f : 0.0f) : (fused ? exp2_32(fmaf(z, weigh.c, -mc)) : weigh(z)) / sum;
-    });
+    if (top == -CUDART_INF_F) return;
+    const Weigher relative{top, weigh.c};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float z[E];
+      unpack<T>(v[i], z);
+#pragma unroll
+      for (int e = 0; e < E; e += 2) {
+        const float2 y = relative.exponents(z[e], z[e + 1]);
+        sums = add2(sums, make_float2(exp2_32(y.x), exp2_32(y.y)));
+      }
+    }
+  });
+  float floor;
+  weigh.m = row.top_of(top, a.K, &floor);
+  row.collect(floor, top);
+  float sum = sums.x + sums.y;
+  if (sum != sum || weigh.m == CUDART_INF_F) {  // NaN or +inf among this lane's elements, or +inf in the row
+    sum = 0.0f;
+    for (int c = row.s.wlo + (int)(threadIdx.x % 32); c < row.s.whi; c += 32) {
+      float z[E];
+      unpack<T>(row.s.chunk(c), z);
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const float w = weigh(z[e]);
+        sum += w > 0.0f ? w : 0.0f;
+      }
+    }
+  } else {
+    sum = top == -CUDART_INF_F ? 0.0f : sum * exp2_32((top - weigh.m) * weigh.c);
   }
-  row.cluster.sync();  // no CTA leaves while its shared memory is read
+  for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
+  if (threadIdx.x % 32 == 0) sh.warp_sum[threadIdx.x / 32] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int w = 1; w < (int)blockDim.x / 32; ++w) sum += sh.warp_sum[w];
+    *row.cluster.map_shared_rank(&sh.sums[rank], 0) = sum;
+  }
+  row.cluster.sync();
+  row.settle(a.K);
+  if (rank != 0) return;
+  sum = 0.0f;
+  for (unsigned i = 0; i < ctas; ++i) sum += sh.sums[i];
+  int32_t* cand = a.cand + r * a.K;
+  float* conf = a.conf + r * a.K;
+  for (int i = sh.count + threadIdx.x; i < a.K; i += blockDim.x) {
+    cand[i] = -1;
+    conf[i] = 0.0f;
+  }
+  row.ranked([&](int at, u64 key) {
+    if (at >= a.K) return;
+    cand[at] = order_index(key);
+    conf[at] = T_ == 0.0f ? (at == 0 ? 1.0f : 0.0f) : weigh(order_value(key)) / sum;
+  });
+  row.cluster.sync();  // the others have looked at the count
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kRowThreads) k_sample(PickArgs a) {
-  extern __shared__ uint4 staged[];
+__global__ void __launch_bounds__(kRowThreads, 2) k_sample(PickArgs a) {
   __shared__ PickShared sh;
   Row<T> row(sh);
   const unsigned ctas = row.cluster.num_blocks(), rank = row.cluster.block_rank();
@@ -580,24 +764,33 @@ __global__ void __launch_bounds__(kRowThreads) k_sample(PickArgs a) {
   if (T_ == 0.0f || p24 == 0 || min_p > 1.0f) top_k = 1;
   if (top_k <= 0 || top_k > a.rows.V) top_k = a.rows.V;
   const bool by_list = top_k <= kMaxK;
-  row.s.open(good ? row_address<T>(a.rows, r) : nullptr, a.rows.V, a.rows, rank, staged);
+  row.per_cta = a.rows.per;
+  row.s.open(good ? row_address<T>(a.rows, r) : nullptr, a.rows, rank);
+  const float lane_top = row.lane_maximum();
   Weigher weigh;
   float floor;
-  weigh.m = row.open_top(by_list ? top_k : 0, &floor);
+  weigh.m = row.top_of(lane_top, by_list ? top_k : 0, &floor);
   weigh.c = fminf(__fdiv_rn(kLog2e, T_), CUDART_MAX_NORMAL_F);
   if (by_list) {
-    row.collect(floor);
+    row.collect(floor, lane_top);
     row.cluster.sync();
     row.settle(top_k);
-    if (rank == 0)
-      row.draw_from_list(weigh, top_k, p24, min_p, a.u + r * a.S, a.S, a.tok + r * a.S, a.prob + r * a.S);
-    row.cluster.sync();
+    if (rank != 0) return;
+    row.draw_from_list(weigh, top_k, p24, min_p, a.u + r * a.S, a.S, a.tok + r * a.S, a.prob + r * a.S);
+    row.cluster.sync();  // the others have looked at the count
     return;
   }
-  u64 floor_key = 0, mine, ahead;
-  if (top_k < a.rows.V) floor_key = row.template select<false>(weigh, 0, top_k - 1);
-  if (p24 < (1u << 24)) floor_key = row.template select<true>(weigh, floor_key, p24);
-  const u64 all = row.mass(weigh, floor_key, min_p, &mine, &ahead);
+  const bool by_mass = p24 < (1u << 24);
+  Kept kept{0, fmaxf(min_p, 0.0f)};
+  if (top_k < a.rows.V) kept.floor_key = row.template select<false>(weigh, 0, top_k - 1, by_mass ? -1.0f : kept.min_p);
+  if (by_mass) kept.floor_key = row.template select<true>(weigh, kept.floor_key, p24, kept.min_p);
+  if (top_k == a.rows.V && !by_mass) {
+    row.masses(weigh, kept);
+    row.cluster.sync();
+  }
+  u64 mine, ahead;
+  const u64 all = row.all_mass(&mine, &ahead);
+  __syncwarp();
   for (int i = threadIdx.x / 32; i < a.S; i += blockDim.x / 32) {
     const long long o = r * a.S + i;
     const float u = a.u[o];
@@ -609,16 +802,15 @@ __global__ void __launch_bounds__(kRowThreads) k_sample(PickArgs a) {
       continue;
     }
     const u64 t = min(share24((u64)(u * 16777216.0f), all), all - 1);
-    if (t >= ahead && t < ahead + mine) row.draw(t - ahead, weigh, floor_key, min_p, all, &a.tok[o], &a.prob[o]);
+    if (t >= ahead && t < ahead + mine) row.draw(t - ahead, weigh, kept, all, &a.tok[o], &a.prob[o]);
   }
-  row.cluster.sync();
+  row.cluster.sync();  // no CTA leaves while its masses are read
 }
 
 template <typename T>
 epic_status launch(PickArgs& a, long long rows, bool sample, cudaStream_t st) {
   const RowShape p = row_shape(rows, a.rows.V, sizeof(T));
   a.rows.per = p.per;
-  a.rows.staged = p.staged;
   return launch_rows(sample ? (const void*)k_sample<T> : (const void*)k_propose<T>, p, rows, &a, st);
 }
 
@@ -648,7 +840,7 @@ epic_status epic_propose_topk(const void* d_logits, int32_t dtype, int32_t B, in
   if (rows == 0 || K == 0) return EPIC_OK;
   if (!d_cand || !d_conf) return EPIC_ERR_INVALID_ARG;
   PickArgs a = {};
-  a.rows = {d_logits, stride_b, stride_n, d_pos, n, k, V, 0, 0};
+  a.rows = {d_logits, stride_b, stride_n, d_pos, n, k, V, 0};
   a.temperature = d_temperature;
   a.K = K;
   a.cand = d_cand;
@@ -668,7 +860,7 @@ epic_status epic_sample_tokens(const void* d_logits, int32_t dtype, int32_t B, i
   if (rows == 0 || S == 0) return EPIC_OK;
   if (!d_u || !d_tok || !d_prob) return EPIC_ERR_INVALID_ARG;
   PickArgs a = {};
-  a.rows = {d_logits, stride_b, stride_n, d_pos, n, k, V, 0, 0};
+  a.rows = {d_logits, stride_b, stride_n, d_pos, n, k, V, 0};
   a.temperature = d_temperature;
   a.top_k = d_top_k;
   a.top_p = d_top_p;
