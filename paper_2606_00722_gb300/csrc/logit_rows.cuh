@@ -3,16 +3,15 @@
 //
 // A row of V logits belongs to a cluster of CTAs (one CTA where there are rows
 // enough).  It is cut into chunks of 16 bytes from the aligned address at or
-// below its first element; a CTA owns a run of chunks (its slice), a warp of it
-// a run of those, and reads 128 of them at a time, four a lane.  So sums by warp
-// and by batch are sums in index order, and a lane meets the same chunks in
-// every pass.  Nothing is staged: the first pass comes from memory, later ones
-// from the L2 cache, which holds the rows in flight (two CTAs of 512 threads an
-// SM are 304 rows, 77 MB at 126,000 tokens of 16 bits).  Slices staged in shared
-// memory were slower: an SM then holds three of 63 KB, each for the 10 us of
-// two cluster barriers and its passes, where 4 us would keep memory busy (the
-// 32 best of 1,024 x 126,000: 111 us staged in clusters of four, 99 us from L2
-// with a CTA a row, everything else alike).
+// below its first element; a CTA owns a run of chunks (its slice), which its
+// warps take in turn by batches of 128, four a lane.  So sums by batch are sums in
+// index order, and a lane meets the same chunks in every pass.  Nothing is
+// staged: the first pass comes from memory, later ones from the L2 cache, which
+// holds the rows in flight (three CTAs of 512 threads an SM are 456 rows, 115 MB
+// at 126,000 tokens of 16 bits).  Slices staged in shared memory were slower: an
+// SM then holds three of 63 KB, each for the 10 us of two cluster barriers and its
+// passes, where 4 us would keep memory busy (the 32 best of 1,024 x 126,000: 111
+// us staged in clusters of four, 99 us from L2 with a CTA a row, all else alike).
 //
 // The order of a row: value descending, ties by index ascending, as one 64-bit
 // key (larger comes first).  NaN and -inf are not in the order.
@@ -115,7 +114,7 @@ __device__ __forceinline__ uint4 pack(const float (&f)[ElemOf<T>::E]) {
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-constexpr int kBatch = 128;  // chunks that a warp reads at a time
+constexpr int kBatch = 128;  // chunks that a warp takes at a time, four a lane
 
 template <typename T>
 __device__ __forceinline__ uint4 empty_chunk() {  // all -inf
@@ -131,24 +130,18 @@ struct Slice {
   int head;           // elements between row16 and the row
   int c0, n;          // first chunk and number of chunks
   int V;
-  int wper;      // chunks of a warp: warp w has those from w * wper on
-  int wlo, whi;  // this warp's
   int flo, fhi;  // the chunks whose 16 bytes are all of this row
+  const uint4* ends;  // in shared memory: what the others, the row's first and last, have of it, else -inf
 
   // index of a chunk's first element (negative in a row's first chunk)
   __device__ __forceinline__ int first(int c) const { return (c0 + c) * E - head; }
 
   __device__ __forceinline__ const char* address(int c) const { return row16 + (size_t)(c0 + c) * 16; }
 
-  // a chunk of the slice; -inf for what is outside the row
-  __device__ uint4 chunk(int c) const {
+  // chunk c of the slice, of -inf past its end
+  __device__ __forceinline__ uint4 chunk(int c) const {
     if (c >= flo && c < fhi) return __ldg(reinterpret_cast<const uint4*>(address(c)));
-    const T* p = reinterpret_cast<const T*>(address(c));
-    const int i0 = first(c);
-    float f[E];
-#pragma unroll
-    for (int e = 0; e < E; ++e) f[e] = i0 + e >= 0 && i0 + e < V ? to_float<T>(p[e]) : -CUDART_INF_F;
-    return pack<T>(f);
+    return c >= n ? empty_chunk<T>() : ends[c < flo ? 0 : 1];
   }
 
   // the value of an element of the row
@@ -159,7 +152,7 @@ struct Slice {
   __device__ __forceinline__ int hi() const { return min(max(first(n), 0), V); }
 
   // the slice of the row at `addr` (NULL: a row of no elements) for CTA `rank` of the cluster
-  __device__ void open(const void* addr, const RowArgs& a, int rank) {
+  __device__ void open(const void* addr, const RowArgs& a, int rank, uint4 (&shared)[2]) {
     V = addr ? a.V : 0;
     const uintptr_t p = reinterpret_cast<uintptr_t>(addr);
     row16 = reinterpret_cast<const char*>(p & ~(uintptr_t)15);
@@ -167,31 +160,57 @@ struct Slice {
     const int total = V ? (head + V - 1) / E + 1 : 0;
     c0 = rank * a.per;
     n = min(max(total - c0, 0), a.per);
-    const int warps = blockDim.x / 32, w = threadIdx.x / 32;
-    wper = (n + warps - 1) / warps;
-    wlo = min(w * wper, n);
-    whi = min(wlo + wper, n);
     // the row's first and last chunk may have elements of other rows
     flo = c0 == 0 && head > 0 ? 1 : 0;
-    fhi = c0 + n == total && (head + V) % E != 0 ? n - 1 : n;
+    fhi = max(c0 + n == total && (head + V) % E != 0 ? n - 1 : n, flo);
+    ends = shared;
+    if (threadIdx.x < 2 && n > 0) {
+      const int c = threadIdx.x == 0 ? 0 : n - 1, i0 = first(c);
+      const T* p = reinterpret_cast<const T*>(address(c));
+      float f[E];
+#pragma unroll
+      for (int e = 0; e < E; ++e) f[e] = i0 + e >= 0 && i0 + e < V ? to_float<T>(p[e]) : -CUDART_INF_F;
+      shared[threadIdx.x] = pack<T>(f);
+    }
+    __syncthreads();
   }
 
-  // f(v, c) for this warp's batches: v are this lane's chunks c, c + 32, c + 64 and c + 96, of -inf past the warp's end
+  __device__ __forceinline__ int batches() const { return (n + kBatch - 1) / kBatch; }
+
+  // f(v, c) for this warp's batches: v are this lane's chunks c, c + 32, c + 64 and c + 96, of -inf past the slice's end
   template <typename F>
   __device__ __forceinline__ void sweep(F f) const {
-    for (int base = wlo; base < whi; base += kBatch) {
-      const int c = base + (int)(threadIdx.x % 32);
+    const int lane = threadIdx.x % 32;
+    for (int base = (int)(threadIdx.x / 32) * kBatch; base < n; base += (int)blockDim.x * 4) {
       uint4 v[4];
-      if (base >= flo && base + kBatch <= min(fhi, whi)) {
+      const int c = base + lane;
+      if (base >= flo && base + kBatch <= fhi) {
         const uint4* p = reinterpret_cast<const uint4*>(address(c));
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = __ldg(p + 32 * i);
       } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = c + 32 * i < whi ? chunk(c + 32 * i) : empty_chunk<T>();
+        for (int i = 0; i < 4; ++i) v[i] = chunk(c + 32 * i);
       }
       f(v, c);
     }
+  }
+};
+
+// The CTAs of a row.  A single one needs no cluster barrier (several times a block's in time).
+struct RowGroup {
+  unsigned n, rank;
+  __device__ RowGroup() : n(cg::this_cluster().num_blocks()), rank(cg::this_cluster().block_rank()) {}
+  __device__ __forceinline__ void sync() const {
+    if (n == 1)
+      __syncthreads();
+    else
+      cg::this_cluster().sync();
+  }
+  // CTA r's copy of a shared variable
+  template <typename P>
+  __device__ __forceinline__ P* at(P* p, unsigned r) const {
+    return n == 1 ? p : cg::this_cluster().map_shared_rank(p, r);
   }
 };
 

@@ -39,6 +39,7 @@ struct Targets {
   float p[kMaxTargets];
   float lp[kMaxTargets];
   int id[kMaxTargets];  // -1: does not count
+  uint4 ends[2];
   int any;
   float warp_m[kRowWarps], warp_s[kRowWarps];
   float m, s;  // of the CTA
@@ -124,7 +125,7 @@ __device__ void write_row(const Slice<T>& s, T* grad, G g) {
     s.sweep([&](const uint4 (&v)[4], int c) {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        if (c + 32 * i < s.whi) put(v[i], s.first(c + 32 * i));
+        if (c + 32 * i < s.n) put(v[i], s.first(c + 32 * i));
     });
     return;
   }
@@ -194,7 +195,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_distill(DistillArgs a) {
   const T* logits = row_address<T>(a.rows, r);
   T* grad = a.grad ? gradient_row<T>(a, r) : nullptr;
   Slice<T> s;
-  s.open(logits, a.rows, rank);
+  s.open(logits, a.rows, rank, t.ends);
   if (weight == 0.0f) {  // the same in all CTAs of the row
     if (rank == 0 && threadIdx.x == 0) {
       a.loss[r] = 0.0f;
@@ -212,11 +213,11 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_distill(DistillArgs a) {
     ChunkMax<T, true> batch;
     batch.add(v);
     const float x = batch.value();
-    if (!(x <= top)) {  // larger, or NaN: the sums are NaN from then on
-      const float less = exp2_32((top - x) * c2);
+    if (!(x <= top)) {  // larger, or NaN now or before: maximum and sums stay NaN from then on
+      const float now = max_nan(top, x), less = exp2_32((top - now) * c2);
       sums.x *= less;
       sums.y *= less;
-      top = x;
+      top = now;
     }
     if (top == -CUDART_INF_F) return;
     const float2 off = make_float2(-top, -top);
@@ -293,7 +294,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_distill_backward(DistillArgs
   const float coef = weight == 0.0f || lse == CUDART_INF_F ? 0.0f : weight * a.tau * a.up[r];
   T* grad = gradient_row<T>(a, r);
   Slice<T> s;
-  s.open(row_address<T>(a.rows, r), a.rows, (int)(blockIdx.x % parts));
+  s.open(row_address<T>(a.rows, r), a.rows, (int)(blockIdx.x % parts), t.ends);
   if (coef == 0.0f) {
     write_zeros(s, grad);
     return;

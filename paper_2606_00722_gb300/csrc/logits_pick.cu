@@ -16,22 +16,27 @@
 // masses; the draw is the first kept token in index order whose mass up to and
 // with it passes u times the kept mass.
 #include "../../include/epic.h"
+#include <limits.h>
+
 #include "logit_launch.h"
 #include "logit_rows.cuh"
 
 namespace epic {
 namespace {
 
-constexpr int kListMax = 512;   // most keys collected for ranking
+constexpr int kListMax = 2048;  // most keys collected for ranking
 constexpr int kMaxK = 256;      // most candidates of a position, and the longest top-k list
 constexpr int kBins = 2048;     // of a threshold's histogram
 constexpr int kGroups = kBins / 32;
-constexpr int kParts = 32;      // masses kept of a warp's chunks
+constexpr int kParts = 512;     // masses kept of a slice's batches
 constexpr int kTops = 2 * kMaxK + kRowWarps * kRowCluster;
 constexpr float kBinsPerUnit = kBins / 32;  // bins to a power of two; past 2^-32 of the maximum weights are 0
 constexpr float kGrid = 1073741824.0f;      // 2^30: the weights' grid
-constexpr float kMagic = 12582912.0f;       // 1.5 * 2^23: x + kMagic holds rint(x) in its low bits, |x| < 2^22
-constexpr uint32_t kMagicBits = 0x4b400000u;
+// Rounding to whole numbers by addition: x + kOnes holds rint(x) in its low bits (|x| < 2^22), x + kHigh rint(x / 2^15)
+// (|x| < 2^37).
+constexpr float kOnes = 12582912.0f;       // 1.5 * 2^23
+constexpr float kHigh = 412316860416.0f;   // 1.5 * 2^38
+constexpr uint32_t kOnesBits = 0x4b400000u, kHighBits = 0x52c00000u;
 
 struct PickArgs {
   RowArgs rows;
@@ -48,11 +53,12 @@ struct PickArgs {
   float* prob;
 };
 
-// a bin's mass is low + 2^15 high: parts of 15 and 16 bits of each element's mass, whose sums over a slice of at most
-// kSliceElems elements fit 32 bits
+// A bin's mass is low + 2^15 high, as an element's is: its high part is at most 2^15, its low one within 2^14 of 0, so
+// the sums over a slice of at most kSliceElems elements fit 32 bits (low a signed one).
 struct Histogram {
   uint32_t low[kBins], high[kBins];
   u64 group[kGroups];
+  __device__ __forceinline__ u64 mass(int i) const { return ((u64)high[i] << 15) + (u64)(long long)(int)low[i]; }
 };
 
 struct TopList {  // a sampler's top-k list, in order
@@ -71,15 +77,17 @@ struct PickShared {
     Histogram bins;
     u64 radix[2][256];
     TopList top;
-    Tops tops;
   };
+  Tops tops;
   u64 list[kListMax];
-  u64 parts[kRowWarps][kParts];  // kept masses by runs of batches
-  u64 warp_q[kRowWarps];         // and by warp
+  u64 parts[kParts];  // kept masses by runs of batches
+  u64 cta_q;          // and of the CTA
+  uint4 ends[2];
   u64 found, before;
-  uint32_t row_top, row_floor;  // value keys
-  float warp_sum[kRowWarps];
-  float sums[kRowCluster];  // in the first CTA
+  float bin_low, bin_high;
+  int last;
+  uint32_t row_top, row_floor;             // value keys
+  float sums[kRowWarps * kRowCluster];     // of warps, in the first CTA
   int count;
 };
 
@@ -90,15 +98,30 @@ struct Weigher {
     if (m == CUDART_INF_F) return z == m ? 1.0f : 0.0f;
     return exp2_32(__fmul_rn(__fsub_rn(z, m), c));
   }
-  // exponents of two elements
+  __device__ __forceinline__ float exponent(float z) const { return __fmul_rn(__fsub_rn(z, m), c); }
   __device__ __forceinline__ float2 exponents(float a, float b) const {
     return mul2(add2(make_float2(a, b), make_float2(-m, -m)), make_float2(c, c));
   }
-  // Whether all elements up to `top` weigh less than 2^-8, so that their masses are below 2^22.  False for NaN.
-  __device__ __forceinline__ bool light(float top) const { return __fmul_rn(__fsub_rn(top, m), c) < -8.01f; }
 };
 
 __device__ __forceinline__ uint32_t grid_mass(float w) { return __float2uint_rn(w * kGrid); }
+
+// The masses of two weights in parts, grid_mass = 2^15 high + low, high and low as bits over kHighBits and kOnesBits.
+// Three additions for two elements: the conversion instruction does a quarter of a warp a cycle on the pipe that the
+// exponentials need.  Not for NaN.
+struct Parts2 {
+  uint32_t high[2], low[2];
+  __device__ __forceinline__ explicit Parts2(float2 w) {
+    const float2 grid = make_float2(kGrid, kGrid);
+    const float2 h = fma2(w, grid, make_float2(kHigh, kHigh));
+    const float2 rest = add2(make_float2(kHigh + kOnes, kHigh + kOnes), make_float2(-h.x, -h.y));
+    const float2 l = fma2(w, grid, rest);
+    high[0] = __float_as_uint(h.x);
+    high[1] = __float_as_uint(h.y);
+    low[0] = __float_as_uint(l.x);
+    low[1] = __float_as_uint(l.y);
+  }
+};
 
 // floor(a q / 2^24) for a <= 2^24, without passing 64 bits
 __device__ __forceinline__ u64 share24(u64 a, u64 q) { return a * (q >> 24) + ((a * (q & 0xffffffu)) >> 24); }
@@ -118,22 +141,36 @@ __device__ __forceinline__ u64 warp_scan(u64 x) {
   return x;
 }
 
-// Which tokens are kept: keys from floor_key on, with a weight of at least min_p.
+// A place in a row's order; elements at it or ahead of it are `in`.
+struct Floor {
+  float z;
+  int i;
+  __device__ __forceinline__ bool in(float value, int index) const { return value > z || (value == z && index <= i); }
+};
+__device__ __forceinline__ Floor no_floor() { return Floor{-CUDART_INF_F, INT_MIN}; }  // -inf and NaN are not in
+__device__ __forceinline__ Floor floor_of(u64 key) {
+  if (key == ~0ull) return Floor{CUDART_INF_F, INT_MIN};  // of an empty row: nothing is in
+  return Floor{order_value(key), order_index(key)};
+}
+
+// Which tokens are kept: from the floor on, with a weight of at least min_p.
 struct Kept {
-  u64 floor_key;
+  Floor floor;
   float min_p;
-  __device__ __forceinline__ bool all() const { return floor_key == 0 && !(min_p > 0.0f); }
+  __device__ __forceinline__ bool all() const { return floor.z == -CUDART_INF_F && !(min_p > 0.0f); }
 };
 
 template <typename T>
 struct Row {
   Slice<T> s;
-  cg::cluster_group cluster;
+  const RowGroup group;
   PickShared& sh;
   int parity;
+  int per_cta;   // chunks
+  bool special;  // this warp's elements have NaN, or the row +inf or nothing
   static constexpr int E = ElemOf<T>::E;
 
-  __device__ Row(PickShared& shared) : cluster(cg::this_cluster()), sh(shared), parity(0) {}
+  __device__ Row(PickShared& shared) : sh(shared), parity(0) {}
 
   // f(value, index) for the elements of this warp's chunks (and -inf past their end)
   template <typename F>
@@ -156,7 +193,7 @@ struct Row {
   // no ranking, lets ten times K through at one lane maximum a warp.
   __device__ float top_of(float lane_top, int K, float* floor) {
     const int warps = blockDim.x / 32, w = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const int all = warps * (int)cluster.num_blocks();
+    const int all = warps * (int)group.n;
     const int j = K > 0 ? min((2 * K + all - 1) / all, 32) : 1;
     uint32_t key = value_key(lane_top);
     for (int i = 0; i < j; ++i) {
@@ -168,17 +205,15 @@ struct Row {
       sh.count = 0;
       sh.row_floor = 0;
     }
-    cluster.sync();
+    group.sync();
     const int n = all * j, per = warps * j;
     if (K == 0) {  // every warp looks at all warps of the row
       uint32_t m = 0;
-      for (int i = lane; i < n; i += 32) m = max(m, *cluster.map_shared_rank(&sh.tops.mine[i % per], i / per));
-      m = __reduce_max_sync(~0u, m);
-      cluster.sync();  // the tops' memory is free
-      return key_value(m);
+      for (int i = lane; i < n; i += 32) m = max(m, *group.at(&sh.tops.mine[i % per], i / per));
+      return key_value(__reduce_max_sync(~0u, m));
     }
     for (int i = threadIdx.x; i < n; i += blockDim.x)
-      sh.tops.all[i] = *cluster.map_shared_rank(&sh.tops.mine[i % per], i / per);
+      sh.tops.all[i] = *group.at(&sh.tops.mine[i % per], i / per);
     __syncthreads();
     for (int i = threadIdx.x; i < n; i += blockDim.x) {
       const uint32_t x = sh.tops.all[i];
@@ -192,28 +227,55 @@ struct Row {
     return key_value(sh.row_top);
   }
 
-  __device__ float lane_maximum() const {
-    ChunkMax<T, false> top;
+  // this lane's maximum, NaN left out; `special` tells of NaN
+  __device__ float lane_maximum() {
+    ChunkMax<T, true> top;
     s.sweep([&](const uint4 (&v)[4], int) { top.add(v); });
-    return top.value();
+    float m = top.value();
+    special = __any_sync(~0u, m != m);
+    if (special) {
+      ChunkMax<T, false> numbers;
+      s.sweep([&](const uint4 (&v)[4], int) { numbers.add(v); });
+      m = numbers.value();
+      if (m != m) m = -CUDART_INF_F;
+    }
+    return m;
   }
 
   // Keys of elements >= floor to the first CTA's list (past its end they are only counted).  A lane whose maximum
-  // reaches the floor has such elements; its chunks are looked at by the whole warp.
+  // reaches the floor has such elements; its chunks are looked at by the whole warp, those of four lanes at a time.
   __device__ void collect(float floor, float lane_top) {
-    int* count = cluster.map_shared_rank(&sh.count, 0);
-    u64* list = cluster.map_shared_rank(sh.list, 0);
-    const int lane = threadIdx.x % 32;
-    for (uint32_t who = __ballot_sync(~0u, lane_top >= floor && lane_top > -CUDART_INF_F); who; who &= who - 1) {
-      for (int c = s.wlo + __ffs(who) - 1 + 32 * lane; c < s.whi; c += 32 * 32) {
-        float z[E];
-        unpack<T>(s.chunk(c), z);
+    int* count = group.at(&sh.count, 0);
+    u64* list = group.at(sh.list, 0);
+    const int lane = threadIdx.x % 32, w = threadIdx.x / 32, stride = (int)blockDim.x * 4;
+    const int own = 4 * ((s.n - w * kBatch + stride - 1) / stride);  // a lane's chunks, with those past the end
+    uint32_t who = __ballot_sync(~0u, lane_top >= floor && lane_top > -CUDART_INF_F);
+    while (who) {
+      int of[4];
 #pragma unroll
-        for (int e = 0; e < E; ++e)
-          if (z[e] >= floor && z[e] > -CUDART_INF_F) {
-            const int at = atomicAdd(count, 1);
-            if (at < kListMax) list[at] = order_key(z[e], s.first(c) + e);
-          }
+      for (int i = 0; i < 4; ++i) {
+        of[i] = who ? __ffs(who) - 1 : -1;
+        who &= who - 1;
+      }
+      for (int k = lane; k < own; k += 32) {
+        const int c = w * kBatch + (k / 4) * stride + 32 * (k % 4);
+        uint4 v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = of[i] >= 0 ? s.chunk(c + of[i]) : empty_chunk<T>();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          ChunkMax<T, false> top;
+          top.add(v[i]);
+          if (!(top.value() >= floor)) continue;
+          float z[E];
+          unpack<T>(v[i], z);
+#pragma unroll
+          for (int e = 0; e < E; ++e)
+            if (z[e] >= floor && z[e] > -CUDART_INF_F) {
+              const int at = atomicAdd(count, 1);
+              if (at < kListMax) list[at] = order_key(z[e], s.first(c + of[i]) + e);
+            }
+        }
       }
     }
   }
@@ -221,16 +283,16 @@ struct Row {
   // After a barrier: the K first keys of the row are in the first CTA's list, with others or (where more than a list
   // was collected) alone.
   __device__ void settle(int K) {
-    if (*cluster.map_shared_rank(&sh.count, 0) <= kListMax) return;  // the same in all CTAs
-    const u64 floor_key = radix_select<false>(Weigher(), 0, K - 1);
-    if (cluster.block_rank() == 0 && threadIdx.x == 0) sh.count = 0;
-    cluster.sync();
-    int* count = cluster.map_shared_rank(&sh.count, 0);
-    u64* list = cluster.map_shared_rank(sh.list, 0);
+    if (*group.at(&sh.count, 0) <= kListMax) return;  // the same in all CTAs
+    const Floor floor = floor_of(radix_select<false>(Weigher(), no_floor(), K - 1));
+    if (group.rank == 0 && threadIdx.x == 0) sh.count = 0;
+    group.sync();
+    int* count = group.at(&sh.count, 0);
+    u64* list = group.at(sh.list, 0);
     each([&](float z, int i) {
-      if (in_range(z, i, floor_key)) list[atomicAdd(count, 1)] = order_key(z, i);
+      if (floor.in(z, i)) list[atomicAdd(count, 1)] = order_key(z, i);
     });
-    cluster.sync();
+    group.sync();
   }
 
   // f(rank, key) for the list's keys, by one thread each
@@ -247,12 +309,8 @@ struct Row {
 
   // ---- masses
 
-  __device__ __forceinline__ bool in_range(float z, int i, u64 floor_key) const {
-    return z > -CUDART_INF_F && order_key(z, i) >= floor_key;
-  }
-
   __device__ __forceinline__ uint32_t kept_mass(float z, int i, const Weigher& weigh, const Kept& kept) const {
-    if (!in_range(z, i, kept.floor_key)) return 0;
+    if (!kept.floor.in(z, i)) return 0;
     const float w = weigh(z);
     return w >= kept.min_p ? grid_mass(w) : 0;
   }
@@ -267,254 +325,359 @@ struct Row {
     return q;
   }
 
-  // A lane's kept mass of a batch.  Where all tokens are kept and all weigh below 2^-8 the conversions are additions
-  // (the conversion instruction shares its pipe, a quarter of a warp an SM cycle, with the exponential) and 32 masses
-  // fit 32 bits.
-  __device__ __forceinline__ u64 batch_mass(const uint4 (&v)[4], int c, const Weigher& weigh, const Kept& kept) const {
-    if (kept.all()) {
-      ChunkMax<T, true> top;
-      top.add(v);
-      if (weigh.light(top.value())) {
-        uint32_t q = 0u - 4u * E * kMagicBits;
+  // A lane's kept mass of a batch in parts, whose sums over a warp's batch are below 32 bits.
+  struct LaneMass {
+    uint32_t high, low;
+    __device__ __forceinline__ u64 value() const { return ((u64)high << 15) + (u64)(long long)(int)low; }
+  };
+  template <bool kAll>
+  __device__ __forceinline__ LaneMass batch_mass(const uint4 (&v)[4], int c, const Weigher& weigh,
+                                                 const Kept& kept) const {
+    LaneMass sum = {0, 0};
+    if (special) {
+      u64 q = 0;
+#pragma unroll 1
+      for (int i = 0; i < 4; ++i) q += chunk_mass(s.chunk(c + 32 * i), c + 32 * i, weigh, kept);
+      return LaneMass{(uint32_t)(q >> 15), (uint32_t)q & 0x7fffu};
+    }
+    if (kAll) sum = {0u - 4u * E * kHighBits, 0u - 4u * E * kOnesBits};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float z[E];
-          unpack<T>(v[i], z);
+    for (int i = 0; i < 4; ++i) {
+      float z[E];
+      unpack<T>(v[i], z);
+      const int i0 = s.first(c + 32 * i);
 #pragma unroll
-          for (int e = 0; e < E; e += 2) {
-            const float2 y = weigh.exponents(z[e], z[e + 1]);
-            const float2 x = fma2(make_float2(exp2_32(y.x), exp2_32(y.y)), make_float2(kGrid, kGrid),
-                                  make_float2(kMagic, kMagic));
-            q += __float_as_uint(x.x) + __float_as_uint(x.y);
+      for (int e = 0; e < E; e += 2) {
+        const float2 y = weigh.exponents(z[e], z[e + 1]);
+        const float2 w = make_float2(exp2_32(y.x), exp2_32(y.y));
+        const Parts2 q(w);
+        if (kAll) {
+          sum.high += q.high[0] + q.high[1];
+          sum.low += q.low[0] + q.low[1];
+        } else {
+          if (kept.floor.in(z[e], i0 + e) && w.x >= kept.min_p) {
+            sum.high += q.high[0] - kHighBits;
+            sum.low += q.low[0] - kOnesBits;
+          }
+          if (kept.floor.in(z[e + 1], i0 + e + 1) && w.y >= kept.min_p) {
+            sum.high += q.high[1] - kHighBits;
+            sum.low += q.low[1] - kOnesBits;
           }
         }
-        return q;
       }
     }
-    u64 q = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) q += chunk_mass(v[i], c + 32 * i, weigh, kept);
-    return q;
+    return sum;
   }
 
   // a part is 2^shift batches
-  __device__ __forceinline__ int part_shift() const {
+  __device__ __forceinline__ static int part_shift(int chunks) {
     int shift = 0;
-    while ((s.wper + kBatch - 1) / kBatch > kParts << shift) ++shift;
+    while ((chunks + kBatch - 1) / kBatch > kParts << shift) ++shift;
     return shift;
   }
 
-  // warp sums of a batch's masses (below 2^35 a lane) into its part
-  __device__ __forceinline__ void add_part(u64 q, int c, int shift, u64& total) {
-    const uint32_t low = __reduce_add_sync(~0u, (uint32_t)q & 0xffffffu);
-    const uint32_t high = __reduce_add_sync(~0u, (uint32_t)(q >> 24));
-    if (threadIdx.x % 32 == 0 && (low | high)) {
-      const u64 x = low + ((u64)high << 24);
-      sh.parts[threadIdx.x / 32][((c - s.wlo) / kBatch) >> shift] += x;
-      total += x;
-    }
+  // the warp's sum of a batch's masses to its part (a warp's own, unless parts are of several batches)
+  __device__ __forceinline__ void add_part(LaneMass q, int c, int shift, u64& total) {
+    const LaneMass sum = {__reduce_add_sync(~0u, q.high), __reduce_add_sync(~0u, q.low)};
+    if (threadIdx.x % 32) return;
+    const u64 x = sum.value();
+    total += x;
+    if (shift == 0)
+      sh.parts[c / kBatch] = x;
+    else
+      atomicAdd(&sh.parts[(c / kBatch) >> shift], x);
+  }
+  __device__ __forceinline__ void clear_parts() {  // before a barrier, for add_part with a shift
+    for (int i = threadIdx.x; i < kParts; i += blockDim.x) sh.parts[i] = 0;
+    if (threadIdx.x == 0) sh.cta_q = 0;
   }
 
-  __device__ void clear_parts() {
-    for (int i = threadIdx.x % 32; i < kParts; i += 32) sh.parts[threadIdx.x / 32][i] = 0;
-    __syncwarp();
-  }
-
-  // masses of the row's kept tokens, by part and by warp
-  __device__ void masses(const Weigher& weigh, const Kept& kept) {
-    const int shift = part_shift();
+  // masses of the row's kept tokens, by part and by CTA
+  __device__ __noinline__ void masses(const Weigher& weigh, const Kept& kept) {
+    const int shift = part_shift(s.n);
     clear_parts();
+    __syncthreads();
     u64 total = 0;
-    s.sweep([&](const uint4 (&v)[4], int c) { add_part(batch_mass(v, c, weigh, kept), c, shift, total); });
-    if (threadIdx.x % 32 == 0) sh.warp_q[threadIdx.x / 32] = total;
+    if (kept.all())
+      s.sweep([&](const uint4 (&v)[4], int c) { add_part(batch_mass<true>(v, c, weigh, kept), c, shift, total); });
+    else
+      s.sweep([&](const uint4 (&v)[4], int c) { add_part(batch_mass<false>(v, c, weigh, kept), c, shift, total); });
+    if (threadIdx.x % 32 == 0) atomicAdd(&sh.cta_q, total);
   }
 
-  // After a cluster barrier: the row's kept mass, the CTA's own and that of the CTAs ahead of it.  Every warp for itself.
+  // After a barrier of the group: the row's kept mass, the CTA's own and that of the CTAs ahead of it.
   __device__ u64 all_mass(u64* mine, u64* ahead) const {
-    const int warps = blockDim.x / 32, all = warps * (int)cluster.num_blocks();
-    const int rank = (int)cluster.block_rank();
-    u64 total = 0, own = 0, before = 0;
-    for (int i = threadIdx.x % 32; i < all; i += 32) {
-      const int r = i / warps;
-      const u64 x = *cluster.map_shared_rank(&sh.warp_q[i - r * warps], r);
+    u64 total = 0;
+    *mine = sh.cta_q;
+    *ahead = 0;
+    for (unsigned r = 0; r < group.n; ++r) {
+      const u64 x = *group.at(&sh.cta_q, r);
+      if (r < group.rank) *ahead += x;
       total += x;
-      if (r < rank) before += x;
-      if (r == rank) own += x;
     }
-    *mine = warp_sum(own);
-    *ahead = warp_sum(before);
-    return warp_sum(total);
+    return total;
   }
 
   // ---- thresholds
 
-  // The key of the element, among keys >= floor, at which the running total of the order passes the target: with kMass
-  // totals are masses and the target floor(arg all / 2^24) - 1, else they are counts and it is arg (or the last).
-  // All ones for a row without elements.  A histogram over evenly spaced exponents finds the bin; where it has more
-  // elements than a list, a second one cuts it again; the first CTA ranks the bin's elements.  Rows of many equal
+  // Bins go down the order, by exponent; past 2^-32 of the maximum the last one.
+  __device__ __forceinline__ static int bin_of(float y) {
+    return (int)(__float_as_uint(fminf(y * -kBinsPerUnit, (float)(kBins - 1)) + kOnes) - kOnesBits);
+  }
+  // A bin cut in as many again; b is the bin of y.
+  __device__ __forceinline__ static int bin_within(float y, int b) {
+    const float x = fminf(y * -kBinsPerUnit, (float)(kBins - 1));
+    return (int)fminf((x - ((float)b - 0.5f)) * kBins, (float)(kBins - 1));
+  }
+
+  // One warp: the lowest value whose bin is at most b (with `outer` >= 0: whose bin is less than `outer`, or is `outer`
+  // with a bin within of at most b), +inf if no value up to the maximum is.  The bins do not increase with the value; 32
+  // values are tried at a time.
+  __device__ __noinline__ static float lowest_of_bin(const Weigher& weigh, int b, int outer) {
+    const uint32_t lane = threadIdx.x % 32;
+    const auto in = [&](uint32_t key) {
+      const float y = weigh.exponent(key_value(key));
+      const int own = bin_of(y);
+      return outer < 0 ? own <= b : own < outer || (own == outer && bin_within(y, own) <= b);
+    };
+    uint32_t lo = value_key(-CUDART_MAX_NORMAL_F), hi = value_key(weigh.m);
+    if (!in(hi)) return CUDART_INF_F;
+    while (lo < hi) {  // the answer is in [lo, hi]
+      const uint32_t step = (hi - lo) / 32 + 1;
+      const uint32_t hit = __ballot_sync(~0u, in(min(lo + lane * step, hi)));
+      if (!hit) {
+        lo = min(lo + 31 * step, hi - 1) + 1;
+      } else {
+        const int first = __ffs(hit) - 1;
+        hi = min(lo + first * step, hi);
+        lo = first ? lo + (first - 1) * step + 1 : hi;
+      }
+    }
+    return key_value(lo);
+  }
+
+  // After a barrier, in one warp: the bin of the cluster's histograms at which the running total passes t, and the rest
+  // of t within it, to sh.found and sh.before; all ones for histograms of nothing.  t may be given as a share of all.
+  template <bool kMass>
+  __device__ __noinline__ void find_bin(u64 t, bool share) {
+    static_assert(kGroups == 64, "two groups of bins a lane");
+    const int lane = threadIdx.x % 32;
+    const unsigned ctas = group.n;
+    u64 x0 = 0, x1 = 0;
+    for (unsigned r = 0; r < ctas; ++r) {
+      const Histogram* h = group.at(&sh.bins, r);
+      x0 += h->group[2 * lane];
+      x1 += h->group[2 * lane + 1];
+    }
+    u64 upto = warp_scan(x0 + x1);
+    const u64 all = __shfl_sync(~0u, upto, 31);
+    if (share) t = kMass ? share24(t, all) - 1 : min(t, all - 1);
+    int g = min(__popc(__ballot_sync(~0u, upto <= t)), 31);
+    u64 ahead = __shfl_sync(~0u, upto - x0 - x1, g);
+    const u64 half = __shfl_sync(~0u, x0, g);
+    g *= 2;
+    if (ahead + half <= t) {
+      ahead += half;
+      ++g;
+    }
+    u64 x = 0;
+    for (unsigned r = 0; r < ctas; ++r) x += group.at(&sh.bins, r)->mass(32 * g + lane);
+    upto = ahead + warp_scan(x);
+    const int l = min(__popc(__ballot_sync(~0u, upto <= t)), 31);
+    const u64 before = __shfl_sync(~0u, upto - x, l);
+    if (lane == 0) {
+      sh.found = all ? (u64)(32 * g + l) : ~0ull;
+      sh.before = t - before;
+    }
+  }
+
+  // The list's first n keys into descending order.
+  __device__ __noinline__ void sort_list(int n) {
+    int size = 2;
+    while (size < n) size *= 2;
+    for (int i = n + threadIdx.x; i < size; i += blockDim.x) sh.list[i] = 0;
+    for (int k = 2; k <= size; k *= 2)
+      for (int d = k / 2; d; d /= 2) {
+        __syncthreads();
+        for (int t = threadIdx.x; t < size / 2; t += blockDim.x) {
+          const int i = 2 * t - (t & (d - 1));
+          const u64 a = sh.list[i], b = sh.list[i + d];
+          if ((a < b) == ((i & k) == 0)) {
+            sh.list[i] = b;
+            sh.list[i + d] = a;
+          }
+        }
+      }
+    __syncthreads();
+  }
+
+  // The key of the element, among those from the floor on, at which the running total of the order passes the target:
+  // with kMass totals are masses and the target floor(arg all / 2^24) - 1, else they are counts and it is arg (or the
+  // last).  All ones for a row without elements.  A histogram over evenly spaced exponents finds the bin; where it has
+  // more elements than a list, a second one cuts it again; the first CTA sorts the bin's elements.  Rows of many equal
   // values go by radix selection.
   // With min_p >= 0 the masses of the kept tokens (from the threshold on, of at least min_p) are left by part and by warp
   // as masses() leaves them, a cluster barrier included.
   template <bool kMass>
-  __device__ u64 select(const Weigher& weigh, u64 floor_key, u64 arg, float min_p) {
+  __device__ __noinline__ u64 select(const Weigher& weigh, Floor floor, u64 arg, float min_p) {
     const int lane = threadIdx.x % 32, warps = blockDim.x / 32, warp = threadIdx.x / 32;
-    int* count = cluster.map_shared_rank(&sh.count, 0);
-    u64* list = cluster.map_shared_rank(sh.list, 0);
-    const bool keep = min_p >= 0.0f;
-    const int shift = part_shift();
-    u64 t = 0;
-    uint32_t outer = 0;  // the bin of the first level
-    int n = kListMax + 1;
+    int* count = group.at(&sh.count, 0);
+    u64* list = group.at(sh.list, 0);
+    const bool keep = min_p >= 0.0f, free = floor.z == -CUDART_INF_F;
     const bool fits = (long long)per_cta * E <= kSliceElems && weigh.m < CUDART_INF_F;
+    u64 t = arg;
+    int outer = -1;  // the bin of the first level
+    int n = kListMax + 1;
     for (int level = 0; level < 2 && fits; ++level) {
       // the cluster's CTAs have left the memory of the bins and the count behind: a barrier is above
       for (int i = threadIdx.x; i < kBins; i += blockDim.x) sh.bins.low[i] = sh.bins.high[i] = 0;
       if (threadIdx.x == 0) sh.count = 0;
       __syncthreads();
-      // Bins go down the order, by exponent; in the second level those outside the first's bin are below 0 or kBins.
-      const auto bin_of = [&](float y) -> int {
-        const float x = fminf(y * -kBinsPerUnit, (float)(kBins - 1));
-        const int b = (int)(__float_as_uint(x + kMagic) - kMagicBits);
-        if (level == 0) return b;
-        if (b != (int)outer) return b < (int)outer ? -1 : kBins;
-        return (int)fminf((x - ((float)outer - 0.5f)) * kBins, (float)(kBins - 1));
-      };
-      const auto exponent = [&](float z) { return __fmul_rn(__fsub_rn(z, weigh.m), weigh.c); };
-      each([&](float z, int i) {
-        const float y = exponent(z);
-        if (kMass) {
-          const uint32_t q = grid_mass(exp2_32(y));
-          if (q == 0 || (floor_key && order_key(z, i) < floor_key)) return;
-          const int b = bin_of(y);
-          if (b < 0 || b >= kBins) return;
-          atomicAdd(&sh.bins.low[b], q & 0x7fffu);
-          if (q >> 15) atomicAdd(&sh.bins.high[b], q >> 15);
-        } else {
-          if (!in_range(z, i, floor_key)) return;
-          const int b = bin_of(y);
-          if (b >= 0 && b < kBins) atomicAdd(&sh.bins.low[b], 1u);
-        }
-      });
+      if (kMass && level == 0 && !special) {
+        s.sweep([&](const uint4 (&v)[4], int c) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float z[E];
+            unpack<T>(v[i], z);
+            const int i0 = s.first(c + 32 * i);
+#pragma unroll
+            for (int e = 0; e < E; e += 2) {
+              const float2 y = weigh.exponents(z[e], z[e + 1]);
+              const Parts2 q(make_float2(exp2_32(y.x), exp2_32(y.y)));
+              const float2 b = fma2(y, make_float2(-kBinsPerUnit, -kBinsPerUnit), make_float2(kOnes, kOnes));
+              // a mass above 0 has an exponent above -32: its bin needs no bound
+#pragma unroll
+              for (int o = 0; o < 2; ++o) {
+                const uint32_t high = q.high[o] - kHighBits, low = q.low[o] - kOnesBits;
+                const uint32_t bin = __float_as_uint(o ? b.y : b.x) - kOnesBits;
+                const bool in = free || floor.in(z[e + o], i0 + e + o);
+                if (in && low) atomicAdd(&sh.bins.low[bin], low);
+                if (in && high) atomicAdd(&sh.bins.high[bin], high);
+              }
+            }
+          }
+        });
+      } else {
+        each([&](float z, int i) {
+          if (!floor.in(z, i)) return;
+          const float y = weigh.exponent(z);
+          int b = bin_of(y);
+          if (level) {
+            if (b != outer) return;
+            b = bin_within(y, b);
+          }
+          if (kMass) {
+            const uint32_t q = grid_mass(exp2_32(y));
+            if (q & 0x7fffu) atomicAdd(&sh.bins.low[b], q & 0x7fffu);
+            if (q >> 15) atomicAdd(&sh.bins.high[b], q >> 15);
+          } else {
+            atomicAdd(&sh.bins.low[b], 1u);
+          }
+        });
+      }
       __syncthreads();
       for (int g = warp; g < kGroups; g += warps) {
-        const u64 x = warp_sum(sh.bins.low[32 * g + lane] + ((u64)sh.bins.high[32 * g + lane] << 15));
+        const u64 x = warp_sum(sh.bins.mass(32 * g + lane));
         if (lane == 0) sh.bins.group[g] = x;
       }
-      cluster.sync();
-      if (warp == 0) {  // every CTA finds the bin for itself
-        static_assert(kGroups == 64, "two groups of bins a lane");
-        u64 x0 = 0, x1 = 0;
-        for (unsigned r = 0; r < cluster.num_blocks(); ++r) {
-          const Histogram* h = cluster.map_shared_rank(&sh.bins, r);
-          x0 += h->group[2 * lane];
-          x1 += h->group[2 * lane + 1];
-        }
-        u64 upto = warp_scan(x0 + x1);
-        const u64 all = __shfl_sync(~0u, upto, 31);
-        if (level == 0) t = kMass ? share24(arg, all) - 1 : min(arg, all - 1);
-        int g = min(__popc(__ballot_sync(~0u, upto <= t)), 31);
-        u64 ahead = __shfl_sync(~0u, upto - x0 - x1, g);
-        const u64 half = __shfl_sync(~0u, x0, g);
-        g *= 2;
-        if (ahead + half <= t) {
-          ahead += half;
-          ++g;
-        }
-        u64 x = 0;
-        for (unsigned r = 0; r < cluster.num_blocks(); ++r) {
-          const Histogram* h = cluster.map_shared_rank(&sh.bins, r);
-          x += h->low[32 * g + lane] + ((u64)h->high[32 * g + lane] << 15);
-        }
-        upto = ahead + warp_scan(x);
-        const int l = min(__popc(__ballot_sync(~0u, upto <= t)), 31);
-        const u64 before = __shfl_sync(~0u, upto - x, l);
-        if (lane == 0) {
-          sh.found = all ? (u64)(32 * g + l) : ~0ull;
-          sh.before = t - before;  // the target within the bin
+      group.sync();
+      if (warp == 0) {  // every CTA for itself
+        find_bin<kMass>(t, level == 0);
+        __syncwarp();
+        if (sh.found != ~0ull) {
+          const int bin = (int)sh.found;
+          const float low = lowest_of_bin(weigh, bin, outer), high = lowest_of_bin(weigh, bin - 1, outer);
+          if (lane == 0) {
+            sh.bin_low = low;
+            sh.bin_high = high;
+          }
         }
       }
       __syncthreads();
       if (sh.found == ~0ull) {
-        if (lane == 0) sh.warp_q[warp] = 0;
-        cluster.sync();
+        if (threadIdx.x == 0) sh.cta_q = 0;
+        group.sync();
         return ~0ull;
       }
       const int bin = (int)sh.found;
+      const float low = sh.bin_low, high = sh.bin_high;
       t = sh.before;
-      // the bin's elements to the list; the mass of what is kept for sure to the parts
+      // the bin's elements, from low to below high, to the list; the mass of what is above to the parts
+      const Floor above = Floor{high, 0x7fffffff};
+      const Kept sure{above.z > floor.z ? above : floor, fmaxf(min_p, 0.0f)};
+      const int shift = part_shift(s.n);
       u64 total = 0;
       if (keep) clear_parts();
+      __syncthreads();
       s.sweep([&](const uint4 (&v)[4], int c) {
-        u64 sum = 0;
+        ChunkMax<T, false> top;
+        top.add(v);
+        const float m = top.value();
+        if (m >= low) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float z[E];
-          unpack<T>(v[i], z);
-          const int i0 = s.first(c + 32 * i);
+          for (int i = 0; i < 4; ++i) {
+            float z[E];
+            unpack<T>(v[i], z);
 #pragma unroll
-          for (int e = 0; e < E; ++e) {
-            const float y = exponent(z[e]);
-            const int b = bin_of(y);
-            if (b > bin || !(z[e] > -CUDART_INF_F)) continue;
-            if (floor_key && order_key(z[e], i0 + e) < floor_key) continue;
-            if (b == bin) {
-              const int at = atomicAdd(count, 1);
-              if (at < kListMax) list[at] = order_key(z[e], i0 + e);
-            } else if (keep) {
-              const float w = exp2_32(y);
-              if (w >= min_p) sum += grid_mass(w);
-            }
+            for (int e = 0; e < E; ++e)
+              if (z[e] >= low && z[e] < high && floor.in(z[e], s.first(c + 32 * i) + e)) {
+                const int at = atomicAdd(count, 1);
+                if (at < kListMax) list[at] = order_key(z[e], s.first(c + 32 * i) + e);
+              }
           }
         }
-        if (keep) add_part(sum, c, shift, total);
+        if (keep && __any_sync(~0u, m >= high)) add_part(batch_mass<false>(v, c, weigh, sure), c, shift, total);
       });
-      if (keep && lane == 0) sh.warp_q[warp] = total;
-      cluster.sync();
+      if (keep && lane == 0 && total) atomicAdd(&sh.cta_q, total);
+      group.sync();
       n = *count;
       if (n <= kListMax) break;
-      outer = (uint32_t)bin;
-      cluster.sync();  // all have seen the count
+      outer = bin;
+      group.sync();  // all have seen the count
     }
     if (n > kListMax) {
-      const u64 key = radix_select<kMass>(weigh, floor_key, arg);
+      const u64 key = radix_select<kMass>(weigh, floor, arg);
       if (keep) {
-        masses(weigh, Kept{max(key, 1ull), min_p});
-        cluster.sync();
+        masses(weigh, Kept{floor_of(key), min_p});
+        group.sync();
       }
       return key;
     }
-    if (cluster.block_rank() == 0) {
-      for (int i = threadIdx.x; i < n; i += blockDim.x) {
-        const u64 key = sh.list[i];
-        u64 ahead = 0;
-        for (int j = 0; j < n; ++j)
-          if (sh.list[j] > key) ahead += kMass ? grid_mass(weigh(order_value(sh.list[j]))) : 1u;
-        const u64 own = kMass ? grid_mass(weigh(order_value(key))) : 1u;
-        if (ahead <= t && t < ahead + own) sh.found = key;
+    if (group.rank == 0) {
+      sort_list(n);
+      // the running total down the list, by one warp
+      if (warp == 0) {
+        u64 upto = 0;
+        for (int i0 = 0; i0 < n; i0 += 32) {
+          const u64 key = i0 + lane < n ? sh.list[i0 + lane] : 0;
+          const u64 q = i0 + lane >= n ? 0 : kMass ? grid_mass(weigh(order_value(key))) : 1u;
+          const u64 sum = upto + warp_scan(q);
+          if (sum - q <= t && t < sum) {
+            sh.found = key;
+            sh.last = i0 + lane;
+          }
+          upto = __shfl_sync(~0u, sum, 31);
+        }
       }
       __syncthreads();
       if (keep)
-        for (int i = threadIdx.x; i < n; i += blockDim.x) {
+        for (int i = threadIdx.x; i <= sh.last; i += blockDim.x) {
           const u64 key = sh.list[i];
           const float w = weigh(order_value(key));
-          if (key < sh.found || !(w >= min_p)) continue;
-          // the element's CTA, warp and part: head is the same in all CTAs, the warps' shares are not
+          if (!(w >= min_p)) continue;
+          // the element's CTA and part
           const int c = (order_index(key) + s.head) / E, r = c / per_cta, at = c - r * per_cta;
-          const int there = (slice_chunks(r) + warps - 1) / warps, w_at = at / there;
-          int sh_there = 0;
-          while ((there + kBatch - 1) / kBatch > kParts << sh_there) ++sh_there;
           const u64 q = grid_mass(w);
-          atomicAdd(cluster.map_shared_rank(&sh.parts[w_at][((at - w_at * there) / kBatch) >> sh_there], r), q);
-          atomicAdd(cluster.map_shared_rank(&sh.warp_q[w_at], r), q);
+          atomicAdd(group.at(&sh.parts[(at / kBatch) >> part_shift(slice_chunks(r))], r), q);
+          atomicAdd(group.at(&sh.cta_q, r), q);
         }
     }
-    cluster.sync();
-    const u64 key = *cluster.map_shared_rank(&sh.found, 0);
-    if (!keep) cluster.sync();  // found and the list may be written again
+    group.sync();
+    const u64 key = *group.at(&sh.found, 0);
+    if (!keep) group.sync();  // found and the list may be written again
     return key;
   }
 
-  int per_cta;
   // chunks of CTA r's slice
   __device__ int slice_chunks(int r) const {
     const int total = s.V ? (s.head + s.V - 1) / E + 1 : 0;
@@ -523,9 +686,9 @@ struct Row {
 
   // The same by eight bits of the keys at a time.
   template <bool kMass>
-  __device__ u64 radix_select(const Weigher& weigh, u64 floor_key, u64 arg) {
+  __device__ __noinline__ u64 radix_select(const Weigher& weigh, Floor floor, u64 arg) {
     u64 prefix = 0, before = 0, t = 0;
-    cluster.sync();
+    group.sync();
     for (int shift = 56; shift >= 0; shift -= 8) {
       if (shift < 32 && shift > 0 && s.V > 0 && (uint32_t)(s.V - 1) >> shift == 0) {
         prefix |= 0xffull << shift;  // every index has these bits clear
@@ -536,20 +699,20 @@ struct Row {
       __syncthreads();
       each([&](float z, int i) {
         const u64 key = order_key(z, i);
-        if (z > -CUDART_INF_F && key >= floor_key && (shift == 56 || (key ^ prefix) >> (shift + 8) == 0)) {
+        if (floor.in(z, i) && (shift == 56 || (key ^ prefix) >> (shift + 8) == 0)) {
           const u64 add = kMass ? (u64)grid_mass(weigh(z)) : 1ull;
           if (add) atomicAdd(&hist[(key >> shift) & 255], add);
         }
       });
-      cluster.sync();
+      group.sync();
       if (threadIdx.x < 32) {
         // lane l holds bins 255 - 8 l downwards: a scan over lanes is a scan down the order
         u64 b[8], sum = 0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           b[i] = 0;
-          for (unsigned r = 0; r < cluster.num_blocks(); ++r)
-            b[i] += *cluster.map_shared_rank(&hist[255 - 8 * threadIdx.x - i], r);
+          for (unsigned r = 0; r < group.n; ++r)
+            b[i] += *group.at(&hist[255 - 8 * threadIdx.x - i], r);
           sum += b[i];
         }
         const u64 upto = before + warp_scan(sum);
@@ -570,26 +733,31 @@ struct Row {
       parity ^= 1;
       if (prefix == ~0ull) break;
     }
-    cluster.sync();
+    group.sync();
     return prefix;
   }
 
   // ---- draws
 
   // one warp: the token of the slice whose kept mass covers t (counted from the slice's start)
-  __device__ void draw(u64 t, const Weigher& weigh, const Kept& kept, u64 all, int32_t* tok, float* prob) const {
-    const int lane = threadIdx.x % 32, warps = blockDim.x / 32;
-    int w = 0;
-    while (w < warps - 1 && t >= sh.warp_q[w]) t -= sh.warp_q[w++];
-    const u64 part = sh.parts[w][lane];
-    const u64 parts = warp_scan(part);
-    const int p = min(__popc(__ballot_sync(~0u, parts <= t)), kParts - 1);
-    t -= __shfl_sync(~0u, parts - part, p);
-    for (int c0 = w * s.wper + ((p << part_shift()) * kBatch); c0 < s.n; c0 += 32) {
-      // lanes past the warp's last chunk look into the next one's: the answer is never there
+  __device__ __noinline__ void draw(u64 t, const Weigher& weigh, const Kept& kept, u64 all, int32_t* tok,
+                                    float* prob) const {
+    const int lane = threadIdx.x % 32;
+    int p = 0;  // the part
+    for (int p0 = 0;; p0 += 32) {
+      const u64 part = sh.parts[p0 + lane], upto = warp_scan(part), sum = __shfl_sync(~0u, upto, 31);
+      if (t >= sum && p0 + 32 < kParts) {
+        t -= sum;
+        continue;
+      }
+      const int l = min(__popc(__ballot_sync(~0u, upto <= t)), 31);
+      p = p0 + l;
+      t -= __shfl_sync(~0u, upto - part, l);
+      break;
+    }
+    for (int c0 = (p << part_shift(s.n)) * kBatch; c0 < s.n; c0 += 32) {
       const int c = c0 + lane;
-      uint4 v = empty_chunk<T>();
-      if (c < s.n) v = s.chunk(c);
+      const uint4 v = s.chunk(c);
       const u64 q = chunk_mass(v, c, weigh, kept);
       const u64 upto = warp_scan(q);
       const u64 total = __shfl_sync(~0u, upto, 31);
@@ -620,7 +788,7 @@ struct Row {
   }
 
   // the first CTA: draws from the top-k list that settle() left
-  __device__ void draw_from_list(const Weigher& weigh, int top_k, u64 p24, float min_p, const float* u, int S,
+  __device__ __noinline__ void draw_from_list(const Weigher& weigh, int top_k, u64 p24, float min_p, const float* u, int S,
                                  int32_t* tok, float* prob) {
     TopList& l = sh.top;
     const int n = min(top_k, sh.count);
@@ -668,14 +836,14 @@ struct Row {
 };
 
 template <typename T>
-__global__ void __launch_bounds__(kRowThreads, 2) k_propose(PickArgs a) {
+__global__ void __launch_bounds__(kRowThreads, 3) k_propose(PickArgs a) {
   __shared__ PickShared sh;
   Row<T> row(sh);
   constexpr int E = ElemOf<T>::E;
-  const unsigned ctas = row.cluster.num_blocks(), rank = row.cluster.block_rank();
+  const unsigned ctas = row.group.n, rank = row.group.rank;
   const long long r = blockIdx.x / ctas;
   const float T_ = a.temperature ? a.temperature[r / a.rows.k] : 1.0f;
-  row.s.open(T_ >= 0.0f ? row_address<T>(a.rows, r) : nullptr, a.rows, rank);
+  row.s.open(T_ >= 0.0f ? row_address<T>(a.rows, r) : nullptr, a.rows, rank, sh.ends);
   Weigher weigh;
   weigh.c = fminf(__fdiv_rn(kLog2e, T_), CUDART_MAX_NORMAL_F);
   // one pass: each lane's maximum so far and the sum of its weights relative to it
@@ -708,32 +876,23 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_propose(PickArgs a) {
   weigh.m = row.top_of(top, a.K, &floor);
   row.collect(floor, top);
   float sum = sums.x + sums.y;
-  if (sum != sum || weigh.m == CUDART_INF_F) {  // NaN or +inf among this lane's elements, or +inf in the row
+  if (__any_sync(~0u, sum != sum) || weigh.m == CUDART_INF_F) {  // NaN or +inf among the warp's elements or the row's
     sum = 0.0f;
-    for (int c = row.s.wlo + (int)(threadIdx.x % 32); c < row.s.whi; c += 32) {
-      float z[E];
-      unpack<T>(row.s.chunk(c), z);
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const float w = weigh(z[e]);
-        sum += w > 0.0f ? w : 0.0f;
-      }
-    }
+    row.each([&](float z, int) {
+      const float w = weigh(z);
+      sum += w > 0.0f ? w : 0.0f;
+    });
   } else {
     sum = top == -CUDART_INF_F ? 0.0f : sum * exp2_32((top - weigh.m) * weigh.c);
   }
   for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
-  if (threadIdx.x % 32 == 0) sh.warp_sum[threadIdx.x / 32] = sum;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int w = 1; w < (int)blockDim.x / 32; ++w) sum += sh.warp_sum[w];
-    *row.cluster.map_shared_rank(&sh.sums[rank], 0) = sum;
-  }
-  row.cluster.sync();
+  const int warps = blockDim.x / 32;
+  if (threadIdx.x % 32 == 0) *row.group.at(&sh.sums[rank * warps + threadIdx.x / 32], 0) = sum;
+  row.group.sync();
   row.settle(a.K);
   if (rank != 0) return;
   sum = 0.0f;
-  for (unsigned i = 0; i < ctas; ++i) sum += sh.sums[i];
+  for (unsigned i = 0; i < ctas * warps; ++i) sum += sh.sums[i];
   int32_t* cand = a.cand + r * a.K;
   float* conf = a.conf + r * a.K;
   for (int i = sh.count + threadIdx.x; i < a.K; i += blockDim.x) {
@@ -745,14 +904,14 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_propose(PickArgs a) {
     cand[at] = order_index(key);
     conf[at] = T_ == 0.0f ? (at == 0 ? 1.0f : 0.0f) : weigh(order_value(key)) / sum;
   });
-  row.cluster.sync();  // the others have looked at the count
+  if (ctas > 1) row.group.sync();  // the others have looked at the count
 }
 
 template <typename T>
 __global__ void __launch_bounds__(kRowThreads, 2) k_sample(PickArgs a) {
   __shared__ PickShared sh;
   Row<T> row(sh);
-  const unsigned ctas = row.cluster.num_blocks(), rank = row.cluster.block_rank();
+  const unsigned ctas = row.group.n, rank = row.group.rank;
   const long long r = blockIdx.x / ctas, b = r / a.rows.k;
   const float T_ = a.temperature ? a.temperature[b] : 1.0f;
   float top_p = a.top_p ? a.top_p[b] : 1.0f;
@@ -765,7 +924,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_sample(PickArgs a) {
   if (top_k <= 0 || top_k > a.rows.V) top_k = a.rows.V;
   const bool by_list = top_k <= kMaxK;
   row.per_cta = a.rows.per;
-  row.s.open(good ? row_address<T>(a.rows, r) : nullptr, a.rows, rank);
+  row.s.open(good ? row_address<T>(a.rows, r) : nullptr, a.rows, rank, sh.ends);
   const float lane_top = row.lane_maximum();
   Weigher weigh;
   float floor;
@@ -773,24 +932,25 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_sample(PickArgs a) {
   weigh.c = fminf(__fdiv_rn(kLog2e, T_), CUDART_MAX_NORMAL_F);
   if (by_list) {
     row.collect(floor, lane_top);
-    row.cluster.sync();
+    row.group.sync();
     row.settle(top_k);
     if (rank != 0) return;
     row.draw_from_list(weigh, top_k, p24, min_p, a.u + r * a.S, a.S, a.tok + r * a.S, a.prob + r * a.S);
-    row.cluster.sync();  // the others have looked at the count
+    if (ctas > 1) row.group.sync();  // the others have looked at the count
     return;
   }
   const bool by_mass = p24 < (1u << 24);
-  Kept kept{0, fmaxf(min_p, 0.0f)};
-  if (top_k < a.rows.V) kept.floor_key = row.template select<false>(weigh, 0, top_k - 1, by_mass ? -1.0f : kept.min_p);
-  if (by_mass) kept.floor_key = row.template select<true>(weigh, kept.floor_key, p24, kept.min_p);
+  row.special |= fabsf(weigh.m) == CUDART_INF_F;
+  Kept kept{no_floor(), fmaxf(min_p, 0.0f)};
+  if (top_k < a.rows.V)
+    kept.floor = floor_of(row.template select<false>(weigh, kept.floor, top_k - 1, by_mass ? -1.0f : kept.min_p));
+  if (by_mass) kept.floor = floor_of(row.template select<true>(weigh, kept.floor, p24, kept.min_p));
   if (top_k == a.rows.V && !by_mass) {
     row.masses(weigh, kept);
-    row.cluster.sync();
+    row.group.sync();
   }
   u64 mine, ahead;
   const u64 all = row.all_mass(&mine, &ahead);
-  __syncwarp();
   for (int i = threadIdx.x / 32; i < a.S; i += blockDim.x / 32) {
     const long long o = r * a.S + i;
     const float u = a.u[o];
@@ -804,7 +964,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_sample(PickArgs a) {
     const u64 t = min(share24((u64)(u * 16777216.0f), all), all - 1);
     if (t >= ahead && t < ahead + mine) row.draw(t - ahead, weigh, kept, all, &a.tok[o], &a.prob[o]);
   }
-  row.cluster.sync();  // no CTA leaves while its masses are read
+  if (ctas > 1) row.group.sync();  // no CTA leaves while its masses are read
 }
 
 template <typename T>
