@@ -164,7 +164,8 @@ struct Slice {
     flo = c0 == 0 && head > 0 ? 1 : 0;
     fhi = max(c0 + n == total && (head + V) % E != 0 ? n - 1 : n, flo);
     ends = shared;
-    if (threadIdx.x < 2 && n > 0) {
+    if (flo == 0 && fhi == n) return;  // the same in all threads
+    if (threadIdx.x < 2) {
       const int c = threadIdx.x == 0 ? 0 : n - 1, i0 = first(c);
       const T* p = reinterpret_cast<const T*>(address(c));
       float f[E];
@@ -175,15 +176,12 @@ struct Slice {
     __syncthreads();
   }
 
-  __device__ __forceinline__ int batches() const { return (n + kBatch - 1) / kBatch; }
-
   // f(v, c) for this warp's batches: v are this lane's chunks c, c + 32, c + 64 and c + 96, of -inf past the slice's end
   template <typename F>
   __device__ __forceinline__ void sweep(F f) const {
-    const int lane = threadIdx.x % 32;
     for (int base = (int)(threadIdx.x / 32) * kBatch; base < n; base += (int)blockDim.x * 4) {
       uint4 v[4];
-      const int c = base + lane;
+      const int c = base + (int)(threadIdx.x % 32);
       if (base >= flo && base + kBatch <= fhi) {
         const uint4* p = reinterpret_cast<const uint4*>(address(c));
 #pragma unroll
@@ -289,12 +287,11 @@ struct ChunkMax {
 };
 
 template <typename T>
-__device__ __forceinline__ const T* row_address(const RowArgs& a, long long r) {
-  const long long b = r / a.k;
-  const int j = (int)(r - b * a.k);
+__device__ __forceinline__ const T* row_address(const RowArgs& a, int r) {
+  const int b = r / a.k, j = r - b * a.k;
   const int i = a.pos ? a.pos[r] : j;
   if (i < 0 || i >= a.n || a.V == 0) return nullptr;
-  return static_cast<const T*>(a.base) + b * a.stride_b + (long long)i * a.stride_n;
+  return static_cast<const T*>(a.base) + b * a.stride_b + i * a.stride_n;
 }
 
 // ---------------------------------------------------------------- the order

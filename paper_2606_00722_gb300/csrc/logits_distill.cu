@@ -58,11 +58,11 @@ __device__ __forceinline__ float warp_max_nan(float x) {
 }
 
 // One warp: p and log p of the row's entries, and whether any counts.
-__device__ void teacher(const DistillArgs& a, long long r, Targets& t) {
+__device__ void teacher(const DistillArgs& a, int r, Targets& t) {
   const int lane = threadIdx.x % 32;
   float m = -CUDART_INF_F;
   for (int k = lane; k < a.K; k += 32) {
-    const long long o = r * a.K + k;
+    const long long o = (long long)r * a.K + k;
     const int id = a.ids[o];
     const float v = a.vals[o];
     const bool counts = id >= 0 && id < a.rows.V && (!a.valid || a.valid[o] == 1) && v != -CUDART_INF_F;
@@ -176,8 +176,8 @@ __device__ void write_gradient(const Slice<T>& s, T* grad, float coef, const Tar
 }
 
 template <typename T>
-__device__ __forceinline__ T* gradient_row(const DistillArgs& a, long long r) {
-  const long long b = r / a.rows.k;
+__device__ __forceinline__ T* gradient_row(const DistillArgs& a, int r) {
+  const int b = r / a.rows.k;
   return static_cast<T*>(a.grad) + b * a.gstride_b + (r - b * a.rows.k) * a.gstride_n;
 }
 
@@ -190,7 +190,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_distill(DistillArgs a) {
   constexpr int E = ElemOf<T>::E;
   const unsigned ctas = cluster.num_blocks(), rank = cluster.block_rank();
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, warps = blockDim.x / 32;
-  const long long r = blockIdx.x / ctas;
+  const int r = (int)(blockIdx.x / ctas);
   const float weight = a.weight ? a.weight[r] : 1.0f;
   const T* logits = row_address<T>(a.rows, r);
   T* grad = a.grad ? gradient_row<T>(a, r) : nullptr;
@@ -289,7 +289,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_distill(DistillArgs a) {
 template <typename T>
 __global__ void __launch_bounds__(kRowThreads, 2) k_distill_backward(DistillArgs a, int parts) {
   __shared__ Targets t;
-  const long long r = blockIdx.x / parts;
+  const int r = (int)(blockIdx.x / (unsigned)parts);
   const float weight = a.weight ? a.weight[r] : 1.0f, lse = a.lse_in[r];
   const float coef = weight == 0.0f || lse == CUDART_INF_F ? 0.0f : weight * a.tau * a.up[r];
   T* grad = gradient_row<T>(a, r);

@@ -126,6 +126,14 @@ struct Parts2 {
 // floor(a q / 2^24) for a <= 2^24, without passing 64 bits
 __device__ __forceinline__ u64 share24(u64 a, u64 q) { return a * (q >> 24) + ((a * (q & 0xffffffu)) >> 24); }
 
+// *at += x where x is not 0, without a branch
+__device__ __forceinline__ void add_shared(uint32_t* at, uint32_t x) {
+  asm volatile("{.reg .pred p; setp.ne.u32 p, %1, 0; @p red.shared.add.u32 [%0], %1;}" ::"r"(
+                   (uint32_t)__cvta_generic_to_shared(at)),
+               "r"(x)
+               : "memory");
+}
+
 __device__ __forceinline__ u64 warp_sum(u64 x) {
   for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(~0u, x, o);
   return x;
@@ -170,7 +178,7 @@ struct Row {
   bool special;  // this warp's elements have NaN, or the row +inf or nothing
   static constexpr int E = ElemOf<T>::E;
 
-  __device__ Row(PickShared& shared) : sh(shared), parity(0) {}
+  __device__ explicit Row(PickShared& shared) : sh(shared), parity(0) {}
 
   // f(value, index) for the elements of this warp's chunks (and -inf past their end)
   template <typename F>
@@ -192,7 +200,7 @@ struct Row {
   // twice K of them.  About 1.4 K elements of a row in random order reach it; the lowest of the warps' j-th, which needs
   // no ranking, lets ten times K through at one lane maximum a warp.
   __device__ float top_of(float lane_top, int K, float* floor) {
-    const int warps = blockDim.x / 32, w = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int warps = (int)blockDim.x / 32, w = (int)threadIdx.x / 32, lane = (int)threadIdx.x % 32;
     const int all = warps * (int)group.n;
     const int j = K > 0 ? min((2 * K + all - 1) / all, 32) : 1;
     uint32_t key = value_key(lane_top);
@@ -212,15 +220,22 @@ struct Row {
       for (int i = lane; i < n; i += 32) m = max(m, *group.at(&sh.tops.mine[i % per], i / per));
       return key_value(__reduce_max_sync(~0u, m));
     }
-    for (int i = threadIdx.x; i < n; i += blockDim.x)
-      sh.tops.all[i] = *group.at(&sh.tops.mine[i % per], i / per);
-    __syncthreads();
-    for (int i = threadIdx.x; i < n; i += blockDim.x) {
-      const uint32_t x = sh.tops.all[i];
+    const uint32_t* tops = sh.tops.mine;
+    if (group.n > 1) {
+      for (int i = (int)threadIdx.x; i < n; i += (int)blockDim.x)
+        sh.tops.all[i] = *group.at(&sh.tops.mine[i % per], i / per);
+      __syncthreads();
+      tops = sh.tops.all;
+    }
+    for (int i = w; i < n; i += warps) {  // a warp finds a value's rank
+      const uint32_t x = tops[i];
       int above = 0;
-      for (int o = 0; o < n; ++o) above += sh.tops.all[o] > x || (sh.tops.all[o] == x && o < i);
-      if (above == 0) sh.row_top = x;
-      if (above == K - 1) sh.row_floor = x;
+      for (int o = lane; o < n + lane; o += 32) {
+        const uint32_t y = o < n ? tops[o] : 0;
+        above += __popc(__ballot_sync(~0u, y > x || (y == x && o < i)));
+      }
+      if (lane == 0 && above == 0) sh.row_top = x;
+      if (lane == 0 && above == K - 1) sh.row_floor = x;
     }
     __syncthreads();
     *floor = sh.row_floor ? key_value(sh.row_floor) : -CUDART_INF_F;
@@ -247,7 +262,7 @@ struct Row {
   __device__ void collect(float floor, float lane_top) {
     int* count = group.at(&sh.count, 0);
     u64* list = group.at(sh.list, 0);
-    const int lane = threadIdx.x % 32, w = threadIdx.x / 32, stride = (int)blockDim.x * 4;
+    const int lane = (int)threadIdx.x % 32, w = (int)threadIdx.x / 32, stride = (int)blockDim.x * 4;
     const int own = 4 * ((s.n - w * kBatch + stride - 1) / stride);  // a lane's chunks, with those past the end
     uint32_t who = __ballot_sync(~0u, lane_top >= floor && lane_top > -CUDART_INF_F);
     while (who) {
@@ -297,13 +312,18 @@ struct Row {
 
   // f(rank, key) for the list's keys, by one thread each
   template <typename F>
-  __device__ void ranked(F f) const {
+  __device__ __forceinline__ void ranked(F f) {
     const int n = sh.count;
-    for (int i = threadIdx.x; i < n; i += blockDim.x) {
+    if (n > 512) {
+      sort_list(n);
+      for (int i = (int)threadIdx.x; i < n; i += (int)blockDim.x) f(i, sh.list[i]);
+      return;
+    }
+    for (int i = (int)threadIdx.x / 32; i < n; i += (int)blockDim.x / 32) {  // a warp finds a key's rank
       const u64 key = sh.list[i];
       int at = 0;
-      for (int j = 0; j < n; ++j) at += sh.list[j] > key;
-      f(at, key);
+      for (int o = (int)threadIdx.x % 32; o < n + (int)threadIdx.x % 32; o += 32) at += __popc(__ballot_sync(~0u, o < n && sh.list[o] > key));
+      if (threadIdx.x % 32 == 0) f(at, key);
     }
   }
 
@@ -388,7 +408,7 @@ struct Row {
       atomicAdd(&sh.parts[(c / kBatch) >> shift], x);
   }
   __device__ __forceinline__ void clear_parts() {  // before a barrier, for add_part with a shift
-    for (int i = threadIdx.x; i < kParts; i += blockDim.x) sh.parts[i] = 0;
+    for (int i = (int)threadIdx.x; i < kParts; i += (int)blockDim.x) sh.parts[i] = 0;
     if (threadIdx.x == 0) sh.cta_q = 0;
   }
 
@@ -419,6 +439,58 @@ struct Row {
   }
 
   // ---- thresholds
+
+  // Elements from low to below high, and from the floor on, to the first CTA's list; with kKeep the masses of those from
+  // high on, from the floor on and of at least min_p, to the parts.  kFree: there is no floor.
+  template <bool kKeep, bool kFree>
+  __device__ __forceinline__ void collect_bin(const Weigher& weigh, Floor floor, float low, float high, float min_p) {
+    int* count = group.at(&sh.count, 0);
+    u64* list = group.at(sh.list, 0);
+    const int shift = part_shift(s.n);
+    u64 total = 0;
+    s.sweep([&](const uint4 (&v)[4], int c) {
+      ChunkMax<T, false> top;
+      top.add(v);
+      if (!__any_sync(~0u, top.value() >= low)) return;
+      LaneMass sum = {0, 0};
+      uint32_t in_bin = 0;  // a bit for each element
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float z[E];
+        unpack<T>(v[i], z);
+        const int i0 = s.first(c + 32 * i);
+#pragma unroll
+        for (int e = 0; e < E; e += 2) {
+          if (kKeep) {
+            const float2 y = weigh.exponents(z[e], z[e + 1]);
+            const float2 w = make_float2(exp2_32(y.x), exp2_32(y.y));
+            const Parts2 q(w);
+#pragma unroll
+            for (int o = 0; o < 2; ++o)
+              if (z[e + o] >= high && (o ? w.y : w.x) >= min_p && (kFree || floor.in(z[e + o], i0 + e + o))) {
+                sum.high += q.high[o] - kHighBits;
+                sum.low += q.low[o] - kOnesBits;
+              }
+          }
+#pragma unroll
+          for (int o = 0; o < 2; ++o)
+            if (z[e + o] >= low && z[e + o] < high) in_bin |= 1u << (E * i + e + o);
+        }
+      }
+      for (; in_bin; in_bin &= in_bin - 1) {
+        const int bit = __ffs(in_bin) - 1, index = s.first(c + 32 * (bit / E)) + bit % E;
+        const float z = s.at(index);
+        if (!kFree && !floor.in(z, index)) continue;
+        const int at = atomicAdd(count, 1);
+        if (at < kListMax) list[at] = order_key(z, index);
+      }
+      if (kKeep) {
+        __syncwarp();
+        add_part(sum, c, shift, total);
+      }
+    });
+    if (kKeep && threadIdx.x % 32 == 0 && total) atomicAdd(&sh.cta_q, total);
+  }
 
   // Bins go down the order, by exponent; past 2^-32 of the maximum the last one.
   __device__ __forceinline__ static int bin_of(float y) {
@@ -461,7 +533,7 @@ struct Row {
   template <bool kMass>
   __device__ __noinline__ void find_bin(u64 t, bool share) {
     static_assert(kGroups == 64, "two groups of bins a lane");
-    const int lane = threadIdx.x % 32;
+    const int lane = (int)threadIdx.x % 32;
     const unsigned ctas = group.n;
     u64 x0 = 0, x1 = 0;
     for (unsigned r = 0; r < ctas; ++r) {
@@ -495,11 +567,11 @@ struct Row {
   __device__ __noinline__ void sort_list(int n) {
     int size = 2;
     while (size < n) size *= 2;
-    for (int i = n + threadIdx.x; i < size; i += blockDim.x) sh.list[i] = 0;
+    for (int i = n + (int)threadIdx.x; i < size; i += (int)blockDim.x) sh.list[i] = 0;
     for (int k = 2; k <= size; k *= 2)
       for (int d = k / 2; d; d /= 2) {
         __syncthreads();
-        for (int t = threadIdx.x; t < size / 2; t += blockDim.x) {
+        for (int t = (int)threadIdx.x; t < size / 2; t += (int)blockDim.x) {
           const int i = 2 * t - (t & (d - 1));
           const u64 a = sh.list[i], b = sh.list[i + d];
           if ((a < b) == ((i & k) == 0)) {
@@ -520,9 +592,8 @@ struct Row {
   // as masses() leaves them, a cluster barrier included.
   template <bool kMass>
   __device__ __noinline__ u64 select(const Weigher& weigh, Floor floor, u64 arg, float min_p) {
-    const int lane = threadIdx.x % 32, warps = blockDim.x / 32, warp = threadIdx.x / 32;
+    const int lane = (int)threadIdx.x % 32, warps = (int)blockDim.x / 32, warp = (int)threadIdx.x / 32;
     int* count = group.at(&sh.count, 0);
-    u64* list = group.at(sh.list, 0);
     const bool keep = min_p >= 0.0f, free = floor.z == -CUDART_INF_F;
     const bool fits = (long long)per_cta * E <= kSliceElems && weigh.m < CUDART_INF_F;
     u64 t = arg;
@@ -530,7 +601,7 @@ struct Row {
     int n = kListMax + 1;
     for (int level = 0; level < 2 && fits; ++level) {
       // the cluster's CTAs have left the memory of the bins and the count behind: a barrier is above
-      for (int i = threadIdx.x; i < kBins; i += blockDim.x) sh.bins.low[i] = sh.bins.high[i] = 0;
+      for (int i = (int)threadIdx.x; i < kBins; i += (int)blockDim.x) sh.bins.low[i] = sh.bins.high[i] = 0;
       if (threadIdx.x == 0) sh.count = 0;
       __syncthreads();
       if (kMass && level == 0 && !special) {
@@ -551,8 +622,8 @@ struct Row {
                 const uint32_t high = q.high[o] - kHighBits, low = q.low[o] - kOnesBits;
                 const uint32_t bin = __float_as_uint(o ? b.y : b.x) - kOnesBits;
                 const bool in = free || floor.in(z[e + o], i0 + e + o);
-                if (in && low) atomicAdd(&sh.bins.low[bin], low);
-                if (in && high) atomicAdd(&sh.bins.high[bin], high);
+                add_shared(&sh.bins.low[bin], in ? low : 0);
+                add_shared(&sh.bins.high[bin], in ? high : 0);
               }
             }
           }
@@ -603,32 +674,16 @@ struct Row {
       const float low = sh.bin_low, high = sh.bin_high;
       t = sh.before;
       // the bin's elements, from low to below high, to the list; the mass of what is above to the parts
-      const Floor above = Floor{high, 0x7fffffff};
-      const Kept sure{above.z > floor.z ? above : floor, fmaxf(min_p, 0.0f)};
-      const int shift = part_shift(s.n);
-      u64 total = 0;
       if (keep) clear_parts();
       __syncthreads();
-      s.sweep([&](const uint4 (&v)[4], int c) {
-        ChunkMax<T, false> top;
-        top.add(v);
-        const float m = top.value();
-        if (m >= low) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            float z[E];
-            unpack<T>(v[i], z);
-#pragma unroll
-            for (int e = 0; e < E; ++e)
-              if (z[e] >= low && z[e] < high && floor.in(z[e], s.first(c + 32 * i) + e)) {
-                const int at = atomicAdd(count, 1);
-                if (at < kListMax) list[at] = order_key(z[e], s.first(c + 32 * i) + e);
-              }
-          }
-        }
-        if (keep && __any_sync(~0u, m >= high)) add_part(batch_mass<false>(v, c, weigh, sure), c, shift, total);
-      });
-      if (keep && lane == 0 && total) atomicAdd(&sh.cta_q, total);
+      if (keep) {
+        if (free)
+          collect_bin<true, true>(weigh, floor, low, high, min_p);
+        else
+          collect_bin<true, false>(weigh, floor, low, high, min_p);
+      } else {
+        collect_bin<false, false>(weigh, floor, low, high, min_p);
+      }
       group.sync();
       n = *count;
       if (n <= kListMax) break;
@@ -661,7 +716,7 @@ struct Row {
       }
       __syncthreads();
       if (keep)
-        for (int i = threadIdx.x; i <= sh.last; i += blockDim.x) {
+        for (int i = (int)threadIdx.x; i <= sh.last; i += (int)blockDim.x) {
           const u64 key = sh.list[i];
           const float w = weigh(order_value(key));
           if (!(w >= min_p)) continue;
@@ -695,7 +750,7 @@ struct Row {
         continue;
       }
       u64* hist = sh.radix[parity];
-      for (int i = threadIdx.x; i < 256; i += blockDim.x) hist[i] = 0;
+      for (int i = (int)threadIdx.x; i < 256; i += (int)blockDim.x) hist[i] = 0;
       __syncthreads();
       each([&](float z, int i) {
         const u64 key = order_key(z, i);
@@ -712,7 +767,7 @@ struct Row {
         for (int i = 0; i < 8; ++i) {
           b[i] = 0;
           for (unsigned r = 0; r < group.n; ++r)
-            b[i] += *group.at(&hist[255 - 8 * threadIdx.x - i], r);
+            b[i] += *group.at(&hist[255 - 8 * (int)threadIdx.x - i], r);
           sum += b[i];
         }
         const u64 upto = before + warp_scan(sum);
@@ -722,7 +777,7 @@ struct Row {
           u64 at = upto - sum;
           int i = 0;
           while (at + b[i] <= t) at += b[i++];
-          sh.found = prefix | (u64)(255 - 8 * threadIdx.x - i) << shift;
+          sh.found = prefix | (u64)(255 - 8 * (int)threadIdx.x - i) << shift;
           sh.before = at;
         }
         if (!all && threadIdx.x == 0) sh.found = ~0ull;
@@ -742,48 +797,53 @@ struct Row {
   // one warp: the token of the slice whose kept mass covers t (counted from the slice's start)
   __device__ __noinline__ void draw(u64 t, const Weigher& weigh, const Kept& kept, u64 all, int32_t* tok,
                                     float* prob) const {
-    const int lane = threadIdx.x % 32;
-    int p = 0;  // the part
-    for (int p0 = 0;; p0 += 32) {
-      const u64 part = sh.parts[p0 + lane], upto = warp_scan(part), sum = __shfl_sync(~0u, upto, 31);
-      if (t >= sum && p0 + 32 < kParts) {
-        t -= sum;
-        continue;
-      }
-      const int l = min(__popc(__ballot_sync(~0u, upto <= t)), 31);
-      p = p0 + l;
-      t -= __shfl_sync(~0u, upto - part, l);
-      break;
-    }
-    for (int c0 = (p << part_shift(s.n)) * kBatch; c0 < s.n; c0 += 32) {
-      const int c = c0 + lane;
-      const uint4 v = s.chunk(c);
-      const u64 q = chunk_mass(v, c, weigh, kept);
-      const u64 upto = warp_scan(q);
-      const u64 total = __shfl_sync(~0u, upto, 31);
-      if (t >= total) {
-        t -= total;
-        continue;
-      }
-      if (t >= upto - q && t < upto) {
-        t -= upto - q;
+    const int lane = (int)threadIdx.x % 32, shift = part_shift(s.n);
+    const int parts = ((s.n + kBatch - 1) / kBatch + (1 << shift) - 1) >> shift, per = (parts + 31) / 32;
+    u64 sum = 0;
+    for (int i = 0; i < per; ++i) sum += sh.parts[min(lane * per + i, kParts - 1)];  // past the last all are 0
+    u64 upto = warp_scan(sum);
+    const int l = min(__popc(__ballot_sync(~0u, upto <= t)), 31);
+    t -= __shfl_sync(~0u, upto - sum, l);
+    int p = l * per;
+    while (p < l * per + per - 1 && t >= sh.parts[p]) t -= sh.parts[p++];
+    for (int c0 = (p << shift) * kBatch + lane; c0 - lane < s.n; c0 += kBatch) {
+      uint4 v[4];
+      u64 q[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = s.chunk(c0 + 32 * i);
+      bool found = false;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        q[i] = chunk_mass(v[i], c0 + 32 * i, weigh, kept);
+        const u64 all32 = __reduce_add_sync(~0u, (uint32_t)q[i] & 0xffffffu) +
+                          ((u64)__reduce_add_sync(~0u, (uint32_t)(q[i] >> 24)) << 24);
+        if (found) continue;
+        if (t >= all32) {
+          t -= all32;
+          continue;
+        }
+        found = true;
+        upto = warp_scan(q[i]);
+        if (t < upto - q[i] || t >= upto) continue;
+        t -= upto - q[i];
         float z[E];
-        unpack<T>(v, z);
+        unpack<T>(v[i], z);
+        const int i0 = s.first(c0 + 32 * i);
         float hit = 0.0f;
         int at = -1;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-          const uint32_t x = kept_mass(z[e], s.first(c) + e, weigh, kept);
+          const uint32_t x = kept_mass(z[e], i0 + e, weigh, kept);
           if (at < 0 && t < x) {
             at = e;
             hit = z[e];
           }
           t -= at < 0 ? x : 0;
         }
-        *tok = s.first(c) + at;
+        *tok = i0 + at;
         *prob = weigh(hit) * kGrid / (float)all;
       }
-      break;
+      if (found) break;
     }
   }
 
@@ -799,7 +859,7 @@ struct Row {
       }
     });
     __syncthreads();
-    for (int i = threadIdx.x; i < n; i += blockDim.x) {
+    for (int i = (int)threadIdx.x; i < n; i += (int)blockDim.x) {
       u64 before = 0, all = 0;
       for (int j = 0; j < n; ++j) {
         all += l.q[j];
@@ -810,7 +870,7 @@ struct Row {
     __syncthreads();
     u64 all = 0;
     for (int j = 0; j < n; ++j) all += l.kept[j];
-    for (int i = threadIdx.x; i < n; i += blockDim.x) {
+    for (int i = (int)threadIdx.x; i < n; i += (int)blockDim.x) {
       const int index = order_index(l.key[i]);
       u64 first = 0;
       for (int j = 0; j < n; ++j)
@@ -818,7 +878,7 @@ struct Row {
       l.first[i] = first;
     }
     __syncthreads();
-    for (int d = threadIdx.x; d < S; d += blockDim.x) {
+    for (int d = (int)threadIdx.x; d < S; d += (int)blockDim.x) {
       const float x = u[d];
       int token = -1;
       float p = 0.0f;
@@ -835,143 +895,208 @@ struct Row {
   }
 };
 
-template <typename T>
-__global__ void __launch_bounds__(kRowThreads, 3) k_propose(PickArgs a) {
-  __shared__ PickShared sh;
-  Row<T> row(sh);
-  constexpr int E = ElemOf<T>::E;
-  const unsigned ctas = row.group.n, rank = row.group.rank;
-  const long long r = blockIdx.x / ctas;
-  const float T_ = a.temperature ? a.temperature[r / a.rows.k] : 1.0f;
-  row.s.open(T_ >= 0.0f ? row_address<T>(a.rows, r) : nullptr, a.rows, rank, sh.ends);
-  Weigher weigh;
-  weigh.c = fminf(__fdiv_rn(kLog2e, T_), CUDART_MAX_NORMAL_F);
-  // one pass: each lane's maximum so far and the sum of its weights relative to it
-  float top = -CUDART_INF_F;
-  float2 sums = make_float2(0.0f, 0.0f);
-  row.s.sweep([&](const uint4 (&v)[4], int) {
-    ChunkMax<T, false> batch;
-    batch.add(v);
-    const float x = batch.value();
-    if (x > top) {
-      const float by = exp2_32((top - x) * weigh.c);
-      sums.x *= by;
-      sums.y *= by;
-      top = x;
-    }
-    if (top == -CUDART_INF_F) return;
-    const Weigher relative{top, weigh.c};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float z[E];
-      unpack<T>(v[i], z);
-#pragma unroll
-      for (int e = 0; e < E; e += 2) {
-        const float2 y = relative.exponents(z[e], z[e + 1]);
-        sums = add2(sums, make_float2(exp2_32(y.x), exp2_32(y.y)));
-      }
-    }
-  });
-  float floor;
-  weigh.m = row.top_of(top, a.K, &floor);
-  row.collect(floor, top);
-  float sum = sums.x + sums.y;
-  if (__any_sync(~0u, sum != sum) || weigh.m == CUDART_INF_F) {  // NaN or +inf among the warp's elements or the row's
-    sum = 0.0f;
-    row.each([&](float z, int) {
-      const float w = weigh(z);
-      sum += w > 0.0f ? w : 0.0f;
-    });
-  } else {
-    sum = top == -CUDART_INF_F ? 0.0f : sum * exp2_32((top - weigh.m) * weigh.c);
-  }
-  for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
-  const int warps = blockDim.x / 32;
-  if (threadIdx.x % 32 == 0) *row.group.at(&sh.sums[rank * warps + threadIdx.x / 32], 0) = sum;
-  row.group.sync();
-  row.settle(a.K);
-  if (rank != 0) return;
-  sum = 0.0f;
-  for (unsigned i = 0; i < ctas * warps; ++i) sum += sh.sums[i];
-  int32_t* cand = a.cand + r * a.K;
-  float* conf = a.conf + r * a.K;
-  for (int i = sh.count + threadIdx.x; i < a.K; i += blockDim.x) {
-    cand[i] = -1;
-    conf[i] = 0.0f;
-  }
-  row.ranked([&](int at, u64 key) {
-    if (at >= a.K) return;
-    cand[at] = order_index(key);
-    conf[at] = T_ == 0.0f ? (at == 0 ? 1.0f : 0.0f) : weigh(order_value(key)) / sum;
-  });
-  if (ctas > 1) row.group.sync();  // the others have looked at the count
-}
+// What the pass from memory finds of a row: each lane's maximum, and for the confidences each warp's maximum and the sum
+// of its weights relative to it.
+struct Found {
+  float top[kRowThreads];
+  float warp_top[kRowWarps], warp_sum[kRowWarps];
+  bool special[kRowWarps];
+};
+
+// ---- the K best
 
 template <typename T>
-__global__ void __launch_bounds__(kRowThreads, 2) k_sample(PickArgs a) {
-  __shared__ PickShared sh;
-  Row<T> row(sh);
-  const unsigned ctas = row.group.n, rank = row.group.rank;
-  const long long r = blockIdx.x / ctas, b = r / a.rows.k;
-  const float T_ = a.temperature ? a.temperature[b] : 1.0f;
-  float top_p = a.top_p ? a.top_p[b] : 1.0f;
-  const float min_p = a.min_p ? a.min_p[b] : 0.0f;
-  int top_k = a.top_k ? a.top_k[b] : 0;
-  const bool good = T_ >= 0.0f && top_p == top_p && min_p == min_p;
-  top_p = fminf(fmaxf(top_p, 0.0f), 1.0f);
-  const u64 p24 = __float2uint_rn(top_p * 16777216.0f);
-  if (T_ == 0.0f || p24 == 0 || min_p > 1.0f) top_k = 1;
-  if (top_k <= 0 || top_k > a.rows.V) top_k = a.rows.V;
-  const bool by_list = top_k <= kMaxK;
-  row.per_cta = a.rows.per;
-  row.s.open(good ? row_address<T>(a.rows, r) : nullptr, a.rows, rank, sh.ends);
-  const float lane_top = row.lane_maximum();
-  Weigher weigh;
-  float floor;
-  weigh.m = row.top_of(lane_top, by_list ? top_k : 0, &floor);
-  weigh.c = fminf(__fdiv_rn(kLog2e, T_), CUDART_MAX_NORMAL_F);
-  if (by_list) {
-    row.collect(floor, lane_top);
-    row.group.sync();
-    row.settle(top_k);
-    if (rank != 0) return;
-    row.draw_from_list(weigh, top_k, p24, min_p, a.u + r * a.S, a.S, a.tok + r * a.S, a.prob + r * a.S);
-    if (ctas > 1) row.group.sync();  // the others have looked at the count
-    return;
+struct Propose {
+  typedef PickArgs Args;
+  const Args& a;
+  __device__ explicit Propose(const Args& args) : a(args) {}
+  __device__ __forceinline__ float temperature(int r) const {
+    return a.temperature ? a.temperature[r / a.rows.k] : 1.0f;
   }
-  const bool by_mass = p24 < (1u << 24);
-  row.special |= fabsf(weigh.m) == CUDART_INF_F;
-  Kept kept{no_floor(), fmaxf(min_p, 0.0f)};
-  if (top_k < a.rows.V)
-    kept.floor = floor_of(row.template select<false>(weigh, kept.floor, top_k - 1, by_mass ? -1.0f : kept.min_p));
-  if (by_mass) kept.floor = floor_of(row.template select<true>(weigh, kept.floor, p24, kept.min_p));
-  if (top_k == a.rows.V && !by_mass) {
-    row.masses(weigh, kept);
-    row.group.sync();
+  // A row of a temperature that is none is read like others, and answered with nothing.
+  __device__ __forceinline__ static float scale(float t) {
+    return t >= 0.0f ? fminf(__fdiv_rn(kLog2e, t), CUDART_MAX_NORMAL_F) : 1.0f;
   }
-  u64 mine, ahead;
-  const u64 all = row.all_mass(&mine, &ahead);
-  for (int i = threadIdx.x / 32; i < a.S; i += blockDim.x / 32) {
-    const long long o = r * a.S + i;
-    const float u = a.u[o];
-    if (all == 0 || !(u >= 0.0f && u <= 1.0f)) {
-      if (rank == 0 && threadIdx.x % 32 == 0) {
-        a.tok[o] = -1;
-        a.prob[o] = 0.0f;
-      }
-      continue;
+
+  // one pass: each lane's maximum so far and the sum of its weights relative to it
+  __device__ __forceinline__ void pass(Row<T>& row, int r, Found& found) const {
+    constexpr int E = ElemOf<T>::E;
+    const float c = scale(temperature(r));
+    float top = -CUDART_INF_F;
+    float2 sums = make_float2(0.0f, 0.0f);
+    row.s.sweep(
+        [&](const uint4 (&v)[4], int) {
+          ChunkMax<T, false> batch;
+          batch.add(v);
+          const float x = batch.value();
+          if (x > top) {
+            const float by = exp2_32((top - x) * c);
+            sums.x *= by;
+            sums.y *= by;
+            top = x;
+          }
+          if (top == -CUDART_INF_F) return;
+          const Weigher relative{top, c};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float z[E];
+            unpack<T>(v[i], z);
+#pragma unroll
+            for (int e = 0; e < E; e += 2) {
+              const float2 y = relative.exponents(z[e], z[e + 1]);
+              sums = add2(sums, make_float2(exp2_32(y.x), exp2_32(y.y)));
+            }
+          }
+        });
+    float m = top;
+    for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, o));
+    float sum = top == -CUDART_INF_F ? 0.0f : (sums.x + sums.y) * exp2_32((top - m) * c);
+    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
+    found.top[threadIdx.x] = top;
+    if (threadIdx.x % 32 == 0) {
+      found.warp_top[threadIdx.x / 32] = m;
+      found.warp_sum[threadIdx.x / 32] = sum;
     }
-    const u64 t = min(share24((u64)(u * 16777216.0f), all), all - 1);
-    if (t >= ahead && t < ahead + mine) row.draw(t - ahead, weigh, kept, all, &a.tok[o], &a.prob[o]);
   }
-  if (ctas > 1) row.group.sync();  // no CTA leaves while its masses are read
+
+  __device__ __forceinline__ void finish(Row<T>& row, int r, const Found& found) const {
+    const int lane = (int)threadIdx.x % 32, warps = (int)blockDim.x / 32;
+    const float temp = temperature(r), top = found.top[threadIdx.x];
+    Weigher weigh;
+    weigh.c = scale(temp);
+    float floor;
+    weigh.m = row.top_of(top, a.K, &floor);
+    row.collect(floor, top);
+    float sum = found.warp_sum[threadIdx.x / 32], m = found.warp_top[threadIdx.x / 32];
+    if (sum != sum || weigh.m == CUDART_INF_F) {  // NaN or +inf among the warp's elements or the row's
+      sum = 0.0f;
+      row.each([&](float z, int) {
+        const float w = weigh(z);
+        sum += w > 0.0f ? w : 0.0f;
+      });
+      for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
+    } else {
+      sum = m == -CUDART_INF_F ? 0.0f : sum * exp2_32((m - weigh.m) * weigh.c);
+    }
+    if (lane == 0) *row.group.at(&row.sh.sums[row.group.rank * warps + (int)threadIdx.x / 32], 0) = sum;
+    row.group.sync();
+    row.settle(a.K);
+    if (row.group.rank != 0) return;
+    sum = 0.0f;
+    for (int i = 0; i < (int)row.group.n * warps; ++i) sum += row.sh.sums[i];
+    int32_t* cand = a.cand + (long long)r * a.K;
+    float* conf = a.conf + (long long)r * a.K;
+    const bool good = temp >= 0.0f;
+    for (int i = (int)threadIdx.x; i < a.K; i += (int)blockDim.x)
+      if (!good || i >= row.sh.count) {
+        cand[i] = -1;
+        conf[i] = 0.0f;
+      }
+    if (good)
+      row.ranked([&](int at, u64 key) {
+        if (at >= a.K) return;
+        cand[at] = order_index(key);
+        conf[at] = temp == 0.0f ? (at == 0 ? 1.0f : 0.0f) : weigh(order_value(key)) / sum;
+      });
+    if (row.group.n > 1) row.group.sync();  // the others have looked at the count
+  }
+};
+
+// ---- draws
+
+template <typename T>
+struct Sample {
+  typedef PickArgs Args;
+  const Args& a;
+  __device__ explicit Sample(const Args& args) : a(args) {}
+
+  __device__ __forceinline__ void pass(Row<T>& row, int, Found& found) const {
+    found.top[threadIdx.x] = row.lane_maximum();
+    if (threadIdx.x % 32 == 0) found.special[threadIdx.x / 32] = row.special;
+  }
+
+  __device__ __forceinline__ void finish(Row<T>& row, int r, const Found& found) const {
+    const int lane = (int)threadIdx.x % 32;
+    const int b = r / a.rows.k;
+    float temp = a.temperature ? a.temperature[b] : 1.0f;
+    float top_p = a.top_p ? a.top_p[b] : 1.0f;
+    const float min_p = a.min_p ? a.min_p[b] : 0.0f;
+    int top_k = a.top_k ? a.top_k[b] : 0;
+    const bool good = temp >= 0.0f && top_p == top_p && min_p == min_p;
+    top_p = fminf(fmaxf(top_p, 0.0f), 1.0f);
+    const u64 p24 = __float2uint_rn(top_p * 16777216.0f);
+    if (temp == 0.0f || p24 == 0 || min_p > 1.0f || !good) top_k = 1;
+    if (top_k <= 0 || top_k > a.rows.V) top_k = a.rows.V;
+    const bool by_list = top_k <= kMaxK;
+    const float* u = a.u + (long long)r * a.S;
+    int32_t* tok = a.tok + (long long)r * a.S;
+    float* prob = a.prob + (long long)r * a.S;
+    Weigher weigh;
+    float floor;
+    weigh.m = row.top_of(found.top[threadIdx.x], by_list ? top_k : 0, &floor);
+    weigh.c = good ? fminf(__fdiv_rn(kLog2e, temp), CUDART_MAX_NORMAL_F) : 1.0f;
+    if (by_list) {
+      row.collect(floor, found.top[threadIdx.x]);
+      row.group.sync();
+      row.settle(top_k);
+      if (row.group.rank != 0) return;
+      row.draw_from_list(weigh, good ? top_k : 0, p24, min_p, u, a.S, tok, prob);
+      if (row.group.n > 1) row.group.sync();  // the others have looked at the count
+      return;
+    }
+    row.special = found.special[threadIdx.x / 32] || fabsf(weigh.m) == CUDART_INF_F;
+    const bool by_mass = p24 < (1u << 24);
+    Kept kept{no_floor(), fmaxf(min_p, 0.0f)};
+    if (top_k < a.rows.V)
+      kept.floor = floor_of(row.template select<false>(weigh, kept.floor, top_k - 1, by_mass ? -1.0f : kept.min_p));
+    if (by_mass) kept.floor = floor_of(row.template select<true>(weigh, kept.floor, p24, kept.min_p));
+    if (top_k == a.rows.V && !by_mass) {
+      row.masses(weigh, kept);
+      row.group.sync();
+    }
+    u64 mine, ahead;
+    const u64 all = row.all_mass(&mine, &ahead);
+    for (int i = (int)threadIdx.x / 32; i < a.S; i += (int)blockDim.x / 32) {
+      const float x = u[i];
+      if (all == 0 || !(x >= 0.0f && x <= 1.0f)) {
+        if (row.group.rank == 0 && lane == 0) {
+          tok[i] = -1;
+          prob[i] = 0.0f;
+        }
+        continue;
+      }
+      const u64 t = min(share24((u64)(x * 16777216.0f), all), all - 1);
+      if (t >= ahead && t < ahead + mine) row.draw(t - ahead, weigh, kept, all, &tok[i], &prob[i]);
+    }
+    if (row.group.n > 1) row.group.sync();  // no CTA leaves while its masses are read
+  }
+};
+
+// a cluster of CTAs for each row
+template <typename T, template <typename> class Op, int kPerSm>
+__global__ void __launch_bounds__(kRowThreads, kPerSm) k_rows(PickArgs a) {
+  __shared__ PickShared sh;
+  __shared__ Found found;
+  Row<T> row(sh);
+  row.per_cta = a.rows.per;
+  const int r = (int)(blockIdx.x / row.group.n);
+  row.s.open(row_address<T>(a.rows, r), a.rows, row.group.rank, sh.ends);
+  const Op<T> op(a);
+  op.pass(row, r, found);
+  __syncwarp();
+  op.finish(row, r, found);
+}
+
+template <typename T, template <typename> class Op, int kPerSm>
+epic_status launch(PickArgs& a, long long rows, cudaStream_t st) {
+  const RowShape p = row_shape(rows, a.rows.V, sizeof(T));
+  a.rows.per = p.per;
+  return launch_rows((const void*)k_rows<T, Op, kPerSm>, p, rows, &a, st);
 }
 
 template <typename T>
 epic_status launch(PickArgs& a, long long rows, bool sample, cudaStream_t st) {
-  const RowShape p = row_shape(rows, a.rows.V, sizeof(T));
-  a.rows.per = p.per;
-  return launch_rows(sample ? (const void*)k_sample<T> : (const void*)k_propose<T>, p, rows, &a, st);
+  return sample ? launch<T, Sample, 2>(a, rows, st) : launch<T, Propose, 3>(a, rows, st);
 }
 
 epic_status by_type(int dtype, PickArgs& a, long long rows, bool sample, void* stream) {

@@ -149,6 +149,36 @@ def test_propose_temperatures_and_positions(cuda):
         np.testing.assert_allclose(conf.cpu().numpy(), want_conf, rtol=RTOL, atol=1e-30)
 
 
+# Rows enough for every place on the GPU: a CTA takes several in a pipeline.
+MANY = [  # B, n, V, dtype, kind, pad, shift
+    (62, 5, 16411, 'bf16', 'normal', 0, 1),
+    (62, 5, 16411, 'f16', 'specials', 3, 0),
+    (103, 7, 8209, 'f32', 'specials', 0, 1),
+    (64, 5, 16384, 'bf16', 'ties', 0, 0),
+    (41, 8, 32771, 'bf16', 'peaked', 5, 0),
+]
+
+
+@pytest.mark.parametrize('B,n,V,dtype,kind,pad,shift', MANY)
+def test_propose_many_rows(cuda, B, n, V, dtype, kind, pad, shift):
+    import torch
+    import paper_2606_00722_gb300 as epic
+    logits = make_logits(B, n, V, dtype, kind, V, pad, shift)
+    K = 12
+    g = torch.Generator().manual_seed(V)
+    pos = torch.stack([torch.randperm(n, generator=g) for _ in range(B)]).to(torch.int32)
+    pos[3, 0], pos[B - 1, n - 1] = -1, n  # rows of nothing among the others
+    pos = pos.cuda()
+    T = torch.tensor([(0.7, 1.0, 1.9, 0.0, -1.0)[b % 5] for b in range(B)], device='cuda')
+    for _ in range(2):
+        cand = torch.full((B, n, K), -7, dtype=torch.int32, device='cuda')
+        conf = torch.full((B, n, K), -7.0, device='cuda')
+        epic.propose_topk(logits, cand, conf, pos=pos, temperature=T)
+        want_cand, want_conf = propose64(rows64(logits, pos), T.double().tolist(), K)
+        assert np.array_equal(cand.cpu().numpy(), want_cand)
+        np.testing.assert_allclose(conf.cpu().numpy(), want_conf, rtol=RTOL, atol=1e-30)
+
+
 # ---------------------------------------------------------------- draws
 
 def share(a, q):
@@ -163,7 +193,8 @@ def sample_whole(z, T, top_k, top_p, min_p, u):
     z = torch.where(torch.isnan(z), -math.inf, z)
     T, top_k, top_p, min_p = (x[:, None, None] for x in (T, top_k, top_p, min_p))
     m = z.amax(-1, keepdim=True)
-    c = torch.clamp(1.4426950408889634 / T, max=3.4028234663852886e38)
+    # a division: a number over a tensor would be torch's reciprocal times the number, with one more rounding
+    c = torch.clamp(torch.full_like(T, 1.4426950408889634) / T, max=3.4028234663852886e38)
     w = torch.exp2((z - m) * c)
     w = torch.where(m == math.inf, (z == m).float(), w)
     w = torch.where(z > -math.inf, w, 0.0)
@@ -244,6 +275,16 @@ SAMPLES = [  # B, n, V, S, dtype, kind, pad, shift
 def test_sample_is_the_definition(cuda, B, n, V, S, dtype, kind, pad, shift, rules):
     logits = make_logits(B, n, V, dtype, kind, V + S, pad, shift)
     tok, prob, u, r = run_sample(logits, RULES[rules], S)
+    want_tok, want_prob, _ = sample_whole(logits.float(), *r, u)
+    assert np.array_equal(tok.cpu().numpy(), want_tok.cpu().numpy())
+    np.testing.assert_allclose(prob.cpu().numpy(), want_prob.cpu().numpy(), rtol=2.0 ** -21, atol=0)
+
+
+@pytest.mark.parametrize('rules', ['temperature', 'large all', 'mixed'])
+@pytest.mark.parametrize('B,n,V,dtype,kind,pad,shift', MANY)
+def test_sample_many_rows(cuda, B, n, V, dtype, kind, pad, shift, rules):
+    logits = make_logits(B, n, V, dtype, kind, V + 1, pad, shift)
+    tok, prob, u, r = run_sample(logits, RULES[rules], 5)
     want_tok, want_prob, _ = sample_whole(logits.float(), *r, u)
     assert np.array_equal(tok.cpu().numpy(), want_tok.cpu().numpy())
     np.testing.assert_allclose(prob.cpu().numpy(), want_prob.cpu().numpy(), rtol=2.0 ** -21, atol=0)
