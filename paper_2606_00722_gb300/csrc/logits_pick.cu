@@ -91,6 +91,12 @@ struct PickShared {
   int count;
 };
 
+// The kernels' shared memory, by name: through a reference kept in an object its loads would be generic ones.
+__device__ __forceinline__ PickShared& shared() {
+  __shared__ PickShared sh;
+  return sh;
+}
+
 // 2^((z - m) c); a row whose maximum is +inf has weight 1 on its +inf elements and 0 elsewhere
 struct Weigher {
   float m, c;
@@ -168,17 +174,33 @@ struct Kept {
   __device__ __forceinline__ bool all() const { return floor.z == -CUDART_INF_F && !(min_p > 0.0f); }
 };
 
+// Of a lane's batches, the largest maximum and that batch's first chunk, and the second largest maximum.
+struct LaneTop {
+  float first, second;
+  int at;
+  __device__ LaneTop() {
+    first = second = -CUDART_INF_F;
+    at = 0;
+  }
+  __device__ __forceinline__ void add(float x, int c) {
+    if (x > first) {
+      second = first;
+      first = x;
+      at = c;
+    } else {
+      second = fmaxf(second, x);
+    }
+  }
+};
+
 template <typename T>
 struct Row {
   Slice<T> s;
-  const RowGroup group;
-  PickShared& sh;
-  int parity;
+  RowGroup group;
   int per_cta;   // chunks
   bool special;  // this warp's elements have NaN, or the row +inf or nothing
   static constexpr int E = ElemOf<T>::E;
 
-  __device__ explicit Row(PickShared& shared) : sh(shared), parity(0) {}
 
   // f(value, index) for the elements of this warp's chunks (and -inf past their end)
   template <typename F>
@@ -206,26 +228,26 @@ struct Row {
     uint32_t key = value_key(lane_top);
     for (int i = 0; i < j; ++i) {
       const uint32_t x = __reduce_max_sync(~0u, key);
-      if (lane == 0) sh.tops.mine[w * j + i] = x;
+      if (lane == 0) shared().tops.mine[w * j + i] = x;
       if (__ffs(__ballot_sync(~0u, key == x)) - 1 == lane) key = 0;
     }
     if (threadIdx.x == 0) {
-      sh.count = 0;
-      sh.row_floor = 0;
+      shared().count = 0;
+      shared().row_floor = 0;
     }
     group.sync();
     const int n = all * j, per = warps * j;
     if (K == 0) {  // every warp looks at all warps of the row
       uint32_t m = 0;
-      for (int i = lane; i < n; i += 32) m = max(m, *group.at(&sh.tops.mine[i % per], i / per));
+      for (int i = lane; i < n; i += 32) m = max(m, *group.at(&shared().tops.mine[i % per], i / per));
       return key_value(__reduce_max_sync(~0u, m));
     }
-    const uint32_t* tops = sh.tops.mine;
+    const uint32_t* tops = shared().tops.mine;
     if (group.n > 1) {
       for (int i = (int)threadIdx.x; i < n; i += (int)blockDim.x)
-        sh.tops.all[i] = *group.at(&sh.tops.mine[i % per], i / per);
+        shared().tops.all[i] = *group.at(&shared().tops.mine[i % per], i / per);
       __syncthreads();
-      tops = sh.tops.all;
+      tops = shared().tops.all;
     }
     for (int i = w; i < n; i += warps) {  // a warp finds a value's rank
       const uint32_t x = tops[i];
@@ -234,76 +256,85 @@ struct Row {
         const uint32_t y = o < n ? tops[o] : 0;
         above += __popc(__ballot_sync(~0u, y > x || (y == x && o < i)));
       }
-      if (lane == 0 && above == 0) sh.row_top = x;
-      if (lane == 0 && above == K - 1) sh.row_floor = x;
+      if (lane == 0 && above == 0) shared().row_top = x;
+      if (lane == 0 && above == K - 1) shared().row_floor = x;
     }
     __syncthreads();
-    *floor = sh.row_floor ? key_value(sh.row_floor) : -CUDART_INF_F;
-    return key_value(sh.row_top);
+    *floor = shared().row_floor ? key_value(shared().row_floor) : -CUDART_INF_F;
+    return key_value(shared().row_top);
   }
 
-  // this lane's maximum, NaN left out; `special` tells of NaN
-  __device__ float lane_maximum() {
-    ChunkMax<T, true> top;
-    s.sweep([&](const uint4 (&v)[4], int) { top.add(v); });
-    float m = top.value();
-    special = __any_sync(~0u, m != m);
-    if (special) {
-      ChunkMax<T, false> numbers;
-      s.sweep([&](const uint4 (&v)[4], int) { numbers.add(v); });
-      m = numbers.value();
-      if (m != m) m = -CUDART_INF_F;
-    }
-    return m;
+  // the maxima of this lane's batches, NaN left out; `special` tells of NaN
+  __device__ __forceinline__ LaneTop lane_top() {
+    LaneTop top;
+    bool nan = false;
+    s.sweep([&](const uint4 (&v)[4], int c) {
+      ChunkMax<T, true> batch;
+      batch.add(v);
+      float x = batch.value();
+      if (x != x) {
+        nan = true;
+        ChunkMax<T, false> numbers;
+        numbers.add(v);
+        x = numbers.value();
+      }
+      top.add(x, c);
+    });
+    special = __any_sync(~0u, nan);
+    return top;
   }
 
   // Keys of elements >= floor to the first CTA's list (past its end they are only counted).  A lane whose maximum
-  // reaches the floor has such elements; its chunks are looked at by the whole warp, those of four lanes at a time.
-  __device__ void collect(float floor, float lane_top) {
-    int* count = group.at(&sh.count, 0);
-    u64* list = group.at(sh.list, 0);
-    const int lane = (int)threadIdx.x % 32, w = (int)threadIdx.x / 32, stride = (int)blockDim.x * 4;
-    const int own = 4 * ((s.n - w * kBatch + stride - 1) / stride);  // a lane's chunks, with those past the end
-    uint32_t who = __ballot_sync(~0u, lane_top >= floor && lane_top > -CUDART_INF_F);
-    while (who) {
-      int of[4];
+  // reaches the floor has such elements in the batch of its maximum, whose four chunks are looked at by four lanes; where
+  // the second of its batches reaches it too (few lanes), the warp looks at all of them.
+  __device__ __forceinline__ void collect(float floor, const LaneTop& top) const {
+    const int lane = (int)threadIdx.x % 32, w = (int)threadIdx.x / 32;
+    int* count = group.at(&shared().count, 0);
+    u64* list = group.at(shared().list, 0);
+    const auto look = [&](int c) {
+      float z[E];
+      unpack<T>(s.chunk(c), z);
+      uint32_t hits = 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        of[i] = who ? __ffs(who) - 1 : -1;
+      for (int e = 0; e < E; ++e) hits |= z[e] >= floor && z[e] > -CUDART_INF_F ? 1u << e : 0u;
+      for (; hits; hits &= hits - 1) {
+        const int index = s.first(c) + __ffs(hits) - 1;
+        const int at = atomicAdd(count, 1);
+        if (at < kListMax) list[at] = order_key(s.at(index), index);
+      }
+    };
+    uint32_t who = __ballot_sync(~0u, top.first >= floor && top.first > -CUDART_INF_F);
+    while (who) {
+      int of = -1;  // this lane looks at one of the chunks of the lane / 4-th of the next eight
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if (lane / 4 == i && who) of = __ffs(who) - 1;
         who &= who - 1;
       }
-      for (int k = lane; k < own; k += 32) {
-        const int c = w * kBatch + (k / 4) * stride + 32 * (k % 4);
-        uint4 v[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = of[i] >= 0 ? s.chunk(c + of[i]) : empty_chunk<T>();
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          ChunkMax<T, false> top;
-          top.add(v[i]);
-          if (!(top.value() >= floor)) continue;
-          float z[E];
-          unpack<T>(v[i], z);
-#pragma unroll
-          for (int e = 0; e < E; ++e)
-            if (z[e] >= floor && z[e] > -CUDART_INF_F) {
-              const int at = atomicAdd(count, 1);
-              if (at < kListMax) list[at] = order_key(z[e], s.first(c + of[i]) + e);
-            }
-        }
+      const int c = __shfl_sync(~0u, top.at, max(of, 0)) + 32 * (lane % 4);
+      if (of >= 0 && c < s.n) look(c);
+      __syncwarp();
+    }
+    for (who = __ballot_sync(~0u, top.second >= floor && top.second > -CUDART_INF_F); who; who &= who - 1) {
+      const int of = __ffs(who) - 1, best = __shfl_sync(~0u, top.at, of);
+      for (int k = lane;; k += 32) {
+        const int base = w * kBatch + of + k / 4 * ((int)blockDim.x * 4);
+        if (base >= s.n) break;
+        if (base != best && base + 32 * (k % 4) < s.n) look(base + 32 * (k % 4));
       }
+      __syncwarp();
     }
   }
 
   // After a barrier: the K first keys of the row are in the first CTA's list, with others or (where more than a list
   // was collected) alone.
   __device__ void settle(int K) {
-    if (*group.at(&sh.count, 0) <= kListMax) return;  // the same in all CTAs
-    const Floor floor = floor_of(radix_select<false>(Weigher(), no_floor(), K - 1));
-    if (group.rank == 0 && threadIdx.x == 0) sh.count = 0;
+    if (*group.at(&shared().count, 0) <= kListMax) return;  // the same in all CTAs
+    const Floor floor = floor_of(radix_select<false>(*this, Weigher(), no_floor(), K - 1));
+    if (group.rank == 0 && threadIdx.x == 0) shared().count = 0;
     group.sync();
-    int* count = group.at(&sh.count, 0);
-    u64* list = group.at(sh.list, 0);
+    int* count = group.at(&shared().count, 0);
+    u64* list = group.at(shared().list, 0);
     each([&](float z, int i) {
       if (floor.in(z, i)) list[atomicAdd(count, 1)] = order_key(z, i);
     });
@@ -313,16 +344,16 @@ struct Row {
   // f(rank, key) for the list's keys, by one thread each
   template <typename F>
   __device__ __forceinline__ void ranked(F f) {
-    const int n = sh.count;
+    const int n = shared().count;
     if (n > 512) {
       sort_list(n);
-      for (int i = (int)threadIdx.x; i < n; i += (int)blockDim.x) f(i, sh.list[i]);
+      for (int i = (int)threadIdx.x; i < n; i += (int)blockDim.x) f(i, shared().list[i]);
       return;
     }
     for (int i = (int)threadIdx.x / 32; i < n; i += (int)blockDim.x / 32) {  // a warp finds a key's rank
-      const u64 key = sh.list[i];
+      const u64 key = shared().list[i];
       int at = 0;
-      for (int o = (int)threadIdx.x % 32; o < n + (int)threadIdx.x % 32; o += 32) at += __popc(__ballot_sync(~0u, o < n && sh.list[o] > key));
+      for (int o = (int)threadIdx.x % 32; o < n + (int)threadIdx.x % 32; o += 32) at += __popc(__ballot_sync(~0u, o < n && shared().list[o] > key));
       if (threadIdx.x % 32 == 0) f(at, key);
     }
   }
@@ -403,17 +434,18 @@ struct Row {
     const u64 x = sum.value();
     total += x;
     if (shift == 0)
-      sh.parts[c / kBatch] = x;
+      shared().parts[c / kBatch] = x;
     else
-      atomicAdd(&sh.parts[(c / kBatch) >> shift], x);
+      atomicAdd(&shared().parts[(c / kBatch) >> shift], x);
   }
   __device__ __forceinline__ void clear_parts() {  // before a barrier, for add_part with a shift
-    for (int i = (int)threadIdx.x; i < kParts; i += (int)blockDim.x) sh.parts[i] = 0;
-    if (threadIdx.x == 0) sh.cta_q = 0;
+    for (int i = (int)threadIdx.x; i < kParts; i += (int)blockDim.x) shared().parts[i] = 0;
+    if (threadIdx.x == 0) shared().cta_q = 0;
   }
 
   // masses of the row's kept tokens, by part and by CTA
-  __device__ __noinline__ void masses(const Weigher& weigh, const Kept& kept) {
+  __device__ __noinline__ static void masses(Row row, Weigher weigh, Kept kept) { row.add_masses(weigh, kept); }
+  __device__ __forceinline__ void add_masses(const Weigher& weigh, const Kept& kept) {
     const int shift = part_shift(s.n);
     clear_parts();
     __syncthreads();
@@ -422,16 +454,16 @@ struct Row {
       s.sweep([&](const uint4 (&v)[4], int c) { add_part(batch_mass<true>(v, c, weigh, kept), c, shift, total); });
     else
       s.sweep([&](const uint4 (&v)[4], int c) { add_part(batch_mass<false>(v, c, weigh, kept), c, shift, total); });
-    if (threadIdx.x % 32 == 0) atomicAdd(&sh.cta_q, total);
+    if (threadIdx.x % 32 == 0) atomicAdd(&shared().cta_q, total);
   }
 
   // After a barrier of the group: the row's kept mass, the CTA's own and that of the CTAs ahead of it.
   __device__ u64 all_mass(u64* mine, u64* ahead) const {
     u64 total = 0;
-    *mine = sh.cta_q;
+    *mine = shared().cta_q;
     *ahead = 0;
     for (unsigned r = 0; r < group.n; ++r) {
-      const u64 x = *group.at(&sh.cta_q, r);
+      const u64 x = *group.at(&shared().cta_q, r);
       if (r < group.rank) *ahead += x;
       total += x;
     }
@@ -444,8 +476,8 @@ struct Row {
   // high on, from the floor on and of at least min_p, to the parts.  kFree: there is no floor.
   template <bool kKeep, bool kFree>
   __device__ __forceinline__ void collect_bin(const Weigher& weigh, Floor floor, float low, float high, float min_p) {
-    int* count = group.at(&sh.count, 0);
-    u64* list = group.at(sh.list, 0);
+    int* count = group.at(&shared().count, 0);
+    u64* list = group.at(shared().list, 0);
     const int shift = part_shift(s.n);
     u64 total = 0;
     s.sweep([&](const uint4 (&v)[4], int c) {
@@ -489,7 +521,7 @@ struct Row {
         add_part(sum, c, shift, total);
       }
     });
-    if (kKeep && threadIdx.x % 32 == 0 && total) atomicAdd(&sh.cta_q, total);
+    if (kKeep && threadIdx.x % 32 == 0 && total) atomicAdd(&shared().cta_q, total);
   }
 
   // Bins go down the order, by exponent; past 2^-32 of the maximum the last one.
@@ -505,7 +537,7 @@ struct Row {
   // One warp: the lowest value whose bin is at most b (with `outer` >= 0: whose bin is less than `outer`, or is `outer`
   // with a bin within of at most b), +inf if no value up to the maximum is.  The bins do not increase with the value; 32
   // values are tried at a time.
-  __device__ __noinline__ static float lowest_of_bin(const Weigher& weigh, int b, int outer) {
+  __device__ __noinline__ static float lowest_of_bin(Weigher weigh, int b, int outer) {
     const uint32_t lane = threadIdx.x % 32;
     const auto in = [&](uint32_t key) {
       const float y = weigh.exponent(key_value(key));
@@ -529,15 +561,15 @@ struct Row {
   }
 
   // After a barrier, in one warp: the bin of the cluster's histograms at which the running total passes t, and the rest
-  // of t within it, to sh.found and sh.before; all ones for histograms of nothing.  t may be given as a share of all.
+  // of t within it, to shared().found and shared().before; all ones for histograms of nothing.  t may be given as a share of all.
   template <bool kMass>
-  __device__ __noinline__ void find_bin(u64 t, bool share) {
+  __device__ __forceinline__ void find_bin(u64 t, bool share) const {
     static_assert(kGroups == 64, "two groups of bins a lane");
     const int lane = (int)threadIdx.x % 32;
     const unsigned ctas = group.n;
     u64 x0 = 0, x1 = 0;
     for (unsigned r = 0; r < ctas; ++r) {
-      const Histogram* h = group.at(&sh.bins, r);
+      const Histogram* h = group.at(&shared().bins, r);
       x0 += h->group[2 * lane];
       x1 += h->group[2 * lane + 1];
     }
@@ -553,30 +585,30 @@ struct Row {
       ++g;
     }
     u64 x = 0;
-    for (unsigned r = 0; r < ctas; ++r) x += group.at(&sh.bins, r)->mass(32 * g + lane);
+    for (unsigned r = 0; r < ctas; ++r) x += group.at(&shared().bins, r)->mass(32 * g + lane);
     upto = ahead + warp_scan(x);
     const int l = min(__popc(__ballot_sync(~0u, upto <= t)), 31);
     const u64 before = __shfl_sync(~0u, upto - x, l);
     if (lane == 0) {
-      sh.found = all ? (u64)(32 * g + l) : ~0ull;
-      sh.before = t - before;
+      shared().found = all ? (u64)(32 * g + l) : ~0ull;
+      shared().before = t - before;
     }
   }
 
   // The list's first n keys into descending order.
-  __device__ __noinline__ void sort_list(int n) {
+  __device__ __noinline__ static void sort_list(int n) {
     int size = 2;
     while (size < n) size *= 2;
-    for (int i = n + (int)threadIdx.x; i < size; i += (int)blockDim.x) sh.list[i] = 0;
+    for (int i = n + (int)threadIdx.x; i < size; i += (int)blockDim.x) shared().list[i] = 0;
     for (int k = 2; k <= size; k *= 2)
       for (int d = k / 2; d; d /= 2) {
         __syncthreads();
         for (int t = (int)threadIdx.x; t < size / 2; t += (int)blockDim.x) {
           const int i = 2 * t - (t & (d - 1));
-          const u64 a = sh.list[i], b = sh.list[i + d];
+          const u64 a = shared().list[i], b = shared().list[i + d];
           if ((a < b) == ((i & k) == 0)) {
-            sh.list[i] = b;
-            sh.list[i + d] = a;
+            shared().list[i] = b;
+            shared().list[i + d] = a;
           }
         }
       }
@@ -591,9 +623,13 @@ struct Row {
   // With min_p >= 0 the masses of the kept tokens (from the threshold on, of at least min_p) are left by part and by warp
   // as masses() leaves them, a cluster barrier included.
   template <bool kMass>
-  __device__ __noinline__ u64 select(const Weigher& weigh, Floor floor, u64 arg, float min_p) {
+  __device__ __noinline__ static u64 select(Row row, Weigher weigh, Floor floor, u64 arg, float min_p) {
+    return row.template threshold<kMass>(weigh, floor, arg, min_p);
+  }
+  template <bool kMass>
+  __device__ __forceinline__ u64 threshold(const Weigher& weigh, Floor floor, u64 arg, float min_p) {
     const int lane = (int)threadIdx.x % 32, warps = (int)blockDim.x / 32, warp = (int)threadIdx.x / 32;
-    int* count = group.at(&sh.count, 0);
+    int* count = group.at(&shared().count, 0);
     const bool keep = min_p >= 0.0f, free = floor.z == -CUDART_INF_F;
     const bool fits = (long long)per_cta * E <= kSliceElems && weigh.m < CUDART_INF_F;
     u64 t = arg;
@@ -601,8 +637,8 @@ struct Row {
     int n = kListMax + 1;
     for (int level = 0; level < 2 && fits; ++level) {
       // the cluster's CTAs have left the memory of the bins and the count behind: a barrier is above
-      for (int i = (int)threadIdx.x; i < kBins; i += (int)blockDim.x) sh.bins.low[i] = sh.bins.high[i] = 0;
-      if (threadIdx.x == 0) sh.count = 0;
+      for (int i = (int)threadIdx.x; i < kBins; i += (int)blockDim.x) shared().bins.low[i] = shared().bins.high[i] = 0;
+      if (threadIdx.x == 0) shared().count = 0;
       __syncthreads();
       if (kMass && level == 0 && !special) {
         s.sweep([&](const uint4 (&v)[4], int c) {
@@ -622,8 +658,8 @@ struct Row {
                 const uint32_t high = q.high[o] - kHighBits, low = q.low[o] - kOnesBits;
                 const uint32_t bin = __float_as_uint(o ? b.y : b.x) - kOnesBits;
                 const bool in = free || floor.in(z[e + o], i0 + e + o);
-                add_shared(&sh.bins.low[bin], in ? low : 0);
-                add_shared(&sh.bins.high[bin], in ? high : 0);
+                add_shared(&shared().bins.low[bin], in ? low : 0);
+                add_shared(&shared().bins.high[bin], in ? high : 0);
               }
             }
           }
@@ -639,40 +675,40 @@ struct Row {
           }
           if (kMass) {
             const uint32_t q = grid_mass(exp2_32(y));
-            if (q & 0x7fffu) atomicAdd(&sh.bins.low[b], q & 0x7fffu);
-            if (q >> 15) atomicAdd(&sh.bins.high[b], q >> 15);
+            if (q & 0x7fffu) atomicAdd(&shared().bins.low[b], q & 0x7fffu);
+            if (q >> 15) atomicAdd(&shared().bins.high[b], q >> 15);
           } else {
-            atomicAdd(&sh.bins.low[b], 1u);
+            atomicAdd(&shared().bins.low[b], 1u);
           }
         });
       }
       __syncthreads();
       for (int g = warp; g < kGroups; g += warps) {
-        const u64 x = warp_sum(sh.bins.mass(32 * g + lane));
-        if (lane == 0) sh.bins.group[g] = x;
+        const u64 x = warp_sum(shared().bins.mass(32 * g + lane));
+        if (lane == 0) shared().bins.group[g] = x;
       }
       group.sync();
       if (warp == 0) {  // every CTA for itself
         find_bin<kMass>(t, level == 0);
         __syncwarp();
-        if (sh.found != ~0ull) {
-          const int bin = (int)sh.found;
+        if (shared().found != ~0ull) {
+          const int bin = (int)shared().found;
           const float low = lowest_of_bin(weigh, bin, outer), high = lowest_of_bin(weigh, bin - 1, outer);
           if (lane == 0) {
-            sh.bin_low = low;
-            sh.bin_high = high;
+            shared().bin_low = low;
+            shared().bin_high = high;
           }
         }
       }
       __syncthreads();
-      if (sh.found == ~0ull) {
-        if (threadIdx.x == 0) sh.cta_q = 0;
+      if (shared().found == ~0ull) {
+        if (threadIdx.x == 0) shared().cta_q = 0;
         group.sync();
         return ~0ull;
       }
-      const int bin = (int)sh.found;
-      const float low = sh.bin_low, high = sh.bin_high;
-      t = sh.before;
+      const int bin = (int)shared().found;
+      const float low = shared().bin_low, high = shared().bin_high;
+      t = shared().before;
       // the bin's elements, from low to below high, to the list; the mass of what is above to the parts
       if (keep) clear_parts();
       __syncthreads();
@@ -691,9 +727,9 @@ struct Row {
       group.sync();  // all have seen the count
     }
     if (n > kListMax) {
-      const u64 key = radix_select<kMass>(weigh, floor, arg);
+      const u64 key = radix_select<kMass>(*this, weigh, floor, arg);
       if (keep) {
-        masses(weigh, Kept{floor_of(key), min_p});
+        masses(*this, weigh, Kept{floor_of(key), min_p});
         group.sync();
       }
       return key;
@@ -704,31 +740,31 @@ struct Row {
       if (warp == 0) {
         u64 upto = 0;
         for (int i0 = 0; i0 < n; i0 += 32) {
-          const u64 key = i0 + lane < n ? sh.list[i0 + lane] : 0;
+          const u64 key = i0 + lane < n ? shared().list[i0 + lane] : 0;
           const u64 q = i0 + lane >= n ? 0 : kMass ? grid_mass(weigh(order_value(key))) : 1u;
           const u64 sum = upto + warp_scan(q);
           if (sum - q <= t && t < sum) {
-            sh.found = key;
-            sh.last = i0 + lane;
+            shared().found = key;
+            shared().last = i0 + lane;
           }
           upto = __shfl_sync(~0u, sum, 31);
         }
       }
       __syncthreads();
       if (keep)
-        for (int i = (int)threadIdx.x; i <= sh.last; i += (int)blockDim.x) {
-          const u64 key = sh.list[i];
+        for (int i = (int)threadIdx.x; i <= shared().last; i += (int)blockDim.x) {
+          const u64 key = shared().list[i];
           const float w = weigh(order_value(key));
           if (!(w >= min_p)) continue;
           // the element's CTA and part
           const int c = (order_index(key) + s.head) / E, r = c / per_cta, at = c - r * per_cta;
           const u64 q = grid_mass(w);
-          atomicAdd(group.at(&sh.parts[(at / kBatch) >> part_shift(slice_chunks(r))], r), q);
-          atomicAdd(group.at(&sh.cta_q, r), q);
+          atomicAdd(group.at(&shared().parts[(at / kBatch) >> part_shift(slice_chunks(r))], r), q);
+          atomicAdd(group.at(&shared().cta_q, r), q);
         }
     }
     group.sync();
-    const u64 key = *group.at(&sh.found, 0);
+    const u64 key = *group.at(&shared().found, 0);
     if (!keep) group.sync();  // found and the list may be written again
     return key;
   }
@@ -741,15 +777,20 @@ struct Row {
 
   // The same by eight bits of the keys at a time.
   template <bool kMass>
-  __device__ __noinline__ u64 radix_select(const Weigher& weigh, Floor floor, u64 arg) {
+  __device__ __noinline__ static u64 radix_select(Row row, Weigher weigh, Floor floor, u64 arg) {
+    return row.template radix<kMass>(weigh, floor, arg);
+  }
+  template <bool kMass>
+  __device__ __forceinline__ u64 radix(const Weigher& weigh, Floor floor, u64 arg) {
     u64 prefix = 0, before = 0, t = 0;
+    int parity = 0;
     group.sync();
     for (int shift = 56; shift >= 0; shift -= 8) {
       if (shift < 32 && shift > 0 && s.V > 0 && (uint32_t)(s.V - 1) >> shift == 0) {
         prefix |= 0xffull << shift;  // every index has these bits clear
         continue;
       }
-      u64* hist = sh.radix[parity];
+      u64* hist = shared().radix[parity];
       for (int i = (int)threadIdx.x; i < 256; i += (int)blockDim.x) hist[i] = 0;
       __syncthreads();
       each([&](float z, int i) {
@@ -777,14 +818,14 @@ struct Row {
           u64 at = upto - sum;
           int i = 0;
           while (at + b[i] <= t) at += b[i++];
-          sh.found = prefix | (u64)(255 - 8 * (int)threadIdx.x - i) << shift;
-          sh.before = at;
+          shared().found = prefix | (u64)(255 - 8 * (int)threadIdx.x - i) << shift;
+          shared().before = at;
         }
-        if (!all && threadIdx.x == 0) sh.found = ~0ull;
+        if (!all && threadIdx.x == 0) shared().found = ~0ull;
       }
       __syncthreads();
-      prefix = sh.found;
-      before = sh.before;
+      prefix = shared().found;
+      before = shared().before;
       parity ^= 1;
       if (prefix == ~0ull) break;
     }
@@ -795,17 +836,20 @@ struct Row {
   // ---- draws
 
   // one warp: the token of the slice whose kept mass covers t (counted from the slice's start)
-  __device__ __noinline__ void draw(u64 t, const Weigher& weigh, const Kept& kept, u64 all, int32_t* tok,
-                                    float* prob) const {
+  __device__ __noinline__ static void draw(Row row, u64 t, Weigher weigh, Kept kept, u64 all, int32_t* tok, float* prob) {
+    row.find_token(t, weigh, kept, all, tok, prob);
+  }
+  __device__ __forceinline__ void find_token(u64 t, const Weigher& weigh, const Kept& kept, u64 all, int32_t* tok,
+                                             float* prob) const {
     const int lane = (int)threadIdx.x % 32, shift = part_shift(s.n);
     const int parts = ((s.n + kBatch - 1) / kBatch + (1 << shift) - 1) >> shift, per = (parts + 31) / 32;
     u64 sum = 0;
-    for (int i = 0; i < per; ++i) sum += sh.parts[min(lane * per + i, kParts - 1)];  // past the last all are 0
+    for (int i = 0; i < per; ++i) sum += shared().parts[min(lane * per + i, kParts - 1)];  // past the last all are 0
     u64 upto = warp_scan(sum);
     const int l = min(__popc(__ballot_sync(~0u, upto <= t)), 31);
     t -= __shfl_sync(~0u, upto - sum, l);
     int p = l * per;
-    while (p < l * per + per - 1 && t >= sh.parts[p]) t -= sh.parts[p++];
+    while (p < l * per + per - 1 && t >= shared().parts[p]) t -= shared().parts[p++];
     for (int c0 = (p << shift) * kBatch + lane; c0 - lane < s.n; c0 += kBatch) {
       uint4 v[4];
       u64 q[4];
@@ -848,10 +892,10 @@ struct Row {
   }
 
   // the first CTA: draws from the top-k list that settle() left
-  __device__ __noinline__ void draw_from_list(const Weigher& weigh, int top_k, u64 p24, float min_p, const float* u, int S,
+  __device__ __forceinline__ void draw_from_list(const Weigher& weigh, int top_k, u64 p24, float min_p, const float* u, int S,
                                  int32_t* tok, float* prob) {
-    TopList& l = sh.top;
-    const int n = min(top_k, sh.count);
+    TopList& l = shared().top;
+    const int n = min(top_k, shared().count);
     ranked([&](int at, u64 key) {
       if (at < n) {
         l.key[at] = key;
@@ -895,14 +939,6 @@ struct Row {
   }
 };
 
-// What the pass from memory finds of a row: each lane's maximum, and for the confidences each warp's maximum and the sum
-// of its weights relative to it.
-struct Found {
-  float top[kRowThreads];
-  float warp_top[kRowWarps], warp_sum[kRowWarps];
-  bool special[kRowWarps];
-};
-
 // ---- the K best
 
 template <typename T>
@@ -918,77 +954,63 @@ struct Propose {
     return t >= 0.0f ? fminf(__fdiv_rn(kLog2e, t), CUDART_MAX_NORMAL_F) : 1.0f;
   }
 
-  // one pass: each lane's maximum so far and the sum of its weights relative to it
-  __device__ __forceinline__ void pass(Row<T>& row, int r, Found& found) const {
+  __device__ __forceinline__ void run(Row<T>& row, int r) const {
     constexpr int E = ElemOf<T>::E;
-    const float c = scale(temperature(r));
-    float top = -CUDART_INF_F;
-    float2 sums = make_float2(0.0f, 0.0f);
-    row.s.sweep(
-        [&](const uint4 (&v)[4], int) {
-          ChunkMax<T, false> batch;
-          batch.add(v);
-          const float x = batch.value();
-          if (x > top) {
-            const float by = exp2_32((top - x) * c);
-            sums.x *= by;
-            sums.y *= by;
-            top = x;
-          }
-          if (top == -CUDART_INF_F) return;
-          const Weigher relative{top, c};
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            float z[E];
-            unpack<T>(v[i], z);
-#pragma unroll
-            for (int e = 0; e < E; e += 2) {
-              const float2 y = relative.exponents(z[e], z[e + 1]);
-              sums = add2(sums, make_float2(exp2_32(y.x), exp2_32(y.y)));
-            }
-          }
-        });
-    float m = top;
-    for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, o));
-    float sum = top == -CUDART_INF_F ? 0.0f : (sums.x + sums.y) * exp2_32((top - m) * c);
-    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
-    found.top[threadIdx.x] = top;
-    if (threadIdx.x % 32 == 0) {
-      found.warp_top[threadIdx.x / 32] = m;
-      found.warp_sum[threadIdx.x / 32] = sum;
-    }
-  }
-
-  __device__ __forceinline__ void finish(Row<T>& row, int r, const Found& found) const {
-    const int lane = (int)threadIdx.x % 32, warps = (int)blockDim.x / 32;
-    const float temp = temperature(r), top = found.top[threadIdx.x];
+    const int lane = (int)threadIdx.x % 32, warps = (int)blockDim.x / 32, warp = (int)threadIdx.x / 32;
+    const float temp = temperature(r);
     Weigher weigh;
     weigh.c = scale(temp);
+    // one pass: the lane's maximum so far and the sum of its weights relative to it
+    LaneTop top;
+    float2 sums = make_float2(0.0f, 0.0f);
+    row.s.sweep([&](const uint4 (&v)[4], int c) {
+      ChunkMax<T, false> batch;
+      batch.add(v);
+      const float x = batch.value();
+      if (x > top.first) {
+        const float by = exp2_32((top.first - x) * weigh.c);
+        sums.x *= by;
+        sums.y *= by;
+      }
+      top.add(x, c);
+      if (top.first == -CUDART_INF_F) return;
+      const Weigher relative{top.first, weigh.c};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float z[E];
+        unpack<T>(v[i], z);
+#pragma unroll
+        for (int e = 0; e < E; e += 2) {
+          const float2 y = relative.exponents(z[e], z[e + 1]);
+          sums = add2(sums, make_float2(exp2_32(y.x), exp2_32(y.y)));
+        }
+      }
+    });
     float floor;
-    weigh.m = row.top_of(top, a.K, &floor);
+    weigh.m = row.top_of(top.first, a.K, &floor);
     row.collect(floor, top);
-    float sum = found.warp_sum[threadIdx.x / 32], m = found.warp_top[threadIdx.x / 32];
-    if (sum != sum || weigh.m == CUDART_INF_F) {  // NaN or +inf among the warp's elements or the row's
+    float sum = sums.x + sums.y;
+    if (__any_sync(~0u, sum != sum) || weigh.m == CUDART_INF_F) {  // NaN or +inf among the warp's elements or the row's
       sum = 0.0f;
       row.each([&](float z, int) {
         const float w = weigh(z);
         sum += w > 0.0f ? w : 0.0f;
       });
-      for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
     } else {
-      sum = m == -CUDART_INF_F ? 0.0f : sum * exp2_32((m - weigh.m) * weigh.c);
+      sum = top.first == -CUDART_INF_F ? 0.0f : sum * exp2_32((top.first - weigh.m) * weigh.c);
     }
-    if (lane == 0) *row.group.at(&row.sh.sums[row.group.rank * warps + (int)threadIdx.x / 32], 0) = sum;
+    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
+    if (lane == 0) *row.group.at(&shared().sums[row.group.rank * warps + warp], 0) = sum;
     row.group.sync();
     row.settle(a.K);
     if (row.group.rank != 0) return;
     sum = 0.0f;
-    for (int i = 0; i < (int)row.group.n * warps; ++i) sum += row.sh.sums[i];
+    for (int i = 0; i < (int)row.group.n * warps; ++i) sum += shared().sums[i];
     int32_t* cand = a.cand + (long long)r * a.K;
     float* conf = a.conf + (long long)r * a.K;
     const bool good = temp >= 0.0f;
     for (int i = (int)threadIdx.x; i < a.K; i += (int)blockDim.x)
-      if (!good || i >= row.sh.count) {
+      if (!good || i >= shared().count) {
         cand[i] = -1;
         conf[i] = 0.0f;
       }
@@ -1010,12 +1032,7 @@ struct Sample {
   const Args& a;
   __device__ explicit Sample(const Args& args) : a(args) {}
 
-  __device__ __forceinline__ void pass(Row<T>& row, int, Found& found) const {
-    found.top[threadIdx.x] = row.lane_maximum();
-    if (threadIdx.x % 32 == 0) found.special[threadIdx.x / 32] = row.special;
-  }
-
-  __device__ __forceinline__ void finish(Row<T>& row, int r, const Found& found) const {
+  __device__ __forceinline__ void run(Row<T>& row, int r) const {
     const int lane = (int)threadIdx.x % 32;
     const int b = r / a.rows.k;
     float temp = a.temperature ? a.temperature[b] : 1.0f;
@@ -1033,10 +1050,11 @@ struct Sample {
     float* prob = a.prob + (long long)r * a.S;
     Weigher weigh;
     float floor;
-    weigh.m = row.top_of(found.top[threadIdx.x], by_list ? top_k : 0, &floor);
+    const LaneTop top = row.lane_top();
+    weigh.m = row.top_of(top.first, by_list ? top_k : 0, &floor);
     weigh.c = good ? fminf(__fdiv_rn(kLog2e, temp), CUDART_MAX_NORMAL_F) : 1.0f;
     if (by_list) {
-      row.collect(floor, found.top[threadIdx.x]);
+      row.collect(floor, top);
       row.group.sync();
       row.settle(top_k);
       if (row.group.rank != 0) return;
@@ -1044,14 +1062,14 @@ struct Sample {
       if (row.group.n > 1) row.group.sync();  // the others have looked at the count
       return;
     }
-    row.special = found.special[threadIdx.x / 32] || fabsf(weigh.m) == CUDART_INF_F;
+    row.special = row.special || fabsf(weigh.m) == CUDART_INF_F;
     const bool by_mass = p24 < (1u << 24);
     Kept kept{no_floor(), fmaxf(min_p, 0.0f)};
     if (top_k < a.rows.V)
-      kept.floor = floor_of(row.template select<false>(weigh, kept.floor, top_k - 1, by_mass ? -1.0f : kept.min_p));
-    if (by_mass) kept.floor = floor_of(row.template select<true>(weigh, kept.floor, p24, kept.min_p));
+      kept.floor = floor_of(Row<T>::template select<false>(row, weigh, kept.floor, top_k - 1, by_mass ? -1.0f : kept.min_p));
+    if (by_mass) kept.floor = floor_of(Row<T>::template select<true>(row, weigh, kept.floor, p24, kept.min_p));
     if (top_k == a.rows.V && !by_mass) {
-      row.masses(weigh, kept);
+      Row<T>::masses(row, weigh, kept);
       row.group.sync();
     }
     u64 mine, ahead;
@@ -1066,7 +1084,7 @@ struct Sample {
         continue;
       }
       const u64 t = min(share24((u64)(x * 16777216.0f), all), all - 1);
-      if (t >= ahead && t < ahead + mine) row.draw(t - ahead, weigh, kept, all, &tok[i], &prob[i]);
+      if (t >= ahead && t < ahead + mine) Row<T>::draw(row, t - ahead, weigh, kept, all, &tok[i], &prob[i]);
     }
     if (row.group.n > 1) row.group.sync();  // no CTA leaves while its masses are read
   }
@@ -1075,16 +1093,11 @@ struct Sample {
 // a cluster of CTAs for each row
 template <typename T, template <typename> class Op, int kPerSm>
 __global__ void __launch_bounds__(kRowThreads, kPerSm) k_rows(PickArgs a) {
-  __shared__ PickShared sh;
-  __shared__ Found found;
-  Row<T> row(sh);
+  Row<T> row;
   row.per_cta = a.rows.per;
   const int r = (int)(blockIdx.x / row.group.n);
-  row.s.open(row_address<T>(a.rows, r), a.rows, row.group.rank, sh.ends);
-  const Op<T> op(a);
-  op.pass(row, r, found);
-  __syncwarp();
-  op.finish(row, r, found);
+  row.s.open(row_address<T>(a.rows, r), a.rows, row.group.rank, shared().ends);
+  Op<T>(a).run(row, r);
 }
 
 template <typename T, template <typename> class Op, int kPerSm>
