@@ -37,6 +37,10 @@ constexpr int kRowWarps = kRowThreads / 32;
 constexpr int kRowCluster = 8;  // most CTAs of a row (the portable limit of a cluster)
 constexpr float kLog2e = 1.4426950408889634f;
 
+// The warp's number, the same in all lanes also to the compiler: votes and sums in loops over it need no check that the
+// lanes have come together (such a check took 300 cycles).
+__device__ __forceinline__ int warp_index() { return __shfl_sync(~0u, (int)threadIdx.x / 32, 0); }
+
 __device__ __forceinline__ float exp2_32(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -179,7 +183,7 @@ struct Slice {
   // f(v, c) for this warp's batches: v are this lane's chunks c, c + 32, c + 64 and c + 96, of -inf past the slice's end
   template <typename F>
   __device__ __forceinline__ void sweep(F f) const {
-    for (int base = (int)(threadIdx.x / 32) * kBatch; base < n; base += (int)blockDim.x * 4) {
+    for (int base = warp_index() * kBatch; base < n; base += (int)blockDim.x * 4) {
       uint4 v[4];
       const int c = base + (int)(threadIdx.x % 32);
       if (base >= flo && base + kBatch <= fhi) {

@@ -189,7 +189,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_distill(DistillArgs a) {
   auto cluster = cg::this_cluster();
   constexpr int E = ElemOf<T>::E;
   const unsigned ctas = cluster.num_blocks(), rank = cluster.block_rank();
-  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, warps = blockDim.x / 32;
+  const int lane = threadIdx.x % 32, warp = warp_index(), warps = blockDim.x / 32;
   const int r = (int)(blockIdx.x / ctas);
   const float weight = a.weight ? a.weight[r] : 1.0f;
   const T* logits = row_address<T>(a.rows, r);
@@ -299,7 +299,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_distill_backward(DistillArgs
     write_zeros(s, grad);
     return;
   }
-  if (threadIdx.x / 32 == blockDim.x / 32 - 1) teacher(a, r, t);
+  if (warp_index() == blockDim.x / 32 - 1) teacher(a, r, t);
   const float inv = 1.0f / a.tau;
   write_gradient(s, grad, coef, t, a.K, [=](float z) {
     return z == -CUDART_INF_F ? 0.0f : exp2_32(fmaf(z, inv, -lse) * kLog2e);

@@ -28,6 +28,7 @@ constexpr int kListMax = 2048;  // most keys collected for ranking
 constexpr int kMaxK = 256;      // most candidates of a position, and the longest top-k list
 constexpr int kBins = 2048;     // of a threshold's histogram
 constexpr int kGroups = kBins / 32;
+constexpr int kLevels = 4;      // of histograms for one threshold
 constexpr int kParts = 512;     // masses kept of a slice's batches
 constexpr int kTops = 2 * kMaxK + kRowWarps * kRowCluster;
 constexpr float kBinsPerUnit = kBins / 32;  // bins to a power of two; past 2^-32 of the maximum weights are 0
@@ -68,8 +69,8 @@ struct TopList {  // a sampler's top-k list, in order
   uint32_t kept[kMaxK];
 };
 
-struct Tops {  // largest lane maxima (value keys): of this CTA's warps, and of all of the row's
-  uint32_t mine[kTops], all[kTops];
+struct Tops {  // largest lane maxima (value keys): of this CTA's warps, and past kTops of all of the row's
+  uint32_t value[2 * kTops];
 };
 
 struct PickShared {
@@ -217,18 +218,33 @@ struct Row {
     });
   }
 
+  // f(i, how many o < n are ahead(i, o)) for i < n, by one thread each; eight lanes count for one i.  (A vote for every
+  // 32 of them took 250 cycles.)
+  template <typename A, typename F>
+  __device__ __forceinline__ static void each_rank(int n, A ahead, F f) {
+    const int part = (int)threadIdx.x % 8;
+    for (int i0 = 0; i0 < n; i0 += (int)blockDim.x / 8) {
+      const int i = min(i0 + (int)threadIdx.x / 8, n - 1);
+      int count = 0;
+#pragma unroll 4
+      for (int o = part; o < n; o += 8) count += ahead(i, o);
+      for (int m = 1; m < 8; m *= 2) count += __shfl_xor_sync(~0u, count, m);
+      if (part == 0 && i0 + (int)threadIdx.x / 8 < n) f(i, count);
+    }
+  }
+
   // The row's maximum from the lanes' (NaN left out, -inf for a row without elements).  For K > 0 *floor is a value
   // that at least K elements reach (or -inf): the K-th largest of the largest j lane maxima of every warp, where j gives
   // twice K of them.  About 1.4 K elements of a row in random order reach it; the lowest of the warps' j-th, which needs
   // no ranking, lets ten times K through at one lane maximum a warp.
   __device__ float top_of(float lane_top, int K, float* floor) {
-    const int warps = (int)blockDim.x / 32, w = (int)threadIdx.x / 32, lane = (int)threadIdx.x % 32;
+    const int warps = (int)blockDim.x / 32, w = warp_index(), lane = (int)threadIdx.x % 32;
     const int all = warps * (int)group.n;
     const int j = K > 0 ? min((2 * K + all - 1) / all, 32) : 1;
     uint32_t key = value_key(lane_top);
     for (int i = 0; i < j; ++i) {
       const uint32_t x = __reduce_max_sync(~0u, key);
-      if (lane == 0) shared().tops.mine[w * j + i] = x;
+      if (lane == 0) shared().tops.value[w * j + i] = x;
       if (__ffs(__ballot_sync(~0u, key == x)) - 1 == lane) key = 0;
     }
     if (threadIdx.x == 0) {
@@ -239,26 +255,22 @@ struct Row {
     const int n = all * j, per = warps * j;
     if (K == 0) {  // every warp looks at all warps of the row
       uint32_t m = 0;
-      for (int i = lane; i < n; i += 32) m = max(m, *group.at(&shared().tops.mine[i % per], i / per));
+      for (int i = lane; i < n; i += 32) m = max(m, *group.at(&shared().tops.value[i % per], i / per));
       return key_value(__reduce_max_sync(~0u, m));
     }
-    const uint32_t* tops = shared().tops.mine;
+    int from = 0;
     if (group.n > 1) {
-      for (int i = (int)threadIdx.x; i < n; i += (int)blockDim.x)
-        shared().tops.all[i] = *group.at(&shared().tops.mine[i % per], i / per);
+      from = kTops;
+      for (int i = threadIdx.x; i < n; i += (int)blockDim.x)
+        shared().tops.value[from + i] = *group.at(&shared().tops.value[i % per], i / per);
       __syncthreads();
-      tops = shared().tops.all;
     }
-    for (int i = w; i < n; i += warps) {  // a warp finds a value's rank
-      const uint32_t x = tops[i];
-      int above = 0;
-      for (int o = lane; o < n + lane; o += 32) {
-        const uint32_t y = o < n ? tops[o] : 0;
-        above += __popc(__ballot_sync(~0u, y > x || (y == x && o < i)));
-      }
-      if (lane == 0 && above == 0) shared().row_top = x;
-      if (lane == 0 && above == K - 1) shared().row_floor = x;
-    }
+    const uint32_t* tops = &shared().tops.value[from];
+    each_rank(n, [&](int i, int o) { return tops[o] > tops[i] || (tops[o] == tops[i] && o < i); },
+              [&](int i, int above) {
+                if (above == 0) shared().row_top = tops[i];
+                if (above == K - 1) shared().row_floor = tops[i];
+              });
     __syncthreads();
     *floor = shared().row_floor ? key_value(shared().row_floor) : -CUDART_INF_F;
     return key_value(shared().row_top);
@@ -288,7 +300,7 @@ struct Row {
   // reaches the floor has such elements in the batch of its maximum, whose four chunks are looked at by four lanes; where
   // the second of its batches reaches it too (few lanes), the warp looks at all of them.
   __device__ __forceinline__ void collect(float floor, const LaneTop& top) const {
-    const int lane = (int)threadIdx.x % 32, w = (int)threadIdx.x / 32;
+    const int lane = (int)threadIdx.x % 32, w = warp_index();
     int* count = group.at(&shared().count, 0);
     u64* list = group.at(shared().list, 0);
     const auto look = [&](int c) {
@@ -350,12 +362,8 @@ struct Row {
       for (int i = (int)threadIdx.x; i < n; i += (int)blockDim.x) f(i, shared().list[i]);
       return;
     }
-    for (int i = (int)threadIdx.x / 32; i < n; i += (int)blockDim.x / 32) {  // a warp finds a key's rank
-      const u64 key = shared().list[i];
-      int at = 0;
-      for (int o = (int)threadIdx.x % 32; o < n + (int)threadIdx.x % 32; o += 32) at += __popc(__ballot_sync(~0u, o < n && shared().list[o] > key));
-      if (threadIdx.x % 32 == 0) f(at, key);
-    }
+    each_rank(n, [&](int i, int o) { return shared().list[o] > shared().list[i]; },
+              [&](int i, int at) { f(at, shared().list[i]); });
   }
 
   // ---- masses
@@ -524,28 +532,37 @@ struct Row {
     if (kKeep && threadIdx.x % 32 == 0 && total) atomicAdd(&shared().cta_q, total);
   }
 
-  // Bins go down the order, by exponent; past 2^-32 of the maximum the last one.
-  __device__ __forceinline__ static int bin_of(float y) {
-    return (int)(__float_as_uint(fminf(y * -kBinsPerUnit, (float)(kBins - 1)) + kOnes) - kOnesBits);
-  }
-  // A bin cut in as many again; b is the bin of y.
-  __device__ __forceinline__ static int bin_within(float y, int b) {
-    const float x = fminf(y * -kBinsPerUnit, (float)(kBins - 1));
-    return (int)fminf((x - ((float)b - 0.5f)) * kBins, (float)(kBins - 1));
-  }
+  // One level of a threshold's search: kBins bins, evenly spaced in the exponent, that go down the order.  Bin 0 has what
+  // is above, the last bin what is below; of the row's values only those from low to below high count.
+  struct Level {
+    float from, scale;
+    float low, high;
+    __device__ __forceinline__ int bin(float y) const {
+      const float x = fminf(fmaxf((-y - from) * scale, 0.0f), (float)(kBins - 1));
+      return (int)(__float_as_uint(x + kOnes) - kOnesBits);
+    }
+    __device__ __forceinline__ bool has(float z) const { return z >= low && z < high; }
+    // the level that resolves bin b, whose values are from `l` to below `h`
+    __device__ __forceinline__ void enter(int b, float l, float h) {
+      low = l;
+      high = h;
+      if (b == kBins - 1) {  // what is below, on a coarser scale
+        from += (b - 0.5f) / scale;
+        scale *= 1.0f / 64;
+      } else {
+        from += fmaxf(b - 0.5f, 0.0f) / scale;
+        scale *= kBins / 2;
+      }
+    }
+  };
 
-  // One warp: the lowest value whose bin is at most b (with `outer` >= 0: whose bin is less than `outer`, or is `outer`
-  // with a bin within of at most b), +inf if no value up to the maximum is.  The bins do not increase with the value; 32
-  // values are tried at a time.
-  __device__ __noinline__ static float lowest_of_bin(Weigher weigh, int b, int outer) {
+  // One warp: the lowest of the level's values whose bin is at most b, or the level's end.  The bins do not increase with
+  // the value; 32 values are tried at a time.
+  __device__ __noinline__ static float lowest_of_bin(Weigher weigh, Level level, int b) {
     const uint32_t lane = threadIdx.x % 32;
-    const auto in = [&](uint32_t key) {
-      const float y = weigh.exponent(key_value(key));
-      const int own = bin_of(y);
-      return outer < 0 ? own <= b : own < outer || (own == outer && bin_within(y, own) <= b);
-    };
-    uint32_t lo = value_key(-CUDART_MAX_NORMAL_F), hi = value_key(weigh.m);
-    if (!in(hi)) return CUDART_INF_F;
+    const auto in = [&](uint32_t key) { return level.bin(weigh.exponent(key_value(key))) <= b; };
+    uint32_t lo = value_key(level.low), hi = level.high <= weigh.m ? value_key(level.high) - 1 : value_key(weigh.m);
+    if (!in(hi)) return level.high;
     while (lo < hi) {  // the answer is in [lo, hi]
       const uint32_t step = (hi - lo) / 32 + 1;
       const uint32_t hit = __ballot_sync(~0u, in(min(lo + lane * step, hi)));
@@ -618,7 +635,7 @@ struct Row {
   // The key of the element, among those from the floor on, at which the running total of the order passes the target:
   // with kMass totals are masses and the target floor(arg all / 2^24) - 1, else they are counts and it is arg (or the
   // last).  All ones for a row without elements.  A histogram over evenly spaced exponents finds the bin; where it has
-  // more elements than a list, a second one cuts it again; the first CTA sorts the bin's elements.  Rows of many equal
+  // more elements than a list, the next one cuts it again; the first CTA sorts the bin's elements.  Rows of many equal
   // values go by radix selection.
   // With min_p >= 0 the masses of the kept tokens (from the threshold on, of at least min_p) are left by part and by warp
   // as masses() leaves them, a cluster barrier included.
@@ -628,19 +645,19 @@ struct Row {
   }
   template <bool kMass>
   __device__ __forceinline__ u64 threshold(const Weigher& weigh, Floor floor, u64 arg, float min_p) {
-    const int lane = (int)threadIdx.x % 32, warps = (int)blockDim.x / 32, warp = (int)threadIdx.x / 32;
+    const int lane = (int)threadIdx.x % 32, warps = (int)blockDim.x / 32, warp = warp_index();
     int* count = group.at(&shared().count, 0);
     const bool keep = min_p >= 0.0f, free = floor.z == -CUDART_INF_F;
     const bool fits = (long long)per_cta * E <= kSliceElems && weigh.m < CUDART_INF_F;
     u64 t = arg;
-    int outer = -1;  // the bin of the first level
+    Level level{0.0f, kBinsPerUnit, -CUDART_MAX_NORMAL_F, CUDART_INF_F};
     int n = kListMax + 1;
-    for (int level = 0; level < 2 && fits; ++level) {
+    for (int depth = 0; depth < kLevels && fits; ++depth) {
       // the cluster's CTAs have left the memory of the bins and the count behind: a barrier is above
       for (int i = (int)threadIdx.x; i < kBins; i += (int)blockDim.x) shared().bins.low[i] = shared().bins.high[i] = 0;
       if (threadIdx.x == 0) shared().count = 0;
       __syncthreads();
-      if (kMass && level == 0 && !special) {
+      if (kMass && depth == 0 && !special) {
         s.sweep([&](const uint4 (&v)[4], int c) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
@@ -666,13 +683,9 @@ struct Row {
         });
       } else {
         each([&](float z, int i) {
-          if (!floor.in(z, i)) return;
+          if (!level.has(z) || !floor.in(z, i)) return;
           const float y = weigh.exponent(z);
-          int b = bin_of(y);
-          if (level) {
-            if (b != outer) return;
-            b = bin_within(y, b);
-          }
+          const int b = level.bin(y);
           if (kMass) {
             const uint32_t q = grid_mass(exp2_32(y));
             if (q & 0x7fffu) atomicAdd(&shared().bins.low[b], q & 0x7fffu);
@@ -689,11 +702,11 @@ struct Row {
       }
       group.sync();
       if (warp == 0) {  // every CTA for itself
-        find_bin<kMass>(t, level == 0);
+        find_bin<kMass>(t, depth == 0);
         __syncwarp();
         if (shared().found != ~0ull) {
           const int bin = (int)shared().found;
-          const float low = lowest_of_bin(weigh, bin, outer), high = lowest_of_bin(weigh, bin - 1, outer);
+          const float low = lowest_of_bin(weigh, level, bin), high = bin ? lowest_of_bin(weigh, level, bin - 1) : level.high;
           if (lane == 0) {
             shared().bin_low = low;
             shared().bin_high = high;
@@ -723,7 +736,7 @@ struct Row {
       group.sync();
       n = *count;
       if (n <= kListMax) break;
-      outer = bin;
+      level.enter(bin, low, high);
       group.sync();  // all have seen the count
     }
     if (n > kListMax) {
@@ -956,7 +969,7 @@ struct Propose {
 
   __device__ __forceinline__ void run(Row<T>& row, int r) const {
     constexpr int E = ElemOf<T>::E;
-    const int lane = (int)threadIdx.x % 32, warps = (int)blockDim.x / 32, warp = (int)threadIdx.x / 32;
+    const int lane = (int)threadIdx.x % 32, warps = (int)blockDim.x / 32, warp = warp_index();
     const float temp = temperature(r);
     Weigher weigh;
     weigh.c = scale(temp);
@@ -1074,7 +1087,7 @@ struct Sample {
     }
     u64 mine, ahead;
     const u64 all = row.all_mass(&mine, &ahead);
-    for (int i = (int)threadIdx.x / 32; i < a.S; i += (int)blockDim.x / 32) {
+    for (int i = warp_index(); i < a.S; i += (int)blockDim.x / 32) {
       const float x = u[i];
       if (all == 0 || !(x >= 0.0f && x <= 1.0f)) {
         if (row.group.rank == 0 && lane == 0) {

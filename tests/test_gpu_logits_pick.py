@@ -222,6 +222,7 @@ RULES = {  # temperature, top-k, top-p, min-p of the batch's sequences in turn; 
     'top-k': ([0.9, 1.4], [1, 50, 64, 3], None, None),
     'large top-k': ([1.0], [65, 300, 4000, 100000], None, None),
     'top-p': ([1.0, 0.8], None, [0.9, 0.5, 0.99, 0.0], None),
+    'cold large top-k': ([0.05, 0.3], [300, 4000, 40000], [1.0, 0.9], None),
     'min-p': ([1.0], None, None, [0.05, 0.3, 1.0, 2.0]),
     'all': ([0.6, 1.1], [40, 64, 7], [0.95, 0.6], [0.02, 0.1]),
     'large all': ([1.3, 3.0], [500, 2000], [0.95, 0.7], [1e-4, 0.0]),
