@@ -4,7 +4,6 @@
 
 namespace epic {
 
-constexpr int kClusterMax = 8;
 constexpr int kThreadsMax = 512;
 
 // One CTA a row where the rows fill the GPU (two CTAs an SM).  Fewer rows are cut over clusters of up to eight CTAs,
@@ -15,7 +14,7 @@ RowShape row_shape(long long rows, int V, int size) {
   const long long full = 2 * 152;
   RowShape p = {};
   p.ctas = 1;
-  while (p.ctas < kClusterMax &&
+  while (p.ctas < kRowCtasMax &&
          (chunks * E > (long long)p.ctas * kSliceElems || (rows * p.ctas * 2 <= full && chunks > p.ctas * 2048)))
     p.ctas *= 2;
   p.per = (int)((chunks + p.ctas - 1) / p.ctas);

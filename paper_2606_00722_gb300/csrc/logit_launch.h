@@ -10,6 +10,7 @@ namespace epic {
 
 // Most elements of a slice whose masses, in parts of 15 and 16 bits, a histogram's 32-bit bins can add up.
 constexpr int kSliceElems = 131000;
+constexpr int kRowCtasMax = 8;  // the portable limit of a cluster
 
 struct RowShape {
   int ctas;     // CTAs of a row: one cluster

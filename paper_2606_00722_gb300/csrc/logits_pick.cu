@@ -24,12 +24,13 @@
 namespace epic {
 namespace {
 
-constexpr int kListMax = 2048;  // most keys collected for ranking
+constexpr int kListMax = 1536;  // most keys collected for ranking
 constexpr int kMaxK = 256;      // most candidates of a position, and the longest top-k list
+constexpr int kMaxV = kRowCtasMax * (kSliceElems - 16);  // 1,047,872: histograms and parts of a row's slices
 constexpr int kBins = 2048;     // of a threshold's histogram
 constexpr int kGroups = kBins / 32;
-constexpr int kLevels = 4;      // of histograms for one threshold
-constexpr int kParts = 512;     // masses kept of a slice's batches
+constexpr int kLevels = 4;      // of histograms by exponent for one threshold
+constexpr int kParts = (kSliceElems + 127) / 128;  // runs of 32 chunks of a slice, whose kept masses are noted
 constexpr int kTops = 2 * kMaxK + kRowWarps * kRowCluster;
 constexpr float kBinsPerUnit = kBins / 32;  // bins to a power of two; past 2^-32 of the maximum weights are 0
 constexpr float kGrid = 1073741824.0f;      // 2^30: the weights' grid
@@ -76,13 +77,13 @@ struct Tops {  // largest lane maxima (value keys): of this CTA's warps, and pas
 struct PickShared {
   union {
     Histogram bins;
-    u64 radix[2][256];
     TopList top;
   };
   Tops tops;
   u64 list[kListMax];
-  u64 parts[kParts];  // kept masses by runs of batches
+  u64 parts[kParts + kParts / 16];  // kept masses by runs of 32 chunks, at part_at()
   u64 cta_q;          // and of the CTA
+  u64 warp_q[kRowWarps];
   uint4 ends[2];
   u64 found, before;
   float bin_low, bin_high;
@@ -194,6 +195,9 @@ struct LaneTop {
   }
 };
 
+// A gap after every 16 parts: lanes that read runs of them are in different banks.
+__device__ __forceinline__ int part_at(int p) { return p + p / 16; }
+
 template <typename T>
 struct Row {
   Slice<T> s;
@@ -203,19 +207,17 @@ struct Row {
   static constexpr int E = ElemOf<T>::E;
 
 
-  // f(value, index) for the elements of this warp's chunks (and -inf past their end)
+  // f(value, index) for the elements of this lane's chunks, one at a time: small code for rare ways.  (The whole kernel
+  // unrolled was 460 KB, and each phase of a row waited for its instructions.)
   template <typename F>
   __device__ __forceinline__ void each(F f) const {
-    s.sweep([&](const uint4 (&v)[4], int c) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float z[E];
-        unpack<T>(v[i], z);
-        const int i0 = s.first(c + 32 * i);
-#pragma unroll
-        for (int e = 0; e < E; ++e) f(z[e], i0 + e);
+#pragma unroll 1
+    for (int base = warp_index() * kBatch; base < s.n; base += (int)blockDim.x * 4)
+#pragma unroll 1
+      for (int k = 0; k < 4 * E; ++k) {
+        const int i = s.first(base + (int)threadIdx.x % 32 + 32 * (k / E)) + k % E;
+        if (i >= s.lo() && i < s.hi()) f(s.at(i), i);
       }
-    });
   }
 
   // f(i, how many o < n are ahead(i, o)) for i < n, by one thread each; eight lanes count for one i.  (A vote for every
@@ -342,7 +344,7 @@ struct Row {
   // was collected) alone.
   __device__ void settle(int K) {
     if (*group.at(&shared().count, 0) <= kListMax) return;  // the same in all CTAs
-    const Floor floor = floor_of(radix_select<false>(*this, Weigher(), no_floor(), K - 1));
+    const Floor floor = floor_of(threshold(*this, Weigher{CUDART_INF_F, 0.0f}, no_floor(), K - 1, false, -1.0f));
     if (group.rank == 0 && threadIdx.x == 0) shared().count = 0;
     group.sync();
     int* count = group.at(&shared().count, 0);
@@ -384,84 +386,76 @@ struct Row {
     return q;
   }
 
-  // A lane's kept mass of a batch in parts, whose sums over a warp's batch are below 32 bits.
+  // A lane's kept mass of a chunk in parts, whose sums over a warp are below 32 bits.
   struct LaneMass {
     uint32_t high, low;
     __device__ __forceinline__ u64 value() const { return ((u64)high << 15) + (u64)(long long)(int)low; }
   };
   template <bool kAll>
-  __device__ __forceinline__ LaneMass batch_mass(const uint4 (&v)[4], int c, const Weigher& weigh,
-                                                 const Kept& kept) const {
+  __device__ __forceinline__ LaneMass lane_mass(const uint4& v, int c, const Weigher& weigh, const Kept& kept) const {
     LaneMass sum = {0, 0};
-    if (special) {
-      u64 q = 0;
-#pragma unroll 1
-      for (int i = 0; i < 4; ++i) q += chunk_mass(s.chunk(c + 32 * i), c + 32 * i, weigh, kept);
-      return LaneMass{(uint32_t)(q >> 15), (uint32_t)q & 0x7fffu};
-    }
-    if (kAll) sum = {0u - 4u * E * kHighBits, 0u - 4u * E * kOnesBits};
+    if (kAll) sum = {0u - (uint32_t)E * kHighBits, 0u - (uint32_t)E * kOnesBits};
+    float z[E];
+    unpack<T>(v, z);
+    const int i0 = s.first(c);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float z[E];
-      unpack<T>(v[i], z);
-      const int i0 = s.first(c + 32 * i);
+    for (int e = 0; e < E; e += 2) {
+      const float2 y = weigh.exponents(z[e], z[e + 1]);
+      const float2 w = make_float2(exp2_32(y.x), exp2_32(y.y));
+      const Parts2 q(w);
+      if (kAll) {
+        sum.high += q.high[0] + q.high[1];
+        sum.low += q.low[0] + q.low[1];
+      } else {
 #pragma unroll
-      for (int e = 0; e < E; e += 2) {
-        const float2 y = weigh.exponents(z[e], z[e + 1]);
-        const float2 w = make_float2(exp2_32(y.x), exp2_32(y.y));
-        const Parts2 q(w);
-        if (kAll) {
-          sum.high += q.high[0] + q.high[1];
-          sum.low += q.low[0] + q.low[1];
-        } else {
-          if (kept.floor.in(z[e], i0 + e) && w.x >= kept.min_p) {
-            sum.high += q.high[0] - kHighBits;
-            sum.low += q.low[0] - kOnesBits;
+        for (int o = 0; o < 2; ++o)
+          if ((o ? w.y : w.x) >= kept.min_p && kept.floor.in(z[e + o], i0 + e + o)) {
+            sum.high += q.high[o] - kHighBits;
+            sum.low += q.low[o] - kOnesBits;
           }
-          if (kept.floor.in(z[e + 1], i0 + e + 1) && w.y >= kept.min_p) {
-            sum.high += q.high[1] - kHighBits;
-            sum.low += q.low[1] - kOnesBits;
-          }
-        }
       }
     }
     return sum;
   }
 
-  // a part is 2^shift batches
-  __device__ __forceinline__ static int part_shift(int chunks) {
-    int shift = 0;
-    while ((chunks + kBatch - 1) / kBatch > kParts << shift) ++shift;
-    return shift;
-  }
-
-  // the warp's sum of a batch's masses to its part (a warp's own, unless parts are of several batches)
-  __device__ __forceinline__ void add_part(LaneMass q, int c, int shift, u64& total) {
+  // the warp's sum of its lanes' masses of 32 chunks to their part; lane 0 adds it up
+  __device__ __forceinline__ void add_part(LaneMass q, int c, u64& total) {
     const LaneMass sum = {__reduce_add_sync(~0u, q.high), __reduce_add_sync(~0u, q.low)};
-    if (threadIdx.x % 32) return;
+    if (threadIdx.x % 32 || c >= s.n) return;
     const u64 x = sum.value();
     total += x;
-    if (shift == 0)
-      shared().parts[c / kBatch] = x;
-    else
-      atomicAdd(&shared().parts[(c / kBatch) >> shift], x);
+    shared().parts[part_at(c / 32)] = x;
   }
-  __device__ __forceinline__ void clear_parts() {  // before a barrier, for add_part with a shift
-    for (int i = (int)threadIdx.x; i < kParts; i += (int)blockDim.x) shared().parts[i] = 0;
+  // Before a barrier.
+  __device__ __forceinline__ void clear_parts() {
+    for (int i = (int)threadIdx.x; i < kParts + kParts / 16; i += (int)blockDim.x) shared().parts[i] = 0;
     if (threadIdx.x == 0) shared().cta_q = 0;
   }
 
   // masses of the row's kept tokens, by part and by CTA
-  __device__ __noinline__ static void masses(Row row, Weigher weigh, Kept kept) { row.add_masses(weigh, kept); }
-  __device__ __forceinline__ void add_masses(const Weigher& weigh, const Kept& kept) {
-    const int shift = part_shift(s.n);
-    clear_parts();
+  __device__ __noinline__ static void masses(Row row, Weigher weigh, Kept kept) {
+    row.clear_parts();
     __syncthreads();
     u64 total = 0;
-    if (kept.all())
-      s.sweep([&](const uint4 (&v)[4], int c) { add_part(batch_mass<true>(v, c, weigh, kept), c, shift, total); });
-    else
-      s.sweep([&](const uint4 (&v)[4], int c) { add_part(batch_mass<false>(v, c, weigh, kept), c, shift, total); });
+    if (row.special) {
+      row.s.sweep([&](const uint4 (&)[4], int c) {
+#pragma unroll 1
+        for (int i = 0; i < 4; ++i) {
+          const u64 q = row.chunk_mass(row.s.chunk(c + 32 * i), c + 32 * i, weigh, kept);
+          row.add_part(LaneMass{(uint32_t)(q >> 15), (uint32_t)q & 0x7fffu}, c + 32 * i, total);
+        }
+      });
+    } else if (kept.all()) {
+      row.s.sweep([&](const uint4 (&v)[4], int c) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) row.add_part(row.template lane_mass<true>(v[i], c + 32 * i, weigh, kept), c + 32 * i, total);
+      });
+    } else {
+      row.s.sweep([&](const uint4 (&v)[4], int c) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) row.add_part(row.template lane_mass<false>(v[i], c + 32 * i, weigh, kept), c + 32 * i, total);
+      });
+    }
     if (threadIdx.x % 32 == 0) atomicAdd(&shared().cta_q, total);
   }
 
@@ -480,42 +474,43 @@ struct Row {
 
   // ---- thresholds
 
-  // Elements from low to below high, and from the floor on, to the first CTA's list; with kKeep the masses of those from
-  // high on, from the floor on and of at least min_p, to the parts.  kFree: there is no floor.
-  template <bool kKeep, bool kFree>
+  // The elements of a bin of the level, its values from low to below high, from the floor on, to the first CTA's list; with
+  // min_p >= 0 the masses of those from high on, from the floor on and of at least min_p, to the parts.  kFree: min_p >= 0
+  // and there is no floor.
+  template <bool kFree>
   __device__ __forceinline__ void collect_bin(const Weigher& weigh, Floor floor, float low, float high, float min_p) {
     int* count = group.at(&shared().count, 0);
     u64* list = group.at(shared().list, 0);
-    const int shift = part_shift(s.n);
+    const bool keep = kFree || min_p >= 0.0f;
     u64 total = 0;
     s.sweep([&](const uint4 (&v)[4], int c) {
       ChunkMax<T, false> top;
       top.add(v);
       if (!__any_sync(~0u, top.value() >= low)) return;
-      LaneMass sum = {0, 0};
       uint32_t in_bin = 0;  // a bit for each element
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         float z[E];
         unpack<T>(v[i], z);
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (z[e] >= low && !(z[e] >= high)) in_bin |= 1u << (E * i + e);
+        if (!keep) continue;
+        LaneMass sum = {0, 0};
         const int i0 = s.first(c + 32 * i);
 #pragma unroll
         for (int e = 0; e < E; e += 2) {
-          if (kKeep) {
-            const float2 y = weigh.exponents(z[e], z[e + 1]);
-            const float2 w = make_float2(exp2_32(y.x), exp2_32(y.y));
-            const Parts2 q(w);
-#pragma unroll
-            for (int o = 0; o < 2; ++o)
-              if (z[e + o] >= high && (o ? w.y : w.x) >= min_p && (kFree || floor.in(z[e + o], i0 + e + o))) {
-                sum.high += q.high[o] - kHighBits;
-                sum.low += q.low[o] - kOnesBits;
-              }
-          }
+          const float2 y = weigh.exponents(z[e], z[e + 1]);
+          const float2 w = make_float2(exp2_32(y.x), exp2_32(y.y));
+          const Parts2 q(w);
 #pragma unroll
           for (int o = 0; o < 2; ++o)
-            if (z[e + o] >= low && z[e + o] < high) in_bin |= 1u << (E * i + e + o);
+            if (z[e + o] >= high && (o ? w.y : w.x) >= min_p && (kFree || floor.in(z[e + o], i0 + e + o))) {
+              sum.high += q.high[o] - kHighBits;
+              sum.low += q.low[o] - kOnesBits;
+            }
         }
+        add_part(sum, c + 32 * i, total);
       }
       for (; in_bin; in_bin &= in_bin - 1) {
         const int bit = __ffs(in_bin) - 1, index = s.first(c + 32 * (bit / E)) + bit % E;
@@ -524,16 +519,13 @@ struct Row {
         const int at = atomicAdd(count, 1);
         if (at < kListMax) list[at] = order_key(z, index);
       }
-      if (kKeep) {
-        __syncwarp();
-        add_part(sum, c, shift, total);
-      }
+      __syncwarp();
     });
-    if (kKeep && threadIdx.x % 32 == 0 && total) atomicAdd(&shared().cta_q, total);
+    if (keep && threadIdx.x % 32 == 0 && total) atomicAdd(&shared().cta_q, total);
   }
 
   // One level of a threshold's search: kBins bins, evenly spaced in the exponent, that go down the order.  Bin 0 has what
-  // is above, the last bin what is below; of the row's values only those from low to below high count.
+  // is above, the last bin what is below; of the row's values only those from low to below high (NaN: all) count.
   struct Level {
     float from, scale;
     float low, high;
@@ -541,7 +533,7 @@ struct Row {
       const float x = fminf(fmaxf((-y - from) * scale, 0.0f), (float)(kBins - 1));
       return (int)(__float_as_uint(x + kOnes) - kOnesBits);
     }
-    __device__ __forceinline__ bool has(float z) const { return z >= low && z < high; }
+    __device__ __forceinline__ bool has(float z) const { return z >= low && !(z >= high); }
     // the level that resolves bin b, whose values are from `l` to below `h`
     __device__ __forceinline__ void enter(int b, float l, float h) {
       low = l;
@@ -556,35 +548,41 @@ struct Row {
     }
   };
 
-  // One warp: the lowest of the level's values whose bin is at most b, or the level's end.  The bins do not increase with
-  // the value; 32 values are tried at a time.
-  __device__ __noinline__ static float lowest_of_bin(Weigher weigh, Level level, int b) {
-    const uint32_t lane = threadIdx.x % 32;
+  // One warp: the lowest of the level's values whose bin is at most b, to the lower half of the lanes, and the lowest whose
+  // bin is less, to the upper half (the level's end where there is none).  The bins do not increase with the value; each
+  // half tries sixteen values at a time.
+  __device__ __noinline__ static float ends_of_bin(Weigher weigh, Level level, int b) {
+    const uint32_t lane = threadIdx.x % 32, part = lane % 16;
+    const int shift = lane < 16 ? 0 : 16;
+    if (shift) --b;
     const auto in = [&](uint32_t key) { return level.bin(weigh.exponent(key_value(key))) <= b; };
     uint32_t lo = value_key(level.low), hi = level.high <= weigh.m ? value_key(level.high) - 1 : value_key(weigh.m);
-    if (!in(hi)) return level.high;
-    while (lo < hi) {  // the answer is in [lo, hi]
-      const uint32_t step = (hi - lo) / 32 + 1;
-      const uint32_t hit = __ballot_sync(~0u, in(min(lo + lane * step, hi)));
-      if (!hit) {
-        lo = min(lo + 31 * step, hi - 1) + 1;
-      } else {
-        const int first = __ffs(hit) - 1;
-        hi = min(lo + first * step, hi);
-        lo = first ? lo + (first - 1) * step + 1 : hi;
+    const bool none = !in(hi);
+    if (none) lo = hi;
+    while (__any_sync(~0u, lo < hi)) {  // the answer is in [lo, hi]
+      const uint32_t step = (hi - lo) / 16 + 1;
+      const uint32_t hit = __ballot_sync(~0u, in(min(lo + part * step, hi))) >> shift & 0xffffu;
+      if (lo < hi) {
+        if (!hit) {
+          lo = min(lo + 15 * step, hi - 1) + 1;
+        } else {
+          const int first = __ffs(hit) - 1;
+          hi = min(lo + first * step, hi);
+          lo = first ? lo + (first - 1) * step + 1 : hi;
+        }
       }
     }
-    return key_value(lo);
+    return none ? level.high : key_value(lo);
   }
 
   // After a barrier, in one warp: the bin of the cluster's histograms at which the running total passes t, and the rest
   // of t within it, to shared().found and shared().before; all ones for histograms of nothing.  t may be given as a share of all.
-  template <bool kMass>
-  __device__ __forceinline__ void find_bin(u64 t, bool share) const {
+  __device__ __forceinline__ void find_bin(u64 t, bool share, bool mass) const {
     static_assert(kGroups == 64, "two groups of bins a lane");
     const int lane = (int)threadIdx.x % 32;
     const unsigned ctas = group.n;
     u64 x0 = 0, x1 = 0;
+#pragma unroll 1
     for (unsigned r = 0; r < ctas; ++r) {
       const Histogram* h = group.at(&shared().bins, r);
       x0 += h->group[2 * lane];
@@ -592,7 +590,7 @@ struct Row {
     }
     u64 upto = warp_scan(x0 + x1);
     const u64 all = __shfl_sync(~0u, upto, 31);
-    if (share) t = kMass ? share24(t, all) - 1 : min(t, all - 1);
+    if (share) t = mass ? share24(t, all) - 1 : min(t, all - 1);
     int g = min(__popc(__ballot_sync(~0u, upto <= t)), 31);
     u64 ahead = __shfl_sync(~0u, upto - x0 - x1, g);
     const u64 half = __shfl_sync(~0u, x0, g);
@@ -602,6 +600,7 @@ struct Row {
       ++g;
     }
     u64 x = 0;
+#pragma unroll 1
     for (unsigned r = 0; r < ctas; ++r) x += group.at(&shared().bins, r)->mass(32 * g + lane);
     upto = ahead + warp_scan(x);
     const int l = min(__popc(__ballot_sync(~0u, upto <= t)), 31);
@@ -614,18 +613,41 @@ struct Row {
 
   // The list's first n keys into descending order.
   __device__ __noinline__ static void sort_list(int n) {
-    int size = 2;
+    u64* list = shared().list;
+    int size = 32;
     while (size < n) size *= 2;
-    for (int i = n + (int)threadIdx.x; i < size; i += (int)blockDim.x) shared().list[i] = 0;
+    if (size <= (int)blockDim.x) {  // a key a thread; exchanges within a warp by shuffles
+      const int i = threadIdx.x;
+      u64 key = i < n ? list[i] : 0;
+      for (int k = 2; k <= size; k *= 2)
+        for (int d = k / 2; d; d /= 2) {
+          u64 other;
+          if (d < 32) {
+            other = __shfl_xor_sync(~0u, key, d);
+          } else {
+            __syncthreads();
+            if (i < size) list[i] = key;
+            __syncthreads();
+            other = list[(i ^ d) % size];
+          }
+          // the lower place of a descending run takes the larger key
+          if (((i & k) == 0) == ((i & d) == 0) ? other > key : other < key) key = other;
+        }
+      __syncthreads();
+      if (i < size) list[i] = key;
+      __syncthreads();
+      return;
+    }
+    for (int i = n + threadIdx.x; i < size; i += (int)blockDim.x) list[i] = 0;
     for (int k = 2; k <= size; k *= 2)
       for (int d = k / 2; d; d /= 2) {
         __syncthreads();
-        for (int t = (int)threadIdx.x; t < size / 2; t += (int)blockDim.x) {
+        for (int t = threadIdx.x; t < size / 2; t += (int)blockDim.x) {
           const int i = 2 * t - (t & (d - 1));
-          const u64 a = shared().list[i], b = shared().list[i + d];
+          const u64 a = list[i], b = list[i + d];
           if ((a < b) == ((i & k) == 0)) {
-            shared().list[i] = b;
-            shared().list[i + d] = a;
+            list[i] = b;
+            list[i + d] = a;
           }
         }
       }
@@ -633,66 +655,58 @@ struct Row {
   }
 
   // The key of the element, among those from the floor on, at which the running total of the order passes the target:
-  // with kMass totals are masses and the target floor(arg all / 2^24) - 1, else they are counts and it is arg (or the
+  // with `mass` totals are masses and the target floor(arg all / 2^24) - 1, else they are counts and it is arg (or the
   // last).  All ones for a row without elements.  A histogram over evenly spaced exponents finds the bin; where it has
-  // more elements than a list, the next one cuts it again; the first CTA sorts the bin's elements.  Rows of many equal
-  // values go by radix selection.
-  // With min_p >= 0 the masses of the kept tokens (from the threshold on, of at least min_p) are left by part and by warp
-  // as masses() leaves them, a cluster barrier included.
-  template <bool kMass>
-  __device__ __noinline__ static u64 select(Row row, Weigher weigh, Floor floor, u64 arg, float min_p) {
-    return row.template threshold<kMass>(weigh, floor, arg, min_p);
+  // more elements than a list, the next one cuts it again; the first CTA sorts the bin's elements.  What still does not
+  // fit, many equal values, is told apart by eight bits of the keys at a time.
+  // With min_p >= 0 the masses of the kept tokens (from the threshold on, of at least min_p) are left by part and by CTA
+  // as masses() leaves them, a barrier of the group included.
+  __device__ __noinline__ static u64 threshold(Row row, Weigher weigh, Floor floor, u64 arg, bool mass, float min_p) {
+    return row.find_threshold(weigh, floor, arg, mass, min_p);
   }
-  template <bool kMass>
-  __device__ __forceinline__ u64 threshold(const Weigher& weigh, Floor floor, u64 arg, float min_p) {
+  __device__ __forceinline__ u64 find_threshold(const Weigher& weigh, Floor floor, u64 arg, bool mass, float min_p) {
     const int lane = (int)threadIdx.x % 32, warps = (int)blockDim.x / 32, warp = warp_index();
-    int* count = group.at(&shared().count, 0);
     const bool keep = min_p >= 0.0f, free = floor.z == -CUDART_INF_F;
-    const bool fits = (long long)per_cta * E <= kSliceElems && weigh.m < CUDART_INF_F;
-    u64 t = arg;
-    Level level{0.0f, kBinsPerUnit, -CUDART_MAX_NORMAL_F, CUDART_INF_F};
-    int n = kListMax + 1;
-    for (int depth = 0; depth < kLevels && fits; ++depth) {
-      // the cluster's CTAs have left the memory of the bins and the count behind: a barrier is above
+    Level level{0.0f, kBinsPerUnit, -CUDART_MAX_NORMAL_F, CUDART_NAN_F};
+    if (weigh.m == CUDART_INF_F) level.low = -CUDART_INF_F;
+    u64 t = arg, prefix = 0;
+    int shift = 64;  // digits of the keys from here on are found
+    int depth = weigh.m == CUDART_INF_F ? kLevels : 0;
+    bool first = true;
+    group.sync();
+#pragma unroll 1
+    for (;; ++depth) {
+      // the group's CTAs have left the memory of the bins and the count behind: a barrier is above
+      const bool digits = depth >= kLevels;
+      if (digits) {
+        shift -= 8;
+        if (shift < 32 && shift > 0 && s.V > 0 && (uint32_t)(s.V - 1) >> shift == 0) {
+          prefix |= 0xffull << shift;  // every index has these bits clear
+          continue;
+        }
+      }
       for (int i = (int)threadIdx.x; i < kBins; i += (int)blockDim.x) shared().bins.low[i] = shared().bins.high[i] = 0;
       if (threadIdx.x == 0) shared().count = 0;
       __syncthreads();
-      if (kMass && depth == 0 && !special) {
-        s.sweep([&](const uint4 (&v)[4], int c) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            float z[E];
-            unpack<T>(v[i], z);
-            const int i0 = s.first(c + 32 * i);
-#pragma unroll
-            for (int e = 0; e < E; e += 2) {
-              const float2 y = weigh.exponents(z[e], z[e + 1]);
-              const Parts2 q(make_float2(exp2_32(y.x), exp2_32(y.y)));
-              const float2 b = fma2(y, make_float2(-kBinsPerUnit, -kBinsPerUnit), make_float2(kOnes, kOnes));
-              // a mass above 0 has an exponent above -32: its bin needs no bound
-#pragma unroll
-              for (int o = 0; o < 2; ++o) {
-                const uint32_t high = q.high[o] - kHighBits, low = q.low[o] - kOnesBits;
-                const uint32_t bin = __float_as_uint(o ? b.y : b.x) - kOnesBits;
-                const bool in = free || floor.in(z[e + o], i0 + e + o);
-                add_shared(&shared().bins.low[bin], in ? low : 0);
-                add_shared(&shared().bins.high[bin], in ? high : 0);
-              }
-            }
-          }
-        });
+      if (first && !digits && !special) {
+        if (mass)
+          count_masses(weigh, floor, free);
+        else
+          count_elements(weigh, floor, level);
       } else {
         each([&](float z, int i) {
           if (!level.has(z) || !floor.in(z, i)) return;
-          const float y = weigh.exponent(z);
-          const int b = level.bin(y);
-          if (kMass) {
-            const uint32_t q = grid_mass(exp2_32(y));
-            if (q & 0x7fffu) atomicAdd(&shared().bins.low[b], q & 0x7fffu);
-            if (q >> 15) atomicAdd(&shared().bins.high[b], q >> 15);
+          int b;
+          if (digits) {
+            const u64 key = order_key(z, i);
+            if (shift < 56 && (key ^ prefix) >> (shift + 8)) return;
+            b = 255 - (int)(key >> shift & 255);
           } else {
-            atomicAdd(&shared().bins.low[b], 1u);
+            b = level.bin(weigh.exponent(z));
           }
+          const uint32_t q = mass ? grid_mass(weigh(z)) : 1u;
+          add_shared(&shared().bins.low[b], q & 0x7fffu);
+          add_shared(&shared().bins.high[b], q >> 15);
         });
       }
       __syncthreads();
@@ -702,17 +716,15 @@ struct Row {
       }
       group.sync();
       if (warp == 0) {  // every CTA for itself
-        find_bin<kMass>(t, depth == 0);
+        find_bin(t, first, mass);
         __syncwarp();
-        if (shared().found != ~0ull) {
-          const int bin = (int)shared().found;
-          const float low = lowest_of_bin(weigh, level, bin), high = bin ? lowest_of_bin(weigh, level, bin - 1) : level.high;
-          if (lane == 0) {
-            shared().bin_low = low;
-            shared().bin_high = high;
-          }
+        if (!digits && shared().found != ~0ull) {
+          const float end = ends_of_bin(weigh, level, (int)shared().found);
+          if (lane == 0) shared().bin_low = end;
+          if (lane == 16) shared().bin_high = end;
         }
       }
+      first = false;
       __syncthreads();
       if (shared().found == ~0ull) {
         if (threadIdx.x == 0) shared().cta_q = 0;
@@ -720,51 +732,103 @@ struct Row {
         return ~0ull;
       }
       const int bin = (int)shared().found;
-      const float low = shared().bin_low, high = shared().bin_high;
       t = shared().before;
-      // the bin's elements, from low to below high, to the list; the mass of what is above to the parts
+      if (digits) {
+        prefix |= (u64)(255 - bin) << shift;
+        if (shift == 0) break;
+        group.sync();  // all have read the bins
+        continue;
+      }
+      const float low = shared().bin_low, high = shared().bin_high;
       if (keep) clear_parts();
       __syncthreads();
-      if (keep) {
-        if (free)
-          collect_bin<true, true>(weigh, floor, low, high, min_p);
-        else
-          collect_bin<true, false>(weigh, floor, low, high, min_p);
-      } else {
-        collect_bin<false, false>(weigh, floor, low, high, min_p);
-      }
+      if (free && keep)
+        collect_bin<true>(weigh, floor, low, high, min_p);
+      else
+        collect_bin<false>(weigh, floor, low, high, min_p);
       group.sync();
-      n = *count;
-      if (n <= kListMax) break;
+      const int n = *group.at(&shared().count, 0);
+      if (n <= kListMax) return by_list(n, weigh, t, mass, min_p);
       level.enter(bin, low, high);
       group.sync();  // all have seen the count
     }
-    if (n > kListMax) {
-      const u64 key = radix_select<kMass>(*this, weigh, floor, arg);
-      if (keep) {
-        masses(*this, weigh, Kept{floor_of(key), min_p});
-        group.sync();
-      }
-      return key;
-    }
-    if (group.rank == 0) {
-      sort_list(n);
-      // the running total down the list, by one warp
-      if (warp == 0) {
-        u64 upto = 0;
-        for (int i0 = 0; i0 < n; i0 += 32) {
-          const u64 key = i0 + lane < n ? shared().list[i0 + lane] : 0;
-          const u64 q = i0 + lane >= n ? 0 : kMass ? grid_mass(weigh(order_value(key))) : 1u;
-          const u64 sum = upto + warp_scan(q);
-          if (sum - q <= t && t < sum) {
-            shared().found = key;
-            shared().last = i0 + lane;
+    if (keep) masses(*this, weigh, Kept{floor_of(prefix), min_p});
+    group.sync();
+    return prefix;
+  }
+
+  // the first histogram, of masses
+  __device__ __forceinline__ void count_masses(const Weigher& weigh, Floor floor, bool free) const {
+    s.sweep([&](const uint4 (&v)[4], int c) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float z[E];
+        unpack<T>(v[i], z);
+        const int i0 = s.first(c + 32 * i);
+#pragma unroll
+        for (int e = 0; e < E; e += 2) {
+          const float2 y = weigh.exponents(z[e], z[e + 1]);
+          const Parts2 q(make_float2(exp2_32(y.x), exp2_32(y.y)));
+          const float2 b = fma2(y, make_float2(-kBinsPerUnit, -kBinsPerUnit), make_float2(kOnes, kOnes));
+          // a mass above 0 has an exponent above -32: its bin needs no bound
+#pragma unroll
+          for (int o = 0; o < 2; ++o) {
+            const uint32_t high = q.high[o] - kHighBits, low = q.low[o] - kOnesBits;
+            const uint32_t bin = __float_as_uint(o ? b.y : b.x) - kOnesBits;
+            const bool in = free || floor.in(z[e + o], i0 + e + o);
+            add_shared(&shared().bins.low[bin], in ? low : 0);
+            add_shared(&shared().bins.high[bin], in ? high : 0);
           }
-          upto = __shfl_sync(~0u, sum, 31);
         }
       }
-      __syncthreads();
+    });
+  }
+
+  // the first histogram, of counts
+  __device__ __forceinline__ void count_elements(const Weigher& weigh, Floor floor, const Level& level) const {
+    s.sweep([&](const uint4 (&v)[4], int c) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float z[E];
+        unpack<T>(v[i], z);
+        const int i0 = s.first(c + 32 * i);
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          add_shared(&shared().bins.low[level.bin(weigh.exponent(z[e]))], floor.in(z[e], i0 + e) ? 1u : 0u);
+      }
+    });
+  }
+
+  // The rest of a threshold's search, in the n elements of the first CTA's list.
+  __device__ __forceinline__ u64 by_list(int n, const Weigher& weigh, u64 t, bool mass, float min_p) {
+    const int lane = (int)threadIdx.x % 32, warps = (int)blockDim.x / 32, warp = warp_index();
+    const bool keep = min_p >= 0.0f;
+    if (group.rank == 0) {
+      sort_list(n);
+      // the running total down the list
+      u64 ahead = 0;
+#pragma unroll 1
+      for (int i0 = 0; i0 < n; i0 += (int)blockDim.x) {
+        const int i = i0 + (int)threadIdx.x;
+        const u64 key = i < n ? shared().list[i] : 0;
+        const u64 q = i >= n ? 0 : mass ? grid_mass(weigh(order_value(key))) : 1u;
+        const u64 upto = warp_scan(q);
+        if (lane == 31) shared().warp_q[warp] = upto;
+        __syncthreads();
+        u64 before = ahead;
+#pragma unroll 1
+        for (int w = 0; w < warps; ++w) {
+          if (w < warp) before += shared().warp_q[w];
+          ahead += shared().warp_q[w];
+        }
+        if (before + upto - q <= t && t < before + upto) {
+          shared().found = key;
+          shared().last = i;
+        }
+        __syncthreads();
+      }
       if (keep)
+#pragma unroll 1
         for (int i = (int)threadIdx.x; i <= shared().last; i += (int)blockDim.x) {
           const u64 key = shared().list[i];
           const float w = weigh(order_value(key));
@@ -772,7 +836,7 @@ struct Row {
           // the element's CTA and part
           const int c = (order_index(key) + s.head) / E, r = c / per_cta, at = c - r * per_cta;
           const u64 q = grid_mass(w);
-          atomicAdd(group.at(&shared().parts[(at / kBatch) >> part_shift(slice_chunks(r))], r), q);
+          atomicAdd(group.at(&shared().parts[part_at(at / 32)], r), q);
           atomicAdd(group.at(&shared().cta_q, r), q);
         }
     }
@@ -780,70 +844,6 @@ struct Row {
     const u64 key = *group.at(&shared().found, 0);
     if (!keep) group.sync();  // found and the list may be written again
     return key;
-  }
-
-  // chunks of CTA r's slice
-  __device__ int slice_chunks(int r) const {
-    const int total = s.V ? (s.head + s.V - 1) / E + 1 : 0;
-    return min(max(total - r * per_cta, 0), per_cta);
-  }
-
-  // The same by eight bits of the keys at a time.
-  template <bool kMass>
-  __device__ __noinline__ static u64 radix_select(Row row, Weigher weigh, Floor floor, u64 arg) {
-    return row.template radix<kMass>(weigh, floor, arg);
-  }
-  template <bool kMass>
-  __device__ __forceinline__ u64 radix(const Weigher& weigh, Floor floor, u64 arg) {
-    u64 prefix = 0, before = 0, t = 0;
-    int parity = 0;
-    group.sync();
-    for (int shift = 56; shift >= 0; shift -= 8) {
-      if (shift < 32 && shift > 0 && s.V > 0 && (uint32_t)(s.V - 1) >> shift == 0) {
-        prefix |= 0xffull << shift;  // every index has these bits clear
-        continue;
-      }
-      u64* hist = shared().radix[parity];
-      for (int i = (int)threadIdx.x; i < 256; i += (int)blockDim.x) hist[i] = 0;
-      __syncthreads();
-      each([&](float z, int i) {
-        const u64 key = order_key(z, i);
-        if (floor.in(z, i) && (shift == 56 || (key ^ prefix) >> (shift + 8) == 0)) {
-          const u64 add = kMass ? (u64)grid_mass(weigh(z)) : 1ull;
-          if (add) atomicAdd(&hist[(key >> shift) & 255], add);
-        }
-      });
-      group.sync();
-      if (threadIdx.x < 32) {
-        // lane l holds bins 255 - 8 l downwards: a scan over lanes is a scan down the order
-        u64 b[8], sum = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          b[i] = 0;
-          for (unsigned r = 0; r < group.n; ++r)
-            b[i] += *group.at(&hist[255 - 8 * (int)threadIdx.x - i], r);
-          sum += b[i];
-        }
-        const u64 upto = before + warp_scan(sum);
-        const u64 all = __shfl_sync(~0u, upto, 31) - before;
-        if (shift == 56) t = kMass ? share24(arg, all) - 1 : min(arg, all - 1);
-        if (all && upto - sum <= t && t < upto) {
-          u64 at = upto - sum;
-          int i = 0;
-          while (at + b[i] <= t) at += b[i++];
-          shared().found = prefix | (u64)(255 - 8 * (int)threadIdx.x - i) << shift;
-          shared().before = at;
-        }
-        if (!all && threadIdx.x == 0) shared().found = ~0ull;
-      }
-      __syncthreads();
-      prefix = shared().found;
-      before = shared().before;
-      parity ^= 1;
-      if (prefix == ~0ull) break;
-    }
-    group.sync();
-    return prefix;
   }
 
   // ---- draws
@@ -854,54 +854,41 @@ struct Row {
   }
   __device__ __forceinline__ void find_token(u64 t, const Weigher& weigh, const Kept& kept, u64 all, int32_t* tok,
                                              float* prob) const {
-    const int lane = (int)threadIdx.x % 32, shift = part_shift(s.n);
-    const int parts = ((s.n + kBatch - 1) / kBatch + (1 << shift) - 1) >> shift, per = (parts + 31) / 32;
+    const int lane = (int)threadIdx.x % 32;
+    const int parts = (s.n + 31) / 32, per = (parts + 31) / 32;  // parts of a lane
     u64 sum = 0;
-    for (int i = 0; i < per; ++i) sum += shared().parts[min(lane * per + i, kParts - 1)];  // past the last all are 0
+#pragma unroll 4
+    for (int i = 0; i < per; ++i) sum += lane * per + i < parts ? shared().parts[part_at(lane * per + i)] : 0;
     u64 upto = warp_scan(sum);
     const int l = min(__popc(__ballot_sync(~0u, upto <= t)), 31);
     t -= __shfl_sync(~0u, upto - sum, l);
-    int p = l * per;
-    while (p < l * per + per - 1 && t >= shared().parts[p]) t -= shared().parts[p++];
-    for (int c0 = (p << shift) * kBatch + lane; c0 - lane < s.n; c0 += kBatch) {
-      uint4 v[4];
-      u64 q[4];
+    sum = lane < per && l * per + lane < parts ? shared().parts[part_at(l * per + lane)] : 0;
+    upto = warp_scan(sum);
+    const int p = min(__popc(__ballot_sync(~0u, upto <= t)), 31);
+    t -= __shfl_sync(~0u, upto - sum, p);
+    const int c = (l * per + p) * 32 + lane, i0 = s.first(c);
+    float z[E];
+    unpack<T>(s.chunk(c), z);
+    uint32_t q[E];
+    sum = 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = s.chunk(c0 + 32 * i);
-      bool found = false;
+    for (int e = 0; e < E; ++e) sum += q[e] = kept_mass(z[e], i0 + e, weigh, kept);
+    upto = warp_scan(sum);
+    if (t < upto - sum || t >= upto) return;
+    t -= upto - sum;
+    // this lane's chunk has the token
+    float value = 0.0f;
+    int at = -1;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        q[i] = chunk_mass(v[i], c0 + 32 * i, weigh, kept);
-        const u64 all32 = __reduce_add_sync(~0u, (uint32_t)q[i] & 0xffffffu) +
-                          ((u64)__reduce_add_sync(~0u, (uint32_t)(q[i] >> 24)) << 24);
-        if (found) continue;
-        if (t >= all32) {
-          t -= all32;
-          continue;
-        }
-        found = true;
-        upto = warp_scan(q[i]);
-        if (t < upto - q[i] || t >= upto) continue;
-        t -= upto - q[i];
-        float z[E];
-        unpack<T>(v[i], z);
-        const int i0 = s.first(c0 + 32 * i);
-        float hit = 0.0f;
-        int at = -1;
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const uint32_t x = kept_mass(z[e], i0 + e, weigh, kept);
-          if (at < 0 && t < x) {
-            at = e;
-            hit = z[e];
-          }
-          t -= at < 0 ? x : 0;
-        }
-        *tok = i0 + at;
-        *prob = weigh(hit) * kGrid / (float)all;
+    for (int e = 0; e < E; ++e) {
+      if (at < 0 && t < q[e]) {
+        at = e;
+        value = z[e];
       }
-      if (found) break;
+      t -= at < 0 ? q[e] : 0;
     }
+    *tok = i0 + at;
+    *prob = weigh(value) * kGrid / (float)all;
   }
 
   // the first CTA: draws from the top-k list that settle() left
@@ -1059,6 +1046,8 @@ struct Sample {
     if (top_k <= 0 || top_k > a.rows.V) top_k = a.rows.V;
     const bool by_list = top_k <= kMaxK;
     const float* u = a.u + (long long)r * a.S;
+    const int warp = warp_index(), warps = (int)blockDim.x / 32;
+    const float first_u = warp < a.S ? u[warp] : 0.0f;  // on its way during the passes
     int32_t* tok = a.tok + (long long)r * a.S;
     float* prob = a.prob + (long long)r * a.S;
     Weigher weigh;
@@ -1079,16 +1068,16 @@ struct Sample {
     const bool by_mass = p24 < (1u << 24);
     Kept kept{no_floor(), fmaxf(min_p, 0.0f)};
     if (top_k < a.rows.V)
-      kept.floor = floor_of(Row<T>::template select<false>(row, weigh, kept.floor, top_k - 1, by_mass ? -1.0f : kept.min_p));
-    if (by_mass) kept.floor = floor_of(Row<T>::template select<true>(row, weigh, kept.floor, p24, kept.min_p));
+      kept.floor = floor_of(Row<T>::threshold(row, weigh, kept.floor, top_k - 1, false, by_mass ? -1.0f : kept.min_p));
+    if (by_mass) kept.floor = floor_of(Row<T>::threshold(row, weigh, kept.floor, p24, true, kept.min_p));
     if (top_k == a.rows.V && !by_mass) {
       Row<T>::masses(row, weigh, kept);
       row.group.sync();
     }
     u64 mine, ahead;
     const u64 all = row.all_mass(&mine, &ahead);
-    for (int i = warp_index(); i < a.S; i += (int)blockDim.x / 32) {
-      const float x = u[i];
+    for (int i = warp; i < a.S; i += warps) {
+      const float x = i == warp ? first_u : u[i];
       if (all == 0 || !(x >= 0.0f && x <= 1.0f)) {
         if (row.group.rank == 0 && lane == 0) {
           tok[i] = -1;
@@ -1146,7 +1135,7 @@ epic_status epic_propose_topk(const void* d_logits, int32_t dtype, int32_t B, in
   if (K < 0) return EPIC_ERR_INVALID_ARG;
   epic_status s = check_rows(d_logits, dtype, B, n, V, stride_b, stride_n, d_pos, k);
   if (s != EPIC_OK) return s;
-  if (K > kMaxK) return EPIC_ERR_CAPACITY;
+  if (K > kMaxK || V > kMaxV) return EPIC_ERR_CAPACITY;
   const long long rows = (long long)B * k;
   if (rows == 0 || K == 0) return EPIC_OK;
   if (!d_cand || !d_conf) return EPIC_ERR_INVALID_ARG;
@@ -1167,6 +1156,7 @@ epic_status epic_sample_tokens(const void* d_logits, int32_t dtype, int32_t B, i
   if (S < 0) return EPIC_ERR_INVALID_ARG;
   epic_status s = check_rows(d_logits, dtype, B, n, V, stride_b, stride_n, d_pos, k);
   if (s != EPIC_OK) return s;
+  if (V > kMaxV) return EPIC_ERR_CAPACITY;
   const long long rows = (long long)B * k;
   if (rows == 0 || S == 0) return EPIC_OK;
   if (!d_u || !d_tok || !d_prob) return EPIC_ERR_INVALID_ARG;
