@@ -38,18 +38,24 @@ epic_status check_rows(const void* logits, int dtype, int B, int n, int V, int64
 
 epic_status launch_rows(const void* kernel, const RowShape& p, long long rows, void* args, cudaStream_t st) {
   if (rows > 0x7fffffffll / p.ctas) return EPIC_ERR_CAPACITY;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(rows * p.ctas));
-  cfg.blockDim = dim3(p.threads);
-  cfg.stream = st;
-  cudaLaunchAttribute at = {};
-  at.id = cudaLaunchAttributeClusterDimension;
-  at.val.clusterDim.x = p.ctas;
-  at.val.clusterDim.y = at.val.clusterDim.z = 1;
-  cfg.attrs = &at;
-  cfg.numAttrs = 1;
   void* argv[] = {args};
-  if (cudaLaunchKernelExC(&cfg, kernel, argv) != cudaSuccess) {
+  cudaError_t e;
+  if (p.ctas == 1) {
+    e = cudaLaunchKernel(kernel, dim3((unsigned)rows), dim3(p.threads), argv, 0, st);
+  } else {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(rows * p.ctas));
+    cfg.blockDim = dim3(p.threads);
+    cfg.stream = st;
+    cudaLaunchAttribute at = {};
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim.x = p.ctas;
+    at.val.clusterDim.y = at.val.clusterDim.z = 1;
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    e = cudaLaunchKernelExC(&cfg, kernel, argv);
+  }
+  if (e != cudaSuccess) {
     cudaGetLastError();
     return EPIC_ERR_CUDA;
   }

@@ -364,11 +364,28 @@ def extract_witness(g: Grammar, t: LexTable, x, terms, lengths, stream=None):
 
 
 # ---------------------------------------------------------------- rows of logits
+# A small call takes the GPU 5 us, so its marshalling is kept short: no imports, stream objects or
+# attribute chains that can be had once.
+
+_DTYPES = {}  # torch dtype of logits -> the C-ABI's code; filled on the first call
+_T = None     # torch, and what the calls need of it
+_raw_stream = None
+
+
+def _logits_init():
+    global _T, _raw_stream
+    import torch
+    _DTYPES.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2})
+    _raw_stream = getattr(torch._C, '_cuda_getCurrentRawStream', None) or (
+        lambda device: torch.cuda.current_stream(device).cuda_stream)
+    _T = (torch.float32, torch.int32, torch.uint8)
+
 
 def _rows(logits):
     """(address, dtype, B, n, V, strides) of logits [B][n][V]; the last dimension has unit stride, the others any."""
-    import torch
-    code = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}.get(logits.dtype)
+    if _T is None:
+        _logits_init()
+    code = _DTYPES.get(logits.dtype)
     if code is None:
         raise ValueError('expected float32, float16 or bfloat16 logits, got %s' % logits.dtype)
     if not logits.is_cuda:
@@ -382,14 +399,23 @@ def _rows(logits):
     return logits.data_ptr(), code, B, n, V, sb, sn
 
 
-def _arg(t, shape, dtype, name):
-    """Device pointer of a contiguous tensor of that shape and type (None stays None)."""
+def _arg(t, shape, dtype, name, device):
+    """Device pointer of a contiguous tensor of that shape, type and device (None stays None)."""
     if t is None:
         return None
     if t.shape != shape or t.dtype != dtype:
         raise ValueError('%s: expected %s of shape %s, got %s of shape %s' % (name, dtype, tuple(shape), t.dtype,
                                                                              tuple(t.shape)))
-    return _ptr(t)
+    if t.device != device or not t.is_contiguous():
+        raise ValueError('%s: expected a contiguous tensor on %s' % (name, device))
+    return t.data_ptr()
+
+
+def _on(device, stream):
+    """The stream of a call on that device's tensors (None: the device's current one)."""
+    if stream is None:
+        return _raw_stream(device.index)
+    return stream if isinstance(stream, int) else stream.cuda_stream
 
 
 def propose_topk(logits, cand, conf, pos=None, temperature=None, stream=None):
@@ -397,13 +423,16 @@ def propose_topk(logits, cand, conf, pos=None, temperature=None, stream=None):
     of logits [B][n][V] and their softmax probabilities, into cand [B][k][K]
     int32 and conf [B][k][K] float32.  pos [B][k] int32 (None: the first k);
     temperature [B] float32 (None: 1)."""
-    import torch
     rows = _rows(logits)
-    B, k, K = cand.shape
-    _check(load().epic_propose_topk(
-        *rows, _arg(pos, (B, k), torch.int32, 'pos'), k, _arg(temperature, rows[2:3], torch.float32, 'temperature'), K,
-        _arg(cand, (rows[2], k, K), torch.int32, 'cand'), _arg(conf, (B, k, K), torch.float32, 'conf'),
-        _stream(stream)), 'epic_propose_topk')
+    f32, i32, _ = _T
+    device = logits.device
+    B = rows[2]
+    k, K = cand.shape[1:]
+    shape = (B, k, K)
+    _check((_lib or load()).epic_propose_topk(
+        *rows, _arg(pos, (B, k), i32, 'pos', device), k, _arg(temperature, (B,), f32, 'temperature', device), K,
+        _arg(cand, shape, i32, 'cand', device), _arg(conf, shape, f32, 'conf', device), _on(device, stream)),
+        'epic_propose_topk')
 
 
 def sample_tokens(logits, u, tok, prob, pos=None, temperature=None, top_k=None, top_p=None, min_p=None, stream=None):
@@ -411,30 +440,29 @@ def sample_tokens(logits, u, tok, prob, pos=None, temperature=None, top_k=None, 
     [B][n][V] for every given number u [B][k][S] float32 of [0, 1], into tok
     [B][k][S] int32 and prob [B][k][S] float32.  The rules are [B] tensors
     (float32, top_k int32) or None (off)."""
-    import torch
     rows = _rows(logits)
+    f32, i32, _ = _T
+    device = logits.device
     B = rows[2:3]
-    shape = (rows[2],) + tuple(u.shape[1:])
-    k, S = shape[1:]
-    f32, i32 = torch.float32, torch.int32
-    _check(load().epic_sample_tokens(
-        *rows, _arg(pos, shape[:2], i32, 'pos'), k, _arg(temperature, B, f32, 'temperature'),
-        _arg(top_k, B, i32, 'top_k'), _arg(top_p, B, f32, 'top_p'), _arg(min_p, B, f32, 'min_p'),
-        _arg(u, shape, f32, 'u'), S, _arg(tok, shape, i32, 'tok'), _arg(prob, shape, f32, 'prob'),
-        _stream(stream)), 'epic_sample_tokens')
+    k, S = u.shape[1:]
+    shape = (rows[2], k, S)
+    _check((_lib or load()).epic_sample_tokens(
+        *rows, _arg(pos, shape[:2], i32, 'pos', device), k, _arg(temperature, B, f32, 'temperature', device),
+        _arg(top_k, B, i32, 'top_k', device), _arg(top_p, B, f32, 'top_p', device),
+        _arg(min_p, B, f32, 'min_p', device), _arg(u, shape, f32, 'u', device), S, _arg(tok, shape, i32, 'tok', device),
+        _arg(prob, shape, f32, 'prob', device), _on(device, stream)), 'epic_sample_tokens')
 
 
-def _targets(rows, ids, vals, tau, weight, valid):
-    import torch
-    shape = tuple(rows[2:4]) + (ids.shape[-1],)
-    return (_arg(ids, shape, torch.int32, 'ids'), _arg(vals, shape, torch.float32, 'vals'),
-            _arg(valid, shape, torch.uint8, 'valid'), shape[2], tau,
-            _arg(weight, shape[:2], torch.float32, 'weight'))
+def _targets(rows, ids, vals, tau, weight, valid, device):
+    f32, i32, u8 = _T
+    shape = (rows[2], rows[3], ids.shape[-1])
+    return (_arg(ids, shape, i32, 'ids', device), _arg(vals, shape, f32, 'vals', device),
+            _arg(valid, shape, u8, 'valid', device), shape[2], tau, _arg(weight, shape[:2], f32, 'weight', device))
 
 
 def _gradient(logits, grad):
     rows = _rows(grad)
-    if grad.shape != logits.shape or grad.dtype != logits.dtype:
+    if grad.shape != logits.shape or grad.dtype != logits.dtype or grad.device != logits.device:
         raise ValueError('grad: expected %s of shape %s' % (logits.dtype, tuple(logits.shape)))
     return rows[0], rows[5], rows[6]
 
@@ -443,29 +471,30 @@ def distill_forward(logits, ids, vals, loss, lse, tau=1.0, weight=None, valid=No
     """epic_distill_forward: loss and lse [B][n] float32 of student logits
     [B][n][V] against a teacher's entries ids [B][n][K] int32, vals [B][n][K]
     float32; weight [B][n] float32, valid [B][n][K] uint8 (None: all count)."""
-    import torch
     rows = _rows(logits)
-    _check(load().epic_distill_forward(
-        *rows, *_targets(rows, ids, vals, tau, weight, valid), _arg(loss, rows[2:4], torch.float32, 'loss'),
-        _arg(lse, rows[2:4], torch.float32, 'lse'), _stream(stream)), 'epic_distill_forward')
+    f32, device = _T[0], logits.device
+    _check((_lib or load()).epic_distill_forward(
+        *rows, *_targets(rows, ids, vals, tau, weight, valid, device), _arg(loss, rows[2:4], f32, 'loss', device),
+        _arg(lse, rows[2:4], f32, 'lse', device), _on(device, stream)), 'epic_distill_forward')
 
 
 def distill_backward(logits, ids, vals, lse, grad_loss, grad, tau=1.0, weight=None, valid=None, stream=None):
     """epic_distill_backward: grad [B][n][V], of the logits' type, from the
     forward call's lse and the gradient grad_loss [B][n] of its loss."""
-    import torch
     rows = _rows(logits)
-    _check(load().epic_distill_backward(
-        *rows, *_targets(rows, ids, vals, tau, weight, valid), _arg(lse, rows[2:4], torch.float32, 'lse'),
-        _arg(grad_loss, rows[2:4], torch.float32, 'grad_loss'), *_gradient(logits, grad), _stream(stream)),
+    f32, device = _T[0], logits.device
+    _check((_lib or load()).epic_distill_backward(
+        *rows, *_targets(rows, ids, vals, tau, weight, valid, device), _arg(lse, rows[2:4], f32, 'lse', device),
+        _arg(grad_loss, rows[2:4], f32, 'grad_loss', device), *_gradient(logits, grad), _on(device, stream)),
         'epic_distill_backward')
 
 
 def distill_step(logits, ids, vals, loss, grad, tau=1.0, weight=None, valid=None, stream=None):
     """epic_distill_step: loss [B][n] and its gradient [B][n][V] in one call,
     for a training loop whose row weights are known before the loss."""
-    import torch
     rows = _rows(logits)
-    _check(load().epic_distill_step(
-        *rows, *_targets(rows, ids, vals, tau, weight, valid), _arg(loss, rows[2:4], torch.float32, 'loss'),
-        *_gradient(logits, grad), _stream(stream)), 'epic_distill_step')
+    device = logits.device
+    _check((_lib or load()).epic_distill_step(
+        *rows, *_targets(rows, ids, vals, tau, weight, valid, device),
+        _arg(loss, rows[2:4], _T[0], 'loss', device), *_gradient(logits, grad), _on(device, stream)),
+        'epic_distill_step')
