@@ -4,11 +4,10 @@
 
 namespace epic {
 
-constexpr int kThreadsMax = 512;
 
 // One CTA a row where the rows fill the GPU (two CTAs an SM).  Fewer rows are cut over clusters of up to eight CTAs,
 // down to a batch of 128 chunks a warp.
-RowShape row_shape(long long rows, int V, int size) {
+RowShape row_shape(long long rows, int V, int size, int threads) {
   const long long E = 16 / size;
   const long long chunks = V ? (V + E - 2) / E + 1 : 0;  // wherever the row starts in its first chunk
   const long long full = 2 * 152;
@@ -18,7 +17,7 @@ RowShape row_shape(long long rows, int V, int size) {
          (chunks * E > (long long)p.ctas * kSliceElems || (rows * p.ctas * 2 <= full && chunks > p.ctas * 2048)))
     p.ctas *= 2;
   p.per = (int)((chunks + p.ctas - 1) / p.ctas);
-  p.threads = (int)std::min<long long>(kThreadsMax, std::max<long long>(64, (p.per + 127) / 128 * 32));
+  p.threads = (int)std::min<long long>(threads, std::max<long long>(64, (p.per + 127) / 128 * 32));
   return p;
 }
 

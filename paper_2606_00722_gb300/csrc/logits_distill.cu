@@ -18,6 +18,8 @@ namespace epic {
 namespace {
 
 constexpr int kMaxTargets = 1024;  // most teacher entries of a row
+constexpr int kDistillThreads = 384;
+constexpr int kDistillPerSm = 4;
 
 struct DistillArgs {
   RowArgs rows;
@@ -38,6 +40,7 @@ struct DistillArgs {
 struct Targets {
   float p[kMaxTargets];
   float lp[kMaxTargets];
+  float z[kMaxTargets];  // the student's logits of the tokens
   int id[kMaxTargets];  // -1: does not count
   uint4 ends[2];
   int any;
@@ -57,34 +60,55 @@ __device__ __forceinline__ float warp_max_nan(float x) {
   return x;
 }
 
-// One warp: p and log p of the row's entries, and whether any counts.
-__device__ void teacher(const DistillArgs& a, int r, Targets& t) {
-  const int lane = threadIdx.x % 32;
-  float m = -CUDART_INF_F;
-  for (int k = lane; k < a.K; k += 32) {
+// One warp's work: the row's entries in shared memory, p and log p of them, and whether any counts.  load() asks for what
+// is in memory and is called before the pass over the row, finish() after it; entries past the 32nd wait for finish().
+template <typename T>
+struct Teacher {
+  int id;
+  float value, z;
+  // entry k: its token (-1: does not count), its scaled value, and the student's logit of the token
+  __device__ __forceinline__ void entry(const DistillArgs& a, int r, const T* logits, int k) {
     const long long o = (long long)r * a.K + k;
-    const int id = a.ids[o];
+    const int token = a.ids[o];
     const float v = a.vals[o];
-    const bool counts = id >= 0 && id < a.rows.V && (!a.valid || a.valid[o] == 1) && v != -CUDART_INF_F;
-    t.id[k] = counts ? id : -1;
-    t.lp[k] = v / a.tau;
-    if (counts) m = max_nan(m, t.lp[k]);
+    const bool counts = token >= 0 && token < a.rows.V && (!a.valid || a.valid[o] == 1) && v != -CUDART_INF_F;
+    id = counts ? token : -1;
+    value = v / a.tau;
+    z = counts ? to_float<T>(logits[token]) : 0.0f;
   }
-  m = warp_max_nan(m);
-  if (lane == 0) t.any = m != -CUDART_INF_F;
-  float sum = 0.0f;
-  for (int k = lane; k < a.K; k += 32) {
-    t.lp[k] -= m;
-    t.p[k] = t.id[k] >= 0 ? expf(t.lp[k]) : 0.0f;
-    sum += t.p[k];
+  __device__ __forceinline__ void load(const DistillArgs& a, int r, const T* logits) {
+    const int lane = threadIdx.x % 32;
+    if (lane < a.K) entry(a, r, logits, lane);
   }
-  sum = warp_add(sum);
-  const float log_sum = logf(sum);
-  for (int k = lane; k < a.K; k += 32) {
-    t.p[k] /= sum;
-    t.lp[k] -= log_sum;
+  __device__ __forceinline__ void finish(const DistillArgs& a, int r, const T* logits, Targets& t) {
+    const int lane = threadIdx.x % 32;
+    float m = -CUDART_INF_F;
+#pragma unroll 1
+    for (int k = lane; k < a.K; k += 32) {
+      if (k >= 32) entry(a, r, logits, k);
+      t.id[k] = id;
+      t.lp[k] = value;
+      t.z[k] = z;
+      if (id >= 0) m = max_nan(m, value);
+    }
+    m = warp_max_nan(m);
+    if (lane == 0) t.any = m != -CUDART_INF_F;
+    float sum = 0.0f;
+#pragma unroll 1
+    for (int k = lane; k < a.K; k += 32) {
+      t.lp[k] -= m;
+      t.p[k] = t.id[k] >= 0 ? expf(t.lp[k]) : 0.0f;
+      sum += t.p[k];
+    }
+    sum = warp_add(sum);
+    const float log_sum = logf(sum);
+#pragma unroll 1
+    for (int k = lane; k < a.K; k += 32) {
+      t.p[k] /= sum;
+      t.lp[k] -= log_sum;
+    }
   }
-}
+};
 
 // A chunk of the row at a distance of `by` bytes (0..15) past the start of `a`, b being the chunk after a.
 __device__ __forceinline__ uint4 shifted(const uint4& a, const uint4& b, int by) {
@@ -101,7 +125,7 @@ __device__ __forceinline__ uint4 shifted(const uint4& a, const uint4& b, int by)
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// The slice's elements of a gradient row, g(z) each.  The chunks are the gradient's: where its row starts elsewhere in
+// The slice's elements of a gradient row, g(z) for two of them at a time.  The chunks are the gradient's: where its row starts elsewhere in
 // 16 bytes than the logits' row does, two chunks of logits are read for one of gradient.
 template <typename T, typename G>
 __device__ void write_row(const Slice<T>& s, T* grad, G g) {
@@ -112,7 +136,11 @@ __device__ void write_row(const Slice<T>& s, T* grad, G g) {
     float f[E];
     unpack<T>(v, f);
 #pragma unroll
-    for (int e = 0; e < E; ++e) f[e] = g(f[e]);
+    for (int e = 0; e < E; e += 2) {
+      const float2 y = g(make_float2(f[e], f[e + 1]));
+      f[e] = y.x;
+      f[e + 1] = y.y;
+    }
     if (i0 >= lo && i0 + E <= hi) {
       *reinterpret_cast<uint4*>(grad + i0) = pack<T>(f);
     } else {
@@ -158,20 +186,21 @@ __device__ void write_zeros(const Slice<T>& s, T* grad) {
   }
 }
 
-// coef (q(z) - the target's share) over the slice.  The few elements that have a share are written again, each by a
-// thread of its own, after a barrier.
-template <typename T, typename Q>
-__device__ void write_gradient(const Slice<T>& s, T* grad, float coef, const Targets& t, int K, Q q) {
-  write_row(s, grad, [=](float z) { return coef * q(z); });
+// coef (q(z) - the target's share) over the slice, coef q(z) being g(z).  The few elements that have a share are written
+// again, each by a thread of its own, after a barrier.
+template <typename T, typename G>
+__device__ __forceinline__ void write_gradient(const Slice<T>& s, T* grad, float coef, const Targets& t, int K, G g) {
+  write_row(s, grad, g);
   __syncthreads();
   const int lo = s.lo(), hi = s.hi();
+#pragma unroll 1
   for (int k = threadIdx.x; k < K; k += blockDim.x) {
     const int id = t.id[k];
     if (id < lo || id >= hi) continue;
     float p = 0.0f;  // entries of the same token add up, in every thread that has one of them alike
     for (int j = 0; j < K; ++j)
       if (t.id[j] == id) p += t.p[j];
-    grad[id] = from_float<T>(coef * (q(s.at(id)) - p));
+    grad[id] = from_float<T>(g(make_float2(t.z[k], 0.0f)).x - coef * p);
   }
 }
 
@@ -184,7 +213,7 @@ __device__ __forceinline__ T* gradient_row(const DistillArgs& a, int r) {
 // Loss, and with a.grad the gradient: one cluster a row.  One pass keeps each lane's maximum so far and the sum of
 // exponentials relative to it; the gradient's pass reads the row again, from the caches.
 template <typename T>
-__global__ void __launch_bounds__(kRowThreads, 2) k_distill(DistillArgs a) {
+__global__ void __launch_bounds__(kDistillThreads, kDistillPerSm) k_distill(DistillArgs a) {
   __shared__ Targets t;
   auto cluster = cg::this_cluster();
   constexpr int E = ElemOf<T>::E;
@@ -204,7 +233,8 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_distill(DistillArgs a) {
     if (grad) write_zeros(s, grad);
     return;
   }
-  if (warp == warps - 1) teacher(a, r, t);
+  Teacher<T> teacher;
+  if (warp == warps - 1) teacher.load(a, r, logits);
   const float c2 = kLog2e / a.tau;
   float top = -CUDART_INF_F;
   float2 sums = make_float2(0.0f, 0.0f);
@@ -232,6 +262,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_distill(DistillArgs a) {
       }
     }
   });
+  if (warp == warps - 1) teacher.finish(a, r, logits, t);
   // lanes, warps, CTAs; a part without elements has maximum -inf and sum 0
   const auto part = [&](float sum, float of, float m) { return of == -CUDART_INF_F ? 0.0f : sum * exp2_32((of - m) * c2); };
   float m = warp_max_nan(top);
@@ -259,13 +290,13 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_distill(DistillArgs a) {
   }
   const bool any = t.any;
   const float log_sum = m == -CUDART_INF_F ? -CUDART_INF_F : logf(sum);
-  if (rank == 0 && warp == 0) {
+  if (rank == 0 && warp == warps - 1) {
     float loss = 0.0f;
     if (any)
       for (int k = lane; k < a.K; k += 32) {
         const float p = t.p[k];
         if (t.id[k] < 0 || p == 0.0f) continue;
-        const float z = to_float<T>(logits[t.id[k]]);
+        const float z = t.z[k];
         const float lq = z == -CUDART_INF_F ? z : (z - m) / a.tau - log_sum;
         loss += p * (t.lp[k] - lq);
       }
@@ -276,9 +307,13 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_distill(DistillArgs a) {
     }
   }
   if (grad) {
-    const float scale = m == -CUDART_INF_F ? 0.0f : 1.0f / sum, at = m == -CUDART_INF_F ? 0.0f : m;
+    const float coef = weight * a.tau;
+    const float scale = m == -CUDART_INF_F ? 0.0f : coef / sum, at = m == -CUDART_INF_F ? 0.0f : m;
     if (any)
-      write_gradient(s, grad, weight * a.tau, t, a.K, [=](float z) { return exp2_32((z - at) * c2) * scale; });
+      write_gradient(s, grad, coef, t, a.K, [=](float2 z) {
+        const float2 y = mul2(add2(z, make_float2(-at, -at)), make_float2(c2, c2));
+        return mul2(make_float2(exp2_32(y.x), exp2_32(y.y)), make_float2(scale, scale));
+      });
     else
       write_zeros(s, grad);
   }
@@ -287,7 +322,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_distill(DistillArgs a) {
 
 // the gradient from the row's logsumexp: a CTA per slice, nothing shared between them
 template <typename T>
-__global__ void __launch_bounds__(kRowThreads, 2) k_distill_backward(DistillArgs a, int parts) {
+__global__ void __launch_bounds__(kDistillThreads, kDistillPerSm) k_distill_backward(DistillArgs a, int parts) {
   __shared__ Targets t;
   const int r = (int)(blockIdx.x / (unsigned)parts);
   const float weight = a.weight ? a.weight[r] : 1.0f, lse = a.lse_in[r];
@@ -299,16 +334,22 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_distill_backward(DistillArgs
     write_zeros(s, grad);
     return;
   }
-  if (warp_index() == blockDim.x / 32 - 1) teacher(a, r, t);
-  const float inv = 1.0f / a.tau;
-  write_gradient(s, grad, coef, t, a.K, [=](float z) {
-    return z == -CUDART_INF_F ? 0.0f : exp2_32(fmaf(z, inv, -lse) * kLog2e);
+  if (warp_index() == (int)blockDim.x / 32 - 1) {
+    Teacher<T> teacher;
+    teacher.load(a, r, row_address<T>(a.rows, r));
+    teacher.finish(a, r, row_address<T>(a.rows, r), t);
+  }
+  // in a row of -inf alone every probability is 0
+  const float inv = 1.0f / a.tau, off = lse == -CUDART_INF_F ? 0.0f : -lse;
+  write_gradient(s, grad, coef, t, a.K, [=](float2 z) {
+    const float2 y = mul2(fma2(z, make_float2(inv, inv), make_float2(off, off)), make_float2(kLog2e, kLog2e));
+    return mul2(make_float2(exp2_32(y.x), exp2_32(y.y)), make_float2(coef, coef));
   });
 }
 
 template <typename T>
 epic_status launch_distill(DistillArgs& a, long long rows, cudaStream_t st) {
-  const RowShape p = row_shape(rows, a.rows.V, sizeof(T));
+  RowShape p = row_shape(rows, a.rows.V, sizeof(T), kDistillThreads);
   a.rows.per = p.per;
   if (!a.lse_in) return launch_rows((const void*)k_distill<T>, p, rows, &a, st);
   if (rows > 0x7fffffffll / p.ctas) return EPIC_ERR_CAPACITY;

@@ -82,7 +82,7 @@ struct PickShared {
   Tops tops;
   u64 list[kListMax];
   u64 parts[kParts + kParts / 16];  // kept masses by runs of 32 chunks, at part_at()
-  u64 cta_q;          // and of the CTA
+  u64 cta_q;  // the CTA's kept mass
   u64 warp_q[kRowWarps];
   uint4 ends[2];
   u64 found, before;
@@ -418,52 +418,56 @@ struct Row {
     return sum;
   }
 
-  // the warp's sum of its lanes' masses of 32 chunks to their part; lane 0 adds it up
-  __device__ __forceinline__ void add_part(LaneMass q, int c, u64& total) {
+  // the warp's sum of its lanes' masses of 32 chunks to their part
+  __device__ __forceinline__ void add_part(LaneMass q, int c) const {
     const LaneMass sum = {__reduce_add_sync(~0u, q.high), __reduce_add_sync(~0u, q.low)};
-    if (threadIdx.x % 32 || c >= s.n) return;
-    const u64 x = sum.value();
-    total += x;
-    shared().parts[part_at(c / 32)] = x;
+    if (threadIdx.x % 32 == 0 && c < s.n) shared().parts[part_at(c / 32)] = sum.value();
   }
-  // Before a barrier.
+  // before a barrier
   __device__ __forceinline__ void clear_parts() {
     for (int i = (int)threadIdx.x; i < kParts + kParts / 16; i += (int)blockDim.x) shared().parts[i] = 0;
-    if (threadIdx.x == 0) shared().cta_q = 0;
   }
 
-  // masses of the row's kept tokens, by part and by CTA
+  // masses of the row's kept tokens, by part
   __device__ __noinline__ static void masses(Row row, Weigher weigh, Kept kept) {
     row.clear_parts();
     __syncthreads();
-    u64 total = 0;
     if (row.special) {
       row.s.sweep([&](const uint4 (&)[4], int c) {
 #pragma unroll 1
         for (int i = 0; i < 4; ++i) {
           const u64 q = row.chunk_mass(row.s.chunk(c + 32 * i), c + 32 * i, weigh, kept);
-          row.add_part(LaneMass{(uint32_t)(q >> 15), (uint32_t)q & 0x7fffu}, c + 32 * i, total);
+          row.add_part(LaneMass{(uint32_t)(q >> 15), (uint32_t)q & 0x7fffu}, c + 32 * i);
         }
       });
     } else if (kept.all()) {
       row.s.sweep([&](const uint4 (&v)[4], int c) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) row.add_part(row.template lane_mass<true>(v[i], c + 32 * i, weigh, kept), c + 32 * i, total);
+        for (int i = 0; i < 4; ++i) row.add_part(row.template lane_mass<true>(v[i], c + 32 * i, weigh, kept), c + 32 * i);
       });
     } else {
       row.s.sweep([&](const uint4 (&v)[4], int c) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) row.add_part(row.template lane_mass<false>(v[i], c + 32 * i, weigh, kept), c + 32 * i, total);
+        for (int i = 0; i < 4; ++i) row.add_part(row.template lane_mass<false>(v[i], c + 32 * i, weigh, kept), c + 32 * i);
       });
     }
-    if (threadIdx.x % 32 == 0) atomicAdd(&shared().cta_q, total);
   }
 
-  // After a barrier of the group: the row's kept mass, the CTA's own and that of the CTAs ahead of it.
-  __device__ u64 all_mass(u64* mine, u64* ahead) const {
-    u64 total = 0;
-    *mine = shared().cta_q;
+  // After a barrier of the group: the row's kept mass, the CTA's own and that of the CTAs ahead of it, from the parts; every
+  // warp for itself.
+  __device__ __forceinline__ u64 all_mass(u64* mine, u64* ahead) const {
+    const int lane = (int)threadIdx.x % 32, parts = (s.n + 31) / 32;
+    u64 own = 0;
+#pragma unroll 4
+    for (int p = lane; p < parts; p += 32) own += shared().parts[part_at(p)];
+    own = warp_sum(own);
+    *mine = own;
     *ahead = 0;
+    if (group.n == 1) return own;
+    if (threadIdx.x == 0) shared().cta_q = own;
+    group.sync();
+    u64 total = 0;
+#pragma unroll 1
     for (unsigned r = 0; r < group.n; ++r) {
       const u64 x = *group.at(&shared().cta_q, r);
       if (r < group.rank) *ahead += x;
@@ -482,7 +486,6 @@ struct Row {
     int* count = group.at(&shared().count, 0);
     u64* list = group.at(shared().list, 0);
     const bool keep = kFree || min_p >= 0.0f;
-    u64 total = 0;
     s.sweep([&](const uint4 (&v)[4], int c) {
       ChunkMax<T, false> top;
       top.add(v);
@@ -496,21 +499,20 @@ struct Row {
         for (int e = 0; e < E; ++e)
           if (z[e] >= low && !(z[e] >= high)) in_bin |= 1u << (E * i + e);
         if (!keep) continue;
-        LaneMass sum = {0, 0};
+        LaneMass sum = {0u - (uint32_t)E * kHighBits, 0u - (uint32_t)E * kOnesBits};
         const int i0 = s.first(c + 32 * i);
 #pragma unroll
         for (int e = 0; e < E; e += 2) {
           const float2 y = weigh.exponents(z[e], z[e + 1]);
           const float2 w = make_float2(exp2_32(y.x), exp2_32(y.y));
           const Parts2 q(w);
-#pragma unroll
-          for (int o = 0; o < 2; ++o)
-            if (z[e + o] >= high && (o ? w.y : w.x) >= min_p && (kFree || floor.in(z[e + o], i0 + e + o))) {
-              sum.high += q.high[o] - kHighBits;
-              sum.low += q.low[o] - kOnesBits;
-            }
+          // what is not kept adds a mass of 0
+          const bool in0 = z[e] >= high && w.x >= min_p && (kFree || floor.in(z[e], i0 + e));
+          const bool in1 = z[e + 1] >= high && w.y >= min_p && (kFree || floor.in(z[e + 1], i0 + e + 1));
+          sum.high += (in0 ? q.high[0] : kHighBits) + (in1 ? q.high[1] : kHighBits);
+          sum.low += (in0 ? q.low[0] : kOnesBits) + (in1 ? q.low[1] : kOnesBits);
         }
-        add_part(sum, c + 32 * i, total);
+        add_part(sum, c + 32 * i);
       }
       for (; in_bin; in_bin &= in_bin - 1) {
         const int bit = __ffs(in_bin) - 1, index = s.first(c + 32 * (bit / E)) + bit % E;
@@ -521,7 +523,6 @@ struct Row {
       }
       __syncwarp();
     });
-    if (keep && threadIdx.x % 32 == 0 && total) atomicAdd(&shared().cta_q, total);
   }
 
   // One level of a threshold's search: kBins bins, evenly spaced in the exponent, that go down the order.  Bin 0 has what
@@ -659,7 +660,7 @@ struct Row {
   // last).  All ones for a row without elements.  A histogram over evenly spaced exponents finds the bin; where it has
   // more elements than a list, the next one cuts it again; the first CTA sorts the bin's elements.  What still does not
   // fit, many equal values, is told apart by eight bits of the keys at a time.
-  // With min_p >= 0 the masses of the kept tokens (from the threshold on, of at least min_p) are left by part and by CTA
+  // With min_p >= 0 the masses of the kept tokens (from the threshold on, of at least min_p) are left by part
   // as masses() leaves them, a barrier of the group included.
   __device__ __noinline__ static u64 threshold(Row row, Weigher weigh, Floor floor, u64 arg, bool mass, float min_p) {
     return row.find_threshold(weigh, floor, arg, mass, min_p);
@@ -688,11 +689,10 @@ struct Row {
       for (int i = (int)threadIdx.x; i < kBins; i += (int)blockDim.x) shared().bins.low[i] = shared().bins.high[i] = 0;
       if (threadIdx.x == 0) shared().count = 0;
       __syncthreads();
-      if (first && !digits && !special) {
-        if (mass)
-          count_masses(weigh, floor, free);
-        else
-          count_elements(weigh, floor, level);
+      if (mass && first && !digits && !special) {
+        count_masses(weigh, floor, free);
+      } else if (!mass && !digits) {
+        count_elements(weigh, floor, level);
       } else {
         each([&](float z, int i) {
           if (!level.has(z) || !floor.in(z, i)) return;
@@ -727,7 +727,7 @@ struct Row {
       first = false;
       __syncthreads();
       if (shared().found == ~0ull) {
-        if (threadIdx.x == 0) shared().cta_q = 0;
+        clear_parts();
         group.sync();
         return ~0ull;
       }
@@ -784,7 +784,7 @@ struct Row {
     });
   }
 
-  // the first histogram, of counts
+  // a level's histogram of counts
   __device__ __forceinline__ void count_elements(const Weigher& weigh, Floor floor, const Level& level) const {
     s.sweep([&](const uint4 (&v)[4], int c) {
 #pragma unroll
@@ -794,7 +794,7 @@ struct Row {
         const int i0 = s.first(c + 32 * i);
 #pragma unroll
         for (int e = 0; e < E; ++e)
-          add_shared(&shared().bins.low[level.bin(weigh.exponent(z[e]))], floor.in(z[e], i0 + e) ? 1u : 0u);
+          add_shared(&shared().bins.low[level.bin(weigh.exponent(z[e]))], level.has(z[e]) && floor.in(z[e], i0 + e) ? 1u : 0u);
       }
     });
   }
@@ -837,7 +837,6 @@ struct Row {
           const int c = (order_index(key) + s.head) / E, r = c / per_cta, at = c - r * per_cta;
           const u64 q = grid_mass(w);
           atomicAdd(group.at(&shared().parts[part_at(at / 32)], r), q);
-          atomicAdd(group.at(&shared().cta_q, r), q);
         }
     }
     group.sync();
@@ -1104,7 +1103,7 @@ __global__ void __launch_bounds__(kRowThreads, kPerSm) k_rows(PickArgs a) {
 
 template <typename T, template <typename> class Op, int kPerSm>
 epic_status launch(PickArgs& a, long long rows, cudaStream_t st) {
-  const RowShape p = row_shape(rows, a.rows.V, sizeof(T));
+  const RowShape p = row_shape(rows, a.rows.V, sizeof(T), kRowThreads);
   a.rows.per = p.per;
   return launch_rows((const void*)k_rows<T, Op, kPerSm>, p, rows, &a, st);
 }
