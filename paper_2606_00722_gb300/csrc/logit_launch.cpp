@@ -6,7 +6,7 @@ namespace epic {
 
 
 // One CTA a row where the rows fill the GPU (two CTAs an SM).  Fewer rows are cut over clusters of up to eight CTAs,
-// down to a batch of 128 chunks a warp.
+// down to 4,096 chunks a CTA.
 RowShape row_shape(long long rows, int V, int size, int threads) {
   const long long E = 16 / size;
   const long long chunks = V ? (V + E - 2) / E + 1 : 0;  // wherever the row starts in its first chunk
@@ -14,7 +14,7 @@ RowShape row_shape(long long rows, int V, int size, int threads) {
   RowShape p = {};
   p.ctas = 1;
   while (p.ctas < kRowCtasMax &&
-         (chunks * E > (long long)p.ctas * kSliceElems || (rows * p.ctas * 2 <= full && chunks > p.ctas * 2048)))
+         (chunks * E > (long long)p.ctas * kSliceElems || (rows * p.ctas * 2 <= full && V / E > p.ctas * 4096)))
     p.ctas *= 2;
   p.per = (int)((chunks + p.ctas - 1) / p.ctas);
   p.threads = (int)std::min<long long>(threads, std::max<long long>(64, (p.per + 127) / 128 * 32));

@@ -478,62 +478,16 @@ struct Row {
 
   // ---- thresholds
 
-  // The elements of a bin of the level, its values from low to below high, from the floor on, to the first CTA's list; with
-  // min_p >= 0 the masses of those from high on, from the floor on and of at least min_p, to the parts.  kFree: min_p >= 0
-  // and there is no floor.
-  template <bool kFree>
-  __device__ __forceinline__ void collect_bin(const Weigher& weigh, Floor floor, float low, float high, float min_p) {
-    int* count = group.at(&shared().count, 0);
-    u64* list = group.at(shared().list, 0);
-    const bool keep = kFree || min_p >= 0.0f;
-    s.sweep([&](const uint4 (&v)[4], int c) {
-      ChunkMax<T, false> top;
-      top.add(v);
-      if (!__any_sync(~0u, top.value() >= low)) return;
-      uint32_t in_bin = 0;  // a bit for each element
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float z[E];
-        unpack<T>(v[i], z);
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-          if (z[e] >= low && !(z[e] >= high)) in_bin |= 1u << (E * i + e);
-        if (!keep) continue;
-        LaneMass sum = {0u - (uint32_t)E * kHighBits, 0u - (uint32_t)E * kOnesBits};
-        const int i0 = s.first(c + 32 * i);
-#pragma unroll
-        for (int e = 0; e < E; e += 2) {
-          const float2 y = weigh.exponents(z[e], z[e + 1]);
-          const float2 w = make_float2(exp2_32(y.x), exp2_32(y.y));
-          const Parts2 q(w);
-          // what is not kept adds a mass of 0
-          const bool in0 = z[e] >= high && w.x >= min_p && (kFree || floor.in(z[e], i0 + e));
-          const bool in1 = z[e + 1] >= high && w.y >= min_p && (kFree || floor.in(z[e + 1], i0 + e + 1));
-          sum.high += (in0 ? q.high[0] : kHighBits) + (in1 ? q.high[1] : kHighBits);
-          sum.low += (in0 ? q.low[0] : kOnesBits) + (in1 ? q.low[1] : kOnesBits);
-        }
-        add_part(sum, c + 32 * i);
-      }
-      for (; in_bin; in_bin &= in_bin - 1) {
-        const int bit = __ffs(in_bin) - 1, index = s.first(c + 32 * (bit / E)) + bit % E;
-        const float z = s.at(index);
-        if (!kFree && !floor.in(z, index)) continue;
-        const int at = atomicAdd(count, 1);
-        if (at < kListMax) list[at] = order_key(z, index);
-      }
-      __syncwarp();
-    });
-  }
-
   // One level of a threshold's search: kBins bins, evenly spaced in the exponent, that go down the order.  Bin 0 has what
   // is above, the last bin what is below; of the row's values only those from low to below high (NaN: all) count.
   struct Level {
     float from, scale;
     float low, high;
-    __device__ __forceinline__ int bin(float y) const {
-      const float x = fminf(fmaxf((-y - from) * scale, 0.0f), (float)(kBins - 1));
-      return (int)(__float_as_uint(x + kOnes) - kOnesBits);
+    // kOnes and the bin of an exponent
+    __device__ __forceinline__ float place(float y) const {
+      return fminf(fmaxf((-y - from) * scale, 0.0f), (float)(kBins - 1)) + kOnes;
     }
+    __device__ __forceinline__ int bin(float y) const { return (int)(__float_as_uint(place(y)) - kOnesBits); }
     __device__ __forceinline__ bool has(float z) const { return z >= low && !(z >= high); }
     // the level that resolves bin b, whose values are from `l` to below `h`
     __device__ __forceinline__ void enter(int b, float l, float h) {
@@ -548,6 +502,63 @@ struct Row {
       }
     }
   };
+
+  // The elements of a bin of the level, from the floor on, to the first CTA's list; with min_p >= 0 the masses of those of
+  // the level's bins ahead and above the level, from the floor on and of at least min_p, to the parts.  kFree: min_p >= 0,
+  // there is no floor, and the level is the first.
+  template <bool kFree>
+  __device__ __forceinline__ void collect_bin(const Weigher& weigh, Floor floor, const Level& level, int bin, float min_p) {
+    int* count = group.at(&shared().count, 0);
+    u64* list = group.at(shared().list, 0);
+    const bool keep = kFree || min_p >= 0.0f;
+    s.sweep([&](const uint4 (&v)[4], int c) {
+      ChunkMax<T, false> top;
+      top.add(v);
+      const float most = top.value();
+      if (!__any_sync(~0u, most > -CUDART_INF_F && level.place(weigh.exponent(most)) <= kOnes + bin)) return;
+      uint32_t in_bin = 0;  // a bit for each element
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float z[E];
+        unpack<T>(v[i], z);
+        LaneMass sum = {0u - (uint32_t)E * kHighBits, 0u - (uint32_t)E * kOnesBits};
+        const int i0 = s.first(c + 32 * i);
+#pragma unroll
+        for (int e = 0; e < E; e += 2) {
+          const float2 y = weigh.exponents(z[e], z[e + 1]);
+          float2 at = fma2(y, make_float2(-kBinsPerUnit, -kBinsPerUnit), make_float2(kOnes, kOnes));
+          bool ahead0 = at.x < kOnes + bin, ahead1 = at.y < kOnes + bin;
+          bool here0 = at.x == kOnes + bin, here1 = at.y == kOnes + bin;
+          if (!kFree) {
+            at = make_float2(level.place(y.x), level.place(y.y));
+            ahead0 = z[e] >= level.high || (level.has(z[e]) && at.x < kOnes + bin);
+            ahead1 = z[e + 1] >= level.high || (level.has(z[e + 1]) && at.y < kOnes + bin);
+            here0 = level.has(z[e]) && at.x == kOnes + bin;
+            here1 = level.has(z[e + 1]) && at.y == kOnes + bin;
+          }
+          if (here0) in_bin |= 1u << (E * i + e);
+          if (here1) in_bin |= 1u << (E * i + e + 1);
+          if (!keep) continue;
+          const float2 w = make_float2(exp2_32(y.x), exp2_32(y.y));
+          const Parts2 q(w);
+          // what is not kept adds a mass of 0
+          const bool in0 = ahead0 && w.x >= min_p && (kFree || floor.in(z[e], i0 + e));
+          const bool in1 = ahead1 && w.y >= min_p && (kFree || floor.in(z[e + 1], i0 + e + 1));
+          sum.high += (in0 ? q.high[0] : kHighBits) + (in1 ? q.high[1] : kHighBits);
+          sum.low += (in0 ? q.low[0] : kOnesBits) + (in1 ? q.low[1] : kOnesBits);
+        }
+        if (keep) add_part(sum, c + 32 * i);
+      }
+      for (; in_bin; in_bin &= in_bin - 1) {
+        const int bit = __ffs(in_bin) - 1, index = s.first(c + 32 * (bit / E)) + bit % E;
+        const float z = s.at(index);
+        if (!kFree && !floor.in(z, index)) continue;
+        const int at = atomicAdd(count, 1);
+        if (at < kListMax) list[at] = order_key(z, index);
+      }
+      __syncwarp();
+    });
+  }
 
   // One warp: the lowest of the level's values whose bin is at most b, to the lower half of the lanes, and the lowest whose
   // bin is less, to the upper half (the level's end where there is none).  The bins do not increase with the value; each
@@ -576,6 +587,24 @@ struct Row {
     return none ? level.high : key_value(lo);
   }
 
+  // The histogram's sums by groups of 32 bins, four groups of a warp at a time.
+  __device__ __forceinline__ static void sum_groups() {
+    const int lane = (int)threadIdx.x % 32;
+#pragma unroll 1
+    for (int g = 4 * warp_index(); g < kGroups; g += (int)blockDim.x / 8) {
+      u64 x[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = shared().bins.mass(32 * (g + i) + lane);
+#pragma unroll
+      for (int o = 16; o; o >>= 1)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] += __shfl_xor_sync(~0u, x[i], o);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (lane == i) shared().bins.group[g + i] = x[i];
+    }
+  }
+
   // After a barrier, in one warp: the bin of the cluster's histograms at which the running total passes t, and the rest
   // of t within it, to shared().found and shared().before; all ones for histograms of nothing.  t may be given as a share of all.
   __device__ __forceinline__ void find_bin(u64 t, bool share, bool mass) const {
@@ -583,8 +612,9 @@ struct Row {
     const int lane = (int)threadIdx.x % 32;
     const unsigned ctas = group.n;
     u64 x0 = 0, x1 = 0;
-#pragma unroll 1
-    for (unsigned r = 0; r < ctas; ++r) {
+#pragma unroll
+    for (unsigned r = 0; r < kRowCluster; ++r) {  // the loads from all CTAs at once
+      if (r >= ctas) break;
       const Histogram* h = group.at(&shared().bins, r);
       x0 += h->group[2 * lane];
       x1 += h->group[2 * lane + 1];
@@ -666,7 +696,7 @@ struct Row {
     return row.find_threshold(weigh, floor, arg, mass, min_p);
   }
   __device__ __forceinline__ u64 find_threshold(const Weigher& weigh, Floor floor, u64 arg, bool mass, float min_p) {
-    const int lane = (int)threadIdx.x % 32, warps = (int)blockDim.x / 32, warp = warp_index();
+    const int lane = (int)threadIdx.x % 32, warp = warp_index();
     const bool keep = min_p >= 0.0f, free = floor.z == -CUDART_INF_F;
     Level level{0.0f, kBinsPerUnit, -CUDART_MAX_NORMAL_F, CUDART_NAN_F};
     if (weigh.m == CUDART_INF_F) level.low = -CUDART_INF_F;
@@ -710,19 +740,11 @@ struct Row {
         });
       }
       __syncthreads();
-      for (int g = warp; g < kGroups; g += warps) {
-        const u64 x = warp_sum(shared().bins.mass(32 * g + lane));
-        if (lane == 0) shared().bins.group[g] = x;
-      }
+      sum_groups();
       group.sync();
       if (warp == 0) {  // every CTA for itself
         find_bin(t, first, mass);
         __syncwarp();
-        if (!digits && shared().found != ~0ull) {
-          const float end = ends_of_bin(weigh, level, (int)shared().found);
-          if (lane == 0) shared().bin_low = end;
-          if (lane == 16) shared().bin_high = end;
-        }
       }
       first = false;
       __syncthreads();
@@ -739,17 +761,22 @@ struct Row {
         group.sync();  // all have read the bins
         continue;
       }
-      const float low = shared().bin_low, high = shared().bin_high;
       if (keep) clear_parts();
       __syncthreads();
-      if (free && keep)
-        collect_bin<true>(weigh, floor, low, high, min_p);
+      if (free && keep && depth == 0 && bin < kBins - 1)
+        collect_bin<true>(weigh, floor, level, bin, min_p);
       else
-        collect_bin<false>(weigh, floor, low, high, min_p);
+        collect_bin<false>(weigh, floor, level, bin, min_p);
       group.sync();
       const int n = *group.at(&shared().count, 0);
       if (n <= kListMax) return by_list(n, weigh, t, mass, min_p);
-      level.enter(bin, low, high);
+      if (warp == 0) {
+        const float end = ends_of_bin(weigh, level, bin);
+        if (lane == 0) shared().bin_low = end;
+        if (lane == 16) shared().bin_high = end;
+      }
+      __syncthreads();
+      level.enter(bin, shared().bin_low, shared().bin_high);
       group.sync();  // all have seen the count
     }
     if (keep) masses(*this, weigh, Kept{floor_of(prefix), min_p});
@@ -815,12 +842,9 @@ struct Row {
         const u64 upto = warp_scan(q);
         if (lane == 31) shared().warp_q[warp] = upto;
         __syncthreads();
-        u64 before = ahead;
-#pragma unroll 1
-        for (int w = 0; w < warps; ++w) {
-          if (w < warp) before += shared().warp_q[w];
-          ahead += shared().warp_q[w];
-        }
+        const u64 w_q = lane < warps ? shared().warp_q[lane] : 0, w_upto = warp_scan(w_q);
+        const u64 before = ahead + __shfl_sync(~0u, w_upto - w_q, warp);
+        ahead += __shfl_sync(~0u, w_upto, 31);
         if (before + upto - q <= t && t < before + upto) {
           shared().found = key;
           shared().last = i;
