@@ -337,7 +337,7 @@ enum { EPIC_F32 = 0, EPIC_F16 = 1, EPIC_BF16 = 2 }; /* the element type of logit
  * T = 0 gives confidences 1, 0, 0, ...; a T below 0 or NaN gives no candidates.
  * +inf logits share all probability.  Errors: EPIC_ERR_INVALID_ARG (NULL
  * pointers, sizes < 0, a bad dtype, d_logits not aligned to its elements, k > n
- * without d_pos), EPIC_ERR_CAPACITY when K > 256.
+ * without d_pos), EPIC_ERR_CAPACITY when K > 256 or V > 1047872.
  */
 epic_status epic_propose_topk(const void* d_logits, int32_t dtype, int32_t B, int32_t n, int32_t V, int64_t stride_b,
                               int64_t stride_n, const int32_t* d_pos, int32_t k, const float* d_temperature,
@@ -360,7 +360,7 @@ epic_status epic_propose_topk(const void* d_logits, int32_t dtype, int32_t B, in
  * probability among the kept ones: candidates and confidences with K = S.
  * T = 0 takes the likeliest token.  A row of no tokens (all -inf or NaN), a T
  * below 0 or NaN, a NaN rule, or a number outside [0, 1] gives -1 and 0.
- * Errors as epic_propose_topk.
+ * Errors as epic_propose_topk, without a limit on S.
  */
 epic_status epic_sample_tokens(const void* d_logits, int32_t dtype, int32_t B, int32_t n, int32_t V, int64_t stride_b,
                                int64_t stride_n, const int32_t* d_pos, int32_t k, const float* d_temperature,
@@ -382,14 +382,15 @@ epic_status epic_sample_tokens(const void* d_logits, int32_t dtype, int32_t B, i
  * the teacher wants gives loss +inf and a finite gradient; NaN or +inf logits
  * give NaN.  Entries of one token add up.
  * epic_distill_forward: d_loss and d_lse [B][n] float32 (d_lse is for the
- * backward call; 0 where the row was not read).
+ * backward call; +inf for a row that nothing flows back into: of weight 0, or
+ * without entries that count).
  * epic_distill_backward: d_grad, of the logits' type, [B][n][V] with its own
  * strides in elements, from d_lse and g = d_grad_loss [B][n].
  * epic_distill_step: loss and gradient in one call with g = 1, reading the
  * logits once.
  * d_grad must not overlap d_logits; rows of d_grad must not overlap each other.
  * Errors: EPIC_ERR_INVALID_ARG as epic_propose_topk, and for tau not in
- * (0, 3e38]; EPIC_ERR_CAPACITY when K > 1024.
+ * (0, 3e38]; EPIC_ERR_CAPACITY when K > 1024 or V > 2^31 - 4097.
  */
 epic_status epic_distill_forward(const void* d_logits, int32_t dtype, int32_t B, int32_t n, int32_t V,
                                  int64_t stride_b, int64_t stride_n, const int32_t* d_ids, const float* d_vals,

@@ -4,6 +4,7 @@ selection and commit, behind the C-ABI of ``include/epic.h``."""
 from .epic import (Grammar, LexTable, EpicError, build, load, validate_batch,  # noqa: F401
                    validate_batch_noalloc, measure_int_peak,
                    pick_candidates, select_compatible_subset, commit, fallback_commit, decode_step, extract_witness,
-                   propose_topk, sample_tokens, distill_forward, distill_backward, distill_step,
+                   propose_topk, sample_tokens, distill_forward, distill_backward, distill_step, distill_loss,
+                   decode_step_from_logits,
                    GAP_BIT,
                    LIB_PATH, EXPORTS)

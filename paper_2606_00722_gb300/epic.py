@@ -498,3 +498,43 @@ def distill_step(logits, ids, vals, loss, grad, tau=1.0, weight=None, valid=None
         *rows, *_targets(rows, ids, vals, tau, weight, valid, device),
         _arg(loss, rows[2:4], _T[0], 'loss', device), *_gradient(logits, grad), _on(device, stream)),
         'epic_distill_step')
+
+
+def distill_loss(logits, ids, vals, tau=1.0, weight=None, valid=None):
+    """The distillation loss [B][n] of student logits [B][n][V] as a torch
+    operation with a gradient for the logits (forward: epic_distill_forward,
+    backward: epic_distill_backward); the other arguments are constants.
+    Streams are torch's own."""
+    import torch
+
+    class Loss(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, z):
+            loss = torch.empty(z.shape[:2], dtype=torch.float32, device=z.device)
+            lse = torch.empty_like(loss)
+            distill_forward(z, ids, vals, loss, lse, tau, weight, valid)
+            ctx.save_for_backward(z, lse)
+            return loss
+
+        @staticmethod
+        def backward(ctx, grad_loss):
+            z, lse = ctx.saved_tensors
+            grad = torch.empty(z.shape, dtype=z.dtype, device=z.device)
+            distill_backward(z, ids, vals, lse, grad_loss.to(torch.float32).contiguous(), grad, tau, weight, valid)
+            return grad
+
+    return Loss.apply(logits)
+
+
+def decode_step_from_logits(g: Grammar, t: LexTable, x, pos, logits, n_target, bufs, temperature=None, u=None,
+                            top_k=None, top_p=None, min_p=None, stream=None):
+    """One denoising step from the model's logits [B][n][V] on: the K = bufs['cand'].shape[2] most likely tokens of the
+    proposed positions pos [B][k] (propose_topk), or with numbers u [B][k][K] as many draws (sample_tokens, by the rules
+    of each sequence), then decode_step on them.  bufs holds decode_step's buffers and cand [B][k][K] int32, cand_conf
+    [B][k][K] float32.  The vocabulary of the logits may be padded: tokens past the lexing table's are no valid
+    candidates."""
+    if u is None:
+        propose_topk(logits, bufs['cand'], bufs['cand_conf'], pos, temperature, stream)
+    else:
+        sample_tokens(logits, u, bufs['cand'], bufs['cand_conf'], pos, temperature, top_k, top_p, min_p, stream)
+    decode_step(g, t, x, pos, bufs['cand'], bufs['cand_conf'], n_target, bufs, stream)

@@ -135,6 +135,20 @@ def test_loss_and_gradient(cuda, B, n, V, K, dtype, kind, pad, shift, tau):
         assert (store.view(-1)[:at + other] == 7).all()
 
 
+@pytest.mark.parametrize('V,dtype,pad,shift', [(4099, 'bf16', 3, 1), (8192, 'f32', 0, 0), (16411, 'f16', 0, 5)])
+def test_many_rows(cuda, V, dtype, pad, shift):
+    """Rows enough for every place on the GPU."""
+    import torch
+    import paper_2606_00722_gb300 as epic
+    B, n, K, tau = 70, 9, 12, 1.5
+    logits, ids, vals, valid, weight = make(B, n, V, K, dtype, 'edges', V, pad, shift)
+    weight[::3] = 0.0
+    want_loss, want_grad = distill64(logits, ids, vals, valid, weight, tau)
+    loss, grad = torch.full((B, n), -7.0, device='cuda'), torch.full((B, n, V), 7.0, dtype=logits.dtype, device='cuda')
+    epic.distill_step(logits, ids, vals, loss, grad, tau=tau, weight=weight, valid=valid)
+    check(loss, grad, want_loss, want_grad, ids, weight, tau, dtype)
+
+
 def test_without_weights_or_bits(cuda):
     import torch
     import paper_2606_00722_gb300 as epic

@@ -43,6 +43,9 @@ def test_bad_outputs_and_sizes_are_refused():
     for bad in (dict(K=-1), dict(cand=None), dict(conf=None)):
         assert propose(**bad) == epic.epic.ERR_INVALID_ARG, bad
     assert propose(K=257) == epic.epic.ERR_CAPACITY
+    for call in (propose, sample):  # one more than the histograms of a row's slices take
+        assert call(V=1047873, sn=1047873, sb=4000000) == epic.epic.ERR_CAPACITY
+    assert step(V=0x7fffffff) == epic.epic.ERR_CAPACITY
     for bad in (dict(S=-1), dict(u=None), dict(tok=None), dict(prob=None)):
         assert sample(**bad) == epic.epic.ERR_INVALID_ARG, bad
     for bad in (dict(K=-1), dict(ids=None), dict(vals=None), dict(loss=None), dict(grad=None), dict(grad=P + 1),
