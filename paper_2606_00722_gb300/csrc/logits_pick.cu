@@ -12,19 +12,19 @@
 // less likely than 2^-31 of the likeliest.
 //
 // The kept tokens of a draw are a prefix of the row's order cut by top-k, then by
-// the nucleus, each found as a threshold key by radix selection on counts or on
-// masses; the draw is the first kept token in index order whose mass up to and
-// with it passes u times the kept mass.
-#include "../../include/epic.h"
+// the nucleus, each found as a threshold key on a histogram of counts or of masses;
+// the draw is the first kept token in index order whose mass up to and with it
+// passes u times the kept mass.
 #include <limits.h>
 
+#include "../../include/epic.h"
 #include "logit_launch.h"
 #include "logit_rows.cuh"
 
 namespace epic {
 namespace {
 
-constexpr int kListMax = 1536;  // most keys collected for ranking
+constexpr int kListMax = 2048;  // most keys collected for ranking; a power of two, to which sorting fills up
 constexpr int kMaxK = 256;      // most candidates of a position, and the longest top-k list
 constexpr int kMaxV = kRowCtasMax * (kSliceElems - 16);  // 1,047,872: histograms and parts of a row's slices
 constexpr int kBins = 2048;     // of a threshold's histogram
@@ -205,7 +205,6 @@ struct Row {
   int per_cta;   // chunks
   bool special;  // this warp's elements have NaN, or the row +inf or nothing
   static constexpr int E = ElemOf<T>::E;
-
 
   // f(value, index) for the elements of this lane's chunks, one at a time: small code for rare ways.  (The whole kernel
   // unrolled was 460 KB, and each phase of a row waited for its instructions.)

@@ -281,6 +281,18 @@ def test_sample_is_the_definition(cuda, B, n, V, S, dtype, kind, pad, shift, rul
     np.testing.assert_allclose(prob.cpu().numpy(), want_prob.cpu().numpy(), rtol=2.0 ** -21, atol=0)
 
 
+@pytest.mark.parametrize('rules', ['large top-k', 'top-p', 'large all'])
+@pytest.mark.parametrize('V', [700, 1900, 3500, 5120, 6500, 9000, 10235, 10245, 12000])
+def test_sample_many_equal_values(cuda, V, rules):
+    """Five values share the row, so the threshold falls among 140 to 2,400 equal ones: lists of every size that is sorted,
+    full ones, and the first that are too long."""
+    logits = make_logits(4, 2, V, 'f32', 'ties', V)
+    tok, prob, u, r = run_sample(logits, RULES[rules], 12)
+    want_tok, want_prob, _ = sample_whole(logits, *r, u)
+    assert np.array_equal(tok.cpu().numpy(), want_tok.cpu().numpy())
+    np.testing.assert_allclose(prob.cpu().numpy(), want_prob.cpu().numpy(), rtol=2.0 ** -21, atol=0)
+
+
 @pytest.mark.parametrize('rules', ['temperature', 'large all', 'mixed'])
 @pytest.mark.parametrize('B,n,V,dtype,kind,pad,shift', MANY)
 def test_sample_many_rows(cuda, B, n, V, dtype, kind, pad, shift, rules):
