@@ -388,15 +388,22 @@ def _rows(logits):
     code = _DTYPES.get(logits.dtype)
     if code is None:
         raise ValueError('expected float32, float16 or bfloat16 logits, got %s' % logits.dtype)
-    if not logits.is_cuda:
-        raise ValueError('expected a CUDA tensor')
-    if logits.dim() != 3:
+    shape = logits.shape
+    if len(shape) != 3:
         raise ValueError('expected logits [B][n][V]')
-    B, n, V = logits.shape
+    B, n, V = shape
     sb, sn, sv = logits.stride()
     if sv != 1 and V > 1:
         raise ValueError('expected logits with unit stride along the vocabulary')
     return logits.data_ptr(), code, B, n, V, sb, sn
+
+
+def _device(logits):
+    """The index of the device of a CUDA tensor."""
+    device = logits.get_device()
+    if device < 0:
+        raise ValueError('expected a CUDA tensor')
+    return device
 
 
 def _arg(t, shape, dtype, name, device):
@@ -406,15 +413,15 @@ def _arg(t, shape, dtype, name, device):
     if t.shape != shape or t.dtype != dtype:
         raise ValueError('%s: expected %s of shape %s, got %s of shape %s' % (name, dtype, tuple(shape), t.dtype,
                                                                              tuple(t.shape)))
-    if t.device != device or not t.is_contiguous():
-        raise ValueError('%s: expected a contiguous tensor on %s' % (name, device))
+    if t.get_device() != device or not t.is_contiguous():
+        raise ValueError('%s: expected a contiguous tensor on CUDA device %d' % (name, device))
     return t.data_ptr()
 
 
 def _on(device, stream):
     """The stream of a call on that device's tensors (None: the device's current one)."""
     if stream is None:
-        return _raw_stream(device.index)
+        return _raw_stream(device)
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 
@@ -425,7 +432,7 @@ def propose_topk(logits, cand, conf, pos=None, temperature=None, stream=None):
     temperature [B] float32 (None: 1)."""
     rows = _rows(logits)
     f32, i32, _ = _T
-    device = logits.device
+    device = _device(logits)
     B = rows[2]
     k, K = cand.shape[1:]
     shape = (B, k, K)
@@ -442,7 +449,7 @@ def sample_tokens(logits, u, tok, prob, pos=None, temperature=None, top_k=None, 
     (float32, top_k int32) or None (off)."""
     rows = _rows(logits)
     f32, i32, _ = _T
-    device = logits.device
+    device = _device(logits)
     B = rows[2:3]
     k, S = u.shape[1:]
     shape = (rows[2], k, S)
@@ -472,7 +479,7 @@ def distill_forward(logits, ids, vals, loss, lse, tau=1.0, weight=None, valid=No
     [B][n][V] against a teacher's entries ids [B][n][K] int32, vals [B][n][K]
     float32; weight [B][n] float32, valid [B][n][K] uint8 (None: all count)."""
     rows = _rows(logits)
-    f32, device = _T[0], logits.device
+    f32, device = _T[0], _device(logits)
     _check((_lib or load()).epic_distill_forward(
         *rows, *_targets(rows, ids, vals, tau, weight, valid, device), _arg(loss, rows[2:4], f32, 'loss', device),
         _arg(lse, rows[2:4], f32, 'lse', device), _on(device, stream)), 'epic_distill_forward')
@@ -482,7 +489,7 @@ def distill_backward(logits, ids, vals, lse, grad_loss, grad, tau=1.0, weight=No
     """epic_distill_backward: grad [B][n][V], of the logits' type, from the
     forward call's lse and the gradient grad_loss [B][n] of its loss."""
     rows = _rows(logits)
-    f32, device = _T[0], logits.device
+    f32, device = _T[0], _device(logits)
     _check((_lib or load()).epic_distill_backward(
         *rows, *_targets(rows, ids, vals, tau, weight, valid, device), _arg(lse, rows[2:4], f32, 'lse', device),
         _arg(grad_loss, rows[2:4], f32, 'grad_loss', device), *_gradient(logits, grad), _on(device, stream)),
@@ -493,7 +500,7 @@ def distill_step(logits, ids, vals, loss, grad, tau=1.0, weight=None, valid=None
     """epic_distill_step: loss [B][n] and its gradient [B][n][V] in one call,
     for a training loop whose row weights are known before the loss."""
     rows = _rows(logits)
-    device = logits.device
+    device = _device(logits)
     _check((_lib or load()).epic_distill_step(
         *rows, *_targets(rows, ids, vals, tau, weight, valid, device),
         _arg(loss, rows[2:4], _T[0], 'loss', device), *_gradient(logits, grad), _on(device, stream)),
