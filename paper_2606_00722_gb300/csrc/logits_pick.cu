@@ -203,7 +203,7 @@ struct Row {
   Slice<T> s;
   RowGroup group;
   int per_cta;   // chunks
-  bool special;  // this warp's elements have NaN, or the row +inf or nothing
+  bool special;  // this warp's elements have NaN, or the row +inf, or nothing, or T = inf
   static constexpr int E = ElemOf<T>::E;
 
   // f(value, index) for the elements of this lane's chunks, one at a time: small code for rare ways.  (The whole kernel
@@ -1086,7 +1086,8 @@ struct Sample {
       if (row.group.n > 1) row.group.sync();  // the others have looked at the count
       return;
     }
-    row.special = row.special || fabsf(weigh.m) == CUDART_INF_F;
+    // T = inf: the exponents of -inf, which also fills the last chunks up, are -inf times 0
+    row.special = row.special || fabsf(weigh.m) == CUDART_INF_F || weigh.c == 0.0f;
     const bool by_mass = p24 < (1u << 24);
     Kept kept{no_floor(), fmaxf(min_p, 0.0f)};
     if (top_k < a.rows.V)

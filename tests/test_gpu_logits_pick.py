@@ -293,6 +293,38 @@ def test_sample_many_equal_values(cuda, V, rules):
     np.testing.assert_allclose(prob.cpu().numpy(), want_prob.cpu().numpy(), rtol=2.0 ** -21, atol=0)
 
 
+@pytest.mark.parametrize('V,dtype,kind', [(1, 'f32', 'normal'), (700, 'bf16', 'specials'), (4099, 'f32', 'normal'),
+                                          (5003, 'f16', 'specials'), (40001, 'bf16', 'specials')])
+@pytest.mark.parametrize('rules', [(None, None, None), (None, [0.9, 0.3], None), ([300, 600], [1.0, 0.7], [0.5]),
+                                   ([7], [0.9], None)])
+def test_sample_at_infinite_temperature(cuda, V, dtype, kind, rules):
+    """Every token that is one weighs 1; -inf and NaN, times an exponent's factor of 0, still weigh nothing."""
+    logits = make_logits(2, 3, V, dtype, kind, V)
+    tok, prob, u, r = run_sample(logits, ([math.inf],) + rules, 6)
+    want_tok, want_prob, _ = sample_whole(logits.float(), *r, u)
+    assert np.array_equal(tok.cpu().numpy(), want_tok.cpu().numpy())
+    np.testing.assert_allclose(prob.cpu().numpy(), want_prob.cpu().numpy(), rtol=2.0 ** -21, atol=0)
+
+
+@pytest.mark.parametrize('V,dtype', [(3, 'f32'), (700, 'bf16'), (40001, 'f16')])
+def test_propose_at_infinite_temperature(cuda, V, dtype):
+    import torch
+    import paper_2606_00722_gb300 as epic
+    K = 8
+    logits = make_logits(2, 3, V, dtype, 'specials', V)
+    pos = torch.arange(3, dtype=torch.int32).repeat(2, 1).cuda()
+    cand = torch.full((2, 3, K), -7, dtype=torch.int32, device='cuda')
+    conf = torch.full((2, 3, K), -7.0, device='cuda')
+    epic.propose_topk(logits, cand, conf, temperature=torch.full((2,), math.inf, device='cuda'))
+    z = rows64(logits, pos)
+    want_cand, _ = propose64(z, [1.0, 1.0], K)  # the order does not depend on the temperature
+    assert np.array_equal(cand.cpu().numpy(), want_cand)
+    some = np.where(np.isposinf(z).any(-1), np.isposinf(z).sum(-1), (z > -np.inf).sum(-1))  # NaN is not above -inf
+    want = np.where(want_cand >= 0, 1.0 / np.maximum(some, 1)[..., None], 0.0)
+    want[np.isposinf(z).any(-1)[..., None] & ~np.isposinf(np.take_along_axis(z, want_cand.clip(0), -1))] = 0.0
+    np.testing.assert_allclose(conf.cpu().numpy(), want, rtol=RTOL, atol=1e-30)
+
+
 @pytest.mark.parametrize('rules', ['temperature', 'large all', 'mixed'])
 @pytest.mark.parametrize('B,n,V,dtype,kind,pad,shift', MANY)
 def test_sample_many_rows(cuda, B, n, V, dtype, kind, pad, shift, rules):
