@@ -10,6 +10,8 @@
 // Each row is read from memory once: for the loss in one pass with a running
 // maximum, for loss and gradient with a second pass from the caches.  The
 // backward pass has the row's logsumexp and reads the row once again.
+#include <limits.h>
+
 #include "../../include/epic.h"
 #include "logit_launch.h"
 #include "logit_rows.cuh"
@@ -18,6 +20,10 @@ namespace epic {
 namespace {
 
 constexpr int kMaxTargets = 1024;  // most teacher entries of a row
+// Largest size of a logsumexp from which the backward pass takes probabilities.  32 bits hold it to 2^-18 there, which is
+// the probabilities' relative error; of a row at its type's lowest value they hold the maximum and nothing of the sum.
+// Larger ones are taken apart again, from the row.
+constexpr float kLseFine = 128.0f;
 constexpr int kDistillThreads = 384;
 constexpr int kDistillPerSm = 4;
 
@@ -42,7 +48,7 @@ struct Targets {
   float lp[kMaxTargets];
   float z[kMaxTargets];  // the student's logits of the tokens
   int id[kMaxTargets];  // -1: does not count
-  uint4 ends[2];
+  uint4 ends[2], row_ends[2];
   int any;
   float warp_m[kRowWarps], warp_s[kRowWarps];
   float m, s;  // of the CTA
@@ -50,6 +56,8 @@ struct Targets {
 
 // larger of two, NaN if either is
 __device__ __forceinline__ float max_nan(float a, float b) { return ChunkMax<float, true>::max1(a, b); }
+
+__device__ __forceinline__ float below_inf(float x) { return x == CUDART_INF_F ? CUDART_MAX_NORMAL_F : x; }
 
 __device__ __forceinline__ float warp_add(float x) {
   for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(~0u, x, o);
@@ -210,32 +218,10 @@ __device__ __forceinline__ T* gradient_row(const DistillArgs& a, int r) {
   return static_cast<T*>(a.grad) + b * a.gstride_b + (r - b * a.rows.k) * a.gstride_n;
 }
 
-// Loss, and with a.grad the gradient: one cluster a row.  One pass keeps each lane's maximum so far and the sum of
-// exponentials relative to it; the gradient's pass reads the row again, from the caches.
+// This lane's elements of the slice: the maximum (NaN if any is, or +inf) and the sum of 2^((z - maximum) c2).
 template <typename T>
-__global__ void __launch_bounds__(kDistillThreads, kDistillPerSm) k_distill(DistillArgs a) {
-  __shared__ Targets t;
-  auto cluster = cg::this_cluster();
+__device__ __forceinline__ float lane_sums(const Slice<T>& s, float c2, float* sum) {
   constexpr int E = ElemOf<T>::E;
-  const unsigned ctas = cluster.num_blocks(), rank = cluster.block_rank();
-  const int lane = threadIdx.x % 32, warp = warp_index(), warps = blockDim.x / 32;
-  const int r = (int)(blockIdx.x / ctas);
-  const float weight = a.weight ? a.weight[r] : 1.0f;
-  const T* logits = row_address<T>(a.rows, r);
-  T* grad = a.grad ? gradient_row<T>(a, r) : nullptr;
-  Slice<T> s;
-  s.open(logits, a.rows, rank, t.ends);
-  if (weight == 0.0f) {  // the same in all CTAs of the row
-    if (rank == 0 && threadIdx.x == 0) {
-      a.loss[r] = 0.0f;
-      if (a.lse) a.lse[r] = CUDART_INF_F;
-    }
-    if (grad) write_zeros(s, grad);
-    return;
-  }
-  Teacher<T> teacher;
-  if (warp == warps - 1) teacher.load(a, r, logits);
-  const float c2 = kLog2e / a.tau;
   float top = -CUDART_INF_F;
   float2 sums = make_float2(0.0f, 0.0f);
   const float2 by = make_float2(c2, c2);
@@ -262,18 +248,58 @@ __global__ void __launch_bounds__(kDistillThreads, kDistillPerSm) k_distill(Dist
       }
     }
   });
-  if (warp == warps - 1) teacher.finish(a, r, logits, t);
-  // lanes, warps, CTAs; a part without elements has maximum -inf and sum 0
-  const auto part = [&](float sum, float of, float m) { return of == -CUDART_INF_F ? 0.0f : sum * exp2_32((of - m) * c2); };
-  float m = warp_max_nan(top);
-  float sum = warp_add(part(sums.x + sums.y, top, m));
+  *sum = sums.x + sums.y;
+  return top;
+}
+
+// A part's sum relative to a maximum `of`, relative to m instead; a part without elements has maximum -inf and sum 0.
+__device__ __forceinline__ float rebase(float sum, float of, float m, float c2) {
+  return of == -CUDART_INF_F ? 0.0f : sum * exp2_32((of - m) * c2);
+}
+
+// The CTA's, from its lanes'; a barrier included.
+__device__ __forceinline__ float cta_sums(Targets& t, float top, float c2, float* sum) {
+  const int lane = threadIdx.x % 32, warp = warp_index(), warps = blockDim.x / 32;
+  float m = warp_max_nan(top), x = warp_add(rebase(*sum, top, m, c2));
   if (lane == 0) {
     t.warp_m[warp] = m;
-    t.warp_s[warp] = sum;
+    t.warp_s[warp] = x;
   }
   __syncthreads();
   m = warp_max_nan(lane < warps ? t.warp_m[lane] : -CUDART_INF_F);
-  sum = warp_add(lane < warps ? part(t.warp_s[lane], t.warp_m[lane], m) : 0.0f);
+  *sum = warp_add(lane < warps ? rebase(t.warp_s[lane], t.warp_m[lane], m, c2) : 0.0f);
+  return m;
+}
+
+// Loss, and with a.grad the gradient: one cluster a row.  One pass keeps each lane's maximum so far and the sum of
+// exponentials relative to it; the gradient's pass reads the row again, from the caches.
+template <typename T>
+__global__ void __launch_bounds__(kDistillThreads, kDistillPerSm) k_distill(DistillArgs a) {
+  __shared__ Targets t;
+  auto cluster = cg::this_cluster();
+  const unsigned ctas = cluster.num_blocks(), rank = cluster.block_rank();
+  const int lane = threadIdx.x % 32, warp = warp_index(), warps = blockDim.x / 32;
+  const int r = (int)(blockIdx.x / ctas);
+  const float weight = a.weight ? a.weight[r] : 1.0f;
+  const T* logits = row_address<T>(a.rows, r);
+  T* grad = a.grad ? gradient_row<T>(a, r) : nullptr;
+  Slice<T> s;
+  s.open(logits, a.rows, rank, t.ends);
+  if (weight == 0.0f) {  // the same in all CTAs of the row
+    if (rank == 0 && threadIdx.x == 0) {
+      a.loss[r] = 0.0f;
+      if (a.lse) a.lse[r] = CUDART_INF_F;
+    }
+    if (grad) write_zeros(s, grad);
+    return;
+  }
+  Teacher<T> teacher;
+  if (warp == warps - 1) teacher.load(a, r, logits);
+  const float c2 = kLog2e / a.tau;
+  float sum;
+  const float top = lane_sums(s, c2, &sum);
+  if (warp == warps - 1) teacher.finish(a, r, logits, t);
+  float m = cta_sums(t, top, c2, &sum);
   if (ctas > 1) {
     if (threadIdx.x == 0) {
       t.m = m;
@@ -286,7 +312,7 @@ __global__ void __launch_bounds__(kDistillThreads, kDistillPerSm) k_distill(Dist
       x = *cluster.map_shared_rank(&t.s, lane);
     }
     m = warp_max_nan(of);
-    sum = warp_add(part(x, of, m));
+    sum = warp_add(rebase(x, of, m, c2));
   }
   const bool any = t.any;
   const float log_sum = m == -CUDART_INF_F ? -CUDART_INF_F : logf(sum);
@@ -303,7 +329,8 @@ __global__ void __launch_bounds__(kDistillThreads, kDistillPerSm) k_distill(Dist
     loss = warp_add(loss);
     if (lane == 0) {
       a.loss[r] = any ? weight * a.tau * a.tau * loss : 0.0f;
-      if (a.lse) a.lse[r] = !any ? CUDART_INF_F : m == -CUDART_INF_F ? m : m / a.tau + log_sum;
+      // +inf says that nothing flows back
+      if (a.lse) a.lse[r] = !any ? CUDART_INF_F : m == -CUDART_INF_F ? m : below_inf(m / a.tau + log_sum);
     }
   }
   if (grad) {
@@ -318,6 +345,18 @@ __global__ void __launch_bounds__(kDistillThreads, kDistillPerSm) k_distill(Dist
       write_zeros(s, grad);
   }
   if (ctas > 1) cluster.sync();  // no CTA leaves while its shared memory is read
+}
+
+// A whole row's maximum and sum, by one CTA: for a backward pass whose logsumexp is too coarse.
+template <typename T>
+__device__ __noinline__ float2 row_sums(const DistillArgs& a, int r, Targets& t, float c2) {
+  RowArgs rows = a.rows;
+  rows.per = INT_MAX;
+  Slice<T> s;
+  s.open(row_address<T>(rows, r), rows, 0, t.row_ends);
+  float sum;
+  const float top = lane_sums(s, c2, &sum), m = cta_sums(t, top, c2, &sum);
+  return make_float2(m, sum);
 }
 
 // the gradient from the row's logsumexp: a CTA per slice, nothing shared between them
@@ -339,11 +378,16 @@ __global__ void __launch_bounds__(kDistillThreads, kDistillPerSm) k_distill_back
     teacher.load(a, r, row_address<T>(a.rows, r));
     teacher.finish(a, r, row_address<T>(a.rows, r), t);
   }
-  // in a row of -inf alone every probability is 0
-  const float inv = 1.0f / a.tau, off = lse == -CUDART_INF_F ? 0.0f : -lse;
+  const float c2 = kLog2e / a.tau;
+  float at = lse * a.tau, scale = coef;
+  if (fabsf(lse) > kLseFine) {
+    const float2 sums = row_sums<T>(a, r, t, c2);
+    at = sums.x == -CUDART_INF_F ? 0.0f : sums.x;
+    scale = sums.x == -CUDART_INF_F ? 0.0f : coef / sums.y;  // in a row of -inf alone every probability is 0
+  }
   write_gradient(s, grad, coef, t, a.K, [=](float2 z) {
-    const float2 y = mul2(fma2(z, make_float2(inv, inv), make_float2(off, off)), make_float2(kLog2e, kLog2e));
-    return mul2(make_float2(exp2_32(y.x), exp2_32(y.y)), make_float2(coef, coef));
+    const float2 y = mul2(add2(z, make_float2(-at, -at)), make_float2(c2, c2));
+    return mul2(make_float2(exp2_32(y.x), exp2_32(y.y)), make_float2(scale, scale));
   });
 }
 

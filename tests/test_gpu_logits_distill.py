@@ -240,3 +240,37 @@ def test_refusals(cuda):
     assert (loss == 0).all()
     epic.distill_step(logits, ids[..., :0].contiguous(), vals[..., :0].contiguous(), loss.fill_(7), grad.fill_(7))
     assert (loss == 0).all() and (grad == 0).all()
+
+
+@pytest.mark.parametrize('tau', [0.5, 1.0, 2.5])
+@pytest.mark.parametrize('dtype', ['f32', 'f16', 'bf16'])
+@pytest.mark.parametrize('n,V,K', [(4, 1000, 5), (3, 40003, 16), (40, 4099, 3)])
+def test_backward_far_from_zero(cuda, n, V, K, dtype, tau):
+    """Rows at the type's lowest value (a mask that left nothing), and logits of a size whose logsumexp in 32 bits has little
+    or nothing left of the sum's logarithm: forward and backward agree with the formulas as the single call does."""
+    import torch
+    import paper_2606_00722_gb300 as epic
+    logits, ids, vals, valid, weight = make(2, n, V, K, dtype, 'normal', V + n)
+    logits[0, 0] = torch.finfo(logits.dtype).min
+    logits[0, 1] += 20000.0
+    logits[0, 2] -= 130.0 * tau
+    logits[1, 0] = -3.0e4
+    logits[1, 0, ::5] = -1.0e4
+    logits[1, 1] = torch.finfo(logits.dtype).max
+    logits[1, 2] += 110.0 * tau
+    valid.fill_(1)
+    g = torch.Generator().manual_seed(1)
+    up = (torch.rand((2, n), generator=g) + 0.2).cuda()
+    z = logits.double()
+    z -= z.amax(-1, keepdim=True)  # which the formulas do not notice, but 64 bits do at 1e38
+    want_loss, want_step = distill64(z, ids, vals, valid, weight, tau)
+    _, want_grad = distill64(z, ids, vals, valid, weight, tau, up)
+    loss, lse = torch.full((2, n), -7.0, device='cuda'), torch.full((2, n), -7.0, device='cuda')
+    grad = torch.full((2, n, V), 7.0, dtype=logits.dtype, device='cuda')
+    epic.distill_step(logits, ids, vals, loss, grad, tau=tau, weight=weight, valid=valid)
+    check(loss, grad, want_loss, want_step, ids, weight, tau, dtype)
+    loss.fill_(-7.0)
+    grad.fill_(7.0)
+    epic.distill_forward(logits, ids, vals, loss, lse, tau=tau, weight=weight, valid=valid)
+    epic.distill_backward(logits, ids, vals, lse, up, grad, tau=tau, weight=weight, valid=valid)
+    check(loss, grad, want_loss, want_grad, ids, weight, tau, dtype, up)
