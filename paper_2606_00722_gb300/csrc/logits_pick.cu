@@ -70,7 +70,7 @@ struct TopList {  // a sampler's top-k list, in order
   uint32_t kept[kMaxK];
 };
 
-struct Tops {  // largest lane maxima (value keys): of this CTA's warps, and past kTops of all of the row's
+struct Tops {  // value keys: largest lane maxima of this CTA's warps, and past kTops of all of the row's; ends of a range
   uint32_t value[2 * kTops];
 };
 
@@ -341,15 +341,30 @@ struct Row {
 
   // After a barrier: the K first keys of the row are in the first CTA's list, with others or (where more than a list
   // was collected) alone.
-  __device__ void settle(int K) {
+  __device__ void settle(int K, float m) {
     if (*group.at(&shared().count, 0) <= kListMax) return;  // the same in all CTAs
-    const Floor floor = floor_of(threshold(*this, Weigher{CUDART_INF_F, 0.0f}, no_floor(), K - 1, false, -1.0f));
+    const Floor floor = floor_of(threshold(*this, Weigher{m, 1.0f}, no_floor(), K - 1, false, -1.0f));
     if (group.rank == 0 && threadIdx.x == 0) shared().count = 0;
     group.sync();
     int* count = group.at(&shared().count, 0);
     u64* list = group.at(shared().list, 0);
-    each([&](float z, int i) {
-      if (floor.in(z, i)) list[atomicAdd(count, 1)] = order_key(z, i);
+    s.sweep([&](const uint4 (&v)[4], int c) {
+      ChunkMax<T, false> top;
+      top.add(v);
+      if (!__any_sync(~0u, top.value() >= floor.z)) return;
+#pragma unroll 1
+      for (int i = 0; i < 4; ++i) {
+        float z[E];
+        unpack<T>(s.chunk(c + 32 * i), z);
+        const int i0 = s.first(c + 32 * i);
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (floor.in(z[e], i0 + e)) {
+            const int at = atomicAdd(count, 1);
+            if (at < kListMax) list[at] = order_key(z[e], i0 + e);
+          }
+      }
+      __syncwarp();
     });
     group.sync();
   }
@@ -510,6 +525,7 @@ struct Row {
     int* count = group.at(&shared().count, 0);
     u64* list = group.at(shared().list, 0);
     const bool keep = kFree || min_p >= 0.0f;
+    bool full = false;  // this lane has seen the list full: how many more there are does not matter
     s.sweep([&](const uint4 (&v)[4], int c) {
       ChunkMax<T, false> top;
       top.add(v);
@@ -551,12 +567,79 @@ struct Row {
       for (; in_bin; in_bin &= in_bin - 1) {
         const int bit = __ffs(in_bin) - 1, index = s.first(c + 32 * (bit / E)) + bit % E;
         const float z = s.at(index);
-        if (!kFree && !floor.in(z, index)) continue;
+        if (full || (!kFree && !floor.in(z, index))) continue;
         const int at = atomicAdd(count, 1);
-        if (at < kListMax) list[at] = order_key(z, index);
+        full = at >= kListMax;
+        if (!full) list[at] = order_key(z, index);
       }
       __syncwarp();
     });
+  }
+
+  // After a barrier, before another: the largest and smallest of the level's values from the floor on, by each warp, as
+  // value keys to tops[warp] and tops[kRowWarps + warp].
+  __device__ __noinline__ static void range_of(Row row, Level level, Floor floor) {
+    const int warp = warp_index();
+    float most = -CUDART_INF_F, least = CUDART_INF_F;
+    row.s.sweep([&](const uint4 (&v)[4], int c) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float z[E];
+        unpack<T>(v[i], z);
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (level.has(z[e]) && floor.in(z[e], row.s.first(c + 32 * i) + e)) {
+            most = fmaxf(most, z[e]);
+            least = fminf(least, z[e]);
+          }
+      }
+    });
+    const uint32_t hi = __reduce_max_sync(~0u, value_key(most)), lo = __reduce_min_sync(~0u, value_key(least));
+    if (threadIdx.x % 32 == 0) {
+      shared().tops.value[warp] = hi;
+      shared().tops.value[kRowWarps + warp] = lo;
+    }
+  }
+
+  // After a barrier of the group: whether the values that range_of() saw are all the same, and that value.
+  __device__ __noinline__ static bool one_value(Row row, float* value) {
+    const int lane = (int)threadIdx.x % 32, warps = (int)blockDim.x / 32;
+    uint32_t most = 0, least = ~0u;
+#pragma unroll 1
+    for (unsigned r = 0; r < row.group.n; ++r)
+      if (lane < warps) {
+        most = max(most, *row.group.at(&shared().tops.value[lane], r));
+        least = min(least, *row.group.at(&shared().tops.value[kRowWarps + lane], r));
+      }
+    most = __reduce_max_sync(~0u, most);
+    *value = key_value(most);
+    return most == __reduce_min_sync(~0u, least);
+  }
+
+  // The rest of a threshold's search among elements of one value, which follow each other by index: the key of the one with
+  // `ahead` others from the floor on before it.
+  __device__ __noinline__ static u64 by_index(Row row, float value, Floor floor, u64 ahead) {
+    row.s.sweep([&](const uint4 (&v)[4], int c) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float z[E];
+        unpack<T>(v[i], z);
+        uint32_t n = 0;
+#pragma unroll
+        for (int e = 0; e < E; ++e) n += z[e] == value && floor.in(z[e], row.s.first(c + 32 * i) + e);
+        row.add_part(LaneMass{0, n}, c + 32 * i);
+      }
+    });
+    row.group.sync();
+    u64 mine, before;
+    row.all_mass(&mine, &before);
+    if (warp_index() == 0 && ahead >= before && ahead < before + mine)
+      row.locate(ahead - before, [&](float z, int i) { return z == value && floor.in(z, i) ? 1u : 0u; },
+                 [&](float z, int i) { *row.group.at(&shared().found, 0) = order_key(z, i); });
+    row.group.sync();
+    const u64 key = *row.group.at(&shared().found, 0);
+    row.group.sync();
+    return key;
   }
 
   // One warp: the lowest of the level's values whose bin is at most b, to the lower half of the lanes, and the lowest whose
@@ -687,8 +770,9 @@ struct Row {
   // The key of the element, among those from the floor on, at which the running total of the order passes the target:
   // with `mass` totals are masses and the target floor(arg all / 2^24) - 1, else they are counts and it is arg (or the
   // last).  All ones for a row without elements.  A histogram over evenly spaced exponents finds the bin; where it has
-  // more elements than a list, the next one cuts it again; the first CTA sorts the bin's elements.  What still does not
-  // fit, many equal values, is told apart by eight bits of the keys at a time.
+  // more elements than a list, the next one cuts it again, or where they are equal they are counted off; the first CTA
+  // sorts the bin's elements.  What does not fit after kLevels (values whose exponents a high temperature leaves too close),
+  // and rows of +inf, is told apart by eight bits of the keys at a time.
   // With min_p >= 0 the masses of the kept tokens (from the threshold on, of at least min_p) are left by part
   // as masses() leaves them, a barrier of the group included.
   __device__ __noinline__ static u64 threshold(Row row, Weigher weigh, Floor floor, u64 arg, bool mass, float min_p) {
@@ -718,25 +802,23 @@ struct Row {
       for (int i = (int)threadIdx.x; i < kBins; i += (int)blockDim.x) shared().bins.low[i] = shared().bins.high[i] = 0;
       if (threadIdx.x == 0) shared().count = 0;
       __syncthreads();
-      if (mass && first && !digits && !special) {
-        count_masses(weigh, floor, free);
-      } else if (!mass && !digits) {
-        count_elements(weigh, floor, level);
-      } else {
+      if (digits) {
         each([&](float z, int i) {
           if (!level.has(z) || !floor.in(z, i)) return;
-          int b;
-          if (digits) {
-            const u64 key = order_key(z, i);
-            if (shift < 56 && (key ^ prefix) >> (shift + 8)) return;
-            b = 255 - (int)(key >> shift & 255);
-          } else {
-            b = level.bin(weigh.exponent(z));
-          }
+          const u64 key = order_key(z, i);
+          if (shift < 56 && (key ^ prefix) >> (shift + 8)) return;
+          const int b = 255 - (int)(key >> shift & 255);
           const uint32_t q = mass ? grid_mass(weigh(z)) : 1u;
           add_shared(&shared().bins.low[b], q & 0x7fffu);
           add_shared(&shared().bins.high[b], q >> 15);
         });
+      } else if (mass && first && !special) {
+        count_masses(weigh, floor, free);
+      } else {
+        if (mass)
+          count_elements<true>(weigh, floor, level);
+        else
+          count_elements<false>(weigh, floor, level);
       }
       __syncthreads();
       sum_groups();
@@ -776,7 +858,13 @@ struct Row {
       }
       __syncthreads();
       level.enter(bin, shared().bin_low, shared().bin_high);
+      range_of(*this, level, floor);
       group.sync();  // all have seen the count
+      float value;
+      if (one_value(*this, &value)) {
+        prefix = by_index(*this, value, floor, mass ? t / max(grid_mass(weigh(value)), 1u) : t);
+        break;
+      }
     }
     if (keep) masses(*this, weigh, Kept{floor_of(prefix), min_p});
     group.sync();
@@ -810,7 +898,8 @@ struct Row {
     });
   }
 
-  // a level's histogram of counts
+  // any level's histogram, of counts or masses
+  template <bool kMass>
   __device__ __forceinline__ void count_elements(const Weigher& weigh, Floor floor, const Level& level) const {
     s.sweep([&](const uint4 (&v)[4], int c) {
 #pragma unroll
@@ -819,8 +908,18 @@ struct Row {
         unpack<T>(v[i], z);
         const int i0 = s.first(c + 32 * i);
 #pragma unroll
-        for (int e = 0; e < E; ++e)
-          add_shared(&shared().bins.low[level.bin(weigh.exponent(z[e]))], level.has(z[e]) && floor.in(z[e], i0 + e) ? 1u : 0u);
+        for (int e = 0; e < E; ++e) {
+          const float y = weigh.exponent(z[e]);
+          const int b = level.bin(y);
+          const bool in = level.has(z[e]) && floor.in(z[e], i0 + e);
+          if (!kMass) {
+            add_shared(&shared().bins.low[b], in ? 1u : 0u);
+          } else {
+            const uint32_t q = in ? grid_mass(exp2_32(y)) : 0u;
+            add_shared(&shared().bins.low[b], q & 0x7fffu);
+            add_shared(&shared().bins.high[b], q >> 15);
+          }
+        }
       }
     });
   }
@@ -876,6 +975,16 @@ struct Row {
   }
   __device__ __forceinline__ void find_token(u64 t, const Weigher& weigh, const Kept& kept, u64 all, int32_t* tok,
                                              float* prob) const {
+    locate(t, [&](float z, int i) { return kept_mass(z, i, weigh, kept); },
+           [&](float z, int i) {
+             *tok = i;
+             *prob = weigh(z) * kGrid / (float)all;
+           });
+  }
+  // one warp: found(value, index), by one lane, of the element at which the total of mass(value, index), noted by part,
+  // passes t
+  template <typename M, typename F>
+  __device__ __forceinline__ void locate(u64 t, M mass, F found) const {
     const int lane = (int)threadIdx.x % 32;
     const int parts = (s.n + 31) / 32, per = (parts + 31) / 32;  // parts of a lane
     u64 sum = 0;
@@ -894,23 +1003,23 @@ struct Row {
     uint32_t q[E];
     sum = 0;
 #pragma unroll
-    for (int e = 0; e < E; ++e) sum += q[e] = kept_mass(z[e], i0 + e, weigh, kept);
+    for (int e = 0; e < E; ++e) sum += q[e] = mass(z[e], i0 + e);
     upto = warp_scan(sum);
-    if (t < upto - sum || t >= upto) return;
-    t -= upto - sum;
-    // this lane's chunk has the token
-    float value = 0.0f;
-    int at = -1;
+    if (t >= upto - sum && t < upto) {  // this lane's chunk has the element
+      t -= upto - sum;
+      float value = 0.0f;
+      int at = -1;
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      if (at < 0 && t < q[e]) {
-        at = e;
-        value = z[e];
+      for (int e = 0; e < E; ++e) {
+        if (at < 0 && t < q[e]) {
+          at = e;
+          value = z[e];
+        }
+        t -= at < 0 ? q[e] : 0;
       }
-      t -= at < 0 ? q[e] : 0;
+      found(value, i0 + at);
     }
-    *tok = i0 + at;
-    *prob = weigh(value) * kGrid / (float)all;
+    __syncwarp();
   }
 
   // the first CTA: draws from the top-k list that settle() left
@@ -1024,7 +1133,7 @@ struct Propose {
     for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
     if (lane == 0) *row.group.at(&shared().sums[row.group.rank * warps + warp], 0) = sum;
     row.group.sync();
-    row.settle(a.K);
+    row.settle(a.K, weigh.m);
     if (row.group.rank != 0) return;
     sum = 0.0f;
     for (int i = 0; i < (int)row.group.n * warps; ++i) sum += shared().sums[i];
@@ -1080,7 +1189,7 @@ struct Sample {
     if (by_list) {
       row.collect(floor, top);
       row.group.sync();
-      row.settle(top_k);
+      row.settle(top_k, weigh.m);
       if (row.group.rank != 0) return;
       row.draw_from_list(weigh, good ? top_k : 0, p24, min_p, u, a.S, tok, prob);
       if (row.group.n > 1) row.group.sync();  // the others have looked at the count
