@@ -18,8 +18,8 @@ struct RowShape {
   int per;      // chunks of 16 bytes per CTA
 };
 
-// A row of V elements of `size` bytes, `rows` of them in the call; CTAs of at most `threads` threads.
-RowShape row_shape(long long rows, int V, int size, int threads);
+// A row of V elements of `size` bytes, `rows` of them in the call; CTAs of at least `least` and at most `most` threads.
+RowShape row_shape(long long rows, int V, int size, int least, int most);
 
 // EPIC_OK, or the error of a bad description of rows
 epic_status check_rows(const void* logits, int dtype, int B, int n, int V, int64_t stride_b, int64_t stride_n,

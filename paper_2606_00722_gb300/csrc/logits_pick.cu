@@ -25,6 +25,7 @@ namespace epic {
 namespace {
 
 constexpr int kListMax = 2048;  // most keys collected for ranking; a power of two, to which sorting fills up
+constexpr int kRankMax = 192;  // longest list whose ranks are counted, n^2 / threads steps; longer ones are sorted
 constexpr int kMaxK = 256;      // most candidates of a position, and the longest top-k list
 constexpr int kMaxV = kRowCtasMax * (kSliceElems - 16);  // 1,047,872: histograms and parts of a row's slices
 constexpr int kBins = 2048;     // of a threshold's histogram
@@ -39,6 +40,10 @@ constexpr float kGrid = 1073741824.0f;      // 2^30: the weights' grid
 constexpr float kOnes = 12582912.0f;       // 1.5 * 2^23
 constexpr float kHigh = 412316860416.0f;   // 1.5 * 2^38
 constexpr uint32_t kOnesBits = 0x4b400000u, kHighBits = 0x52c00000u;
+
+// Fewest threads of a CTA: short rows have less to read than to rank, clear and draw (80 rows of 1,280, 64 best of them drawn
+// from: 80 us with 64 threads, 31 with 256; 2,688 rows of 300: 158, 87, and 152 with 512, which leave an SM two rows for four).
+constexpr int kPickThreadsMin = 256;
 
 struct PickArgs {
   RowArgs rows;
@@ -239,11 +244,13 @@ struct Row {
   // twice K of them.  About 1.4 K elements of a row in random order reach it; the lowest of the warps' j-th, which needs
   // no ranking, lets ten times K through at one lane maximum a warp.
   __device__ float top_of(float lane_top, int K, float* floor) {
-    const int warps = (int)blockDim.x / 32, w = warp_index(), lane = (int)threadIdx.x % 32;
+    const int w = warp_index(), lane = (int)threadIdx.x % 32;
+    // a short row's warps without elements have no say
+    const int warps = group.n == 1 ? min((int)blockDim.x / 32, max((s.n + kBatch - 1) / kBatch, 1)) : (int)blockDim.x / 32;
     const int all = warps * (int)group.n;
     const int j = K > 0 ? min((2 * K + all - 1) / all, 32) : 1;
     uint32_t key = value_key(lane_top);
-    for (int i = 0; i < j; ++i) {
+    for (int i = 0; i < j && w < warps; ++i) {
       const uint32_t x = __reduce_max_sync(~0u, key);
       if (lane == 0) shared().tops.value[w * j + i] = x;
       if (__ffs(__ballot_sync(~0u, key == x)) - 1 == lane) key = 0;
@@ -373,7 +380,7 @@ struct Row {
   template <typename F>
   __device__ __forceinline__ void ranked(F f) {
     const int n = shared().count;
-    if (n > 512) {
+    if (n > kRankMax) {
       sort_list(n);
       for (int i = (int)threadIdx.x; i < n; i += (int)blockDim.x) f(i, shared().list[i]);
       return;
@@ -1071,6 +1078,11 @@ struct Row {
 };
 
 // ---- the K best
+//
+// conf = 2^((z - m) c) / sum, one pass from memory with a running maximum, then a few thousand elements from L2.  1,024 rows
+// of 126,000 bf16, 32 best: 62 us, 4.2 TB/s, where a copy of the bytes at 6.7 TB/s is 39 us.  What is left: issue slots
+// (57 % used; eight instructions an element) and the waits of a row's ranking, which three rows an SM cover in part.
+// Two CTAs an SM with 64 registers: 72 us.  Few rows: a call on the host takes 6.7 us, 64 rows of 32,768 on the GPU 6.1.
 
 template <typename T>
 struct Propose {
@@ -1156,6 +1168,12 @@ struct Propose {
 };
 
 // ---- draws
+//
+// A pass from memory for the maximum, one from L2 for the masses by part, a chunk a lane for each draw; with a nucleus or a
+// long top-k a pass for the histogram and one for the bin's elements and the kept masses in place of that of masses.
+// 1,024 rows of 126,000 bf16: 100 us by temperature, 301 us with top-p; bound by instructions (55 and 67 % of the issue
+// slots; 17 and 55 an element, of which the histogram's two additions to shared memory are the slowest: one of 64 bits
+// took 570 us in all).  Two CTAs an SM: three of 40 registers spill (161 us by temperature).
 
 template <typename T>
 struct Sample {
@@ -1236,7 +1254,7 @@ __global__ void __launch_bounds__(kRowThreads, kPerSm) k_rows(PickArgs a) {
 
 template <typename T, template <typename> class Op, int kPerSm>
 epic_status launch(PickArgs& a, long long rows, cudaStream_t st) {
-  const RowShape p = row_shape(rows, a.rows.V, sizeof(T), kRowThreads);
+  const RowShape p = row_shape(rows, a.rows.V, sizeof(T), kPickThreadsMin, kRowThreads);
   a.rows.per = p.per;
   return launch_rows((const void*)k_rows<T, Op, kPerSm>, p, rows, &a, st);
 }
