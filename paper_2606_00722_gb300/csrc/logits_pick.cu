@@ -317,10 +317,10 @@ struct Row {
       uint32_t hits = 0;
 #pragma unroll
       for (int e = 0; e < E; ++e) hits |= z[e] >= floor && z[e] > -CUDART_INF_F ? 1u << e : 0u;
-      for (; hits; hits &= hits - 1) {
+      if (!hits) return;
+      for (int at = atomicAdd(count, __popc(hits)); hits && at < kListMax; hits &= hits - 1, ++at) {
         const int index = s.first(c) + __ffs(hits) - 1;
-        const int at = atomicAdd(count, 1);
-        if (at < kListMax) list[at] = order_key(s.at(index), index);
+        list[at] = order_key(s.at(index), index);
       }
     };
     uint32_t who = __ballot_sync(~0u, top.first >= floor && top.first > -CUDART_INF_F);
