@@ -4,10 +4,10 @@
 
 namespace epic {
 
-// One CTA a row where the rows fill the GPU (two CTAs an SM), or have at most 4,096 chunks: 259 rows of 50,021 halves take
-// 12.8 us so and 20.5 in clusters of two, 64 rows of 32,768 (4,096 chunks) 6.2 and 7.4.  Fewer long rows are cut over clusters
-// of up to eight CTAs: one row of 126,000 takes 8.7 us in four CTAs and 10.0 in one.  Slices are cut further where they would
-// be longer than a histogram's sums allow.
+// One CTA a row where the rows fill the GPU (two CTAs an SM), or have at most 4,096 chunks: 259 rows of 50,021 halves
+// take 12.8 us so and 20.5 in clusters of two, 64 rows of 32,768 (4,096 chunks) 6.2 and 7.4.  Fewer long rows are cut over
+// clusters of up to eight CTAs: one row of 126,000 takes 8.7 us in four CTAs and 10.0 in one.  Slices are cut further where
+// they would be longer than a histogram's sums allow.
 RowShape row_shape(long long rows, int V, int size, int least, int most) {
   const long long E = 16 / size;
   const long long chunks = V ? (V + E - 2) / E + 1 : 0;  // wherever the row starts in its first chunk

@@ -133,8 +133,8 @@ __device__ __forceinline__ uint4 shifted(const uint4& a, const uint4& b, int by)
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// The slice's elements of a gradient row, g(z) for two of them at a time.  The chunks are the gradient's: where its row starts elsewhere in
-// 16 bytes than the logits' row does, two chunks of logits are read for one of gradient.
+// The slice's elements of a gradient row, g(z) for two of them at a time.  The chunks are the gradient's: where its row
+// starts elsewhere in 16 bytes than the logits' row does, two chunks of logits are read for one of gradient.
 template <typename T, typename G>
 __device__ void write_row(const Slice<T>& s, T* grad, G g) {
   constexpr int E = ElemOf<T>::E;
@@ -271,9 +271,9 @@ __device__ __forceinline__ float cta_sums(Targets& t, float top, float c2, float
   return m;
 }
 
-// Loss, and with a.grad the gradient: one cluster a row (32,768 bf16, 4,096 rows, half of them of weight 0: 72 us, 5.6 TB/s
-// of a copy's 6.7; 384 threads, four CTAs an SM: 74 us where 512 and two took 90.  The loss alone, 1,024 rows of 126,000:
-// 48 us, 5.4 TB/s).  Bound by memory, and by the barriers between a row's two passes.
+// Loss, and with a.grad the gradient: one cluster a row.  Bound by memory, and by the barriers between a row's two passes:
+// both for 4,096 rows of 32,768 bf16, half of them of weight 0, take 72 us, 5.6 TB/s where a copy reaches 6.7 (with 384
+// threads and four CTAs an SM; 512 and two took 90 when these took 74); the loss of 1,024 rows of 126,000 takes 48, 5.4 TB/s.
 //  One pass keeps each lane's maximum so far and the sum of
 // exponentials relative to it; the gradient's pass reads the row again, from the caches.
 template <typename T>

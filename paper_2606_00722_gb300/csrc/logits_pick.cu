@@ -695,7 +695,8 @@ struct Row {
   }
 
   // After a barrier, in one warp: the bin of the cluster's histograms at which the running total passes t, and the rest
-  // of t within it, to shared().found and shared().before; all ones for histograms of nothing.  t may be given as a share of all.
+  // of t within it, to shared().found and shared().before; all ones for histograms of nothing.  t may be given as a share of
+  // all.
   __device__ __forceinline__ void find_bin(u64 t, bool share, bool mass) const {
     static_assert(kGroups == 64, "two groups of bins a lane");
     const int lane = (int)threadIdx.x % 32;
@@ -1081,7 +1082,7 @@ struct Row {
 //
 // conf = 2^((z - m) c) / sum, one pass from memory with a running maximum, then a few thousand elements from L2.  1,024 rows
 // of 126,000 bf16, 32 best: 62 us, 4.2 TB/s, where a copy of the bytes at 6.7 TB/s is 39 us.  What is left: issue slots
-// (57 % used; eight instructions an element) and the waits of a row's ranking, which three rows an SM cover in part.
+// (56 % used; nine instructions an element) and the waits of a row's ranking, which three rows an SM cover in part.
 // Two CTAs an SM with 64 registers: 72 us.  Few rows: a call on the host takes 6.7 us, 64 rows of 32,768 on the GPU 6.1.
 
 template <typename T>
