@@ -516,21 +516,22 @@ def distill_loss(logits, ids, vals, tau=1.0, weight=None, valid=None):
 
     class Loss(torch.autograd.Function):
         @staticmethod
-        def forward(ctx, z):
+        def forward(ctx, z, ids, vals, weight, valid):
             loss = torch.empty(z.shape[:2], dtype=torch.float32, device=z.device)
             lse = torch.empty_like(loss)
             distill_forward(z, ids, vals, loss, lse, tau, weight, valid)
-            ctx.save_for_backward(z, lse)
+            ctx.save_for_backward(z, lse, ids, vals, weight, valid)
             return loss
 
         @staticmethod
+        @torch.autograd.function.once_differentiable
         def backward(ctx, grad_loss):
-            z, lse = ctx.saved_tensors
+            z, lse, ids, vals, weight, valid = ctx.saved_tensors
             grad = torch.empty(z.shape, dtype=z.dtype, device=z.device)
             distill_backward(z, ids, vals, lse, grad_loss.to(torch.float32).contiguous(), grad, tau, weight, valid)
-            return grad
+            return grad, None, None, None, None
 
-    return Loss.apply(logits)
+    return Loss.apply(logits, ids, vals, weight, valid)
 
 
 def decode_step_from_logits(g: Grammar, t: LexTable, x, pos, logits, n_target, bufs, temperature=None, u=None,

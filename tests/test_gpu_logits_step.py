@@ -110,3 +110,22 @@ def test_loss_as_a_torch_operation(cuda):
     (want * up.double()).sum().backward()
     assert ((loss.double() - want).abs() <= 3.2e-5 * weight.double() * tau ** 2).all()
     assert ((z.grad.double() - z64.grad).abs() <= (6e-5 * tau * (weight * up).double())[..., None]).all()
+
+
+def test_loss_keeps_what_its_gradient_needs(cuda):
+    """Targets overwritten between the loss and its gradient are an error, not a wrong gradient; the gradient itself has no
+    further one; without rows that need gradients there is none."""
+    import torch
+    import paper_2606_00722_gb300 as epic
+    z = torch.randn((1, 2, 50), device=cuda, requires_grad=True)
+    ids = torch.arange(3, dtype=torch.int32, device=cuda).repeat(1, 2, 1)
+    vals = torch.zeros((1, 2, 3), device=cuda)
+    loss = epic.distill_loss(z, ids, vals)
+    vals.add_(1.0)
+    with pytest.raises(RuntimeError):
+        loss.sum().backward()
+    loss = epic.distill_loss(z, ids, vals)
+    grad, = torch.autograd.grad(loss.sum(), z, create_graph=True)
+    with pytest.raises(RuntimeError):
+        grad.sum().backward()
+    assert not epic.distill_loss(z.detach(), ids, vals).requires_grad
