@@ -118,12 +118,6 @@ def work(case):
 
 # ---------------------------------------------------------------- inputs
 
-def _distinct(gen, rows, h, V, dev):
-    """h different ids below V for each row: from a random one on, in random steps of V / h at most."""
-    steps = torch.randint(1, V // h + 1, (rows, h), generator=gen, device=dev).cumsum(1)
-    return (torch.randint(0, V, (rows, 1), generator=gen, device=dev) + steps) % V
-
-
 def _logits(gen, B, n, V, pad, dtype, dev):
     """A model's output: a broad bulk, a few dozen likely tokens of very different strength in each row, and the mask
     token (the last id) never allowed.  One row in eight is hard text (flat), one in eight nearly certain."""
@@ -131,7 +125,7 @@ def _logits(gen, B, n, V, pad, dtype, dev):
     kind = torch.randint(0, 8, (B * n, 1), generator=gen, device=dev)
     z *= torch.where(kind == 0, 0.8, 1.9)
     h = min(V, 24)
-    at = _distinct(gen, B * n, h, V, dev)
+    at = torch.randint(0, V, (B * n, h), generator=gen, device=dev)
     up = torch.rand((B * n, h), generator=gen, device=dev) ** 2 * (math.log(V) + 1.0)
     up = torch.where(kind == 0, up * 0.3, torch.where(kind == 1, up * 1.8, up))
     z.scatter_add_(1, at, up)
@@ -169,7 +163,7 @@ def prepare(case, seed):
     s = {'case': case, 'logits': _logits(gen, B, n, V, case['pad'], case['dtype'], dev)}
     if case['op'] == 'distill':
         K, rows = case['K'], B * n
-        ids = _distinct(gen, rows, K, V - 1, dev).view(B, n, K).to(torch.int32)
+        ids = torch.randint(0, V - 1, (B, n, K), generator=gen, device=dev).to(torch.int32)
         vals = -torch.sort(torch.rand((B, n, K), generator=gen, device=dev) * 8.0, dim=-1).values
         # the student knows some of it: its logits lean towards the teacher's
         s['logits'].scatter_(2, ids.long(), (vals * 0.7 + math.log(V)).to(s['logits'].dtype))
