@@ -5,11 +5,10 @@
 #include <stdint.h>
 
 #include "../../include/epic.h"
+#include "mass_parts.h"
 
 namespace epic {
 
-// Most elements of a slice whose masses, in parts of 15 and 16 bits, a histogram's 32-bit bins can add up.
-constexpr int kSliceElems = 131000;
 constexpr int kRowCtasMax = 8;  // the portable limit of a cluster
 
 struct RowShape {

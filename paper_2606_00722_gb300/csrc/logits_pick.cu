@@ -20,6 +20,7 @@
 #include "../../include/epic.h"
 #include "logit_launch.h"
 #include "logit_rows.cuh"
+#include "mass_parts.h"
 
 namespace epic {
 namespace {
@@ -60,12 +61,11 @@ struct PickArgs {
   float* prob;
 };
 
-// A bin's mass is low + 2^15 high, as an element's is: its high part is at most 2^15, its low one within 2^14 of 0, so
-// the sums over a slice of at most kSliceElems elements fit 32 bits (low a signed one).
+// The bins hold the sums of their elements' parts (MassParts, whatever adds to them); counts are sums of low parts of 1.
 struct Histogram {
   uint32_t low[kBins], high[kBins];
   u64 group[kGroups];
-  __device__ __forceinline__ u64 mass(int i) const { return ((u64)high[i] << 15) + (u64)(long long)(int)low[i]; }
+  __device__ __forceinline__ u64 mass(int i) const { return MassParts{high[i], low[i]}.value(); }
 };
 
 struct TopList {  // a sampler's top-k list, in order
@@ -119,7 +119,7 @@ struct Weigher {
 
 __device__ __forceinline__ uint32_t grid_mass(float w) { return __float2uint_rn(w * kGrid); }
 
-// The masses of two weights in parts, grid_mass = 2^15 high + low, high and low as bits over kHighBits and kOnesBits.
+// The masses of two weights in parts, low ones within 2^14 of 0, high and low as bits over kHighBits and kOnesBits.
 // Three additions for two elements: the conversion instruction does a quarter of a warp a cycle on the pipe that the
 // exponentials need.  Not for NaN.
 struct Parts2 {
@@ -408,13 +408,9 @@ struct Row {
   }
 
   // A lane's kept mass of a chunk in parts, whose sums over a warp are below 32 bits.
-  struct LaneMass {
-    uint32_t high, low;
-    __device__ __forceinline__ u64 value() const { return ((u64)high << 15) + (u64)(long long)(int)low; }
-  };
   template <bool kAll>
-  __device__ __forceinline__ LaneMass lane_mass(const uint4& v, int c, const Weigher& weigh, const Kept& kept) const {
-    LaneMass sum = {0, 0};
+  __device__ __forceinline__ MassParts lane_mass(const uint4& v, int c, const Weigher& weigh, const Kept& kept) const {
+    MassParts sum = {0, 0};
     if (kAll) sum = {0u - (uint32_t)E * kHighBits, 0u - (uint32_t)E * kOnesBits};
     float z[E];
     unpack<T>(v, z);
@@ -440,8 +436,8 @@ struct Row {
   }
 
   // the warp's sum of its lanes' masses of 32 chunks to their part
-  __device__ __forceinline__ void add_part(LaneMass q, int c) const {
-    const LaneMass sum = {__reduce_add_sync(~0u, q.high), __reduce_add_sync(~0u, q.low)};
+  __device__ __forceinline__ void add_part(MassParts q, int c) const {
+    const MassParts sum = {__reduce_add_sync(~0u, q.high), __reduce_add_sync(~0u, q.low)};
     if (threadIdx.x % 32 == 0 && c < s.n) shared().parts[part_at(c / 32)] = sum.value();
   }
   // before a barrier
@@ -458,7 +454,7 @@ struct Row {
 #pragma unroll 1
         for (int i = 0; i < 4; ++i) {
           const u64 q = row.chunk_mass(row.s.chunk(c + 32 * i), c + 32 * i, weigh, kept);
-          row.add_part(LaneMass{(uint32_t)(q >> 15), (uint32_t)q & 0x7fffu}, c + 32 * i);
+          row.add_part(MassParts{(uint32_t)(q >> 15), (uint32_t)q & 0x7fffu}, c + 32 * i);
         }
       });
     } else if (kept.all()) {
@@ -543,7 +539,7 @@ struct Row {
       for (int i = 0; i < 4; ++i) {
         float z[E];
         unpack<T>(v[i], z);
-        LaneMass sum = {0u - (uint32_t)E * kHighBits, 0u - (uint32_t)E * kOnesBits};
+        MassParts sum = {0u - (uint32_t)E * kHighBits, 0u - (uint32_t)E * kOnesBits};
         const int i0 = s.first(c + 32 * i);
 #pragma unroll
         for (int e = 0; e < E; e += 2) {
@@ -634,7 +630,7 @@ struct Row {
         uint32_t n = 0;
 #pragma unroll
         for (int e = 0; e < E; ++e) n += z[e] == value && floor.in(z[e], row.s.first(c + 32 * i) + e);
-        row.add_part(LaneMass{0, n}, c + 32 * i);
+        row.add_part(MassParts{0, n}, c + 32 * i);
       }
     });
     row.group.sync();
@@ -816,9 +812,9 @@ struct Row {
           const u64 key = order_key(z, i);
           if (shift < 56 && (key ^ prefix) >> (shift + 8)) return;
           const int b = 255 - (int)(key >> shift & 255);
-          const uint32_t q = mass ? grid_mass(weigh(z)) : 1u;
-          add_shared(&shared().bins.low[b], q & 0x7fffu);
-          add_shared(&shared().bins.high[b], q >> 15);
+          const MassParts q = mass_parts(mass ? grid_mass(weigh(z)) : 1u);
+          add_shared(&shared().bins.low[b], q.low);
+          add_shared(&shared().bins.high[b], q.high);
         });
       } else if (mass && first && !special) {
         count_masses(weigh, floor, free);
@@ -923,9 +919,9 @@ struct Row {
           if (!kMass) {
             add_shared(&shared().bins.low[b], in ? 1u : 0u);
           } else {
-            const uint32_t q = in ? grid_mass(exp2_32(y)) : 0u;
-            add_shared(&shared().bins.low[b], q & 0x7fffu);
-            add_shared(&shared().bins.high[b], q >> 15);
+            const MassParts q = mass_parts(in ? grid_mass(exp2_32(y)) : 0u);
+            add_shared(&shared().bins.low[b], q.low);
+            add_shared(&shared().bins.high[b], q.high);
           }
         }
       }

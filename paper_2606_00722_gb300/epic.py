@@ -23,7 +23,7 @@ _SRC = [os.path.join(_HERE, 'csrc', f) for f in
 _DEPS = _SRC + [os.path.join(_HERE, 'csrc', f) for f in
                 ('grammar.h', 'device.cuh', 'walk.cuh', 'cover.cuh', 'warpwalk.cuh', 'packs.cuh',
                  'seqpack.cuh', 'launch.h', 'region.cuh', 'gscols.cuh', 'rows.cuh', 'skeleton.cuh',
-                 'logit_rows.cuh', 'logit_launch.h')] + \
+                 'logit_rows.cuh', 'logit_launch.h', 'mass_parts.h')] + \
     [os.path.join(_HERE, '..', 'include', 'epic.h'), os.path.join(_HERE, '..', 'include', 'epic_measure.h')]
 LIB_PATH = os.path.join(_HERE, '_build', 'libepic.so')
 ARCH_FLAGS = ['-gencode', 'arch=compute_103a,code=sm_103a']
