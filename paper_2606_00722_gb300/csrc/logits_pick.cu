@@ -635,7 +635,7 @@ struct Row {
     });
     row.group.sync();
     u64 mine, before;
-    row.all_mass(&mine, &before);
+    ahead = min(ahead, row.all_mass(&mine, &before) - 1);  // the last one takes what lies past the end
     if (warp_index() == 0 && ahead >= before && ahead < before + mine)
       row.locate(ahead - before, [&](float z, int i) { return z == value && floor.in(z, i) ? 1u : 0u; },
                  [&](float z, int i) { *row.group.at(&shared().found, 0) = order_key(z, i); });
@@ -933,6 +933,10 @@ struct Row {
     const int lane = (int)threadIdx.x % 32, warps = (int)blockDim.x / 32, warp = warp_index();
     const bool keep = min_p >= 0.0f;
     if (group.rank == 0) {
+      if (threadIdx.x == 0) {  // the answer of an empty list
+        shared().found = ~0ull;
+        shared().last = -1;
+      }
       sort_list(n);
       // the running total down the list
       u64 ahead = 0;
@@ -947,7 +951,7 @@ struct Row {
         const u64 w_q = lane < warps ? shared().warp_q[lane] : 0, w_upto = warp_scan(w_q);
         const u64 before = ahead + __shfl_sync(~0u, w_upto - w_q, warp);
         ahead += __shfl_sync(~0u, w_upto, 31);
-        if (before + upto - q <= t && t < before + upto) {
+        if (i < n && passes(before + upto - q, q, t, i == n - 1)) {
           shared().found = key;
           shared().last = i;
         }

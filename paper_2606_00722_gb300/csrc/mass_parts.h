@@ -1,5 +1,5 @@
-// Masses of a histogram's bins in two 32-bit sums.  Plain C++: the kernels and
-// the host's test of the sums' range include it.
+// Masses of a histogram's bins in two 32-bit sums, and where a running total
+// passes a target.  Plain C++: the kernels and the host's tests include it.
 #pragma once
 #include <stdint.h>
 
@@ -25,6 +25,12 @@ struct MassParts {
 EPIC_INLINE MassParts mass_parts(uint32_t mass) {
   const uint32_t high = (mass + (1u << 14)) >> 15;
   return {high, mass - (high << 15)};
+}
+
+// Whether the running total passes t at an element of mass q with `before` ahead of it; the last one takes what lies past
+// the end, so of a list's elements exactly one answers, whatever t is.
+EPIC_INLINE bool passes(uint64_t before, uint64_t q, uint64_t t, bool last) {
+  return before <= t && (t - before < q || last);
 }
 
 }  // namespace epic

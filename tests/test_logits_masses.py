@@ -1,5 +1,6 @@
 """The two-part sums of the histograms' bins, on the host: exact up to the longest
-slice for any mass, whatever its low bits."""
+slice for any mass, whatever its low bits; and the search of a target in a
+list's running total, which always ends at one of its elements."""
 import os
 import subprocess
 
@@ -42,6 +43,47 @@ int main() {
 def test_sums_of_the_longest_slice_are_exact(tmp_path):
     source, program = tmp_path / 'sums.cpp', tmp_path / 'sums'
     source.write_text(PROGRAM)
+    subprocess.check_call(['g++', '-std=c++17', '-O2', '-I', CSRC, str(source), '-o', str(program)])
+    seen, wrong = map(int, subprocess.check_output([str(program)]).split())
+    assert seen > 5000 and wrong == 0
+
+
+SEARCH = r'''
+#include <stdio.h>
+#include <initializer_list>
+#include "mass_parts.h"
+using namespace epic;
+int main() {
+  long long wrong = 0, seen = 0;
+  uint32_t x = 7;
+  for (int n = 1; n < 40; ++n)
+    for (int round = 0; round < 20; ++round) {
+      uint64_t q[40], total = 0;
+      for (int i = 0; i < n; ++i) {
+        x = x * 1664525u + 1013904223u;
+        total += q[i] = round == 0 ? 0 : x >> 28 & 7;  // some of them nothing
+      }
+      for (uint64_t t : {uint64_t(0), total / 2, total - 1, total, total + 1, total + 1000000, ~uint64_t(0)}) {
+        int first = n - 1, hits = 0, at = -1;
+        uint64_t upto = 0;
+        for (int i = n; i--;) upto += q[i];
+        for (int i = n; i--; upto -= q[i])
+          if (upto > t) first = i;
+        upto = 0;
+        for (int i = 0; i < n; upto += q[i++])
+          if (passes(upto, q[i], t, i == n - 1)) ++hits, at = i;
+        ++seen;
+        wrong += hits != 1 || at != first;
+      }
+    }
+  printf("%lld %lld\n", seen, wrong);
+}
+'''
+
+
+def test_a_target_past_the_end_is_the_last_element(tmp_path):
+    source, program = tmp_path / 'search.cpp', tmp_path / 'search'
+    source.write_text(SEARCH)
     subprocess.check_call(['g++', '-std=c++17', '-O2', '-I', CSRC, str(source), '-o', str(program)])
     seen, wrong = map(int, subprocess.check_output([str(program)]).split())
     assert seen > 5000 and wrong == 0
