@@ -334,7 +334,7 @@ enum { EPIC_F32 = 0, EPIC_F16 = 1, EPIC_BF16 = 2 }; /* the element type of logit
  * float32, as epic_validate_batch and epic_pick_candidates take them.  A token
  * whose logit is -inf or NaN is no candidate; where fewer than K are left the
  * rest are -1 with confidence 0 (no validity bit of theirs is ever 1).
- * T = 0 gives confidences 1, 0, 0, ..., T = +inf the same to all tokens; a T
+ * T = 0 or -0 gives confidences 1, 0, 0, ..., T = +inf the same to all tokens; a T
  * below 0 or NaN gives no candidates.
  * +inf logits share all probability.  Errors: EPIC_ERR_INVALID_ARG (NULL
  * pointers, sizes < 0, a bad dtype, d_logits not aligned to its elements, k > n
@@ -359,7 +359,7 @@ epic_status epic_propose_topk(const void* d_logits, int32_t dtype, int32_t B, in
  * tokens less likely than 2^-31 of the likeliest are not drawn.)
  * Outputs d_tok [B][k][S] int32 and d_prob [B][k][S] float32, the token's
  * probability among the kept ones: candidates and confidences with K = S.
- * T = 0 takes the likeliest token, at T = +inf all weigh 1.  A row of no tokens (all -inf or NaN), a T
+ * T = 0 or -0 takes the likeliest token, at T = +inf all weigh 1.  A row of no tokens (all -inf or NaN), a T
  * below 0 or NaN, a NaN rule, or a number outside [0, 1] gives -1 and 0.
  * Errors as epic_propose_topk, without a limit on S.
  */

@@ -98,6 +98,16 @@ struct PickShared {
   int count;
 };
 
+// The temperature of a row; -0 becomes 0.
+__device__ __forceinline__ float row_temperature(const PickArgs& a, int r) {
+  return a.temperature ? a.temperature[r / a.rows.k] + 0.0f : 1.0f;
+}
+
+// log2(e) / T.  A row of a temperature that is none is read like others, and answered with nothing.
+__device__ __forceinline__ float exponent_scale(float t) {
+  return t >= 0.0f ? fminf(__fdiv_rn(kLog2e, t), CUDART_MAX_NORMAL_F) : 1.0f;
+}
+
 // The kernels' shared memory, by name: through a reference kept in an object its loads would be generic ones.
 __device__ __forceinline__ PickShared& shared() {
   __shared__ PickShared sh;
@@ -1090,20 +1100,13 @@ struct Propose {
   typedef PickArgs Args;
   const Args& a;
   __device__ explicit Propose(const Args& args) : a(args) {}
-  __device__ __forceinline__ float temperature(int r) const {
-    return a.temperature ? a.temperature[r / a.rows.k] : 1.0f;
-  }
-  // A row of a temperature that is none is read like others, and answered with nothing.
-  __device__ __forceinline__ static float scale(float t) {
-    return t >= 0.0f ? fminf(__fdiv_rn(kLog2e, t), CUDART_MAX_NORMAL_F) : 1.0f;
-  }
 
   __device__ __forceinline__ void run(Row<T>& row, int r) const {
     constexpr int E = ElemOf<T>::E;
     const int lane = (int)threadIdx.x % 32, warps = (int)blockDim.x / 32, warp = warp_index();
-    const float temp = temperature(r);
+    const float temp = row_temperature(a, r);
     Weigher weigh;
-    weigh.c = scale(temp);
+    weigh.c = exponent_scale(temp);
     // one pass: the lane's maximum so far and the sum of its weights relative to it
     LaneTop top;
     float2 sums = make_float2(0.0f, 0.0f);
@@ -1185,7 +1188,7 @@ struct Sample {
   __device__ __forceinline__ void run(Row<T>& row, int r) const {
     const int lane = (int)threadIdx.x % 32;
     const int b = r / a.rows.k;
-    float temp = a.temperature ? a.temperature[b] : 1.0f;
+    const float temp = row_temperature(a, r);
     float top_p = a.top_p ? a.top_p[b] : 1.0f;
     const float min_p = a.min_p ? a.min_p[b] : 0.0f;
     int top_k = a.top_k ? a.top_k[b] : 0;
@@ -1204,7 +1207,7 @@ struct Sample {
     float floor;
     const LaneTop top = row.lane_top();
     weigh.m = row.top_of(top.first, by_list ? top_k : 0, &floor);
-    weigh.c = good ? fminf(__fdiv_rn(kLog2e, temp), CUDART_MAX_NORMAL_F) : 1.0f;
+    weigh.c = exponent_scale(temp);
     if (by_list) {
       row.collect(floor, top);
       row.group.sync();
