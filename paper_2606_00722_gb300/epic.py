@@ -370,14 +370,16 @@ def extract_witness(g: Grammar, t: LexTable, x, terms, lengths, stream=None):
 _DTYPES = {}  # torch dtype of logits -> the C-ABI's code; filled on the first call
 _T = None     # torch, and what the calls need of it
 _raw_stream = None
+_current_device = None
 
 
 def _logits_init():
-    global _T, _raw_stream
+    global _T, _raw_stream, _current_device
     import torch
     _DTYPES.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2})
     _raw_stream = getattr(torch._C, '_cuda_getCurrentRawStream', None) or (
         lambda device: torch.cuda.current_stream(device).cuda_stream)
+    _current_device = getattr(torch._C, '_cuda_getDevice', None) or torch.cuda.current_device
     _T = (torch.float32, torch.int32, torch.uint8)
 
 
@@ -399,10 +401,13 @@ def _rows(logits):
 
 
 def _device(logits):
-    """The index of the device of a CUDA tensor."""
+    """The index of the device of a CUDA tensor, which has to be the current one: kernels start there, and the default
+    stream of another device is the current device's to the runtime."""
     device = logits.get_device()
     if device < 0:
         raise ValueError('expected a CUDA tensor')
+    if device != _current_device():
+        raise ValueError('tensors on CUDA device %d, but the current device is %d' % (device, _current_device()))
     return device
 
 
