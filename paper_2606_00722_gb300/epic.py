@@ -512,20 +512,21 @@ def distill_step(logits, ids, vals, loss, grad, tau=1.0, weight=None, valid=None
         'epic_distill_step')
 
 
-def distill_loss(logits, ids, vals, tau=1.0, weight=None, valid=None):
-    """The distillation loss [B][n] of student logits [B][n][V] as a torch
-    operation with a gradient for the logits (forward: epic_distill_forward,
-    backward: epic_distill_backward); the other arguments are constants.
-    Streams are torch's own."""
+_Loss = None  # distill_loss's torch operation; made on the first call
+
+
+def _loss_init():
+    global _Loss
     import torch
 
-    class Loss(torch.autograd.Function):
+    class DistillLoss(torch.autograd.Function):
         @staticmethod
-        def forward(ctx, z, ids, vals, weight, valid):
+        def forward(ctx, z, ids, vals, tau, weight, valid):
             loss = torch.empty(z.shape[:2], dtype=torch.float32, device=z.device)
             lse = torch.empty_like(loss)
             distill_forward(z, ids, vals, loss, lse, tau, weight, valid)
             ctx.save_for_backward(z, lse, ids, vals, weight, valid)
+            ctx.tau = tau
             return loss
 
         @staticmethod
@@ -533,10 +534,20 @@ def distill_loss(logits, ids, vals, tau=1.0, weight=None, valid=None):
         def backward(ctx, grad_loss):
             z, lse, ids, vals, weight, valid = ctx.saved_tensors
             grad = torch.empty(z.shape, dtype=z.dtype, device=z.device)
-            distill_backward(z, ids, vals, lse, grad_loss.to(torch.float32).contiguous(), grad, tau, weight, valid)
-            return grad, None, None, None, None
+            distill_backward(z, ids, vals, lse, grad_loss.to(torch.float32).contiguous(), grad, ctx.tau, weight, valid)
+            return grad, None, None, None, None, None
 
-    return Loss.apply(logits, ids, vals, weight, valid)
+    _Loss = DistillLoss
+
+
+def distill_loss(logits, ids, vals, tau=1.0, weight=None, valid=None):
+    """The distillation loss [B][n] of student logits [B][n][V] as a torch
+    operation with a gradient for the logits (forward: epic_distill_forward,
+    backward: epic_distill_backward); the other arguments are constants.
+    Streams are torch's own."""
+    if _Loss is None:
+        _loss_init()
+    return _Loss.apply(logits, ids, vals, tau, weight, valid)
 
 
 def decode_step_from_logits(g: Grammar, t: LexTable, x, pos, logits, n_target, bufs, temperature=None, u=None,

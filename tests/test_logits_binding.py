@@ -77,3 +77,35 @@ def test_tensors_of_two_devices_are_refused(device):
     for call in calls(1, others=0):
         with pytest.raises(ValueError):
             call()
+
+
+def fake_loss(monkeypatch):
+    """distill_loss on CPU tensors, with calls that note what they were given."""
+    import torch
+    seen = []
+
+    def forward(z, ids, vals, loss, lse, tau, weight, valid):
+        loss.fill_(tau)
+        seen.append(('forward', tau, weight, valid))
+
+    def backward(z, ids, vals, lse, grad_loss, grad, tau, weight, valid):
+        grad.copy_(grad_loss[..., None].expand_as(grad) * tau)
+        seen.append(('backward', tau, weight, valid))
+    monkeypatch.setattr(binding, 'distill_forward', forward)
+    monkeypatch.setattr(binding, 'distill_backward', backward)
+    z = torch.zeros((2, 3, 5), requires_grad=True)
+    return z, torch.zeros((2, 3, 4), dtype=torch.int32), torch.zeros((2, 3, 4)), torch.ones((2, 3)), seen
+
+
+def test_the_loss_is_one_operation(monkeypatch):
+    """Every call is of the same torch operation, each with its own temperature and constants."""
+    z, ids, vals, weight, seen = fake_loss(monkeypatch)
+    one, two = epic.distill_loss(z, ids, vals, 0.5, weight), epic.distill_loss(z, ids, vals, 3.0)
+    assert type(one.grad_fn) is type(two.grad_fn)
+    two.sum().backward()
+    assert (z.grad == 3.0).all()
+    z.grad = None
+    one.sum().backward()
+    assert (z.grad == 0.5).all()
+    assert [(form, tau, w is not None) for form, tau, w, _ in seen] == [
+        ('forward', 0.5, True), ('forward', 3.0, False), ('backward', 3.0, False), ('backward', 0.5, True)]
