@@ -543,10 +543,14 @@ def _loss_init():
 def distill_loss(logits, ids, vals, tau=1.0, weight=None, valid=None):
     """The distillation loss [B][n] of student logits [B][n][V] as a torch
     operation with a gradient for the logits (forward: epic_distill_forward,
-    backward: epic_distill_backward); the other arguments are constants.
-    Streams are torch's own."""
+    backward: epic_distill_backward); the other arguments are constants, and
+    refused where they ask for a gradient.  Streams are torch's own."""
+    import torch
     if _Loss is None:
         _loss_init()
+    for name, t in (('vals', vals), ('weight', weight)):
+        if t is not None and t.requires_grad and torch.is_grad_enabled():
+            raise ValueError('%s: the loss has no gradient for it; detach it' % name)
     return _Loss.apply(logits, ids, vals, tau, weight, valid)
 
 

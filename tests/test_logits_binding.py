@@ -109,3 +109,15 @@ def test_the_loss_is_one_operation(monkeypatch):
     assert (z.grad == 0.5).all()
     assert [(form, tau, w is not None) for form, tau, w, _ in seen] == [
         ('forward', 0.5, True), ('forward', 3.0, False), ('backward', 3.0, False), ('backward', 0.5, True)]
+
+
+def test_constants_of_the_loss_that_ask_for_a_gradient_are_refused(monkeypatch):
+    import torch
+    z, ids, vals, weight, seen = fake_loss(monkeypatch)
+    for bad in (dict(vals=vals.clone().requires_grad_()), dict(vals=vals, weight=weight.clone().requires_grad_())):
+        with pytest.raises(ValueError, match='detach'):
+            epic.distill_loss(z, ids, **bad)
+        with torch.no_grad():
+            epic.distill_loss(z, ids, **bad)
+    epic.distill_loss(z, ids, vals.clone().requires_grad_().detach(), weight=weight).sum().backward()
+    assert (z.grad == 1.0).all() and len(seen) == 4
