@@ -325,8 +325,8 @@ __global__ void __launch_bounds__(kDistillThreads, kDistillPerSm) k_distill(Dist
       for (int k = lane; k < a.K; k += 32) {
         const float p = t.p[k];
         if (t.id[k] < 0 || p == 0.0f) continue;
-        const float z = t.z[k];
-        const float lq = z == -CUDART_INF_F ? z : (z - m) / a.tau - log_sum;
+        // -inf where the token is, NaN where the row has NaN or +inf; a row of -inf alone has no sum
+        const float lq = m == -CUDART_INF_F ? m : (t.z[k] - m) / a.tau - log_sum;
         loss += p * (t.lp[k] - lq);
       }
     loss = warp_add(loss);
