@@ -5,6 +5,11 @@
 //   loss   = w tau^2 sum_k p_k (log p_k - lq[t_k])
 //   dz_j   = w tau (softmax(z / tau)_j - sum_{k: t_k = j} p_k)
 // A row with no entry that counts, or with w = 0, has loss and gradient 0.
+// With a' and z' relative to their largest (of the entries, of the row), and
+// log A, log Z the logarithms of the sums of exponentials relative to these,
+//   loss = w tau sum_k p_k (a'_k - z'[t_k] + tau (log Z - log A)):
+// nothing is divided by tau but exponents, so values at the type's lowest and any
+// tau stay in range.
 // Sums are held in 32 bits; the gradient is rounded once, to the logits' type.
 //
 // Each row is read from memory once: for the loss in one pass with a running
@@ -45,7 +50,7 @@ struct DistillArgs {
 
 struct Targets {
   float p[kMaxTargets];
-  float lp[kMaxTargets];
+  float a[kMaxTargets];  // values relative to the largest
   float z[kMaxTargets];  // the student's logits of the tokens
   int id[kMaxTargets];  // -1: does not count
   uint4 ends[2], row_ends[2];
@@ -56,6 +61,9 @@ struct Targets {
 
 // larger of two, NaN if either is
 __device__ __forceinline__ float max_nan(float a, float b) { return ChunkMax<float, true>::max1(a, b); }
+
+// log2(e) / tau
+__device__ __forceinline__ float exponent_scale(float tau) { return fminf(kLog2e / tau, CUDART_MAX_NORMAL_F); }
 
 __device__ __forceinline__ float below_inf(float x) { return x == CUDART_INF_F ? CUDART_MAX_NORMAL_F : x; }
 
@@ -68,34 +76,35 @@ __device__ __forceinline__ float warp_max_nan(float x) {
   return x;
 }
 
-// One warp's work: the row's entries in shared memory, p and log p of them, and whether any counts.  load() asks for what
-// is in memory and is called before the pass over the row, finish() after it; entries past the 32nd wait for finish().
+// One warp's work: the row's entries in shared memory, p of them, and whether any counts.  load() asks for what is in
+// memory and is called before the pass over the row, finish() after it; entries past the 32nd wait for finish(), which
+// returns the logarithm of the sum of exponentials.
 template <typename T>
 struct Teacher {
   int id;
   float value, z;
-  // entry k: its token (-1: does not count), its scaled value, and the student's logit of the token
+  // entry k: its token (-1: does not count), its value, and the student's logit of the token
   __device__ __forceinline__ void entry(const DistillArgs& a, int r, const T* logits, int k) {
     const long long o = (long long)r * a.K + k;
     const int token = a.ids[o];
     const float v = a.vals[o];
     const bool counts = token >= 0 && token < a.rows.V && (!a.valid || a.valid[o] == 1) && v != -CUDART_INF_F;
     id = counts ? token : -1;
-    value = v / a.tau;
+    value = v;
     z = counts ? to_float<T>(logits[token]) : 0.0f;
   }
   __device__ __forceinline__ void load(const DistillArgs& a, int r, const T* logits) {
     const int lane = threadIdx.x % 32;
     if (lane < a.K) entry(a, r, logits, lane);
   }
-  __device__ __forceinline__ void finish(const DistillArgs& a, int r, const T* logits, Targets& t) {
+  __device__ __forceinline__ float finish(const DistillArgs& a, int r, const T* logits, Targets& t) {
     const int lane = threadIdx.x % 32;
     float m = -CUDART_INF_F;
 #pragma unroll 1
     for (int k = lane; k < a.K; k += 32) {
       if (k >= 32) entry(a, r, logits, k);
       t.id[k] = id;
-      t.lp[k] = value;
+      t.a[k] = value;
       t.z[k] = z;
       if (id >= 0) m = max_nan(m, value);
     }
@@ -104,17 +113,14 @@ struct Teacher {
     float sum = 0.0f;
 #pragma unroll 1
     for (int k = lane; k < a.K; k += 32) {
-      t.lp[k] -= m;
-      t.p[k] = t.id[k] >= 0 ? expf(t.lp[k]) : 0.0f;
+      t.a[k] -= m;
+      t.p[k] = t.id[k] >= 0 ? expf(t.a[k] / a.tau) : 0.0f;
       sum += t.p[k];
     }
     sum = warp_add(sum);
-    const float log_sum = logf(sum);
 #pragma unroll 1
-    for (int k = lane; k < a.K; k += 32) {
-      t.p[k] /= sum;
-      t.lp[k] -= log_sum;
-    }
+    for (int k = lane; k < a.K; k += 32) t.p[k] /= sum;
+    return logf(sum);
   }
 };
 
@@ -298,10 +304,11 @@ __global__ void __launch_bounds__(kDistillThreads, kDistillPerSm) k_distill(Dist
   }
   Teacher<T> teacher;
   if (warp == warps - 1) teacher.load(a, r, logits);
-  const float c2 = kLog2e / a.tau;
+  const float c2 = exponent_scale(a.tau);
   float sum;
   const float top = lane_sums(s, c2, &sum);
-  if (warp == warps - 1) teacher.finish(a, r, logits, t);
+  float teacher_log = 0.0f;
+  if (warp == warps - 1) teacher_log = teacher.finish(a, r, logits, t);
   float m = cta_sums(t, top, c2, &sum);
   if (ctas > 1) {
     if (threadIdx.x == 0) {
@@ -325,13 +332,12 @@ __global__ void __launch_bounds__(kDistillThreads, kDistillPerSm) k_distill(Dist
       for (int k = lane; k < a.K; k += 32) {
         const float p = t.p[k];
         if (t.id[k] < 0 || p == 0.0f) continue;
-        // -inf where the token is, NaN where the row has NaN or +inf; a row of -inf alone has no sum
-        const float lq = m == -CUDART_INF_F ? m : (t.z[k] - m) / a.tau - log_sum;
-        loss += p * (t.lp[k] - lq);
+        // +inf where the token is at -inf, NaN where the row has NaN or +inf; a row of -inf alone has no sum
+        loss += p * (m == -CUDART_INF_F ? CUDART_INF_F : t.a[k] - (t.z[k] - m) + a.tau * (log_sum - teacher_log));
       }
     loss = warp_add(loss);
     if (lane == 0) {
-      a.loss[r] = any ? weight * a.tau * a.tau * loss : 0.0f;
+      a.loss[r] = any ? weight * (a.tau * loss) : 0.0f;
       // +inf says that nothing flows back
       if (a.lse) a.lse[r] = !any ? CUDART_INF_F : m == -CUDART_INF_F ? m : below_inf(m / a.tau + log_sum);
     }
@@ -382,7 +388,7 @@ __global__ void __launch_bounds__(kDistillThreads, kDistillPerSm) k_distill_back
     teacher.load(a, r, row_address<T>(a.rows, r));
     teacher.finish(a, r, row_address<T>(a.rows, r), t);
   }
-  const float c2 = kLog2e / a.tau;
+  const float c2 = exponent_scale(a.tau);
   float at = lse * a.tau, scale = coef;
   if (fabsf(lse) > kLseFine) {
     const float2 sums = row_sums<T>(a, r, t, c2);

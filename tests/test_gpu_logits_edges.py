@@ -65,3 +65,66 @@ def test_nan_shows_where_the_wanted_token_is_ruled_out(cuda, n, V):
         assert torch.isnan(loss[0, 1:3]).all(), form
         assert torch.isnan(grad[0, 1:3, 200]).all() and torch.isfinite(grad[0, 0]).all(), form
         assert torch.isfinite(grad[0, 3]).all() and (loss[0, 4:] == math.inf).all(), form
+
+
+def distill_rows64(z, ids, vals, tau, weight):
+    """The loss by its definition in 64 bits, without a quotient by tau until differences are taken, and the gradient."""
+    z, v, ids = z.double().cpu().numpy(), vals.double().cpu().numpy(), ids.cpu().numpy()
+    w = weight.double().cpu().numpy()
+    loss, grad = np.zeros(z.shape[:2]), np.zeros(z.shape)
+    for b, i in np.ndindex(*z.shape[:2]):
+        da, dz = v[b, i] - v[b, i].max(), z[b, i] - z[b, i].max()
+        with np.errstate(under='ignore'):
+            p, q = np.exp(da / tau), np.exp(dz / tau)
+        log_a, log_z = math.log(p.sum()), math.log(q.sum())
+        p, q = p / p.sum(), q / q.sum()
+        for k, t in enumerate(ids[b, i]):
+            if p[k] > 0:
+                loss[b, i] += w[b, i] * tau * p[k] * (da[k] - dz[t] + tau * (log_z - log_a))
+            q[t] -= p[k]
+        grad[b, i] = w[b, i] * tau * q
+    return loss, grad
+
+
+@pytest.mark.parametrize('tau', [0.1, 0.5, 1.0, 1e-3, 1e-30, 1e-39])
+@pytest.mark.parametrize('dtype', ['float32', 'float16', 'bfloat16'])
+@pytest.mark.parametrize('n,V', [(6, 300), (6, 70001)])
+def test_quotients_by_the_temperature_stay_in_range(cuda, n, V, dtype, tau):
+    """Values and logits at the lowest and largest of 32 bits, divided by a small temperature, would pass 32 bits: entries
+    that all are at the lowest value are alike, and a wanted token at the student's lowest value costs what it costs.
+    Tolerances: 3.2e-5 w tau^2 of a loss and 6e-5 w tau of a gradient element, as derived in the distillation tests, 1e-6 of
+    a loss, half a unit of the gradient's type, and for results below 2^-126 four units of 2^-149."""
+    import torch
+    low, most = torch.finfo(torch.float32).min, torch.finfo(torch.float32).max
+    dt = getattr(torch, dtype)
+    z = torch.randn((1, n, V), generator=torch.Generator().manual_seed(1)).to(dt).cuda()
+    ids = torch.tensor([3, 9, 250], dtype=torch.int32, device='cuda').expand(1, n, 3).contiguous()
+    vals = torch.tensor([0.5, -0.3, 0.1], device='cuda').expand(1, n, 3).contiguous()
+    vals[0, 0] = low
+    vals[0, 1, 1:] = low
+    vals[0, 2, 0] = most
+    z[0, 3, 3] = torch.finfo(dt).min
+    z[0, 4] = torch.finfo(dt).min
+    z[0, 4, 9] = 0.0
+    weight = torch.tensor([[0.4, 0.3, 0.2, 0.1, 0.1, 1.0]], device='cuda')
+    tau32 = float(np.float32(tau))
+    want_loss, want_grad = distill_rows64(z, ids, vals, tau32, weight)
+    assert np.isfinite(want_loss).all() and (np.abs(want_loss) < 3e38).all()
+    w = weight.double().cpu().numpy()
+    rel, tiny = {'float32': (2.0 ** -23, 2.0 ** -147), 'float16': (2.0 ** -11, 2.0 ** -25),
+                 'bfloat16': (2.0 ** -8, 2.0 ** -132)}[dtype]  # bf16's smallest number is 2^-133
+    for form, loss, grad in both_forms(z, ids, vals, tau, weight):
+        loss, grad = loss.double().cpu().numpy(), grad.double().cpu().numpy()
+        assert (np.abs(loss - want_loss) <= 3.2e-5 * w * tau32 ** 2 + 1e-6 * np.abs(want_loss) + 2.0 ** -147).all(), form
+        assert (np.abs(grad - want_grad) <= np.abs(want_grad) * rel + w[..., None] * tau32 * 6e-5 + tiny).all(), form
+
+
+@pytest.mark.parametrize('tau', [1e20, 1e30, 3e38])
+def test_a_row_that_agrees_costs_nothing_at_any_temperature(cuda, tau):
+    """One token, wanted: loss and gradient 0, also where tau^2 passes 32 bits."""
+    import torch
+    z = torch.tensor([[[2.5]], [[-3.0]]], device='cuda')
+    ids = torch.zeros((2, 1, 1), dtype=torch.int32, device='cuda')
+    vals = torch.tensor([[[0.0]], [[7.0]]], device='cuda')
+    for form, loss, grad in both_forms(z, ids, vals, tau, torch.ones((2, 1), device='cuda')):
+        assert (loss == 0).all() and (grad == 0).all(), form
