@@ -127,6 +127,12 @@ struct Weigher {
   }
 };
 
+// For a row whose largest logit is `most`.  At T = inf every exponent is 0, whatever is taken off: not the largest, from
+// which a difference may pass 32 bits.
+__device__ __forceinline__ Weigher weigher(float most, float c) {
+  return Weigher{c == 0.0f && fabsf(most) < CUDART_INF_F ? 0.0f : most, c};
+}
+
 __device__ __forceinline__ uint32_t grid_mass(float w) { return __float2uint_rn(w * kGrid); }
 
 // The masses of two weights in parts, low ones within 2^14 of 0, high and low as bits over kHighBits and kOnesBits.
@@ -1105,23 +1111,22 @@ struct Propose {
     constexpr int E = ElemOf<T>::E;
     const int lane = (int)threadIdx.x % 32, warps = (int)blockDim.x / 32, warp = warp_index();
     const float temp = row_temperature(a, r);
-    Weigher weigh;
-    weigh.c = exponent_scale(temp);
+    const float c = exponent_scale(temp);
     // one pass: the lane's maximum so far and the sum of its weights relative to it
     LaneTop top;
     float2 sums = make_float2(0.0f, 0.0f);
-    row.s.sweep([&](const uint4 (&v)[4], int c) {
+    row.s.sweep([&](const uint4 (&v)[4], int at) {
       ChunkMax<T, false> batch;
       batch.add(v);
       const float x = batch.value();
       if (x > top.first) {
-        const float by = exp2_32((top.first - x) * weigh.c);
+        const float by = exp2_32((top.first - x) * c);
         sums.x *= by;
         sums.y *= by;
       }
-      top.add(x, c);
+      top.add(x, at);
       if (top.first == -CUDART_INF_F) return;
-      const Weigher relative{top.first, weigh.c};
+      const Weigher relative{top.first, c};
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         float z[E];
@@ -1134,10 +1139,11 @@ struct Propose {
       }
     });
     float floor;
-    weigh.m = row.top_of(top.first, a.K, &floor);
+    const float most = row.top_of(top.first, a.K, &floor);
+    const Weigher weigh = weigher(most, c);
     row.collect(floor, top);
     float sum = sums.x + sums.y;
-    if (__any_sync(~0u, sum != sum) || weigh.m == CUDART_INF_F) {  // NaN or +inf among the warp's elements or the row's
+    if (__any_sync(~0u, sum != sum) || most == CUDART_INF_F) {  // NaN or +inf among the warp's elements or the row's
       sum = 0.0f;
       row.each([&](float z, int) {
         const float w = weigh(z);
@@ -1149,7 +1155,7 @@ struct Propose {
     for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
     if (lane == 0) *row.group.at(&shared().sums[row.group.rank * warps + warp], 0) = sum;
     row.group.sync();
-    row.settle(a.K, weigh.m);
+    row.settle(a.K, most);
     if (row.group.rank != 0) return;
     sum = 0.0f;
     for (int i = 0; i < (int)row.group.n * warps; ++i) sum += shared().sums[i];
@@ -1203,15 +1209,14 @@ struct Sample {
     const float first_u = warp < a.S ? u[warp] : 0.0f;  // on its way during the passes
     int32_t* tok = a.tok + (long long)r * a.S;
     float* prob = a.prob + (long long)r * a.S;
-    Weigher weigh;
     float floor;
     const LaneTop top = row.lane_top();
-    weigh.m = row.top_of(top.first, by_list ? top_k : 0, &floor);
-    weigh.c = exponent_scale(temp);
+    const float most = row.top_of(top.first, by_list ? top_k : 0, &floor);
+    const Weigher weigh = weigher(most, exponent_scale(temp));
     if (by_list) {
       row.collect(floor, top);
       row.group.sync();
-      row.settle(top_k, weigh.m);
+      row.settle(top_k, most);
       if (row.group.rank != 0) return;
       row.draw_from_list(weigh, good ? top_k : 0, p24, min_p, u, a.S, tok, prob);
       if (row.group.n > 1) row.group.sync();  // the others have looked at the count

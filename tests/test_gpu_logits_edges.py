@@ -128,3 +128,36 @@ def test_a_row_that_agrees_costs_nothing_at_any_temperature(cuda, tau):
     vals = torch.tensor([[[0.0]], [[7.0]]], device='cuda')
     for form, loss, grad in both_forms(z, ids, vals, tau, torch.ones((2, 1), device='cuda')):
         assert (loss == 0).all() and (grad == 0).all(), form
+
+
+@pytest.mark.parametrize('V,dtype', [(9, 'float32'), (3000, 'bfloat16'), (3000, 'float32'), (70001, 'float32')])
+@pytest.mark.parametrize('top_k,top_p', [(0, 1.0), (100, 1.0), (1500, 0.7), (0, 0.4)])
+def test_infinite_temperature_of_logits_whose_differences_pass_32_bits(cuda, V, dtype, top_k, top_p):
+    """All tokens weigh 1 at T = +inf, also where the largest logit less theirs is no 32-bit number.  The reference takes
+    the logits times 2^-40, which changes neither their order nor, at that temperature, their weights."""
+    import torch
+    import paper_2606_00722_gb300 as epic
+    from test_gpu_logits_pick import sample_whole
+    B, S, K = 3, 9, 8
+    z = (torch.randn((B, 1, V), generator=torch.Generator().manual_seed(V)) * 1.1e38).clamp_(-3.3e38, 3.3e38)
+    z = z.to(getattr(torch, dtype)).cuda()
+    z[:, 0, 0], z[:, 0, 1] = torch.finfo(z.dtype).min, torch.finfo(z.dtype).max
+    z[1, 0, 2::3] = -math.inf
+    z[2, 0, 3] = math.nan
+    u = torch.rand((B, 1, S), generator=torch.Generator().manual_seed(1)).cuda()
+    T = torch.full((B,), math.inf, device='cuda')
+    rules = [torch.full((B,), top_k, dtype=torch.int32, device='cuda'), torch.full((B,), top_p, device='cuda'),
+             torch.zeros((B,), device='cuda')]
+    tok = torch.full((B, 1, S), -7, dtype=torch.int32, device='cuda')
+    prob = torch.full((B, 1, S), -7.0, device='cuda')
+    epic.sample_tokens(z, u, tok, prob, temperature=T, top_k=rules[0], top_p=rules[1], min_p=rules[2])
+    want_tok, want_prob, _ = sample_whole(z.float() * 2.0 ** -40, T, *rules, u)
+    assert torch.equal(tok, want_tok)
+    np.testing.assert_allclose(prob.cpu().numpy(), want_prob.cpu().numpy(), rtol=2.0 ** -21, atol=0)
+    cand = torch.full((B, 1, K), -7, dtype=torch.int32, device='cuda')
+    conf = torch.full((B, 1, K), -7.0, device='cuda')
+    epic.propose_topk(z, cand, conf, temperature=T)
+    there = (z > -math.inf).sum(-1, keepdim=True)
+    want = torch.where(torch.arange(K, device='cuda') < there, 1.0 / there.double(), 0.0)
+    assert ((conf.double() - want).abs() <= 2.4e-5 * want).all()
+    assert ((cand >= 0) == (want > 0)).all()
