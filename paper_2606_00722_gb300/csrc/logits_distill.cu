@@ -333,11 +333,13 @@ __global__ void __launch_bounds__(kDistillThreads, kDistillPerSm) k_distill(Dist
         const float p = t.p[k];
         if (t.id[k] < 0 || p == 0.0f) continue;
         // +inf where the token is at -inf, NaN where the row has NaN or +inf; a row of -inf alone has no sum
-        loss += p * (m == -CUDART_INF_F ? CUDART_INF_F : t.a[k] - (t.z[k] - m) + a.tau * (log_sum - teacher_log));
+        // Quarters of it: p adds up to 1 but for roundings, and so a sum of costs near the largest number stays in range.
+        loss += 0.25f * p * (m == -CUDART_INF_F ? CUDART_INF_F : t.a[k] - (t.z[k] - m) + a.tau * (log_sum - teacher_log));
       }
     loss = warp_add(loss);
     if (lane == 0) {
-      a.loss[r] = any ? weight * (a.tau * loss) : 0.0f;
+      // the smaller factor first
+      a.loss[r] = any ? 4.0f * (a.tau < 1.0f ? weight * (a.tau * loss) : weight * a.tau * loss) : 0.0f;
       // +inf says that nothing flows back
       if (a.lse) a.lse[r] = !any ? CUDART_INF_F : m == -CUDART_INF_F ? m : below_inf(m / a.tau + log_sum);
     }

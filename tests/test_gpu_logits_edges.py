@@ -119,6 +119,25 @@ def test_quotients_by_the_temperature_stay_in_range(cuda, n, V, dtype, tau):
         assert (np.abs(grad - want_grad) <= np.abs(want_grad) * rel + w[..., None] * tau32 * 6e-5 + tiny).all(), form
 
 
+@pytest.mark.parametrize('tau,weight', [(0.5, 1.0), (0.999, 0.9), (1.0, 0.9), (10.0, 0.09), (10.0, 0.05), (1e-3, 50.0)])
+@pytest.mark.parametrize('K', [1, 3, 40, 1000])
+def test_costs_near_the_largest_number_do_not_overflow_on_the_way(cuda, K, tau, weight):
+    """All wanted tokens at the lowest value of 32 bits: w tau 3.4e38, where that is a number.  Tolerance: 2.2e-6 of it for
+    the probabilities' sum (2^-24 for each of 32 additions in a lane and 5 between lanes) and 1e-6 for what else rounds."""
+    import torch
+    n, V = 3, 5000
+    z = torch.randn((1, n, V), generator=torch.Generator().manual_seed(1)).cuda()
+    ids = torch.randperm(V, generator=torch.Generator().manual_seed(2))[:K].to(torch.int32).expand(1, n, K).contiguous().cuda()
+    vals = torch.randn((1, n, K), generator=torch.Generator().manual_seed(3)).cuda()
+    z.scatter_(2, ids.long(), torch.finfo(torch.float32).min)
+    w = torch.full((1, n), weight, device='cuda')
+    want = weight * tau * torch.finfo(torch.float32).max
+    assert want < torch.finfo(torch.float32).max
+    for form, loss, grad in both_forms(z, ids, vals, tau, w):
+        assert ((loss.double() - want).abs() <= 3.2e-6 * want).all(), form
+        assert torch.isfinite(grad).all(), form
+
+
 @pytest.mark.parametrize('tau', [1e20, 1e30, 3e38])
 def test_a_row_that_agrees_costs_nothing_at_any_temperature(cuda, tau):
     """One token, wanted: loss and gradient 0, also where tau^2 passes 32 bits."""
