@@ -349,8 +349,9 @@ epic_status epic_propose_topk(const void* d_logits, int32_t dtype, int32_t B, in
  * given number d_u [B][k][S] of [0, 1].  Each sequence has its own rules, [B]
  * or NULL (off): temperature T (1), top-k (<= 0: off), top-p (>= 1: off), min-p
  * (<= 0: off).  With c = log2(e) / T and m the row's largest logit, a token
- * weighs w = 2^((z - m) c), each operation rounded to 32 bits, in whole units
- * q = rint(2^30 w).  In the order of epic_propose_topk, kept are the first top-k
+ * weighs w = 2^((z - m) c), difference, product and power each in 32 bits (the
+ * power is the GPU's ex2.approx.ftz, as in epic_propose_topk: within 2 units in the
+ * last place, 0 below 2^-126), in whole units q = rint(2^30 w).  In the order of epic_propose_topk, kept are the first top-k
  * tokens; of these the ones before which less than floor(rint(2^24 top-p) Q / 2^24)
  * of their mass Q lies; of these the ones with w >= min-p; always the first.  With
  * Q the kept mass, the token is the first in order of ids whose kept mass up to and
@@ -378,7 +379,7 @@ epic_status epic_sample_tokens(const void* d_logits, int32_t dtype, int32_t B, i
  *   loss    = w tau^2 sum_k p_k (log p_k - (z[id_k] / tau - lse))
  *   grad_j  = w tau g (softmax(z / tau)_j - sum over entries of token j of p)
  * with w = d_weight[b][i] (NULL: 1) and g the gradient that comes down.  A row
- * without entries that count and a row of weight 0 (whose logits are not read)
+ * without entries that count and a row of weight 0 (whatever its logits are)
  * have loss and gradient 0.  A token of probability 0 under the student that
  * the teacher wants gives loss +inf and a finite gradient; NaN or +inf logits
  * give NaN.  Entries of one token add up.
@@ -388,7 +389,10 @@ epic_status epic_sample_tokens(const void* d_logits, int32_t dtype, int32_t B, i
  * epic_distill_backward: d_grad, of the logits' type, [B][n][V] with its own
  * strides in elements, from d_lse and g = d_grad_loss [B][n].
  * epic_distill_step: loss and gradient in one call with g = 1, reading the
- * logits once.
+ * logits once.  Its probabilities are relative to the row's own sum; those of
+ * epic_distill_backward come from d_lse in 32 bits, up to |lse| = 128, where they
+ * are off by up to 4.4e-5 of themselves, and from the row itself past that.  So the two
+ * forms of one gradient may differ by that much.
  * d_grad must not overlap d_logits; rows of d_grad must not overlap each other.
  * Errors: EPIC_ERR_INVALID_ARG as epic_propose_topk, and for tau not in
  * (0, 3e38]; EPIC_ERR_CAPACITY when K > 1024 or V > 2^31 - 4097.

@@ -278,9 +278,9 @@ __device__ __forceinline__ float cta_sums(Targets& t, float top, float c2, float
 }
 
 // Loss, and with a.grad the gradient: one cluster a row.  Bound by memory, and by the barriers between a row's two passes:
-// both for 4,096 rows of 32,768 bf16, half of them of weight 0, take 72 us, 5.6 TB/s where a copy reaches 6.7 (with 384
+// both for 4,096 rows of 32,768 bf16, half of them of weight 0, take 73 us, 5.5 TB/s where a copy reaches 6.7 (with 384
 // threads and four CTAs an SM; 512 and two took 90 when these took 74); the loss of 1,024 rows of 126,000 takes 48, 5.4 TB/s.
-//  One pass keeps each lane's maximum so far and the sum of
+// One pass keeps each lane's maximum so far and the sum of
 // exponentials relative to it; the gradient's pass reads the row again, from the caches.
 template <typename T>
 __global__ void __launch_bounds__(kDistillThreads, kDistillPerSm) k_distill(DistillArgs a) {

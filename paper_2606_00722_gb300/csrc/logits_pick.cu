@@ -3,7 +3,8 @@
 // min-p from given uniform numbers (epic_sample_tokens).
 //
 // With m the row's maximum and c = log2(e) / T a token's weight is
-// w = 2^((z - m) c), every operation rounded to 32 bits.  Confidences are w over
+// w = 2^((z - m) c), every operation rounded to 32 bits (the power to 2 units in the
+// last place, and to 0 below 2^-126).  Confidences are w over
 // the sum of w in 32 bits.  Sampling adds whole numbers instead,
 // q = rint(2^30 w) in 64 bits: such sums are exact, so which token a number
 // draws depends on the row and the number alone, not on how the row was split
@@ -42,8 +43,9 @@ constexpr float kOnes = 12582912.0f;       // 1.5 * 2^23
 constexpr float kHigh = 412316860416.0f;   // 1.5 * 2^38
 constexpr uint32_t kOnesBits = 0x4b400000u, kHighBits = 0x52c00000u;
 
-// Fewest threads of a CTA: short rows have less to read than to rank, clear and draw (80 rows of 1,280, 64 best of them drawn
-// from: 80 us with 64 threads, 31 with 256; 2,688 rows of 300: 158, 87, and 152 with 512, which leave an SM two rows for four).
+// Fewest threads of a CTA: short rows have less to read than to rank, clear and draw.  On the GPU with 64, 128, 256 and 512:
+// the 64 best of 80 rows of 1,280 33, 22, 18 and 17 us, draws from them 35, 25, 21 and 20; the nucleus of 2,688 rows of 300
+// 86, 72, 78 and 131 (512 leave an SM two rows for four).
 constexpr int kPickThreadsMin = 256;
 
 struct PickArgs {
@@ -1097,9 +1099,10 @@ struct Row {
 // ---- the K best
 //
 // conf = 2^((z - m) c) / sum, one pass from memory with a running maximum, then a few thousand elements from L2.  1,024 rows
-// of 126,000 bf16, 32 best: 62 us, 4.2 TB/s, where a copy of the bytes at 6.7 TB/s is 39 us.  What is left: issue slots
-// (56 % used; nine instructions an element) and the waits of a row's ranking, which three rows an SM cover in part.
-// Two CTAs an SM with 64 registers: 72 us.  Few rows: a call on the host takes 6.7 us, 64 rows of 32,768 on the GPU 6.1.
+// of 126,000 bf16, 32 best: 61 us, 4.2 TB/s, where a copy of the bytes at 6.7 TB/s is 39 us.  What is left: issue slots
+// (55 % used; nine instructions an element) and the waits of a row's ranking, which three rows an SM cover in part.
+// Two CTAs an SM with 64 registers: 64 us; three have 40 and spill 60 to 72 bytes, in the ways of a full list.  Few rows: a
+// call on the host takes 6.8 us, 64 rows of 32,768 on the GPU 6.2.
 
 template <typename T>
 struct Propose {
@@ -1181,9 +1184,11 @@ struct Propose {
 //
 // A pass from memory for the maximum, one from L2 for the masses by part, a chunk a lane for each draw; with a nucleus or a
 // long top-k a pass for the histogram and one for the bin's elements and the kept masses in place of that of masses.
-// 1,024 rows of 126,000 bf16: 100 us by temperature, 301 us with top-p; bound by instructions (55 and 67 % of the issue
-// slots; 17 and 55 an element, of which the histogram's two additions to shared memory are the slowest: one of 64 bits
-// took 570 us in all).  Two CTAs an SM: three of 40 registers spill (161 us by temperature).
+// 1,024 rows of 126,000 bf16: 100 us by temperature, 303 us with top-p.  17 and 54 instructions an element use 56 and 66 % of
+// the issue slots; the rest is waits that two rows an SM (46 % of its warps) leave open.  Of the nucleus's instructions the
+// histogram's two additions to shared memory are the slowest: one of 64 bits took 570 us in all.  Two CTAs an SM have 64
+// registers and spill 188 bytes; three have 40 and spill 304: 115 us by temperature, 320 with top-p.  With 512, 384 and 256
+// threads: 100, 117, 111 us and 303, 336, 321.
 
 template <typename T>
 struct Sample {

@@ -127,7 +127,8 @@ def test_costs_near_the_largest_number_do_not_overflow_on_the_way(cuda, K, tau, 
     import torch
     n, V = 3, 5000
     z = torch.randn((1, n, V), generator=torch.Generator().manual_seed(1)).cuda()
-    ids = torch.randperm(V, generator=torch.Generator().manual_seed(2))[:K].to(torch.int32).expand(1, n, K).contiguous().cuda()
+    ids = torch.randperm(V, generator=torch.Generator().manual_seed(2))[:K].to(torch.int32)
+    ids = ids.expand(1, n, K).contiguous().cuda()
     vals = torch.randn((1, n, K), generator=torch.Generator().manual_seed(3)).cuda()
     z.scatter_(2, ids.long(), torch.finfo(torch.float32).min)
     w = torch.full((1, n), weight, device='cuda')
