@@ -411,6 +411,110 @@ epic_status epic_distill_step(const void* d_logits, int32_t dtype, int32_t B, in
                               int32_t K, float tau, const float* d_weight, float* d_loss, void* d_grad,
                               int64_t grad_stride_b, int64_t grad_stride_n, void* cuda_stream);
 
+/*
+ * ---- The head itself: from hidden states ----
+ *
+ * The calls above begin at logits; the calls below begin one step before, at hidden
+ * states [B][n][d] (element c of position i of sequence b at b * stride_b + i *
+ * stride_n + c, strides >= 0 in elements, rows may start at any multiple of the
+ * element size) and the weights [V][d] of the output layer, a row of which is at
+ * v * head_stride.  They allocate nothing, are asynchronous on `cuda_stream`, may be
+ * captured in a CUDA graph, and may overlap on different streams with workspaces of
+ * their own.  A workspace is device memory of the caller's, aligned to 256 bytes, of at
+ * least the size that the call's *_workspace function gives for the same sizes and
+ * head; its contents do not matter and nothing is kept in it from call to call.
+ */
+
+/* The forms of the head's loss, for epic_head_loss_workspace */
+enum { EPIC_HEAD_FORWARD = 0, EPIC_HEAD_BACKWARD = 1, EPIC_HEAD_STEP = 2 };
+
+/*
+ * The loss of training a masked diffusion LM: softmax cross entropy of the head's
+ * logits z = h W^T at every position that has a target, d_target [B][n] int32 (an id
+ * outside 0..V-1, such as -1, says that the position does not count), weighted by
+ * w = d_weight [B][n] float32 (NULL: 1; a position of weight 0 does not count):
+ *   loss = w (lse - z[target]),  lse = log sum_v exp z[v]
+ * The logits are never kept: they are made in pieces, and of a step or backward call
+ * at most EPIC_HEAD_PIECE_MB [2048] of exponentials exist at a time, in 16 bits.
+ * dtype is EPIC_F16 or EPIC_BF16, of hidden states, head and both gradients.  Products
+ * are of that type with sums in 32 bits.
+ * epic_head_loss_forward: d_loss and d_lse [B][n] float32, 0 where a position does
+ * not count.
+ * epic_head_loss_backward: gradients of sum(grad_loss * loss), d_grad_loss [B][n]:
+ *   g = w grad_loss,  dz[v] = g (exp(z[v] - lse) - [v = target]),  dh = dz W,  dW = dz^T h
+ * into d_grad_hidden [B][n][d] (0 where a position does not count) and d_grad_head
+ * [V][d], both written whole, each with its own strides; either may be NULL.  d_lse is
+ * what the forward call gave for the same inputs; exponentials are taken relative to it
+ * and summed anew, so it does not limit their precision.
+ * epic_head_loss_step: loss and both gradients in one call with grad_loss = 1, making
+ * the logits once (bf16).
+ * In both, exponentials and hidden states times a row's factor are rounded to dtype
+ * (off by at most 2^-8 of a value in bf16, 2^-11 in fp16) before they are multiplied and summed.
+ * A target of probability 0 gives loss +inf and a finite gradient.  NaN or +inf
+ * logits give NaN, in the gradient of the head at all tokens.  What is in the rows of
+ * positions that do not count does not matter.
+ * The same call on the same inputs gives the same bits.
+ * Outputs must not overlap inputs, each other or the workspace; rows of a gradient
+ * must not overlap.  Errors: EPIC_ERR_INVALID_ARG (NULL pointers, sizes < 0, d < 1, a
+ * bad dtype, form or alignment, negative strides, head rows that overlap, a workspace
+ * that is too small), EPIC_ERR_CAPACITY when V > 2^31 - 4097 or d > 2^20.
+ */
+epic_status epic_head_loss_workspace(int32_t form, int32_t dtype, int32_t B, int32_t n, int32_t d, int32_t V,
+                                     const void* d_head, int64_t head_stride, size_t* bytes);
+epic_status epic_head_loss_forward(const void* d_hidden, int32_t dtype, int32_t B, int32_t n, int32_t d,
+                                   int64_t stride_b, int64_t stride_n, const void* d_head, int32_t V,
+                                   int64_t head_stride, const int32_t* d_target, const float* d_weight, float* d_loss,
+                                   float* d_lse, void* d_workspace, size_t workspace_bytes, void* cuda_stream);
+epic_status epic_head_loss_backward(const void* d_hidden, int32_t dtype, int32_t B, int32_t n, int32_t d,
+                                    int64_t stride_b, int64_t stride_n, const void* d_head, int32_t V,
+                                    int64_t head_stride, const int32_t* d_target, const float* d_weight,
+                                    const float* d_lse, const float* d_grad_loss, void* d_grad_hidden,
+                                    int64_t grad_stride_b, int64_t grad_stride_n, void* d_grad_head,
+                                    int64_t grad_head_stride, void* d_workspace, size_t workspace_bytes,
+                                    void* cuda_stream);
+epic_status epic_head_loss_step(const void* d_hidden, int32_t dtype, int32_t B, int32_t n, int32_t d, int64_t stride_b,
+                                int64_t stride_n, const void* d_head, int32_t V, int64_t head_stride,
+                                const int32_t* d_target, const float* d_weight, float* d_loss, void* d_grad_hidden,
+                                int64_t grad_stride_b, int64_t grad_stride_n, void* d_grad_head,
+                                int64_t grad_head_stride, void* d_workspace, size_t workspace_bytes,
+                                void* cuda_stream);
+
+/*
+ * Rows in 8 bits with a scale for each: of the positions d_pos [B][k] (NULL: the first
+ * k <= n) of d_x [B][n][d] (EPIC_F32, EPIC_F16 or EPIC_BF16),
+ *   s = max|x| / 127,  q = rint(x / s) kept within -127..127
+ * with quotients rounded to the nearest 32-bit number and halves to even; s = 0 gives
+ * q = 0.  A row with a NaN has scale NaN, one with an infinity scale +inf, and so has no finite logits;
+ * a position outside 0..n-1 is a row of zeros with scale NaN, so that its logits are
+ * NaN and it has no candidates.  Outputs d_q [B][k][d] int8 and d_scale [B][k] float32.  The same call
+ * on a head [1][V][d] gives its 8-bit weights and the scales of its tokens.
+ * Errors: EPIC_ERR_INVALID_ARG (NULL pointers, sizes < 0, d < 1, a bad dtype or
+ * alignment, negative strides, k > n without d_pos), EPIC_ERR_CAPACITY when B k > 2^31 - 1.
+ */
+epic_status epic_quantize_rows(const void* d_x, int32_t dtype, int32_t B, int32_t n, int32_t d, int64_t stride_b,
+                               int64_t stride_n, const int32_t* d_pos, int32_t k, int8_t* d_q, float* d_scale,
+                               void* cuda_stream);
+
+/*
+ * Rows of logits from hidden states d_q [B][k][d] and a head d_head [V][d] in 8-bit
+ * integers (any from -128 to 127), with a scale for each row, d_scale [B][k], and each token, d_head_scale
+ * [V] (float32):
+ *   z[b][i][v] = (sum_c q[b][i][c] head[v][c]) scale[b][i] head_scale[v]
+ * The sum is exact; its value in 32 bits times scale, then times head_scale, is rounded
+ * to d_logits' dtype (EPIC_F32, EPIC_F16, EPIC_BF16).  d_logits [B][k][V] has its own
+ * strides in elements, as epic_propose_topk and epic_sample_tokens take them; rows
+ * must not overlap.  Elements between the rows are left as they were.
+ * Errors: EPIC_ERR_INVALID_ARG (NULL pointers, sizes < 0, d < 1, a bad dtype or
+ * alignment, negative strides, head rows that overlap, a workspace that is too small),
+ * EPIC_ERR_CAPACITY when d > 131071, V > 2^31 - 4097 or B k > 2^21.
+ */
+epic_status epic_int8_logits_workspace(int32_t B, int32_t k, int32_t d, int32_t V, const int8_t* d_head,
+                                       int64_t head_stride, size_t* bytes);
+epic_status epic_int8_logits(const int8_t* d_q, const float* d_scale, int32_t B, int32_t k, int32_t d,
+                             const int8_t* d_head, const float* d_head_scale, int32_t V, int64_t head_stride,
+                             void* d_logits, int32_t dtype, int64_t stride_b, int64_t stride_n, void* d_workspace,
+                             size_t workspace_bytes, void* cuda_stream);
+
 /* Device counters accumulated since the object was created (or reset). */
 typedef struct {
   uint64_t checks;           /* single-candidate validity checks run           */

@@ -1,0 +1,472 @@
+// Softmax cross entropy through a head, without the logits: hidden states [B][n][d], head [V][d].
+//
+// Per position that counts, with z = W h, y its target, w its weight and g the
+// gradient from above:
+//   loss = w (lse - z_y),  lse = log sum_v exp z_v
+//   dz_v = w g (exp(z_v - lse) - [v = y]),  dh = dz W,  dW = sum over positions of dz h
+//
+// A call goes through its positions in pieces.  Of each, the positions that
+// count are packed (masked training leaves out half and more), then
+//   forward:   logits -> records (sums of exponentials by column range) -> loss
+//   step:      logits -> records and exponentials e, relative to a reference known before (the target's logit, from a
+//              product of two rows) -> loss, and each row's sum S -> dh = (w / S) e W, dW = e^T (h w / S)
+//   backward:  the same relative to the logsumexp of the forward call
+// so a step makes the logits once.  e is kept for a piece in 16 bits, like the operands of the products that read it:
+// one rounding of at most 2^-8 (bf16) or 2^-11 (fp16) each, independent ones that a sum over many evens out.  At the target, e - S
+// cancels where the model is sure; there e holds minus the sum of the others, which is summed apart.
+// Sums, references and losses are 32 bits.
+#include <stdlib.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "head_loss.h"
+#include "head_rows.cuh"
+
+namespace epic {
+namespace {
+
+constexpr int kPieceRows = 16384;  // most positions of a piece: each CTA of k_head_rows counts over all of them
+constexpr int kRowsThreads = 256;
+
+struct RowsArgs {
+  HeadPlan p;
+  const void* hidden;
+  long long stride_b, stride_n;
+  long long r0;  // first position of the piece
+  int n;
+  const int32_t* target;
+  const float* weight;    // or NULL
+  const float* up;        // the backward pass, else NULL
+  const float* lse;       // the backward pass, else NULL
+  float *loss, *lse_out;  // of positions that do not count: 0; or NULL
+  HiddenGrad out;         // grad NULL: none
+  int per;                // positions of a CTA
+  bool probs;             // rows' references are wanted (step)
+  bool scaled;            // fp16: exponentials up to 2^14, factors of the gradient relative to their largest
+};
+
+__device__ __forceinline__ float row_factor(const RowsArgs& a, long long r) {
+  const int y = a.target[r];
+  if (y < 0 || y >= a.p.V) return 0.0f;
+  const float w = a.weight ? a.weight[r] : 1.0f;
+  return w == 0.0f ? 0.0f : a.up ? w * a.up[r] : w;
+}
+
+// Smallest power of two that is not below x > 0, of finite x within 2^-100 .. 2^100; 1 otherwise
+__device__ __forceinline__ float pow2_above(float x) {
+  if (!(x > 7.9e-31f && x < 1.2e30f)) return 1.0f;
+  return pow2_whole((float)(((__float_as_int(x) + 0x7fffff) >> 23) - 127));
+}
+
+constexpr float kHalfScale = 14.0f;  // exponentials in fp16 are up to 2^14.5: 2^-28 of a row's sum is still a normal number
+
+// The reference of a row whose logsumexp is known
+__device__ __forceinline__ float lse_ref(float lse, bool scaled) {
+  const float ref = rintf(lse * kLog2E) - (scaled ? kHalfScale : 0.0f);
+  return fabsf(ref) < 3.0e38f ? ref : 0.0f;
+}
+
+// Packs the positions that count.  Every CTA counts those before its own, so nothing waits; it also finds the largest
+// factor.  A warp copies a row, and with `probs` takes its product with the target's row of the head.
+template <typename T>
+__global__ void __launch_bounds__(kRowsThreads) k_head_rows(RowsArgs a) {
+  __shared__ int s_before[kRowsThreads / 32], s_all[kRowsThreads / 32];
+  __shared__ float s_top[kRowsThreads / 32];
+  const HeadPlan& p = a.p;
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, warps = kRowsThreads / 32;
+  const int first = blockIdx.x * a.per, last = min(first + a.per, p.rows);
+  int before = 0, all = 0;
+  float top = 0.0f;
+  for (int i = threadIdx.x; i < p.rows; i += kRowsThreads) {
+    const float f = row_factor(a, a.r0 + i);
+    all += f != 0.0f;
+    before += f != 0.0f && i < first;
+    top = fmaxf(top, fabsf(f));
+  }
+  for (int o = 16; o; o >>= 1) {
+    before += __shfl_xor_sync(~0u, before, o);
+    all += __shfl_xor_sync(~0u, all, o);
+    top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
+  }
+  if (lane == 0) s_before[warp] = before, s_all[warp] = all, s_top[warp] = top;
+  __syncthreads();
+  before = all = 0, top = 0.0f;
+  for (int w = 0; w < warps; w++) before += s_before[w], all += s_all[w], top = fmaxf(top, s_top[w]);
+  const float post = a.scaled ? pow2_above(top) * pow2_whole(-kHalfScale) : 1.0f;
+  if (blockIdx.x == 0 && threadIdx.x == 0) *p.count = all, *p.again = a.scaled, *p.post = post;
+
+  for (int i0 = first; i0 < last; i0 += 32) {
+    const long long mine = i0 + lane;
+    const float f = mine < last ? row_factor(a, a.r0 + mine) : 0.0f;
+    const unsigned there = __ballot_sync(~0u, f != 0.0f);
+    for (int j = warp; j < min(32, last - i0); j += warps) {
+      const long long i = i0 + j, r = a.r0 + i, b = r / a.n, at = r % a.n;
+      const float g = __shfl_sync(~0u, f, j);
+      if (g == 0.0f) {
+        if (lane == 0 && a.loss) a.loss[r] = 0.0f;
+        if (lane == 0 && a.lse_out) a.lse_out[r] = 0.0f;
+        if (a.out.grad) {
+          T* o = (T*)a.out.grad + b * a.out.stride_b + at * a.out.stride_n;
+          for (int k = lane; k < p.d; k += 32) o[k] = of_float<T>(0.0f);
+        }
+        continue;
+      }
+      const int q = before + __popc(there & ((1u << j) - 1)), y = a.target[r];
+      const T* h = (const T*)a.hidden + b * a.stride_b + at * a.stride_n;
+      const T* w = (const T*)p.head + y * p.ldw;
+      T* hc = (T*)p.hc + q * p.ldh;
+      float ref = 0.0f, dot = 0.0f;
+      if (a.lse) ref = lse_ref(a.lse[r], a.scaled);
+      for (int k = lane; k < p.ldh; k += 32) {
+        const float x = k < p.d ? as_float(h[k]) : 0.0f;
+        hc[k] = of_float<T>(x);
+        if (a.probs && k < p.d) dot = fmaf(x, as_float(w[k]), dot);
+      }
+      if (a.probs) {
+        for (int o = 16; o; o >>= 1) dot += __shfl_xor_sync(~0u, dot, o);
+        ref = whole_ref(dot);
+      }
+      if (lane == 0) {
+        p.src[q] = (int)i;
+        p.tgt[q] = y;
+        p.g[q] = g;
+        p.ref[q] = ref;
+      }
+    }
+    before += __popc(there);
+  }
+  // rows up to the end of the tile
+  const int end = (all + kRowTile - 1) / kRowTile * kRowTile;
+  for (int q = all + blockIdx.x * warps + warp; q < end; q += gridDim.x * warps)
+    for (int k = lane; k < p.ldh; k += 32)
+      ((T*)p.hc)[q * p.ldh + k] = ((T*)p.hs)[q * p.ldh + k] = of_float<T>(0.0f);
+}
+
+constexpr int kMeetRows = 32, kMeetWarps = 16;
+
+struct MeetArgs {
+  HeadPlan p;
+  long long r0;
+  const float* weight;
+  float *loss, *lse;  // by position, or NULL
+  bool probs;         // exponentials are wanted: factors, and hs
+  bool stored;        // they are in e already, relative to p.ref
+  bool known;         // p.ref comes from the logsumexp: no row can have left its window
+};
+
+// Loss and factors of 32 packed rows from their records; a lane a row, the records dealt to the warps and met in a fixed
+// order.
+template <typename T>
+__global__ void __launch_bounds__(kMeetWarps * 32) k_head_meet(MeetArgs a) {
+  __shared__ float s_ref[kMeetWarps][32], s_sum[kMeetWarps][32], s_scale[32];
+  __shared__ int s_left[kMeetWarps][32];
+  const HeadPlan& p = a.p;
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+  const int n = *p.count, q0 = blockIdx.x * kMeetRows, q = q0 + lane;
+  if (q0 >= n) return;
+  float ref = kNoRef, s = 0.0f;
+  int left = 0;
+  if (q < n) {
+    const float own = a.stored ? p.ref[q] : 0.0f;
+#pragma unroll 4
+    for (int t = warp; t < p.nrec; t += kMeetWarps) {
+      const float2 x = p.rec[(long long)t * p.cap + q];
+      left |= a.stored && x.x != own;
+      meet(ref, s, x.x, x.y);
+    }
+  }
+  s_ref[warp][lane] = ref, s_sum[warp][lane] = s, s_left[warp][lane] = left;
+  __syncthreads();
+  if (warp == 0) {
+    float scale = 0.0f;
+    if (q < n) {
+      for (int w = 1; w < kMeetWarps; w++) {
+        meet(ref, s, s_ref[w][lane], s_sum[w][lane]);
+        left |= s_left[w][lane];
+      }
+      // the others' sum against the target: loss = log(1 + sum / e_y)
+      const float zt = p.zt[q], by = s == 0.0f && zt > -CUDART_INF_F ? -CUDART_INF_F : log2f(s) + fmaf(-zt, kLog2E, ref);
+      const float x = by * kLn2, rest = log1pf(expf(-fabsf(x)));
+      float nll = x > 0.0f ? x + rest : rest;
+      if (!(zt < CUDART_INF_F) || s != s) nll = CUDART_NAN_F;
+      const float lse = x > 0.0f ? (ref + log2f(s)) * kLn2 + rest : zt + nll;
+      const long long r = a.r0 + p.src[q];
+      if (a.loss) a.loss[r] = (a.weight ? a.weight[r] : 1.0f) * nll;
+      if (a.lse) a.lse[r] = lse;
+      if (a.probs) {
+        float to = p.ref[q];
+        if (!a.known && (!a.stored || left || !(fmaf(zt, kLog2E, -to) <= kWindow))) {
+          to = lse_ref(lse, std::is_same<T, __half>::value);
+          *p.again = 1;
+        }
+        const float others = s == 0.0f ? 0.0f : s * pow2_whole(ref - to);
+        const float coef = p.g[q] / (others + ex2(fmaf(zt, kLog2E, -to)));
+        p.ref[q] = to;
+        p.at[q] = -others;
+        p.coef[q] = coef;
+        if (a.stored) ((T*)p.e)[q * p.lde + p.tgt[q]] = of_float<T>(-others);
+        scale = coef / *p.post;
+      }
+    }
+    s_scale[lane] = scale;
+  }
+  if (!a.probs) return;
+  __syncthreads();
+  for (int j = warp; j < min(kMeetRows, n - q0); j += kMeetWarps) {
+    const T* hc = (const T*)p.hc + (q0 + j) * p.ldh;
+    T* hs = (T*)p.hs + (q0 + j) * p.ldh;
+    const float scale = s_scale[j];
+    for (int k = lane; k < p.ldh; k += 32) hs[k] = of_float<T>(as_float(hc[k]) * scale);
+  }
+}
+
+template <typename T>
+__global__ void k_fill_zero(T* grad, long long stride, int d) {
+  for (int k = threadIdx.x; k < d; k += blockDim.x) grad[blockIdx.x * stride + k] = of_float<T>(0.0f);
+}
+
+// ---------------------------------------------------------------- host
+
+enum HeadForm { kForward = 0, kBackward = 1, kStep = 2 };
+
+size_t round_up(size_t n, size_t m) { return (n + m - 1) / m * m; }
+
+// Where the parts of a workspace lie; base NULL only counts.
+struct Carver {
+  char* base;
+  size_t used;
+  template <typename P>
+  void take(P*& p, size_t count, size_t size) {
+    p = base ? (P*)(base + used) : nullptr;
+    used += round_up(count * size, 256);
+  }
+};
+
+struct HeadCall {
+  int form, dtype, B, n, d, V;
+  const void* head;
+  int64_t head_stride;
+};
+
+bool bad_call(const HeadCall& c) {
+  return c.form < kForward || c.form > kStep || (c.dtype != EPIC_F16 && c.dtype != EPIC_BF16) || c.B < 0 || c.n < 0 ||
+         c.d < 1 || c.V < 0 || (c.V > 1 && c.head_stride < c.d);
+}
+
+constexpr int kMostTokens = 0x7fffffff - 4096, kMostWidth = 1 << 20;
+
+// The plan of the first piece and the bytes that all pieces share
+size_t plan_head(const HeadCall& c, void* base, HeadPlan& p) {
+  const long long rows = (long long)c.B * c.n;
+  p = HeadPlan{};
+  p.d = c.d;
+  p.V = c.V;
+  p.ldw = c.head_stride;
+  p.head = c.head;
+  p.ldh = round_up(c.d, 8);
+  p.lde = round_up(std::max(c.V, 1), 64);
+  p.nrec = (c.V + kRecCols - 1) / kRecCols;
+  size_t bytes = (size_t)2048 << 20;  // of exponentials
+  if (const char* e = getenv("EPIC_HEAD_PIECE_MB")) bytes = strtoull(e, nullptr, 10) << 20;
+  const long long fit = (long long)(bytes / (p.lde * 2)) / kRowTile * kRowTile;
+  p.cap = (int)std::min<long long>(round_up(std::max(rows, 1ll), kRowTile),
+                                   std::min<long long>(kPieceRows, std::max<long long>(kRowTile, fit)));
+  const size_t cap = p.cap;
+  Carver w = {(char*)base, 0};
+  w.take(p.count, 1, 4);
+  w.take(p.again, 1, 4);
+  w.take(p.post, 1, 4);
+  w.take(p.src, cap, 4);
+  w.take(p.tgt, cap, 4);
+  for (float** f : {&p.g, &p.ref, &p.coef, &p.at, &p.zt}) w.take(*f, cap, 4);
+  w.take(p.hc, cap * p.ldh, 2);
+  w.take(p.hs, cap * p.ldh, 2);
+  w.take(p.rec, cap * p.nrec, sizeof(float2));
+  if (c.form != kForward) {
+    w.take(p.e, cap * p.lde, 2);
+    if (rows > p.cap) w.take(p.acc, (size_t)c.V * c.d, 4);
+  }
+  return w.used;
+}
+
+struct HeadTensors {
+  const void* hidden;
+  int64_t stride_b, stride_n;
+  const int32_t* target;
+  const float *weight, *lse_in, *up;
+  float *loss, *lse;
+  void* grad_hidden;
+  int64_t gstride_b, gstride_n;
+  void* grad_head;
+  int64_t ghead_stride;
+};
+
+epic_status last_error() {
+  if (cudaGetLastError() == cudaSuccess) return EPIC_OK;
+  return EPIC_ERR_CUDA;
+}
+
+#define EPIC_TRY(call)                     \
+  do {                                     \
+    const epic_status s_ = (call);         \
+    if (s_ != EPIC_OK) return s_;          \
+  } while (0)
+
+template <typename T>
+epic_status run_head(const HeadCall& c, const HeadTensors& t, HeadPlan p, cudaStream_t st) {
+  const long long rows = (long long)c.B * c.n;
+  const bool half = c.dtype == EPIC_F16, grads = c.form != kForward;
+  if (rows == 0 || c.V == 0) {
+    if (rows == 0 && t.grad_head && c.V > 0) {
+      k_fill_zero<T><<<c.V, 256, 0, st>>>((T*)t.grad_head, t.ghead_stride, c.d);
+      EPIC_TRY(last_error());
+    }
+    if (rows == 0) return EPIC_OK;
+  }
+  for (long long r0 = 0; r0 < rows; r0 += p.cap) {
+    p.rows = (int)std::min<long long>(p.cap, rows - r0);
+    RowsArgs a = {};
+    a.p = p;
+    a.hidden = t.hidden;
+    a.stride_b = t.stride_b;
+    a.stride_n = t.stride_n;
+    a.r0 = r0;
+    a.n = c.n;
+    a.target = t.target;
+    a.weight = t.weight;
+    a.up = t.up;
+    a.lse = t.lse_in;
+    a.loss = t.loss;
+    a.lse_out = t.lse;
+    a.out = {t.grad_hidden, t.gstride_b, t.gstride_n, r0, c.n};
+    a.per = std::max(8, (p.rows + 511) / 512);
+    a.probs = c.form == kStep && !half;
+    a.scaled = half && grads;
+    k_head_rows<T><<<(p.rows + a.per - 1) / a.per, kRowsThreads, 0, st>>>(a);
+    EPIC_TRY(last_error());
+    if (c.V == 0) continue;
+    // A step's exponentials are relative to the target's logit; fp16 has not the range for that and makes them once the
+    // logsumexp is known, as do rows that leave the window.
+    const bool known = c.form == kBackward, stored = known || a.probs;
+    EPIC_TRY(launch_head_logits(p, c.dtype, {true, stored, false}, st));
+    MeetArgs m = {p, r0, t.weight, t.loss, t.lse, grads, stored, known};
+    k_head_meet<T><<<(p.rows + kMeetRows - 1) / kMeetRows, kMeetWarps * 32, 0, st>>>(m);
+    EPIC_TRY(last_error());
+    if (grads && !known) EPIC_TRY(launch_head_logits(p, c.dtype, {false, true, true}, st));
+    if (t.grad_hidden) EPIC_TRY(launch_hidden_grad(p, c.dtype, a.out, st));
+    if (t.grad_head) {
+      const bool first = r0 == 0, last = r0 + p.cap >= rows;
+      const HeadSum sum = first ? (last ? kOnly : kFirst) : last ? kLast : kMiddle;
+      EPIC_TRY(launch_head_grad(p, c.dtype, t.grad_head, t.ghead_stride, sum, st));
+    }
+  }
+  return EPIC_OK;
+}
+
+bool misaligned(const void* p, size_t to) { return (uintptr_t)p % to != 0; }
+
+epic_status head_call(const HeadCall& c, const HeadTensors& t, void* ws, size_t ws_bytes, void* stream) {
+  if (bad_call(c) || t.stride_b < 0 || t.stride_n < 0) return EPIC_ERR_INVALID_ARG;
+  if (c.V > kMostTokens || c.d > kMostWidth) return EPIC_ERR_CAPACITY;
+  if (t.grad_hidden && (t.gstride_b < 0 || t.gstride_n < 0)) return EPIC_ERR_INVALID_ARG;
+  if (t.grad_head && c.V > 1 && t.ghead_stride < c.d) return EPIC_ERR_INVALID_ARG;
+  const long long rows = (long long)c.B * c.n;
+  for (const void* p : {t.hidden, c.head, (const void*)t.grad_hidden, (const void*)t.grad_head})
+    if (misaligned(p, 2)) return EPIC_ERR_INVALID_ARG;
+  for (const void* p : {(const void*)t.target, (const void*)t.weight, (const void*)t.lse_in, (const void*)t.up,
+                        (const void*)t.loss, (const void*)t.lse})
+    if (misaligned(p, 4)) return EPIC_ERR_INVALID_ARG;
+  if (c.V > 0 && !c.head && rows > 0) return EPIC_ERR_INVALID_ARG;
+  if (rows > 0) {
+    if (!t.hidden || !t.target) return EPIC_ERR_INVALID_ARG;
+    if (c.form == kBackward ? !t.lse_in || !t.up : !t.loss) return EPIC_ERR_INVALID_ARG;
+    if (c.form == kForward && !t.lse) return EPIC_ERR_INVALID_ARG;
+  }
+  if (rows == 0 && (!t.grad_head || c.V == 0)) return EPIC_OK;
+  HeadPlan p;
+  if (!ws || misaligned(ws, 256) || ws_bytes < plan_head(c, nullptr, p)) return EPIC_ERR_INVALID_ARG;
+  plan_head(c, ws, p);
+  cudaStream_t st = (cudaStream_t)stream;
+  return c.dtype == EPIC_F16 ? run_head<__half>(c, t, p, st) : run_head<__nv_bfloat16>(c, t, p, st);
+}
+
+}  // namespace
+}  // namespace epic
+
+extern "C" {
+
+epic_status epic_head_loss_workspace(int32_t form, int32_t dtype, int32_t B, int32_t n, int32_t d, int32_t V,
+                                     const void* d_head, int64_t head_stride, size_t* bytes) {
+  using namespace epic;
+  const HeadCall c = {form, dtype, B, n, d, V, d_head, head_stride};
+  if (!bytes || bad_call(c)) return EPIC_ERR_INVALID_ARG;
+  if (V > kMostTokens || d > kMostWidth) return EPIC_ERR_CAPACITY;
+  HeadPlan p;
+  *bytes = plan_head(c, nullptr, p);
+  return EPIC_OK;
+}
+
+epic_status epic_head_loss_forward(const void* d_hidden, int32_t dtype, int32_t B, int32_t n, int32_t d,
+                                   int64_t stride_b, int64_t stride_n, const void* d_head, int32_t V,
+                                   int64_t head_stride, const int32_t* d_target, const float* d_weight, float* d_loss,
+                                   float* d_lse, void* d_workspace, size_t workspace_bytes, void* cuda_stream) {
+  using namespace epic;
+  HeadTensors t = {};
+  t.hidden = d_hidden;
+  t.stride_b = stride_b;
+  t.stride_n = stride_n;
+  t.target = d_target;
+  t.weight = d_weight;
+  t.loss = d_loss;
+  t.lse = d_lse;
+  return head_call({kForward, dtype, B, n, d, V, d_head, head_stride}, t, d_workspace, workspace_bytes, cuda_stream);
+}
+
+epic_status epic_head_loss_backward(const void* d_hidden, int32_t dtype, int32_t B, int32_t n, int32_t d,
+                                    int64_t stride_b, int64_t stride_n, const void* d_head, int32_t V,
+                                    int64_t head_stride, const int32_t* d_target, const float* d_weight,
+                                    const float* d_lse, const float* d_grad_loss, void* d_grad_hidden,
+                                    int64_t grad_stride_b, int64_t grad_stride_n, void* d_grad_head,
+                                    int64_t grad_head_stride, void* d_workspace, size_t workspace_bytes,
+                                    void* cuda_stream) {
+  using namespace epic;
+  HeadTensors t = {};
+  t.hidden = d_hidden;
+  t.stride_b = stride_b;
+  t.stride_n = stride_n;
+  t.target = d_target;
+  t.weight = d_weight;
+  t.lse_in = d_lse;
+  t.up = d_grad_loss;
+  t.grad_hidden = d_grad_hidden;
+  t.gstride_b = grad_stride_b;
+  t.gstride_n = grad_stride_n;
+  t.grad_head = d_grad_head;
+  t.ghead_stride = grad_head_stride;
+  return head_call({kBackward, dtype, B, n, d, V, d_head, head_stride}, t, d_workspace, workspace_bytes, cuda_stream);
+}
+
+epic_status epic_head_loss_step(const void* d_hidden, int32_t dtype, int32_t B, int32_t n, int32_t d, int64_t stride_b,
+                                int64_t stride_n, const void* d_head, int32_t V, int64_t head_stride,
+                                const int32_t* d_target, const float* d_weight, float* d_loss, void* d_grad_hidden,
+                                int64_t grad_stride_b, int64_t grad_stride_n, void* d_grad_head,
+                                int64_t grad_head_stride, void* d_workspace, size_t workspace_bytes,
+                                void* cuda_stream) {
+  using namespace epic;
+  HeadTensors t = {};
+  t.hidden = d_hidden;
+  t.stride_b = stride_b;
+  t.stride_n = stride_n;
+  t.target = d_target;
+  t.weight = d_weight;
+  t.loss = d_loss;
+  t.grad_hidden = d_grad_hidden;
+  t.gstride_b = grad_stride_b;
+  t.gstride_n = grad_stride_n;
+  t.grad_head = d_grad_head;
+  t.ghead_stride = grad_head_stride;
+  return head_call({kStep, dtype, B, n, d, V, d_head, head_stride}, t, d_workspace, workspace_bytes, cuda_stream);
+}
+
+}  // extern "C"

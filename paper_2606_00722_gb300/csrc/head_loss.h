@@ -1,0 +1,58 @@
+// What the kernels of the head's loss share: the plan of one piece of a call
+// (sizes, operands, workspace) and their launchers.
+#pragma once
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "../../include/epic.h"
+
+namespace epic {
+
+constexpr int kRowTile = 256;   // rows of a workspace come in whole tiles
+constexpr int kRecCols = 64;    // tokens whose exponentials one record sums
+
+// A piece: up to `cap` positions of the call.  Those that count stand in order, packed, in rows 0..*count-1 of the
+// workspace; rows from there to the end of the tile are zeros in hc, hs and e.
+struct HeadPlan {
+  int rows, cap;            // positions of this piece; rows of room (a multiple of kRowTile)
+  int d, V, nrec;
+  long long ldh, lde, ldw;  // elements from row to row of hc and hs, of e, of the head
+  const void* head;         // [V][ldw]
+  int* count;               // rows that count
+  int* again;               // != 0: rows whose exponentials left the window of their reference
+  float* post;              // what gradients of the head are multiplied with at the end
+  int* src;                 // [cap] position in the piece
+  int* tgt;                 // [cap] target token
+  float *g;                 // [cap] what the row's gradient is multiplied with (weight, gradient from above)
+  float *ref;               // [cap] exponentials are 2^(z log2 e - ref), ref a whole number
+  float *coef;              // [cap] gradient of a logit = coef (e - its sum at the target)
+  float *at;                // [cap] the row's e at the target: minus the sum of the others
+  float *zt;                // [cap] logit of the target
+  float2* rec;              // [nrec][cap] (whole reference, sum of exponentials relative to it), target left out
+  void *hc, *hs;            // [cap][ldh] hidden states; the same times coef / *post
+  void* e;                  // [cap][lde]
+  float* acc;               // [V][d] or NULL: gradient of the head so far, of calls in several pieces
+};
+
+// How a piece's gradient of the head meets the pieces before it
+enum HeadSum { kOnly = 0, kFirst = 1, kMiddle = 2, kLast = 3 };
+
+// Where gradients of hidden states go: position r of the piece is grad[r0 + r], split into [b][i] by n.
+struct HiddenGrad {
+  void* grad;
+  long long stride_b, stride_n, r0;
+  int n;
+};
+
+// Logits of the packed rows.  sums: records and target logits.  probs: exponentials into e.  only_again: nothing unless
+// *again; then with `at` at the targets.
+struct LogitsPass {
+  bool sums, probs, only_again;
+};
+epic_status launch_head_logits(const HeadPlan& p, int dtype, const LogitsPass& pass, cudaStream_t st);
+// grad[src] = coef e W
+epic_status launch_hidden_grad(const HeadPlan& p, int dtype, const HiddenGrad& out, cudaStream_t st);
+// grad [V][stride] = post e^T hs, with the pieces before
+epic_status launch_head_grad(const HeadPlan& p, int dtype, void* grad, long long stride, HeadSum sum, cudaStream_t st);
+
+}  // namespace epic

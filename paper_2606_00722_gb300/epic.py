@@ -19,11 +19,11 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 _SRC = [os.path.join(_HERE, 'csrc', f) for f in
         ('epic.cu', 'kernels_walk.cu', 'kernels_cta.cu', 'kernels_select.cu', 'region_forward.cu', 'region_good.cu',
          'region_check.cu', 'peak.cu', 'witness.cu', 'logits_pick.cu', 'logits_distill.cu', 'logit_launch.cpp',
-         'grammar.cpp')]
+         'head_loss.cu', 'head_gemm.cu', 'head_int8.cu', 'grammar.cpp')]
 _DEPS = _SRC + [os.path.join(_HERE, 'csrc', f) for f in
                 ('grammar.h', 'device.cuh', 'walk.cuh', 'cover.cuh', 'warpwalk.cuh', 'packs.cuh',
                  'seqpack.cuh', 'launch.h', 'region.cuh', 'gscols.cuh', 'rows.cuh', 'skeleton.cuh',
-                 'logit_rows.cuh', 'logit_launch.h', 'mass_parts.h')] + \
+                 'logit_rows.cuh', 'logit_launch.h', 'mass_parts.h', 'head_loss.h', 'head_rows.cuh')] + \
     [os.path.join(_HERE, '..', 'include', 'epic.h'), os.path.join(_HERE, '..', 'include', 'epic_measure.h')]
 LIB_PATH = os.path.join(_HERE, '_build', 'libepic.so')
 ARCH_FLAGS = ['-gencode', 'arch=compute_103a,code=sm_103a']
@@ -95,6 +95,8 @@ EXPORTS = ('epic_grammar_create', 'epic_grammar_destroy', 'epic_grammar_lexer_st
            'epic_extract_witness',
            'epic_propose_topk', 'epic_sample_tokens', 'epic_distill_forward', 'epic_distill_backward',
            'epic_distill_step',
+           'epic_head_loss_workspace', 'epic_head_loss_forward', 'epic_head_loss_backward', 'epic_head_loss_step',
+           'epic_quantize_rows', 'epic_int8_logits_workspace', 'epic_int8_logits',
            'epic_get_stats', 'epic_status_string', 'epic_measure_int_peak', 'epic_last_kernel_times')
 
 
@@ -130,6 +132,16 @@ def load(path: str | None = None):
     lib.epic_distill_forward.argtypes = rows + target + [vp, vp, vp]
     lib.epic_distill_backward.argtypes = rows + target + [vp, vp, vp, i64, i64, vp]
     lib.epic_distill_step.argtypes = rows + target + [vp, vp, i64, i64, vp]
+    size = C.POINTER(C.c_size_t)
+    head = [vp, i32, i64]  # head, V and its stride
+    work = [vp, C.c_size_t, vp]  # workspace, its bytes, stream
+    lib.epic_head_loss_workspace.argtypes = [i32, i32, i32, i32, i32, i32, vp, i64, size]
+    lib.epic_head_loss_forward.argtypes = rows + head + [vp, vp, vp, vp] + work
+    lib.epic_head_loss_backward.argtypes = rows + head + [vp, vp, vp, vp, vp, i64, i64, vp, i64] + work
+    lib.epic_head_loss_step.argtypes = rows + head + [vp, vp, vp, vp, i64, i64, vp, i64] + work
+    lib.epic_quantize_rows.argtypes = rows + [vp, i32, vp, vp, vp]
+    lib.epic_int8_logits_workspace.argtypes = [i32, i32, i32, i32, vp, i64, size]
+    lib.epic_int8_logits.argtypes = [vp, vp, i32, i32, i32, vp, vp, i32, i64, vp, i32, i64, i64] + work
     lib.epic_get_stats.argtypes = [vp, C.POINTER(_Stats), C.c_size_t, C.c_int]
     lib.epic_measure_int_peak.argtypes = [C.POINTER(C.c_double), C.POINTER(C.c_double), vp]
     lib.epic_measure_int_peak.restype = C.c_int
@@ -369,17 +381,19 @@ def extract_witness(g: Grammar, t: LexTable, x, terms, lengths, stream=None):
 
 _DTYPES = {}  # torch dtype of logits -> the C-ABI's code; filled on the first call
 _T = None     # torch, and what the calls need of it
+_INT8 = None
 _raw_stream = None
 _current_device = None
 
 
 def _logits_init():
-    global _T, _raw_stream, _current_device
+    global _T, _INT8, _raw_stream, _current_device
     import torch
     _DTYPES.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2})
     _raw_stream = getattr(torch._C, '_cuda_getCurrentRawStream', None) or (
         lambda device: torch.cuda.current_stream(device).cuda_stream)
     _current_device = getattr(torch._C, '_cuda_getDevice', None) or torch.cuda.current_device
+    _INT8 = torch.int8
     _T = (torch.float32, torch.int32, torch.uint8)
 
 
@@ -565,4 +579,211 @@ def decode_step_from_logits(g: Grammar, t: LexTable, x, pos, logits, n_target, b
         propose_topk(logits, bufs['cand'], bufs['cand_conf'], pos, temperature, stream)
     else:
         sample_tokens(logits, u, bufs['cand'], bufs['cand_conf'], pos, temperature, top_k, top_p, min_p, stream)
+    decode_step(g, t, x, pos, bufs['cand'], bufs['cand_conf'], n_target, bufs, stream)
+
+
+# ---------------------------------------------------------------- the head
+# Hidden states [B][n][d] are rows like logits; a workspace of each call's own comes from torch's allocator, on the
+# call's stream, unless the caller brings one.
+
+_HEAD_FORWARD, _HEAD_BACKWARD, _HEAD_STEP = range(3)
+
+
+def _hidden(hidden):
+    """_rows of hidden states, in 16 bits."""
+    rows = _rows(hidden)
+    if rows[1] == 0:
+        raise ValueError('expected float16 or bfloat16 hidden states, got %s' % hidden.dtype)
+    return rows
+
+
+def _weights(t, d, dtype, name, device):
+    """(address, V, stride) of head weights [V][d]; rows have unit stride and do not overlap."""
+    if t.dim() != 2 or t.shape[1] != d or t.dtype != dtype:
+        raise ValueError('%s: expected %s of shape [V][%d], got %s of shape %s' % (name, dtype, d, t.dtype,
+                                                                                  tuple(t.shape)))
+    if t.get_device() != device or (t.stride(1) != 1 and d > 1):
+        raise ValueError('%s: expected rows of unit stride on CUDA device %d' % (name, device))
+    V = t.shape[0]
+    return t.data_ptr(), V, t.stride(0) if V > 1 else d
+
+
+def _scratch(query, args, workspace, device, stream):
+    """(tensor, address, bytes) of the workspace that the library asks for; a caller's own has to be that large."""
+    need = C.c_size_t()
+    _check(query(*args, C.byref(need)), query.__name__)
+    if workspace is None:
+        import torch
+        if stream is None:
+            workspace = torch.empty(need.value, dtype=torch.uint8, device=device)
+        else:
+            on = torch.cuda.ExternalStream(stream, device=device) if isinstance(stream, int) else stream
+            with torch.cuda.stream(on):
+                workspace = torch.empty(need.value, dtype=torch.uint8, device=device)
+    elif workspace.get_device() != device or not workspace.is_contiguous():
+        raise ValueError('workspace: expected a contiguous tensor on CUDA device %d' % device)
+    return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def _head_args(form, hidden, head, workspace, stream):
+    """The arguments that the forms of the loss share: (rows, device, head, scratch); the scratch tensor has to live until
+    the call returns."""
+    rows = _hidden(hidden)
+    device = _device(hidden)
+    weights = _weights(head, rows[4], hidden.dtype, 'head', device)
+    lib = _lib or load()
+    scratch = _scratch(lib.epic_head_loss_workspace,
+                       (form, rows[1], rows[2], rows[3], rows[4], weights[1], weights[0], weights[2]), workspace, device,
+                       stream)
+    return rows, device, weights, scratch
+
+
+def _head_gradient(head, grad, device):
+    if grad is None:
+        return None, 0
+    address, V, stride = _weights(grad, head.shape[1], head.dtype, 'grad_head', device)
+    if V != head.shape[0]:
+        raise ValueError('grad_head: expected shape %s' % (tuple(head.shape),))
+    return address, stride
+
+
+def _hidden_gradient(hidden, grad):
+    return (None, 0, 0) if grad is None else _gradient(hidden, grad)
+
+
+def head_loss_workspace(form, hidden, head):
+    """Bytes that a call of that form ('forward', 'backward' or 'step') needs as its workspace, a uint8 tensor that a
+    program may keep and pass to calls that do not overlap."""
+    rows = _hidden(hidden)
+    address, V, stride = _weights(head, rows[4], hidden.dtype, 'head', _device(hidden))
+    need = C.c_size_t()
+    _check((_lib or load()).epic_head_loss_workspace(('forward', 'backward', 'step').index(form), rows[1], rows[2],
+                                                     rows[3], rows[4], V, address, stride, C.byref(need)),
+           'epic_head_loss_workspace')
+    return need.value
+
+
+def head_loss_forward(hidden, head, target, loss, lse, weight=None, stream=None, workspace=None):
+    """epic_head_loss_forward: cross entropy loss and lse [B][n] float32 of hidden states [B][n][d] through head weights
+    [V][d] against target [B][n] int32 (an id outside 0..V-1: the position does not count); weight [B][n] float32."""
+    rows, device, weights, scratch = _head_args(_HEAD_FORWARD, hidden, head, workspace, stream)
+    f32, i32, _ = _T
+    shape = rows[2:4]
+    _check(_lib.epic_head_loss_forward(
+        *rows, *weights, _arg(target, shape, i32, 'target', device), _arg(weight, shape, f32, 'weight', device),
+        _arg(loss, shape, f32, 'loss', device), _arg(lse, shape, f32, 'lse', device), *scratch[1:],
+        _on(device, stream)), 'epic_head_loss_forward')
+
+
+def head_loss_backward(hidden, head, target, lse, grad_loss, grad_hidden, grad_head, weight=None, stream=None,
+                       workspace=None):
+    """epic_head_loss_backward: grad_hidden [B][n][d] and grad_head [V][d] (either may be None) from the forward call's
+    lse and the gradient grad_loss [B][n] of its loss."""
+    rows, device, weights, scratch = _head_args(_HEAD_BACKWARD, hidden, head, workspace, stream)
+    f32, i32, _ = _T
+    shape = rows[2:4]
+    _check(_lib.epic_head_loss_backward(
+        *rows, *weights, _arg(target, shape, i32, 'target', device), _arg(weight, shape, f32, 'weight', device),
+        _arg(lse, shape, f32, 'lse', device), _arg(grad_loss, shape, f32, 'grad_loss', device),
+        *_hidden_gradient(hidden, grad_hidden), *_head_gradient(head, grad_head, device), *scratch[1:],
+        _on(device, stream)), 'epic_head_loss_backward')
+
+
+def head_loss_step(hidden, head, target, loss, grad_hidden, grad_head, weight=None, stream=None, workspace=None):
+    """epic_head_loss_step: loss [B][n] and its gradients [B][n][d] and [V][d] in one call, for a training loop whose row
+    weights are known before the loss."""
+    rows, device, weights, scratch = _head_args(_HEAD_STEP, hidden, head, workspace, stream)
+    f32, i32, _ = _T
+    shape = rows[2:4]
+    _check(_lib.epic_head_loss_step(
+        *rows, *weights, _arg(target, shape, i32, 'target', device), _arg(weight, shape, f32, 'weight', device),
+        _arg(loss, shape, f32, 'loss', device), *_hidden_gradient(hidden, grad_hidden),
+        *_head_gradient(head, grad_head, device), *scratch[1:], _on(device, stream)), 'epic_head_loss_step')
+
+
+_HeadLoss = None  # head_loss's torch operation; made on the first call
+
+
+def _head_loss_init():
+    global _HeadLoss
+    import torch
+
+    class HeadLoss(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, hidden, head, target, weight):
+            loss = torch.empty(hidden.shape[:2], dtype=torch.float32, device=hidden.device)
+            lse = torch.empty_like(loss)
+            head_loss_forward(hidden, head, target, loss, lse, weight)
+            ctx.save_for_backward(hidden, head, target, weight, lse)
+            return loss
+
+        @staticmethod
+        @torch.autograd.function.once_differentiable
+        def backward(ctx, grad_loss):
+            hidden, head, target, weight, lse = ctx.saved_tensors
+            grads = [torch.empty(t.shape, dtype=t.dtype, device=t.device) if need else None
+                     for t, need in zip((hidden, head), ctx.needs_input_grad)]
+            head_loss_backward(hidden, head, target, lse, grad_loss.to(torch.float32).contiguous(), *grads, weight)
+            return grads[0], grads[1], None, None
+
+    _HeadLoss = HeadLoss
+
+
+def head_loss(hidden, head, target, weight=None):
+    """The cross entropy loss [B][n] of hidden states [B][n][d] through head weights [V][d] as a torch operation with
+    gradients for both (forward: epic_head_loss_forward, backward: epic_head_loss_backward); target and weight are
+    constants.  Streams are torch's own."""
+    import torch
+    if _HeadLoss is None:
+        _head_loss_init()
+    if weight is not None and weight.requires_grad and torch.is_grad_enabled():
+        raise ValueError('weight: the loss has no gradient for it; detach it')
+    return _HeadLoss.apply(hidden, head, target, weight)
+
+
+def quantize_rows(x, q, scale, pos=None, stream=None):
+    """epic_quantize_rows: rows pos [B][k] (None: the first k) of x [B][n][d] in 8 bits, q [B][k][d] int8 with scale
+    [B][k] float32.  A head [V][d] is quantized as head[None], with q[None] and scale[None]."""
+    rows = _rows(x)
+    device = _device(x)
+    B, d = rows[2], rows[4]
+    k = q.shape[1]
+    _check((_lib or load()).epic_quantize_rows(
+        *rows, _arg(pos, (B, k), _T[1], 'pos', device), k, _arg(q, (B, k, d), _INT8, 'q', device),
+        _arg(scale, (B, k), _T[0], 'scale', device), _on(device, stream)), 'epic_quantize_rows')
+
+
+def int8_logits(q, scale, head_q, head_scale, logits, stream=None, workspace=None):
+    """epic_int8_logits: logits [B][k][V] (float32, float16 or bfloat16, any strides along B and k) of 8-bit hidden states
+    q [B][k][d] with scale [B][k] through an 8-bit head head_q [V][d] with head_scale [V]."""
+    out = _rows(logits)
+    device = _device(logits)
+    B, k, V = out[2:5]
+    if q.dim() != 3:
+        raise ValueError('expected q [B][k][d]')
+    d = q.shape[2]
+    address, tokens, stride = _weights(head_q, d, _INT8, 'head_q', device)
+    if tokens != V:
+        raise ValueError('logits: expected [%d][%d][%d]' % (B, k, tokens))
+    lib = _lib or load()
+    scratch = _scratch(lib.epic_int8_logits_workspace, (B, k, d, V, address, stride), workspace, device, stream)
+    f32 = _T[0]
+    _check(lib.epic_int8_logits(
+        _arg(q, (B, k, d), _INT8, 'q', device), _arg(scale, (B, k), f32, 'scale', device), B, k, d, address,
+        _arg(head_scale, (V,), f32, 'head_scale', device), V, stride, out[0], out[1], out[5], out[6], *scratch[1:],
+        _on(device, stream)), 'epic_int8_logits')
+
+
+def decode_step_from_hidden(g: Grammar, t: LexTable, x, pos, hidden, head_q, head_scale, n_target, bufs,
+                            temperature=None, u=None, top_k=None, top_p=None, min_p=None, stream=None, workspace=None):
+    """One denoising step from the model's hidden states [B][n][d] on: those of the proposed positions pos [B][k] in 8 bits
+    (quantize_rows), their logits through an 8-bit head (int8_logits), then candidates by rank or by draws and decode_step
+    as decode_step_from_logits does.  bufs holds its buffers and q [B][k][d] int8, scale [B][k] float32, logits [B][k][V]
+    in float32, float16 or bfloat16."""
+    quantize_rows(hidden, bufs['q'], bufs['scale'], pos, stream)
+    int8_logits(bufs['q'], bufs['scale'], head_q, head_scale, bufs['logits'], stream, workspace)
+    if u is None:
+        propose_topk(bufs['logits'], bufs['cand'], bufs['cand_conf'], None, temperature, stream)
+    else:
+        sample_tokens(bufs['logits'], u, bufs['cand'], bufs['cand_conf'], None, temperature, top_k, top_p, min_p, stream)
     decode_step(g, t, x, pos, bufs['cand'], bufs['cand_conf'], n_target, bufs, stream)
