@@ -1,140 +1,553 @@
-// The three matrix products of the head's loss, in their simplest form: a CTA
-// computes a tile of 64 x 64 with operands staged in shared memory in 32 bits.
+// The matrix products of the head's loss, on the tensor units: logits = h W^T,
+// gradients dh = e W and dW = e^T hs.
+//
+// A tile of 256 x 256 is a pair of CTAs': each copies 128 rows of both operands in steps of 64 of the sum (TMA, six steps
+// ahead), one thread of the pair issues the products, sums lie in tensor memory, twice, so that eight warps a CTA work on
+// one tile's sums while the next tile's are made.  Operands are read as they lie: e along and across its rows, the head by
+// tokens and by hidden dimensions.
+#include <cuda.h>
+
+#include <algorithm>
+
 #include "head_loss.h"
 #include "head_rows.cuh"
+#include "tensor_tiles.cuh"
 
 namespace epic {
 namespace {
 
-constexpr int kT = 64, kStep = 16;
+constexpr int kTile = 256, kHalf = 128;  // a pair's tile, a CTA's share of an operand
+constexpr int kStepK = 64, kStages = 6;
+constexpr int kOperand = kHalf * kStepK * 2, kStage = 2 * kOperand;  // bytes
+constexpr int kWorkWarps = 8, kThreads = 128 + 32 * kWorkWarps;
+constexpr int kPairs = 76;  // of the GB300's 152 SMs
+constexpr int kTurnRow = 34;  // 16-bit elements from row to row of a warp's turning buffer
+constexpr int kTurn = 32 * kTurnRow * 2;
+constexpr int kShared = kStages * kStage + kWorkWarps * kTurn + 1024;
 
-struct Tile {
-  float a[kStep][kT + 1], b[kStep][kT + 1];
-  float out[kT][kT + 1];
+struct Bars {
+  uint64_t full[kStages], empty[kStages], sums_full[2], sums_empty[2];
+  uint32_t sums;
 };
 
-// out = sum_k fa(k, m) fb(k, n) over the tile at (m0, n0)
-template <typename FA, typename FB>
-__device__ void tile_product(Tile& t, int K, FA fa, FB fb) {
-  float acc[4][4] = {};
-  const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-  for (int k0 = 0; k0 < K; k0 += kStep) {
-    for (int i = threadIdx.x; i < kStep * kT; i += 256) {
-      const int k = i / kT, m = i % kT;
-      t.a[k][m] = k0 + k < K ? fa(k0 + k, m) : 0.0f;
-      t.b[k][m] = k0 + k < K ? fb(k0 + k, m) : 0.0f;
-    }
-    __syncthreads();
-    for (int k = 0; k < kStep; k++)
-      for (int i = 0; i < 4; i++)
-        for (int j = 0; j < 4; j++) acc[i][j] = fmaf(t.a[k][ty * 4 + i], t.b[k][tx * 4 + j], acc[i][j]);
-    __syncthreads();
+// One tile of a product: where its operands' boxes lie and how many steps its sum has
+struct Task {
+  int m0, n0;      // rows of A and B
+  int k0, steps;   // first step
+  int job;         // 0: logits, or gradient of hidden states; 1: gradient of the head
+  int part;        // of a sum in several parts
+};
+
+struct TileArgs {
+  HeadPlan p;
+  LogitsPass pass;
+  HiddenGrad out;
+  void* grad_head;
+  long long grad_head_stride;
+  HeadSum sum;
+  int bf16;
+};
+
+struct Maps {
+  CUtensorMap hc, hs, head_k, head_mn, e_k, e_mn;
+};
+
+__device__ __forceinline__ int up_div(int a, int b) { return (a + b - 1) / b; }
+
+// The i-th tile of pair `pair`, or false.  Logits: the rows' tiles of one column of tiles after another, so that the head is
+// read once.
+__device__ __forceinline__ bool logits_task(const TileArgs& a, int n, int pair, int i, Task& t) {
+  const int mt = up_div(n, kTile), at = pair + i * kPairs;
+  if (at >= mt * up_div(a.p.V, kTile)) return false;
+  t = {at % mt * kTile, at / mt * kTile, 0, up_div(a.p.d, kStepK), 0, 0};
+  return true;
+}
+
+// Gradients: first all tiles of hidden states' (long sums), then the head's.  Where the former do not come out even, the
+// pairs without a last one take as many of the latter as it is worth before the rest is dealt to all.
+__device__ __forceinline__ bool grads_task(const TileArgs& a, int n, int pair, int i, Task& t) {
+  const GradSplit& s = a.p.split;
+  const int ct = up_div(a.p.d, kTile);
+  const int mt = up_div(n, kTile), vt = up_div(a.p.V, kTile);
+  const int hidden = s.hidden_parts * mt * ct, head = s.head_parts * vt * ct;
+  const int own = hidden / kPairs + (pair < hidden % kPairs);
+  if (i < own) {
+    const int at = pair + i * kPairs, part = at / (mt * ct), tile = at % (mt * ct);
+    const int all = up_div(a.p.V, kStepK), k0 = (int)((long long)all * part / s.hidden_parts);
+    t = {tile / ct * kTile, tile % ct * kTile, k0, (int)((long long)all * (part + 1) / s.hidden_parts) - k0, 0, part};
+    return true;
   }
-  for (int i = 0; i < 4; i++)
-    for (int j = 0; j < 4; j++) t.out[ty * 4 + i][tx * 4 + j] = acc[i][j];
+  i -= own;
+  const int all = up_div(n, kStepK), last = hidden % kPairs, idle = last ? kPairs - last : 0;
+  int at;
+  const int per = up_div(all, max(1, s.head_parts)) + s.tile_cost;
+  const int first = idle ? min(head / idle, (up_div(up_div(a.p.V, kStepK), s.hidden_parts) + s.tile_cost) / per) : 0;
+  if (pair >= last && idle) {
+    if (i < first) at = pair - last + i * idle;
+    else at = first * idle + pair + (i - first) * kPairs;
+  } else {
+    at = first * idle + pair + i * kPairs;
+  }
+  if (at >= head) return false;
+  const int part = at / (vt * ct), tile = at % (vt * ct), k0 = (int)((long long)all * part / s.head_parts);
+  t = {tile / ct * kTile, tile % ct * kTile, k0, (int)((long long)all * (part + 1) / s.head_parts) - k0, 1, part};
+  return true;
+}
+
+template <typename T>
+__device__ __forceinline__ uint32_t pack2(float a, float b);
+template <>
+__device__ __forceinline__ uint32_t pack2<__half>(float a, float b) {
+  const __half2 h = __floats2half2_rn(a, b);
+  return *(const uint32_t*)&h;
+}
+template <>
+__device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float a, float b) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+  return *(const uint32_t*)&h;
+}
+
+// 32 bytes at a multiple of 32
+__device__ __forceinline__ void store_sector(void* to, const uint32_t (&v)[16], int at) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(v[at]), "r"(v[at + 1]), "r"(v[at + 2]),
+               "r"(v[at + 3]), "r"(v[at + 4]), "r"(v[at + 5]), "r"(v[at + 6]), "r"(v[at + 7])
+               : "memory");
+}
+
+// 32 elements of each lane's row to `to` (NULL: none), of which the first `count` exist (the same in all lanes).  Rows that
+// start at any element are turned in shared memory, so that lanes write one row's elements.
+template <typename T>
+__device__ __forceinline__ void store_rows(T* to, const float (&v)[32], int count, bool whole, T* turn, int lane) {
+  uint32_t w[16];
+#pragma unroll
+  for (int j = 0; j < 16; j++) w[j] = pack2<T>(v[2 * j], v[2 * j + 1]);
+  if (whole && count >= 32) {
+    if (to) {
+      store_sector(to, w, 0);
+      store_sector(to + 16, w, 8);
+    }
+    return;
+  }
+  __syncwarp();
+#pragma unroll
+  for (int j = 0; j < 16; j++) ((uint32_t*)(turn + lane * kTurnRow))[j] = w[j];
+  __syncwarp();
+  for (int r = 0; r < 32; r++) {
+    T* row = (T*)__shfl_sync(~0u, (unsigned long long)to, r);
+    if (row && lane < count) row[lane] = turn[r * kTurnRow + lane];
+  }
+}
+
+__device__ __forceinline__ float sum32(const float (&v)[32]) {
+  float s[8];
+#pragma unroll
+  for (int j = 0; j < 8; j++) s[j] = (v[j] + v[j + 8]) + (v[j + 16] + v[j + 24]);
+  return ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]));
+}
+
+__device__ __forceinline__ float max32(const float (&v)[32]) {
+  float m = v[0];
+#pragma unroll
+  for (int j = 1; j < 32; j++) m = fmaxf(m, v[j]);
+  return m;
+}
+
+// Logits of one row, kRecCols columns from `sums`: the record, and with `probs` the exponentials.  z is only ever in registers.
+template <typename T, bool kProbs>
+__device__ __forceinline__ void logits_rows(const TileArgs& a, int n, uint32_t sums, int row, int col, int lane) {
+  const HeadPlan& p = a.p;
+  const bool real = row < n;
+  const int y = real ? p.tgt[row] - col : -1;
+  const float ref = kProbs && real ? p.ref[row] : 0.0f;
+  const float at = kProbs && real && a.pass.only_again ? p.at[row] : 0.0f;
+  float to = kProbs ? ref : kNoRef, s = 0.0f;
+#pragma unroll 1
+  for (int c = 0; c < kRecCols; c += 32) {
+    if (col + c >= p.lde) break;
+    float z[32];
+    sums_load(sums + c, z);
+    sums_loaded(z);
+    const int here = y - c;
+    if (col + c + 32 > p.V) {
+#pragma unroll
+      for (int j = 0; j < 32; j++)
+        if (col + c + j >= p.V) z[j] = -CUDART_INF_F;
+    }
+    float zt = 0.0f;
+    const bool target = here >= 0 && here < 32;
+    if (target) {
+#pragma unroll
+      for (int j = 0; j < 32; j++)
+        if (j == here) zt = z[j], z[j] = -CUDART_INF_F;
+      if (a.pass.sums) p.zt[row] = zt;
+    }
+    if (kProbs) {
+#pragma unroll
+      for (int j = 0; j < 32; j++) z[j] = ex2(fmaf(z[j], kLog2E, -ref));
+      s += sum32(z);
+      if (target) {
+        const float e = a.pass.only_again ? at : ex2(fmaf(zt, kLog2E, -ref));
+#pragma unroll
+        for (int j = 0; j < 32; j++)
+          if (j == here) z[j] = e;
+      }
+      if (row < up_div(n, kStepK) * kStepK) {
+        uint32_t w[16];
+#pragma unroll
+        for (int j = 0; j < 16; j++) w[j] = real ? pack2<T>(z[2 * j], z[2 * j + 1]) : 0u;
+        T* e = (T*)p.e + (long long)row * p.lde + col + c;
+        store_sector(e, w, 0);
+        store_sector(e + 16, w, 8);
+      }
+    } else {
+      const float top = whole_ref(max32(z));
+#pragma unroll
+      for (int j = 0; j < 32; j++) z[j] = ex2(fmaf(z[j], kLog2E, -top));
+      meet(to, s, top, sum32(z));
+    }
+  }
+  if (!a.pass.sums || col >= p.V) return;
+  // exponentials past the window: once more, relative to the largest
+  const bool past = kProbs && real && !(s <= 1.2e18f);
+  if (kProbs && __any_sync(~0u, past)) {
+    float to2 = kNoRef, s2 = 0.0f;
+#pragma unroll 1
+    for (int c = 0; c < kRecCols; c += 32) {
+      float z[32];
+      sums_load(sums + c, z);
+      sums_loaded(z);
+#pragma unroll
+      for (int j = 0; j < 32; j++)
+        if (col + c + j >= p.V || j == y - c) z[j] = -CUDART_INF_F;
+      const float top = whole_ref(max32(z));
+#pragma unroll
+      for (int j = 0; j < 32; j++) z[j] = ex2(fmaf(z[j], kLog2E, -top));
+      meet(to2, s2, top, sum32(z));
+    }
+    if (past) to = to2, s = s2;
+  }
+  if (real) p.rec[(long long)(col / kRecCols) * p.cap + row] = record(to, s);
+}
+
+template <typename T>
+__device__ __forceinline__ void store_part(float* part, const float (&v)[32]) {
+#pragma unroll
+  for (int j = 0; j < 32; j += 4) ((float4*)part)[j / 4] = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+}
+
+// Sums of a gradient's tile: kHalf columns of each lane's row
+template <typename T>
+__device__ __forceinline__ void grad_rows(const TileArgs& a, int n, const Task& t, uint32_t sums, int row, int col, T* turn,
+                                          int lane) {
+  const HeadPlan& p = a.p;
+  const GradSplit& sp = a.p.split;
+  const bool hidden = t.job == 0;
+  const bool parts = (hidden ? sp.hidden_parts : sp.head_parts) > 1;
+  const bool there = row < (hidden ? n : p.V);
+  T* to = nullptr;
+  float scale = 1.0f;
+  if (there && !parts) {
+    if (hidden) {
+      const long long r = a.out.r0 + p.src[row];
+      to = (T*)a.out.grad + (r / a.out.n) * a.out.stride_b + (r % a.out.n) * a.out.stride_n;
+      scale = p.coef[row];
+    } else {
+      to = (T*)a.grad_head + row * a.grad_head_stride;
+      scale = *p.post;
+    }
+  }
+  const bool whole = __all_sync(~0u, ((uintptr_t)(to + col) & 31) == 0 || !to);
+  float* part = hidden ? sp.hidden + ((long long)t.part * p.cap + row) * p.ldp : sp.head + ((long long)t.part * p.V + row) * p.ldp;
+  float* acc = p.acc + (long long)row * p.ldp;
+#pragma unroll 1
+  for (int c = col; c < col + kHalf && c < p.d; c += 32) {
+    float v[32];
+    if (t.steps > 0) {
+      sums_load(sums + (c - col), v);
+      sums_loaded(v);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 32; j++) v[j] = 0.0f;
+    }
+    if (parts) {
+      if (there) store_part<T>(part + c, v);
+      continue;
+    }
+#pragma unroll
+    for (int j = 0; j < 32; j++) v[j] *= scale;
+    if (!hidden && a.sum != kOnly && there) {
+      if (a.sum != kFirst) {
+#pragma unroll
+        for (int j = 0; j < 32; j++) v[j] += acc[c + j];
+      }
+      if (a.sum != kLast) store_part<T>(acc + c, v);
+    }
+    if (hidden || a.sum == kOnly || a.sum == kLast) store_rows<T>(to ? to + c : nullptr, v, p.d - c, whole, turn, lane);
+  }
+}
+
+// kForm 0: records; 1: exponentials (and records); 2: gradients
+template <typename T, int kForm>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+    k_head_tiles(const __grid_constant__ Maps maps, const __grid_constant__ TileArgs a) {
+  extern __shared__ uint8_t shared_raw[];
+  __shared__ Bars bars;
+  if (kForm != 2 && a.pass.only_again && *a.p.again == 0) return;
+  const int n = *a.p.count;
+  uint8_t* shared = (uint8_t*)(((uintptr_t)shared_raw + 1023) / 1024 * 1024);
+  const uint32_t stages = smem_address(shared);
+  T* turns = (T*)(shared + kStages * kStage);
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, pair = blockIdx.x / 2;
+  const uint32_t rank = cluster_rank();
+  const uint32_t full = smem_address(bars.full), empty = smem_address(bars.empty);
+  const uint32_t sums_full = smem_address(bars.sums_full), sums_empty = smem_address(bars.sums_empty);
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; s++) {
+      bar_init(full + 8 * s, 1);
+      bar_init(empty + 8 * s, 1);
+    }
+    for (int s = 0; s < 2; s++) {
+      bar_init(sums_full + 8 * s, 1);
+      bar_init(sums_empty + 8 * s, 2 * kWorkWarps);
+    }
+    bar_init_visible();
+  }
+  if (warp == 1) sums_take_pair(smem_address(&bars.sums));
+  products_fence_before();
   __syncthreads();
+  cluster_arrive();
+  cluster_wait();
+  products_fence_after();
+  const uint32_t sums = bars.sums;
+
+  auto task = [&](int i, Task& t) {
+    return kForm == 2 ? grads_task(a, n, pair, i, t) : logits_task(a, n, pair, i, t);
+  };
+  bool ok = true;
+  if (warp == 0) {
+    if (lane == 0) {  // copies
+      const uint32_t full0 = at_rank(full, 0);
+      int s = 0;
+      uint32_t turn = 0;
+      Task t;
+      for (int i = 0; ok && task(i, t); i++) {
+        const int m = t.m0 + rank * kHalf, c = t.n0 + rank * kHalf;
+        for (int k = t.k0; k < t.k0 + t.steps; k++) {
+          if (!(ok = bar_wait(empty + 8 * s, turn ^ 1))) break;
+          if (rank == 0) bar_expect(full + 8 * s, 2 * kStage);
+          const uint32_t A = stages + s * kStage, B = A + kOperand, bar = full0 + 8 * s;
+          if (kForm != 2) {
+            load_box_pair(&maps.hc, A, bar, k * kStepK, m);
+            load_box_pair(&maps.head_k, B, bar, k * kStepK, c);
+          } else if (t.job == 0) {
+            load_box_pair(&maps.e_k, A, bar, k * kStepK, m);
+            load_box_pair(&maps.head_mn, B, bar, c, k * kStepK);
+            load_box_pair(&maps.head_mn, B + kOperand / 2, bar, c + 64, k * kStepK);
+          } else {
+            load_box_pair(&maps.e_mn, A, bar, m, k * kStepK);
+            load_box_pair(&maps.e_mn, A + kOperand / 2, bar, m + 64, k * kStepK);
+            load_box_pair(&maps.hs, B, bar, c, k * kStepK);
+            load_box_pair(&maps.hs, B + kOperand / 2, bar, c + 64, k * kStepK);
+          }
+          if (++s == kStages) s = 0, turn ^= 1;
+        }
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0 && rank == 0) {  // products
+      int s = 0, use = 0;
+      uint32_t turn = 0;
+      Task t;
+      for (int i = 0; ok && task(i, t); i++) {
+        if (t.steps <= 0) continue;
+        const int half = use & 1;
+        if (!(ok = bar_wait(sums_empty + 8 * half, (use >> 1 & 1) ^ 1))) break;
+        products_fence_after();
+        const bool a_across = kForm == 2 && t.job == 1, b_across = kForm == 2;
+        const uint32_t kind = product_kind(a.bf16, a_across, b_across, kTile, kTile);
+        const uint32_t to = sums + half * kTile;
+        for (int k = 0; k < t.steps; k++) {
+          if (!(ok = bar_wait(full + 8 * s, turn))) break;
+          products_fence_after();
+          const uint32_t A = stages + s * kStage, B = A + kOperand;
+          const uint64_t da = a_across ? operand_mn(A) : operand_k(A), db = b_across ? operand_mn(B) : operand_k(B);
+          const uint32_t na = a_across ? kNextMN : kNextK, nb = b_across ? kNextMN : kNextK;
+#pragma unroll
+          for (int j = 0; j < kStepK / 16; j++) product_pair(to, da + j * na, db + j * nb, kind, k > 0 || j > 0);
+          products_arrive_pair(empty + 8 * s);
+          if (++s == kStages) s = 0, turn ^= 1;
+        }
+        if (!ok) break;
+        products_arrive_pair(sums_full + 8 * half);
+        use++;
+      }
+    }
+  } else if (warp >= 4) {
+    const int part = warp - 4, quarter = warp % 4;
+    T* turn = turns + part * 32 * kTurnRow;
+    int use = 0;
+    Task t;
+    for (int i = 0; task(i, t); i++) {
+      const int half = use & 1;
+      const int row = t.m0 + rank * kHalf + quarter * 32 + lane, off = part / 4 * kHalf;
+      const uint32_t from = sums + half * kTile + off + ((uint32_t)quarter * 32 << 16);
+      if (t.steps > 0) {
+        if (!(ok = bar_wait(sums_full + 8 * half, use >> 1 & 1))) break;
+        products_fence_after();
+      }
+      if (kForm == 2) {
+        grad_rows<T>(a, n, t, from, row, t.n0 + off, turn, lane);
+      } else if (row - lane < up_div(n, kStepK) * kStepK) {
+        logits_rows<T, kForm == 1>(a, n, from, row, t.n0 + off, lane);
+      }
+      if (t.steps > 0) {
+        products_fence_before();
+        __syncwarp();
+        if (lane == 0) bar_arrive_cluster(at_rank(sums_empty + 8 * half, 0));
+        use++;
+      }
+    }
+  }
+  if (!ok) {
+    *a.p.failed = 1;
+    let_copies_land();
+  }
+  products_fence_before();
+  __syncwarp();
+  __syncthreads();
+  cluster_arrive();
+  cluster_wait();
+  products_fence_after();
+  if (warp == 1) sums_free_pair(sums);
 }
 
+// Parts of a gradient's sums, in order
 template <typename T>
-__global__ void __launch_bounds__(256) k_head_logits(HeadPlan p, LogitsPass pass) {
-  __shared__ Tile t;
-  if (pass.only_again && *p.again == 0) return;
-  const int n = *p.count, m0 = blockIdx.y * kT, v0 = blockIdx.x * kT;
-  if (m0 >= (n + kRowTile - 1) / kRowTile * kRowTile) return;
-  const T* h = (const T*)p.hc;
-  const T* w = (const T*)p.head;
-  tile_product(t, p.d, [&](int k, int m) { return as_float(h[(m0 + m) * p.ldh + k]); },
-               [&](int k, int v) { return v0 + v < p.V ? as_float(w[(v0 + v) * p.ldw + k]) : 0.0f; });
-  if (threadIdx.x >= kT) return;
-  const int r = m0 + threadIdx.x, end = min(kT, p.V - v0);
-  const float* z = t.out[threadIdx.x];
-  const bool real = r < n;
-  const int y = real ? p.tgt[r] - v0 : -1;
-  const float ref = !real || !pass.probs ? 0.0f : p.ref[r];
-  if (pass.sums && real) {
-    float m = -CUDART_INF_F;
-    for (int j = 0; j < end; j++)
-      if (j != y) m = fmaxf(m, z[j]);
-    float to = whole_ref(m);
-    if (pass.probs && !(m * kLog2E > ref + kWindow)) to = ref;
-    float s = 0.0f;
-    for (int j = 0; j < end; j++)
-      if (j != y) s += ex2(fmaf(z[j], kLog2E, -to));
-    p.rec[(long long)blockIdx.x * p.cap + r] = record(to, s);
-    if (y >= 0 && y < end) p.zt[r] = z[y];
-  }
-  if (pass.probs) {
-    T* e = (T*)p.e + r * p.lde + v0;
-    for (int j = 0; j < kT && v0 + j < p.lde; j++) {
-      float v = real && j < end ? ex2(fmaf(z[j], kLog2E, -ref)) : 0.0f;
-      if (real && j == y) v = pass.only_again ? p.at[r] : v;
-      e[j] = of_float<T>(v);
+__global__ void __launch_bounds__(256) k_head_parts(const __grid_constant__ TileArgs a) {
+  const HeadPlan& p = a.p;
+  const GradSplit& sp = a.p.split;
+  const bool hidden = blockIdx.y == 0 && sp.hidden_parts > 1;
+  const int parts = hidden ? sp.hidden_parts : sp.head_parts, chunks = up_div(p.d, 4);
+  const long long rows = hidden ? *p.count : p.V, room = hidden ? p.cap : p.V;
+  const float* from = hidden ? sp.hidden : sp.head;
+  const float post = *p.post;
+  for (long long i = blockIdx.x * 256ll + threadIdx.x; i < rows * chunks; i += gridDim.x * 256ll) {
+    const long long row = i / chunks;
+    const int c = (int)(i % chunks) * 4;
+    float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int k = 0; k < parts; k++) {
+      const float4 v = *(const float4*)(from + (k * room + row) * p.ldp + c);
+      s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+    }
+    float v[4] = {s.x, s.y, s.z, s.w};
+    T* to;
+    if (hidden) {
+      const long long r = a.out.r0 + p.src[row];
+      to = (T*)a.out.grad + (r / a.out.n) * a.out.stride_b + (r % a.out.n) * a.out.stride_n;
+    } else {
+      to = (T*)a.grad_head + row * a.grad_head_stride;
+    }
+    const float scale = hidden ? p.coef[row] : post;
+    float* acc = p.acc + row * p.ldp + c;
+    for (int j = 0; j < 4 && c + j < p.d; j++) {
+      float x = v[j] * scale;
+      if (!hidden && (a.sum == kMiddle || a.sum == kLast)) x += acc[j];
+      if (!hidden && (a.sum == kFirst || a.sum == kMiddle)) acc[j] = x;
+      else to[c + j] = of_float<T>(x);
     }
   }
 }
 
-template <typename T>
-__global__ void __launch_bounds__(256) k_hidden_grad(HeadPlan p, HiddenGrad g) {
-  __shared__ Tile t;
-  const int n = *p.count, m0 = blockIdx.y * kT, c0 = blockIdx.x * kT;
-  if (m0 >= n) return;
-  const T* e = (const T*)p.e;
-  const T* w = (const T*)p.head;
-  tile_product(t, p.V, [&](int k, int m) { return as_float(e[(m0 + m) * p.lde + k]); },
-               [&](int k, int c) { return c0 + c < p.d ? as_float(w[k * p.ldw + c0 + c]) : 0.0f; });
-  for (int i = threadIdx.x; i < kT * kT; i += 256) {
-    const int m = i / kT, c = i % kT;
-    if (m0 + m >= n || c0 + c >= p.d) continue;
-    const long long r = g.r0 + p.src[m0 + m];
-    T* out = (T*)g.grad + (r / g.n) * g.stride_b + (r % g.n) * g.stride_n;
-    out[c0 + c] = of_float<T>(t.out[m][c] * p.coef[m0 + m]);
-  }
+// ---------------------------------------------------------------- host
+
+typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiled encode_tiled() {
+  static const EncodeTiled f = [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+        found != cudaDriverEntryPointSuccess)
+      return (EncodeTiled)nullptr;
+    return (EncodeTiled)p;
+  }();
+  return f;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(256) k_head_grad(HeadPlan p, T* grad, long long stride, HeadSum sum) {
-  __shared__ Tile t;
-  const int n = *p.count, v0 = blockIdx.x * kT, c0 = blockIdx.y * kT;
-  const T* e = (const T*)p.e;
-  const T* h = (const T*)p.hs;
-  tile_product(t, n, [&](int k, int v) { return v0 + v < p.V ? as_float(e[k * p.lde + v0 + v]) : 0.0f; },
-               [&](int k, int c) { return c0 + c < p.d ? as_float(h[k * p.ldh + c0 + c]) : 0.0f; });
-  const float post = *p.post;
-  for (int i = threadIdx.x; i < kT * kT; i += 256) {
-    const int v = i / kT, c = i % kT;
-    if (v0 + v >= p.V || c0 + c >= p.d) continue;
-    float x = t.out[v][c] * post;
-    float* acc = p.acc + (long long)(v0 + v) * p.d + c0 + c;
-    if (sum == kMiddle || sum == kLast) x += *acc;
-    if (sum == kFirst || sum == kMiddle) *acc = x;
-    else grad[(v0 + v) * stride + c0 + c] = of_float<T>(x);
-  }
+// [rows][cols] of 16-bit elements, `ld` apart: boxes of 64 columns and `box` rows
+bool make_map(CUtensorMap* map, int dtype, const void* base, long long cols, long long rows, long long ld, int box) {
+  const cuuint64_t size[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, stride[1] = {(cuuint64_t)ld * 2};
+  const cuuint32_t part[2] = {64, (cuuint32_t)box}, step[2] = {1, 1};
+  return encode_tiled()(map, dtype == EPIC_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2,
+                        (void*)base, size, stride, part, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 epic_status launched() { return cudaGetLastError() == cudaSuccess ? EPIC_OK : EPIC_ERR_CUDA; }
 
-unsigned tiles(long long n) { return (unsigned)((n + kT - 1) / kT); }
+template <typename T, int kForm>
+epic_status launch_tiles(const Maps& maps, const TileArgs& a, cudaStream_t st) {
+  if (cudaFuncSetAttribute(k_head_tiles<T, kForm>, cudaFuncAttributeMaxDynamicSharedMemorySize, kShared) != cudaSuccess)
+    return cudaGetLastError(), EPIC_ERR_CUDA;
+  k_head_tiles<T, kForm><<<2 * kPairs, kThreads, kShared, st>>>(maps, a);
+  return launched();
+}
 
 }  // namespace
 
+GradSplit split_grads(int rows, int d, int V) {
+  GradSplit s = {};
+  const long long ct = (d + kTile - 1) / kTile, mt = (rows + kTile - 1) / kTile, vt = (V + (long long)kTile - 1) / kTile;
+  const long long kv = (V + (long long)kStepK - 1) / kStepK, kr = (rows + kStepK - 1) / kStepK;
+  s.tile_cost = 4;
+  const long long all = mt * ct * (kv + s.tile_cost) + vt * ct * (kr + s.tile_cost), unit = std::max(8ll, all / (3 * kPairs));
+  s.hidden_parts = (int)std::min<long long>(kMostParts, (kv + unit - 1) / unit);
+  s.head_parts = (int)std::min<long long>(kMostParts, (kr + unit - 1) / unit);
+  return s;
+}
+
 epic_status launch_head_logits(const HeadPlan& p, int dtype, const LogitsPass& pass, cudaStream_t st) {
-  const dim3 grid(tiles(p.V), tiles(p.cap));
-  if (dtype == EPIC_F16) k_head_logits<__half><<<grid, 256, 0, st>>>(p, pass);
-  else k_head_logits<__nv_bfloat16><<<grid, 256, 0, st>>>(p, pass);
-  return launched();
+  if (!encode_tiled()) return EPIC_ERR_CUDA;
+  Maps maps = {};
+  TileArgs a = {};
+  a.p = p;
+  a.pass = pass;
+  a.bf16 = dtype == EPIC_BF16;
+  if (!make_map(&maps.hc, dtype, p.hc, p.ldh, p.cap, p.ldh, kHalf) ||
+      !make_map(&maps.head_k, dtype, p.head, p.d, p.V, p.ldw, kHalf))
+    return EPIC_ERR_CUDA;
+  if (pass.probs) return dtype == EPIC_F16 ? launch_tiles<__half, 1>(maps, a, st) : launch_tiles<__nv_bfloat16, 1>(maps, a, st);
+  return dtype == EPIC_F16 ? launch_tiles<__half, 0>(maps, a, st) : launch_tiles<__nv_bfloat16, 0>(maps, a, st);
 }
 
-epic_status launch_hidden_grad(const HeadPlan& p, int dtype, const HiddenGrad& out, cudaStream_t st) {
-  const dim3 grid(tiles(p.d), tiles(p.cap));
-  if (dtype == EPIC_F16) k_hidden_grad<__half><<<grid, 256, 0, st>>>(p, out);
-  else k_hidden_grad<__nv_bfloat16><<<grid, 256, 0, st>>>(p, out);
-  return launched();
-}
-
-epic_status launch_head_grad(const HeadPlan& p, int dtype, void* grad, long long stride, HeadSum sum, cudaStream_t st) {
-  const dim3 grid(tiles(p.V), tiles(p.d));
-  if (dtype == EPIC_F16) k_head_grad<__half><<<grid, 256, 0, st>>>(p, (__half*)grad, stride, sum);
-  else k_head_grad<__nv_bfloat16><<<grid, 256, 0, st>>>(p, (__nv_bfloat16*)grad, stride, sum);
+epic_status launch_head_grads(const HeadPlan& p, int dtype, const HiddenGrad& out, void* grad_head, long long stride,
+                              HeadSum sum, cudaStream_t st) {
+  if (!encode_tiled()) return EPIC_ERR_CUDA;
+  Maps maps = {};
+  TileArgs a = {};
+  a.p = p;
+  a.out = out;
+  a.grad_head = grad_head;
+  a.grad_head_stride = stride;
+  a.sum = sum;
+  a.bf16 = dtype == EPIC_BF16;
+  if (!out.grad) a.p.split.hidden_parts = 0;
+  if (!grad_head) a.p.split.head_parts = 0;
+  if (!make_map(&maps.hs, dtype, p.hs, p.ldh, p.cap, p.ldh, 64) || !make_map(&maps.e_k, dtype, p.e, p.lde, p.cap, p.lde, kHalf) ||
+      !make_map(&maps.e_mn, dtype, p.e, p.lde, p.cap, p.lde, 64) ||
+      !make_map(&maps.head_mn, dtype, p.head, p.d, p.V, p.ldw, 64))
+    return EPIC_ERR_CUDA;
+  const epic_status s = dtype == EPIC_F16 ? launch_tiles<__half, 2>(maps, a, st) : launch_tiles<__nv_bfloat16, 2>(maps, a, st);
+  if (s != EPIC_OK) return s;
+  const bool hidden = a.p.split.hidden_parts > 1, head = a.p.split.head_parts > 1;
+  if (!hidden && !head) return EPIC_OK;
+  const long long most = std::max(hidden ? (long long)p.rows : 0, head ? (long long)p.V : 0) * ((p.d + 3) / 4);
+  const dim3 grid((unsigned)std::min(1216ll, (most + 255) / 256), hidden && head ? 2 : 1);
+  if (dtype == EPIC_F16) k_head_parts<__half><<<grid, 256, 0, st>>>(a);
+  else k_head_parts<__nv_bfloat16><<<grid, 256, 0, st>>>(a);
   return launched();
 }
 

@@ -94,7 +94,7 @@ __global__ void __launch_bounds__(kRowsThreads) k_head_rows(RowsArgs a) {
   before = all = 0, top = 0.0f;
   for (int w = 0; w < warps; w++) before += s_before[w], all += s_all[w], top = fmaxf(top, s_top[w]);
   const float post = a.scaled ? pow2_above(top) * pow2_whole(-kHalfScale) : 1.0f;
-  if (blockIdx.x == 0 && threadIdx.x == 0) *p.count = all, *p.again = a.scaled, *p.post = post;
+  if (blockIdx.x == 0 && threadIdx.x == 0) *p.count = all, *p.failed = 0, *p.again = a.scaled, *p.post = post;
 
   for (int i0 = first; i0 < last; i0 += 32) {
     const long long mine = i0 + lane;
@@ -189,7 +189,7 @@ __global__ void __launch_bounds__(kMeetWarps * 32) k_head_meet(MeetArgs a) {
       const float zt = p.zt[q], by = s == 0.0f && zt > -CUDART_INF_F ? -CUDART_INF_F : log2f(s) + fmaf(-zt, kLog2E, ref);
       const float x = by * kLn2, rest = log1pf(expf(-fabsf(x)));
       float nll = x > 0.0f ? x + rest : rest;
-      if (!(zt < CUDART_INF_F) || s != s) nll = CUDART_NAN_F;
+      if (!(zt < CUDART_INF_F) || s != s || *p.failed) nll = CUDART_NAN_F;
       const float lse = x > 0.0f ? (ref + log2f(s)) * kLn2 + rest : zt + nll;
       const long long r = a.r0 + p.src[q];
       if (a.loss) a.loss[r] = (a.weight ? a.weight[r] : 1.0f) * nll;
@@ -218,6 +218,17 @@ __global__ void __launch_bounds__(kMeetWarps * 32) k_head_meet(MeetArgs a) {
     T* hs = (T*)p.hs + (q0 + j) * p.ldh;
     const float scale = s_scale[j];
     for (int k = lane; k < p.ldh; k += 32) hs[k] = of_float<T>(as_float(hc[k]) * scale);
+  }
+}
+
+// The head at rows of a multiple of 16 bytes, a warp a row
+template <typename T>
+__global__ void __launch_bounds__(256) k_head_pack(const T* head, long long stride, T* to, long long ld, int d, int V) {
+  const int lane = threadIdx.x % 32;
+  for (long long v = blockIdx.x * 8ll + threadIdx.x / 32; v < V; v += gridDim.x * 8ll) {
+    const T* w = head + v * stride;
+#pragma unroll 8
+    for (int k = lane; k < ld; k += 32) to[v * ld + k] = k < d ? w[k] : of_float<T>(0.0f);
   }
 }
 
@@ -256,16 +267,22 @@ bool bad_call(const HeadCall& c) {
 
 constexpr int kMostTokens = 0x7fffffff - 4096, kMostWidth = 1 << 20;
 
+// Boxes are copied from rows that start at multiples of 16 bytes; another head is laid out anew, in each call.
+bool head_lies_askew(const HeadCall& c, const HeadPlan& p) {
+  return (uintptr_t)c.head % 16 != 0 || p.ldw % 8 != 0 || p.ldw >= 1ll << 38;
+}
+
 // The plan of the first piece and the bytes that all pieces share
 size_t plan_head(const HeadCall& c, void* base, HeadPlan& p) {
   const long long rows = (long long)c.B * c.n;
   p = HeadPlan{};
   p.d = c.d;
   p.V = c.V;
-  p.ldw = c.head_stride;
+  p.ldw = c.V > 1 ? c.head_stride : (int64_t)round_up(c.d, 8);
   p.head = c.head;
   p.ldh = round_up(c.d, 8);
   p.lde = round_up(std::max(c.V, 1), 64);
+  p.ldp = round_up(c.d, 32);
   p.nrec = (c.V + kRecCols - 1) / kRecCols;
   size_t bytes = (size_t)2048 << 20;  // of exponentials
   if (const char* e = getenv("EPIC_HEAD_PIECE_MB")) bytes = strtoull(e, nullptr, 10) << 20;
@@ -275,6 +292,7 @@ size_t plan_head(const HeadCall& c, void* base, HeadPlan& p) {
   const size_t cap = p.cap;
   Carver w = {(char*)base, 0};
   w.take(p.count, 1, 4);
+  w.take(p.failed, 1, 4);
   w.take(p.again, 1, 4);
   w.take(p.post, 1, 4);
   w.take(p.src, cap, 4);
@@ -285,7 +303,16 @@ size_t plan_head(const HeadCall& c, void* base, HeadPlan& p) {
   w.take(p.rec, cap * p.nrec, sizeof(float2));
   if (c.form != kForward) {
     w.take(p.e, cap * p.lde, 2);
-    if (rows > p.cap) w.take(p.acc, (size_t)c.V * c.d, 4);
+    if (rows > p.cap) w.take(p.acc, (size_t)c.V * p.ldp, 4);
+    p.split = split_grads((int)std::min<long long>(rows, p.cap), c.d, c.V);
+    if (p.split.hidden_parts > 1) w.take(p.split.hidden, p.split.hidden_parts * cap * p.ldp, 4);
+    if (p.split.head_parts > 1) w.take(p.split.head, (size_t)p.split.head_parts * c.V * p.ldp, 4);
+  }
+  if (head_lies_askew(c, p)) {
+    void* packed;
+    w.take(packed, (size_t)c.V * p.ldh, 2);
+    p.head = packed;
+    p.ldw = p.ldh;
   }
   return w.used;
 }
@@ -324,6 +351,11 @@ epic_status run_head(const HeadCall& c, const HeadTensors& t, HeadPlan p, cudaSt
     }
     if (rows == 0) return EPIC_OK;
   }
+  if (c.V > 0 && p.head != c.head) {
+    k_head_pack<T><<<(unsigned)std::min(2432, (c.V + 7) / 8), 256, 0, st>>>((const T*)c.head, c.head_stride, (T*)p.head, p.ldw,
+                                                                        c.d, c.V);
+    EPIC_TRY(last_error());
+  }
   for (long long r0 = 0; r0 < rows; r0 += p.cap) {
     p.rows = (int)std::min<long long>(p.cap, rows - r0);
     RowsArgs a = {};
@@ -354,11 +386,10 @@ epic_status run_head(const HeadCall& c, const HeadTensors& t, HeadPlan p, cudaSt
     k_head_meet<T><<<(p.rows + kMeetRows - 1) / kMeetRows, kMeetWarps * 32, 0, st>>>(m);
     EPIC_TRY(last_error());
     if (grads && !known) EPIC_TRY(launch_head_logits(p, c.dtype, {false, true, true}, st));
-    if (t.grad_hidden) EPIC_TRY(launch_hidden_grad(p, c.dtype, a.out, st));
-    if (t.grad_head) {
+    if (t.grad_hidden || t.grad_head) {
       const bool first = r0 == 0, last = r0 + p.cap >= rows;
       const HeadSum sum = first ? (last ? kOnly : kFirst) : last ? kLast : kMiddle;
-      EPIC_TRY(launch_head_grad(p, c.dtype, t.grad_head, t.ghead_stride, sum, st));
+      EPIC_TRY(launch_head_grads(p, c.dtype, a.out, t.grad_head, t.ghead_stride, sum, st));
     }
   }
   return EPIC_OK;

@@ -9,7 +9,16 @@
 namespace epic {
 
 constexpr int kRowTile = 256;   // rows of a workspace come in whole tiles
-constexpr int kRecCols = 64;    // tokens whose exponentials one record sums
+constexpr int kRecCols = 128;   // tokens whose exponentials one record sums
+constexpr int kMostParts = 64;  // of a gradient's sum
+
+// Few tiles with long sums are cut into parts, whose sums meet in a second kernel: of gradients of hidden states over the
+// tokens, of the head's over the positions.  1: not cut; 0: no such gradient.
+struct GradSplit {
+  int hidden_parts, head_parts;
+  int tile_cost;        // what a tile costs beside its sum, in steps of it
+  float *hidden, *head; // [parts][cap][ldp], [parts][V][ldp]
+};
 
 // A piece: up to `cap` positions of the call.  Those that count stand in order, packed, in rows 0..*count-1 of the
 // workspace; rows from there to the end of the tile are zeros in hc, hs and e.
@@ -19,6 +28,7 @@ struct HeadPlan {
   long long ldh, lde, ldw;  // elements from row to row of hc and hs, of e, of the head
   const void* head;         // [V][ldw]
   int* count;               // rows that count
+  int* failed;              // != 0: a wait gave up
   int* again;               // != 0: rows whose exponentials left the window of their reference
   float* post;              // what gradients of the head are multiplied with at the end
   int* src;                 // [cap] position in the piece
@@ -31,7 +41,9 @@ struct HeadPlan {
   float2* rec;              // [nrec][cap] (whole reference, sum of exponentials relative to it), target left out
   void *hc, *hs;            // [cap][ldh] hidden states; the same times coef / *post
   void* e;                  // [cap][lde]
-  float* acc;               // [V][d] or NULL: gradient of the head so far, of calls in several pieces
+  float* acc;               // [V][ldp] or NULL: gradient of the head so far, of calls in several pieces
+  long long ldp;            // elements from row to row of acc and of parts, a multiple of 32
+  GradSplit split;
 };
 
 // How a piece's gradient of the head meets the pieces before it
@@ -50,9 +62,10 @@ struct LogitsPass {
   bool sums, probs, only_again;
 };
 epic_status launch_head_logits(const HeadPlan& p, int dtype, const LogitsPass& pass, cudaStream_t st);
-// grad[src] = coef e W
-epic_status launch_hidden_grad(const HeadPlan& p, int dtype, const HiddenGrad& out, cudaStream_t st);
-// grad [V][stride] = post e^T hs, with the pieces before
-epic_status launch_head_grad(const HeadPlan& p, int dtype, void* grad, long long stride, HeadSum sum, cudaStream_t st);
+// Gradients of hidden states, grad[src] = coef e W (out.grad NULL: none), and of the head, grad_head [V][stride] = post e^T hs
+// with the pieces before (NULL: none)
+epic_status launch_head_grads(const HeadPlan& p, int dtype, const HiddenGrad& out, void* grad_head, long long stride,
+                              HeadSum sum, cudaStream_t st);
+GradSplit split_grads(int rows, int d, int V);
 
 }  // namespace epic

@@ -1,0 +1,153 @@
+// Tensor-core tiles of two CTAs: barriers in shared memory, copies of boxes of
+// tensors (TMA), products into tensor memory (tcgen05), for kernels that compute
+// tiles of 256 x 256 by pairs of CTAs.
+//
+// Every wait gives up after kWaitCycles (some 4 s); a kernel whose wait gave up notes it,
+// leaves its loops, lets its copies land and frees its tensor memory.
+#pragma once
+#include <cuda.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+namespace epic {
+namespace {
+
+constexpr long long kWaitCycles = 1ll << 33;
+
+__device__ __forceinline__ uint32_t smem_address(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+// the same place in the shared memory of the cluster's CTA `rank`
+__device__ __forceinline__ uint32_t at_rank(uint32_t addr, uint32_t rank) {
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
+__device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void bar_init_visible() { asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory"); }
+__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void bar_arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+// of a barrier in any CTA of the cluster
+__device__ __forceinline__ void bar_arrive_cluster(uint32_t bar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
+  uint32_t done;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(done)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return done;
+}
+// false: gave up
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {
+  if (bar_try(bar, parity)) return true;
+  const long long t = clock64();
+  while (!bar_try(bar, parity))
+    if (clock64() - t > kWaitCycles) return false;
+  return true;
+}
+
+// A box of a tensor in two dimensions at (x, y) into this CTA's shared memory; its bytes are counted at `bar`, which may be
+// the pair's other CTA's.
+__device__ __forceinline__ void load_box_pair(const CUtensorMap* map, uint32_t dst, uint32_t bar, int x, int y) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::
+          "r"(dst),
+      "l"(map), "r"(bar), "r"(x), "r"(y)
+      : "memory");
+}
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* map) {
+  asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
+}
+
+// ---- operands in shared memory: rows of 128 bytes, their chunks of 16 swizzled by the row's number in 8
+
+constexpr uint64_t kSwizzle128 = (uint64_t)2 << 61 | (uint64_t)1 << 46;
+// [rows][64 elements] along the product's sum: the next 8 rows are 1,024 bytes on; 16 elements of the sum, 32 bytes
+__device__ __forceinline__ uint64_t operand_k(uint32_t addr) {
+  return kSwizzle128 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 16 | (addr >> 4 & 0x3fff);
+}
+constexpr uint32_t kNextK = 32 >> 4;
+// [64 of the sum][64 elements] blocks across the sum: the next 8 of the sum are 1,024 bytes on, the next block 8,192; 16 of
+// the sum, 2,048 bytes
+__device__ __forceinline__ uint64_t operand_mn(uint32_t addr) {
+  return kSwizzle128 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)(8192 >> 4) << 16 | (addr >> 4 & 0x3fff);
+}
+constexpr uint32_t kNextMN = 2048 >> 4;
+
+// What a product is: 16-bit operands (bf16 or fp16) along or across the sum, 32-bit sums, m x n
+__host__ __device__ constexpr uint32_t product_kind(bool bf16, bool a_across, bool b_across, int m, int n) {
+  return 1u << 4 | (bf16 ? 1u << 7 | 1u << 10 : 0u) | (a_across ? 1u << 15 : 0u) | (b_across ? 1u << 16 : 0u) |
+         (uint32_t)(n >> 3) << 17 | (uint32_t)(m >> 4) << 24;
+}
+
+__device__ __forceinline__ void product_pair(uint32_t sums, uint64_t a, uint64_t b, uint32_t kind, bool add) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(sums),
+      "l"(a), "l"(b), "r"(kind), "r"((uint32_t)add)
+      : "memory");
+}
+// an arrival at that barrier of both CTAs once all products so far are done
+__device__ __forceinline__ void products_arrive_pair(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
+               "h"((uint16_t)3)
+               : "memory");
+}
+
+// all of tensor memory, by one warp of each CTA of the pair
+__device__ __forceinline__ void sums_take_pair(uint32_t dst) {
+  asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(dst) : "memory");
+  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void sums_free_pair(uint32_t sums) {
+  asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(sums) : "memory");
+}
+__device__ __forceinline__ void products_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void products_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+// 32 columns of the warp's 32 rows, a lane a row; there after sums_loaded(v)
+__device__ __forceinline__ void sums_load(uint32_t sums, float (&v)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]),
+        "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]),
+        "=f"(v[16]), "=f"(v[17]), "=f"(v[18]), "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]),
+        "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31])
+      : "r"(sums));
+}
+__device__ __forceinline__ void sums_loaded(float (&v)[32]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+      : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]),
+        "+f"(v[8]), "+f"(v[9]), "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15]),
+        "+f"(v[16]), "+f"(v[17]), "+f"(v[18]), "+f"(v[19]), "+f"(v[20]), "+f"(v[21]), "+f"(v[22]), "+f"(v[23]),
+        "+f"(v[24]), "+f"(v[25]), "+f"(v[26]), "+f"(v[27]), "+f"(v[28]), "+f"(v[29]), "+f"(v[30]), "+f"(v[31])
+      :: "memory");
+}
+
+// a microsecond's worth of waiting for copies in flight, many times over: after a wait that gave up
+__device__ __noinline__ void let_copies_land() {
+  for (int i = 0; i < 2000; i++) __nanosleep(1000);
+}
+
+}  // namespace
+}  // namespace epic
