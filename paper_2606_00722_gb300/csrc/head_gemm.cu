@@ -461,31 +461,6 @@ __global__ void __launch_bounds__(256) k_head_parts(const __grid_constant__ Tile
 
 // ---------------------------------------------------------------- host
 
-typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                                const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiled encode_tiled() {
-  static const EncodeTiled f = [] {
-    void* p = nullptr;
-    cudaDriverEntryPointQueryResult found;
-    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) != cudaSuccess ||
-        found != cudaDriverEntryPointSuccess)
-      return (EncodeTiled)nullptr;
-    return (EncodeTiled)p;
-  }();
-  return f;
-}
-
-// [rows][cols] of 16-bit elements, `ld` apart: boxes of 64 columns and `box` rows
-bool make_map(CUtensorMap* map, int dtype, const void* base, long long cols, long long rows, long long ld, int box) {
-  const cuuint64_t size[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, stride[1] = {(cuuint64_t)ld * 2};
-  const cuuint32_t part[2] = {64, (cuuint32_t)box}, step[2] = {1, 1};
-  return encode_tiled()(map, dtype == EPIC_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2,
-                        (void*)base, size, stride, part, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 epic_status launched() { return cudaGetLastError() == cudaSuccess ? EPIC_OK : EPIC_ERR_CUDA; }
 
 template <typename T, int kForm>
@@ -510,14 +485,13 @@ GradSplit split_grads(int rows, int d, int V) {
 }
 
 epic_status launch_head_logits(const HeadPlan& p, int dtype, const LogitsPass& pass, cudaStream_t st) {
-  if (!encode_tiled()) return EPIC_ERR_CUDA;
   Maps maps = {};
   TileArgs a = {};
   a.p = p;
   a.pass = pass;
   a.bf16 = dtype == EPIC_BF16;
-  if (!make_map(&maps.hc, dtype, p.hc, p.ldh, p.cap, p.ldh, kHalf) ||
-      !make_map(&maps.head_k, dtype, p.head, p.d, p.V, p.ldw, kHalf))
+  if (!make_map(&maps.hc, a.bf16, p.hc, p.ldh, p.cap, p.ldh, kHalf) ||
+      !make_map(&maps.head_k, a.bf16, p.head, p.d, p.V, p.ldw, kHalf))
     return EPIC_ERR_CUDA;
   if (pass.probs) return dtype == EPIC_F16 ? launch_tiles<__half, 1>(maps, a, st) : launch_tiles<__nv_bfloat16, 1>(maps, a, st);
   return dtype == EPIC_F16 ? launch_tiles<__half, 0>(maps, a, st) : launch_tiles<__nv_bfloat16, 0>(maps, a, st);
@@ -525,7 +499,6 @@ epic_status launch_head_logits(const HeadPlan& p, int dtype, const LogitsPass& p
 
 epic_status launch_head_grads(const HeadPlan& p, int dtype, const HiddenGrad& out, void* grad_head, long long stride,
                               HeadSum sum, cudaStream_t st) {
-  if (!encode_tiled()) return EPIC_ERR_CUDA;
   Maps maps = {};
   TileArgs a = {};
   a.p = p;
@@ -536,9 +509,9 @@ epic_status launch_head_grads(const HeadPlan& p, int dtype, const HiddenGrad& ou
   a.bf16 = dtype == EPIC_BF16;
   if (!out.grad) a.p.split.hidden_parts = 0;
   if (!grad_head) a.p.split.head_parts = 0;
-  if (!make_map(&maps.hs, dtype, p.hs, p.ldh, p.cap, p.ldh, 64) || !make_map(&maps.e_k, dtype, p.e, p.lde, p.cap, p.lde, kHalf) ||
-      !make_map(&maps.e_mn, dtype, p.e, p.lde, p.cap, p.lde, 64) ||
-      !make_map(&maps.head_mn, dtype, p.head, p.d, p.V, p.ldw, 64))
+  if (!make_map(&maps.hs, a.bf16, p.hs, p.ldh, p.cap, p.ldh, 64) || !make_map(&maps.e_k, a.bf16, p.e, p.lde, p.cap, p.lde, kHalf) ||
+      !make_map(&maps.e_mn, a.bf16, p.e, p.lde, p.cap, p.lde, 64) ||
+      !make_map(&maps.head_mn, a.bf16, p.head, p.d, p.V, p.ldw, 64))
     return EPIC_ERR_CUDA;
   const epic_status s = dtype == EPIC_F16 ? launch_tiles<__half, 2>(maps, a, st) : launch_tiles<__nv_bfloat16, 2>(maps, a, st);
   if (s != EPIC_OK) return s;
