@@ -25,10 +25,32 @@ struct QuantArgs {
 
 constexpr int kQuantThreads = 256;
 
+// 16 bytes of a row as numbers of 32 bits
+template <typename T>
+struct Chunk {
+  static constexpr int kCount = 16 / sizeof(T);
+  float v[kCount];
+  __device__ __forceinline__ Chunk(const T* x, int count, bool whole) {
+    if (whole && count >= kCount) {
+      const uint4 w = *(const uint4*)x;
+      const T* t = (const T*)&w;
+#pragma unroll
+      for (int i = 0; i < kCount; i++) v[i] = as_float(t[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kCount; i++) v[i] = i < count ? as_float(x[i]) : 0.0f;
+    }
+  }
+};
+
+// |v| as a whole number of the same order, NaN above infinity
+__device__ __forceinline__ uint32_t size_order(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+
 // A CTA a row: the largest size in one pass, the quotients in a second one, from the caches.
 template <typename T>
 __global__ void __launch_bounds__(kQuantThreads) k_quantize_rows(QuantArgs a) {
-  __shared__ float s_top[kQuantThreads / 32];
+  constexpr int E = Chunk<T>::kCount;
+  __shared__ uint32_t s_top[kQuantThreads / 32];
   const long long r = blockIdx.x, b = r / a.k;
   const int at = a.pos ? a.pos[r] : (int)(r % a.k);
   int8_t* q = a.q + r * a.d;
@@ -38,25 +60,39 @@ __global__ void __launch_bounds__(kQuantThreads) k_quantize_rows(QuantArgs a) {
     return;
   }
   const T* x = (const T*)a.x + b * a.stride_b + at * a.stride_n;
-  float top = 0.0f;
-  for (int k = threadIdx.x; k < a.d; k += kQuantThreads) {
-    const float v = fabsf(as_float(x[k]));
-    top = v <= top ? top : v;  // a NaN stays
-    if (v != v) break;
+  const bool whole = (uintptr_t)x % 16 == 0, words = (uintptr_t)q % 4 == 0;
+  uint32_t top = 0;
+#pragma unroll 2
+  for (int k = threadIdx.x * E; k < a.d; k += kQuantThreads * E) {
+    const Chunk<T> c(x + k, a.d - k, whole);
+#pragma unroll
+    for (int i = 0; i < E; i++) top = max(top, size_order(c.v[i]));
   }
-  for (int o = 16; o; o >>= 1) {
-    const float v = __shfl_xor_sync(~0u, top, o);
-    top = v <= top || top != top ? top : v;
-  }
+  top = __reduce_max_sync(~0u, top);
   if (threadIdx.x % 32 == 0) s_top[threadIdx.x / 32] = top;
   __syncthreads();
-  top = s_top[0];
-  for (int w = 1; w < kQuantThreads / 32; w++) top = s_top[w] <= top || top != top ? top : s_top[w];
-  const float s = __fdiv_rn(top, 127.0f);
+  for (int w = 0; w < kQuantThreads / 32; w++) top = max(top, s_top[w]);
+  const float s = __fdiv_rn(__uint_as_float(top), 127.0f);
   if (threadIdx.x == 0) a.scale[r] = s;
-  for (int k = threadIdx.x; k < a.d; k += kQuantThreads) {
-    const float v = rintf(__fdiv_rn(as_float(x[k]), s));
-    q[k] = s > 0.0f && v == v ? (int8_t)fminf(fmaxf(v, -127.0f), 127.0f) : 0;
+#pragma unroll 2
+  for (int k = threadIdx.x * E; k < a.d; k += kQuantThreads * E) {
+    const Chunk<T> c(x + k, a.d - k, whole);
+    uint32_t w[E / 4] = {};
+#pragma unroll
+    for (int i = 0; i < E; i++) {
+      const float v = rintf(__fdiv_rn(c.v[i], s));
+      const int n = s > 0.0f && v == v ? (int)fminf(fmaxf(v, -127.0f), 127.0f) : 0;
+      w[i / 4] |= (uint32_t)(n & 255) << i % 4 * 8;
+    }
+#pragma unroll
+    for (int i = 0; i < E; i += 4) {
+      if (words && k + i + 4 <= a.d) {
+        *(uint32_t*)(q + k + i) = w[i / 4];
+      } else {
+        for (int j = 0; j < 4; j++)
+          if (k + i + j < a.d) q[k + i + j] = (int8_t)(w[i / 4] >> j * 8);
+      }
+    }
   }
 }
 
@@ -145,30 +181,34 @@ __global__ void __launch_bounds__(kFewThreads) k_few_logits(Int8Args a) {
 //
 // This GPU's tensor units have no fast products of 8-bit integers, but a product of two of them in fp16 is exact, and so are
 // sums in 32-bit floats while they stay below 2^24, which 1,024 products do; they are then taken over into 32-bit
-// integers.  A pair of CTAs makes 256 tokens x up to 256 rows.  The head's bytes come through a queue of copies that each
-// thread keeps for itself; the thread turns them into fp16 (byte + 128 in the low bits of 1024.0, less 1152) in the
-// operand's place.  Hidden states are turned once, in the workspace, and come by boxes.
-
+// integers.  A pair of CTAs makes 256 tokens x up to 256 rows.  The head's bytes come into a queue in shared memory, by boxes
+// or, where rows start anywhere, row by row with the aligned 16 bytes that they begin and end in; the work warps turn them
+// into fp16 (byte + 128 in the low bits of 1024.0, less 1152) in tensor memory, where the tensor units take them from.
+// Hidden states are turned once, in the workspace, and come by boxes.  Each of four teams of four warps turns every fourth
+// step, so that four chains of loads, stores and arrivals overlap.
+//
+// What was tried before: copies of the work warps' own (cp.async), which every fence between what a warp writes and the tensor
+// units waits for, 1.5 us a step; arrivals released to the whole cluster, 1.3 us; one chain, 0.6 us; the turned operand in
+// shared memory, where it is written and read on top of the queue and the hidden states, 80 KB a step, 0.41 us.
 constexpr int kWorkWarps = 16, kWork = 32 * kWorkWarps, kThreads = kWork + 128;
-constexpr int kTileTokens = 256, kHalf = 128, kStepK = 64, kRing = 4, kExactSteps = 1024 / kStepK;
-constexpr int kOperandA = kHalf * kStepK * 2, kOperandB = kHalf * kStepK * 2;
-constexpr int kQueue = 8, kQueueBytes = kQueue * kWork * 16;  // askew: half as many steps of twice the bytes
-constexpr int kShared = kRing * (kOperandA + kOperandB) + kQueueBytes + 1024;
+constexpr int kTileTokens = 256, kHalf = 128, kStepK = 64, kRing = 8, kTeams = 4, kExactSteps = 1024 / kStepK;
+constexpr int kTeam = kWorkWarps / kTeams;  // warps
+constexpr int kOperand = kHalf * kStepK * 2;  // bytes of a step of hidden states
+// A unit of the queue: 64 bytes of each token by a box, or 256 and up to 16 more by a copy a row
+template <bool kAskew>
+struct Queue {
+  static constexpr int kSteps = kAskew ? 4 : 1, kRow = kSteps * kStepK + (kAskew ? 16 : 0), kUnit = kHalf * kRow;
+  static constexpr int kUnits = kAskew ? 2 : 10;
+  static constexpr int kWarps = kSteps * kTeam;  // that read a unit
+};
+constexpr int kShared = kRing * kOperand + 10 * kHalf * kStepK + 1024;
+static_assert(2 * Queue<true>::kUnit <= 10 * kHalf * kStepK, "the queue of either form has its place");
 constexpr int kPairs = 76;
 
 struct Int8Bars {
-  uint64_t full[kRing], empty[kRing], sums_full[2], sums_empty[2];
+  uint64_t full[kRing], empty[kRing], sums_full[2], sums_empty[2], come[10], gone[10];
   uint32_t sums;
 };
-
-__device__ __forceinline__ void copy16(uint32_t to, const void* from, int bytes) {
-  asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void copies_wait() {
-  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
-}
 
 // four bytes as four numbers of fp16
 __device__ __forceinline__ uint2 halves_of(uint32_t w) {
@@ -184,27 +224,41 @@ __device__ __forceinline__ uint4 load_shared(uint32_t at) {
   asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
   return v;
 }
-__device__ __forceinline__ void store_shared(uint32_t at, uint2 a, uint2 b) {
-  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a.x), "r"(a.y), "r"(b.x), "r"(b.y) : "memory");
+// 16 bytes from byte m of two times 16 on
+__device__ __forceinline__ uint4 shifted(uint4 a, uint4 b, uint32_t m) {
+  uint32_t x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+  for (int c = 0; c < 6; c++) x[c] = m & 8 ? x[c + 2] : x[c];
+#pragma unroll
+  for (int c = 0; c < 5; c++) x[c] = m & 4 ? x[c + 1] : x[c];
+  const int by = (m & 3) * 8;
+  return make_uint4(__funnelshift_r(x[0], x[1], by), __funnelshift_r(x[1], x[2], by), __funnelshift_r(x[2], x[3], by),
+                    __funnelshift_r(x[3], x[4], by));
 }
 
-// kRows: rows of a tile.  kAskew: rows of the head start anywhere; a thread copies the two aligned chunks of 16 that its 16
-// bytes lie in (the first may begin up to 15 bytes ahead of the row, within its aligned 16).
+// kRows: rows of a tile.  kAskew: rows of the head start anywhere.
 template <typename T, int kRows, bool kAskew>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
-    k_int8_tiles(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ Int8Args a) {
+    k_int8_tiles(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap head_map,
+                 const __grid_constant__ Int8Args a) {
+  typedef Queue<kAskew> Q;
   extern __shared__ uint8_t shared_raw[];
   __shared__ Int8Bars bars;
   const uint32_t ring = (smem_address(shared_raw) + 1023) / 1024 * 1024;
-  const uint32_t queue = ring + kRing * (kOperandA + kOperandB);
+  const uint32_t queue = ring + kRing * kOperand;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, pair = blockIdx.x / 2;
   const uint32_t rank = cluster_rank();
   const uint32_t full = smem_address(bars.full), empty = smem_address(bars.empty);
   const uint32_t sums_full = smem_address(bars.sums_full), sums_empty = smem_address(bars.sums_empty);
+  const uint32_t come = smem_address(bars.come), gone = smem_address(bars.gone);
   if (threadIdx.x == 0) {
     for (int s = 0; s < kRing; s++) {
-      bar_init(full + 8 * s, 1 + 2 * kWorkWarps);
+      bar_init(full + 8 * s, 1 + 2 * kTeam);
       bar_init(empty + 8 * s, 1);
+    }
+    for (int s = 0; s < Q::kUnits; s++) {
+      bar_init(come + 8 * s, kAskew ? 32 : 1);
+      bar_init(gone + 8 * s, Q::kWarps);
     }
     for (int s = 0; s < 2; s++) {
       bar_init(sums_full + 8 * s, 1);
@@ -222,6 +276,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   const int row_tiles = (a.rows + kRows - 1) / kRows, steps = (a.d + kStepK - 1) / kStepK;
   const int tiles = (int)((a.V + (long long)kTileTokens - 1) / kTileTokens) * row_tiles;
   constexpr int kBoxBytes = kRows / 2 * kStepK * 2;
+  // tensor memory: sums, twice if they leave room for the operand's ring in the last 256 columns
+  constexpr int kSums = kRows == 256 ? 1 : 2;
+  const uint32_t operands = sums + 256;
   bool ok = true;
 
   // Of 96 registers a thread that a block of 256 rows is launched with, 61,440, the four warpgroups that hold sums take 112
@@ -237,8 +294,41 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         for (int k = 0; k < steps; k++) {
           if (!(ok = bar_wait(empty + 8 * s, turn ^ 1))) break;
           if (rank == 0) bar_expect(full + 8 * s, 2 * kBoxBytes);
-          load_box_pair(&q_map, ring + s * (kOperandA + kOperandB) + kOperandA, full0 + 8 * s, k * kStepK, r0);
+          load_box_pair(&q_map, ring + s * kOperand, full0 + 8 * s, k * kStepK, r0);
           if (++s == kRing) s = 0, turn ^= 1;
+        }
+      }
+    }
+    if (warp == kWorkWarps + 2 && (kAskew || lane == 0)) {  // the head's bytes
+      int s = 0;
+      uint32_t turn = 0;
+      for (int t = pair; ok && t < tiles; t += kPairs) {
+        const long long v0 = (long long)(t / row_tiles) * kTileTokens + rank * kHalf;
+        for (int k = 0; k < steps; k += Q::kSteps) {
+          if (!(ok = bar_wait(gone + 8 * s, turn ^ 1))) break;
+          const uint32_t to = queue + s * Q::kUnit, bar = come + 8 * s;
+          if (!kAskew) {
+            bar_expect(bar, Q::kUnit);
+            load_box(&head_map, to, bar, k * kStepK, (int)v0);
+          } else {
+            // from the aligned 16 bytes that the part begins in to those that it ends in; a barrier counts what comes
+            uint32_t bytes[kHalf / 32], all = 0;
+            const int part = min(a.d - k * kStepK, Q::kSteps * kStepK);
+#pragma unroll
+            for (int i = 0; i < kHalf / 32; i++) {
+              const long long v = v0 + i * 32 + lane;
+              const int m = (int)((uintptr_t)(a.head + v * a.head_stride) & 15);
+              bytes[i] = v < a.V ? (m + part + 15) / 16 * 16 : 0;
+              all += bytes[i];
+            }
+            bar_expect(bar, all);
+#pragma unroll
+            for (int i = 0; i < kHalf / 32; i++) {
+              const int8_t* w = a.head + (v0 + i * 32 + lane) * a.head_stride + k * kStepK;
+              if (bytes[i]) load_run(to + (i * 32 + lane) * Q::kRow, (const void*)((uintptr_t)w & ~(uintptr_t)15), bytes[i], bar);
+            }
+          }
+          if (++s == Q::kUnits) s = 0, turn ^= 1;
         }
       }
     }
@@ -248,17 +338,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       uint32_t turn = 0;
       for (int t = pair; ok && t < tiles; t += kPairs) {
         for (int k = 0; ok && k < steps; use++) {
-          const int half = use & 1, end = min(k + kExactSteps, steps);
-          if (!(ok = bar_wait(sums_empty + 8 * half, (use >> 1 & 1) ^ 1))) break;
+          const int half = use % kSums, end = min(k + kExactSteps, steps);
+          if (!(ok = bar_wait(sums_empty + 8 * half, (use / kSums & 1) ^ 1))) break;
           products_fence_after();
           for (bool add = false; k < end; k++) {
             if (!(ok = bar_wait(full + 8 * s, turn))) break;
             products_fence_after();
-            const uint32_t A = ring + s * (kOperandA + kOperandB);
-            const uint64_t da = operand_k(A), db = operand_k(A + kOperandA);
+            const uint64_t b = operand_k(ring + s * kOperand);
 #pragma unroll
             for (int j = 0; j < kStepK / 16; j++, add = true)
-              product_pair(sums + half * 256, da + j * kNextK, db + j * kNextK, kind, add);
+              product_pair_in(sums + half * kRows, operands + s * 32 + j * 8, b + j * kNextK, kind, add);
             products_arrive_pair(empty + 8 * s);
             if (++s == kRing) s = 0, turn ^= 1;
           }
@@ -270,46 +359,23 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     if (kRows == 256) asm volatile("setmaxnreg.inc.sync.aligned.u32 112;");
     constexpr int kCols = kRows / 4;               // a warp's rows of logits
     constexpr int kLoad = kCols < 16 ? kCols : 16;  // at a time
-    constexpr int kDepth = kAskew ? kQueue / 2 : kQueue;
-    const int tid = threadIdx.x, token = tid / 4, j = tid % 4, quarter = warp % 4, group = warp / 4;
-    const uint32_t slot = queue + tid * 16;
-    const uint32_t place = token * 128, c0 = ((2 * j) ^ (token & 7)) * 16, c1 = ((2 * j + 1) ^ (token & 7)) * 16;
+    const int quarter = warp % 4, team = warp / 4, token = quarter * 32 + lane;  // of the CTA's
     const uint32_t full0 = at_rank(full, 0), sums_empty0 = at_rank(sums_empty, 0);
-    const uint32_t from = sums + group * kCols + ((uint32_t)quarter * 32 << 16);
+    const uint32_t lanes = (uint32_t)quarter * 32 << 16, from = sums + lanes + team * kCols;
+    const int own = (tiles - pair + kPairs - 1) / kPairs, per = (steps + kExactSteps - 1) / kExactSteps;  // tiles, takes each
     int acc[kCols];
 #pragma unroll
     for (int i = 0; i < kCols; i++) acc[i] = 0;
 
-    int ahead_t = pair, ahead_k = 0, ahead_s = 0;  // the next copy
-    auto copy = [&] {
-      if (ahead_t < tiles) {
-        const long long v = (long long)(ahead_t / row_tiles) * kTileTokens + rank * kHalf + token;
-        const int k = ahead_k * kStepK + j * 16, left = v < a.V ? a.d - k : 0;
-        const int8_t* w = left > 0 ? a.head + v * a.head_stride + k : a.head;
-        const uint32_t to = slot + ahead_s * (kAskew ? 2 : 1) * kWork * 16;
-        if (!kAskew) {
-          copy16(to, w, max(0, min(left, 16)));
-        } else {
-          const int m = (int)((uintptr_t)w & 15);
-          w -= m;
-          copy16(to, w, left > 0 ? min(left + m, 16) : 0);
-          copy16(to + kWork * 16, left + m > 16 ? w + 16 : w, left > 0 ? max(0, min(left + m - 16, 16)) : 0);
-        }
-        if (++ahead_s == kDepth) ahead_s = 0;
-        if (++ahead_k == steps) ahead_k = 0, ahead_t += kPairs;
-      }
-      copies_commit();
-    };
-    int use = 0, waiting = -1, since = 0;  // sums that are taken over next: of tile `waiting`, its last if `whole`
-    bool whole = false;
+    int use = 0, past = min(kExactSteps, steps);  // the next sums to take over, and the step past them
     auto take = [&] {
-      const int half = use & 1;
-      if (!(ok = bar_wait(sums_full + 8 * half, use >> 1 & 1))) return;
+      const int half = use % kSums;
+      if (!(ok = bar_wait(sums_full + 8 * half, use / kSums & 1))) return;
       products_fence_after();
 #pragma unroll
       for (int c = 0; c < kCols; c += kLoad) {
         float v[kLoad];
-        sums_load(from + half * 256 + c, v);
+        sums_load(from + half * kRows + c, v);
         sums_loaded(v);
 #pragma unroll
         for (int i = 0; i < kLoad; i++) acc[c + i] += __float2int_rn(v[i]);
@@ -317,72 +383,73 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       products_fence_before();
       __syncwarp();
       if (lane == 0) bar_arrive_cluster(sums_empty0 + 8 * half);
-      use++;
-      if (whole) {
-        const int r0 = waiting % row_tiles * kRows + group * kCols;
-        const long long v = (long long)(waiting / row_tiles) * kTileTokens + rank * kHalf + quarter * 32 + lane;
-        if (v < a.V) {
-          const float S = a.head_scale[v];
-          int b = r0 / a.k, i = r0 % a.k;
-          T* z = (T*)a.logits + b * a.stride_b + i * a.stride_n + v;
+      const int tile = use / per, t = pair + tile * kPairs;
+      if (++use % per == 0) {
+        past = (tile + 1) * steps;
+        const int r0 = t % row_tiles * kRows + team * kCols;
+        const long long v = (long long)(t / row_tiles) * kTileTokens + rank * kHalf + token;
+        const float S = v < a.V ? a.head_scale[v] : 0.0f;
+        int b = r0 / a.k, i = r0 % a.k;
+        T* z = (T*)a.logits + b * a.stride_b + i * a.stride_n + v;
+        float s = 0.0f;  // a lane a row
 #pragma unroll
-          for (int c = 0; c < kCols; c++) {
-            if (r0 + c < a.rows) *z = of_float<T>((float)acc[c] * a.scale[r0 + c] * S);
-            z += a.stride_n;
-            if (++i == a.k) i = 0, b++, z = (T*)a.logits + b * a.stride_b + v;
-          }
+        for (int c = 0; c < kCols; c++) {
+          if (c % 32 == 0) s = r0 + c + lane < a.rows ? a.scale[r0 + c + lane] : 0.0f;
+          const float x = (float)acc[c] * __shfl_sync(~0u, s, c % 32) * S;
+          if (r0 + c < a.rows && v < a.V) *z = of_float<T>(x);
+          z += a.stride_n;
+          if (++i == a.k) i = 0, b++, z = (T*)a.logits + b * a.stride_b + v;
         }
 #pragma unroll
         for (int i = 0; i < kCols; i++) acc[i] = 0;
       }
-      waiting = -1;
+      past = min(past + kExactSteps, use / per * steps + steps);
     };
 
-    int s = 0, qs = 0, t = pair, k = 0;
-    uint32_t turn = 0;
-    for (int i = 1 - kDepth; t < tiles || waiting >= 0; i++) {
-      copy();
-      if (i < 0) continue;
-      bool end = true;
-      if (t < tiles) {
-        copies_wait<kDepth - 1>();
-        const uint32_t at = slot + qs * (kAskew ? 2 : 1) * kWork * 16;
-        if (++qs == kDepth) qs = 0;
-        uint4 w = load_shared(at);
-        if (kAskew) {
-          const long long v = (long long)(t / row_tiles) * kTileTokens + rank * kHalf + token;
-          const int m = (int)((uintptr_t)(a.head + min(v, (long long)a.V - 1) * a.head_stride) & 15);
-          const uint4 w2 = load_shared(at + kWork * 16);
-          uint32_t x[8] = {w.x, w.y, w.z, w.w, w2.x, w2.y, w2.z, w2.w};
+    // n: the team's next step of all, step k of the pair's tile `tile`
+    int n = team, tile = n / steps, k = n % steps;
+    while (ok) {
+      // sums are taken over before the step in whose place this one comes waits for theirs
+      while (ok && use < own * per && (tile >= own || past + kRing <= n)) take();
+      if (!ok || tile >= own) break;
+      const int unit = kAskew ? tile * ((steps + Q::kSteps - 1) / Q::kSteps) + k / Q::kSteps : n, place = unit % Q::kUnits;
+      const uint32_t at = queue + place * Q::kUnit + token * Q::kRow + k % Q::kSteps * kStepK;
+      const int s = n % kRing;
+      if (!(ok = bar_wait(come + 8 * place, unit / Q::kUnits & 1))) break;
+      if (!(ok = bar_wait(empty + 8 * s, (n / kRing & 1) ^ 1))) break;
+      products_fence_after();
+      uint32_t m = 0;  // bytes ahead of the token's row in its first 16
+      if (kAskew) {
+        const uint32_t v = (uint32_t)((pair + tile * kPairs) / row_tiles) * kTileTokens + rank * kHalf + token;
+        m = ((uint32_t)(uintptr_t)a.head + v * (uint32_t)a.head_stride) & 15;
+      }
 #pragma unroll
-          for (int i = 0; i < 6; i++) x[i] = m & 8 ? x[i + 2] : x[i];
+      for (int i = 0; i < 4; i += 2) {
+        uint32_t x[16];
 #pragma unroll
-          for (int i = 0; i < 5; i++) x[i] = m & 4 ? x[i + 1] : x[i];
-          const int by = (m & 3) * 8;
-          w = make_uint4(__funnelshift_r(x[0], x[1], by), __funnelshift_r(x[1], x[2], by), __funnelshift_r(x[2], x[3], by),
-                         __funnelshift_r(x[3], x[4], by));
+        for (int j = 0; j < 2; j++) {
+          uint4 w = load_shared(kAskew ? at + (i + j) * 16 : at + ((i + j) ^ (token >> 1 & 3)) * 16);
+          if (kAskew) w = shifted(w, load_shared(at + (i + j + 1) * 16), m);
+          const uint32_t y[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+          for (int c = 0; c < 4; c++) {
+            const uint2 h = halves_of(y[c]);
+            x[8 * j + 2 * c] = h.x, x[8 * j + 2 * c + 1] = h.y;
+          }
         }
-        if (!(ok = bar_wait(empty + 8 * s, turn ^ 1))) break;
-        const uint32_t A = ring + s * (kOperandA + kOperandB) + place;
-        store_shared(A + c0, halves_of(w.x), halves_of(w.y));
-        store_shared(A + c1, halves_of(w.z), halves_of(w.w));
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
-        if (lane == 0) bar_arrive_cluster(full0 + 8 * s);
-        if (++s == kRing) s = 0, turn ^= 1;
-        end = (k + 1) % kExactSteps == 0 || k + 1 == steps;
+        operand_store(operands + lanes + s * 32 + i * 8, x);
       }
-      // sums are taken over once the products are past them, or before the next ones are whole
-      if (waiting >= 0 && (++since >= kRing || end)) {
-        take();
-        if (!ok) break;
+      operand_stored();
+      products_fence_before();
+      __syncwarp();
+      if (lane == 0) {
+        bar_arrive_cluster(full0 + 8 * s);
+        // the last step of a row also answers for the unit's that do not exist
+        bar_arrive(gone + 8 * place, k + 1 == steps ? Q::kSteps - k % Q::kSteps : 1);
       }
-      if (t < tiles) {
-        if (end) waiting = t, whole = k + 1 == steps, since = 0;
-        if (++k == steps) k = 0, t += kPairs;
-      }
+      n += kTeams;
+      for (k += kTeams; k >= steps; k -= steps) tile++;
     }
-    copies_wait<0>();
   }
   if (!ok) {
     *a.failed = 1;
@@ -397,13 +464,23 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   if (warp == kWorkWarps) sums_free_pair(sums);
 }
 
-// Hidden states of 8 bits as fp16, rows of a multiple of 16 bytes
+// Hidden states of 8 bits as fp16, rows of a multiple of 16 bytes; a thread's four
 __global__ void __launch_bounds__(256) k_rows_as_halves(const int8_t* q, __half* to, int d, int ld, long long rows, int* failed) {
   if (blockIdx.x == 0 && threadIdx.x == 0) *failed = 0;
-  const int lane = threadIdx.x % 32;
-  for (long long r = blockIdx.x * 8ll + threadIdx.x / 32; r < rows; r += gridDim.x * 8ll)
-#pragma unroll 4
-    for (int k = lane; k < ld; k += 32) to[r * ld + k] = __float2half_rn(k < d ? (float)q[r * d + k] : 0.0f);
+  const int per = ld / 4;
+  const bool words = d % 4 == 0 && (uintptr_t)q % 4 == 0;
+  for (long long i = blockIdx.x * 256ll + threadIdx.x; i < rows * per; i += gridDim.x * 256ll) {
+    const long long r = i / per;
+    const int k = (int)(i % per) * 4;
+    uint32_t w = 0;
+    if (words) {
+      if (k < d) w = *(const uint32_t*)(q + r * d + k);
+    } else {
+      for (int j = 0; j < 4; j++)
+        if (k + j < d) w |= (uint32_t)(uint8_t)q[r * d + k + j] << 8 * j;
+    }
+    *(uint2*)(to + r * ld + k) = halves_of(w);
+  }
 }
 
 // ---- on the host
@@ -422,15 +499,18 @@ template <typename T, int kRows>
 epic_status launch_tiles(const Int8Args& a, __half* q16, int ld, bool askew, cudaStream_t st) {
   CUtensorMap map;
   if (!make_map(&map, false, q16, ld, a.rows, ld, kRows / 2)) return EPIC_ERR_CUDA;
+  CUtensorMap head = map;  // of a head that lies askew: unused
+  if (!askew && !make_byte_map(&head, a.head, a.d, a.V, a.V > 1 ? a.head_stride : (a.d + 15) / 16 * 16, kHalf))
+    return EPIC_ERR_CUDA;
   const auto kernel = askew ? k_int8_tiles<T, kRows, true> : k_int8_tiles<T, kRows, false>;
   if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kShared) != cudaSuccess)
     return cudaGetLastError(), EPIC_ERR_CUDA;
-  kernel<<<2 * kPairs, kThreads, kShared, st>>>(map, a);
+  kernel<<<2 * kPairs, kThreads, kShared, st>>>(map, head, a);
   return cudaGetLastError() == cudaSuccess ? EPIC_OK : EPIC_ERR_CUDA;
 }
 
 bool head_lies_askew(const int8_t* head, long long stride, int V) {
-  return (uintptr_t)head % 16 != 0 || (V > 1 && stride % 16 != 0);
+  return (uintptr_t)head % 16 != 0 || (V > 1 && (stride % 16 != 0 || stride >= 1ll << 39));
 }
 
 bool few_rows(long long rows, int d, bool askew) {
@@ -443,7 +523,7 @@ int tile_rows(long long rows) {
   long long least = -1;
   for (const int n : {256, 128, 64, 32}) {
     const long long cost = (rows + n - 1) / n * std::max(2 * n, 320);
-    if (least < 0 || cost < least) best = n, least = cost;
+    if (least < 0 || cost <= least) best = n, least = cost;
   }
   return best;
 }
@@ -459,7 +539,7 @@ epic_status launch_int8(Int8Args a, void* ws, cudaStream_t st) {
   a.failed = (int*)ws;
   __half* q16 = (__half*)((char*)ws + 256);
   const int ld = (a.d + 7) / 8 * 8;
-  k_rows_as_halves<<<(unsigned)std::min(1216, (a.rows + 7) / 8), 256, 0, st>>>(a.q, q16, a.d, ld, a.rows, a.failed);
+  k_rows_as_halves<<<(unsigned)std::min(2432ll, ((long long)a.rows * (ld / 4) + 255) / 256), 256, 0, st>>>(a.q, q16, a.d, ld, a.rows, a.failed);
   if (cudaGetLastError() != cudaSuccess) return EPIC_ERR_CUDA;
   switch (tile_rows(a.rows)) {
     case 32: return launch_tiles<T, 32>(a, q16, ld, askew, st);

@@ -36,18 +36,19 @@ __device__ __forceinline__ void bar_init_visible() { asm volatile("fence.mbarrie
 __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ void bar_arrive(uint32_t bar) {
-  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+__device__ __forceinline__ void bar_arrive(uint32_t bar, uint32_t count) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(count) : "memory");
 }
-// of a barrier in any CTA of the cluster
+// of a barrier in any CTA of the cluster.  What it orders is in shared memory and told to the tensor units by a proxy fence,
+// or in tensor memory and fenced by tcgen05.fence: a release to the whole cluster would wait for much more.
 __device__ __forceinline__ void bar_arrive_cluster(uint32_t bar) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
   uint32_t done;
   asm volatile(
       "{\n\t.reg .pred p;\n\t"
-      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
       "selp.u32 %0, 1, 0, p;\n\t}"
       : "=r"(done)
       : "r"(bar), "r"(parity)
@@ -71,6 +72,19 @@ __device__ __forceinline__ void load_box_pair(const CUtensorMap* map, uint32_t d
           "r"(dst),
       "l"(map), "r"(bar), "r"(x), "r"(y)
       : "memory");
+}
+// the same, counted in this CTA
+__device__ __forceinline__ void load_box(const CUtensorMap* map, uint32_t dst, uint32_t bar, int x, int y) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(dst),
+      "l"(map), "r"(bar), "r"(x), "r"(y)
+      : "memory");
+}
+// `bytes` of memory, addresses and bytes multiples of 16
+__device__ __forceinline__ void load_run(uint32_t dst, const void* from, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(from),
+               "r"(bytes), "r"(bar)
+               : "memory");
 }
 __device__ __forceinline__ void prefetch_map(const CUtensorMap* map) {
   asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
@@ -103,6 +117,15 @@ __device__ __forceinline__ void product_pair(uint32_t sums, uint64_t a, uint64_t
       "setp.ne.b32 p, %4, 0;\n\t"
       "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(sums),
       "l"(a), "l"(b), "r"(kind), "r"((uint32_t)add)
+      : "memory");
+}
+// the same with the first operand in tensor memory: a lane a row, 16 of the sum in 8 columns
+__device__ __forceinline__ void product_pair_in(uint32_t sums, uint32_t a, uint64_t b, uint32_t kind, bool add) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(sums),
+      "r"(a), "l"(b), "r"(kind), "r"((uint32_t)add)
       : "memory");
 }
 // an arrival at that barrier of both CTAs once all products so far are done
@@ -152,6 +175,15 @@ __device__ __forceinline__ void sums_loaded(float (&v)[32]) {
   asm volatile("tcgen05.wait::ld.sync.aligned;" : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]), "+f"(v[8]), "+f"(v[9]), "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15]), "+f"(v[16]), "+f"(v[17]), "+f"(v[18]), "+f"(v[19]), "+f"(v[20]), "+f"(v[21]), "+f"(v[22]), "+f"(v[23]), "+f"(v[24]), "+f"(v[25]), "+f"(v[26]), "+f"(v[27]), "+f"(v[28]), "+f"(v[29]), "+f"(v[30]), "+f"(v[31])::"memory");
 }
 
+// 16 columns of the warp's 32 lanes; there after operand_stored()
+__device__ __forceinline__ void operand_store(uint32_t to, const uint32_t (&v)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(to),
+      "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
+      : "memory");
+}
+__device__ __forceinline__ void operand_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
 // a microsecond's worth of waiting for copies in flight, many times over: after a wait that gave up
 __device__ __noinline__ void let_copies_land() {
   for (int i = 0; i < 2000; i++) __nanosleep(1000);
@@ -173,6 +205,16 @@ inline EncodeTiled encode_tiled() {
     return (EncodeTiled)p;
   }();
   return f;
+}
+
+// [rows][cols] of bytes, `ld` apart: boxes of 64 columns and `box` rows, chunks of 16 swizzled by the row's number / 2 in 4
+inline bool make_byte_map(CUtensorMap* map, const void* base, long long cols, long long rows, long long ld, int box) {
+  const cuuint64_t size[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, stride[1] = {(cuuint64_t)ld};
+  const cuuint32_t part[2] = {64, (cuuint32_t)box}, step[2] = {1, 1};
+  return encode_tiled() &&
+         encode_tiled()(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, (void*)base, size, stride, part, step,
+                        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // [rows][cols] of 16-bit elements, `ld` apart: boxes of 64 columns and `box` rows
