@@ -297,7 +297,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   uint8_t* shared = (uint8_t*)(((uintptr_t)shared_raw + 1023) / 1024 * 1024);
   const uint32_t stages = smem_address(shared);
   T* turns = (T*)(shared + kStages * kStage);
-  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, pair = blockIdx.x / 2;
+  const int warp = warp_of_thread(), lane = threadIdx.x % 32, pair = blockIdx.x / 2;
   const uint32_t rank = cluster_rank();
   const uint32_t full = smem_address(bars.full), empty = smem_address(bars.empty);
   const uint32_t sums_full = smem_address(bars.sums_full), sums_empty = smem_address(bars.sums_empty);
@@ -355,7 +355,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       }
     }
   } else if (warp == 1) {
-    if (lane == 0 && rank == 0) {  // products
+    if (rank == 0) {  // products
       int s = 0, use = 0;
       uint32_t turn = 0;
       Task t;
@@ -370,16 +370,20 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         for (int k = 0; k < t.steps; k++) {
           if (!(ok = bar_wait(full + 8 * s, turn))) break;
           products_fence_after();
-          const uint32_t A = stages + s * kStage, B = A + kOperand;
-          const uint64_t da = a_across ? operand_mn(A) : operand_k(A), db = b_across ? operand_mn(B) : operand_k(B);
-          const uint32_t na = a_across ? kNextMN : kNextK, nb = b_across ? kNextMN : kNextK;
+          if (one_lane()) {
+            const uint32_t A = stages + s * kStage, B = A + kOperand;
+            const uint64_t da = a_across ? operand_mn(A) : operand_k(A), db = b_across ? operand_mn(B) : operand_k(B);
+            const uint32_t na = a_across ? kNextMN : kNextK, nb = b_across ? kNextMN : kNextK;
 #pragma unroll
-          for (int j = 0; j < kStepK / 16; j++) product_pair(to, da + j * na, db + j * nb, kind, k > 0 || j > 0);
-          products_arrive_pair(empty + 8 * s);
+            for (int j = 0; j < kStepK / 16; j++) product_pair(to, da + j * na, db + j * nb, kind, k > 0 || j > 0);
+            products_arrive_pair(empty + 8 * s);
+          }
+          __syncwarp();
           if (++s == kStages) s = 0, turn ^= 1;
         }
         if (!ok) break;
-        products_arrive_pair(sums_full + 8 * half);
+        if (one_lane()) products_arrive_pair(sums_full + 8 * half);
+        __syncwarp();
         use++;
       }
     }

@@ -246,7 +246,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   __shared__ Int8Bars bars;
   const uint32_t ring = (smem_address(shared_raw) + 1023) / 1024 * 1024;
   const uint32_t queue = ring + kRing * kOperand;
-  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, pair = blockIdx.x / 2;
+  const int warp = warp_of_thread(), lane = threadIdx.x % 32, pair = blockIdx.x / 2;
   const uint32_t rank = cluster_rank();
   const uint32_t full = smem_address(bars.full), empty = smem_address(bars.empty);
   const uint32_t sums_full = smem_address(bars.sums_full), sums_empty = smem_address(bars.sums_empty);
@@ -332,7 +332,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         }
       }
     }
-    if (warp == kWorkWarps + 1 && lane == 0 && rank == 0) {  // products
+    if (warp == kWorkWarps + 1 && rank == 0) {  // products
       constexpr uint32_t kind = product_kind(false, false, false, kTileTokens, kRows);
       int s = 0, use = 0;
       uint32_t turn = 0;
@@ -344,14 +344,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           for (bool add = false; k < end; k++) {
             if (!(ok = bar_wait(full + 8 * s, turn))) break;
             products_fence_after();
-            const uint64_t b = operand_k(ring + s * kOperand);
+            if (one_lane()) {
+              const uint64_t b = operand_k(ring + s * kOperand);
 #pragma unroll
-            for (int j = 0; j < kStepK / 16; j++, add = true)
-              product_pair_in(sums + half * kRows, operands + s * 32 + j * 8, b + j * kNextK, kind, add);
-            products_arrive_pair(empty + 8 * s);
+              for (int j = 0; j < kStepK / 16; j++)
+                product_pair_in(sums + half * kRows, operands + s * 32 + j * 8, b + j * kNextK, kind, add || j);
+              products_arrive_pair(empty + 8 * s);
+            }
+            __syncwarp();
+            add = true;
             if (++s == kRing) s = 0, turn ^= 1;
           }
-          if (ok) products_arrive_pair(sums_full + 8 * half);
+          if (ok && one_lane()) products_arrive_pair(sums_full + 8 * half);
+          __syncwarp();
         }
       }
     }

@@ -20,6 +20,15 @@ __device__ __forceinline__ uint32_t cluster_rank() {
   asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
   return r;
 }
+// the thread's warp, known to be the same in all its lanes
+__device__ __forceinline__ int warp_of_thread() { return __shfl_sync(~0u, threadIdx.x / 32, 0); }
+// true in one lane of a whole warp.  Products are issued so, from loops that the warp goes through together: their operands
+// then are in uniform registers (from one lane's loop a step of four products took 560 clocks to issue).
+__device__ __forceinline__ bool one_lane() {
+  uint32_t p;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+  return p;
+}
 // the same place in the shared memory of the cluster's CTA `rank`
 __device__ __forceinline__ uint32_t at_rank(uint32_t addr, uint32_t rank) {
   uint32_t r;
