@@ -106,6 +106,7 @@ struct Int8Args {
   long long stride_b, stride_n;
   int rows, k, d, V;
   int* failed;
+  const int* sizes;  // of rows, added up
 };
 
 // ---- few rows: a warp's lanes along tokens' rows, whole-number products of four bytes an instruction
@@ -180,7 +181,8 @@ __global__ void __launch_bounds__(kFewThreads) k_few_logits(Int8Args a) {
 // ---- many rows: on the tensor units
 //
 // This GPU's tensor units have no fast products of 8-bit integers, but a product of two of them in fp16 is exact, and so are
-// sums in 32-bit floats while they stay below 2^24, which 1,024 products do; they are then taken over into 32-bit
+// sums in 32-bit floats up to 2^24: of 1,024 products, or of all if 128 times the sum of a row's sizes stays within it in
+// every row (as it does for normally distributed ones up to a width of some 4,500).  Then sums are taken over into 32-bit
 // integers.  A pair of CTAs makes 256 tokens x up to 256 rows.  The head's bytes come into a queue in shared memory, by boxes
 // or, where rows start anywhere, row by row with the aligned 16 bytes that they begin and end in; the work warps turn them
 // into fp16 (byte + 128 in the low bits of 1024.0, less 1152) in tensor memory, where the tensor units take them from.
@@ -208,6 +210,7 @@ constexpr int kPairs = 76;
 struct Int8Bars {
   uint64_t full[kRing], empty[kRing], sums_full[2], sums_empty[2], come[10], gone[10];
   uint32_t sums;
+  int most;
 };
 
 // four bytes as four numbers of fp16
@@ -264,7 +267,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       bar_init(sums_full + 8 * s, 1);
       bar_init(sums_empty + 8 * s, 2 * kWorkWarps);
     }
+    bars.most = 0;
     bar_init_visible();
+  }
+  if (a.d > kExactSteps * kStepK) {
+    __syncthreads();
+    int most = 0;
+    for (int r = threadIdx.x; r < a.rows; r += kThreads) most = max(most, a.sizes[r]);
+    most = __reduce_max_sync(~0u, most);
+    if (lane == 0) atomicMax(&bars.most, most);
   }
   if (warp == kWorkWarps) sums_take_pair(smem_address(&bars.sums));
   products_fence_before();
@@ -274,6 +285,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   products_fence_after();
   const uint32_t sums = bars.sums;
   const int row_tiles = (a.rows + kRows - 1) / kRows, steps = (a.d + kStepK - 1) / kStepK;
+  const int exact = bars.most <= (1 << 24) / 128 ? steps : kExactSteps;  // steps whose sums are exact
   const int tiles = (int)((a.V + (long long)kTileTokens - 1) / kTileTokens) * row_tiles;
   constexpr int kBoxBytes = kRows / 2 * kStepK * 2;
   // tensor memory: sums, twice if they leave room for the operand's ring in the last 256 columns
@@ -338,7 +350,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       uint32_t turn = 0;
       for (int t = pair; ok && t < tiles; t += kPairs) {
         for (int k = 0; ok && k < steps; use++) {
-          const int half = use % kSums, end = min(k + kExactSteps, steps);
+          const int half = use % kSums, end = min(k + exact, steps);
           if (!(ok = bar_wait(sums_empty + 8 * half, (use / kSums & 1) ^ 1))) break;
           products_fence_after();
           for (bool add = false; k < end; k++) {
@@ -363,60 +375,83 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   } else {
     if (kRows == 256) asm volatile("setmaxnreg.inc.sync.aligned.u32 112;");
     constexpr int kCols = kRows / 4;               // a warp's rows of logits
-    constexpr int kLoad = kCols < 16 ? kCols : 16;  // at a time
+    constexpr int kLoad = kCols < 32 ? kCols : 32;  // at a time
+    constexpr int kPiece = 8, kPieces = kCols / kPiece;
     const int quarter = warp % 4, team = warp / 4, token = quarter * 32 + lane;  // of the CTA's
     const uint32_t full0 = at_rank(full, 0), sums_empty0 = at_rank(sums_empty, 0);
     const uint32_t lanes = (uint32_t)quarter * 32 << 16, from = sums + lanes + team * kCols;
-    const int own = (tiles - pair + kPairs - 1) / kPairs, per = (steps + kExactSteps - 1) / kExactSteps;  // tiles, takes each
+    const int own = (tiles - pair + kPairs - 1) / kPairs, per = (steps + exact - 1) / exact;  // tiles, takes each
     int acc[kCols];
-#pragma unroll
-    for (int i = 0; i < kCols; i++) acc[i] = 0;
+    int use = 0, past = min(exact, steps), out = kPieces;  // the next sums to take over, the step past them, the piece to write
 
-    int use = 0, past = min(kExactSteps, steps);  // the next sums to take over, and the step past them
+    // The tile before the next sums': its logits are written 8 rows at a time between the steps of the next tile.
+    T* z = nullptr;           // the next logit of the lane's token,
+    int left = 0, zi = 0;     // how many rows exist; the position of the next one
+    float S = 0.0f, scales[(kCols + 31) / 32];  // of the token; of the rows, a lane a row
+    bool there = false;
+    auto write = [&] {
+#pragma unroll
+      for (int p = 0; p < kPieces; p++) {
+        if (p != out) continue;
+#pragma unroll
+        for (int c = p * kPiece; c < p * kPiece + kPiece; c++) {
+          const float x = (float)acc[c] * __shfl_sync(~0u, scales[c / 32], c % 32) * S;
+          if (c < left && there) *z = of_float<T>(x);
+          z += a.stride_n;
+          if (++zi == a.k) {
+            z += a.stride_b - a.k * a.stride_n;
+            zi = 0;
+          }
+        }
+      }
+      out++;
+    };
     auto take = [&] {
       const int half = use % kSums;
       if (!(ok = bar_wait(sums_full + 8 * half, use / kSums & 1))) return;
       products_fence_after();
+      const bool first = use % per == 0;
 #pragma unroll
       for (int c = 0; c < kCols; c += kLoad) {
         float v[kLoad];
         sums_load(from + half * kRows + c, v);
         sums_loaded(v);
 #pragma unroll
-        for (int i = 0; i < kLoad; i++) acc[c + i] += __float2int_rn(v[i]);
+        for (int i = 0; i < kLoad; i++) acc[c + i] = (first ? 0 : acc[c + i]) + __float2int_rn(v[i]);
       }
       products_fence_before();
       __syncwarp();
       if (lane == 0) bar_arrive_cluster(sums_empty0 + 8 * half);
-      const int tile = use / per, t = pair + tile * kPairs;
+      const int tile = use / per;
+      past = min((tile + 1) * steps, past + exact);
       if (++use % per == 0) {
-        past = (tile + 1) * steps;
-        const int r0 = t % row_tiles * kRows + team * kCols;
+        past = (tile + 1) * steps + min(exact, steps);
+        out = 0;
+        const int t = pair + tile * kPairs, r0 = t % row_tiles * kRows + team * kCols;
         const long long v = (long long)(t / row_tiles) * kTileTokens + rank * kHalf + token;
-        const float S = v < a.V ? a.head_scale[v] : 0.0f;
-        int b = r0 / a.k, i = r0 % a.k;
-        T* z = (T*)a.logits + b * a.stride_b + i * a.stride_n + v;
-        float s = 0.0f;  // a lane a row
+        there = v < a.V;
+        left = a.rows - r0;
+        S = there ? a.head_scale[v] : 0.0f;
 #pragma unroll
-        for (int c = 0; c < kCols; c++) {
-          if (c % 32 == 0) s = r0 + c + lane < a.rows ? a.scale[r0 + c + lane] : 0.0f;
-          const float x = (float)acc[c] * __shfl_sync(~0u, s, c % 32) * S;
-          if (r0 + c < a.rows && v < a.V) *z = of_float<T>(x);
-          z += a.stride_n;
-          if (++i == a.k) i = 0, b++, z = (T*)a.logits + b * a.stride_b + v;
-        }
-#pragma unroll
-        for (int i = 0; i < kCols; i++) acc[i] = 0;
+        for (int c = 0; c < kCols; c += 32) scales[c / 32] = c + lane < left ? a.scale[r0 + c + lane] : 0.0f;
+        zi = r0 % a.k;
+        z = (T*)a.logits + r0 / a.k * a.stride_b + zi * a.stride_n + v;
       }
-      past = min(past + kExactSteps, use / per * steps + steps);
     };
 
     // n: the team's next step of all, step k of the pair's tile `tile`
     int n = team, tile = n / steps, k = n % steps;
     while (ok) {
       // sums are taken over before the step in whose place this one comes waits for theirs
-      while (ok && use < own * per && (tile >= own || past + kRing <= n)) take();
-      if (!ok || tile >= own) break;
+      const bool due = use < own * per && (tile >= own || past + kRing <= n);
+      if (out < kPieces) {
+        write();
+        if (due || tile >= own) continue;
+      } else if (due) {
+        take();
+        continue;
+      }
+      if (tile >= own) break;
       const int unit = kAskew ? tile * ((steps + Q::kSteps - 1) / Q::kSteps) + k / Q::kSteps : n, place = unit % Q::kUnits;
       const uint32_t at = queue + place * Q::kUnit + token * Q::kRow + k % Q::kSteps * kStepK;
       const int s = n % kRing;
@@ -469,22 +504,32 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   if (warp == kWorkWarps) sums_free_pair(sums);
 }
 
-// Hidden states of 8 bits as fp16, rows of a multiple of 16 bytes; a thread's four
-__global__ void __launch_bounds__(256) k_rows_as_halves(const int8_t* q, __half* to, int d, int ld, long long rows, int* failed) {
+// Hidden states of 8 bits as fp16, rows of a multiple of 16 bytes, a CTA a row; and the sum of each row's sizes
+__global__ void __launch_bounds__(256) k_rows_as_halves(const int8_t* q, __half* to, int d, int ld, int* sizes, int* failed) {
+  __shared__ uint32_t s_sum[8];
   if (blockIdx.x == 0 && threadIdx.x == 0) *failed = 0;
-  const int per = ld / 4;
-  const bool words = d % 4 == 0 && (uintptr_t)q % 4 == 0;
-  for (long long i = blockIdx.x * 256ll + threadIdx.x; i < rows * per; i += gridDim.x * 256ll) {
-    const long long r = i / per;
-    const int k = (int)(i % per) * 4;
+  const int8_t* x = q + (long long)blockIdx.x * d;
+  uint2* y = (uint2*)(to + (long long)blockIdx.x * ld);
+  const bool words = (uintptr_t)x % 4 == 0;
+  uint32_t sum = 0;
+#pragma unroll 2
+  for (int k = threadIdx.x * 4; k < ld; k += 1024) {
     uint32_t w = 0;
-    if (words) {
-      if (k < d) w = *(const uint32_t*)(q + r * d + k);
+    if (words && k + 4 <= d) {
+      w = *(const uint32_t*)(x + k);
     } else {
       for (int j = 0; j < 4; j++)
-        if (k + j < d) w |= (uint32_t)(uint8_t)q[r * d + k + j] << 8 * j;
+        if (k + j < d) w |= (uint32_t)(uint8_t)x[k + j] << 8 * j;
     }
-    *(uint2*)(to + r * ld + k) = halves_of(w);
+    y[k / 4] = halves_of(w);
+    sum = __dp4a(__vabs4(w), 0x01010101u, sum);  // 128 is a byte, too
+  }
+  sum = __reduce_add_sync(~0u, sum);
+  if (threadIdx.x % 32 == 0) s_sum[threadIdx.x / 32] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int w = 1; w < 8; w++) sum += s_sum[w];
+    sizes[blockIdx.x] = (int)sum;
   }
 }
 
@@ -522,6 +567,8 @@ bool few_rows(long long rows, int d, bool askew) {
   return rows <= kFewRows && !askew && (rows <= 1 ? 1 : rows <= 2 ? 2 : rows <= 4 ? 4 : 8) * (d + 15ll) <= kFewBytes;
 }
 
+size_t sizes_bytes(long long rows) { return (size_t)(rows * 4 + 255) / 256 * 256; }
+
 // Rows of a tile: a step takes the tensor units 2 clocks a row, and about 320 at least for the head's bytes.
 int tile_rows(long long rows) {
   int best = 256;
@@ -542,9 +589,11 @@ epic_status launch_int8(Int8Args a, void* ws, cudaStream_t st) {
     return a.rows <= 4 ? launch_few<T, 4>(a, st) : launch_few<T, 8>(a, st);
   }
   a.failed = (int*)ws;
-  __half* q16 = (__half*)((char*)ws + 256);
+  int* sizes = (int*)((char*)ws + 256);
+  __half* q16 = (__half*)((char*)ws + 256 + sizes_bytes(a.rows));
   const int ld = (a.d + 7) / 8 * 8;
-  k_rows_as_halves<<<(unsigned)std::min(2432ll, ((long long)a.rows * (ld / 4) + 255) / 256), 256, 0, st>>>(a.q, q16, a.d, ld, a.rows, a.failed);
+  a.sizes = sizes;
+  k_rows_as_halves<<<a.rows, 256, 0, st>>>(a.q, q16, a.d, ld, sizes, a.failed);
   if (cudaGetLastError() != cudaSuccess) return EPIC_ERR_CUDA;
   switch (tile_rows(a.rows)) {
     case 32: return launch_tiles<T, 32>(a, q16, ld, askew, st);
@@ -595,7 +644,7 @@ epic_status epic_int8_logits_workspace(int32_t B, int32_t k, int32_t d, int32_t 
   if (d > kMostProducts || V > 0x7fffffff - 4096 || (long long)B * k > kMostRows) return EPIC_ERR_CAPACITY;
   const long long rows = (long long)B * k;
   *bytes = 256;
-  if (!few_rows(rows, d, head_lies_askew(d_head, head_stride, V))) *bytes += (size_t)rows * ((d + 7) / 8 * 8) * 2;
+  if (!few_rows(rows, d, head_lies_askew(d_head, head_stride, V))) *bytes += sizes_bytes(rows) + (size_t)rows * ((d + 7) / 8 * 8) * 2;
   return EPIC_OK;
 }
 
