@@ -106,7 +106,7 @@ struct Int8Args {
   long long stride_b, stride_n;
   int rows, k, d, V;
   int* failed;
-  const int* sizes;  // of rows, added up
+  const int* sizes;  // [rows][ceil(d / 1024)], added up over 1,024 each
 };
 
 // ---- few rows: a warp's lanes along tokens' rows, whole-number products of four bytes an instruction
@@ -178,12 +178,15 @@ __global__ void __launch_bounds__(kFewThreads) k_few_logits(Int8Args a) {
   }
 }
 
+// 128 * 128 * kMostProducts is the largest sum that 32 bits hold
+constexpr int kMostProducts = 131071;
+
 // ---- many rows: on the tensor units
 //
 // This GPU's tensor units have no fast products of 8-bit integers, but a product of two of them in fp16 is exact, and so are
-// sums in 32-bit floats up to 2^24: of 1,024 products, or of all if 128 times the sum of a row's sizes stays within it in
-// every row (as it does for normally distributed ones up to a width of some 4,500).  Then sums are taken over into 32-bit
-// integers.  A pair of CTAs makes 256 tokens x up to 256 rows.  The head's bytes come into a queue in shared memory, by boxes
+// sums in 32-bit floats up to 2^24: of 1,024 products, or of twice as many, four times and so on if 128 times the sum of as
+// many of a row's sizes stays within it in every row (for normally distributed rows, some 4,000).  Then sums are taken over
+// into 32-bit integers.  A pair of CTAs makes 256 tokens x up to 256 rows.  The head's bytes come into a queue in shared memory, by boxes
 // or, where rows start anywhere, row by row with the aligned 16 bytes that they begin and end in; the work warps turn them
 // into fp16 (byte + 128 in the low bits of 1024.0, less 1152) in tensor memory, where the tensor units take them from.
 // Hidden states are turned once, in the workspace, and come by boxes.  Each of four teams of four warps turns every fourth
@@ -210,7 +213,7 @@ constexpr int kPairs = 76;
 struct Int8Bars {
   uint64_t full[kRing], empty[kRing], sums_full[2], sums_empty[2], come[10], gone[10];
   uint32_t sums;
-  int most;
+  int most[8];
 };
 
 // four bytes as four numbers of fp16
@@ -267,15 +270,24 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       bar_init(sums_full + 8 * s, 1);
       bar_init(sums_empty + 8 * s, 2 * kWorkWarps);
     }
-    bars.most = 0;
+    for (int& m : bars.most) m = 0;
     bar_init_visible();
   }
   if (a.d > kExactSteps * kStepK) {
     __syncthreads();
-    int most = 0;
-    for (int r = threadIdx.x; r < a.rows; r += kThreads) most = max(most, a.sizes[r]);
-    most = __reduce_max_sync(~0u, most);
-    if (lane == 0) atomicMax(&bars.most, most);
+    // the largest sums of 2, 4, 8 .. blocks of a row's sizes
+    const int blocks = (a.d + kExactSteps * kStepK - 1) / (kExactSteps * kStepK);
+    for (int l = 1; 1 << (l - 1) < blocks; l++) {
+      int most = 0;
+      for (int r = threadIdx.x; r < a.rows; r += kThreads)
+        for (int b = 0; b < blocks; b += 1 << l) {
+          int sum = 0;
+          for (int i = b; i < min(b + (1 << l), blocks); i++) sum += a.sizes[(long long)r * blocks + i];
+          most = max(most, sum);
+        }
+      most = __reduce_max_sync(~0u, most);
+      if (lane == 0) atomicMax(&bars.most[l], most);
+    }
   }
   if (warp == kWorkWarps) sums_take_pair(smem_address(&bars.sums));
   products_fence_before();
@@ -285,7 +297,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   products_fence_after();
   const uint32_t sums = bars.sums;
   const int row_tiles = (a.rows + kRows - 1) / kRows, steps = (a.d + kStepK - 1) / kStepK;
-  const int exact = bars.most <= (1 << 24) / 128 ? steps : kExactSteps;  // steps whose sums are exact
+  int exact = kExactSteps;  // steps whose sums are exact
+  for (int l = 1; exact < steps && bars.most[l] <= (1 << 24) / 128; l++) exact *= 2;
   const int tiles = (int)((a.V + (long long)kTileTokens - 1) / kTileTokens) * row_tiles;
   constexpr int kBoxBytes = kRows / 2 * kStepK * 2;
   // tensor memory: sums, twice if they leave room for the operand's ring in the last 256 columns
@@ -504,16 +517,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   if (warp == kWorkWarps) sums_free_pair(sums);
 }
 
-// Hidden states of 8 bits as fp16, rows of a multiple of 16 bytes, a CTA a row; and the sum of each row's sizes
+// Hidden states of 8 bits as fp16, rows of a multiple of 16 bytes, a CTA a row; and their sizes, added up over 1,024 each
 __global__ void __launch_bounds__(256) k_rows_as_halves(const int8_t* q, __half* to, int d, int ld, int* sizes, int* failed) {
-  __shared__ uint32_t s_sum[8];
+  __shared__ uint32_t s_sum[kMostProducts / 1024 + 1];
   if (blockIdx.x == 0 && threadIdx.x == 0) *failed = 0;
+  const int blocks = (d + 1023) / 1024;
+  for (int i = threadIdx.x; i < blocks; i += 256) s_sum[i] = 0;
+  __syncthreads();
   const int8_t* x = q + (long long)blockIdx.x * d;
   uint2* y = (uint2*)(to + (long long)blockIdx.x * ld);
   const bool words = (uintptr_t)x % 4 == 0;
-  uint32_t sum = 0;
 #pragma unroll 2
-  for (int k = threadIdx.x * 4; k < ld; k += 1024) {
+  for (int k = threadIdx.x * 4, i = 0; i < blocks; k += 1024, i++) {
     uint32_t w = 0;
     if (words && k + 4 <= d) {
       w = *(const uint32_t*)(x + k);
@@ -521,16 +536,12 @@ __global__ void __launch_bounds__(256) k_rows_as_halves(const int8_t* q, __half*
       for (int j = 0; j < 4; j++)
         if (k + j < d) w |= (uint32_t)(uint8_t)x[k + j] << 8 * j;
     }
-    y[k / 4] = halves_of(w);
-    sum = __dp4a(__vabs4(w), 0x01010101u, sum);  // 128 is a byte, too
+    if (k < ld) y[k / 4] = halves_of(w);
+    const uint32_t sum = __reduce_add_sync(~0u, __dp4a(__vabs4(w), 0x01010101u, 0u));  // 128 is a byte, too
+    if (threadIdx.x % 32 == 0) atomicAdd(&s_sum[i], sum);
   }
-  sum = __reduce_add_sync(~0u, sum);
-  if (threadIdx.x % 32 == 0) s_sum[threadIdx.x / 32] = sum;
   __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int w = 1; w < 8; w++) sum += s_sum[w];
-    sizes[blockIdx.x] = (int)sum;
-  }
+  for (int i = threadIdx.x; i < blocks; i += 256) sizes[(long long)blockIdx.x * blocks + i] = (int)s_sum[i];
 }
 
 // ---- on the host
@@ -567,7 +578,7 @@ bool few_rows(long long rows, int d, bool askew) {
   return rows <= kFewRows && !askew && (rows <= 1 ? 1 : rows <= 2 ? 2 : rows <= 4 ? 4 : 8) * (d + 15ll) <= kFewBytes;
 }
 
-size_t sizes_bytes(long long rows) { return (size_t)(rows * 4 + 255) / 256 * 256; }
+size_t sizes_bytes(long long rows, int d) { return (size_t)(rows * ((d + 1023) / 1024) * 4 + 255) / 256 * 256; }
 
 // Rows of a tile: a step takes the tensor units 2 clocks a row, and about 320 at least for the head's bytes.
 int tile_rows(long long rows) {
@@ -590,7 +601,7 @@ epic_status launch_int8(Int8Args a, void* ws, cudaStream_t st) {
   }
   a.failed = (int*)ws;
   int* sizes = (int*)((char*)ws + 256);
-  __half* q16 = (__half*)((char*)ws + 256 + sizes_bytes(a.rows));
+  __half* q16 = (__half*)((char*)ws + 256 + sizes_bytes(a.rows, a.d));
   const int ld = (a.d + 7) / 8 * 8;
   a.sizes = sizes;
   k_rows_as_halves<<<a.rows, 256, 0, st>>>(a.q, q16, a.d, ld, sizes, a.failed);
@@ -606,8 +617,6 @@ epic_status launch_int8(Int8Args a, void* ws, cudaStream_t st) {
 bool bad_type(int dtype) { return dtype != EPIC_F32 && dtype != EPIC_F16 && dtype != EPIC_BF16; }
 size_t size_of(int dtype) { return dtype == EPIC_F32 ? 4 : 2; }
 
-// 128 * 128 * kMostProducts is the largest sum that 32 bits hold
-constexpr int kMostProducts = 131071;
 constexpr long long kMostRows = 1 << 21;
 
 }  // namespace
@@ -644,7 +653,7 @@ epic_status epic_int8_logits_workspace(int32_t B, int32_t k, int32_t d, int32_t 
   if (d > kMostProducts || V > 0x7fffffff - 4096 || (long long)B * k > kMostRows) return EPIC_ERR_CAPACITY;
   const long long rows = (long long)B * k;
   *bytes = 256;
-  if (!few_rows(rows, d, head_lies_askew(d_head, head_stride, V))) *bytes += sizes_bytes(rows) + (size_t)rows * ((d + 7) / 8 * 8) * 2;
+  if (!few_rows(rows, d, head_lies_askew(d_head, head_stride, V))) *bytes += sizes_bytes(rows, d) + (size_t)rows * ((d + 7) / 8 * 8) * 2;
   return EPIC_OK;
 }
 
