@@ -443,13 +443,14 @@ enum { EPIC_HEAD_FORWARD = 0, EPIC_HEAD_BACKWARD = 1, EPIC_HEAD_STEP = 2 };
  * epic_head_loss_backward: gradients of sum(grad_loss * loss), d_grad_loss [B][n]:
  *   g = w grad_loss,  dz[v] = g (exp(z[v] - lse) - [v = target]),  dh = dz W,  dW = dz^T h
  * into d_grad_hidden [B][n][d] (0 where a position does not count) and d_grad_head
- * [V][d], both written whole, each with its own strides; either may be NULL.  d_lse is
- * what the forward call gave for the same inputs; exponentials are taken relative to it
- * and summed anew, so it does not limit their precision.
+ * [V][d], both written whole, each with its own strides; either may be NULL.
+ * Probabilities come from d_lse, off by |lse| 2^-24 of themselves; that of the target less
+ * 1 is minus the sum of the others.
  * epic_head_loss_step: loss and both gradients in one call with grad_loss = 1, making
  * the logits once (bf16).
- * In both, exponentials and hidden states times a row's factor are rounded to dtype
- * (off by at most 2^-8 of a value in bf16, 2^-11 in fp16) before they are multiplied and summed.
+ * In both, gradients of logits are rounded to dtype (off by at most 2^-8 of a value in
+ * bf16, 2^-11 in fp16) before they are multiplied and summed; so are, in a step in bf16,
+ * hidden states times a row's factor.
  * A target of probability 0 gives loss +inf and a finite gradient.  NaN or +inf
  * logits give NaN, in the gradient of the head at all tokens.  What is in the rows of
  * positions that do not count does not matter.

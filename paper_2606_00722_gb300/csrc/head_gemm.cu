@@ -49,7 +49,7 @@ struct TileArgs {
 };
 
 struct Maps {
-  CUtensorMap hc, hs, head_k, head_mn, e_k, e_mn;
+  CUtensorMap hc, hc_mn, hs, head_k, head_mn, e_k, e_mn;
 };
 
 __device__ __forceinline__ int up_div(int a, int b) { return (a + b - 1) / b; }
@@ -132,9 +132,21 @@ __device__ __forceinline__ void store_rows(T* to, const float (&v)[32], int coun
 #pragma unroll
   for (int j = 0; j < 16; j++) ((uint32_t*)(turn + lane * kTurnRow))[j] = w[j];
   __syncwarp();
-  for (int r = 0; r < 32; r++) {
+  // half a warp a row, two elements a lane from the first multiple of 4 bytes on; its last lane also has the element before
+  const int at = lane % 16;
+#pragma unroll 4
+  for (int r = lane / 16; r < 32; r += 2) {
     T* row = (T*)__shfl_sync(~0u, (unsigned long long)to, r);
-    if (row && lane < count) row[lane] = turn[r * kTurnRow + lane];
+    if (!row) continue;
+    const T* v = turn + r * kTurnRow;
+    const int odd = (uintptr_t)row / 2 % 2, j = 2 * at + odd;
+    if (j + 1 < min(count, 32)) {
+      const T two[2] = {v[j], v[j + 1]};
+      *(uint32_t*)(row + j) = (uint32_t)*(const uint16_t*)&two[0] | (uint32_t)*(const uint16_t*)&two[1] << 16;
+    } else if (j < min(count, 32)) {
+      row[j] = v[j];
+    }
+    if (odd && at == 15) row[0] = v[0];
   }
 }
 
@@ -158,9 +170,11 @@ __device__ __forceinline__ void logits_rows(const TileArgs& a, int n, uint32_t s
   const HeadPlan& p = a.p;
   const bool real = row < n;
   const int y = real ? p.tgt[row] - col : -1;
-  const float ref = kProbs && real ? p.ref[row] : 0.0f;
-  const float at = kProbs && real && a.pass.only_again ? p.at[row] : 0.0f;
-  float to = kProbs ? ref : kNoRef, s = 0.0f;
+  const bool known = a.pass.known;
+  const float ref = !kProbs || !real ? 0.0f : known ? p.known_ref[row] : p.ref[row];
+  const float mul = kProbs && real && known ? p.known_mul[row] : 1.0f;
+  const float at = kProbs && real && a.pass.only_again ? p.known_at[row] : 0.0f;
+  float to = kProbs ? (known ? 0.0f : ref) : kNoRef, s = 0.0f;
 #pragma unroll 1
   for (int c = 0; c < kRecCols; c += 32) {
     if (col + c >= p.lde) break;
@@ -183,10 +197,10 @@ __device__ __forceinline__ void logits_rows(const TileArgs& a, int n, uint32_t s
     }
     if (kProbs) {
 #pragma unroll
-      for (int j = 0; j < 32; j++) z[j] = ex2(fmaf(z[j], kLog2E, -ref));
+      for (int j = 0; j < 32; j++) z[j] = ex2(fmaf(z[j], kLog2E, -ref)) * mul;
       s += sum32(z);
       if (target) {
-        const float e = a.pass.only_again ? at : ex2(fmaf(zt, kLog2E, -ref));
+        const float e = a.pass.only_again ? at : ex2(fmaf(zt, kLog2E, -ref)) * mul;
 #pragma unroll
         for (int j = 0; j < 32; j++)
           if (j == here) z[j] = e;
@@ -208,7 +222,7 @@ __device__ __forceinline__ void logits_rows(const TileArgs& a, int n, uint32_t s
   }
   if (!a.pass.sums || col >= p.V) return;
   // exponentials past the window: once more, relative to the largest
-  const bool past = kProbs && real && !(s <= 1.2e18f);
+  const bool past = kProbs && !known && real && !(s <= 1.2e18f);
   if (kProbs && __any_sync(~0u, past)) {
     float to2 = kNoRef, s2 = 0.0f;
 #pragma unroll 1
@@ -237,23 +251,22 @@ __device__ __forceinline__ void store_part(float* part, const float (&v)[32]) {
 
 // Sums of a gradient's tile: kHalf columns of each lane's row
 template <typename T>
-__device__ __forceinline__ void grad_rows(const TileArgs& a, int n, const Task& t, uint32_t sums, int row, int col, T* turn,
-                                          int lane) {
+__device__ __forceinline__ void grad_rows(const TileArgs& a, int n, bool again, const Task& t, uint32_t sums, int row, int col,
+                                          T* turn, int lane) {
   const HeadPlan& p = a.p;
   const GradSplit& sp = a.p.split;
   const bool hidden = t.job == 0;
   const bool parts = (hidden ? sp.hidden_parts : sp.head_parts) > 1;
   const bool there = row < (hidden ? n : p.V);
   T* to = nullptr;
-  float scale = 1.0f;
+  float scale = again ? *p.post : 1.0f;
   if (there && !parts) {
     if (hidden) {
       const long long r = a.out.r0 + p.src[row];
       to = (T*)a.out.grad + (r / a.out.n) * a.out.stride_b + (r % a.out.n) * a.out.stride_n;
-      scale = p.coef[row];
+      if (!again) scale = p.coef[row];
     } else {
       to = (T*)a.grad_head + row * a.grad_head_stride;
-      scale = *p.post;
     }
   }
   const bool whole = __all_sync(~0u, ((uintptr_t)(to + col) & 31) == 0 || !to);
@@ -292,7 +305,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     k_head_tiles(const __grid_constant__ Maps maps, const __grid_constant__ TileArgs a) {
   extern __shared__ uint8_t shared_raw[];
   __shared__ Bars bars;
-  if (kForm != 2 && a.pass.only_again && *a.p.again == 0) return;
+  const bool again = *a.p.again != 0;
+  if (kForm != 2 && a.pass.only_again && !again) return;
   const int n = *a.p.count;
   uint8_t* shared = (uint8_t*)(((uintptr_t)shared_raw + 1023) / 1024 * 1024);
   const uint32_t stages = smem_address(shared);
@@ -347,8 +361,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           } else {
             load_box_pair(&maps.e_mn, A, bar, m, k * kStepK);
             load_box_pair(&maps.e_mn, A + kOperand / 2, bar, m + 64, k * kStepK);
-            load_box_pair(&maps.hs, B, bar, c, k * kStepK);
-            load_box_pair(&maps.hs, B + kOperand / 2, bar, c + 64, k * kStepK);
+            const CUtensorMap* h = again ? &maps.hc_mn : &maps.hs;
+            load_box_pair(h, B, bar, c, k * kStepK);
+            load_box_pair(h, B + kOperand / 2, bar, c + 64, k * kStepK);
           }
           if (++s == kStages) s = 0, turn ^= 1;
         }
@@ -401,7 +416,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         products_fence_after();
       }
       if (kForm == 2) {
-        grad_rows<T>(a, n, t, from, row, t.n0 + off, turn, lane);
+        grad_rows<T>(a, n, again, t, from, row, t.n0 + off, turn, lane);
       } else if (row - lane < up_div(n, kStepK) * kStepK) {
         logits_rows<T, kForm == 1>(a, n, from, row, t.n0 + off, lane);
       }
@@ -435,7 +450,8 @@ __global__ void __launch_bounds__(256) k_head_parts(const __grid_constant__ Tile
   const int parts = hidden ? sp.hidden_parts : sp.head_parts, chunks = up_div(p.d, 4);
   const long long rows = hidden ? *p.count : p.V, room = hidden ? p.cap : p.V;
   const float* from = hidden ? sp.hidden : sp.head;
-  const float post = *p.post;
+  const bool again = *p.again != 0;
+  const float post = again ? *p.post : 1.0f;
   for (long long i = blockIdx.x * 256ll + threadIdx.x; i < rows * chunks; i += gridDim.x * 256ll) {
     const long long row = i / chunks;
     const int c = (int)(i % chunks) * 4;
@@ -452,7 +468,7 @@ __global__ void __launch_bounds__(256) k_head_parts(const __grid_constant__ Tile
     } else {
       to = (T*)a.grad_head + row * a.grad_head_stride;
     }
-    const float scale = hidden ? p.coef[row] : post;
+    const float scale = hidden && !again ? p.coef[row] : post;
     float* acc = p.acc + row * p.ldp + c;
     for (int j = 0; j < 4 && c + j < p.d; j++) {
       float x = v[j] * scale;
@@ -513,7 +529,8 @@ epic_status launch_head_grads(const HeadPlan& p, int dtype, const HiddenGrad& ou
   a.bf16 = dtype == EPIC_BF16;
   if (!out.grad) a.p.split.hidden_parts = 0;
   if (!grad_head) a.p.split.head_parts = 0;
-  if (!make_map(&maps.hs, a.bf16, p.hs, p.ldh, p.cap, p.ldh, 64) || !make_map(&maps.e_k, a.bf16, p.e, p.lde, p.cap, p.lde, kHalf) ||
+  if (!make_map(&maps.hc_mn, a.bf16, p.hc, p.ldh, p.cap, p.ldh, 64) ||
+      !make_map(&maps.hs, a.bf16, p.hs ? p.hs : p.hc, p.ldh, p.cap, p.ldh, 64) || !make_map(&maps.e_k, a.bf16, p.e, p.lde, p.cap, p.lde, kHalf) ||
       !make_map(&maps.e_mn, a.bf16, p.e, p.lde, p.cap, p.lde, 64) ||
       !make_map(&maps.head_mn, a.bf16, p.head, p.d, p.V, p.ldw, 64))
     return EPIC_ERR_CUDA;

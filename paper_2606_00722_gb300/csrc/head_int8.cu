@@ -25,24 +25,6 @@ struct QuantArgs {
 
 constexpr int kQuantThreads = 256;
 
-// 16 bytes of a row as numbers of 32 bits
-template <typename T>
-struct Chunk {
-  static constexpr int kCount = 16 / sizeof(T);
-  float v[kCount];
-  __device__ __forceinline__ Chunk(const T* x, int count, bool whole) {
-    if (whole && count >= kCount) {
-      const uint4 w = *(const uint4*)x;
-      const T* t = (const T*)&w;
-#pragma unroll
-      for (int i = 0; i < kCount; i++) v[i] = as_float(t[i]);
-    } else {
-#pragma unroll
-      for (int i = 0; i < kCount; i++) v[i] = i < count ? as_float(x[i]) : 0.0f;
-    }
-  }
-};
-
 // |v| as a whole number of the same order, NaN above infinity
 __device__ __forceinline__ uint32_t size_order(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 
@@ -230,18 +212,6 @@ __device__ __forceinline__ uint4 load_shared(uint32_t at) {
   asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
   return v;
 }
-// 16 bytes from byte m of two times 16 on
-__device__ __forceinline__ uint4 shifted(uint4 a, uint4 b, uint32_t m) {
-  uint32_t x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-  for (int c = 0; c < 6; c++) x[c] = m & 8 ? x[c + 2] : x[c];
-#pragma unroll
-  for (int c = 0; c < 5; c++) x[c] = m & 4 ? x[c + 1] : x[c];
-  const int by = (m & 3) * 8;
-  return make_uint4(__funnelshift_r(x[0], x[1], by), __funnelshift_r(x[1], x[2], by), __funnelshift_r(x[2], x[3], by),
-                    __funnelshift_r(x[3], x[4], by));
-}
-
 // kRows: rows of a tile.  kAskew: rows of the head start anywhere.
 template <typename T, int kRows, bool kAskew>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)

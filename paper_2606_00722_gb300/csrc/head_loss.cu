@@ -10,10 +10,13 @@
 //   forward:   logits -> records (sums of exponentials by column range) -> loss
 //   step:      logits -> records and exponentials e, relative to a reference known before (the target's logit, from a
 //              product of two rows) -> loss, and each row's sum S -> dh = (w / S) e W, dW = e^T (h w / S)
-//   backward:  the same relative to the logsumexp of the forward call
-// so a step makes the logits once.  e is kept for a piece in 16 bits, like the operands of the products that read it:
-// one rounding of at most 2^-8 (bf16) or 2^-11 (fp16) each, independent ones that a sum over many evens out.  At the target, e - S
-// cancels where the model is sure; there e holds minus the sum of the others, which is summed apart.
+//   backward:  logits -> gradients of logits e = g exp(z - lse) from the forward call's lse -> dh = e W, dW = e^T h
+// so a step makes the logits once.  e is kept for a piece in 16 bits, like the operands of the products that read it: one
+// rounding of at most 2^-8 (bf16) or 2^-11 (fp16), independent ones that a sum over many evens out; so is h w / S, where a
+// step multiplies hidden states.  (To round e alone there, the sums would have to be known before e is written: the logits
+// made twice, a third more work.)  Rows of a step whose exponentials leave the range, and all of an fp16 step, which has
+// not the range at all, get their gradients of logits from the logsumexp in a second pass.  At the target, e - S cancels
+// where the model is sure; there e holds minus the sum of the others, which is summed apart.
 // Sums, references and losses are 32 bits.
 #include <stdlib.h>
 
@@ -42,8 +45,9 @@ struct RowsArgs {
   float *loss, *lse_out;  // of positions that do not count: 0; or NULL
   HiddenGrad out;         // grad NULL: none
   int per;                // positions of a CTA
-  bool probs;             // rows' references are wanted (step)
-  bool scaled;            // fp16: exponentials up to 2^14, factors of the gradient relative to their largest
+  bool probs;             // rows' references are wanted (a step in bf16)
+  bool scaled;            // fp16: gradients of logits relative to the largest factor, times 2^14
+  bool again;             // gradients of logits are from a known logsumexp
 };
 
 __device__ __forceinline__ float row_factor(const RowsArgs& a, long long r) {
@@ -59,12 +63,14 @@ __device__ __forceinline__ float pow2_above(float x) {
   return pow2_whole((float)(((__float_as_int(x) + 0x7fffff) >> 23) - 127));
 }
 
-constexpr float kHalfScale = 14.0f;  // exponentials in fp16 are up to 2^14.5: 2^-28 of a row's sum is still a normal number
+constexpr float kHalfScale = 14.0f;  // of a row's gradient, 2^-28 of its factor is still a normal number of fp16
 
-// The reference of a row whose logsumexp is known
-__device__ __forceinline__ float lse_ref(float lse, bool scaled) {
-  const float ref = rintf(lse * kLog2E) - (scaled ? kHalfScale : 0.0f);
-  return fabsf(ref) < 3.0e38f ? ref : 0.0f;
+// How gradients of logits come from a known logsumexp
+__device__ __forceinline__ void know(const HeadPlan& p, int q, float lse, float g, float post) {
+  float ref = rintf(lse * kLog2E);
+  if (!(fabsf(ref) < 3.0e38f)) ref = 0.0f;
+  p.known_ref[q] = ref;
+  p.known_mul[q] = g / post * ex2(fmaf(-lse, kLog2E, ref));
 }
 
 // Packs the positions that count.  Every CTA counts those before its own, so nothing waits; it also finds the largest
@@ -78,6 +84,7 @@ __global__ void __launch_bounds__(kRowsThreads) k_head_rows(RowsArgs a) {
   const int first = blockIdx.x * a.per, last = min(first + a.per, p.rows);
   int before = 0, all = 0;
   float top = 0.0f;
+#pragma unroll 8
   for (int i = threadIdx.x; i < p.rows; i += kRowsThreads) {
     const float f = row_factor(a, a.r0 + i);
     all += f != 0.0f;
@@ -94,7 +101,7 @@ __global__ void __launch_bounds__(kRowsThreads) k_head_rows(RowsArgs a) {
   before = all = 0, top = 0.0f;
   for (int w = 0; w < warps; w++) before += s_before[w], all += s_all[w], top = fmaxf(top, s_top[w]);
   const float post = a.scaled ? pow2_above(top) * pow2_whole(-kHalfScale) : 1.0f;
-  if (blockIdx.x == 0 && threadIdx.x == 0) *p.count = all, *p.failed = 0, *p.again = a.scaled, *p.post = post;
+  if (blockIdx.x == 0 && threadIdx.x == 0) *p.count = all, *p.failed = 0, *p.again = a.again, *p.post = post;
 
   for (int i0 = first; i0 < last; i0 += 32) {
     const long long mine = i0 + lane;
@@ -108,30 +115,40 @@ __global__ void __launch_bounds__(kRowsThreads) k_head_rows(RowsArgs a) {
         if (lane == 0 && a.lse_out) a.lse_out[r] = 0.0f;
         if (a.out.grad) {
           T* o = (T*)a.out.grad + b * a.out.stride_b + at * a.out.stride_n;
-          for (int k = lane; k < p.d; k += 32) o[k] = of_float<T>(0.0f);
+          const int words = (uintptr_t)o % 16 == 0 ? p.d / 8 : 0;
+          for (int k = lane; k < words; k += 32) ((uint4*)o)[k] = make_uint4(0, 0, 0, 0);
+          for (int k = words * 8 + lane; k < p.d; k += 32) o[k] = of_float<T>(0.0f);
         }
         continue;
       }
       const int q = before + __popc(there & ((1u << j) - 1)), y = a.target[r];
       const T* h = (const T*)a.hidden + b * a.stride_b + at * a.stride_n;
       const T* w = (const T*)p.head + y * p.ldw;
-      T* hc = (T*)p.hc + q * p.ldh;
-      float ref = 0.0f, dot = 0.0f;
-      if (a.lse) ref = lse_ref(a.lse[r], a.scaled);
-      for (int k = lane; k < p.ldh; k += 32) {
-        const float x = k < p.d ? as_float(h[k]) : 0.0f;
-        hc[k] = of_float<T>(x);
-        if (a.probs && k < p.d) dot = fmaf(x, as_float(w[k]), dot);
+      uint4* hc = (uint4*)((T*)p.hc + q * p.ldh);
+      float dot = 0.0f;
+      const bool whole = (uintptr_t)h % 16 == 0;
+#pragma unroll 4
+      for (int k = lane * 8; k < p.ldh; k += 256) {
+        const Chunk<T> x(h + k, p.d - k, whole);
+        uint4 v;
+        T* t = (T*)&v;
+#pragma unroll
+        for (int i = 0; i < 8; i++) t[i] = of_float<T>(x.v[i]);
+        hc[k / 8] = v;
+        if (a.probs) {
+          const Chunk<T> y(w + k, p.d - k, true);
+#pragma unroll
+          for (int i = 0; i < 8; i++) dot = fmaf(x.v[i], y.v[i], dot);
+        }
       }
-      if (a.probs) {
+      if (a.probs)
         for (int o = 16; o; o >>= 1) dot += __shfl_xor_sync(~0u, dot, o);
-        ref = whole_ref(dot);
-      }
       if (lane == 0) {
         p.src[q] = (int)i;
         p.tgt[q] = y;
         p.g[q] = g;
-        p.ref[q] = ref;
+        if (a.probs) p.ref[q] = whole_ref(dot);
+        if (a.lse) know(p, q, a.lse[r], g, post);
       }
     }
     before += __popc(there);
@@ -139,96 +156,128 @@ __global__ void __launch_bounds__(kRowsThreads) k_head_rows(RowsArgs a) {
   // rows up to the end of the tile
   const int end = (all + kRowTile - 1) / kRowTile * kRowTile;
   for (int q = all + blockIdx.x * warps + warp; q < end; q += gridDim.x * warps)
-    for (int k = lane; k < p.ldh; k += 32)
-      ((T*)p.hc)[q * p.ldh + k] = ((T*)p.hs)[q * p.ldh + k] = of_float<T>(0.0f);
+    for (int k = lane * 8; k < p.ldh; k += 256) {
+      *(uint4*)((T*)p.hc + q * p.ldh + k) = make_uint4(0, 0, 0, 0);
+      if (p.hs) *(uint4*)((T*)p.hs + q * p.ldh + k) = make_uint4(0, 0, 0, 0);
+    }
 }
 
-constexpr int kMeetRows = 32, kMeetWarps = 16;
+constexpr int kMeetRows = 8, kMeetWarps = 8;
 
 struct MeetArgs {
   HeadPlan p;
   long long r0;
   const float* weight;
   float *loss, *lse;  // by position, or NULL
-  bool probs;         // exponentials are wanted: factors, and hs
-  bool stored;        // they are in e already, relative to p.ref
-  bool known;         // p.ref comes from the logsumexp: no row can have left its window
+  bool grads;         // factors are wanted, and hs
+  bool stored;        // e is there
+  bool known;         // as gradients of logits
 };
 
-// Loss and factors of 32 packed rows from their records; a lane a row, the records dealt to the warps and met in a fixed
-// order.
+// Loss and factors of 8 packed rows from their records: 8 lanes a row's, the records dealt to 32 groups of them and met in a
+// fixed order.
 template <typename T>
 __global__ void __launch_bounds__(kMeetWarps * 32) k_head_meet(MeetArgs a) {
-  __shared__ float s_ref[kMeetWarps][32], s_sum[kMeetWarps][32], s_scale[32];
-  __shared__ int s_left[kMeetWarps][32];
+  __shared__ float s_ref[kMeetWarps][kMeetRows], s_sum[kMeetWarps][kMeetRows], s_coef[kMeetRows];
+  __shared__ int s_left[kMeetWarps][kMeetRows];
   const HeadPlan& p = a.p;
-  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-  const int n = *p.count, q0 = blockIdx.x * kMeetRows, q = q0 + lane;
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, at = lane % kMeetRows;
+  const int n = *p.count, q0 = blockIdx.x * kMeetRows, q = q0 + at;
   if (q0 >= n) return;
   float ref = kNoRef, s = 0.0f;
   int left = 0;
   if (q < n) {
-    const float own = a.stored ? p.ref[q] : 0.0f;
+    const float own = a.stored && !a.known ? p.ref[q] : 0.0f;
 #pragma unroll 4
-    for (int t = warp; t < p.nrec; t += kMeetWarps) {
+    for (int t = warp * 4 + lane / kMeetRows; t < p.nrec; t += kMeetWarps * 4) {
       const float2 x = p.rec[(long long)t * p.cap + q];
       left |= a.stored && x.x != own;
       meet(ref, s, x.x, x.y);
     }
   }
-  s_ref[warp][lane] = ref, s_sum[warp][lane] = s, s_left[warp][lane] = left;
+  for (int o = 16; o >= kMeetRows; o >>= 1) {
+    const float ref2 = __shfl_down_sync(~0u, ref, o), s2 = __shfl_down_sync(~0u, s, o);
+    left |= __shfl_down_sync(~0u, left, o);
+    if (lane < o) meet(ref, s, ref2, s2);
+  }
+  if (lane < kMeetRows) s_ref[warp][at] = ref, s_sum[warp][at] = s, s_left[warp][at] = left;
   __syncthreads();
-  if (warp == 0) {
-    float scale = 0.0f;
+  if (warp == 0 && lane < kMeetRows) {
+    float coef = 0.0f;
     if (q < n) {
       for (int w = 1; w < kMeetWarps; w++) {
         meet(ref, s, s_ref[w][lane], s_sum[w][lane]);
         left |= s_left[w][lane];
       }
-      // the others' sum against the target: loss = log(1 + sum / e_y)
-      const float zt = p.zt[q], by = s == 0.0f && zt > -CUDART_INF_F ? -CUDART_INF_F : log2f(s) + fmaf(-zt, kLog2E, ref);
-      const float x = by * kLn2, rest = log1pf(expf(-fabsf(x)));
-      float nll = x > 0.0f ? x + rest : rest;
-      if (!(zt < CUDART_INF_F) || s != s || *p.failed) nll = CUDART_NAN_F;
-      const float lse = x > 0.0f ? (ref + log2f(s)) * kLn2 + rest : zt + nll;
-      const long long r = a.r0 + p.src[q];
-      if (a.loss) a.loss[r] = (a.weight ? a.weight[r] : 1.0f) * nll;
-      if (a.lse) a.lse[r] = lse;
-      if (a.probs) {
-        float to = p.ref[q];
-        if (!a.known && (!a.stored || left || !(fmaf(zt, kLog2E, -to) <= kWindow))) {
-          to = lse_ref(lse, std::is_same<T, __half>::value);
-          *p.again = 1;
+      if (a.known) {
+        ((T*)p.e)[q * p.lde + p.tgt[q]] = of_float<T>(-s);
+      } else {
+        // the others' sum against the target: loss = log(1 + sum / e_y)
+        const float zt = p.zt[q], by = s == 0.0f && zt > -CUDART_INF_F ? -CUDART_INF_F : log2f(s) + fmaf(-zt, kLog2E, ref);
+        const float x = by * kLn2, small = expf(-fabsf(x)), rest = log1pf(small);
+        float nll = x > 0.0f ? x + rest : rest;
+        if (!(zt < CUDART_INF_F) || s != s || *p.failed) nll = CUDART_NAN_F;
+        const float lse = x > 0.0f ? (ref + log2f(s)) * kLn2 + rest : zt + nll;
+        const long long r = a.r0 + p.src[q];
+        a.loss[r] = (a.weight ? a.weight[r] : 1.0f) * nll;
+        if (a.lse) a.lse[r] = lse;
+        if (a.grads) {
+          const float g = p.g[q], post = *p.post;
+          know(p, q, lse, g, post);
+          p.known_at[q] = -(g / post) * ((x > 0.0f ? 1.0f : small) / (1.0f + small));
+          if (a.stored) {
+            const float to = p.ref[q];
+            if (left || !(fmaf(zt, kLog2E, -to) <= kWindow)) *p.again = 1;
+            const float others = s == 0.0f ? 0.0f : s * pow2_whole(ref - to);
+            coef = g / (others + ex2(fmaf(zt, kLog2E, -to)));
+            p.coef[q] = coef;
+            ((T*)p.e)[q * p.lde + p.tgt[q]] = of_float<T>(-others);
+          }
         }
-        const float others = s == 0.0f ? 0.0f : s * pow2_whole(ref - to);
-        const float coef = p.g[q] / (others + ex2(fmaf(zt, kLog2E, -to)));
-        p.ref[q] = to;
-        p.at[q] = -others;
-        p.coef[q] = coef;
-        if (a.stored) ((T*)p.e)[q * p.lde + p.tgt[q]] = of_float<T>(-others);
-        scale = coef / *p.post;
       }
     }
-    s_scale[lane] = scale;
+    s_coef[lane] = coef;
   }
-  if (!a.probs) return;
+  if (!p.hs) return;
   __syncthreads();
-  for (int j = warp; j < min(kMeetRows, n - q0); j += kMeetWarps) {
-    const T* hc = (const T*)p.hc + (q0 + j) * p.ldh;
-    T* hs = (T*)p.hs + (q0 + j) * p.ldh;
-    const float scale = s_scale[j];
-    for (int k = lane; k < p.ldh; k += 32) hs[k] = of_float<T>(as_float(hc[k]) * scale);
+  if (q0 + warp >= n) return;
+  const T* hc = (const T*)p.hc + (long long)(q0 + warp) * p.ldh;
+  uint4* hs = (uint4*)((T*)p.hs + (long long)(q0 + warp) * p.ldh);
+  const float coef = s_coef[warp];
+#pragma unroll 4
+  for (int k = lane * 8; k < p.ldh; k += 256) {
+    const Chunk<T> x(hc + k, 8, true);
+    uint4 v;
+    T* t = (T*)&v;
+#pragma unroll
+    for (int i = 0; i < 8; i++) t[i] = of_float<T>(x.v[i] * coef);
+    hs[k / 8] = v;
   }
 }
 
-// The head at rows of a multiple of 16 bytes, a warp a row
+// The head at rows of a multiple of 16 bytes, a warp a row.  8 elements come from the two aligned chunks of 16 bytes that they
+// lie in; the first and the last chunk of a row may hold bytes next to it, within the same 16.
 template <typename T>
 __global__ void __launch_bounds__(256) k_head_pack(const T* head, long long stride, T* to, long long ld, int d, int V) {
   const int lane = threadIdx.x % 32;
   for (long long v = blockIdx.x * 8ll + threadIdx.x / 32; v < V; v += gridDim.x * 8ll) {
-    const T* w = head + v * stride;
-#pragma unroll 8
-    for (int k = lane; k < ld; k += 32) to[v * ld + k] = k < d ? w[k] : of_float<T>(0.0f);
+    const uintptr_t w = (uintptr_t)(head + v * stride), end = w + d * sizeof(T);
+    const uint32_t m = w % 16;
+#pragma unroll 4
+    for (int k = lane * 8; k < ld; k += 256) {
+      const uintptr_t from = w - m + k * sizeof(T);
+      const uint4 none = make_uint4(0, 0, 0, 0);
+      const uint4 x = shifted(*(const uint4*)from, m && from + 16 < end ? *(const uint4*)(from + 16) : none, m);
+      const uint32_t y[4] = {x.x, x.y, x.z, x.w};
+      uint4 out;
+      uint32_t* o = (uint32_t*)&out;
+#pragma unroll
+      for (int i = 0; i < 4; i++) {  // two elements
+        const int left = d - k - 2 * i;
+        o[i] = left >= 2 ? y[i] : left == 1 ? y[i] & 0xffff : 0u;
+      }
+      *(uint4*)(to + v * ld + k) = out;
+    }
   }
 }
 
@@ -297,9 +346,9 @@ size_t plan_head(const HeadCall& c, void* base, HeadPlan& p) {
   w.take(p.post, 1, 4);
   w.take(p.src, cap, 4);
   w.take(p.tgt, cap, 4);
-  for (float** f : {&p.g, &p.ref, &p.coef, &p.at, &p.zt}) w.take(*f, cap, 4);
+  for (float** f : {&p.g, &p.zt, &p.ref, &p.coef, &p.known_ref, &p.known_mul, &p.known_at}) w.take(*f, cap, 4);
   w.take(p.hc, cap * p.ldh, 2);
-  w.take(p.hs, cap * p.ldh, 2);
+  if (c.form == kStep && c.dtype == EPIC_BF16) w.take(p.hs, cap * p.ldh, 2);
   w.take(p.rec, cap * p.nrec, sizeof(float2));
   if (c.form != kForward) {
     w.take(p.e, cap * p.lde, 2);
@@ -372,20 +421,21 @@ epic_status run_head(const HeadCall& c, const HeadTensors& t, HeadPlan p, cudaSt
     a.loss = t.loss;
     a.lse_out = t.lse;
     a.out = {t.grad_hidden, t.gstride_b, t.gstride_n, r0, c.n};
-    a.per = std::max(8, (p.rows + 511) / 512);
-    a.probs = c.form == kStep && !half;
+    a.per = std::max(8, (p.rows + 303) / 304);
+    const bool known = c.form == kBackward, stored = known || (grads && !half);
+    a.probs = stored && !known;
     a.scaled = half && grads;
+    a.again = known || a.scaled;
     k_head_rows<T><<<(p.rows + a.per - 1) / a.per, kRowsThreads, 0, st>>>(a);
     EPIC_TRY(last_error());
     if (c.V == 0) continue;
     // A step's exponentials are relative to the target's logit; fp16 has not the range for that and makes them once the
     // logsumexp is known, as do rows that leave the window.
-    const bool known = c.form == kBackward, stored = known || a.probs;
-    EPIC_TRY(launch_head_logits(p, c.dtype, {true, stored, false}, st));
-    MeetArgs m = {p, r0, t.weight, t.loss, t.lse, grads, stored, known};
+    EPIC_TRY(launch_head_logits(p, c.dtype, {true, stored, known, false}, st));
+    const MeetArgs m = {p, r0, t.weight, t.loss, t.lse, grads, stored, known};
     k_head_meet<T><<<(p.rows + kMeetRows - 1) / kMeetRows, kMeetWarps * 32, 0, st>>>(m);
     EPIC_TRY(last_error());
-    if (grads && !known) EPIC_TRY(launch_head_logits(p, c.dtype, {false, true, true}, st));
+    if (grads && !known) EPIC_TRY(launch_head_logits(p, c.dtype, {false, true, true, true}, st));
     if (t.grad_hidden || t.grad_head) {
       const bool first = r0 == 0, last = r0 + p.cap >= rows;
       const HeadSum sum = first ? (last ? kOnly : kFirst) : last ? kLast : kMiddle;

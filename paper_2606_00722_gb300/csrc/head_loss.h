@@ -29,17 +29,20 @@ struct HeadPlan {
   const void* head;         // [V][ldw]
   int* count;               // rows that count
   int* failed;              // != 0: a wait gave up
-  int* again;               // != 0: rows whose exponentials left the window of their reference
-  float* post;              // what gradients of the head are multiplied with at the end
+  int* again;               // != 0: e holds gradients of logits; see below
+  float* post;              // power of two that gradients of logits in e are multiplied with
   int* src;                 // [cap] position in the piece
   int* tgt;                 // [cap] target token
   float *g;                 // [cap] what the row's gradient is multiplied with (weight, gradient from above)
-  float *ref;               // [cap] exponentials are 2^(z log2 e - ref), ref a whole number
-  float *coef;              // [cap] gradient of a logit = coef (e - its sum at the target)
-  float *at;                // [cap] the row's e at the target: minus the sum of the others
   float *zt;                // [cap] logit of the target
+  // Either e = 2^(z log2 e - ref), ref a whole number; a gradient of a logit is coef e, and hs = coef h.
+  float *ref, *coef;        // [cap]
+  // Or, where the logsumexp is known, e = known_mul 2^(z log2 e - known_ref), gradients of logits / *post.
+  float *known_ref, *known_mul;  // [cap]
+  // At the target e is minus the sum of the others, so that little is lost where they are few.
+  float *known_at;          // [cap] that
   float2* rec;              // [nrec][cap] (whole reference, sum of exponentials relative to it), target left out
-  void *hc, *hs;            // [cap][ldh] hidden states; the same times coef / *post
+  void *hc, *hs;            // [cap][ldh] hidden states; the same times coef, or NULL
   void* e;                  // [cap][lde]
   float* acc;               // [V][ldp] or NULL: gradient of the head so far, of calls in several pieces
   long long ldp;            // elements from row to row of acc and of parts, a multiple of 32
@@ -56,14 +59,14 @@ struct HiddenGrad {
   int n;
 };
 
-// Logits of the packed rows.  sums: records and target logits.  probs: exponentials into e.  only_again: nothing unless
-// *again; then with `at` at the targets.
+// Logits of the packed rows.  sums: records and target logits.  probs: e, with a known logsumexp or not.  only_again: nothing
+// unless *again; then with known_at at the targets.
 struct LogitsPass {
-  bool sums, probs, only_again;
+  bool sums, probs, known, only_again;
 };
 epic_status launch_head_logits(const HeadPlan& p, int dtype, const LogitsPass& pass, cudaStream_t st);
-// Gradients of hidden states, grad[src] = coef e W (out.grad NULL: none), and of the head, grad_head [V][stride] = post e^T hs
-// with the pieces before (NULL: none)
+// Gradients of hidden states, grad[src] = coef e W (out.grad NULL: none), and of the head, grad_head [V][stride] = e^T hs with
+// the pieces before (NULL: none); of gradients of logits in e, post e W and post e^T hc.
 epic_status launch_head_grads(const HeadPlan& p, int dtype, const HiddenGrad& out, void* grad_head, long long stride,
                               HeadSum sum, cudaStream_t st);
 GradSplit split_grads(int rows, int d, int V);
