@@ -115,9 +115,11 @@ __device__ __forceinline__ void store_sector(void* to, const uint32_t (&v)[16], 
 }
 
 // 32 elements of each lane's row to `to` (NULL: none), of which the first `count` exist (the same in all lanes).  Rows that
-// start at any element are turned in shared memory, so that lanes write one row's elements.
+// start at any element are turned in shared memory, so that lanes write one row's elements: half a warp a row, two elements a
+// lane from the row's first multiple of 4 bytes on.  The loop has no branches but predicates: waits for one row's
+// elements are no waits for the next's.
 template <typename T>
-__device__ __forceinline__ void store_rows(T* to, const float (&v)[32], int count, bool whole, T* turn, int lane) {
+__device__ __forceinline__ void store_rows(T* to, const float (&v)[32], int count, bool whole, uint16_t* turn, int lane) {
   uint32_t w[16];
 #pragma unroll
   for (int j = 0; j < 16; j++) w[j] = pack2<T>(v[2 * j], v[2 * j + 1]);
@@ -132,21 +134,26 @@ __device__ __forceinline__ void store_rows(T* to, const float (&v)[32], int coun
 #pragma unroll
   for (int j = 0; j < 16; j++) ((uint32_t*)(turn + lane * kTurnRow))[j] = w[j];
   __syncwarp();
-  // half a warp a row, two elements a lane from the first multiple of 4 bytes on; its last lane also has the element before
   const int at = lane % 16;
-#pragma unroll 4
-  for (int r = lane / 16; r < 32; r += 2) {
-    T* row = (T*)__shfl_sync(~0u, (unsigned long long)to, r);
-    if (!row) continue;
-    const T* v = turn + r * kTurnRow;
-    const int odd = (uintptr_t)row / 2 % 2, j = 2 * at + odd;
-    if (j + 1 < min(count, 32)) {
-      const T two[2] = {v[j], v[j + 1]};
-      *(uint32_t*)(row + j) = (uint32_t)*(const uint16_t*)&two[0] | (uint32_t)*(const uint16_t*)&two[1] << 16;
-    } else if (j < min(count, 32)) {
-      row[j] = v[j];
+  count = min(count, 32);
+#pragma unroll
+  for (int r0 = 0; r0 < 32; r0 += 8) {
+    uint16_t* row[4];
+    uint32_t two[4];
+    int j[4];
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      const int r = r0 + 2 * i + lane / 16;
+      row[i] = (uint16_t*)__shfl_sync(~0u, (unsigned long long)to, r);
+      j[i] = 2 * at + (int)((uintptr_t)row[i] / 2 % 2);
+      two[i] = turn[r * kTurnRow + j[i]] | (uint32_t)turn[r * kTurnRow + j[i] + 1] << 16;
     }
-    if (odd && at == 15) row[0] = v[0];
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      if (row[i] && j[i] + 1 < count) *(uint32_t*)(row[i] + j[i]) = two[i];
+      if (row[i] && j[i] + 1 == count) row[i][j[i]] = (uint16_t)two[i];
+      if (row[i] && j[i] == 1) row[i][0] = turn[(r0 + 2 * i + lane / 16) * kTurnRow];
+    }
   }
 }
 
@@ -249,17 +256,17 @@ __device__ __forceinline__ void store_part(float* part, const float (&v)[32]) {
   for (int j = 0; j < 32; j += 4) ((float4*)part)[j / 4] = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
 }
 
-// Sums of a gradient's tile: kHalf columns of each lane's row
+// Sums of a gradient's tile: kHalf columns of each lane's row, two loads of 32 at a time
 template <typename T>
-__device__ __forceinline__ void grad_rows(const TileArgs& a, int n, bool again, const Task& t, uint32_t sums, int row, int col,
-                                          T* turn, int lane) {
+__device__ __forceinline__ void grad_rows(const TileArgs& a, int n, bool again, float post, const Task& t, uint32_t sums,
+                                          int row, int col, uint16_t* turn, int lane) {
   const HeadPlan& p = a.p;
   const GradSplit& sp = a.p.split;
   const bool hidden = t.job == 0;
   const bool parts = (hidden ? sp.hidden_parts : sp.head_parts) > 1;
   const bool there = row < (hidden ? n : p.V);
   T* to = nullptr;
-  float scale = again ? *p.post : 1.0f;
+  float scale = post;
   if (there && !parts) {
     if (hidden) {
       const long long r = a.out.r0 + p.src[row];
@@ -272,22 +279,20 @@ __device__ __forceinline__ void grad_rows(const TileArgs& a, int n, bool again, 
   const bool whole = __all_sync(~0u, ((uintptr_t)(to + col) & 31) == 0 || !to);
   float* part = hidden ? sp.hidden + ((long long)t.part * p.cap + row) * p.ldp : sp.head + ((long long)t.part * p.V + row) * p.ldp;
   float* acc = p.acc + (long long)row * p.ldp;
-#pragma unroll 1
-  for (int c = col; c < col + kHalf && c < p.d; c += 32) {
-    float v[32];
-    if (t.steps > 0) {
-      sums_load(sums + (c - col), v);
-      sums_loaded(v);
-    } else {
+  auto store = [&](float(&v)[32], int c) {
+    if (c >= p.d) return;
+    if (t.steps <= 0) {
 #pragma unroll
       for (int j = 0; j < 32; j++) v[j] = 0.0f;
     }
     if (parts) {
       if (there) store_part<T>(part + c, v);
-      continue;
+      return;
     }
+    if (hidden || post != 1.0f) {
 #pragma unroll
-    for (int j = 0; j < 32; j++) v[j] *= scale;
+      for (int j = 0; j < 32; j++) v[j] *= scale;
+    }
     if (!hidden && a.sum != kOnly && there) {
       if (a.sum != kFirst) {
 #pragma unroll
@@ -296,6 +301,18 @@ __device__ __forceinline__ void grad_rows(const TileArgs& a, int n, bool again, 
       if (a.sum != kLast) store_part<T>(acc + c, v);
     }
     if (hidden || a.sum == kOnly || a.sum == kLast) store_rows<T>(to ? to + c : nullptr, v, p.d - c, whole, turn, lane);
+  };
+#pragma unroll 1
+  for (int c = col; c < col + kHalf && c < p.d; c += 64) {
+    float v[32], w[32];
+    if (t.steps > 0) {
+      sums_load(sums + (c - col), v);
+      sums_load(sums + (c - col) + 32, w);
+      sums_loaded(v);
+      sums_loaded(w);
+    }
+    store(v, c);
+    store(w, c + 32);
   }
 }
 
@@ -310,7 +327,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   const int n = *a.p.count;
   uint8_t* shared = (uint8_t*)(((uintptr_t)shared_raw + 1023) / 1024 * 1024);
   const uint32_t stages = smem_address(shared);
-  T* turns = (T*)(shared + kStages * kStage);
+  uint16_t* turns = (uint16_t*)(shared + kStages * kStage);
   const int warp = warp_of_thread(), lane = threadIdx.x % 32, pair = blockIdx.x / 2;
   const uint32_t rank = cluster_rank();
   const uint32_t full = smem_address(bars.full), empty = smem_address(bars.empty);
@@ -404,7 +421,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     }
   } else if (warp >= 4) {
     const int part = warp - 4, quarter = warp % 4;
-    T* turn = turns + part * 32 * kTurnRow;
+    uint16_t* turn = turns + part * 32 * kTurnRow;
+    const float post = kForm == 2 && again ? *a.p.post : 1.0f;
     int use = 0;
     Task t;
     for (int i = 0; task(i, t); i++) {
@@ -416,7 +434,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         products_fence_after();
       }
       if (kForm == 2) {
-        grad_rows<T>(a, n, again, t, from, row, t.n0 + off, turn, lane);
+        grad_rows<T>(a, n, again, post, t, from, row, t.n0 + off, turn, lane);
       } else if (row - lane < up_div(n, kStepK) * kStepK) {
         logits_rows<T, kForm == 1>(a, n, from, row, t.n0 + off, lane);
       }

@@ -29,8 +29,10 @@
 namespace epic {
 namespace {
 
-constexpr int kPieceRows = 16384;  // most positions of a piece: each CTA of k_head_rows counts over all of them
+constexpr int kPieceRows = 16384;  // most positions of a piece
 constexpr int kRowsThreads = 256;
+constexpr int kFewRows = 608;   // positions that have a CTA each
+constexpr int kCounted = 1024;  // more positions are counted by a kernel before
 
 struct RowsArgs {
   HeadPlan p;
@@ -44,7 +46,7 @@ struct RowsArgs {
   const float* lse;       // the backward pass, else NULL
   float *loss, *lse_out;  // of positions that do not count: 0; or NULL
   HiddenGrad out;         // grad NULL: none
-  int per;                // positions of a CTA
+  int per;                // positions of a CTA, a power of two up to 256
   bool probs;             // rows' references are wanted (a step in bf16)
   bool scaled;            // fp16: gradients of logits relative to the largest factor, times 2^14
   bool again;             // gradients of logits are from a known logsumexp
@@ -73,29 +75,62 @@ __device__ __forceinline__ void know(const HeadPlan& p, int q, float lse, float 
   p.known_mul[q] = g / post * ex2(fmaf(-lse, kLog2E, ref));
 }
 
+__device__ __forceinline__ void sum_and_top(int& count, float& top) {
+  for (int o = 16; o; o >>= 1) {
+    count += __shfl_xor_sync(~0u, count, o);
+    top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
+  }
+}
+
+// How many of 256 positions count, and their largest factor
+__global__ void __launch_bounds__(kRowsThreads) k_head_count(RowsArgs a) {
+  __shared__ int s_count[kRowsThreads / 32];
+  __shared__ float s_top[kRowsThreads / 32];
+  const int i = blockIdx.x * kRowsThreads + threadIdx.x;
+  float top = i < a.p.rows ? fabsf(row_factor(a, a.r0 + i)) : 0.0f;
+  int count = top != 0.0f;
+  sum_and_top(count, top);
+  if (threadIdx.x % 32 == 0) s_count[threadIdx.x / 32] = count, s_top[threadIdx.x / 32] = top;
+  __syncthreads();
+  if (threadIdx.x >= 32) return;
+  count = threadIdx.x < kRowsThreads / 32 ? s_count[threadIdx.x] : 0;
+  top = threadIdx.x < kRowsThreads / 32 ? s_top[threadIdx.x] : 0.0f;
+  sum_and_top(count, top);
+  if (threadIdx.x == 0) a.p.counts[blockIdx.x] = count, a.p.tops[blockIdx.x] = top;
+}
+
 // Packs the positions that count.  Every CTA counts those before its own, so nothing waits; it also finds the largest
-// factor.  A warp copies a row, and with `probs` takes its product with the target's row of the head.
-template <typename T>
+// factor.  A warp copies a row, or with few rows a CTA (kWide), and with `probs` takes its product with the target's row of
+// the head.
+template <typename T, bool kWide>
 __global__ void __launch_bounds__(kRowsThreads) k_head_rows(RowsArgs a) {
   __shared__ int s_before[kRowsThreads / 32], s_all[kRowsThreads / 32];
-  __shared__ float s_top[kRowsThreads / 32];
+  __shared__ float s_top[kRowsThreads / 32], s_dot[kRowsThreads / 32];
   const HeadPlan& p = a.p;
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, warps = kRowsThreads / 32;
   const int first = blockIdx.x * a.per, last = min(first + a.per, p.rows);
   int before = 0, all = 0;
   float top = 0.0f;
-#pragma unroll 8
-  for (int i = threadIdx.x; i < p.rows; i += kRowsThreads) {
-    const float f = row_factor(a, a.r0 + i);
-    all += f != 0.0f;
-    before += f != 0.0f && i < first;
-    top = fmaxf(top, fabsf(f));
+  if (p.rows > kCounted) {
+    const int own = first / kRowsThreads;
+    if (threadIdx.x * kRowsThreads < p.rows) {
+      all = p.counts[threadIdx.x];
+      top = p.tops[threadIdx.x];
+      if (threadIdx.x < own) before = all;
+    }
+    const int i = own * kRowsThreads + threadIdx.x;
+    if (i < first) before += row_factor(a, a.r0 + i) != 0.0f;
+  } else {
+#pragma unroll 4
+    for (int i = threadIdx.x; i < p.rows; i += kRowsThreads) {
+      const float f = row_factor(a, a.r0 + i);
+      all += f != 0.0f;
+      before += f != 0.0f && i < first;
+      top = fmaxf(top, fabsf(f));
+    }
   }
-  for (int o = 16; o; o >>= 1) {
-    before += __shfl_xor_sync(~0u, before, o);
-    all += __shfl_xor_sync(~0u, all, o);
-    top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
-  }
+  sum_and_top(all, top);
+  before = __reduce_add_sync(~0u, before);
   if (lane == 0) s_before[warp] = before, s_all[warp] = all, s_top[warp] = top;
   __syncthreads();
   before = all = 0, top = 0.0f;
@@ -103,32 +138,33 @@ __global__ void __launch_bounds__(kRowsThreads) k_head_rows(RowsArgs a) {
   const float post = a.scaled ? pow2_above(top) * pow2_whole(-kHalfScale) : 1.0f;
   if (blockIdx.x == 0 && threadIdx.x == 0) *p.count = all, *p.failed = 0, *p.again = a.again, *p.post = post;
 
+  const int at = kWide ? threadIdx.x : lane, step = kWide ? kRowsThreads : 32;  // in a row
   for (int i0 = first; i0 < last; i0 += 32) {
     const long long mine = i0 + lane;
     const float f = mine < last ? row_factor(a, a.r0 + mine) : 0.0f;
     const unsigned there = __ballot_sync(~0u, f != 0.0f);
-    for (int j = warp; j < min(32, last - i0); j += warps) {
-      const long long i = i0 + j, r = a.r0 + i, b = r / a.n, at = r % a.n;
+    for (int j = kWide ? 0 : warp; j < min(32, last - i0); j += kWide ? 1 : warps) {
+      const long long i = i0 + j, r = a.r0 + i, b = r / a.n, pos = r % a.n;
       const float g = __shfl_sync(~0u, f, j);
       if (g == 0.0f) {
-        if (lane == 0 && a.loss) a.loss[r] = 0.0f;
-        if (lane == 0 && a.lse_out) a.lse_out[r] = 0.0f;
+        if (at == 0 && a.loss) a.loss[r] = 0.0f;
+        if (at == 0 && a.lse_out) a.lse_out[r] = 0.0f;
         if (a.out.grad) {
-          T* o = (T*)a.out.grad + b * a.out.stride_b + at * a.out.stride_n;
+          T* o = (T*)a.out.grad + b * a.out.stride_b + pos * a.out.stride_n;
           const int words = (uintptr_t)o % 16 == 0 ? p.d / 8 : 0;
-          for (int k = lane; k < words; k += 32) ((uint4*)o)[k] = make_uint4(0, 0, 0, 0);
-          for (int k = words * 8 + lane; k < p.d; k += 32) o[k] = of_float<T>(0.0f);
+          for (int k = at; k < words; k += step) ((uint4*)o)[k] = make_uint4(0, 0, 0, 0);
+          for (int k = words * 8 + at; k < p.d; k += step) o[k] = of_float<T>(0.0f);
         }
         continue;
       }
       const int q = before + __popc(there & ((1u << j) - 1)), y = a.target[r];
-      const T* h = (const T*)a.hidden + b * a.stride_b + at * a.stride_n;
+      const T* h = (const T*)a.hidden + b * a.stride_b + pos * a.stride_n;
       const T* w = (const T*)p.head + y * p.ldw;
       uint4* hc = (uint4*)((T*)p.hc + q * p.ldh);
       float dot = 0.0f;
       const bool whole = (uintptr_t)h % 16 == 0;
 #pragma unroll 4
-      for (int k = lane * 8; k < p.ldh; k += 256) {
+      for (int k = at * 8; k < p.ldh; k += step * 8) {
         const Chunk<T> x(h + k, p.d - k, whole);
         uint4 v;
         T* t = (T*)&v;
@@ -141,9 +177,16 @@ __global__ void __launch_bounds__(kRowsThreads) k_head_rows(RowsArgs a) {
           for (int i = 0; i < 8; i++) dot = fmaf(x.v[i], y.v[i], dot);
         }
       }
-      if (a.probs)
+      if (a.probs) {
         for (int o = 16; o; o >>= 1) dot += __shfl_xor_sync(~0u, dot, o);
-      if (lane == 0) {
+        if (kWide) {
+          if (lane == 0) s_dot[warp] = dot;
+          __syncthreads();
+          dot = 0.0f;
+          for (int w = 0; w < warps; w++) dot += s_dot[w];
+        }
+      }
+      if (at == 0) {
         p.src[q] = (int)i;
         p.tgt[q] = y;
         p.g[q] = g;
@@ -162,7 +205,7 @@ __global__ void __launch_bounds__(kRowsThreads) k_head_rows(RowsArgs a) {
     }
 }
 
-constexpr int kMeetRows = 8, kMeetWarps = 8;
+constexpr int kMeetWarps = 8;
 
 struct MeetArgs {
   HeadPlan p;
@@ -174,9 +217,9 @@ struct MeetArgs {
   bool known;         // as gradients of logits
 };
 
-// Loss and factors of 8 packed rows from their records: 8 lanes a row's, the records dealt to 32 groups of them and met in a
-// fixed order.
-template <typename T>
+// Loss and factors of kMeetRows (8, or with few rows 1) packed rows from their records: as many lanes, the records dealt to
+// groups of them and met in a fixed order.
+template <typename T, int kMeetRows>
 __global__ void __launch_bounds__(kMeetWarps * 32) k_head_meet(MeetArgs a) {
   __shared__ float s_ref[kMeetWarps][kMeetRows], s_sum[kMeetWarps][kMeetRows], s_coef[kMeetRows];
   __shared__ int s_left[kMeetWarps][kMeetRows];
@@ -189,7 +232,7 @@ __global__ void __launch_bounds__(kMeetWarps * 32) k_head_meet(MeetArgs a) {
   if (q < n) {
     const float own = a.stored && !a.known ? p.ref[q] : 0.0f;
 #pragma unroll 4
-    for (int t = warp * 4 + lane / kMeetRows; t < p.nrec; t += kMeetWarps * 4) {
+    for (int t = threadIdx.x / kMeetRows; t < p.nrec; t += kMeetWarps * 32 / kMeetRows) {
       const float2 x = p.rec[(long long)t * p.cap + q];
       left |= a.stored && x.x != own;
       meet(ref, s, x.x, x.y);
@@ -240,12 +283,13 @@ __global__ void __launch_bounds__(kMeetWarps * 32) k_head_meet(MeetArgs a) {
   }
   if (!p.hs) return;
   __syncthreads();
-  if (q0 + warp >= n) return;
-  const T* hc = (const T*)p.hc + (long long)(q0 + warp) * p.ldh;
-  uint4* hs = (uint4*)((T*)p.hs + (long long)(q0 + warp) * p.ldh);
-  const float coef = s_coef[warp];
+  const int own = kMeetRows == 1 ? 0 : warp;  // row
+  if (q0 + own >= n) return;
+  const T* hc = (const T*)p.hc + (long long)(q0 + own) * p.ldh;
+  uint4* hs = (uint4*)((T*)p.hs + (long long)(q0 + own) * p.ldh);
+  const float coef = s_coef[own];
 #pragma unroll 4
-  for (int k = lane * 8; k < p.ldh; k += 256) {
+  for (int k = (kMeetRows == 1 ? threadIdx.x : lane) * 8; k < p.ldh; k += kMeetRows == 1 ? kMeetWarps * 256 : 256) {
     const Chunk<T> x(hc + k, 8, true);
     uint4 v;
     T* t = (T*)&v;
@@ -344,6 +388,8 @@ size_t plan_head(const HeadCall& c, void* base, HeadPlan& p) {
   w.take(p.failed, 1, 4);
   w.take(p.again, 1, 4);
   w.take(p.post, 1, 4);
+  w.take(p.counts, kPieceRows / kRowsThreads, 4);
+  w.take(p.tops, kPieceRows / kRowsThreads, 4);
   w.take(p.src, cap, 4);
   w.take(p.tgt, cap, 4);
   for (float** f : {&p.g, &p.zt, &p.ref, &p.coef, &p.known_ref, &p.known_mul, &p.known_at}) w.take(*f, cap, 4);
@@ -421,19 +467,27 @@ epic_status run_head(const HeadCall& c, const HeadTensors& t, HeadPlan p, cudaSt
     a.loss = t.loss;
     a.lse_out = t.lse;
     a.out = {t.grad_hidden, t.gstride_b, t.gstride_n, r0, c.n};
-    a.per = std::max(8, (p.rows + 303) / 304);
+    // Few positions have a CTA each: 32 of 4,096 numbers take 32 us with a warp each.
+    const bool few = p.rows <= kFewRows;
+    a.per = few ? 1 : 8;
     const bool known = c.form == kBackward, stored = known || (grads && !half);
     a.probs = stored && !known;
     a.scaled = half && grads;
     a.again = known || a.scaled;
-    k_head_rows<T><<<(p.rows + a.per - 1) / a.per, kRowsThreads, 0, st>>>(a);
+    if (p.rows > kCounted) {
+      k_head_count<<<(p.rows + kRowsThreads - 1) / kRowsThreads, kRowsThreads, 0, st>>>(a);
+      EPIC_TRY(last_error());
+    }
+    if (few) k_head_rows<T, true><<<p.rows, kRowsThreads, 0, st>>>(a);
+    else k_head_rows<T, false><<<(p.rows + a.per - 1) / a.per, kRowsThreads, 0, st>>>(a);
     EPIC_TRY(last_error());
     if (c.V == 0) continue;
     // A step's exponentials are relative to the target's logit; fp16 has not the range for that and makes them once the
     // logsumexp is known, as do rows that leave the window.
     EPIC_TRY(launch_head_logits(p, c.dtype, {true, stored, known, false}, st));
     const MeetArgs m = {p, r0, t.weight, t.loss, t.lse, grads, stored, known};
-    k_head_meet<T><<<(p.rows + kMeetRows - 1) / kMeetRows, kMeetWarps * 32, 0, st>>>(m);
+    if (few) k_head_meet<T, 1><<<p.rows, kMeetWarps * 32, 0, st>>>(m);
+    else k_head_meet<T, 8><<<(p.rows + 7) / 8, kMeetWarps * 32, 0, st>>>(m);
     EPIC_TRY(last_error());
     if (grads && !known) EPIC_TRY(launch_head_logits(p, c.dtype, {false, true, true, true}, st));
     if (t.grad_hidden || t.grad_head) {

@@ -31,6 +31,8 @@ struct HeadPlan {
   int* failed;              // != 0: a wait gave up
   int* again;               // != 0: e holds gradients of logits; see below
   float* post;              // power of two that gradients of logits in e are multiplied with
+  int* counts;              // of 256 positions each, and the largest factor among them
+  float* tops;
   int* src;                 // [cap] position in the piece
   int* tgt;                 // [cap] target token
   float *g;                 // [cap] what the row's gradient is multiplied with (weight, gradient from above)
