@@ -8,6 +8,7 @@
 #include <cuda.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "head_loss.h"
 #include "head_rows.cuh"
@@ -21,8 +22,7 @@ constexpr int kStepK = 64, kStages = 6;
 constexpr int kOperand = kHalf * kStepK * 2, kStage = 2 * kOperand;  // bytes
 constexpr int kWorkWarps = 8, kThreads = 128 + 32 * kWorkWarps;
 constexpr int kPairs = 76;  // of the GB300's 152 SMs
-constexpr int kTurnRow = 34;  // 16-bit elements from row to row of a warp's turning buffer
-constexpr int kTurn = 32 * kTurnRow * 2;
+constexpr int kTurn = 32 * 128;  // bytes of a warp's turning buffer: 64 elements of 32 rows
 constexpr int kShared = kStages * kStage + kWorkWarps * kTurn + 1024;
 
 struct Bars {
@@ -46,53 +46,110 @@ struct TileArgs {
   long long grad_head_stride;
   HeadSum sum;
   int bf16;
+  bool boxes;  // rows of grad_head start at multiples of 16 bytes and end there (a box's end is cut in whole 16 bytes)
 };
 
 struct Maps {
-  CUtensorMap hc, hc_mn, hs, head_k, head_mn, e_k, e_mn;
+  CUtensorMap hc, hc_mn, hs, head_k, head_mn, e_k, e_mn, e_out, grad_out;
 };
 
 __device__ __forceinline__ int up_div(int a, int b) { return (a + b - 1) / b; }
 
-// The i-th tile of pair `pair`, or false.  Logits: the rows' tiles of one column of tiles after another, so that the head is
-// read once.
-__device__ __forceinline__ bool logits_task(const TileArgs& a, int n, int pair, int i, Task& t) {
-  const int mt = up_div(n, kTile), at = pair + i * kPairs;
-  if (at >= mt * up_div(a.p.V, kTile)) return false;
-  t = {at % mt * kTile, at / mt * kTile, 0, up_div(a.p.d, kStepK), 0, 0};
-  return true;
-}
+// Division by a number that stays
+struct Divisor {
+  uint32_t by, inverse;
+  __device__ __forceinline__ explicit Divisor(int n) : by(n), inverse(0xffffffffu / (uint32_t)n) {}
+  __device__ __forceinline__ int of(int x, int& rest) const {
+    uint32_t q = __umulhi(x, inverse), left = x - q * by;  // q is at most 2 too small
+    while (left >= by) left -= by, q++;
+    rest = (int)left;
+    return (int)q;
+  }
+};
 
-// Gradients: first all tiles of hidden states' (long sums), then the head's.  Where the former do not come out even, the
-// pairs without a last one take as many of the latter as it is worth before the rest is dealt to all.
-__device__ __forceinline__ bool grads_task(const TileArgs& a, int n, int pair, int i, Task& t) {
-  const GradSplit& s = a.p.split;
-  const int ct = up_div(a.p.d, kTile);
-  const int mt = up_div(n, kTile), vt = up_div(a.p.V, kTile);
-  const int hidden = s.hidden_parts * mt * ct, head = s.head_parts * vt * ct;
-  const int own = hidden / kPairs + (pair < hidden % kPairs);
-  if (i < own) {
-    const int at = pair + i * kPairs, part = at / (mt * ct), tile = at % (mt * ct);
-    const int all = up_div(a.p.V, kStepK), k0 = (int)((long long)all * part / s.hidden_parts);
-    t = {tile / ct * kTile, tile % ct * kTile, k0, (int)((long long)all * (part + 1) / s.hidden_parts) - k0, 0, part};
+// The tiles of a pair, one after another.  (Each warp role goes through them for itself; worked out anew for every tile, with
+// its divisions, a tile of one step took 5,400 clocks.)
+//
+// Logits: the rows' tiles of one column of tiles after another, so that the head is read once.
+struct LogitsTasks {
+  Divisor row_tiles;
+  int at, tiles, steps;
+  __device__ __forceinline__ LogitsTasks(const TileArgs& a, int n, int pair)
+      : row_tiles(max(1, up_div(n, kTile))), at(pair), tiles(up_div(n, kTile) * up_div(a.p.V, kTile)),
+        steps(up_div(a.p.d, kStepK)) {}
+  __device__ __forceinline__ bool next(Task& t) {
+    if (at >= tiles) return false;
+    int m;
+    const int column = row_tiles.of(at, m);
+    t = {m * kTile, column * kTile, 0, steps, 0, 0};
+    at += kPairs;
     return true;
   }
-  i -= own;
-  const int all = up_div(n, kStepK), last = hidden % kPairs, idle = last ? kPairs - last : 0;
-  int at;
-  const int per = up_div(all, max(1, s.head_parts)) + s.tile_cost;
-  const int first = idle ? min(head / idle, (up_div(up_div(a.p.V, kStepK), s.hidden_parts) + s.tile_cost) / per) : 0;
-  if (pair >= last && idle) {
-    if (i < first) at = pair - last + i * idle;
-    else at = first * idle + pair + (i - first) * kPairs;
-  } else {
-    at = first * idle + pair + i * kPairs;
+};
+
+// Gradients: tiles of hidden states (long sums) are dealt to the first hidden_pairs pairs, the head's to all, so that the pairs
+// end together: those without a tile of hidden states take as many of the head's as theirs are worth, then those with one
+// less than others, then all.
+struct GradTasks {
+  Divisor columns;
+  int row_tiles, head_tiles, hidden_parts, head_parts, v_steps, r_steps;
+  int hidden, hidden_by, hidden_left;      // the next tile of hidden states, how far the one after is, how many
+  int head[3], by[3], left[3];             // the same of the head's in the three rounds
+  __device__ __forceinline__ GradTasks(const TileArgs& a, int n, int pair) : columns(up_div(a.p.d, kTile)) {
+    const GradSplit& s = a.p.split;
+    const int ct = columns.by, some = s.hidden_pairs;
+    row_tiles = up_div(n, kTile) * ct;
+    head_tiles = up_div(a.p.V, kTile) * ct;
+    hidden_parts = s.hidden_parts;
+    head_parts = s.head_parts;
+    v_steps = up_div(a.p.V, kStepK);
+    r_steps = up_div(n, kStepK);
+    const int all_hidden = hidden_parts * row_tiles, all_head = head_parts * head_tiles, last = all_hidden % some;
+    hidden = pair;
+    hidden_by = some;
+    hidden_left = pair < some ? all_hidden / some + (pair < last) : 0;
+    const int per = up_div(r_steps, max(1, head_parts)) + s.tile_cost, unit = up_div(v_steps, max(1, hidden_parts)) + s.tile_cost;
+    const int none = kPairs - some, less = last ? kPairs - last : 0;
+    const int first = none ? min(all_head / none, (int)((long long)(all_hidden / some) * unit / per)) : 0;
+    const int second = less ? min((all_head - first * none) / less, unit / per) : 0;
+    head[0] = pair - some, by[0] = none, left[0] = pair >= some ? first : 0;
+    head[1] = first * none + pair - last, by[1] = less, left[1] = pair >= last ? second : 0;
+    head[2] = first * none + second * less + pair, by[2] = kPairs;
+    left[2] = head[2] < all_head ? (all_head - head[2] + kPairs - 1) / kPairs : 0;
   }
-  if (at >= head) return false;
-  const int part = at / (vt * ct), tile = at % (vt * ct), k0 = (int)((long long)all * part / s.head_parts);
-  t = {tile / ct * kTile, tile % ct * kTile, k0, (int)((long long)all * (part + 1) / s.head_parts) - k0, 1, part};
-  return true;
-}
+  __device__ __forceinline__ void sum(Task& t, int job, int at, int tiles, int parts, int steps) const {
+    int part = 0, c;
+    t.k0 = 0;
+    t.steps = steps;
+    if (parts > 1) {
+      part = at / tiles;
+      at -= part * tiles;
+      t.k0 = (int)((long long)steps * part / parts);
+      t.steps = (int)((long long)steps * (part + 1) / parts) - t.k0;
+    }
+    t.m0 = columns.of(at, c) * kTile;
+    t.n0 = c * kTile;
+    t.job = job;
+    t.part = part;
+  }
+  __device__ __forceinline__ bool next(Task& t) {
+    if (hidden_left > 0) {
+      sum(t, 0, hidden, row_tiles, hidden_parts, v_steps);
+      hidden += hidden_by;
+      hidden_left--;
+      return true;
+    }
+#pragma unroll
+    for (int i = 0; i < 3; i++) {
+      if (left[i] <= 0) continue;
+      sum(t, 1, head[i], head_tiles, head_parts, r_steps);
+      head[i] += by[i];
+      left[i]--;
+      return true;
+    }
+    return false;
+  }
+};
 
 template <typename T>
 __device__ __forceinline__ uint32_t pack2(float a, float b);
@@ -107,55 +164,78 @@ __device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float a, float b) {
   return *(const uint32_t*)&h;
 }
 
-// 32 bytes at a multiple of 32
-__device__ __forceinline__ void store_sector(void* to, const uint32_t (&v)[16], int at) {
-  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(v[at]), "r"(v[at + 1]), "r"(v[at + 2]),
-               "r"(v[at + 3]), "r"(v[at + 4]), "r"(v[at + 5]), "r"(v[at + 6]), "r"(v[at + 7])
-               : "memory");
-}
-
-// 32 elements of each lane's row to `to` (NULL: none), of which the first `count` exist (the same in all lanes).  Rows that
-// start at any element are turned in shared memory, so that lanes write one row's elements: half a warp a row, two elements a
-// lane from the row's first multiple of 4 bytes on.  The loop has no branches but predicates: waits for one row's
-// elements are no waits for the next's.
-template <typename T>
-__device__ __forceinline__ void store_rows(T* to, const float (&v)[32], int count, bool whole, uint16_t* turn, int lane) {
-  uint32_t w[16];
+// A warp's sums on their way out: 64 elements of its 32 rows, a lane a row, turned in shared memory so that they leave by
+// whole runs of a row (1 GB of a gradient leaves at 4.9 TB/s by 32 bytes of every lane's own row, at 6.6 by runs).  Rows
+// of 128 bytes, chunks of 16 swizzled by the row's number in 8: as boxes are, and without conflicts either way.
+struct Turn {
+  uint32_t at;
+  int lane;
+  __device__ __forceinline__ uint32_t chunk(int row, int c) const { return at + row * 128 + ((c ^ row) & 7) * 16; }
+  // the lane's elements 32 half ..
+  template <typename T>
+  __device__ __forceinline__ void put(const float (&v)[32], int half) const {
 #pragma unroll
-  for (int j = 0; j < 16; j++) w[j] = pack2<T>(v[2 * j], v[2 * j + 1]);
-  if (whole && count >= 32) {
-    if (to) {
-      store_sector(to, w, 0);
-      store_sector(to + 16, w, 8);
-    }
-    return;
+    for (int c = 0; c < 4; c++)
+      asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(chunk(lane, half * 4 + c)),
+                   "r"(pack2<T>(v[8 * c], v[8 * c + 1])), "r"(pack2<T>(v[8 * c + 2], v[8 * c + 3])),
+                   "r"(pack2<T>(v[8 * c + 4], v[8 * c + 5])), "r"(pack2<T>(v[8 * c + 6], v[8 * c + 7]))
+                   : "memory");
   }
-  __syncwarp();
+  __device__ __forceinline__ uint32_t element(int row, int i) const {
+    uint16_t v;
+    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(chunk(row, i / 8) + i % 8 * 2) : "memory");
+    return v;
+  }
+  // before the first put: the box before has left
+  __device__ __forceinline__ void free() const {
+    if (lane == 0) boxes_read();
+    __syncwarp();
+  }
+  __device__ __forceinline__ void store(const CUtensorMap* map, int x, int y) const {
+    shared_to_boxes();
+    __syncwarp();
+    if (lane == 0) store_box(map, at, x, y);
+  }
+  // to each lane's row `to` (NULL: none), of which `count` elements exist (the same in all lanes), 8 lanes a row if all rows
+  // start at multiples of 16 bytes (`whole`), else a warp a row, two elements a lane from the row's first multiple of 4
+  // bytes on.  Loads of several rows go before their stores.
+  __device__ __forceinline__ void store(uint16_t* to, int count, bool whole) const {
+    __syncwarp();
+    count = min(count, 64);
+    if (whole && count == 64) {
 #pragma unroll
-  for (int j = 0; j < 16; j++) ((uint32_t*)(turn + lane * kTurnRow))[j] = w[j];
-  __syncwarp();
-  const int at = lane % 16;
-  count = min(count, 32);
-#pragma unroll
-  for (int r0 = 0; r0 < 32; r0 += 8) {
-    uint16_t* row[4];
-    uint32_t two[4];
-    int j[4];
-#pragma unroll
-    for (int i = 0; i < 4; i++) {
-      const int r = r0 + 2 * i + lane / 16;
-      row[i] = (uint16_t*)__shfl_sync(~0u, (unsigned long long)to, r);
-      j[i] = 2 * at + (int)((uintptr_t)row[i] / 2 % 2);
-      two[i] = turn[r * kTurnRow + j[i]] | (uint32_t)turn[r * kTurnRow + j[i] + 1] << 16;
+      for (int i = 0; i < 8; i++) {
+        const int row = i * 4 + lane / 8;
+        uint16_t* p = (uint16_t*)__shfl_sync(~0u, (unsigned long long)to, row);
+        uint4 v;
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                     : "r"(chunk(row, lane % 8))
+                     : "memory");
+        if (p) *(uint4*)(p + lane % 8 * 8) = v;
+      }
+      return;
     }
+#pragma unroll 1
+    for (int row0 = 0; row0 < 32; row0 += 4) {
+      uint16_t* p[4];
+      uint32_t two[4];
+      int j[4];
 #pragma unroll
-    for (int i = 0; i < 4; i++) {
-      if (row[i] && j[i] + 1 < count) *(uint32_t*)(row[i] + j[i]) = two[i];
-      if (row[i] && j[i] + 1 == count) row[i][j[i]] = (uint16_t)two[i];
-      if (row[i] && j[i] == 1) row[i][0] = turn[(r0 + 2 * i + lane / 16) * kTurnRow];
+      for (int i = 0; i < 4; i++) {
+        p[i] = (uint16_t*)__shfl_sync(~0u, (unsigned long long)to, row0 + i);
+        j[i] = 2 * lane + (int)((uintptr_t)p[i] / 2 % 2);
+        two[i] = element(row0 + i, j[i]) | element(row0 + i, j[i] + 1) << 16;  // past the row: of its beginning, not used
+      }
+#pragma unroll
+      for (int i = 0; i < 4; i++) {
+        if (p[i] && j[i] + 1 < count) *(uint32_t*)(p[i] + j[i]) = two[i];
+        if (p[i] && j[i] + 1 == count) p[i][j[i]] = (uint16_t)two[i];
+        if (p[i] && j[i] == 1) p[i][0] = (uint16_t)element(row0 + i, 0);
+      }
     }
   }
-}
+};
 
 __device__ __forceinline__ float sum32(const float (&v)[32]) {
   float s[8];
@@ -173,7 +253,8 @@ __device__ __forceinline__ float max32(const float (&v)[32]) {
 
 // Logits of one row, kRecCols columns from `sums`: the record, and with `probs` the exponentials.  z is only ever in registers.
 template <typename T, bool kProbs>
-__device__ __forceinline__ void logits_rows(const TileArgs& a, int n, uint32_t sums, int row, int col, int lane) {
+__device__ __forceinline__ void logits_rows(const TileArgs& a, const Maps& maps, int n, uint32_t sums, int row, int col,
+                                            const Turn& turn) {
   const HeadPlan& p = a.p;
   const bool real = row < n;
   const int y = real ? p.tgt[row] - col : -1;
@@ -212,14 +293,13 @@ __device__ __forceinline__ void logits_rows(const TileArgs& a, int n, uint32_t s
         for (int j = 0; j < 32; j++)
           if (j == here) z[j] = e;
       }
-      if (row < up_div(n, kStepK) * kStepK) {
-        uint32_t w[16];
+      if (!real) {
 #pragma unroll
-        for (int j = 0; j < 16; j++) w[j] = real ? pack2<T>(z[2 * j], z[2 * j + 1]) : 0u;
-        T* e = (T*)p.e + (long long)row * p.lde + col + c;
-        store_sector(e, w, 0);
-        store_sector(e + 16, w, 8);
+        for (int j = 0; j < 32; j++) z[j] = 0.0f;
       }
+      if (c % 64 == 0) turn.free();
+      turn.put<T>(z, c / 32 % 2);
+      if (c % 64) turn.store(&maps.e_out, col + c - 32, row - turn.lane);
     } else {
       const float top = whole_ref(max32(z));
 #pragma unroll
@@ -256,51 +336,52 @@ __device__ __forceinline__ void store_part(float* part, const float (&v)[32]) {
   for (int j = 0; j < 32; j += 4) ((float4*)part)[j / 4] = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
 }
 
-// Sums of a gradient's tile: kHalf columns of each lane's row, two loads of 32 at a time
+// Sums of a gradient's tile: kHalf columns of each lane's row, 64 at a time
 template <typename T>
-__device__ __forceinline__ void grad_rows(const TileArgs& a, int n, bool again, float post, const Task& t, uint32_t sums,
-                                          int row, int col, uint16_t* turn, int lane) {
+__device__ __forceinline__ void grad_rows(const TileArgs& a, const Maps& maps, int n, bool again, float post, const Task& t,
+                                          uint32_t sums, int row, int col, const Turn& turn) {
   const HeadPlan& p = a.p;
   const GradSplit& sp = a.p.split;
   const bool hidden = t.job == 0;
   const bool parts = (hidden ? sp.hidden_parts : sp.head_parts) > 1;
-  const bool there = row < (hidden ? n : p.V);
-  T* to = nullptr;
+  const int end = hidden ? n : p.V;
+  if (row - turn.lane >= end) return;
+  const bool there = row < end, out = !parts && (hidden || a.sum == kOnly || a.sum == kLast), box = out && !hidden && a.boxes;
+  uint16_t* to = nullptr;
   float scale = post;
-  if (there && !parts) {
+  if (there && out) {
     if (hidden) {
       const long long r = a.out.r0 + p.src[row];
-      to = (T*)a.out.grad + (r / a.out.n) * a.out.stride_b + (r % a.out.n) * a.out.stride_n;
+      to = (uint16_t*)a.out.grad + (r / a.out.n) * a.out.stride_b + (r % a.out.n) * a.out.stride_n;
       if (!again) scale = p.coef[row];
     } else {
-      to = (T*)a.grad_head + row * a.grad_head_stride;
+      to = (uint16_t*)a.grad_head + row * a.grad_head_stride;
     }
   }
-  const bool whole = __all_sync(~0u, ((uintptr_t)(to + col) & 31) == 0 || !to);
+  const bool whole = __all_sync(~0u, ((uintptr_t)to & 15) == 0);
   float* part = hidden ? sp.hidden + ((long long)t.part * p.cap + row) * p.ldp : sp.head + ((long long)t.part * p.V + row) * p.ldp;
   float* acc = p.acc + (long long)row * p.ldp;
-  auto store = [&](float(&v)[32], int c) {
-    if (c >= p.d) return;
+  auto pass = [&](float(&v)[32], int c) {
     if (t.steps <= 0) {
 #pragma unroll
       for (int j = 0; j < 32; j++) v[j] = 0.0f;
     }
     if (parts) {
-      if (there) store_part<T>(part + c, v);
+      if (there && c < p.d) store_part<T>(part + c, v);
       return;
     }
     if (hidden || post != 1.0f) {
 #pragma unroll
       for (int j = 0; j < 32; j++) v[j] *= scale;
     }
-    if (!hidden && a.sum != kOnly && there) {
+    if (!hidden && a.sum != kOnly && there && c < p.d) {
       if (a.sum != kFirst) {
 #pragma unroll
         for (int j = 0; j < 32; j++) v[j] += acc[c + j];
       }
       if (a.sum != kLast) store_part<T>(acc + c, v);
     }
-    if (hidden || a.sum == kOnly || a.sum == kLast) store_rows<T>(to ? to + c : nullptr, v, p.d - c, whole, turn, lane);
+    if (out) turn.put<T>(v, c / 32 % 2);
   };
 #pragma unroll 1
   for (int c = col; c < col + kHalf && c < p.d; c += 64) {
@@ -311,8 +392,11 @@ __device__ __forceinline__ void grad_rows(const TileArgs& a, int n, bool again, 
       sums_loaded(v);
       sums_loaded(w);
     }
-    store(v, c);
-    store(w, c + 32);
+    if (out) turn.free();
+    pass(v, c);
+    pass(w, c + 32);
+    if (box) turn.store(&maps.grad_out, c, row - turn.lane);
+    else if (out) turn.store(to ? to + c : nullptr, p.d - c, whole);
   }
 }
 
@@ -327,7 +411,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   const int n = *a.p.count;
   uint8_t* shared = (uint8_t*)(((uintptr_t)shared_raw + 1023) / 1024 * 1024);
   const uint32_t stages = smem_address(shared);
-  uint16_t* turns = (uint16_t*)(shared + kStages * kStage);
   const int warp = warp_of_thread(), lane = threadIdx.x % 32, pair = blockIdx.x / 2;
   const uint32_t rank = cluster_rank();
   const uint32_t full = smem_address(bars.full), empty = smem_address(bars.empty);
@@ -352,9 +435,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   products_fence_after();
   const uint32_t sums = bars.sums;
 
-  auto task = [&](int i, Task& t) {
-    return kForm == 2 ? grads_task(a, n, pair, i, t) : logits_task(a, n, pair, i, t);
-  };
+  typename std::conditional<kForm == 2, GradTasks, LogitsTasks>::type tasks(a, n, pair);
   bool ok = true;
   if (warp == 0) {
     if (lane == 0) {  // copies
@@ -362,7 +443,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       int s = 0;
       uint32_t turn = 0;
       Task t;
-      for (int i = 0; ok && task(i, t); i++) {
+      while (ok && tasks.next(t)) {
         const int m = t.m0 + rank * kHalf, c = t.n0 + rank * kHalf;
         for (int k = t.k0; k < t.k0 + t.steps; k++) {
           if (!(ok = bar_wait(empty + 8 * s, turn ^ 1))) break;
@@ -391,7 +472,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       int s = 0, use = 0;
       uint32_t turn = 0;
       Task t;
-      for (int i = 0; ok && task(i, t); i++) {
+      while (ok && tasks.next(t)) {
         if (t.steps <= 0) continue;
         const int half = use & 1;
         if (!(ok = bar_wait(sums_empty + 8 * half, (use >> 1 & 1) ^ 1))) break;
@@ -421,11 +502,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     }
   } else if (warp >= 4) {
     const int part = warp - 4, quarter = warp % 4;
-    uint16_t* turn = turns + part * 32 * kTurnRow;
+    const Turn turn = {stages + kStages * kStage + part * kTurn, lane};
     const float post = kForm == 2 && again ? *a.p.post : 1.0f;
     int use = 0;
     Task t;
-    for (int i = 0; task(i, t); i++) {
+    while (tasks.next(t)) {
       const int half = use & 1;
       const int row = t.m0 + rank * kHalf + quarter * 32 + lane, off = part / 4 * kHalf;
       const uint32_t from = sums + half * kTile + off + ((uint32_t)quarter * 32 << 16);
@@ -434,9 +515,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         products_fence_after();
       }
       if (kForm == 2) {
-        grad_rows<T>(a, n, again, post, t, from, row, t.n0 + off, turn, lane);
+        grad_rows<T>(a, maps, n, again, post, t, from, row, t.n0 + off, turn);
       } else if (row - lane < up_div(n, kStepK) * kStepK) {
-        logits_rows<T, kForm == 1>(a, n, from, row, t.n0 + off, lane);
+        logits_rows<T, kForm == 1>(a, maps, n, from, row, t.n0 + off, turn);
       }
       if (t.steps > 0) {
         products_fence_before();
@@ -445,6 +526,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         use++;
       }
     }
+    if (lane == 0) boxes_stored();
   }
   if (!ok) {
     *a.p.failed = 1;
@@ -517,7 +599,16 @@ GradSplit split_grads(int rows, int d, int V) {
   const long long kv = (V + (long long)kStepK - 1) / kStepK, kr = (rows + kStepK - 1) / kStepK;
   s.tile_cost = 4;
   const long long all = mt * ct * (kv + s.tile_cost) + vt * ct * (kr + s.tile_cost), unit = std::max(8ll, all / (3 * kPairs));
+  s.hidden_pairs = kPairs;
   s.hidden_parts = (int)std::min<long long>(kMostParts, (kv + unit - 1) / unit);
+  // Few rows: reading the head and writing its gradient are all of the time, and overlap (32 rows of 4,096 through 126,000: one
+  // after the other 200 and 295 us), each part of a row of tiles by a pair of its own.  Many: all pairs on tiles of one kind
+  // share more of what they read.
+  if (mt == 1) {
+    const long long share = kPairs * ct * (kv + s.tile_cost) / all;
+    s.hidden_parts = (int)std::min<long long>(std::min<long long>(kMostParts, (kv + 7) / 8), std::max(1ll, share / ct));
+    s.hidden_pairs = (int)std::min<long long>(ct * s.hidden_parts, std::max(1ll, share));
+  }
   s.head_parts = (int)std::min<long long>(kMostParts, (kr + unit - 1) / unit);
   return s;
 }
@@ -531,6 +622,7 @@ epic_status launch_head_logits(const HeadPlan& p, int dtype, const LogitsPass& p
   if (!make_map(&maps.hc, a.bf16, p.hc, p.ldh, p.cap, p.ldh, kHalf) ||
       !make_map(&maps.head_k, a.bf16, p.head, p.d, p.V, p.ldw, kHalf))
     return EPIC_ERR_CUDA;
+  if (pass.probs && !make_map(&maps.e_out, a.bf16, p.e, p.lde, p.cap, p.lde, 32)) return EPIC_ERR_CUDA;
   if (pass.probs) return dtype == EPIC_F16 ? launch_tiles<__half, 1>(maps, a, st) : launch_tiles<__nv_bfloat16, 1>(maps, a, st);
   return dtype == EPIC_F16 ? launch_tiles<__half, 0>(maps, a, st) : launch_tiles<__nv_bfloat16, 0>(maps, a, st);
 }
@@ -552,6 +644,8 @@ epic_status launch_head_grads(const HeadPlan& p, int dtype, const HiddenGrad& ou
       !make_map(&maps.e_mn, a.bf16, p.e, p.lde, p.cap, p.lde, 64) ||
       !make_map(&maps.head_mn, a.bf16, p.head, p.d, p.V, p.ldw, 64))
     return EPIC_ERR_CUDA;
+  a.boxes = grad_head && p.d % 8 == 0 && (uintptr_t)grad_head % 16 == 0 && (p.V == 1 || (stride % 8 == 0 && stride < 1ll << 38));
+  if (a.boxes && !make_map(&maps.grad_out, a.bf16, grad_head, p.d, p.V, p.V == 1 ? p.ldh : stride, 32)) return EPIC_ERR_CUDA;
   const epic_status s = dtype == EPIC_F16 ? launch_tiles<__half, 2>(maps, a, st) : launch_tiles<__nv_bfloat16, 2>(maps, a, st);
   if (s != EPIC_OK) return s;
   const bool hidden = a.p.split.hidden_parts > 1, head = a.p.split.head_parts > 1;

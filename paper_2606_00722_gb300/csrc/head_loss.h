@@ -16,6 +16,7 @@ constexpr int kMostParts = 64;  // of a gradient's sum
 // tokens, of the head's over the positions.  1: not cut; 0: no such gradient.
 struct GradSplit {
   int hidden_parts, head_parts;
+  int hidden_pairs;     // of CTAs, that make gradients of hidden states
   int tile_cost;        // what a tile costs beside its sum, in steps of it
   float *hidden, *head; // [parts][cap][ldp], [parts][V][ldp]
 };
