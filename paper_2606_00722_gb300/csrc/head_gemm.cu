@@ -10,6 +10,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "head_launch.cuh"
 #include "head_loss.h"
 #include "head_rows.cuh"
 #include "tensor_tiles.cuh"
@@ -406,9 +407,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     k_head_tiles(const __grid_constant__ Maps maps, const __grid_constant__ TileArgs a) {
   extern __shared__ uint8_t shared_raw[];
   __shared__ Bars bars;
-  const bool again = *a.p.again != 0;
-  if (kForm != 2 && a.pass.only_again && !again) return;
-  const int n = *a.p.count;
   uint8_t* shared = (uint8_t*)(((uintptr_t)shared_raw + 1023) / 1024 * 1024);
   const uint32_t stages = smem_address(shared);
   const int warp = warp_of_thread(), lane = threadIdx.x % 32, pair = blockIdx.x / 2;
@@ -427,6 +425,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     }
     bar_init_visible();
   }
+  if (kForm != 2 && a.pass.only_again) {  // mostly there is nothing to do
+    follow();
+    if (*a.p.again == 0) return;
+  }
   if (warp == 1) sums_take_pair(smem_address(&bars.sums));
   products_fence_before();
   __syncthreads();
@@ -434,7 +436,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   cluster_wait();
   products_fence_after();
   const uint32_t sums = bars.sums;
-
+  follow();
+  let_next();
+  const bool again = *a.p.again != 0;
+  const int n = *a.p.count;
   typename std::conditional<kForm == 2, GradTasks, LogitsTasks>::type tasks(a, n, pair);
   bool ok = true;
   if (warp == 0) {
@@ -544,6 +549,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 // Parts of a gradient's sums, in order
 template <typename T>
 __global__ void __launch_bounds__(256) k_head_parts(const __grid_constant__ TileArgs a) {
+  follow();
+  let_next();
   const HeadPlan& p = a.p;
   const GradSplit& sp = a.p.split;
   const bool hidden = blockIdx.y == 0 && sp.hidden_parts > 1;
@@ -581,14 +588,9 @@ __global__ void __launch_bounds__(256) k_head_parts(const __grid_constant__ Tile
 
 // ---------------------------------------------------------------- host
 
-epic_status launched() { return cudaGetLastError() == cudaSuccess ? EPIC_OK : EPIC_ERR_CUDA; }
-
 template <typename T, int kForm>
 epic_status launch_tiles(const Maps& maps, const TileArgs& a, cudaStream_t st) {
-  if (cudaFuncSetAttribute(k_head_tiles<T, kForm>, cudaFuncAttributeMaxDynamicSharedMemorySize, kShared) != cudaSuccess)
-    return cudaGetLastError(), EPIC_ERR_CUDA;
-  k_head_tiles<T, kForm><<<2 * kPairs, kThreads, kShared, st>>>(maps, a);
-  return launched();
+  return launch_next(k_head_tiles<T, kForm>, 2 * kPairs, kThreads, kShared, kShared, st, maps, a);
 }
 
 }  // namespace
@@ -652,9 +654,7 @@ epic_status launch_head_grads(const HeadPlan& p, int dtype, const HiddenGrad& ou
   if (!hidden && !head) return EPIC_OK;
   const long long most = std::max(hidden ? (long long)p.rows : 0, head ? (long long)p.V : 0) * ((p.d + 3) / 4);
   const dim3 grid((unsigned)std::min(1216ll, (most + 255) / 256), hidden && head ? 2 : 1);
-  if (dtype == EPIC_F16) k_head_parts<__half><<<grid, 256, 0, st>>>(a);
-  else k_head_parts<__nv_bfloat16><<<grid, 256, 0, st>>>(a);
-  return launched();
+  return launch_next(dtype == EPIC_F16 ? k_head_parts<__half> : k_head_parts<__nv_bfloat16>, grid, 256, 0, kNoCache, st, a);
 }
 
 }  // namespace epic

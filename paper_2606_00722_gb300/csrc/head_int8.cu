@@ -8,6 +8,7 @@
 #include <algorithm>
 
 #include "../../include/epic.h"
+#include "head_launch.cuh"
 #include "head_rows.cuh"
 #include "tensor_tiles.cuh"
 
@@ -33,6 +34,8 @@ template <typename T>
 __global__ void __launch_bounds__(kQuantThreads) k_quantize_rows(QuantArgs a) {
   constexpr int E = Chunk<T>::kCount;
   __shared__ uint32_t s_top[kQuantThreads / 32];
+  follow();
+  let_next();
   const long long r = blockIdx.x, b = r / a.k;
   const int at = a.pos ? a.pos[r] : (int)(r % a.k);
   int8_t* q = a.q + r * a.d;
@@ -117,6 +120,8 @@ __device__ __forceinline__ int totals(int (&v)[N], int lane) {
 template <typename T, int R>
 __global__ void __launch_bounds__(kFewThreads) k_few_logits(Int8Args a) {
   extern __shared__ int4 s_q[];
+  follow();
+  let_next();
   const int lane = threadIdx.x % 32, chunks = (a.d + 15) / 16;
   for (int i = threadIdx.x; i < R * chunks * 16; i += kFewThreads) {
     const int r = i / (chunks * 16), c = i % (chunks * 16);
@@ -243,8 +248,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     for (int& m : bars.most) m = 0;
     bar_init_visible();
   }
+  if (warp == kWorkWarps) sums_take_pair(smem_address(&bars.sums));
+  __syncthreads();
+  follow();
+  let_next();
   if (a.d > kExactSteps * kStepK) {
-    __syncthreads();
     // the largest sums of 2, 4, 8 .. blocks of a row's sizes
     const int blocks = (a.d + kExactSteps * kStepK - 1) / (kExactSteps * kStepK);
     for (int l = 1; 1 << (l - 1) < blocks; l++) {
@@ -259,7 +267,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       if (lane == 0) atomicMax(&bars.most[l], most);
     }
   }
-  if (warp == kWorkWarps) sums_take_pair(smem_address(&bars.sums));
   products_fence_before();
   __syncthreads();
   cluster_arrive();
@@ -490,6 +497,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 // Hidden states of 8 bits as fp16, rows of a multiple of 16 bytes, a CTA a row; and their sizes, added up over 1,024 each
 __global__ void __launch_bounds__(256) k_rows_as_halves(const int8_t* q, __half* to, int d, int ld, int* sizes, int* failed) {
   __shared__ uint32_t s_sum[kMostProducts / 1024 + 1];
+  follow();
+  let_next();
   if (blockIdx.x == 0 && threadIdx.x == 0) *failed = 0;
   const int blocks = (d + 1023) / 1024;
   for (int i = threadIdx.x; i < blocks; i += 256) s_sum[i] = 0;
@@ -519,11 +528,8 @@ __global__ void __launch_bounds__(256) k_rows_as_halves(const int8_t* q, __half*
 template <typename T, int R>
 epic_status launch_few(const Int8Args& a, cudaStream_t st) {
   const int bytes = R * ((a.d + 15) / 16) * 16;
-  if (cudaFuncSetAttribute(k_few_logits<T, R>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess)
-    return cudaGetLastError(), EPIC_ERR_CUDA;
   const long long ctas = (a.V + (long long)kFewThreads / 32 * kFewTokens - 1) / (kFewThreads / 32 * kFewTokens);
-  k_few_logits<T, R><<<(unsigned)std::min(ctas, 152ll * 4), kFewThreads, bytes, st>>>(a);
-  return cudaGetLastError() == cudaSuccess ? EPIC_OK : EPIC_ERR_CUDA;
+  return launch_next(k_few_logits<T, R>, (unsigned)std::min(ctas, 152ll * 4), kFewThreads, bytes, kFewBytes, st, a);
 }
 
 template <typename T, int kRows>
@@ -534,10 +540,7 @@ epic_status launch_tiles(const Int8Args& a, __half* q16, int ld, bool askew, cud
   if (!askew && !make_byte_map(&head, a.head, a.d, a.V, a.V > 1 ? a.head_stride : (a.d + 15) / 16 * 16, kHalf))
     return EPIC_ERR_CUDA;
   const auto kernel = askew ? k_int8_tiles<T, kRows, true> : k_int8_tiles<T, kRows, false>;
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kShared) != cudaSuccess)
-    return cudaGetLastError(), EPIC_ERR_CUDA;
-  kernel<<<2 * kPairs, kThreads, kShared, st>>>(map, head, a);
-  return cudaGetLastError() == cudaSuccess ? EPIC_OK : EPIC_ERR_CUDA;
+  return launch_next(kernel, 2 * kPairs, kThreads, kShared, kShared, st, map, head, a);
 }
 
 bool head_lies_askew(const int8_t* head, long long stride, int V) {
@@ -574,8 +577,8 @@ epic_status launch_int8(Int8Args a, void* ws, cudaStream_t st) {
   __half* q16 = (__half*)((char*)ws + 256 + sizes_bytes(a.rows, a.d));
   const int ld = (a.d + 7) / 8 * 8;
   a.sizes = sizes;
-  k_rows_as_halves<<<a.rows, 256, 0, st>>>(a.q, q16, a.d, ld, sizes, a.failed);
-  if (cudaGetLastError() != cudaSuccess) return EPIC_ERR_CUDA;
+  const epic_status s = launch_next(k_rows_as_halves, a.rows, 256, 0, kNoCache, st, a.q, q16, a.d, ld, sizes, a.failed);
+  if (s != EPIC_OK) return s;
   switch (tile_rows(a.rows)) {
     case 32: return launch_tiles<T, 32>(a, q16, ld, askew, st);
     case 64: return launch_tiles<T, 64>(a, q16, ld, askew, st);
@@ -609,11 +612,10 @@ epic_status epic_quantize_rows(const void* d_x, int32_t dtype, int32_t B, int32_
   const QuantArgs a = {d_x, stride_b, stride_n, d_pos, n, k, d, d_q, d_scale};
   cudaStream_t st = (cudaStream_t)cuda_stream;
   switch (dtype) {
-    case EPIC_F32: k_quantize_rows<float><<<(unsigned)rows, kQuantThreads, 0, st>>>(a); break;
-    case EPIC_F16: k_quantize_rows<__half><<<(unsigned)rows, kQuantThreads, 0, st>>>(a); break;
-    default: k_quantize_rows<__nv_bfloat16><<<(unsigned)rows, kQuantThreads, 0, st>>>(a);
+    case EPIC_F32: return launch_next(k_quantize_rows<float>, (unsigned)rows, kQuantThreads, 0, kCache, st, a);
+    case EPIC_F16: return launch_next(k_quantize_rows<__half>, (unsigned)rows, kQuantThreads, 0, kCache, st, a);
+    default: return launch_next(k_quantize_rows<__nv_bfloat16>, (unsigned)rows, kQuantThreads, 0, kCache, st, a);
   }
-  return cudaGetLastError() == cudaSuccess ? EPIC_OK : EPIC_ERR_CUDA;
 }
 
 epic_status epic_int8_logits_workspace(int32_t B, int32_t k, int32_t d, int32_t V, const int8_t* d_head,

@@ -23,6 +23,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "head_launch.cuh"
 #include "head_loss.h"
 #include "head_rows.cuh"
 
@@ -86,6 +87,8 @@ __device__ __forceinline__ void sum_and_top(int& count, float& top) {
 __global__ void __launch_bounds__(kRowsThreads) k_head_count(RowsArgs a) {
   __shared__ int s_count[kRowsThreads / 32];
   __shared__ float s_top[kRowsThreads / 32];
+  follow();
+  let_next();
   const int i = blockIdx.x * kRowsThreads + threadIdx.x;
   float top = i < a.p.rows ? fabsf(row_factor(a, a.r0 + i)) : 0.0f;
   int count = top != 0.0f;
@@ -106,6 +109,8 @@ template <typename T, bool kWide>
 __global__ void __launch_bounds__(kRowsThreads) k_head_rows(RowsArgs a) {
   __shared__ int s_before[kRowsThreads / 32], s_all[kRowsThreads / 32];
   __shared__ float s_top[kRowsThreads / 32], s_dot[kRowsThreads / 32];
+  follow();
+  let_next();
   const HeadPlan& p = a.p;
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, warps = kRowsThreads / 32;
   const int first = blockIdx.x * a.per, last = min(first + a.per, p.rows);
@@ -223,6 +228,8 @@ template <typename T, int kMeetRows>
 __global__ void __launch_bounds__(kMeetWarps * 32) k_head_meet(MeetArgs a) {
   __shared__ float s_ref[kMeetWarps][kMeetRows], s_sum[kMeetWarps][kMeetRows], s_coef[kMeetRows];
   __shared__ int s_left[kMeetWarps][kMeetRows];
+  follow();
+  let_next();
   const HeadPlan& p = a.p;
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, at = lane % kMeetRows;
   const int n = *p.count, q0 = blockIdx.x * kMeetRows, q = q0 + at;
@@ -303,6 +310,8 @@ __global__ void __launch_bounds__(kMeetWarps * 32) k_head_meet(MeetArgs a) {
 // lie in; the first and the last chunk of a row may hold bytes next to it, within the same 16.
 template <typename T>
 __global__ void __launch_bounds__(256) k_head_pack(const T* head, long long stride, T* to, long long ld, int d, int V) {
+  follow();
+  let_next();
   const int lane = threadIdx.x % 32;
   for (long long v = blockIdx.x * 8ll + threadIdx.x / 32; v < V; v += gridDim.x * 8ll) {
     const uintptr_t w = (uintptr_t)(head + v * stride), end = w + d * sizeof(T);
@@ -327,6 +336,8 @@ __global__ void __launch_bounds__(256) k_head_pack(const T* head, long long stri
 
 template <typename T>
 __global__ void k_fill_zero(T* grad, long long stride, int d) {
+  follow();
+  let_next();
   for (int k = threadIdx.x; k < d; k += blockDim.x) grad[blockIdx.x * stride + k] = of_float<T>(0.0f);
 }
 
@@ -424,11 +435,6 @@ struct HeadTensors {
   int64_t ghead_stride;
 };
 
-epic_status last_error() {
-  if (cudaGetLastError() == cudaSuccess) return EPIC_OK;
-  return EPIC_ERR_CUDA;
-}
-
 #define EPIC_TRY(call)                     \
   do {                                     \
     const epic_status s_ = (call);         \
@@ -441,15 +447,13 @@ epic_status run_head(const HeadCall& c, const HeadTensors& t, HeadPlan p, cudaSt
   const bool half = c.dtype == EPIC_F16, grads = c.form != kForward;
   if (rows == 0 || c.V == 0) {
     if (rows == 0 && t.grad_head && c.V > 0) {
-      k_fill_zero<T><<<c.V, 256, 0, st>>>((T*)t.grad_head, t.ghead_stride, c.d);
-      EPIC_TRY(last_error());
+      EPIC_TRY(launch_next(k_fill_zero<T>, c.V, 256, 0, kNoCache, st, (T*)t.grad_head, t.ghead_stride, c.d));
     }
     if (rows == 0) return EPIC_OK;
   }
   if (c.V > 0 && p.head != c.head) {
-    k_head_pack<T><<<(unsigned)std::min(2432, (c.V + 7) / 8), 256, 0, st>>>((const T*)c.head, c.head_stride, (T*)p.head, p.ldw,
-                                                                        c.d, c.V);
-    EPIC_TRY(last_error());
+    EPIC_TRY(launch_next(k_head_pack<T>, (unsigned)std::min(2432, (c.V + 7) / 8), 256, 0, kNoCache, st, (const T*)c.head,
+                         c.head_stride, (T*)p.head, p.ldw, c.d, c.V));
   }
   for (long long r0 = 0; r0 < rows; r0 += p.cap) {
     p.rows = (int)std::min<long long>(p.cap, rows - r0);
@@ -474,21 +478,17 @@ epic_status run_head(const HeadCall& c, const HeadTensors& t, HeadPlan p, cudaSt
     a.probs = stored && !known;
     a.scaled = half && grads;
     a.again = known || a.scaled;
-    if (p.rows > kCounted) {
-      k_head_count<<<(p.rows + kRowsThreads - 1) / kRowsThreads, kRowsThreads, 0, st>>>(a);
-      EPIC_TRY(last_error());
-    }
-    if (few) k_head_rows<T, true><<<p.rows, kRowsThreads, 0, st>>>(a);
-    else k_head_rows<T, false><<<(p.rows + a.per - 1) / a.per, kRowsThreads, 0, st>>>(a);
-    EPIC_TRY(last_error());
+    if (p.rows > kCounted)
+      EPIC_TRY(launch_next(k_head_count, (p.rows + kRowsThreads - 1) / kRowsThreads, kRowsThreads, 0, kNoCache, st, a));
+    EPIC_TRY(launch_next(few ? k_head_rows<T, true> : k_head_rows<T, false>, (p.rows + a.per - 1) / a.per, kRowsThreads, 0, kNoCache,
+                         st, a));
     if (c.V == 0) continue;
     // A step's exponentials are relative to the target's logit; fp16 has not the range for that and makes them once the
     // logsumexp is known, as do rows that leave the window.
     EPIC_TRY(launch_head_logits(p, c.dtype, {true, stored, known, false}, st));
     const MeetArgs m = {p, r0, t.weight, t.loss, t.lse, grads, stored, known};
-    if (few) k_head_meet<T, 1><<<p.rows, kMeetWarps * 32, 0, st>>>(m);
-    else k_head_meet<T, 8><<<(p.rows + 7) / 8, kMeetWarps * 32, 0, st>>>(m);
-    EPIC_TRY(last_error());
+    EPIC_TRY(launch_next(few ? k_head_meet<T, 1> : k_head_meet<T, 8>, few ? p.rows : (p.rows + 7) / 8, kMeetWarps * 32, 0, kNoCache,
+                         st, m));
     if (grads && !known) EPIC_TRY(launch_head_logits(p, c.dtype, {false, true, true, true}, st));
     if (t.grad_hidden || t.grad_head) {
       const bool first = r0 == 0, last = r0 + p.cap >= rows;
