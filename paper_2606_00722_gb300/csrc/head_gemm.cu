@@ -1,7 +1,7 @@
 // The matrix products of the head's loss, on the tensor units: logits = h W^T,
 // gradients dh = e W and dW = e^T hs.
 //
-// A tile of 256 x 256 is a pair of CTAs': each copies 128 rows of both operands in steps of 64 of the sum (TMA, six steps
+// A tile of 256 x 256 is a pair of CTAs': each copies 128 rows of both operands in steps of 64 of the sum (TMA, five steps
 // ahead), one thread of the pair issues the products, sums lie in tensor memory, twice, so that eight warps a CTA work on
 // one tile's sums while the next tile's are made.  Operands are read as they lie: e along and across its rows, the head by
 // tokens and by hidden dimensions.
@@ -19,11 +19,11 @@ namespace epic {
 namespace {
 
 constexpr int kTile = 256, kHalf = 128;  // a pair's tile, a CTA's share of an operand
-constexpr int kStepK = 64, kStages = 6;
+constexpr int kStepK = 64, kStages = 5;
 constexpr int kOperand = kHalf * kStepK * 2, kStage = 2 * kOperand;  // bytes
 constexpr int kWorkWarps = 8, kThreads = 128 + 32 * kWorkWarps;
 constexpr int kPairs = 76;  // of the GB300's 152 SMs
-constexpr int kTurn = 32 * 128;  // bytes of a warp's turning buffer: 64 elements of 32 rows
+constexpr int kTurn = 2 * 32 * 128;  // bytes of a warp's two turning buffers: 64 elements of 32 rows each
 constexpr int kShared = kStages * kStage + kWorkWarps * kTurn + 1024;
 
 struct Bars {
@@ -88,35 +88,32 @@ struct LogitsTasks {
   }
 };
 
-// Gradients: tiles of hidden states (long sums) are dealt to the first hidden_pairs pairs, the head's to all, so that the pairs
-// end together: those without a tile of hidden states take as many of the head's as theirs are worth, then those with one
-// less than others, then all.
+// Gradients: first all tiles of hidden states (long sums), then the head's.  Where the former do not come out even, the pairs
+// without a last one take as many of the latter as it is worth before the rest is dealt to all.
 struct GradTasks {
   Divisor columns;
   int row_tiles, head_tiles, hidden_parts, head_parts, v_steps, r_steps;
-  int hidden, hidden_by, hidden_left;      // the next tile of hidden states, how far the one after is, how many
-  int head[3], by[3], left[3];             // the same of the head's in the three rounds
+  int hidden, hidden_left;  // the next tile of hidden states, how many
+  int head[2], by[2], left[2];  // the next one of the head's, how far the one after is, how many, in the two rounds
   __device__ __forceinline__ GradTasks(const TileArgs& a, int n, int pair) : columns(up_div(a.p.d, kTile)) {
     const GradSplit& s = a.p.split;
-    const int ct = columns.by, some = s.hidden_pairs;
+    const int ct = columns.by;
     row_tiles = up_div(n, kTile) * ct;
     head_tiles = up_div(a.p.V, kTile) * ct;
     hidden_parts = s.hidden_parts;
     head_parts = s.head_parts;
     v_steps = up_div(a.p.V, kStepK);
     r_steps = up_div(n, kStepK);
-    const int all_hidden = hidden_parts * row_tiles, all_head = head_parts * head_tiles, last = all_hidden % some;
+    const int all_hidden = hidden_parts * row_tiles, all_head = head_parts * head_tiles, last = all_hidden % kPairs;
     hidden = pair;
-    hidden_by = some;
-    hidden_left = pair < some ? all_hidden / some + (pair < last) : 0;
-    const int per = up_div(r_steps, max(1, head_parts)) + s.tile_cost, unit = up_div(v_steps, max(1, hidden_parts)) + s.tile_cost;
-    const int none = kPairs - some, less = last ? kPairs - last : 0;
-    const int first = none ? min(all_head / none, (int)((long long)(all_hidden / some) * unit / per)) : 0;
-    const int second = less ? min((all_head - first * none) / less, unit / per) : 0;
-    head[0] = pair - some, by[0] = none, left[0] = pair >= some ? first : 0;
-    head[1] = first * none + pair - last, by[1] = less, left[1] = pair >= last ? second : 0;
-    head[2] = first * none + second * less + pair, by[2] = kPairs;
-    left[2] = head[2] < all_head ? (all_head - head[2] + kPairs - 1) / kPairs : 0;
+    hidden_left = all_hidden / kPairs + (pair < last);
+    // (an estimate in floats is as good, and the same for all)
+    const float worth = __fdividef((float)(up_div(v_steps, max(1, hidden_parts)) + s.tile_cost),
+                                   (float)(up_div(r_steps, max(1, head_parts)) + s.tile_cost));
+    const int idle = last ? kPairs - last : 0, first = idle ? min(all_head / idle, (int)worth) : 0;
+    head[0] = pair - last, by[0] = idle, left[0] = pair >= last ? first : 0;
+    head[1] = first * idle + pair, by[1] = kPairs;
+    left[1] = head[1] < all_head ? (all_head - head[1] + kPairs - 1) / kPairs : 0;
   }
   __device__ __forceinline__ void sum(Task& t, int job, int at, int tiles, int parts, int steps) const {
     int part = 0, c;
@@ -136,12 +133,12 @@ struct GradTasks {
   __device__ __forceinline__ bool next(Task& t) {
     if (hidden_left > 0) {
       sum(t, 0, hidden, row_tiles, hidden_parts, v_steps);
-      hidden += hidden_by;
+      hidden += kPairs;
       hidden_left--;
       return true;
     }
 #pragma unroll
-    for (int i = 0; i < 3; i++) {
+    for (int i = 0; i < 2; i++) {
       if (left[i] <= 0) continue;
       sum(t, 1, head[i], head_tiles, head_parts, r_steps);
       head[i] += by[i];
@@ -167,9 +164,10 @@ __device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float a, float b) {
 
 // A warp's sums on their way out: 64 elements of its 32 rows, a lane a row, turned in shared memory so that they leave by
 // whole runs of a row (1 GB of a gradient leaves at 4.9 TB/s by 32 bytes of every lane's own row, at 6.6 by runs).  Rows
-// of 128 bytes, chunks of 16 swizzled by the row's number in 8: as boxes are, and without conflicts either way.
+// of 128 bytes, chunks of 16 swizzled by the row's number in 8: as boxes are, and without conflicts either way.  Two buffers
+// in turn, so that a box leaves while the next one is made.
 struct Turn {
-  uint32_t at;
+  uint32_t at, other;
   int lane;
   __device__ __forceinline__ uint32_t chunk(int row, int c) const { return at + row * 128 + ((c ^ row) & 7) * 16; }
   // the lane's elements 32 half ..
@@ -187,9 +185,12 @@ struct Turn {
     asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(chunk(row, i / 8) + i % 8 * 2) : "memory");
     return v;
   }
-  // before the first put: the box before has left
-  __device__ __forceinline__ void free() const {
-    if (lane == 0) boxes_read();
+  // before the first put: to the other buffer, whose box has left
+  __device__ __forceinline__ void next() {
+    const uint32_t now = other;
+    other = at;
+    at = now;
+    if (lane == 0) boxes_read<1>();
     __syncwarp();
   }
   __device__ __forceinline__ void store(const CUtensorMap* map, int x, int y) const {
@@ -197,10 +198,10 @@ struct Turn {
     __syncwarp();
     if (lane == 0) store_box(map, at, x, y);
   }
-  // to each lane's row `to` (NULL: none), of which `count` elements exist (the same in all lanes), 8 lanes a row if all rows
+  // to each lane's row `to` (NULL from row `rows` on), of which `count` elements exist (the same in all lanes), 8 lanes a row if all rows
   // start at multiples of 16 bytes (`whole`), else a warp a row, two elements a lane from the row's first multiple of 4
   // bytes on.  Loads of several rows go before their stores.
-  __device__ __forceinline__ void store(uint16_t* to, int count, bool whole) const {
+  __device__ __forceinline__ void store(uint16_t* to, int rows, int count, bool whole) const {
     __syncwarp();
     count = min(count, 64);
     if (whole && count == 64) {
@@ -217,8 +218,8 @@ struct Turn {
       }
       return;
     }
-#pragma unroll 1
-    for (int row0 = 0; row0 < 32; row0 += 4) {
+#pragma unroll 2
+    for (int row0 = 0; row0 < min(rows, 32); row0 += 4) {
       uint16_t* p[4];
       uint32_t two[4];
       int j[4];
@@ -252,17 +253,29 @@ __device__ __forceinline__ float max32(const float (&v)[32]) {
   return m;
 }
 
+// What a row's logits are made into, read before they are there
+struct LogitsRow {
+  int target;
+  float ref, mul, at;
+  __device__ __forceinline__ LogitsRow(const TileArgs& a, bool probs, int n, int row) : target(-1), ref(0.0f), mul(1.0f), at(0.0f) {
+    if (row >= n) return;
+    const HeadPlan& p = a.p;
+    target = p.tgt[row];
+    if (!probs) return;
+    ref = a.pass.known ? p.known_ref[row] : p.ref[row];
+    if (a.pass.known) mul = p.known_mul[row];
+    if (a.pass.only_again) at = p.known_at[row];
+  }
+};
+
 // Logits of one row, kRecCols columns from `sums`: the record, and with `probs` the exponentials.  z is only ever in registers.
 template <typename T, bool kProbs>
-__device__ __forceinline__ void logits_rows(const TileArgs& a, const Maps& maps, int n, uint32_t sums, int row, int col,
-                                            const Turn& turn) {
+__device__ __forceinline__ void logits_rows(const TileArgs& a, const Maps& maps, int n, const LogitsRow& is, uint32_t sums,
+                                            int row, int col, Turn& turn) {
   const HeadPlan& p = a.p;
-  const bool real = row < n;
-  const int y = real ? p.tgt[row] - col : -1;
-  const bool known = a.pass.known;
-  const float ref = !kProbs || !real ? 0.0f : known ? p.known_ref[row] : p.ref[row];
-  const float mul = kProbs && real && known ? p.known_mul[row] : 1.0f;
-  const float at = kProbs && real && a.pass.only_again ? p.known_at[row] : 0.0f;
+  const bool real = row < n, known = a.pass.known;
+  const int y = real ? is.target - col : -1;
+  const float ref = is.ref, mul = is.mul, at = is.at;
   float to = kProbs ? (known ? 0.0f : ref) : kNoRef, s = 0.0f;
 #pragma unroll 1
   for (int c = 0; c < kRecCols; c += 32) {
@@ -298,7 +311,7 @@ __device__ __forceinline__ void logits_rows(const TileArgs& a, const Maps& maps,
 #pragma unroll
         for (int j = 0; j < 32; j++) z[j] = 0.0f;
       }
-      if (c % 64 == 0) turn.free();
+      if (c % 64 == 0) turn.next();
       turn.put<T>(z, c / 32 % 2);
       if (c % 64) turn.store(&maps.e_out, col + c - 32, row - turn.lane);
     } else {
@@ -339,8 +352,8 @@ __device__ __forceinline__ void store_part(float* part, const float (&v)[32]) {
 
 // Sums of a gradient's tile: kHalf columns of each lane's row, 64 at a time
 template <typename T>
-__device__ __forceinline__ void grad_rows(const TileArgs& a, const Maps& maps, int n, bool again, float post, const Task& t,
-                                          uint32_t sums, int row, int col, const Turn& turn) {
+__device__ __forceinline__ void grad_rows(const TileArgs& a, const Maps& maps, int n, float post, float coef, long long begin,
+                                          const Task& t, uint32_t sums, int row, int col, Turn& turn) {
   const HeadPlan& p = a.p;
   const GradSplit& sp = a.p.split;
   const bool hidden = t.job == 0;
@@ -349,16 +362,8 @@ __device__ __forceinline__ void grad_rows(const TileArgs& a, const Maps& maps, i
   if (row - turn.lane >= end) return;
   const bool there = row < end, out = !parts && (hidden || a.sum == kOnly || a.sum == kLast), box = out && !hidden && a.boxes;
   uint16_t* to = nullptr;
-  float scale = post;
-  if (there && out) {
-    if (hidden) {
-      const long long r = a.out.r0 + p.src[row];
-      to = (uint16_t*)a.out.grad + (r / a.out.n) * a.out.stride_b + (r % a.out.n) * a.out.stride_n;
-      if (!again) scale = p.coef[row];
-    } else {
-      to = (uint16_t*)a.grad_head + row * a.grad_head_stride;
-    }
-  }
+  if (there && out) to = hidden ? (uint16_t*)a.out.grad + begin : (uint16_t*)a.grad_head + row * a.grad_head_stride;
+  const float scale = hidden ? coef : post;
   const bool whole = __all_sync(~0u, ((uintptr_t)to & 15) == 0);
   float* part = hidden ? sp.hidden + ((long long)t.part * p.cap + row) * p.ldp : sp.head + ((long long)t.part * p.V + row) * p.ldp;
   float* acc = p.acc + (long long)row * p.ldp;
@@ -371,7 +376,7 @@ __device__ __forceinline__ void grad_rows(const TileArgs& a, const Maps& maps, i
       if (there && c < p.d) store_part<T>(part + c, v);
       return;
     }
-    if (hidden || post != 1.0f) {
+    if (scale != 1.0f) {
 #pragma unroll
       for (int j = 0; j < 32; j++) v[j] *= scale;
     }
@@ -393,11 +398,11 @@ __device__ __forceinline__ void grad_rows(const TileArgs& a, const Maps& maps, i
       sums_loaded(v);
       sums_loaded(w);
     }
-    if (out) turn.free();
+    if (out) turn.next();
     pass(v, c);
     pass(w, c + 32);
     if (box) turn.store(&maps.grad_out, c, row - turn.lane);
-    else if (out) turn.store(to ? to + c : nullptr, p.d - c, whole);
+    else if (out) turn.store(to ? to + c : nullptr, end - (row - turn.lane), p.d - c, whole);
   }
 }
 
@@ -424,6 +429,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       bar_init(sums_empty + 8 * s, 2 * kWorkWarps);
     }
     bar_init_visible();
+  }
+  if (threadIdx.x == 32) {
+    if (kForm == 2) {
+      for (const CUtensorMap* m : {&maps.e_k, &maps.head_mn, &maps.e_mn, &maps.hs, &maps.hc_mn, &maps.grad_out}) prefetch_map(m);
+    } else {
+      for (const CUtensorMap* m : {&maps.hc, &maps.head_k, &maps.e_out}) prefetch_map(m);
+    }
   }
   if (kForm != 2 && a.pass.only_again) {  // mostly there is nothing to do
     follow();
@@ -507,7 +519,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     }
   } else if (warp >= 4) {
     const int part = warp - 4, quarter = warp % 4;
-    const Turn turn = {stages + kStages * kStage + part * kTurn, lane};
+    const uint32_t turns = stages + kStages * kStage + part * kTurn;
+    Turn turn = {turns, turns + kTurn / 2, lane};
     const float post = kForm == 2 && again ? *a.p.post : 1.0f;
     int use = 0;
     Task t;
@@ -515,14 +528,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       const int half = use & 1;
       const int row = t.m0 + rank * kHalf + quarter * 32 + lane, off = part / 4 * kHalf;
       const uint32_t from = sums + half * kTile + off + ((uint32_t)quarter * 32 << 16);
+      const LogitsRow is(a, kForm == 1, kForm == 2 ? 0 : n, row);
+      long long begin = 0;
+      float coef = post;
+      if (kForm == 2 && t.job == 0 && row < n) {
+        begin = a.p.to[row];
+        if (!again) coef = a.p.coef[row];
+      }
       if (t.steps > 0) {
         if (!(ok = bar_wait(sums_full + 8 * half, use >> 1 & 1))) break;
         products_fence_after();
       }
       if (kForm == 2) {
-        grad_rows<T>(a, maps, n, again, post, t, from, row, t.n0 + off, turn);
+        grad_rows<T>(a, maps, n, post, coef, begin, t, from, row, t.n0 + off, turn);
       } else if (row - lane < up_div(n, kStepK) * kStepK) {
-        logits_rows<T, kForm == 1>(a, maps, n, from, row, t.n0 + off, turn);
+        logits_rows<T, kForm == 1>(a, maps, n, is, from, row, t.n0 + off, turn);
       }
       if (t.steps > 0) {
         products_fence_before();
@@ -531,7 +551,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         use++;
       }
     }
-    if (lane == 0) boxes_stored();
+    if (lane == 0) boxes_read<0>();
   }
   if (!ok) {
     *a.p.failed = 1;
@@ -570,8 +590,7 @@ __global__ void __launch_bounds__(256) k_head_parts(const __grid_constant__ Tile
     float v[4] = {s.x, s.y, s.z, s.w};
     T* to;
     if (hidden) {
-      const long long r = a.out.r0 + p.src[row];
-      to = (T*)a.out.grad + (r / a.out.n) * a.out.stride_b + (r % a.out.n) * a.out.stride_n;
+      to = (T*)a.out.grad + p.to[row];
     } else {
       to = (T*)a.grad_head + row * a.grad_head_stride;
     }
@@ -600,17 +619,8 @@ GradSplit split_grads(int rows, int d, int V) {
   const long long ct = (d + kTile - 1) / kTile, mt = (rows + kTile - 1) / kTile, vt = (V + (long long)kTile - 1) / kTile;
   const long long kv = (V + (long long)kStepK - 1) / kStepK, kr = (rows + kStepK - 1) / kStepK;
   s.tile_cost = 4;
-  const long long all = mt * ct * (kv + s.tile_cost) + vt * ct * (kr + s.tile_cost), unit = std::max(8ll, all / (3 * kPairs));
-  s.hidden_pairs = kPairs;
+  const long long all = mt * ct * (kv + s.tile_cost) + vt * ct * (kr + s.tile_cost), unit = std::max(8ll, all / kPairs);
   s.hidden_parts = (int)std::min<long long>(kMostParts, (kv + unit - 1) / unit);
-  // Few rows: reading the head and writing its gradient are all of the time, and overlap (32 rows of 4,096 through 126,000: one
-  // after the other 200 and 295 us), each part of a row of tiles by a pair of its own.  Many: all pairs on tiles of one kind
-  // share more of what they read.
-  if (mt == 1) {
-    const long long share = kPairs * ct * (kv + s.tile_cost) / all;
-    s.hidden_parts = (int)std::min<long long>(std::min<long long>(kMostParts, (kv + 7) / 8), std::max(1ll, share / ct));
-    s.hidden_pairs = (int)std::min<long long>(ct * s.hidden_parts, std::max(1ll, share));
-  }
   s.head_parts = (int)std::min<long long>(kMostParts, (kr + unit - 1) / unit);
   return s;
 }
@@ -624,6 +634,7 @@ epic_status launch_head_logits(const HeadPlan& p, int dtype, const LogitsPass& p
   if (!make_map(&maps.hc, a.bf16, p.hc, p.ldh, p.cap, p.ldh, kHalf) ||
       !make_map(&maps.head_k, a.bf16, p.head, p.d, p.V, p.ldw, kHalf))
     return EPIC_ERR_CUDA;
+  maps.e_out = maps.hc;
   if (pass.probs && !make_map(&maps.e_out, a.bf16, p.e, p.lde, p.cap, p.lde, 32)) return EPIC_ERR_CUDA;
   if (pass.probs) return dtype == EPIC_F16 ? launch_tiles<__half, 1>(maps, a, st) : launch_tiles<__nv_bfloat16, 1>(maps, a, st);
   return dtype == EPIC_F16 ? launch_tiles<__half, 0>(maps, a, st) : launch_tiles<__nv_bfloat16, 0>(maps, a, st);
@@ -647,6 +658,7 @@ epic_status launch_head_grads(const HeadPlan& p, int dtype, const HiddenGrad& ou
       !make_map(&maps.head_mn, a.bf16, p.head, p.d, p.V, p.ldw, 64))
     return EPIC_ERR_CUDA;
   a.boxes = grad_head && p.d % 8 == 0 && (uintptr_t)grad_head % 16 == 0 && (p.V == 1 || (stride % 8 == 0 && stride < 1ll << 38));
+  maps.grad_out = maps.e_mn;
   if (a.boxes && !make_map(&maps.grad_out, a.bf16, grad_head, p.d, p.V, p.V == 1 ? p.ldh : stride, 32)) return EPIC_ERR_CUDA;
   const epic_status s = dtype == EPIC_F16 ? launch_tiles<__half, 2>(maps, a, st) : launch_tiles<__nv_bfloat16, 2>(maps, a, st);
   if (s != EPIC_OK) return s;

@@ -173,28 +173,30 @@ constexpr int kMostProducts = 131071;
 // This GPU's tensor units have no fast products of 8-bit integers, but a product of two of them in fp16 is exact, and so are
 // sums in 32-bit floats up to 2^24: of 1,024 products, or of twice as many, four times and so on if 128 times the sum of as
 // many of a row's sizes stays within it in every row (for normally distributed rows, some 4,000).  Then sums are taken over
-// into 32-bit integers.  A pair of CTAs makes 256 tokens x up to 256 rows.  The head's bytes come into a queue in shared memory, by boxes
-// or, where rows start anywhere, row by row with the aligned 16 bytes that they begin and end in; the work warps turn them
-// into fp16 (byte + 128 in the low bits of 1024.0, less 1152) in tensor memory, where the tensor units take them from.
-// Hidden states are turned once, in the workspace, and come by boxes.  Each of four teams of four warps turns every fourth
-// step, so that four chains of loads, stores and arrivals overlap.
+// into 32-bit integers.  A pair of CTAs makes 256 tokens x up to 256 rows.  The head's bytes come into a queue in shared
+// memory, by boxes or, where rows start anywhere, by copies of the work warps' own, from the aligned 16 bytes that a row's
+// part begins in to those that it ends in; the work warps turn them into fp16 (byte + 128 in the low bits of 1024.0, less
+// 1152) in tensor memory, where the tensor units take them from.  Hidden states are turned once, in the workspace, and come
+// by boxes.  Each of four teams of four warps turns every fourth step, so that four chains of loads, stores and arrivals
+// overlap.
 //
-// What was tried before: copies of the work warps' own (cp.async), which every fence between what a warp writes and the tensor
-// units waits for, 1.5 us a step; arrivals released to the whole cluster, 1.3 us; one chain, 0.6 us; the turned operand in
-// shared memory, where it is written and read on top of the queue and the hidden states, 80 KB a step, 0.41 us.
+// What was tried before: an operand in shared memory with copies of the work warps' own, which every fence between what a
+// warp writes and the tensor units waits for, 1.5 us a step; a bulk copy for every row, 1.2 us; arrivals released to the
+// whole cluster, 1.3 us; one chain, 0.6 us; the operand in shared memory, where it is written and read on top of the queue
+// and the hidden states, 80 KB a step, 0.41 us.
 constexpr int kWorkWarps = 16, kWork = 32 * kWorkWarps, kThreads = kWork + 128;
 constexpr int kTileTokens = 256, kHalf = 128, kStepK = 64, kRing = 8, kTeams = 4, kExactSteps = 1024 / kStepK;
 constexpr int kTeam = kWorkWarps / kTeams;  // warps
 constexpr int kOperand = kHalf * kStepK * 2;  // bytes of a step of hidden states
-// A unit of the queue: 64 bytes of each token by a box, or 256 and up to 16 more by a copy a row
+// A unit of the queue: 64 bytes of each token by a box; or 80, of a warp's 32 tokens, that the warp copies for itself
 template <bool kAskew>
 struct Queue {
-  static constexpr int kSteps = kAskew ? 4 : 1, kRow = kSteps * kStepK + (kAskew ? 16 : 0), kUnit = kHalf * kRow;
-  static constexpr int kUnits = kAskew ? 2 : 10;
-  static constexpr int kWarps = kSteps * kTeam;  // that read a unit
+  static constexpr int kRow = kAskew ? 80 : 64, kUnit = kHalf * kRow, kUnits = kAskew ? 8 : 10;
 };
-constexpr int kShared = kRing * kOperand + 10 * kHalf * kStepK + 1024;
-static_assert(2 * Queue<true>::kUnit <= 10 * kHalf * kStepK, "the queue of either form has its place");
+constexpr int kQueue = 10 * kHalf * 64;
+static_assert(Queue<true>::kUnits * Queue<true>::kUnit <= kQueue, "the queue of either form has its place");
+constexpr int kAhead = Queue<true>::kUnits / kTeams;  // steps of its team that a warp has places for
+constexpr int kShared = kRing * kOperand + kQueue + 1024;
 constexpr int kPairs = 76;
 
 struct Int8Bars {
@@ -202,6 +204,16 @@ struct Int8Bars {
   uint32_t sums;
   int most[8];
 };
+
+// 16 bytes at multiples of 16, of which the first `bytes` are read and the rest is 0
+__device__ __forceinline__ void copy16(uint32_t to, const void* from, int bytes) {
+  asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kLeft>
+__device__ __forceinline__ void copies_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory");
+}
 
 // four bytes as four numbers of fp16
 __device__ __forceinline__ uint2 halves_of(uint32_t w) {
@@ -238,8 +250,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       bar_init(empty + 8 * s, 1);
     }
     for (int s = 0; s < Q::kUnits; s++) {
-      bar_init(come + 8 * s, kAskew ? 32 : 1);
-      bar_init(gone + 8 * s, Q::kWarps);
+      bar_init(come + 8 * s, 1);
+      bar_init(gone + 8 * s, kTeam);
     }
     for (int s = 0; s < 2; s++) {
       bar_init(sums_full + 8 * s, 1);
@@ -301,35 +313,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         }
       }
     }
-    if (warp == kWorkWarps + 2 && (kAskew || lane == 0)) {  // the head's bytes
+    if (!kAskew && warp == kWorkWarps + 2 && lane == 0) {  // boxes of the head's bytes
       int s = 0;
       uint32_t turn = 0;
       for (int t = pair; ok && t < tiles; t += kPairs) {
-        const long long v0 = (long long)(t / row_tiles) * kTileTokens + rank * kHalf;
-        for (int k = 0; k < steps; k += Q::kSteps) {
+        const int v0 = t / row_tiles * kTileTokens + rank * kHalf;
+        for (int k = 0; k < steps; k++) {
           if (!(ok = bar_wait(gone + 8 * s, turn ^ 1))) break;
-          const uint32_t to = queue + s * Q::kUnit, bar = come + 8 * s;
-          if (!kAskew) {
-            bar_expect(bar, Q::kUnit);
-            load_box(&head_map, to, bar, k * kStepK, (int)v0);
-          } else {
-            // from the aligned 16 bytes that the part begins in to those that it ends in; a barrier counts what comes
-            uint32_t bytes[kHalf / 32], all = 0;
-            const int part = min(a.d - k * kStepK, Q::kSteps * kStepK);
-#pragma unroll
-            for (int i = 0; i < kHalf / 32; i++) {
-              const long long v = v0 + i * 32 + lane;
-              const int m = (int)((uintptr_t)(a.head + v * a.head_stride) & 15);
-              bytes[i] = v < a.V ? (m + part + 15) / 16 * 16 : 0;
-              all += bytes[i];
-            }
-            bar_expect(bar, all);
-#pragma unroll
-            for (int i = 0; i < kHalf / 32; i++) {
-              const int8_t* w = a.head + (v0 + i * 32 + lane) * a.head_stride + k * kStepK;
-              if (bytes[i]) load_run(to + (i * 32 + lane) * Q::kRow, (const void*)((uintptr_t)w & ~(uintptr_t)15), bytes[i], bar);
-            }
-          }
+          bar_expect(come + 8 * s, Q::kUnit);
+          load_box(&head_map, queue + s * Q::kUnit, come + 8 * s, k * kStepK, v0);
           if (++s == Q::kUnits) s = 0, turn ^= 1;
         }
       }
@@ -431,6 +423,28 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 
     // n: the team's next step of all, step k of the pair's tile `tile`
     int n = team, tile = n / steps, k = n % steps;
+
+    // A warp's own copies of its 32 tokens' bytes, 5 chunks of 16 each, kAhead - 1 steps of its team ahead: step ahead_k of
+    // the pair's tile ahead_tile, into its part of place `ahead`
+    int ahead = team, ahead_tile = tile, ahead_k = k;
+    auto copy = [&] {
+      if (ahead_tile < own) {
+        const int v0 = (pair + ahead_tile * kPairs) / row_tiles * kTileTokens + rank * kHalf + quarter * 32;
+#pragma unroll
+        for (int i = 0; i < 5; i++) {
+          const int chunk = i * 32 + lane, row = chunk / 5, v = min(v0 + row, a.V - 1);
+          const uintptr_t w = (uintptr_t)(a.head + v * a.head_stride + ahead_k * kStepK), end = w + (a.d - ahead_k * kStepK);
+          const uintptr_t first = w & ~(uintptr_t)15, from = first + chunk % 5 * 16;
+          copy16(queue + ahead * Q::kUnit + (quarter * 32 * 5 + chunk) * 16, (const void*)(from < end ? from : first),
+                 from < end ? (int)min((uintptr_t)16, end - from) : 0);
+        }
+        if ((ahead += kTeams) >= Q::kUnits) ahead = team;
+        for (ahead_k += kTeams; ahead_k >= steps; ahead_k -= steps) ahead_tile++;
+      }
+      copies_commit();
+    };
+    if (kAskew)
+      for (int i = 1; i < kAhead; i++) copy();
     while (ok) {
       // sums are taken over before the step in whose place this one comes waits for theirs
       const bool due = use < own * per && (tile >= own || past + kRing <= n);
@@ -442,10 +456,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         continue;
       }
       if (tile >= own) break;
-      const int unit = kAskew ? tile * ((steps + Q::kSteps - 1) / Q::kSteps) + k / Q::kSteps : n, place = unit % Q::kUnits;
-      const uint32_t at = queue + place * Q::kUnit + token * Q::kRow + k % Q::kSteps * kStepK;
-      const int s = n % kRing;
-      if (!(ok = bar_wait(come + 8 * place, unit / Q::kUnits & 1))) break;
+      const int s = n % kRing, place = n % Q::kUnits;
+      const uint32_t at = queue + place * Q::kUnit + token * Q::kRow;
+      if (kAskew) {
+        copy();
+        copies_wait<kAhead - 1>();
+        __syncwarp();
+      } else if (!(ok = bar_wait(come + 8 * place, n / Q::kUnits & 1))) {
+        break;
+      }
       if (!(ok = bar_wait(empty + 8 * s, (n / kRing & 1) ^ 1))) break;
       products_fence_after();
       uint32_t m = 0;  // bytes ahead of the token's row in its first 16
@@ -474,8 +493,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       __syncwarp();
       if (lane == 0) {
         bar_arrive_cluster(full0 + 8 * s);
-        // the last step of a row also answers for the unit's that do not exist
-        bar_arrive(gone + 8 * place, k + 1 == steps ? Q::kSteps - k % Q::kSteps : 1);
+        if (!kAskew) bar_arrive(gone + 8 * place, 1);
       }
       n += kTeams;
       for (k += kTeams; k >= steps; k -= steps) tile++;

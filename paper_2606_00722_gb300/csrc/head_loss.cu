@@ -193,6 +193,7 @@ __global__ void __launch_bounds__(kRowsThreads) k_head_rows(RowsArgs a) {
       }
       if (at == 0) {
         p.src[q] = (int)i;
+        p.to[q] = b * a.out.stride_b + pos * a.out.stride_n;
         p.tgt[q] = y;
         p.g[q] = g;
         if (a.probs) p.ref[q] = whole_ref(dot);
@@ -402,6 +403,7 @@ size_t plan_head(const HeadCall& c, void* base, HeadPlan& p) {
   w.take(p.counts, kPieceRows / kRowsThreads, 4);
   w.take(p.tops, kPieceRows / kRowsThreads, 4);
   w.take(p.src, cap, 4);
+  w.take(p.to, cap, 8);
   w.take(p.tgt, cap, 4);
   for (float** f : {&p.g, &p.zt, &p.ref, &p.coef, &p.known_ref, &p.known_mul, &p.known_at}) w.take(*f, cap, 4);
   w.take(p.hc, cap * p.ldh, 2);

@@ -16,7 +16,6 @@ constexpr int kMostParts = 64;  // of a gradient's sum
 // tokens, of the head's over the positions.  1: not cut; 0: no such gradient.
 struct GradSplit {
   int hidden_parts, head_parts;
-  int hidden_pairs;     // of CTAs, that make gradients of hidden states
   int tile_cost;        // what a tile costs beside its sum, in steps of it
   float *hidden, *head; // [parts][cap][ldp], [parts][V][ldp]
 };
@@ -35,6 +34,7 @@ struct HeadPlan {
   int* counts;              // of 256 positions each, and the largest factor among them
   float* tops;
   int* src;                 // [cap] position in the piece
+  long long* to;            // [cap] where the row's gradient begins, from the first position's
   int* tgt;                 // [cap] target token
   float *g;                 // [cap] what the row's gradient is multiplied with (weight, gradient from above)
   float *zt;                // [cap] logit of the target
@@ -55,7 +55,7 @@ struct HeadPlan {
 // How a piece's gradient of the head meets the pieces before it
 enum HeadSum { kOnly = 0, kFirst = 1, kMiddle = 2, kLast = 3 };
 
-// Where gradients of hidden states go: position r of the piece is grad[r0 + r], split into [b][i] by n.
+// Where gradients of hidden states go: position r of the piece is position r0 + r of [b][n].
 struct HiddenGrad {
   void* grad;
   long long stride_b, stride_n, r0;

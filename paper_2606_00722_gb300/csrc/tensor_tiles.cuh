@@ -89,12 +89,6 @@ __device__ __forceinline__ void load_box(const CUtensorMap* map, uint32_t dst, u
       "l"(map), "r"(bar), "r"(x), "r"(y)
       : "memory");
 }
-// `bytes` of memory, addresses and bytes multiples of 16
-__device__ __forceinline__ void load_run(uint32_t dst, const void* from, uint32_t bytes, uint32_t bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(from),
-               "r"(bytes), "r"(bar)
-               : "memory");
-}
 // A box from shared memory to (x, y), x and y not negative; rows past the tensor's end are left out, and columns
 // but for those that begin in the last one's 16 bytes.
 __device__ __forceinline__ void store_box(const CUtensorMap* map, uint32_t from, int x, int y) {
@@ -102,9 +96,14 @@ __device__ __forceinline__ void store_box(const CUtensorMap* map, uint32_t from,
                : "memory");
   asm volatile("cp.async.bulk.commit_group;" ::: "memory");
 }
-// the thread's stores have read their boxes; have written them
-__device__ __forceinline__ void boxes_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
-__device__ __forceinline__ void boxes_stored() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+// the thread's stores have read their boxes, but for the last kLeft
+template <int kLeft>
+__device__ __forceinline__ void boxes_read() {
+  asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kLeft) : "memory");
+}
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* map) {
+  asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
+}
 __device__ __forceinline__ void shared_to_boxes() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 // ---- operands in shared memory: rows of 128 bytes, their chunks of 16 swizzled by the row's number in 8
