@@ -47,11 +47,6 @@ struct TileArgs {
   long long grad_head_stride;
   HeadSum sum;
   int bf16;
-  bool boxes;  // rows of grad_head start at multiples of 16 bytes and end there (a box's end is cut in whole 16 bytes)
-};
-
-struct Maps {
-  CUtensorMap hc, hc_mn, hs, head_k, head_mn, e_k, e_mn, e_out, grad_out;
 };
 
 __device__ __forceinline__ int up_div(int a, int b) { return (a + b - 1) / b; }
@@ -270,7 +265,7 @@ struct LogitsRow {
 
 // Logits of one row, kRecCols columns from `sums`: the record, and with `probs` the exponentials.  z is only ever in registers.
 template <typename T, bool kProbs>
-__device__ __forceinline__ void logits_rows(const TileArgs& a, const Maps& maps, int n, const LogitsRow& is, uint32_t sums,
+__device__ __forceinline__ void logits_rows(const TileArgs& a, const HeadMaps& maps, int n, const LogitsRow& is, uint32_t sums,
                                             int row, int col, Turn& turn) {
   const HeadPlan& p = a.p;
   const bool real = row < n, known = a.pass.known;
@@ -352,7 +347,7 @@ __device__ __forceinline__ void store_part(float* part, const float (&v)[32]) {
 
 // Sums of a gradient's tile: kHalf columns of each lane's row, 64 at a time
 template <typename T>
-__device__ __forceinline__ void grad_rows(const TileArgs& a, const Maps& maps, int n, float post, float coef, long long begin,
+__device__ __forceinline__ void grad_rows(const TileArgs& a, const HeadMaps& maps, int n, float post, float coef, long long begin,
                                           const Task& t, uint32_t sums, int row, int col, Turn& turn) {
   const HeadPlan& p = a.p;
   const GradSplit& sp = a.p.split;
@@ -360,7 +355,7 @@ __device__ __forceinline__ void grad_rows(const TileArgs& a, const Maps& maps, i
   const bool parts = (hidden ? sp.hidden_parts : sp.head_parts) > 1;
   const int end = hidden ? n : p.V;
   if (row - turn.lane >= end) return;
-  const bool there = row < end, out = !parts && (hidden || a.sum == kOnly || a.sum == kLast), box = out && !hidden && a.boxes;
+  const bool there = row < end, out = !parts && (hidden || a.sum == kOnly || a.sum == kLast), box = out && !hidden && maps.boxes;
   uint16_t* to = nullptr;
   if (there && out) to = hidden ? (uint16_t*)a.out.grad + begin : (uint16_t*)a.grad_head + row * a.grad_head_stride;
   const float scale = hidden ? coef : post;
@@ -409,7 +404,7 @@ __device__ __forceinline__ void grad_rows(const TileArgs& a, const Maps& maps, i
 // kForm 0: records; 1: exponentials (and records); 2: gradients
 template <typename T, int kForm>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
-    k_head_tiles(const __grid_constant__ Maps maps, const __grid_constant__ TileArgs a) {
+    k_head_tiles(const __grid_constant__ HeadMaps maps, const __grid_constant__ TileArgs a) {
   extern __shared__ uint8_t shared_raw[];
   __shared__ Bars bars;
   uint8_t* shared = (uint8_t*)(((uintptr_t)shared_raw + 1023) / 1024 * 1024);
@@ -430,13 +425,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     }
     bar_init_visible();
   }
-  if (threadIdx.x == 32) {
-    if (kForm == 2) {
-      for (const CUtensorMap* m : {&maps.e_k, &maps.head_mn, &maps.e_mn, &maps.hs, &maps.hc_mn, &maps.grad_out}) prefetch_map(m);
-    } else {
-      for (const CUtensorMap* m : {&maps.hc, &maps.head_k, &maps.e_out}) prefetch_map(m);
-    }
-  }
+  if (threadIdx.x == 32)
+    for (const CUtensorMap* m : {&maps.hc, &maps.hs, &maps.head, &maps.e, &maps.e_out, &maps.grad_out}) prefetch_map(m);
   if (kForm != 2 && a.pass.only_again) {  // mostly there is nothing to do
     follow();
     if (*a.p.again == 0) return;
@@ -466,19 +456,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           if (!(ok = bar_wait(empty + 8 * s, turn ^ 1))) break;
           if (rank == 0) bar_expect(full + 8 * s, 2 * kStage);
           const uint32_t A = stages + s * kStage, B = A + kOperand, bar = full0 + 8 * s;
-          if (kForm != 2) {
-            load_box_pair(&maps.hc, A, bar, k * kStepK, m);
-            load_box_pair(&maps.head_k, B, bar, k * kStepK, c);
-          } else if (t.job == 0) {
-            load_box_pair(&maps.e_k, A, bar, k * kStepK, m);
-            load_box_pair(&maps.head_mn, B, bar, c, k * kStepK);
-            load_box_pair(&maps.head_mn, B + kOperand / 2, bar, c + 64, k * kStepK);
-          } else {
-            load_box_pair(&maps.e_mn, A, bar, m, k * kStepK);
-            load_box_pair(&maps.e_mn, A + kOperand / 2, bar, m + 64, k * kStepK);
-            const CUtensorMap* h = again ? &maps.hc_mn : &maps.hs;
-            load_box_pair(h, B, bar, c, k * kStepK);
-            load_box_pair(h, B + kOperand / 2, bar, c + 64, k * kStepK);
+          // 128 rows of 64 along the sum, or 64 of the sum by 128 across it: two boxes each
+          const CUtensorMap* ma = kForm == 2 ? &maps.e : &maps.hc;
+          const CUtensorMap* mb = kForm != 2 || t.job == 0 ? &maps.head : again ? &maps.hc : &maps.hs;
+          const bool a_across = kForm == 2 && t.job == 1, b_across = kForm == 2;
+          const int at = k * kStepK;
+#pragma unroll
+          for (int i = 0; i < 2; i++) {
+            load_box_pair(ma, A + i * kOperand / 2, bar, a_across ? m + 64 * i : at, a_across ? at : m + 64 * i);
+            load_box_pair(mb, B + i * kOperand / 2, bar, b_across ? c + 64 * i : at, b_across ? at : c + 64 * i);
           }
           if (++s == kStages) s = 0, turn ^= 1;
         }
@@ -608,7 +594,7 @@ __global__ void __launch_bounds__(256) k_head_parts(const __grid_constant__ Tile
 // ---------------------------------------------------------------- host
 
 template <typename T, int kForm>
-epic_status launch_tiles(const Maps& maps, const TileArgs& a, cudaStream_t st) {
+epic_status launch_tiles(const HeadMaps& maps, const TileArgs& a, cudaStream_t st) {
   return launch_next(k_head_tiles<T, kForm>, 2 * kPairs, kThreads, kShared, kShared, st, maps, a);
 }
 
@@ -625,24 +611,32 @@ GradSplit split_grads(int rows, int d, int V) {
   return s;
 }
 
-epic_status launch_head_logits(const HeadPlan& p, int dtype, const LogitsPass& pass, cudaStream_t st) {
-  Maps maps = {};
+epic_status make_head_maps(HeadMaps& maps, const HeadPlan& p, int dtype, bool grads, void* grad_head, long long stride) {
+  const bool bf16 = dtype == EPIC_BF16;
+  if (!make_map(&maps.hc, bf16, p.hc, p.ldh, p.cap, p.ldh, 64) || !make_map(&maps.head, bf16, p.head, p.d, p.V, p.ldw, 64))
+    return EPIC_ERR_CUDA;
+  maps.hs = maps.e = maps.e_out = maps.grad_out = maps.hc;
+  if (p.V == 1) stride = p.ldh;
+  maps.boxes = grad_head && p.d % 8 == 0 && (uintptr_t)grad_head % 16 == 0 && stride % 8 == 0 && stride < 1ll << 38;
+  if (!grads) return EPIC_OK;
+  if (!make_map(&maps.e, bf16, p.e, p.lde, p.cap, p.lde, 64) || !make_map(&maps.e_out, bf16, p.e, p.lde, p.cap, p.lde, 32) ||
+      (p.hs && !make_map(&maps.hs, bf16, p.hs, p.ldh, p.cap, p.ldh, 64)) ||
+      (maps.boxes && !make_map(&maps.grad_out, bf16, grad_head, p.d, p.V, stride, 32)))
+    return EPIC_ERR_CUDA;
+  return EPIC_OK;
+}
+
+epic_status launch_head_logits(const HeadPlan& p, const HeadMaps& maps, int dtype, const LogitsPass& pass, cudaStream_t st) {
   TileArgs a = {};
   a.p = p;
   a.pass = pass;
   a.bf16 = dtype == EPIC_BF16;
-  if (!make_map(&maps.hc, a.bf16, p.hc, p.ldh, p.cap, p.ldh, kHalf) ||
-      !make_map(&maps.head_k, a.bf16, p.head, p.d, p.V, p.ldw, kHalf))
-    return EPIC_ERR_CUDA;
-  maps.e_out = maps.hc;
-  if (pass.probs && !make_map(&maps.e_out, a.bf16, p.e, p.lde, p.cap, p.lde, 32)) return EPIC_ERR_CUDA;
-  if (pass.probs) return dtype == EPIC_F16 ? launch_tiles<__half, 1>(maps, a, st) : launch_tiles<__nv_bfloat16, 1>(maps, a, st);
-  return dtype == EPIC_F16 ? launch_tiles<__half, 0>(maps, a, st) : launch_tiles<__nv_bfloat16, 0>(maps, a, st);
+  if (pass.probs) return a.bf16 ? launch_tiles<__nv_bfloat16, 1>(maps, a, st) : launch_tiles<__half, 1>(maps, a, st);
+  return a.bf16 ? launch_tiles<__nv_bfloat16, 0>(maps, a, st) : launch_tiles<__half, 0>(maps, a, st);
 }
 
-epic_status launch_head_grads(const HeadPlan& p, int dtype, const HiddenGrad& out, void* grad_head, long long stride,
-                              HeadSum sum, cudaStream_t st) {
-  Maps maps = {};
+epic_status launch_head_grads(const HeadPlan& p, const HeadMaps& maps, int dtype, const HiddenGrad& out, void* grad_head,
+                              long long stride, HeadSum sum, cudaStream_t st) {
   TileArgs a = {};
   a.p = p;
   a.out = out;
@@ -652,21 +646,13 @@ epic_status launch_head_grads(const HeadPlan& p, int dtype, const HiddenGrad& ou
   a.bf16 = dtype == EPIC_BF16;
   if (!out.grad) a.p.split.hidden_parts = 0;
   if (!grad_head) a.p.split.head_parts = 0;
-  if (!make_map(&maps.hc_mn, a.bf16, p.hc, p.ldh, p.cap, p.ldh, 64) ||
-      !make_map(&maps.hs, a.bf16, p.hs ? p.hs : p.hc, p.ldh, p.cap, p.ldh, 64) || !make_map(&maps.e_k, a.bf16, p.e, p.lde, p.cap, p.lde, kHalf) ||
-      !make_map(&maps.e_mn, a.bf16, p.e, p.lde, p.cap, p.lde, 64) ||
-      !make_map(&maps.head_mn, a.bf16, p.head, p.d, p.V, p.ldw, 64))
-    return EPIC_ERR_CUDA;
-  a.boxes = grad_head && p.d % 8 == 0 && (uintptr_t)grad_head % 16 == 0 && (p.V == 1 || (stride % 8 == 0 && stride < 1ll << 38));
-  maps.grad_out = maps.e_mn;
-  if (a.boxes && !make_map(&maps.grad_out, a.bf16, grad_head, p.d, p.V, p.V == 1 ? p.ldh : stride, 32)) return EPIC_ERR_CUDA;
-  const epic_status s = dtype == EPIC_F16 ? launch_tiles<__half, 2>(maps, a, st) : launch_tiles<__nv_bfloat16, 2>(maps, a, st);
+  const epic_status s = a.bf16 ? launch_tiles<__nv_bfloat16, 2>(maps, a, st) : launch_tiles<__half, 2>(maps, a, st);
   if (s != EPIC_OK) return s;
   const bool hidden = a.p.split.hidden_parts > 1, head = a.p.split.head_parts > 1;
   if (!hidden && !head) return EPIC_OK;
   const long long most = std::max(hidden ? (long long)p.rows : 0, head ? (long long)p.V : 0) * ((p.d + 3) / 4);
   const dim3 grid((unsigned)std::min(1216ll, (most + 255) / 256), hidden && head ? 2 : 1);
-  return launch_next(dtype == EPIC_F16 ? k_head_parts<__half> : k_head_parts<__nv_bfloat16>, grid, 256, 0, kNoCache, st, a);
+  return launch_next(a.bf16 ? k_head_parts<__nv_bfloat16> : k_head_parts<__half>, grid, 256, 0, kNoCache, st, a);
 }
 
 }  // namespace epic

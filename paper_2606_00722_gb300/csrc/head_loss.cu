@@ -457,6 +457,8 @@ epic_status run_head(const HeadCall& c, const HeadTensors& t, HeadPlan p, cudaSt
     EPIC_TRY(launch_next(k_head_pack<T>, (unsigned)std::min(2432, (c.V + 7) / 8), 256, 0, kNoCache, st, (const T*)c.head,
                          c.head_stride, (T*)p.head, p.ldw, c.d, c.V));
   }
+  HeadMaps maps;
+  if (c.V > 0) EPIC_TRY(make_head_maps(maps, p, c.dtype, grads, t.grad_head, t.ghead_stride));
   for (long long r0 = 0; r0 < rows; r0 += p.cap) {
     p.rows = (int)std::min<long long>(p.cap, rows - r0);
     RowsArgs a = {};
@@ -487,15 +489,15 @@ epic_status run_head(const HeadCall& c, const HeadTensors& t, HeadPlan p, cudaSt
     if (c.V == 0) continue;
     // A step's exponentials are relative to the target's logit; fp16 has not the range for that and makes them once the
     // logsumexp is known, as do rows that leave the window.
-    EPIC_TRY(launch_head_logits(p, c.dtype, {true, stored, known, false}, st));
+    EPIC_TRY(launch_head_logits(p, maps, c.dtype, {true, stored, known, false}, st));
     const MeetArgs m = {p, r0, t.weight, t.loss, t.lse, grads, stored, known};
     EPIC_TRY(launch_next(few ? k_head_meet<T, 1> : k_head_meet<T, 8>, few ? p.rows : (p.rows + 7) / 8, kMeetWarps * 32, 0, kNoCache,
                          st, m));
-    if (grads && !known) EPIC_TRY(launch_head_logits(p, c.dtype, {false, true, true, true}, st));
+    if (grads && !known) EPIC_TRY(launch_head_logits(p, maps, c.dtype, {false, true, true, true}, st));
     if (t.grad_hidden || t.grad_head) {
       const bool first = r0 == 0, last = r0 + p.cap >= rows;
       const HeadSum sum = first ? (last ? kOnly : kFirst) : last ? kLast : kMiddle;
-      EPIC_TRY(launch_head_grads(p, c.dtype, a.out, t.grad_head, t.ghead_stride, sum, st));
+      EPIC_TRY(launch_head_grads(p, maps, c.dtype, a.out, t.grad_head, t.ghead_stride, sum, st));
     }
   }
   return EPIC_OK;

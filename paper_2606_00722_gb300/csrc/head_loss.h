@@ -1,6 +1,7 @@
 // What the kernels of the head's loss share: the plan of one piece of a call
 // (sizes, operands, workspace) and their launchers.
 #pragma once
+#include <cuda.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -67,11 +68,20 @@ struct HiddenGrad {
 struct LogitsPass {
   bool sums, probs, known, only_again;
 };
-epic_status launch_head_logits(const HeadPlan& p, int dtype, const LogitsPass& pass, cudaStream_t st);
-// Gradients of hidden states, grad[src] = coef e W (out.grad NULL: none), and of the head, grad_head [V][stride] = e^T hs with
-// the pieces before (NULL: none); of gradients of logits in e, post e W and post e^T hc.
-epic_status launch_head_grads(const HeadPlan& p, int dtype, const HiddenGrad& out, void* grad_head, long long stride,
-                              HeadSum sum, cudaStream_t st);
+// How boxes of the operands are copied, the same for all of a call's kernels and pieces: 64 columns by 64 rows, those that go
+// out by 32 rows
+struct HeadMaps {
+  CUtensorMap hc, hs, head, e, e_out, grad_out;
+  bool boxes;  // rows of grad_out start at multiples of 16 bytes and end there (a box's end is cut in whole 16 bytes)
+};
+// grads: they are wanted; grad_head: or NULL
+epic_status make_head_maps(HeadMaps& maps, const HeadPlan& p, int dtype, bool grads, void* grad_head, long long stride);
+
+epic_status launch_head_logits(const HeadPlan& p, const HeadMaps& maps, int dtype, const LogitsPass& pass, cudaStream_t st);
+// Gradients of hidden states, grad[to] = coef e W (out.grad NULL: none), and of the head, grad_head [V][stride] = e^T hs with the
+// pieces before (NULL: none); of gradients of logits in e, post e W and post e^T hc.
+epic_status launch_head_grads(const HeadPlan& p, const HeadMaps& maps, int dtype, const HiddenGrad& out, void* grad_head,
+                              long long stride, HeadSum sum, cudaStream_t st);
 GradSplit split_grads(int rows, int d, int V);
 
 }  // namespace epic

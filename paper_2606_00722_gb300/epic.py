@@ -383,18 +383,19 @@ def extract_witness(g: Grammar, t: LexTable, x, terms, lengths, stream=None):
 _DTYPES = {}  # torch dtype of logits -> the C-ABI's code; filled on the first call
 _T = None     # torch, and what the calls need of it
 _INT8 = None
+_empty = None  # torch.empty
 _raw_stream = None
 _current_device = None
 
 
 def _logits_init():
-    global _T, _INT8, _raw_stream, _current_device
+    global _T, _INT8, _empty, _raw_stream, _current_device
     import torch
     _DTYPES.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2})
     _raw_stream = getattr(torch._C, '_cuda_getCurrentRawStream', None) or (
         lambda device: torch.cuda.current_stream(device).cuda_stream)
     _current_device = getattr(torch._C, '_cuda_getDevice', None) or torch.cuda.current_device
-    _INT8 = torch.int8
+    _INT8, _empty = torch.int8, torch.empty
     _T = (torch.float32, torch.int32, torch.uint8)
 
 
@@ -612,15 +613,19 @@ def _weights(t, d, dtype, name, device):
 def _scratch(query, args, workspace, device, stream):
     """(tensor, address, bytes) of the workspace that the library asks for; a caller's own has to be that large."""
     need = C.c_size_t()
-    _check(query(*args, C.byref(need)), query.__name__)
+    status = query(*args, C.byref(need))
+    if status:
+        _check(status, query.__name__)
     if workspace is None:
-        import torch
+        need = need.value
         if stream is None:
-            workspace = torch.empty(need.value, dtype=torch.uint8, device=device)
+            workspace = _empty(need, dtype=_T[2], device=device)
         else:
+            import torch
             on = torch.cuda.ExternalStream(stream, device=device) if isinstance(stream, int) else stream
             with torch.cuda.stream(on):
-                workspace = torch.empty(need.value, dtype=torch.uint8, device=device)
+                workspace = _empty(need, dtype=_T[2], device=device)
+        return workspace, workspace.data_ptr(), need
     elif workspace.get_device() != device or not workspace.is_contiguous():
         raise ValueError('workspace: expected a contiguous tensor on CUDA device %d' % device)
     return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
