@@ -175,10 +175,22 @@ struct Turn {
                    "r"(pack2<T>(v[8 * c + 4], v[8 * c + 5])), "r"(pack2<T>(v[8 * c + 6], v[8 * c + 7]))
                    : "memory");
   }
-  __device__ __forceinline__ uint32_t element(int row, int i) const {
-    uint16_t v;
-    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(chunk(row, i / 8) + i % 8 * 2) : "memory");
-    return v;
+  // all 64, or from the second on
+  template <typename T>
+  __device__ __forceinline__ void put(const float (&v)[32], const float (&w)[32], bool second) const {
+    float x[65];
+#pragma unroll
+    for (int i = 0; i < 32; i++) x[i] = v[i], x[32 + i] = w[i];
+    x[64] = 0.0f;
+#pragma unroll
+    for (int c = 0; c < 8; c++) {
+      uint32_t o[4];
+#pragma unroll
+      for (int i = 0; i < 4; i++)
+        o[i] = pack2<T>(second ? x[8 * c + 2 * i + 1] : x[8 * c + 2 * i], second ? x[8 * c + 2 * i + 2] : x[8 * c + 2 * i + 1]);
+      asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(chunk(lane, c)), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3])
+                   : "memory");
+    }
   }
   // before the first put: to the other buffer, whose box has left
   __device__ __forceinline__ void next() {
@@ -193,42 +205,45 @@ struct Turn {
     __syncwarp();
     if (lane == 0) store_box(map, at, x, y);
   }
-  // to each lane's row `to` (NULL from row `rows` on), of which `count` elements exist (the same in all lanes), 8 lanes a row if all rows
-  // start at multiples of 16 bytes (`whole`), else a warp a row, two elements a lane from the row's first multiple of 4
-  // bytes on.  Loads of several rows go before their stores.
-  __device__ __forceinline__ void store(uint16_t* to, int rows, int count, bool whole) const {
+  // to each lane's row `to` (NULL from row `rows` on), which starts at a multiple of 16 bytes, 64 elements: 8 lanes a row
+  __device__ __forceinline__ void store_whole(uint16_t* to) const {
     __syncwarp();
-    count = min(count, 64);
-    if (whole && count == 64) {
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+      const int row = i * 4 + lane / 8;
+      uint16_t* p = (uint16_t*)__shfl_sync(~0u, (unsigned long long)to, row);
+      uint4 v;
+      asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                   : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                   : "r"(chunk(row, lane % 8))
+                   : "memory");
+      if (p) *(uint4*)(p + lane % 8 * 8) = v;
+    }
+  }
+  // the same of rows that start anywhere, `count` elements of up to 64 (the same in all lanes): a warp a row, two elements a
+  // lane.  Rows that start at an odd element were put from the second on; lanes write their own row's ends.
+  __device__ __forceinline__ void store_runs(uint16_t* to, int rows, int count, uint32_t first) const {
+    const bool odd = (uintptr_t)to & 2;
+    const uint32_t odds = __ballot_sync(~0u, odd);
+    __syncwarp();
+    if (to && odd) *to = (uint16_t)first;
+    const int last = count - 1 - odd;  // in what was put
+    if (to && last >= 0 && last % 2 == 0) {
+      uint16_t v;
+      asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(chunk(lane, last / 8) + last % 8 * 2) : "memory");
+      to[count - 1] = v;
+    }
+    to += odd;
+#pragma unroll 1
+    for (int row0 = 0; row0 < min(rows, 32); row0 += 8) {
+      uint32_t two[8];
+#pragma unroll
+      for (int i = 0; i < 8; i++)
+        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(two[i]) : "r"(at + (row0 + i) * 128 + ((lane / 4) ^ i) * 16 + lane % 4 * 4) : "memory");
 #pragma unroll
       for (int i = 0; i < 8; i++) {
-        const int row = i * 4 + lane / 8;
-        uint16_t* p = (uint16_t*)__shfl_sync(~0u, (unsigned long long)to, row);
-        uint4 v;
-        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                     : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-                     : "r"(chunk(row, lane % 8))
-                     : "memory");
-        if (p) *(uint4*)(p + lane % 8 * 8) = v;
-      }
-      return;
-    }
-#pragma unroll 2
-    for (int row0 = 0; row0 < min(rows, 32); row0 += 4) {
-      uint16_t* p[4];
-      uint32_t two[4];
-      int j[4];
-#pragma unroll
-      for (int i = 0; i < 4; i++) {
-        p[i] = (uint16_t*)__shfl_sync(~0u, (unsigned long long)to, row0 + i);
-        j[i] = 2 * lane + (int)((uintptr_t)p[i] / 2 % 2);
-        two[i] = element(row0 + i, j[i]) | element(row0 + i, j[i] + 1) << 16;  // past the row: of its beginning, not used
-      }
-#pragma unroll
-      for (int i = 0; i < 4; i++) {
-        if (p[i] && j[i] + 1 < count) *(uint32_t*)(p[i] + j[i]) = two[i];
-        if (p[i] && j[i] + 1 == count) p[i][j[i]] = (uint16_t)two[i];
-        if (p[i] && j[i] == 1) p[i][0] = (uint16_t)element(row0 + i, 0);
+        uint32_t* p = (uint32_t*)__shfl_sync(~0u, (unsigned long long)to, row0 + i);
+        if (row0 + i < rows && 2 * lane + 1 < count - (int)(odds >> (row0 + i) & 1)) p[lane] = two[i];
       }
     }
   }
@@ -382,7 +397,6 @@ __device__ __forceinline__ void grad_rows(const TileArgs& a, const HeadMaps& map
       }
       if (a.sum != kLast) store_part<T>(acc + c, v);
     }
-    if (out) turn.put<T>(v, c / 32 % 2);
   };
 #pragma unroll 1
   for (int c = col; c < col + kHalf && c < p.d; c += 64) {
@@ -396,8 +410,18 @@ __device__ __forceinline__ void grad_rows(const TileArgs& a, const HeadMaps& map
     if (out) turn.next();
     pass(v, c);
     pass(w, c + 32);
-    if (box) turn.store(&maps.grad_out, c, row - turn.lane);
-    else if (out) turn.store(to ? to + c : nullptr, end - (row - turn.lane), p.d - c, whole);
+    if (!out) continue;
+    const bool runs = !box && !(whole && p.d - c >= 64);
+    uint16_t* here = to ? to + c : nullptr;
+    if (runs) {
+      turn.put<T>(v, w, (uintptr_t)here & 2);
+      turn.store_runs(here, end - (row - turn.lane), min(p.d - c, 64), pack2<T>(v[0], v[0]) & 0xffff);
+    } else {
+      turn.put<T>(v, 0);
+      turn.put<T>(w, 1);
+      if (box) turn.store(&maps.grad_out, c, row - turn.lane);
+      else turn.store_whole(here);
+    }
   }
 }
 
