@@ -47,6 +47,7 @@ struct TileArgs {
   long long grad_head_stride;
   HeadSum sum;
   int bf16;
+  int pairs;  // of CTAs
 };
 
 __device__ __forceinline__ int up_div(int a, int b) { return (a + b - 1) / b; }
@@ -69,16 +70,16 @@ struct Divisor {
 // Logits: the rows' tiles of one column of tiles after another, so that the head is read once.
 struct LogitsTasks {
   Divisor row_tiles;
-  int at, tiles, steps;
+  int at, tiles, steps, pairs;
   __device__ __forceinline__ LogitsTasks(const TileArgs& a, int n, int pair)
       : row_tiles(max(1, up_div(n, kTile))), at(pair), tiles(up_div(n, kTile) * up_div(a.p.V, kTile)),
-        steps(up_div(a.p.d, kStepK)) {}
+        steps(up_div(a.p.d, kStepK)), pairs(a.pairs) {}
   __device__ __forceinline__ bool next(Task& t) {
     if (at >= tiles) return false;
     int m;
     const int column = row_tiles.of(at, m);
     t = {m * kTile, column * kTile, 0, steps, 0, 0};
-    at += kPairs;
+    at += pairs;
     return true;
   }
 };
@@ -87,10 +88,11 @@ struct LogitsTasks {
 // without a last one take as many of the latter as it is worth before the rest is dealt to all.
 struct GradTasks {
   Divisor columns;
+  int pairs;
   int row_tiles, head_tiles, hidden_parts, head_parts, v_steps, r_steps;
   int hidden, hidden_left;  // the next tile of hidden states, how many
   int head[2], by[2], left[2];  // the next one of the head's, how far the one after is, how many, in the two rounds
-  __device__ __forceinline__ GradTasks(const TileArgs& a, int n, int pair) : columns(up_div(a.p.d, kTile)) {
+  __device__ __forceinline__ GradTasks(const TileArgs& a, int n, int pair) : columns(up_div(a.p.d, kTile)), pairs(a.pairs) {
     const GradSplit& s = a.p.split;
     const int ct = columns.by;
     row_tiles = up_div(n, kTile) * ct;
@@ -99,16 +101,16 @@ struct GradTasks {
     head_parts = s.head_parts;
     v_steps = up_div(a.p.V, kStepK);
     r_steps = up_div(n, kStepK);
-    const int all_hidden = hidden_parts * row_tiles, all_head = head_parts * head_tiles, last = all_hidden % kPairs;
+    const int all_hidden = hidden_parts * row_tiles, all_head = head_parts * head_tiles, last = all_hidden % pairs;
     hidden = pair;
-    hidden_left = all_hidden / kPairs + (pair < last);
+    hidden_left = all_hidden / pairs + (pair < last);
     // (an estimate in floats is as good, and the same for all)
     const float worth = __fdividef((float)(up_div(v_steps, max(1, hidden_parts)) + s.tile_cost),
                                    (float)(up_div(r_steps, max(1, head_parts)) + s.tile_cost));
-    const int idle = last ? kPairs - last : 0, first = idle ? min(all_head / idle, (int)worth) : 0;
+    const int idle = last ? pairs - last : 0, first = idle ? min(all_head / idle, (int)worth) : 0;
     head[0] = pair - last, by[0] = idle, left[0] = pair >= last ? first : 0;
-    head[1] = first * idle + pair, by[1] = kPairs;
-    left[1] = head[1] < all_head ? (all_head - head[1] + kPairs - 1) / kPairs : 0;
+    head[1] = first * idle + pair, by[1] = pairs;
+    left[1] = head[1] < all_head ? (all_head - head[1] + pairs - 1) / pairs : 0;
   }
   __device__ __forceinline__ void sum(Task& t, int job, int at, int tiles, int parts, int steps) const {
     int part = 0, c;
@@ -128,7 +130,7 @@ struct GradTasks {
   __device__ __forceinline__ bool next(Task& t) {
     if (hidden_left > 0) {
       sum(t, 0, hidden, row_tiles, hidden_parts, v_steps);
-      hidden += kPairs;
+      hidden += pairs;
       hidden_left--;
       return true;
     }
@@ -191,6 +193,14 @@ struct Turn {
       asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(chunk(lane, c)), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3])
                    : "memory");
     }
+  }
+  // 32 numbers of 32 bits of the lane's row
+  __device__ __forceinline__ void put_floats(const float (&v)[32]) const {
+#pragma unroll
+    for (int c = 0; c < 8; c++)
+      asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(chunk(lane, c)), "f"(v[4 * c]), "f"(v[4 * c + 1]),
+                   "f"(v[4 * c + 2]), "f"(v[4 * c + 3])
+                   : "memory");
   }
   // before the first put: to the other buffer, whose box has left
   __device__ __forceinline__ void next() {
@@ -354,8 +364,7 @@ __device__ __forceinline__ void logits_rows(const TileArgs& a, const HeadMaps& m
   if (real) p.rec[(long long)(col / kRecCols) * p.cap + row] = record(to, s);
 }
 
-template <typename T>
-__device__ __forceinline__ void store_part(float* part, const float (&v)[32]) {
+__device__ __forceinline__ void store_floats(float* part, const float (&v)[32]) {
 #pragma unroll
   for (int j = 0; j < 32; j += 4) ((float4*)part)[j / 4] = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
 }
@@ -375,7 +384,8 @@ __device__ __forceinline__ void grad_rows(const TileArgs& a, const HeadMaps& map
   if (there && out) to = hidden ? (uint16_t*)a.out.grad + begin : (uint16_t*)a.grad_head + row * a.grad_head_stride;
   const float scale = hidden ? coef : post;
   const bool whole = __all_sync(~0u, ((uintptr_t)to & 15) == 0);
-  float* part = hidden ? sp.hidden + ((long long)t.part * p.cap + row) * p.ldp : sp.head + ((long long)t.part * p.V + row) * p.ldp;
+  const CUtensorMap* part = hidden ? &maps.hidden_parts : &maps.head_parts;
+  const int part_row = t.part * (hidden ? p.cap : (int)sp.tokens) + row - turn.lane;
   float* acc = p.acc + (long long)row * p.ldp;
   auto pass = [&](float(&v)[32], int c) {
     if (t.steps <= 0) {
@@ -383,7 +393,10 @@ __device__ __forceinline__ void grad_rows(const TileArgs& a, const HeadMaps& map
       for (int j = 0; j < 32; j++) v[j] = 0.0f;
     }
     if (parts) {
-      if (there && c < p.d) store_part<T>(part + c, v);
+      if (c >= p.d) return;
+      turn.next();
+      turn.put_floats(v);
+      turn.store(part, c, part_row);
       return;
     }
     if (scale != 1.0f) {
@@ -395,7 +408,7 @@ __device__ __forceinline__ void grad_rows(const TileArgs& a, const HeadMaps& map
 #pragma unroll
         for (int j = 0; j < 32; j++) v[j] += acc[c + j];
       }
-      if (a.sum != kLast) store_part<T>(acc + c, v);
+      if (a.sum != kLast) store_floats(acc + c, v);
     }
   };
 #pragma unroll 1
@@ -450,7 +463,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     bar_init_visible();
   }
   if (threadIdx.x == 32)
-    for (const CUtensorMap* m : {&maps.hc, &maps.hs, &maps.head, &maps.e, &maps.e_out, &maps.grad_out}) prefetch_map(m);
+    for (const CUtensorMap* m : {&maps.hc, &maps.hs, &maps.head, &maps.e, &maps.e_out, &maps.grad_out, &maps.hidden_parts,
+                                 &maps.head_parts})
+      prefetch_map(m);
   if (kForm != 2 && a.pass.only_again) {  // mostly there is nothing to do
     follow();
     if (*a.p.again == 0) return;
@@ -585,7 +600,7 @@ __global__ void __launch_bounds__(256) k_head_parts(const __grid_constant__ Tile
   const GradSplit& sp = a.p.split;
   const bool hidden = blockIdx.y == 0 && sp.hidden_parts > 1;
   const int parts = hidden ? sp.hidden_parts : sp.head_parts, chunks = up_div(p.d, 4);
-  const long long rows = hidden ? *p.count : p.V, room = hidden ? p.cap : p.V;
+  const long long rows = hidden ? *p.count : p.V, room = hidden ? p.cap : sp.tokens;
   const float* from = hidden ? sp.hidden : sp.head;
   const bool again = *p.again != 0;
   const float post = again ? *p.post : 1.0f;
@@ -617,9 +632,13 @@ __global__ void __launch_bounds__(256) k_head_parts(const __grid_constant__ Tile
 
 // ---------------------------------------------------------------- host
 
+long long up_tiles(long long n) { return (n + kTile - 1) / kTile; }
+// No more than there are tiles
+int pairs_for(long long tiles) { return (int)std::min<long long>(kPairs, std::max(1ll, tiles)); }
+
 template <typename T, int kForm>
 epic_status launch_tiles(const HeadMaps& maps, const TileArgs& a, cudaStream_t st) {
-  return launch_next(k_head_tiles<T, kForm>, 2 * kPairs, kThreads, kShared, kShared, st, maps, a);
+  return launch_next(k_head_tiles<T, kForm>, 2 * a.pairs, kThreads, kShared, kShared, st, maps, a);
 }
 
 }  // namespace
@@ -629,6 +648,7 @@ GradSplit split_grads(int rows, int d, int V) {
   const long long ct = (d + kTile - 1) / kTile, mt = (rows + kTile - 1) / kTile, vt = (V + (long long)kTile - 1) / kTile;
   const long long kv = (V + (long long)kStepK - 1) / kStepK, kr = (rows + kStepK - 1) / kStepK;
   s.tile_cost = 4;
+  s.tokens = vt * kTile;
   const long long all = mt * ct * (kv + s.tile_cost) + vt * ct * (kr + s.tile_cost), unit = std::max(8ll, all / kPairs);
   s.hidden_parts = (int)std::min<long long>(kMostParts, (kv + unit - 1) / unit);
   s.head_parts = (int)std::min<long long>(kMostParts, (kr + unit - 1) / unit);
@@ -639,13 +659,17 @@ epic_status make_head_maps(HeadMaps& maps, const HeadPlan& p, int dtype, bool gr
   const bool bf16 = dtype == EPIC_BF16;
   if (!make_map(&maps.hc, bf16, p.hc, p.ldh, p.cap, p.ldh, 64) || !make_map(&maps.head, bf16, p.head, p.d, p.V, p.ldw, 64))
     return EPIC_ERR_CUDA;
-  maps.hs = maps.e = maps.e_out = maps.grad_out = maps.hc;
+  maps.hs = maps.e = maps.e_out = maps.grad_out = maps.hidden_parts = maps.head_parts = maps.hc;
   if (p.V == 1) stride = p.ldh;
   maps.boxes = grad_head && p.d % 8 == 0 && (uintptr_t)grad_head % 16 == 0 && stride % 8 == 0 && stride < 1ll << 38;
   if (!grads) return EPIC_OK;
   if (!make_map(&maps.e, bf16, p.e, p.lde, p.cap, p.lde, 64) || !make_map(&maps.e_out, bf16, p.e, p.lde, p.cap, p.lde, 32) ||
       (p.hs && !make_map(&maps.hs, bf16, p.hs, p.ldh, p.cap, p.ldh, 64)) ||
       (maps.boxes && !make_map(&maps.grad_out, bf16, grad_head, p.d, p.V, stride, 32)))
+    return EPIC_ERR_CUDA;
+  const GradSplit& s = p.split;
+  if ((s.hidden_parts > 1 && !make_float_map(&maps.hidden_parts, s.hidden, p.ldp, (long long)s.hidden_parts * p.cap, p.ldp)) ||
+      (s.head_parts > 1 && !make_float_map(&maps.head_parts, s.head, p.ldp, s.head_parts * s.tokens, p.ldp)))
     return EPIC_ERR_CUDA;
   return EPIC_OK;
 }
@@ -655,6 +679,7 @@ epic_status launch_head_logits(const HeadPlan& p, const HeadMaps& maps, int dtyp
   a.p = p;
   a.pass = pass;
   a.bf16 = dtype == EPIC_BF16;
+  a.pairs = pairs_for(up_tiles(p.rows) * up_tiles(p.V));
   if (pass.probs) return a.bf16 ? launch_tiles<__nv_bfloat16, 1>(maps, a, st) : launch_tiles<__half, 1>(maps, a, st);
   return a.bf16 ? launch_tiles<__nv_bfloat16, 0>(maps, a, st) : launch_tiles<__half, 0>(maps, a, st);
 }
@@ -670,6 +695,7 @@ epic_status launch_head_grads(const HeadPlan& p, const HeadMaps& maps, int dtype
   a.bf16 = dtype == EPIC_BF16;
   if (!out.grad) a.p.split.hidden_parts = 0;
   if (!grad_head) a.p.split.head_parts = 0;
+  a.pairs = pairs_for(up_tiles(p.d) * (a.p.split.hidden_parts * up_tiles(p.rows) + a.p.split.head_parts * up_tiles(p.V)));
   const epic_status s = a.bf16 ? launch_tiles<__nv_bfloat16, 2>(maps, a, st) : launch_tiles<__half, 2>(maps, a, st);
   if (s != EPIC_OK) return s;
   const bool hidden = a.p.split.hidden_parts > 1, head = a.p.split.head_parts > 1;

@@ -414,7 +414,7 @@ size_t plan_head(const HeadCall& c, void* base, HeadPlan& p) {
     if (rows > p.cap) w.take(p.acc, (size_t)c.V * p.ldp, 4);
     p.split = split_grads((int)std::min<long long>(rows, p.cap), c.d, c.V);
     if (p.split.hidden_parts > 1) w.take(p.split.hidden, p.split.hidden_parts * cap * p.ldp, 4);
-    if (p.split.head_parts > 1) w.take(p.split.head, (size_t)p.split.head_parts * c.V * p.ldp, 4);
+    if (p.split.head_parts > 1) w.take(p.split.head, (size_t)p.split.head_parts * p.split.tokens * p.ldp, 4);
   }
   if (head_lies_askew(c, p)) {
     void* packed;

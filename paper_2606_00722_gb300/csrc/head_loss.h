@@ -18,7 +18,8 @@ constexpr int kMostParts = 64;  // of a gradient's sum
 struct GradSplit {
   int hidden_parts, head_parts;
   int tile_cost;        // what a tile costs beside its sum, in steps of it
-  float *hidden, *head; // [parts][cap][ldp], [parts][V][ldp]
+  float *hidden, *head; // [parts][cap][ldp], [parts][tokens][ldp]
+  long long tokens;     // V in whole tiles
 };
 
 // A piece: up to `cap` positions of the call.  Those that count stand in order, packed, in rows 0..*count-1 of the
@@ -71,7 +72,7 @@ struct LogitsPass {
 // How boxes of the operands are copied, the same for all of a call's kernels and pieces: 64 columns by 64 rows, those that go
 // out by 32 rows
 struct HeadMaps {
-  CUtensorMap hc, hs, head, e, e_out, grad_out;
+  CUtensorMap hc, hs, head, e, e_out, grad_out, hidden_parts, head_parts;
   bool boxes;  // rows of grad_out start at multiples of 16 bytes and end there (a box's end is cut in whole 16 bytes)
 };
 // grads: they are wanted; grad_head: or NULL

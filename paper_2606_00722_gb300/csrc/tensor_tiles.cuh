@@ -233,6 +233,16 @@ inline bool make_byte_map(CUtensorMap* map, const void* base, long long cols, lo
                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// [rows][cols] of 32-bit floats, `ld` apart: boxes of 32 columns and 32 rows
+inline bool make_float_map(CUtensorMap* map, const void* base, long long cols, long long rows, long long ld) {
+  const cuuint64_t size[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, stride[1] = {(cuuint64_t)ld * 4};
+  const cuuint32_t part[2] = {32, 32}, step[2] = {1, 1};
+  return encode_tiled() &&
+         encode_tiled()(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, (void*)base, size, stride, part, step,
+                        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // [rows][cols] of 16-bit elements, `ld` apart: boxes of 64 columns and `box` rows
 inline bool make_map(CUtensorMap* map, bool bf16, const void* base, long long cols, long long rows, long long ld, int box) {
   const cuuint64_t size[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, stride[1] = {(cuuint64_t)ld * 2};
