@@ -308,7 +308,8 @@ __global__ void __launch_bounds__(kMeetWarps * 32) k_head_meet(MeetArgs a) {
 }
 
 // The head at rows of a multiple of 16 bytes, a warp a row.  8 elements come from the two aligned chunks of 16 bytes that they
-// lie in; the first and the last chunk of a row may hold bytes next to it, within the same 16.
+// lie in, the lane's own and the next lane's; the first and the last chunk of a row may hold bytes next to it, within the
+// same 16.
 template <typename T>
 __global__ void __launch_bounds__(256) k_head_pack(const T* head, long long stride, T* to, long long ld, int d, int V) {
   follow();
@@ -318,10 +319,15 @@ __global__ void __launch_bounds__(256) k_head_pack(const T* head, long long stri
     const uintptr_t w = (uintptr_t)(head + v * stride), end = w + d * sizeof(T);
     const uint32_t m = w % 16;
 #pragma unroll 4
-    for (int k = lane * 8; k < ld; k += 256) {
+    for (int k0 = 0; k0 < ld; k0 += 256) {
+      const int k = k0 + lane * 8;
       const uintptr_t from = w - m + k * sizeof(T);
-      const uint4 none = make_uint4(0, 0, 0, 0);
-      const uint4 x = shifted(*(const uint4*)from, m && from + 16 < end ? *(const uint4*)(from + 16) : none, m);
+      const uint4 none = make_uint4(0, 0, 0, 0), own = from < end ? *(const uint4*)from : none;
+      uint4 next = make_uint4(__shfl_down_sync(~0u, own.x, 1), __shfl_down_sync(~0u, own.y, 1), __shfl_down_sync(~0u, own.z, 1),
+                              __shfl_down_sync(~0u, own.w, 1));
+      if (lane == 31) next = from + 16 < end ? *(const uint4*)(from + 16) : none;
+      if (k >= ld) continue;
+      const uint4 x = shifted(own, next, m);
       const uint32_t y[4] = {x.x, x.y, x.z, x.w};
       uint4 out;
       uint32_t* o = (uint32_t*)&out;
@@ -454,7 +460,7 @@ epic_status run_head(const HeadCall& c, const HeadTensors& t, HeadPlan p, cudaSt
     if (rows == 0) return EPIC_OK;
   }
   if (c.V > 0 && p.head != c.head) {
-    EPIC_TRY(launch_next(k_head_pack<T>, (unsigned)std::min(2432, (c.V + 7) / 8), 256, 0, kNoCache, st, (const T*)c.head,
+    EPIC_TRY(launch_next(k_head_pack<T>, (unsigned)(c.V + 7) / 8, 256, 0, kNoCache, st, (const T*)c.head,
                          c.head_stride, (T*)p.head, p.ldw, c.d, c.V));
   }
   HeadMaps maps;
