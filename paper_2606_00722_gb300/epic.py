@@ -383,19 +383,22 @@ def extract_witness(g: Grammar, t: LexTable, x, terms, lengths, stream=None):
 _DTYPES = {}  # torch dtype of logits -> the C-ABI's code; filled on the first call
 _T = None     # torch, and what the calls need of it
 _INT8 = None
-_empty = None  # torch.empty
+_alloc = _free = None  # (bytes, stream) -> address in torch's memory, and back
 _raw_stream = None
 _current_device = None
 
 
 def _logits_init():
-    global _T, _INT8, _empty, _raw_stream, _current_device
+    global _T, _INT8, _alloc, _free, _raw_stream, _current_device
     import torch
     _DTYPES.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2})
     _raw_stream = getattr(torch._C, '_cuda_getCurrentRawStream', None) or (
         lambda device: torch.cuda.current_stream(device).cuda_stream)
     _current_device = getattr(torch._C, '_cuda_getDevice', None) or torch.cuda.current_device
-    _INT8, _empty = torch.int8, torch.empty
+    _INT8 = torch.int8
+    _alloc = getattr(torch._C, '_cuda_cudaCachingAllocator_raw_alloc', None) or (
+        lambda size, stream: torch.cuda.caching_allocator_alloc(size, None, stream))
+    _free = getattr(torch._C, '_cuda_cudaCachingAllocator_raw_delete', None) or torch.cuda.caching_allocator_delete
     _T = (torch.float32, torch.int32, torch.uint8)
 
 
@@ -585,8 +588,8 @@ def decode_step_from_logits(g: Grammar, t: LexTable, x, pos, logits, n_target, b
 
 
 # ---------------------------------------------------------------- the head
-# Hidden states [B][n][d] are rows like logits; a workspace of each call's own comes from torch's allocator, on the
-# call's stream, unless the caller brings one.
+# Hidden states [B][n][d] are rows like logits; a workspace of each call's own comes from torch's memory, on the call's
+# stream, unless the caller brings one.  (As bytes: a tensor's making takes 7 us between two calls of the library.)
 
 _HEAD_FORWARD, _HEAD_BACKWARD, _HEAD_STEP = range(3)
 
@@ -610,38 +613,38 @@ def _weights(t, d, dtype, name, device):
     return t.data_ptr(), V, t.stride(0) if V > 1 else d
 
 
-def _scratch(query, args, workspace, device, stream):
-    """(tensor, address, bytes) of the workspace that the library asks for; a caller's own has to be that large."""
+def _need(query, *args):
+    """Bytes of the workspace that the library asks for."""
     need = C.c_size_t()
     status = query(*args, C.byref(need))
     if status:
         _check(status, query.__name__)
+    return need.value
+
+
+def _with_workspace(call, name, args, workspace, need, device, stream):
+    """The call with a workspace and a stream behind its arguments."""
     if workspace is None:
-        need = need.value
-        if stream is None:
-            workspace = _empty(need, dtype=_T[2], device=device)
-        else:
-            import torch
-            on = torch.cuda.ExternalStream(stream, device=device) if isinstance(stream, int) else stream
-            with torch.cuda.stream(on):
-                workspace = _empty(need, dtype=_T[2], device=device)
-        return workspace, workspace.data_ptr(), need
-    elif workspace.get_device() != device or not workspace.is_contiguous():
-        raise ValueError('workspace: expected a contiguous tensor on CUDA device %d' % device)
-    return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
+        address = _alloc(need, stream)
+        try:
+            status = call(*args, address, need, stream)
+        finally:
+            _free(address)  # back to the stream's own: what follows on it comes after the call
+    else:
+        if workspace.get_device() != device or not workspace.is_contiguous():
+            raise ValueError('workspace: expected a contiguous tensor on CUDA device %d' % device)
+        status = call(*args, workspace.data_ptr(), workspace.numel() * workspace.element_size(), stream)
+    if status:
+        _check(status, name)
 
 
-def _head_args(form, hidden, head, workspace, stream):
-    """The arguments that the forms of the loss share: (rows, device, head, scratch); the scratch tensor has to live until
-    the call returns."""
+def _head_args(form, hidden, head):
+    """What the forms of the loss share: (rows, device, head, bytes of the workspace)."""
     rows = _hidden(hidden)
     device = _device(hidden)
     weights = _weights(head, rows[4], hidden.dtype, 'head', device)
-    lib = _lib or load()
-    scratch = _scratch(lib.epic_head_loss_workspace,
-                       (form, rows[1], rows[2], rows[3], rows[4], weights[1], weights[0], weights[2]), workspace, device,
-                       stream)
-    return rows, device, weights, scratch
+    return rows, device, weights, _need((_lib or load()).epic_head_loss_workspace, form, rows[1], rows[2], rows[3], rows[4],
+                                        weights[1], weights[0], weights[2])
 
 
 def _head_gradient(head, grad, device):
@@ -660,51 +663,46 @@ def _hidden_gradient(hidden, grad):
 def head_loss_workspace(form, hidden, head):
     """Bytes that a call of that form ('forward', 'backward' or 'step') needs as its workspace, a uint8 tensor that a
     program may keep and pass to calls that do not overlap."""
-    rows = _hidden(hidden)
-    address, V, stride = _weights(head, rows[4], hidden.dtype, 'head', _device(hidden))
-    need = C.c_size_t()
-    _check((_lib or load()).epic_head_loss_workspace(('forward', 'backward', 'step').index(form), rows[1], rows[2],
-                                                     rows[3], rows[4], V, address, stride, C.byref(need)),
-           'epic_head_loss_workspace')
-    return need.value
+    return _head_args(('forward', 'backward', 'step').index(form), hidden, head)[3]
 
 
 def head_loss_forward(hidden, head, target, loss, lse, weight=None, stream=None, workspace=None):
     """epic_head_loss_forward: cross entropy loss and lse [B][n] float32 of hidden states [B][n][d] through head weights
     [V][d] against target [B][n] int32 (an id outside 0..V-1: the position does not count); weight [B][n] float32."""
-    rows, device, weights, scratch = _head_args(_HEAD_FORWARD, hidden, head, workspace, stream)
+    rows, device, weights, need = _head_args(_HEAD_FORWARD, hidden, head)
     f32, i32, _ = _T
     shape = rows[2:4]
-    _check(_lib.epic_head_loss_forward(
-        *rows, *weights, _arg(target, shape, i32, 'target', device), _arg(weight, shape, f32, 'weight', device),
-        _arg(loss, shape, f32, 'loss', device), _arg(lse, shape, f32, 'lse', device), *scratch[1:],
-        _on(device, stream)), 'epic_head_loss_forward')
+    _with_workspace(_lib.epic_head_loss_forward, 'epic_head_loss_forward',
+                    (*rows, *weights, _arg(target, shape, i32, 'target', device), _arg(weight, shape, f32, 'weight', device),
+                     _arg(loss, shape, f32, 'loss', device), _arg(lse, shape, f32, 'lse', device)),
+                    workspace, need, device, _on(device, stream))
 
 
 def head_loss_backward(hidden, head, target, lse, grad_loss, grad_hidden, grad_head, weight=None, stream=None,
                        workspace=None):
     """epic_head_loss_backward: grad_hidden [B][n][d] and grad_head [V][d] (either may be None) from the forward call's
     lse and the gradient grad_loss [B][n] of its loss."""
-    rows, device, weights, scratch = _head_args(_HEAD_BACKWARD, hidden, head, workspace, stream)
+    rows, device, weights, need = _head_args(_HEAD_BACKWARD, hidden, head)
     f32, i32, _ = _T
     shape = rows[2:4]
-    _check(_lib.epic_head_loss_backward(
-        *rows, *weights, _arg(target, shape, i32, 'target', device), _arg(weight, shape, f32, 'weight', device),
-        _arg(lse, shape, f32, 'lse', device), _arg(grad_loss, shape, f32, 'grad_loss', device),
-        *_hidden_gradient(hidden, grad_hidden), *_head_gradient(head, grad_head, device), *scratch[1:],
-        _on(device, stream)), 'epic_head_loss_backward')
+    _with_workspace(_lib.epic_head_loss_backward, 'epic_head_loss_backward',
+                    (*rows, *weights, _arg(target, shape, i32, 'target', device), _arg(weight, shape, f32, 'weight', device),
+                     _arg(lse, shape, f32, 'lse', device), _arg(grad_loss, shape, f32, 'grad_loss', device),
+                     *_hidden_gradient(hidden, grad_hidden), *_head_gradient(head, grad_head, device)),
+                    workspace, need, device, _on(device, stream))
 
 
 def head_loss_step(hidden, head, target, loss, grad_hidden, grad_head, weight=None, stream=None, workspace=None):
     """epic_head_loss_step: loss [B][n] and its gradients [B][n][d] and [V][d] in one call, for a training loop whose row
     weights are known before the loss."""
-    rows, device, weights, scratch = _head_args(_HEAD_STEP, hidden, head, workspace, stream)
+    rows, device, weights, need = _head_args(_HEAD_STEP, hidden, head)
     f32, i32, _ = _T
     shape = rows[2:4]
-    _check(_lib.epic_head_loss_step(
-        *rows, *weights, _arg(target, shape, i32, 'target', device), _arg(weight, shape, f32, 'weight', device),
-        _arg(loss, shape, f32, 'loss', device), *_hidden_gradient(hidden, grad_hidden),
-        *_head_gradient(head, grad_head, device), *scratch[1:], _on(device, stream)), 'epic_head_loss_step')
+    _with_workspace(_lib.epic_head_loss_step, 'epic_head_loss_step',
+                    (*rows, *weights, _arg(target, shape, i32, 'target', device), _arg(weight, shape, f32, 'weight', device),
+                     _arg(loss, shape, f32, 'loss', device), *_hidden_gradient(hidden, grad_hidden),
+                     *_head_gradient(head, grad_head, device)),
+                    workspace, need, device, _on(device, stream))
 
 
 _HeadLoss = None  # head_loss's torch operation; made on the first call
@@ -772,12 +770,12 @@ def int8_logits(q, scale, head_q, head_scale, logits, stream=None, workspace=Non
     if tokens != V:
         raise ValueError('logits: expected [%d][%d][%d]' % (B, k, tokens))
     lib = _lib or load()
-    scratch = _scratch(lib.epic_int8_logits_workspace, (B, k, d, V, address, stride), workspace, device, stream)
     f32 = _T[0]
-    _check(lib.epic_int8_logits(
-        _arg(q, (B, k, d), _INT8, 'q', device), _arg(scale, (B, k), f32, 'scale', device), B, k, d, address,
-        _arg(head_scale, (V,), f32, 'head_scale', device), V, stride, out[0], out[1], out[5], out[6], *scratch[1:],
-        _on(device, stream)), 'epic_int8_logits')
+    _with_workspace(lib.epic_int8_logits, 'epic_int8_logits',
+                    (_arg(q, (B, k, d), _INT8, 'q', device), _arg(scale, (B, k), f32, 'scale', device), B, k, d, address,
+                     _arg(head_scale, (V,), f32, 'head_scale', device), V, stride, out[0], out[1], out[5], out[6]),
+                    workspace, _need(lib.epic_int8_logits_workspace, B, k, d, V, address, stride), device,
+                    _on(device, stream))
 
 
 def decode_step_from_hidden(g: Grammar, t: LexTable, x, pos, hidden, head_q, head_scale, n_target, bufs,
