@@ -175,3 +175,60 @@ def test_streams_and_graphs(cuda):
     x.copy_(keep)
     graph.replay()
     assert torch.equal(z, want)
+
+
+@pytest.mark.parametrize('size,d', [(64, 2048), (65, 2048), (32, 4096), (33, 4096), (127, 1024), (16, 8200), (3, 40000)])
+def test_sums_at_the_border_of_what_is_exact(cuda, size, d):
+    """Rows of one size against weights of -128 and 127: 128 times 2,048 times 64 is 2^24 to the bit.  Odd weights in between
+    show a sum that lost its last bit."""
+    import torch
+    import paper_2606_00722_gb300 as epic
+    rows, V = 40, 300
+    g = torch.Generator().manual_seed(size)
+    q = torch.full((1, rows, d), size, dtype=torch.int8)
+    q[:, 1::3] *= -1
+    q[:, 2::3] = torch.randint(-size, size + 1, (rows // 3, d), generator=g).to(torch.int8)
+    w = torch.randint(-128, 128, (V, d), generator=g).to(torch.int8)
+    w[::3] = -128
+    w[1::3] = 127
+    q, w = q.cuda(), w.cuda()
+    z = torch.empty((1, rows, V), device=cuda)
+    epic.int8_logits(q, torch.ones((1, rows), device=cuda), w, torch.ones(V, device=cuda), z)
+    assert torch.equal(z, (q.double() @ w.double().t()).float())
+
+
+def test_logits_do_not_depend_on_the_other_rows(cuda):
+    """A row's logits have the same bits alone, among few rows and among many: whatever way they are made, sums are exact."""
+    import torch
+    import paper_2606_00722_gb300 as epic
+    q, head, s, S = int8_case(1, 300, 1536, 700, 9)
+    z = torch.empty((1, 300, 700), dtype=torch.bfloat16, device=cuda)
+    epic.int8_logits(q, s, head, S, z)
+    for n in (1, 2, 3, 7, 8, 9, 33, 100):
+        part = torch.empty((1, n, 700), dtype=torch.bfloat16, device=cuda)
+        epic.int8_logits(q[:, :n].contiguous(), s[:, :n].contiguous(), head, S, part)
+        assert torch.equal(part, z[:, :n])
+
+
+def test_far_apart_and_past_32_bits(cuda):
+    """Rows of logits 2^31 elements apart; a head of 2.3e9 bytes, seen at its last tokens; workspaces of other contents."""
+    import torch
+    import paper_2606_00722_gb300 as epic
+    q, head, s, S = int8_case(2, 6, 256, 500, 3)
+    far = (1 << 31) + 64
+    store = torch.zeros(far + 6 * 500, dtype=torch.bfloat16, device=cuda)
+    z = store.as_strided((2, 6, 500), (far, 500, 1))
+    epic.int8_logits(q, s, head, S, z)
+    check_logits(z, q, head, s, S, 'bf16')
+    del store, z
+    d, V = 32768, 70000
+    big = torch.zeros((V, d), dtype=torch.int8, device=cuda)
+    big[-2:] = torch.randint(-128, 128, (2, d), generator=torch.Generator().manual_seed(1)).to(torch.int8).cuda()
+    S = torch.ones(V, device=cuda)
+    for rows in (1, 20):
+        q = torch.randint(-128, 128, (1, rows, d), generator=torch.Generator().manual_seed(2)).to(torch.int8).cuda()
+        z = torch.empty((1, rows, V), device=cuda)
+        for fill in (0, 255):
+            work = torch.full((rows * (d * 2 + 4 * 32) + 4096,), fill, dtype=torch.uint8, device=cuda)
+            epic.int8_logits(q, torch.ones((1, rows), device=cuda), big, S, z, workspace=work)
+            assert torch.equal(z[..., -2:], (q.double() @ big[-2:].double().t()).float()) and (z[..., :-2] == 0).all()

@@ -122,6 +122,10 @@ SIZES = [  # B, n, d, V, dtype, pad, shift
     (1, 3, 4096, 9001, 'bf16', 0, 0),
     (2, 5, 1003, 50021, 'bf16', 8, 0),
     (1, 900, 65, 130, 'f16', 0, 0),
+    (1, 1500, 40, 300, 'bf16', 0, 0),    # more positions than one scan counts
+    (2, 2100, 72, 513, 'f16', 1, 3),
+    (1, 200, 320, 3000, 'bf16', 3, 2),   # rows of the head and of gradients at odd places, sums in parts
+    (1, 5000, 64, 260, 'bf16', 0, 0),
 ]
 
 
@@ -166,7 +170,7 @@ def test_pieces_add_up(cuda, monkeypatch, rows, dtype):
     import torch
     import paper_2606_00722_gb300 as epic
     monkeypatch.setenv('EPIC_HEAD_PIECE_MB', '1')
-    d, V = 96, 2051
+    d, V = 96 if rows != 520 else 97, 2051
     h, W, target, weight, up = make(1, rows, d, V, dtype, rows)
     target[:, 256:512] = -1 if rows > 512 else target[:, 256:512]
     want, step = head64(h, W, target, weight, up), head64(h, W, target, weight)
@@ -394,3 +398,92 @@ def test_as_a_torch_operation(cuda):
     target.add_(1)
     with pytest.raises(RuntimeError):
         loss.sum().backward()
+
+
+@pytest.mark.parametrize('dtype', ['bf16', 'f16'])
+@pytest.mark.parametrize('R,d,V', [(40, 64, 300), (300, 97, 2100)])
+def test_what_a_workspace_holds_does_not_matter(cuda, dtype, R, d, V):
+    """All forms with workspaces of NaNs, infinities and numbers give the same bits; a workspace of the size that is asked
+    for is enough, and nothing behind it is written."""
+    import torch
+    import paper_2606_00722_gb300 as epic
+    h, W, target, weight, up = make(1, R, d, V, dtype, R + d)
+    results = []
+    for fill in (0, 0x7f, 0xff, 0x80):
+        loss, lse = torch.empty((1, R), device=cuda), torch.empty((1, R), device=cuda)
+        outs = [loss, lse]
+        for form in ('forward', 'backward', 'step'):
+            need = epic.head_loss_workspace(form, h, W)
+            store = torch.full((need + 512,), fill, dtype=torch.uint8, device=cuda)
+            store[need:] = 77
+            work = store[:need]
+            gh, gw = torch.empty_like(h), torch.empty((V, d), dtype=h.dtype, device=cuda)
+            if form == 'forward':
+                epic.head_loss_forward(h, W, target, loss, lse, weight=weight, workspace=work)
+            elif form == 'backward':
+                epic.head_loss_backward(h, W, target, lse, up, gh, gw, weight=weight, workspace=work)
+                outs += [gh, gw]
+            else:
+                again = torch.empty_like(loss)
+                epic.head_loss_step(h, W, target, again, gh, gw, weight=weight, workspace=work)
+                outs += [again, gh, gw]
+            assert (store[need:] == 77).all()
+        results.append(outs)
+    for outs in results[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(results[0], outs))
+
+
+def test_positions_far_apart(cuda):
+    """Sequences 2^31 elements apart, in hidden states and in their gradient."""
+    import torch
+    import paper_2606_00722_gb300 as epic
+    n, d, V, far = 3, 24, 90, (1 << 31) + 16
+    h, W, target, weight, up = make(2, n, d, V, 'bf16', 5, edges=False)
+    big, grad = [torch.zeros(far + n * d, dtype=h.dtype, device=cuda) for _ in range(2)]
+    x, gh = [t.as_strided((2, n, d), (far, d, 1)) for t in (big, grad)]
+    x.copy_(h)
+    loss, gw = torch.empty((2, n), device=cuda), torch.empty_like(W)
+    epic.head_loss_step(x, W, target, loss, gh, gw, weight=weight)
+    step = head64(h, W, target, weight)
+    close(loss, step['loss'], step['loss_tol'])
+    check_grads(gh, gw, step, 'bf16')
+    assert int((grad != 0).sum()) <= 2 * n * d
+
+
+def test_a_head_past_32_bits(cuda):
+    """2.3e9 weights, all 0 but those of the last token: lse = log(V - 1 + exp z), and gradients by hand."""
+    import torch
+    import paper_2606_00722_gb300 as epic
+    V, d = 70000, 32768
+    W = torch.zeros((V, d), dtype=torch.bfloat16, device=cuda)
+    W[-1, ::2] = 2.0 ** -10
+    h = torch.ones((1, 2, d), dtype=torch.bfloat16, device=cuda) * 0.5  # z of the last token: 16384 / 1024 / 2 = 8
+    target = torch.tensor([[V - 1, 7]], dtype=torch.int32, device=cuda)
+    loss, lse = torch.empty((1, 2), device=cuda), torch.empty((1, 2), device=cuda)
+    want = math.log(V - 1 + math.exp(8.0))
+    epic.head_loss_forward(h, W, target, loss, lse)
+    assert ((lse - want).abs() < 1e-4).all() and abs(float(loss[0, 0]) - (want - 8.0)) < 1e-4
+    assert abs(float(loss[0, 1]) - want) < 1e-4
+    gh, gw = torch.empty_like(h), torch.empty_like(W)
+    epic.head_loss_step(h, W, target, loss, gh, gw)
+    p, rest = math.exp(8.0 - want), math.exp(-want)
+    u = 2.0 ** -8  # three roundings of terms that do not cancel but at the two targets, there of sums of 2
+    assert ((gw[-1].double() - 0.5 * (2 * p - 1)).abs() < 3.1 * u * 0.5 * (1 + 2 * p)).all()
+    assert ((gw[7].double() - 0.5 * (2 * rest - 1)).abs() < 3.1 * u * 0.5 * (1 + 2 * rest)).all()
+    assert ((gw[1000].double() - rest).abs() < 3.1 * u * rest).all()
+    assert ((gh[0, 1, ::2].double() - p * 2.0 ** -10).abs() < 2.1 * u * p * 2.0 ** -10).all() and (gh[0, 1, 1::2] == 0).all()
+    assert ((gh[0, 0, ::2].double() - (p - 1) * 2.0 ** -10).abs() < 2.1 * u * 2.0 ** -10).all()
+
+
+def test_gradients_of_broadcast_hidden_states(cuda):
+    """One sequence's hidden states for all: torch adds up what each position's gradient is."""
+    import torch
+    import paper_2606_00722_gb300 as epic
+    B, n, d, V = 3, 10, 32, 100
+    h, W, target, weight, up = make(B, n, d, V, 'bf16', 2, edges=False)
+    one = h[:1].clone().requires_grad_()
+    (epic.head_loss(one.expand(B, n, d), W, target, weight) * up).sum().backward()
+    r = head64(h[:1].expand(B, n, d), W, target, weight, up)
+    u = 2.0 ** -8
+    tol = ((u + 2.0 ** -12) * r['a'] + r['ae'] + u * r['gh'].abs()).sum(0) + 3 * u * r['gh'].abs().sum(0)
+    assert one.grad.shape == (1, n, d) and ((one.grad[0].double() - r['gh'].sum(0)).abs() <= tol).all()
