@@ -161,8 +161,8 @@ __device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float a, float b) {
 
 // A warp's sums on their way out: 64 elements of its 32 rows, a lane a row, turned in shared memory so that they leave by
 // whole runs of a row (1 GB of a gradient leaves at 4.9 TB/s by 32 bytes of every lane's own row, at 6.6 by runs).  Rows
-// of 128 bytes, chunks of 16 swizzled by the row's number in 8: as boxes are, and without conflicts either way.  Two buffers
-// in turn, so that a box leaves while the next one is made.
+// of 128 bytes, chunks of 16 swizzled by the row's number in 8: as boxes are, and without conflicts either way.  Two buffers,
+// so that one fence (some 500 clocks) is for two boxes.
 struct Turn {
   uint32_t at, other;
   int lane;
@@ -202,18 +202,25 @@ struct Turn {
                    "f"(v[4 * c + 2]), "f"(v[4 * c + 3])
                    : "memory");
   }
-  // before the first put: to the other buffer, whose box has left
+  // to the other buffer
   __device__ __forceinline__ void next() {
     const uint32_t now = other;
     other = at;
     at = now;
-    if (lane == 0) boxes_read<1>();
+  }
+  // before the first put: the boxes before have left
+  __device__ __forceinline__ void free() const {
+    if (lane == 0) boxes_read<0>();
     __syncwarp();
   }
-  __device__ __forceinline__ void store(const CUtensorMap* map, int x, int y) const {
+  // the other buffer's box and, if x2 >= 0, this one's at x2
+  __device__ __forceinline__ void store(const CUtensorMap* map, int x, int x2, int y) const {
     shared_to_boxes();
     __syncwarp();
-    if (lane == 0) store_box(map, at, x, y);
+    if (lane == 0) {
+      store_box(map, other, x, y);
+      if (x2 >= 0) store_box(map, at, x2, y);
+    }
   }
   // to each lane's row `to` (NULL from row `rows` on), which starts at a multiple of 16 bytes, 64 elements: 8 lanes a row
   __device__ __forceinline__ void store_whole(uint16_t* to) const {
@@ -331,15 +338,19 @@ __device__ __forceinline__ void logits_rows(const TileArgs& a, const HeadMaps& m
 #pragma unroll
         for (int j = 0; j < 32; j++) z[j] = 0.0f;
       }
+      if (c == 0) turn.free();
       if (c % 64 == 0) turn.next();
       turn.put<T>(z, c / 32 % 2);
-      if (c % 64) turn.store(&maps.e_out, col + c - 32, row - turn.lane);
     } else {
       const float top = whole_ref(max32(z));
 #pragma unroll
       for (int j = 0; j < 32; j++) z[j] = ex2(fmaf(z[j], kLog2E, -top));
       meet(to, s, top, sum32(z));
     }
+  }
+  if (kProbs && col < p.lde) {
+    if (col + 64 >= p.lde) turn.next();  // one box only
+    turn.store(&maps.e_out, col, col + 64 < p.lde ? col + 64 : -1, row - turn.lane);
   }
   if (!a.pass.sums || col >= p.V) return;
   // exponentials past the window: once more, relative to the largest
@@ -387,18 +398,18 @@ __device__ __forceinline__ void grad_rows(const TileArgs& a, const HeadMaps& map
   const CUtensorMap* part = hidden ? &maps.hidden_parts : &maps.head_parts;
   const int part_row = t.part * (hidden ? p.cap : (int)sp.tokens) + row - turn.lane;
   float* acc = p.acc + (long long)row * p.ldp;
-  auto pass = [&](float(&v)[32], int c) {
-    if (t.steps <= 0) {
+  auto load = [&](float(&v)[32], float(&w)[32], int c) {
+    if (t.steps > 0) {
+      sums_load(sums + (c - col), v);
+      sums_load(sums + (c - col) + 32, w);
+      sums_loaded(v);
+      sums_loaded(w);
+    } else {
 #pragma unroll
-      for (int j = 0; j < 32; j++) v[j] = 0.0f;
+      for (int j = 0; j < 32; j++) v[j] = w[j] = 0.0f;
     }
-    if (parts) {
-      if (c >= p.d) return;
-      turn.next();
-      turn.put_floats(v);
-      turn.store(part, c, part_row);
-      return;
-    }
+  };
+  auto pass = [&](float(&v)[32], int c) {
     if (scale != 1.0f) {
 #pragma unroll
       for (int j = 0; j < 32; j++) v[j] *= scale;
@@ -414,27 +425,34 @@ __device__ __forceinline__ void grad_rows(const TileArgs& a, const HeadMaps& map
 #pragma unroll 1
   for (int c = col; c < col + kHalf && c < p.d; c += 64) {
     float v[32], w[32];
-    if (t.steps > 0) {
-      sums_load(sums + (c - col), v);
-      sums_load(sums + (c - col) + 32, w);
-      sums_loaded(v);
-      sums_loaded(w);
+    load(v, w, c);
+    if (c == col || parts) turn.free();
+    if (parts) {
+      turn.next();
+      turn.put_floats(v);
+      turn.next();
+      turn.put_floats(w);
+      turn.store(part, c, c + 32 < p.d ? c + 32 : -1, part_row);
+      continue;
     }
-    if (out) turn.next();
     pass(v, c);
     pass(w, c + 32);
     if (!out) continue;
-    const bool runs = !box && !(whole && p.d - c >= 64);
     uint16_t* here = to ? to + c : nullptr;
-    if (runs) {
+    if (!box && !(whole && p.d - c >= 64)) {
+      turn.next();
       turn.put<T>(v, w, (uintptr_t)here & 2);
       turn.store_runs(here, end - (row - turn.lane), min(p.d - c, 64), pack2<T>(v[0], v[0]) & 0xffff);
-    } else {
-      turn.put<T>(v, 0);
-      turn.put<T>(w, 1);
-      if (box) turn.store(&maps.grad_out, c, row - turn.lane);
-      else turn.store_whole(here);
+      continue;
     }
+    turn.next();
+    turn.put<T>(v, 0);
+    turn.put<T>(w, 1);
+    if (!box) turn.store_whole(here);
+  }
+  if (box && col < p.d) {
+    if (col + 64 >= p.d) turn.next();  // one box only
+    turn.store(&maps.grad_out, col, col + 64 < p.d ? col + 64 : -1, row - turn.lane);
   }
 }
 
