@@ -418,7 +418,8 @@ epic_status epic_distill_step(const void* d_logits, int32_t dtype, int32_t B, in
  * states [B][n][d] (element c of position i of sequence b at b * stride_b + i *
  * stride_n + c, strides >= 0 in elements, rows may start at any multiple of the
  * element size) and the weights [V][d] of the output layer, a row of which is at
- * v * head_stride.  They allocate nothing, are asynchronous on `cuda_stream`, may be
+ * v * head_stride.  (Rows that start at no multiple of 16 bytes may be read from the 16
+ * bytes that they begin in to those that they end in.)  They allocate nothing, are asynchronous on `cuda_stream`, may be
  * captured in a CUDA graph, and may overlap on different streams with workspaces of
  * their own.  A workspace is device memory of the caller's, aligned to 256 bytes, of at
  * least the size that the call's *_workspace function gives for the same sizes and
@@ -450,7 +451,9 @@ enum { EPIC_HEAD_FORWARD = 0, EPIC_HEAD_BACKWARD = 1, EPIC_HEAD_STEP = 2 };
  * the logits once (bf16).
  * In both, gradients of logits are rounded to dtype (off by at most 2^-8 of a value in
  * bf16, 2^-11 in fp16) before they are multiplied and summed; so are, in a step in bf16,
- * hidden states times a row's factor.
+ * hidden states times a row's factor.  In fp16 they are held relative to the largest
+ * |w grad_loss| of 16,384 positions: what is below 2^-28 of it loses bits, below 2^-39 all.
+ * Sums of the products are the tensor units', which cut what they add to 32 bits.
  * A target of probability 0 gives loss +inf and a finite gradient.  NaN or +inf
  * logits give NaN, in the gradient of the head at all tokens.  What is in the rows of
  * positions that do not count does not matter.

@@ -3,9 +3,9 @@
 #pragma once
 #include <cuda_runtime.h>
 
-#include <mutex>
-#include <set>
-#include <utility>
+#include <stdint.h>
+
+#include <atomic>
 
 #include "../../include/epic.h"
 
@@ -22,17 +22,22 @@ __device__ __forceinline__ void let_next() { asm volatile("griddepcontrol.launch
 // between them ask for the same.
 constexpr int kNoCache = 0, kCache = -1;
 inline bool prepare_kernel(const void* kernel, int shared) {
-  static std::mutex lock;
-  static std::set<std::pair<const void*, int>> done;
+  static std::atomic<uintptr_t> done[256];  // kernel and device, by a hash; a place is taken once and kept
   int device;
   if (cudaGetDevice(&device) != cudaSuccess) return false;
-  std::lock_guard<std::mutex> hold(lock);
-  if (done.count({kernel, device})) return true;
+  const uintptr_t key = (uintptr_t)kernel * 64 + (uintptr_t)device + 1;  // addresses of kernels are even, devices few
+  unsigned at = (unsigned)(key * 0x9e3779b97f4a7c15ull >> 56);
+  for (int i = 0; i < 256; i++, at = (at + 1) % 256) {
+    const uintptr_t here = done[at].load(std::memory_order_acquire);
+    if (here == key) return true;
+    if (here == 0) break;
+  }
   if (shared == kNoCache &&
       cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared) != cudaSuccess)
     return false;
   if (shared > 0 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, shared) != cudaSuccess) return false;
-  done.insert({kernel, device});
+  uintptr_t none = 0;
+  done[at].compare_exchange_strong(none, key, std::memory_order_release);  // another's now: prepared again the next time
   return true;
 }
 
