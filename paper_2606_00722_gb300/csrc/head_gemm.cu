@@ -5,6 +5,12 @@
 // ahead), one thread of the pair issues the products, sums lie in tensor memory, twice, so that eight warps a CTA work on
 // one tile's sums while the next tile's are made.  Operands are read as they lie: e along and across its rows, the head by
 // tokens and by hidden dimensions.
+//
+// A step of a tile takes the tensor units 512 clocks and 64 bytes a clock and SM from L2, about what L2 gives: a CTA's own
+// tile of 128 x 256 would need 96.  Of 4,096 rows through 32,768 x 2,048 the tensor pipe is active 95 % of the time for logits
+// alone, 83 % with exponentials, 90 % for both gradients (258, 293 and 567 us); of 4,096 through 126,000 x 4,096 they take 2.1,
+// 2.2 and 4.6 ms (1.9 to 2.0 PFLOP/s), at the power limit.  With few rows the head's bytes are the time: 32 through 126,000 x 4,096
+// 185 us (5.6 TB/s) for logits, 400 for the gradients, which read it once and write as much.
 #include <cuda.h>
 
 #include <algorithm>
@@ -291,7 +297,7 @@ struct LogitsRow {
     if (!probs) return;
     ref = a.pass.known ? p.known_ref[row] : p.ref[row];
     if (a.pass.known) mul = p.known_mul[row];
-    if (a.pass.only_again) at = p.known_at[row];
+    if (a.pass.only_again) at = p.e_target[row];
   }
 };
 
@@ -302,7 +308,7 @@ __device__ __forceinline__ void logits_rows(const TileArgs& a, const HeadMaps& m
   const HeadPlan& p = a.p;
   const bool real = row < n, known = a.pass.known;
   const int y = real ? is.target - col : -1;
-  const float ref = is.ref, mul = is.mul, at = is.at;
+  const float ref = is.ref, mul = is.mul;
   float to = kProbs ? (known ? 0.0f : ref) : kNoRef, s = 0.0f;
 #pragma unroll 1
   for (int c = 0; c < kRecCols; c += 32) {
@@ -316,9 +322,8 @@ __device__ __forceinline__ void logits_rows(const TileArgs& a, const HeadMaps& m
       for (int j = 0; j < 32; j++)
         if (col + c + j >= p.V) z[j] = -CUDART_INF_F;
     }
-    float zt = 0.0f;
-    const bool target = here >= 0 && here < 32;
-    if (target) {
+    if (here >= 0 && here < 32) {  // the target is left out
+      float zt = 0.0f;
 #pragma unroll
       for (int j = 0; j < 32; j++)
         if (j == here) zt = z[j], z[j] = -CUDART_INF_F;
@@ -328,11 +333,10 @@ __device__ __forceinline__ void logits_rows(const TileArgs& a, const HeadMaps& m
 #pragma unroll
       for (int j = 0; j < 32; j++) z[j] = ex2(fmaf(z[j], kLog2E, -ref)) * mul;
       s += sum32(z);
-      if (target) {
-        const float e = a.pass.only_again ? at : ex2(fmaf(zt, kLog2E, -ref)) * mul;
+      if (is.at != 0.0f && here >= 0 && here < 32) {
 #pragma unroll
         for (int j = 0; j < 32; j++)
-          if (j == here) z[j] = e;
+          if (j == here) z[j] = is.at;
       }
       if (!real) {
 #pragma unroll
@@ -380,9 +384,56 @@ __device__ __forceinline__ void store_floats(float* part, const float (&v)[32]) 
   for (int j = 0; j < 32; j += 4) ((float4*)part)[j / 4] = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
 }
 
+// What a row of a gradient needs beside its sums, read before they are there
+struct GradRow {
+  long long begin;  // of a hidden state's gradient
+  float coef;       // what its sums are multiplied with
+  int4 with;        // of a hidden state: its target; of the head: the listed rows with that target; or -1
+  float4 f;         // what they are multiplied with
+  // a tile ahead
+  __device__ __forceinline__ GradRow(const TileArgs& a, int n, bool again, float post, const Task& t, int row_of_tile)
+      : begin(0), coef(post), with(make_int4(-1, -1, -1, -1)), f(make_float4(0.0f, 0.0f, 0.0f, 0.0f)) {
+    const HeadPlan& p = a.p;
+    const int row = t.m0 + row_of_tile;
+    if (t.job == 0 && row < n) {
+      begin = p.to[row];
+      if (!again) coef = p.coef[row];
+      f.x = p.at_target[row];
+      with.x = p.tgt[row];
+    } else if (t.job == 1 && row < p.V) {
+      with = p.list[row];
+    }
+  }
+  // before the tile's sums are waited for
+  __device__ __forceinline__ void factors(const TileArgs& a, const Task& t) {
+    if (t.job == 0) {
+      if (f.x == 0.0f) with.x = -1;
+      return;
+    }
+    const float* at = a.p.at_target;
+    if (with.x >= 0) f.x = at[with.x];
+    if (with.y >= 0) f.y = at[with.y];
+    if (with.z >= 0) f.z = at[with.z];
+    if (with.w >= 0) f.w = at[with.w];
+  }
+};
+
+// v += f x[0..31], of which those before `end` are used, at a multiple of 16 bytes
+template <typename T>
+__device__ __forceinline__ void add_row(float (&v)[32], float f, const T* x, int end) {
+#pragma unroll
+  for (int j = 0; j < 32; j += 8) {
+    if (j >= end) break;
+    const uint4 w = *(const uint4*)(x + j);
+    const T* t = (const T*)&w;
+#pragma unroll
+    for (int i = 0; i < 8; i++) v[j + i] = fmaf(f, as_float(t[i]), v[j + i]);
+  }
+}
+
 // Sums of a gradient's tile: kHalf columns of each lane's row, 64 at a time
 template <typename T>
-__device__ __forceinline__ void grad_rows(const TileArgs& a, const HeadMaps& maps, int n, float post, float coef, long long begin,
+__device__ __forceinline__ void grad_rows(const TileArgs& a, const HeadMaps& maps, int n, float post, const GradRow& is,
                                           const Task& t, uint32_t sums, int row, int col, Turn& turn) {
   const HeadPlan& p = a.p;
   const GradSplit& sp = a.p.split;
@@ -392,8 +443,8 @@ __device__ __forceinline__ void grad_rows(const TileArgs& a, const HeadMaps& map
   if (row - turn.lane >= end) return;
   const bool there = row < end, out = !parts && (hidden || a.sum == kOnly || a.sum == kLast), box = out && !hidden && maps.boxes;
   uint16_t* to = nullptr;
-  if (there && out) to = hidden ? (uint16_t*)a.out.grad + begin : (uint16_t*)a.grad_head + row * a.grad_head_stride;
-  const float scale = hidden ? coef : post;
+  if (there && out) to = hidden ? (uint16_t*)a.out.grad + is.begin : (uint16_t*)a.grad_head + row * a.grad_head_stride;
+  const float scale = hidden ? is.coef : post;
   const bool whole = __all_sync(~0u, ((uintptr_t)to & 15) == 0);
   const CUtensorMap* part = hidden ? &maps.hidden_parts : &maps.head_parts;
   const int part_row = t.part * (hidden ? p.cap : (int)sp.tokens) + row - turn.lane;
@@ -410,10 +461,6 @@ __device__ __forceinline__ void grad_rows(const TileArgs& a, const HeadMaps& map
     }
   };
   auto pass = [&](float(&v)[32], int c) {
-    if (scale != 1.0f) {
-#pragma unroll
-      for (int j = 0; j < 32; j++) v[j] *= scale;
-    }
     if (!hidden && a.sum != kOnly && there && c < p.d) {
       if (a.sum != kFirst) {
 #pragma unroll
@@ -434,6 +481,23 @@ __device__ __forceinline__ void grad_rows(const TileArgs& a, const HeadMaps& map
       turn.put_floats(w);
       turn.store(part, c, c + 32 < p.d ? c + 32 : -1, part_row);
       continue;
+    }
+    if (scale != 1.0f) {
+#pragma unroll
+      for (int j = 0; j < 32; j++) v[j] *= scale, w[j] *= scale;
+    }
+    const T* x = hidden ? (const T*)p.head + c : (const T*)p.hc + c;
+    const long long ld = hidden ? p.ldw : p.ldh;
+    int4 q = is.with;
+    float4 f = is.f;
+#pragma unroll 1
+    while (__any_sync(~0u, q.x >= 0)) {
+      if (q.x >= 0) {
+        add_row(v, f.x, x + q.x * ld, p.d - c);
+        add_row(w, f.x, x + q.x * ld + 32, p.d - c - 32);
+      }
+      q = make_int4(q.y, q.z, q.w, -1);
+      f = make_float4(f.y, f.z, f.w, 0.0f);
     }
     pass(v, c);
     pass(w, c + 32);
@@ -560,30 +624,35 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         use++;
       }
     }
-  } else if (warp >= 4) {
+  } else if (warp < 4) {
+    if (kForm != 2 && a.p.list && !a.pass.only_again)  // empty lists, for the kernel behind this one
+      for (long long v = blockIdx.x * 64ll + threadIdx.x - 64; v < a.p.V; v += gridDim.x * 64ll)
+        a.p.list[v] = make_int4(-1, -1, -1, -1);
+  } else {
     const int part = warp - 4, quarter = warp % 4;
     const uint32_t turns = stages + kStages * kStage + part * kTurn;
     Turn turn = {turns, turns + kTurn / 2, lane};
     const float post = kForm == 2 && again ? *a.p.post : 1.0f;
     int use = 0;
-    Task t;
-    while (tasks.next(t)) {
-      const int half = use & 1;
-      const int row = t.m0 + rank * kHalf + quarter * 32 + lane, off = part / 4 * kHalf;
+    const int row_of_tile = rank * kHalf + quarter * 32 + lane, off = part / 4 * kHalf;
+    Task t, ahead = {a.p.V, 0, 0, 0, 1, 0};
+    bool more = tasks.next(ahead);
+    GradRow with_ahead(a, kForm == 2 ? n : 0, again, post, ahead, kForm == 2 ? row_of_tile : 0);  // a tile before it is needed
+    while (more) {
+      t = ahead;
+      GradRow with = with_ahead;
+      if (kForm == 2) with.factors(a, t);
+      more = tasks.next(ahead);
+      if (kForm == 2 && more) with_ahead = GradRow(a, n, again, post, ahead, row_of_tile);
+      const int half = use & 1, row = t.m0 + row_of_tile;
       const uint32_t from = sums + half * kTile + off + ((uint32_t)quarter * 32 << 16);
       const LogitsRow is(a, kForm == 1, kForm == 2 ? 0 : n, row);
-      long long begin = 0;
-      float coef = post;
-      if (kForm == 2 && t.job == 0 && row < n) {
-        begin = a.p.to[row];
-        if (!again) coef = a.p.coef[row];
-      }
       if (t.steps > 0) {
         if (!(ok = bar_wait(sums_full + 8 * half, use >> 1 & 1))) break;
         products_fence_after();
       }
       if (kForm == 2) {
-        grad_rows<T>(a, maps, n, post, coef, begin, t, from, row, t.n0 + off, turn);
+        grad_rows<T>(a, maps, n, post, with, t, from, row, t.n0 + off, turn);
       } else if (row - lane < up_div(n, kStepK) * kStepK) {
         logits_rows<T, kForm == 1>(a, maps, n, is, from, row, t.n0 + off, turn);
       }
@@ -609,6 +678,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   if (warp == 1) sums_free_pair(sums);
 }
 
+// v += f x[0..3], at a multiple of 8 bytes; of a row's last four those past it are not used
+template <typename T>
+__device__ __forceinline__ void add_four(float (&v)[4], float f, const T* x) {
+  const uint2 w = *(const uint2*)x;
+  const T* t = (const T*)&w;
+#pragma unroll
+  for (int i = 0; i < 4; i++) v[i] = fmaf(f, as_float(t[i]), v[i]);
+}
+
 // Parts of a gradient's sums, in order
 template <typename T>
 __global__ void __launch_bounds__(256) k_head_parts(const __grid_constant__ TileArgs a) {
@@ -630,17 +708,25 @@ __global__ void __launch_bounds__(256) k_head_parts(const __grid_constant__ Tile
       const float4 v = *(const float4*)(from + (k * room + row) * p.ldp + c);
       s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
     }
-    float v[4] = {s.x, s.y, s.z, s.w};
+    const float scale = hidden && !again ? p.coef[row] : post;
+    float v[4] = {s.x * scale, s.y * scale, s.z * scale, s.w * scale};
+    const int end = min(4, p.d - c);
     T* to;
     if (hidden) {
       to = (T*)a.out.grad + p.to[row];
+      const float f = p.at_target[row];
+      if (f != 0.0f) add_four(v, f, (const T*)p.head + p.tgt[row] * p.ldw + c);
     } else {
       to = (T*)a.grad_head + row * a.grad_head_stride;
+      const int4 list = p.list[row];
+      for (const int q : {list.x, list.y, list.z, list.w}) {
+        if (q < 0) break;
+        add_four(v, p.at_target[q], (const T*)p.hc + q * p.ldh + c);
+      }
     }
-    const float scale = hidden && !again ? p.coef[row] : post;
     float* acc = p.acc + row * p.ldp + c;
-    for (int j = 0; j < 4 && c + j < p.d; j++) {
-      float x = v[j] * scale;
+    for (int j = 0; j < end; j++) {
+      float x = v[j];
       if (!hidden && (a.sum == kMiddle || a.sum == kLast)) x += acc[j];
       if (!hidden && (a.sum == kFirst || a.sum == kMiddle)) acc[j] = x;
       else to[c + j] = of_float<T>(x);
@@ -665,7 +751,7 @@ GradSplit split_grads(int rows, int d, int V) {
   GradSplit s = {};
   const long long ct = (d + kTile - 1) / kTile, mt = (rows + kTile - 1) / kTile, vt = (V + (long long)kTile - 1) / kTile;
   const long long kv = (V + (long long)kStepK - 1) / kStepK, kr = (rows + kStepK - 1) / kStepK;
-  s.tile_cost = 4;
+  s.tile_cost = 4;  // epilogue and first loads of a tile, some 2,000 clocks, in steps of 512
   s.tokens = vt * kTile;
   const long long all = mt * ct * (kv + s.tile_cost) + vt * ct * (kr + s.tile_cost), unit = std::max(8ll, all / kPairs);
   s.hidden_parts = (int)std::min<long long>(kMostParts, (kv + unit - 1) / unit);

@@ -16,7 +16,8 @@
 // step multiplies hidden states.  (To round e alone there, the sums would have to be known before e is written: the logits
 // made twice, a third more work.)  Rows of a step whose exponentials leave the range, and all of an fp16 step, which has
 // not the range at all, get their gradients of logits from the logsumexp in a second pass.  At the target, e - S cancels
-// where the model is sure; there e holds minus the sum of the others, which is summed apart.
+// where the model is sure, and is most of a row's gradient: it is minus the sum of the others, summed apart, and comes to the
+// sums in 32 bits as they leave the tensor units.
 // Sums, references and losses are 32 bits.
 #include <stdlib.h>
 
@@ -223,6 +224,35 @@ struct MeetArgs {
   bool known;         // as gradients of logits
 };
 
+// Each of the CTA's kMeetRows rows counts those before it with the same target, and is listed if they are few.  rank: how many
+// they are; complete after the CTA's next barrier.
+template <int kMeetRows>
+__device__ __forceinline__ void list_targets(const HeadPlan& p, int n, int q0, int (&rank)[kMeetRows]) {
+  __shared__ int s_count[kMeetWarps][kMeetRows];
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+  int target[kMeetRows], count[kMeetRows];
+#pragma unroll
+  for (int i = 0; i < kMeetRows; i++) target[i] = q0 + i < n ? p.tgt[q0 + i] : -1, count[i] = 0;
+#pragma unroll 4
+  for (int q = threadIdx.x; q < min(n, q0 + kMeetRows); q += kMeetWarps * 32) {
+    const int t = p.tgt[q];
+#pragma unroll
+    for (int i = 0; i < kMeetRows; i++) count[i] += t == target[i] && q < q0 + i;
+  }
+#pragma unroll
+  for (int i = 0; i < kMeetRows; i++) {
+    count[i] = __reduce_add_sync(~0u, count[i]);
+    if (lane == 0) s_count[warp][i] = count[i];
+  }
+  __syncthreads();
+  const int q = q0 + threadIdx.x;
+  if (threadIdx.x >= kMeetRows || q >= n) return;
+  int many = 0;
+  for (int w = 0; w < kMeetWarps; w++) many += s_count[w][threadIdx.x];
+  rank[threadIdx.x] = many;
+  if (many < kListed) ((int*)(p.list + p.tgt[q]))[many] = q;
+}
+
 // Loss and factors of kMeetRows (8, or with few rows 1) packed rows from their records: as many lanes, the records dealt to
 // groups of them and met in a fixed order.
 template <typename T, int kMeetRows>
@@ -235,6 +265,8 @@ __global__ void __launch_bounds__(kMeetWarps * 32) k_head_meet(MeetArgs a) {
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, at = lane % kMeetRows;
   const int n = *p.count, q0 = blockIdx.x * kMeetRows, q = q0 + at;
   if (q0 >= n) return;
+  __shared__ int s_rank[kMeetRows];
+  if (p.list) list_targets(p, n, q0, s_rank);
   float ref = kNoRef, s = 0.0f;
   int left = 0;
   if (q < n) {
@@ -260,8 +292,10 @@ __global__ void __launch_bounds__(kMeetWarps * 32) k_head_meet(MeetArgs a) {
         meet(ref, s, s_ref[w][lane], s_sum[w][lane]);
         left |= s_left[w][lane];
       }
+      const bool listed = a.grads && s_rank[lane] < kListed;
       if (a.known) {
-        ((T*)p.e)[q * p.lde + p.tgt[q]] = of_float<T>(-s);
+        p.at_target[q] = listed ? -s * *p.post : 0.0f;
+        if (!listed) ((T*)p.e)[q * p.lde + p.tgt[q]] = of_float<T>(-s);
       } else {
         // the others' sum against the target: loss = log(1 + sum / e_y)
         const float zt = p.zt[q], by = s == 0.0f && zt > -CUDART_INF_F ? -CUDART_INF_F : log2f(s) + fmaf(-zt, kLog2E, ref);
@@ -273,16 +307,17 @@ __global__ void __launch_bounds__(kMeetWarps * 32) k_head_meet(MeetArgs a) {
         a.loss[r] = (a.weight ? a.weight[r] : 1.0f) * nll;
         if (a.lse) a.lse[r] = lse;
         if (a.grads) {
-          const float g = p.g[q], post = *p.post;
+          const float g = p.g[q], post = *p.post, most = -g * ((x > 0.0f ? 1.0f : small) / (1.0f + small));
           know(p, q, lse, g, post);
-          p.known_at[q] = -(g / post) * ((x > 0.0f ? 1.0f : small) / (1.0f + small));
+          p.at_target[q] = listed ? most : 0.0f;
+          p.e_target[q] = listed ? 0.0f : most / post;
           if (a.stored) {
             const float to = p.ref[q];
             if (left || !(fmaf(zt, kLog2E, -to) <= kWindow)) *p.again = 1;
             const float others = s == 0.0f ? 0.0f : s * pow2_whole(ref - to);
             coef = g / (others + ex2(fmaf(zt, kLog2E, -to)));
             p.coef[q] = coef;
-            ((T*)p.e)[q * p.lde + p.tgt[q]] = of_float<T>(-others);
+            if (!listed) ((T*)p.e)[q * p.lde + p.tgt[q]] = of_float<T>(-others);
           }
         }
       }
@@ -411,11 +446,12 @@ size_t plan_head(const HeadCall& c, void* base, HeadPlan& p) {
   w.take(p.src, cap, 4);
   w.take(p.to, cap, 8);
   w.take(p.tgt, cap, 4);
-  for (float** f : {&p.g, &p.zt, &p.ref, &p.coef, &p.known_ref, &p.known_mul, &p.known_at}) w.take(*f, cap, 4);
+  for (float** f : {&p.g, &p.zt, &p.ref, &p.coef, &p.known_ref, &p.known_mul, &p.at_target, &p.e_target}) w.take(*f, cap, 4);
   w.take(p.hc, cap * p.ldh, 2);
   if (c.form == kStep && c.dtype == EPIC_BF16) w.take(p.hs, cap * p.ldh, 2);
   w.take(p.rec, cap * p.nrec, sizeof(float2));
   if (c.form != kForward) {
+    w.take(p.list, (size_t)c.V, sizeof(int4));
     w.take(p.e, cap * p.lde, 2);
     if (rows > p.cap) w.take(p.acc, (size_t)c.V * p.ldp, 4);
     p.split = split_grads((int)std::min<long long>(rows, p.cap), c.d, c.V);

@@ -11,6 +11,7 @@ namespace epic {
 
 constexpr int kRowTile = 256;   // rows of a workspace come in whole tiles
 constexpr int kRecCols = 128;   // tokens whose exponentials one record sums
+constexpr int kListed = 4;      // (an int4) rows of one target whose gradient at it is kept in 32 bits
 constexpr int kMostParts = 64;  // of a gradient's sum
 
 // Few tiles with long sums are cut into parts, whose sums meet in a second kernel: of gradients of hidden states over the
@@ -44,8 +45,12 @@ struct HeadPlan {
   float *ref, *coef;        // [cap]
   // Or, where the logsumexp is known, e = known_mul 2^(z log2 e - known_ref), gradients of logits / *post.
   float *known_ref, *known_mul;  // [cap]
-  // At the target e is minus the sum of the others, so that little is lost where they are few.
-  float *known_at;          // [cap] that
+  // The gradient at the target, minus the sum of the others' (so that little is lost where they are few), is most of a row's.
+  // Of the first kListed rows of a target it is 0 in e, kept in 32 bits, and multiplied with the target's row of the head, and
+  // with the hidden state, as sums leave; more rows of one target even out, and have it in e.
+  float *at_target;         // [cap] that, or 0
+  float *e_target;          // [cap] what e holds there, as gradients of logits
+  int4* list;               // [V] the first rows with that target, or -1; NULL without gradients
   float2* rec;              // [nrec][cap] (whole reference, sum of exponentials relative to it), target left out
   void *hc, *hs;            // [cap][ldh] hidden states; the same times coef, or NULL
   void* e;                  // [cap][lde]
@@ -65,10 +70,11 @@ struct HiddenGrad {
 };
 
 // Logits of the packed rows.  sums: records and target logits.  probs: e, with a known logsumexp or not.  only_again: nothing
-// unless *again; then with known_at at the targets.
+// unless *again; then with e_target at the targets.
 struct LogitsPass {
   bool sums, probs, known, only_again;
 };
+
 // How boxes of the operands are copied, the same for all of a call's kernels and pieces: 64 columns by 64 rows, those that go
 // out by 32 rows
 struct HeadMaps {
@@ -83,6 +89,7 @@ epic_status launch_head_logits(const HeadPlan& p, const HeadMaps& maps, int dtyp
 // pieces before (NULL: none); of gradients of logits in e, post e W and post e^T hc.
 epic_status launch_head_grads(const HeadPlan& p, const HeadMaps& maps, int dtype, const HiddenGrad& out, void* grad_head,
                               long long stride, HeadSum sum, cudaStream_t st);
+
 GradSplit split_grads(int rows, int d, int V);
 
 }  // namespace epic

@@ -508,3 +508,28 @@ def test_weights_of_all_sizes(cuda, dtype):
     epic.head_loss_forward(h, W, target, loss, lse, weight=weight)
     epic.head_loss_backward(h, W, target, lse, up, gh, gw, weight=weight)
     check_grads(gh, gw, want, dtype)
+
+
+@pytest.mark.parametrize('dtype', ['bf16', 'f16'])
+@pytest.mark.parametrize('d,V', [(64, 300), (200, 9000)])
+def test_targets_that_many_positions_share(cuda, dtype, d, V):
+    """One target for a third of 700 positions, a few for the rest, in all forms; also with rows that leave the window."""
+    import torch
+    import paper_2606_00722_gb300 as epic
+    for scale in (1.0, 30.0):
+        h, W, target, weight, up = make(1, 700, d, V, dtype, d, scale=scale)
+        target[0, ::3] = torch.where((target[0, ::3] >= 0) & (target[0, ::3] < V), 7, target[0, ::3])
+        target[0, 1::3] = torch.where((target[0, 1::3] >= 0) & (target[0, 1::3] < V), target[0, 1::3] % 60, target[0, 1::3])
+        step, want = head64(h, W, target, weight), head64(h, W, target, weight, up)
+        z = 2.0 ** -21 * float((h.double().nan_to_num(0, 0, 0) @ W.double().t()).abs().max())  # a power's argument
+        for r in (step, want):
+            r['ae'] += z * r['a']
+            r['be'] += z * r['b']
+        loss, lse = torch.empty((1, 700), device=cuda), torch.empty((1, 700), device=cuda)
+        gh, gw = torch.empty_like(h), torch.empty_like(W)
+        epic.head_loss_step(h, W, target, loss, gh, gw, weight=weight)
+        close(loss, step['loss'], step['loss_tol'])
+        check_grads(gh, gw, step, dtype)
+        epic.head_loss_forward(h, W, target, loss, lse, weight=weight)
+        epic.head_loss_backward(h, W, target, lse, up, gh, gw, weight=weight)
+        check_grads(gh, gw, want, dtype)
