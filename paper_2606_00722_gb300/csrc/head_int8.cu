@@ -96,10 +96,9 @@ struct Int8Args {
 
 // ---- few rows: a warp's lanes along tokens' rows, whole-number products of four bytes an instruction
 //
-// The head is read once: 126,000 x 4,096 bytes for one row in 76 us (6.8 TB/s).  A warp has four tokens at a time, so that
-// what it reads of the hidden states in shared memory serves four; up to eight rows products stay behind memory (1 of 4 bytes
-// a row and clock of the 64 or so that an SM has).  A row's last 16 bytes may hold bytes behind it: hidden states there are 0.
-
+// The head is read once: 126,000 x 4,096 bytes for one row in 84 us (6.1 TB/s), for eight, whose products take nearly as long
+// as the bytes, in 108.  A warp has four tokens at a time, so that what it reads of the hidden states in shared memory
+// serves four.  A row's last 16 bytes may hold bytes behind it: hidden states there are 0.
 constexpr int kFewRows = 8, kFewTokens = 4, kFewThreads = 256;
 constexpr int kFewBytes = 64 << 10;  // of hidden states that a CTA holds
 
@@ -127,9 +126,15 @@ __global__ void __launch_bounds__(kFewThreads) k_few_logits(Int8Args a) {
   follow();
   let_next();
   const int lane = threadIdx.x % 32, chunks = (a.d + 15) / 16;
-  for (int i = threadIdx.x; i < R * chunks * 16; i += kFewThreads) {
-    const int r = i / (chunks * 16), c = i % (chunks * 16);
-    ((int8_t*)s_q)[i] = r < a.rows && c < a.d ? a.q[(long long)r * a.d + c] : 0;
+  if (a.d % 16 == 0 && (uintptr_t)a.q % 16 == 0) {
+#pragma unroll 4
+    for (int i = threadIdx.x; i < R * chunks; i += kFewThreads)
+      s_q[i] = i < a.rows * chunks ? ((const int4*)a.q)[i] : make_int4(0, 0, 0, 0);
+  } else {
+    for (int r = 0; r < R; r++)
+#pragma unroll 4
+      for (int c = threadIdx.x; c < chunks * 16; c += kFewThreads)
+        ((int8_t*)s_q)[r * chunks * 16 + c] = r < a.rows && c < a.d ? a.q[(long long)r * a.d + c] : 0;
   }
   __syncthreads();
   const long long warps = (long long)gridDim.x * (kFewThreads / 32);
@@ -569,13 +574,17 @@ bool head_lies_askew(const int8_t* head, long long stride, int V) {
   return (uintptr_t)head % 16 != 0 || (V > 1 && (stride % 16 != 0 || stride >= 1ll << 39));
 }
 
+// One, four and eight rows through 126,000 x 4,096 take 84, 98 and 108 us so and 114 in tiles, four and eight through 50,000 x
+// 1,024 12 and 16, in tiles 19.
 bool few_rows(long long rows, int d, bool askew) {
   return rows <= kFewRows && !askew && (rows <= 1 ? 1 : rows <= 2 ? 2 : rows <= 4 ? 4 : 8) * (d + 15ll) <= kFewBytes;
 }
 
 size_t sizes_bytes(long long rows, int d) { return (size_t)(rows * ((d + 1023) / 1024) * 4 + 255) / 256 * 256; }
 
-// Rows of a tile: a step takes the tensor units 2 clocks a row, and about 320 at least for the head's bytes.
+// Rows of a tile: a step takes the tensor units 2 clocks a row, and about 320 at least for the head's bytes.  Tiles of 64, 128
+// and 256 rows (us): 64 rows through 32,768 x 2,048 24, 27, 34; 128 rows 39, 27, 34; through 50,000 x 1,024, 165 rows 41, 37,
+// 36; 300 rows 62, 48, 61.
 int tile_rows(long long rows) {
   int best = 256;
   long long least = -1;
