@@ -7,8 +7,8 @@
 // tokens and by hidden dimensions.
 //
 // A step of a tile takes the tensor units 512 clocks and 64 bytes a clock and SM from L2, about what L2 gives: a CTA's own
-// tile of 128 x 256 would need 96.  Of 4,096 rows through 32,768 x 2,048 the tensor pipe is active 95 % of the time for logits
-// alone, 83 % with exponentials, 90 % for both gradients (258, 293 and 567 us); of 4,096 through 126,000 x 4,096 they take 2.1,
+// tile of 128 x 256 would need 96.  Of 4,096 rows through 32,768 x 2,048 the tensor pipe is active 91 % of the time for logits
+// alone, 82 % with exponentials, 87 % for both gradients (267, 290 and 579 us); of 4,096 through 126,000 x 4,096 they take 2.1,
 // 2.2 and 4.6 ms (1.9 to 2.0 PFLOP/s), at the power limit.  With few rows the head's bytes are the time: 32 through 126,000 x 4,096
 // 185 us (5.6 TB/s) for logits, 400 for the gradients, which read it once and write as much.
 #include <cuda.h>
@@ -635,32 +635,46 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     const float post = kForm == 2 && again ? *a.p.post : 1.0f;
     int use = 0;
     const int row_of_tile = rank * kHalf + quarter * 32 + lane, off = part / 4 * kHalf;
-    Task t, ahead = {a.p.V, 0, 0, 0, 1, 0};
-    bool more = tasks.next(ahead);
-    GradRow with_ahead(a, kForm == 2 ? n : 0, again, post, ahead, kForm == 2 ? row_of_tile : 0);  // a tile before it is needed
-    while (more) {
-      t = ahead;
-      GradRow with = with_ahead;
-      if (kForm == 2) with.factors(a, t);
-      more = tasks.next(ahead);
-      if (kForm == 2 && more) with_ahead = GradRow(a, n, again, post, ahead, row_of_tile);
-      const int half = use & 1, row = t.m0 + row_of_tile;
+    // one tile's sums, by `rows`; false: gave up
+    auto tile = [&](const Task& t, auto rows) {
+      const int half = use & 1;
       const uint32_t from = sums + half * kTile + off + ((uint32_t)quarter * 32 << 16);
-      const LogitsRow is(a, kForm == 1, kForm == 2 ? 0 : n, row);
       if (t.steps > 0) {
-        if (!(ok = bar_wait(sums_full + 8 * half, use >> 1 & 1))) break;
+        if (!(ok = bar_wait(sums_full + 8 * half, use >> 1 & 1))) return false;
         products_fence_after();
       }
-      if (kForm == 2) {
-        grad_rows<T>(a, maps, n, post, with, t, from, row, t.n0 + off, turn);
-      } else if (row - lane < up_div(n, kStepK) * kStepK) {
-        logits_rows<T, kForm == 1>(a, maps, n, is, from, row, t.n0 + off, turn);
-      }
+      rows(from);
       if (t.steps > 0) {
         products_fence_before();
         __syncwarp();
         if (lane == 0) bar_arrive_cluster(at_rank(sums_empty + 8 * half, 0));
         use++;
+      }
+      return true;
+    };
+    Task t;
+    if constexpr (kForm == 2) {
+      Task ahead = {a.p.V, 0, 0, 0, 1, 0};
+      bool more = tasks.next(ahead);
+      GradRow with_ahead(a, n, again, post, ahead, row_of_tile);  // a tile before it is needed
+      while (more) {
+        t = ahead;
+        GradRow with = with_ahead;
+        with.factors(a, t);
+        more = tasks.next(ahead);
+        if (more) with_ahead = GradRow(a, n, again, post, ahead, row_of_tile);
+        if (!tile(t, [&](uint32_t from) { grad_rows<T>(a, maps, n, post, with, t, from, t.m0 + row_of_tile, t.n0 + off, turn); }))
+          break;
+      }
+    } else {
+      while (tasks.next(t)) {
+        const int row = t.m0 + row_of_tile;
+        const LogitsRow is(a, kForm == 1, n, row);
+        if (!tile(t, [&](uint32_t from) {
+              if (row - lane < up_div(n, kStepK) * kStepK)
+                logits_rows<T, kForm == 1>(a, maps, n, is, from, row, t.n0 + off, turn);
+            }))
+          break;
       }
     }
     if (lane == 0) boxes_read<0>();
