@@ -25,7 +25,7 @@ inline bool prepare_kernel(const void* kernel, int shared) {
   static std::atomic<uintptr_t> done[256];  // kernel and device, by a hash; a place is taken once and kept
   int device;
   if (cudaGetDevice(&device) != cudaSuccess) return false;
-  const uintptr_t key = (uintptr_t)kernel * 64 + (uintptr_t)device + 1;  // addresses of kernels are even, devices few
+  const uintptr_t key = (uintptr_t)kernel * 64 + (uintptr_t)device + 1;  // different for all kernels and up to 63 devices
   unsigned at = (unsigned)(key * 0x9e3779b97f4a7c15ull >> 56);
   for (int i = 0; i < 256; i++, at = (at + 1) % 256) {
     const uintptr_t here = done[at].load(std::memory_order_acquire);
