@@ -451,8 +451,9 @@ enum { EPIC_HEAD_FORWARD = 0, EPIC_HEAD_BACKWARD = 1, EPIC_HEAD_STEP = 2 };
  * the logits once (bf16).
  * In both, gradients of logits are rounded to dtype (off by at most 2^-8 of a value in
  * bf16, 2^-11 in fp16) before they are multiplied and summed; so are, in a step in bf16,
- * hidden states times a row's factor.  The gradient at the target, most of a row's, stays
- * in 32 bits for the first 4 positions of a target in 16,384.  In fp16 they are held relative to the largest
+ * hidden states times a row's factor.  The gradient at the target, most of a row's, is not
+ * rounded for d_grad_hidden, and for d_grad_head not that of the first 4 positions of a target
+ * in a piece (of 16,384 or fewer).  In fp16 they are held relative to the largest
  * |w grad_loss| of 16,384 positions: what is below 2^-28 of it loses bits, below 2^-39 all.
  * Sums of the products are the tensor units', which cut what they add to 32 bits.
  * A target of probability 0 gives loss +inf and a finite gradient.  NaN or +inf

@@ -337,6 +337,7 @@ __device__ __forceinline__ void logits_rows(const TileArgs& a, const HeadMaps& m
 #pragma unroll
         for (int j = 0; j < 32; j++)
           if (j == here) z[j] = is.at;
+        p.at_target[row] = lost<T>(is.at) * *p.post;
       }
       if (!real) {
 #pragma unroll

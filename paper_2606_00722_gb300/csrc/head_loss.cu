@@ -294,7 +294,7 @@ __global__ void __launch_bounds__(kMeetWarps * 32) k_head_meet(MeetArgs a) {
       }
       const bool listed = a.grads && s_rank[lane] < kListed;
       if (a.known) {
-        p.at_target[q] = listed ? -s * *p.post : 0.0f;
+        p.at_target[q] = (listed ? -s : lost<T>(-s)) * *p.post;
         if (!listed) ((T*)p.e)[q * p.lde + p.tgt[q]] = of_float<T>(-s);
       } else {
         // the others' sum against the target: loss = log(1 + sum / e_y)
@@ -309,7 +309,7 @@ __global__ void __launch_bounds__(kMeetWarps * 32) k_head_meet(MeetArgs a) {
         if (a.grads) {
           const float g = p.g[q], post = *p.post, most = -g * ((x > 0.0f ? 1.0f : small) / (1.0f + small));
           know(p, q, lse, g, post);
-          p.at_target[q] = listed ? most : 0.0f;
+          float at = listed ? most : 0.0f;
           p.e_target[q] = listed ? 0.0f : most / post;
           if (a.stored) {
             const float to = p.ref[q];
@@ -317,8 +317,12 @@ __global__ void __launch_bounds__(kMeetWarps * 32) k_head_meet(MeetArgs a) {
             const float others = s == 0.0f ? 0.0f : s * pow2_whole(ref - to);
             coef = g / (others + ex2(fmaf(zt, kLog2E, -to)));
             p.coef[q] = coef;
-            if (!listed) ((T*)p.e)[q * p.lde + p.tgt[q]] = of_float<T>(-others);
+            if (!listed) {
+              ((T*)p.e)[q * p.lde + p.tgt[q]] = of_float<T>(-others);
+              at = coef * lost<T>(-others);
+            }
           }
+          p.at_target[q] = at;
         }
       }
     }

@@ -47,8 +47,9 @@ struct HeadPlan {
   float *known_ref, *known_mul;  // [cap]
   // The gradient at the target, minus the sum of the others' (so that little is lost where they are few), is most of a row's.
   // Of the first kListed rows of a target it is 0 in e, kept in 32 bits, and multiplied with the target's row of the head, and
-  // with the hidden state, as sums leave; more rows of one target even out, and have it in e.
-  float *at_target;         // [cap] that, or 0
+  // with the hidden state, as sums leave.  More rows of one target have it in e: in the gradient of the head their roundings even
+  // out, and in a row's own, which has no other as large, what the rounding took is added in the same way.
+  float *at_target;         // [cap] that: all of it, or what the rounding took
   float *e_target;          // [cap] what e holds there, as gradients of logits
   int4* list;               // [V] the first rows with that target, or -1; NULL without gradients
   float2* rec;              // [nrec][cap] (whole reference, sum of exponentials relative to it), target left out

@@ -66,6 +66,13 @@ __device__ __forceinline__ __nv_bfloat16 of_float<__nv_bfloat16>(float v) { retu
 template <>
 __device__ __forceinline__ float of_float<float>(float v) { return v; }
 
+// What the rounding of a number to 16 bits takes from it
+template <typename T>
+__device__ __forceinline__ float lost(float v) {
+  const float rest = v - as_float(of_float<T>(v));
+  return fabsf(rest) < CUDART_INF_F ? rest : 0.0f;
+}
+
 // 16 bytes of a row as numbers of 32 bits
 template <typename T>
 struct Chunk {
