@@ -600,13 +600,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       while (ok && tasks.next(t)) {
         if (t.steps <= 0) continue;
         const int half = use & 1;
-        if (!(ok = bar_wait(sums_empty + 8 * half, (use >> 1 & 1) ^ 1))) break;
+        if (!(ok = bar_wait_warp(sums_empty + 8 * half, (use >> 1 & 1) ^ 1))) break;
         products_fence_after();
         const bool a_across = kForm == 2 && t.job == 1, b_across = kForm == 2;
         const uint32_t kind = product_kind(a.bf16, a_across, b_across, kTile, kTile);
         const uint32_t to = sums + half * kTile;
         for (int k = 0; k < t.steps; k++) {
-          if (!(ok = bar_wait(full + 8 * s, turn))) break;
+          if (!(ok = bar_wait_warp(full + 8 * s, turn))) break;
           products_fence_after();
           if (one_lane()) {
             const uint32_t A = stages + s * kStage, B = A + kOperand;
@@ -641,7 +641,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       const int half = use & 1;
       const uint32_t from = sums + half * kTile + off + ((uint32_t)quarter * 32 << 16);
       if (t.steps > 0) {
-        if (!(ok = bar_wait(sums_full + 8 * half, use >> 1 & 1))) return false;
+        if (!(ok = bar_wait_warp(sums_full + 8 * half, use >> 1 & 1))) return false;
         products_fence_after();
       }
       rows(from);

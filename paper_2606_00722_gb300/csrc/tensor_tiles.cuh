@@ -72,6 +72,17 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {
     if (clock64() - t > kWaitCycles) return false;
   return true;
 }
+// The lanes of a warp that wait together go on or give up as one: their clocks need not agree on a wait that ends near the limit,
+// and elections, loads and stores of tensor memory want all of them.
+__device__ __forceinline__ bool all_came(bool ok) { return __all_sync(~0u, ok); }
+__device__ __forceinline__ bool bar_wait_warp(uint32_t bar, uint32_t parity) {
+  if (all_came(bar_try(bar, parity))) return true;
+  const long long t = clock64();
+  do {
+    if (all_came(bar_try(bar, parity))) return true;
+  } while (!__any_sync(~0u, clock64() - t > kWaitCycles));
+  return false;
+}
 
 // A box of a tensor in two dimensions at (x, y) into this CTA's shared memory; its bytes are counted at `bar`, which may be
 // the pair's other CTA's.
