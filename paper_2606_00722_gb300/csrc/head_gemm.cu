@@ -34,7 +34,7 @@ constexpr int kShared = kStages * kStage + kWorkWarps * kTurn + 1024;
 
 struct Bars {
   uint64_t full[kStages], empty[kStages], sums_full[2], sums_empty[2];
-  uint32_t sums;
+  uint32_t sums, gave_up;
 };
 
 // One tile of a product: where its operands' boxes lie and how many steps its sum has
@@ -543,6 +543,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       bar_init(sums_full + 8 * s, 1);
       bar_init(sums_empty + 8 * s, 2 * kWorkWarps);
     }
+    bars.gave_up = 0;
     bar_init_visible();
   }
   if (threadIdx.x == 32)
@@ -682,7 +683,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   }
   if (!ok) {
     *a.p.failed = 1;
-    let_copies_land();
+    give_up(smem_address(&bars.gave_up));
   }
   products_fence_before();
   __syncwarp();
@@ -690,6 +691,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   cluster_arrive();
   cluster_wait();
   products_fence_after();
+  if (*(volatile uint32_t*)&bars.gave_up) {  // in both CTAs, or in neither
+    let_all_end();
+    __syncwarp();
+    cluster_arrive();
+    cluster_wait();
+  }
   if (warp == 1) sums_free_pair(sums);
 }
 

@@ -210,7 +210,7 @@ constexpr int kPairs = 76;
 
 struct Int8Bars {
   uint64_t full[kRing], empty[kRing], sums_full[2], sums_empty[2], come[10], gone[10];
-  uint32_t sums;
+  uint32_t sums, gave_up;
   int most[8];
 };
 
@@ -267,6 +267,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       bar_init(sums_empty + 8 * s, 2 * kWorkWarps);
     }
     for (int& m : bars.most) m = 0;
+    bars.gave_up = 0;
     bar_init_visible();
   }
   if (warp == kWorkWarps) sums_take_pair(smem_address(&bars.sums));
@@ -510,7 +511,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   }
   if (!ok) {
     *a.failed = 1;
-    let_copies_land();
+    give_up(smem_address(&bars.gave_up));
   }
   products_fence_before();
   __syncwarp();
@@ -518,6 +519,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   cluster_arrive();
   cluster_wait();
   products_fence_after();
+  if (*(volatile uint32_t*)&bars.gave_up) {  // in both CTAs, or in neither
+    let_all_end();
+    __syncwarp();
+    cluster_arrive();
+    cluster_wait();
+  }
   if (warp == kWorkWarps) sums_free_pair(sums);
 }
 

@@ -2,8 +2,9 @@
 // tensors (TMA), products into tensor memory (tcgen05), for kernels that compute
 // tiles of 256 x 256 by pairs of CTAs.
 //
-// Every wait gives up after kWaitCycles (some 4 s); a kernel whose wait gave up notes it,
-// leaves its loops, lets its copies land and frees its tensor memory.
+// Every wait gives up after kWaitCycles (some 4 s).  A thread whose wait gave up tells both
+// CTAs of its pair and leaves its loops; when all threads of the pair have left theirs, what
+// is in flight has time to end before tensor memory is freed.
 #pragma once
 #include <cuda.h>
 #include <cuda_runtime.h>
@@ -211,8 +212,13 @@ __device__ __forceinline__ void operand_store(uint32_t to, const uint32_t (&v)[1
 }
 __device__ __forceinline__ void operand_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// a microsecond's worth of waiting for copies in flight, many times over: after a wait that gave up
-__device__ __noinline__ void let_copies_land() {
+// A thread's wait gave up: noted in `flag` of both CTAs, which the pair's next barrier makes known
+__device__ __forceinline__ void give_up(uint32_t flag) {
+  for (uint32_t r = 0; r < 2; r++) asm volatile("st.shared::cluster.u32 [%0], 1;" ::"r"(at_rank(flag, r)) : "memory");
+}
+// a microsecond's worth of waiting for copies and products in flight, many times over: after a wait that gave up, when no thread
+// of the pair starts others
+__device__ __noinline__ void let_all_end() {
   for (int i = 0; i < 2000; i++) __nanosleep(1000);
 }
 
