@@ -424,6 +424,10 @@ epic_status epic_distill_step(const void* d_logits, int32_t dtype, int32_t B, in
  * their own.  A workspace is device memory of the caller's, aligned to 256 bytes, of at
  * least the size that the call's *_workspace function gives for the same sizes and
  * head; its contents do not matter and nothing is kept in it from call to call.
+ * Waits inside the kernels on the tensor units (none in a sound run) end after
+ * EPIC_HEAD_WAIT_MS [4000]; the status of the call is EPIC_OK by then.  NaN stands for
+ * what was not made so: logits of some tokens, losses and gradients of positions with
+ * such logits, rows of gradients.
  */
 
 /* The forms of the head's loss, for epic_head_loss_workspace */

@@ -54,6 +54,7 @@ struct TileArgs {
   HeadSum sum;
   int bf16;
   int pairs;  // of CTAs
+  long long wait;  // limit of a wait, in clocks
 };
 
 __device__ __forceinline__ int up_div(int a, int b) { return (a + b - 1) / b; }
@@ -521,6 +522,38 @@ __device__ __forceinline__ void grad_rows(const TileArgs& a, const HeadMaps& map
   }
 }
 
+// NaN to a row's half, kHalf columns from `half` on, of all of a pair's tiles: whatever comes of them is NaN, too
+template <typename T, int kForm>
+__device__ __noinline__ void spoil_tiles(const TileArgs& a, int n, int pair, int row_of_tile, int half) {
+  const HeadPlan& p = a.p;
+  typename std::conditional<kForm == 2, GradTasks, LogitsTasks>::type tasks(a, n, pair);
+  Task t;
+  while (tasks.next(t)) {
+    const long long row = t.m0 + row_of_tile;
+    const int col = t.n0 + half;
+    if (kForm != 2) {
+      if (row >= n) continue;
+      if (a.pass.sums && col < p.V) p.rec[(long long)(col / kRecCols) * p.cap + row] = make_float2(0.0f, CUDART_NAN_F);
+      if (kForm == 1)
+        for (long long c = col; c < min(col + (long long)kHalf, p.lde); c++) ((T*)p.e)[row * p.lde + c] = of_float<T>(CUDART_NAN_F);
+      continue;
+    }
+    const GradSplit& sp = p.split;
+    const bool hidden = t.job == 0;
+    if (row >= (hidden ? n : p.V)) continue;
+    float* sums = nullptr;
+    if ((hidden ? sp.hidden_parts : sp.head_parts) > 1)
+      sums = (hidden ? sp.hidden + t.part * (long long)p.cap * p.ldp : sp.head + t.part * sp.tokens * p.ldp) + row * p.ldp;
+    else if (!hidden && a.sum != kOnly && a.sum != kLast)
+      sums = p.acc + row * p.ldp;
+    T* to = hidden ? (T*)a.out.grad + p.to[row] : (T*)a.grad_head + row * a.grad_head_stride;
+    for (int c = col; c < min(col + kHalf, p.d); c++) {
+      if (sums) sums[c] = CUDART_NAN_F;
+      else to[c] = of_float<T>(CUDART_NAN_F);
+    }
+  }
+}
+
 // kForm 0: records; 1: exponentials (and records); 2: gradients
 template <typename T, int kForm>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
@@ -566,7 +599,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   const bool again = *a.p.again != 0;
   const int n = *a.p.count;
   typename std::conditional<kForm == 2, GradTasks, LogitsTasks>::type tasks(a, n, pair);
-  bool ok = true;
+  bool ok = a.wait > 0;
   if (warp == 0) {
     if (lane == 0) {  // copies
       const uint32_t full0 = at_rank(full, 0);
@@ -576,7 +609,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       while (ok && tasks.next(t)) {
         const int m = t.m0 + rank * kHalf, c = t.n0 + rank * kHalf;
         for (int k = t.k0; k < t.k0 + t.steps; k++) {
-          if (!(ok = bar_wait(empty + 8 * s, turn ^ 1))) break;
+          if (!(ok = bar_wait(empty + 8 * s, turn ^ 1, a.wait))) break;
           if (rank == 0) bar_expect(full + 8 * s, 2 * kStage);
           const uint32_t A = stages + s * kStage, B = A + kOperand, bar = full0 + 8 * s;
           // 128 rows of 64 along the sum, or 64 of the sum by 128 across it: two boxes each
@@ -601,13 +634,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       while (ok && tasks.next(t)) {
         if (t.steps <= 0) continue;
         const int half = use & 1;
-        if (!(ok = bar_wait_warp(sums_empty + 8 * half, (use >> 1 & 1) ^ 1))) break;
+        if (!(ok = bar_wait_warp(sums_empty + 8 * half, (use >> 1 & 1) ^ 1, a.wait))) break;
         products_fence_after();
         const bool a_across = kForm == 2 && t.job == 1, b_across = kForm == 2;
         const uint32_t kind = product_kind(a.bf16, a_across, b_across, kTile, kTile);
         const uint32_t to = sums + half * kTile;
         for (int k = 0; k < t.steps; k++) {
-          if (!(ok = bar_wait_warp(full + 8 * s, turn))) break;
+          if (!(ok = bar_wait_warp(full + 8 * s, turn, a.wait))) break;
           products_fence_after();
           if (one_lane()) {
             const uint32_t A = stages + s * kStage, B = A + kOperand;
@@ -642,7 +675,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       const int half = use & 1;
       const uint32_t from = sums + half * kTile + off + ((uint32_t)quarter * 32 << 16);
       if (t.steps > 0) {
-        if (!(ok = bar_wait_warp(sums_full + 8 * half, use >> 1 & 1))) return false;
+        if (!(ok = bar_wait_warp(sums_full + 8 * half, use >> 1 & 1, a.wait))) return false;
         products_fence_after();
       }
       rows(from);
@@ -659,7 +692,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       Task ahead = {a.p.V, 0, 0, 0, 1, 0};
       bool more = tasks.next(ahead);
       GradRow with_ahead(a, n, again, post, ahead, row_of_tile);  // a tile before it is needed
-      while (more) {
+      while (ok && more) {
         t = ahead;
         GradRow with = with_ahead;
         with.factors(a, t);
@@ -669,7 +702,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           break;
       }
     } else {
-      while (tasks.next(t)) {
+      while (ok && tasks.next(t)) {
         const int row = t.m0 + row_of_tile;
         const LogitsRow is(a, kForm == 1, n, row);
         if (!tile(t, [&](uint32_t from) {
@@ -681,10 +714,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     }
     if (lane == 0) boxes_read<0>();
   }
-  if (!ok) {
-    *a.p.failed = 1;
-    give_up(smem_address(&bars.gave_up));
-  }
+  if (!ok) give_up(smem_address(&bars.gave_up));
   products_fence_before();
   __syncwarp();
   __syncthreads();
@@ -693,7 +723,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   products_fence_after();
   if (*(volatile uint32_t*)&bars.gave_up) {  // in both CTAs, or in neither
     let_all_end();
-    __syncwarp();
+    if (warp >= 4 && lane == 0) boxes_stored();
+    __syncthreads();
+    if (warp >= 4) spoil_tiles<T, kForm>(a, n, pair, rank * kHalf + threadIdx.x % kHalf, threadIdx.x / kHalf % 2 * kHalf);
+    __syncthreads();
     cluster_arrive();
     cluster_wait();
   }
@@ -805,6 +838,7 @@ epic_status launch_head_logits(const HeadPlan& p, const HeadMaps& maps, int dtyp
   a.p = p;
   a.pass = pass;
   a.bf16 = dtype == EPIC_BF16;
+  a.wait = wait_limit();
   a.pairs = pairs_for(up_tiles(p.rows) * up_tiles(p.V));
   if (pass.probs) return a.bf16 ? launch_tiles<__nv_bfloat16, 1>(maps, a, st) : launch_tiles<__half, 1>(maps, a, st);
   return a.bf16 ? launch_tiles<__nv_bfloat16, 0>(maps, a, st) : launch_tiles<__half, 0>(maps, a, st);
@@ -819,6 +853,7 @@ epic_status launch_head_grads(const HeadPlan& p, const HeadMaps& maps, int dtype
   a.grad_head_stride = stride;
   a.sum = sum;
   a.bf16 = dtype == EPIC_BF16;
+  a.wait = wait_limit();
   if (!out.grad) a.p.split.hidden_parts = 0;
   if (!grad_head) a.p.split.head_parts = 0;
   a.pairs = pairs_for(up_tiles(p.d) * (a.p.split.hidden_parts * up_tiles(p.rows) + a.p.split.head_parts * up_tiles(p.V)));

@@ -90,7 +90,7 @@ struct Int8Args {
   void* logits;
   long long stride_b, stride_n;
   int rows, k, d, V;
-  int* failed;
+  long long wait;    // limit of a wait, in clocks
   const int* sizes;  // [rows][ceil(d / 1024)], added up over 1,024 each
 };
 
@@ -238,6 +238,21 @@ __device__ __forceinline__ uint4 load_shared(uint32_t at) {
   asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
   return v;
 }
+// NaN to the logits of all of a pair's tiles, a thread a token.  (Sizes are hidden from the compiler, which else keeps what it knows
+// of them in registers through the whole kernel.)
+template <typename T, int kRows>
+__device__ __forceinline__ void spoil_tiles(const Int8Args& a) {
+  int rows = a.rows, V = a.V, t = blockIdx.x / 2, at = threadIdx.x;
+  asm volatile("" : "+r"(rows), "+r"(V), "+r"(t), "+r"(at));
+  const int row_tiles = (rows + kRows - 1) / kRows, tiles = (int)((V + (long long)kTileTokens - 1) / kTileTokens) * row_tiles;
+  for (; t < tiles; t += kPairs) {
+    const long long v = (long long)(t / row_tiles) * kTileTokens + cluster_rank() * kHalf + at % kHalf;
+    const int r0 = t % row_tiles * kRows;
+    for (int r = r0 + at / kHalf; r < min(r0 + kRows, rows); r += kWork / kHalf)
+      if (v < a.V) ((T*)a.logits)[r / a.k * a.stride_b + r % a.k * a.stride_n + v] = of_float<T>(CUDART_NAN_F);
+  }
+}
+
 // kRows: rows of a tile.  kAskew: rows of the head start anywhere.
 template <typename T, int kRows, bool kAskew>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
@@ -303,7 +318,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   // tensor memory: sums, twice if they leave room for the operand's ring in the last 256 columns
   constexpr int kSums = kRows == 256 ? 1 : 2;
   const uint32_t operands = sums + 256;
-  bool ok = true;
+  bool ok = a.wait > 0;
 
   // Of 96 registers a thread that a block of 256 rows is launched with, 61,440, the four warpgroups that hold sums take 112
   // each and leave the last one 32.
@@ -316,7 +331,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       for (int t = pair; ok && t < tiles; t += kPairs) {
         const int r0 = t % row_tiles * kRows + rank * (kRows / 2);
         for (int k = 0; k < steps; k++) {
-          if (!(ok = bar_wait(empty + 8 * s, turn ^ 1))) break;
+          if (!(ok = bar_wait(empty + 8 * s, turn ^ 1, a.wait))) break;
           if (rank == 0) bar_expect(full + 8 * s, 2 * kBoxBytes);
           load_box_pair(&q_map, ring + s * kOperand, full0 + 8 * s, k * kStepK, r0);
           if (++s == kRing) s = 0, turn ^= 1;
@@ -329,7 +344,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       for (int t = pair; ok && t < tiles; t += kPairs) {
         const int v0 = t / row_tiles * kTileTokens + rank * kHalf;
         for (int k = 0; k < steps; k++) {
-          if (!(ok = bar_wait(gone + 8 * s, turn ^ 1))) break;
+          if (!(ok = bar_wait(gone + 8 * s, turn ^ 1, a.wait))) break;
           bar_expect(come + 8 * s, Q::kUnit);
           load_box(&head_map, queue + s * Q::kUnit, come + 8 * s, k * kStepK, v0);
           if (++s == Q::kUnits) s = 0, turn ^= 1;
@@ -343,10 +358,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       for (int t = pair; ok && t < tiles; t += kPairs) {
         for (int k = 0; ok && k < steps; use++) {
           const int half = use % kSums, end = min(k + exact, steps);
-          if (!(ok = bar_wait_warp(sums_empty + 8 * half, (use / kSums & 1) ^ 1))) break;
+          if (!(ok = bar_wait_warp(sums_empty + 8 * half, (use / kSums & 1) ^ 1, a.wait))) break;
           products_fence_after();
           for (bool add = false; k < end; k++) {
-            if (!(ok = bar_wait_warp(full + 8 * s, turn))) break;
+            if (!(ok = bar_wait_warp(full + 8 * s, turn, a.wait))) break;
             products_fence_after();
             if (one_lane()) {
               const uint64_t b = operand_k(ring + s * kOperand);
@@ -400,7 +415,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     };
     auto take = [&] {
       const int half = use % kSums;
-      if (!(ok = bar_wait_warp(sums_full + 8 * half, use / kSums & 1))) return;
+      if (!(ok = bar_wait_warp(sums_full + 8 * half, use / kSums & 1, a.wait))) return;
       products_fence_after();
       const bool first = use % per == 0;
 #pragma unroll
@@ -473,9 +488,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         copies_wait<kAhead - 1>();
         __syncwarp();
       } else {  // (lanes agree behind the step's work, within its memory: here it costs 1.6 % of 4,096 rows through 126,000 x 2,048)
-        ok = bar_wait(come + 8 * place, n / Q::kUnits & 1);
+        ok = bar_wait(come + 8 * place, n / Q::kUnits & 1, a.wait);
       }
-      ok &= bar_wait(empty + 8 * s, (n / kRing & 1) ^ 1);
+      ok &= bar_wait(empty + 8 * s, (n / kRing & 1) ^ 1, a.wait);
       products_fence_after();
       uint32_t m = 0;  // bytes ahead of the token's row in its first 16
       if (kAskew) {
@@ -509,10 +524,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       for (k += kTeams; k >= steps; k -= steps) tile++;
     }
   }
-  if (!ok) {
-    *a.failed = 1;
-    give_up(smem_address(&bars.gave_up));
-  }
+  if (!ok) give_up(smem_address(&bars.gave_up));
   products_fence_before();
   __syncwarp();
   __syncthreads();
@@ -521,7 +533,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   products_fence_after();
   if (*(volatile uint32_t*)&bars.gave_up) {  // in both CTAs, or in neither
     let_all_end();
-    __syncwarp();
+    __syncthreads();
+    if (warp < kWorkWarps) spoil_tiles<T, kRows>(a);  // (the other warps lack the registers)
+    __syncthreads();
     cluster_arrive();
     cluster_wait();
   }
@@ -529,11 +543,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 }
 
 // Hidden states of 8 bits as fp16, rows of a multiple of 16 bytes, a CTA a row; and their sizes, added up over 1,024 each
-__global__ void __launch_bounds__(256) k_rows_as_halves(const int8_t* q, __half* to, int d, int ld, int* sizes, int* failed) {
+__global__ void __launch_bounds__(256) k_rows_as_halves(const int8_t* q, __half* to, int d, int ld, int* sizes) {
   __shared__ uint32_t s_sum[kMostProducts / 1024 + 1];
   follow();
   let_next();
-  if (blockIdx.x == 0 && threadIdx.x == 0) *failed = 0;
   const int blocks = (d + 1023) / 1024;
   for (int i = threadIdx.x; i < blocks; i += 256) s_sum[i] = 0;
   __syncthreads();
@@ -610,12 +623,12 @@ epic_status launch_int8(Int8Args a, void* ws, cudaStream_t st) {
     if (a.rows <= 2) return launch_few<T, 2>(a, st);
     return a.rows <= 4 ? launch_few<T, 4>(a, st) : launch_few<T, 8>(a, st);
   }
-  a.failed = (int*)ws;
-  int* sizes = (int*)((char*)ws + 256);
-  __half* q16 = (__half*)((char*)ws + 256 + sizes_bytes(a.rows, a.d));
+  a.wait = wait_limit();
+  int* sizes = (int*)ws;
+  __half* q16 = (__half*)((char*)ws + sizes_bytes(a.rows, a.d));
   const int ld = (a.d + 7) / 8 * 8;
   a.sizes = sizes;
-  const epic_status s = launch_next(k_rows_as_halves, a.rows, 256, 0, kNoCache, st, a.q, q16, a.d, ld, sizes, a.failed);
+  const epic_status s = launch_next(k_rows_as_halves, a.rows, 256, 0, kNoCache, st, a.q, q16, a.d, ld, sizes);
   if (s != EPIC_OK) return s;
   switch (tile_rows(a.rows)) {
     case 32: return launch_tiles<T, 32>(a, q16, ld, askew, st);
@@ -663,7 +676,8 @@ epic_status epic_int8_logits_workspace(int32_t B, int32_t k, int32_t d, int32_t 
   if (d > kMostProducts || V > 0x7fffffff - 4096 || (long long)B * k > kMostRows) return EPIC_ERR_CAPACITY;
   const long long rows = (long long)B * k;
   *bytes = 256;
-  if (!few_rows(rows, d, head_lies_askew(d_head, head_stride, V))) *bytes += sizes_bytes(rows, d) + (size_t)rows * ((d + 7) / 8 * 8) * 2;
+  if (!few_rows(rows, d, head_lies_askew(d_head, head_stride, V)))
+    *bytes = std::max(*bytes, sizes_bytes(rows, d) + (size_t)rows * ((d + 7) / 8 * 8) * 2);
   return EPIC_OK;
 }
 
@@ -682,7 +696,7 @@ epic_status epic_int8_logits(const int8_t* d_q, const float* d_scale, int32_t B,
       (uintptr_t)d_scale % 4 || (uintptr_t)d_head_scale % 4)
     return EPIC_ERR_INVALID_ARG;
   if (!d_workspace || (uintptr_t)d_workspace % 256 || workspace_bytes < need) return EPIC_ERR_INVALID_ARG;
-  const Int8Args a = {d_q, d_scale, d_head, head_stride, d_head_scale, d_logits, stride_b, stride_n, (int)rows, k, d, V, nullptr};
+  const Int8Args a = {d_q, d_scale, d_head, head_stride, d_head_scale, d_logits, stride_b, stride_n, (int)rows, k, d, V};
   cudaStream_t st = (cudaStream_t)cuda_stream;
   switch (dtype) {
     case EPIC_F32: return launch_int8<float>(a, d_workspace, st);

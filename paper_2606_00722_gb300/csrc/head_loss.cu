@@ -142,7 +142,7 @@ __global__ void __launch_bounds__(kRowsThreads) k_head_rows(RowsArgs a) {
   before = all = 0, top = 0.0f;
   for (int w = 0; w < warps; w++) before += s_before[w], all += s_all[w], top = fmaxf(top, s_top[w]);
   const float post = a.scaled ? pow2_above(top) * pow2_whole(-kHalfScale) : 1.0f;
-  if (blockIdx.x == 0 && threadIdx.x == 0) *p.count = all, *p.failed = 0, *p.again = a.again, *p.post = post;
+  if (blockIdx.x == 0 && threadIdx.x == 0) *p.count = all, *p.again = a.again, *p.post = post;
 
   const int at = kWide ? threadIdx.x : lane, step = kWide ? kRowsThreads : 32;  // in a row
   for (int i0 = first; i0 < last; i0 += 32) {
@@ -301,7 +301,7 @@ __global__ void __launch_bounds__(kMeetWarps * 32) k_head_meet(MeetArgs a) {
         const float zt = p.zt[q], by = s == 0.0f && zt > -CUDART_INF_F ? -CUDART_INF_F : log2f(s) + fmaf(-zt, kLog2E, ref);
         const float x = by * kLn2, small = expf(-fabsf(x)), rest = log1pf(small);
         float nll = x > 0.0f ? x + rest : rest;
-        if (!(zt < CUDART_INF_F) || s != s || *p.failed) nll = CUDART_NAN_F;
+        if (!(zt < CUDART_INF_F) || s != s) nll = CUDART_NAN_F;
         const float lse = x > 0.0f ? (ref + log2f(s)) * kLn2 + rest : zt + nll;
         const long long r = a.r0 + p.src[q];
         a.loss[r] = (a.weight ? a.weight[r] : 1.0f) * nll;
@@ -442,7 +442,6 @@ size_t plan_head(const HeadCall& c, void* base, HeadPlan& p) {
   const size_t cap = p.cap;
   Carver w = {(char*)base, 0};
   w.take(p.count, 1, 4);
-  w.take(p.failed, 1, 4);
   w.take(p.again, 1, 4);
   w.take(p.post, 1, 4);
   w.take(p.counts, kPieceRows / kRowsThreads, 4);

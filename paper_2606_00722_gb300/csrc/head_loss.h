@@ -31,7 +31,6 @@ struct HeadPlan {
   long long ldh, lde, ldw;  // elements from row to row of hc and hs, of e, of the head
   const void* head;         // [V][ldw]
   int* count;               // rows that count
-  int* failed;              // != 0: a wait gave up
   int* again;               // != 0: e holds gradients of logits; see below
   float* post;              // power of two that gradients of logits in e are multiplied with
   int* counts;              // of 256 positions each, and the largest factor among them

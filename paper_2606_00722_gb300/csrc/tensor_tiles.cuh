@@ -2,18 +2,20 @@
 // tensors (TMA), products into tensor memory (tcgen05), for kernels that compute
 // tiles of 256 x 256 by pairs of CTAs.
 //
-// Every wait gives up after kWaitCycles (some 4 s).  A thread whose wait gave up tells both
-// CTAs of its pair and leaves its loops; when all threads of the pair have left theirs, what
-// is in flight has time to end before tensor memory is freed.
+// Every wait gives up after a limit, in clocks; a limit of 0 is up before the first one.
+// A thread whose wait gave up tells both CTAs of its pair and leaves its loops; when all
+// threads of the pair have left theirs, what is in flight has time to end, the pair writes
+// NaN to all that it was to write, and tensor memory is freed.
 #pragma once
 #include <cuda.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
+#include <stdlib.h>
+
+#include <algorithm>
 
 namespace epic {
 namespace {
-
-constexpr long long kWaitCycles = 1ll << 33;
 
 __device__ __forceinline__ uint32_t smem_address(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ uint32_t cluster_rank() {
@@ -66,22 +68,22 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
   return done;
 }
 // false: gave up
-__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, long long limit) {
   if (bar_try(bar, parity)) return true;
   const long long t = clock64();
   while (!bar_try(bar, parity))
-    if (clock64() - t > kWaitCycles) return false;
+    if (clock64() - t > limit) return false;
   return true;
 }
 // The lanes of a warp that wait together go on or give up as one: their clocks need not agree on a wait that ends near the limit,
 // and elections, loads and stores of tensor memory want all of them.
 __device__ __forceinline__ bool all_came(bool ok) { return __all_sync(~0u, ok); }
-__device__ __forceinline__ bool bar_wait_warp(uint32_t bar, uint32_t parity) {
+__device__ __forceinline__ bool bar_wait_warp(uint32_t bar, uint32_t parity, long long limit) {
   if (all_came(bar_try(bar, parity))) return true;
   const long long t = clock64();
   do {
     if (all_came(bar_try(bar, parity))) return true;
-  } while (!__any_sync(~0u, clock64() - t > kWaitCycles));
+  } while (!__any_sync(~0u, clock64() - t > limit));
   return false;
 }
 
@@ -113,6 +115,8 @@ template <int kLeft>
 __device__ __forceinline__ void boxes_read() {
   asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kLeft) : "memory");
 }
+// the thread's stores are done
+__device__ __forceinline__ void boxes_stored() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 __device__ __forceinline__ void prefetch_map(const CUtensorMap* map) {
   asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
 }
@@ -223,6 +227,14 @@ __device__ __noinline__ void let_all_end() {
 }
 
 // ---- on the host
+
+// EPIC_HEAD_WAIT_MS [4000] in clocks of some 2.1 GHz
+inline long long wait_limit() {
+  const char* e = getenv("EPIC_HEAD_WAIT_MS");
+  char* end = nullptr;
+  const long long ms = e ? strtoll(e, &end, 10) : 0;
+  return (e && end != e ? std::min(std::max(ms, 0ll), 1ll << 31) : 4000) * 2100000;
+}
 
 typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
