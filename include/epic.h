@@ -460,7 +460,9 @@ enum { EPIC_HEAD_FORWARD = 0, EPIC_HEAD_BACKWARD = 1, EPIC_HEAD_STEP = 2 };
  * in a piece (of 16,384 or fewer).  In fp16 they are held relative to the largest
  * |w grad_loss| of 16,384 positions: what is below 2^-28 of it loses bits, below 2^-39 all.
  * Sums of the products are the tensor units', which cut what they add to 32 bits.
- * A target of probability 0 gives loss +inf and a finite gradient.  NaN or +inf
+ * A target of probability 0 (a logit of -inf, which finite weights make where 32 bits
+ * end) gives loss +inf and, of finite weights, a finite gradient: 0 times an infinite weight
+ * is NaN, in that component of all hidden states' gradients.  NaN or +inf
  * logits give NaN, in the gradient of the head at all tokens.  What is in the rows of
  * positions that do not count does not matter.
  * The same call on the same inputs gives the same bits.
