@@ -439,8 +439,10 @@ enum { EPIC_HEAD_FORWARD = 0, EPIC_HEAD_BACKWARD = 1, EPIC_HEAD_STEP = 2 };
  * outside 0..V-1, such as -1, says that the position does not count), weighted by
  * w = d_weight [B][n] float32 (NULL: 1; a position of weight 0 does not count):
  *   loss = w (lse - z[target]),  lse = log sum_v exp z[v]
- * The logits are never kept: they are made in pieces, and of a step or backward call
- * at most EPIC_HEAD_PIECE_MB [2048] of exponentials exist at a time, in 16 bits.
+ * The logits are never kept: calls go through their positions in pieces, of which a step
+ * or backward call keeps exponentials in 16 bits, a forward call 8 bytes for each 128
+ * tokens.  A piece has at most EPIC_HEAD_PIECE_MB [2048] of them, or 256 positions if those
+ * have more, and at most 16,384 positions.
  * dtype is EPIC_F16 or EPIC_BF16, of hidden states, head and both gradients.  Products
  * are of that type with sums in 32 bits.
  * epic_head_loss_forward: d_loss and d_lse [B][n] float32, 0 where a position does

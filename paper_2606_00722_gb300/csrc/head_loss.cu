@@ -434,9 +434,11 @@ size_t plan_head(const HeadCall& c, void* base, HeadPlan& p) {
   p.lde = round_up(std::max(c.V, 1), 64);
   p.ldp = round_up(c.d, 32);
   p.nrec = (c.V + kRecCols - 1) / kRecCols;
-  size_t bytes = (size_t)2048 << 20;  // of exponentials
+  // of what a position keeps: exponentials, or without gradients its records
+  const size_t row = c.form != kForward ? p.lde * 2 : std::max(p.nrec, 1) * sizeof(float2);
+  size_t bytes = (size_t)2048 << 20;
   if (const char* e = getenv("EPIC_HEAD_PIECE_MB")) bytes = strtoull(e, nullptr, 10) << 20;
-  const long long fit = (long long)(bytes / (p.lde * 2)) / kRowTile * kRowTile;
+  const long long fit = (long long)(bytes / row) / kRowTile * kRowTile;
   p.cap = (int)std::min<long long>(round_up(std::max(rows, 1ll), kRowTile),
                                    std::min<long long>(kPieceRows, std::max<long long>(kRowTile, fit)));
   const size_t cap = p.cap;
