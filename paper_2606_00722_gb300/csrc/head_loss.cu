@@ -521,7 +521,7 @@ epic_status run_head(const HeadCall& c, const HeadTensors& t, HeadPlan p, cudaSt
     a.lse = t.lse_in;
     a.loss = t.loss;
     a.lse_out = t.lse;
-    a.out = {t.grad_hidden, t.gstride_b, t.gstride_n, r0, c.n};
+    a.out = {t.grad_hidden, t.gstride_b, t.gstride_n};
     // Few positions have a CTA each: a step of 100 x 8,000 x 2,048 takes 53 us so and 63 with a warp a position, of 300 x 4,000 x
     // 1,024 42 and 45, of 600 x 8,000 x 2,048 89 and 100.
     const bool few = p.rows <= kFewRows;

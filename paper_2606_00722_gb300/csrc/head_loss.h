@@ -62,11 +62,10 @@ struct HeadPlan {
 // How a piece's gradient of the head meets the pieces before it
 enum HeadSum { kOnly = 0, kFirst = 1, kMiddle = 2, kLast = 3 };
 
-// Where gradients of hidden states go: position r of the piece is position r0 + r of [b][n].
+// Where gradients of hidden states [B][n][d] go; a packed row's begins `to` elements behind
 struct HiddenGrad {
   void* grad;
-  long long stride_b, stride_n, r0;
-  int n;
+  long long stride_b, stride_n;
 };
 
 // Logits of the packed rows.  sums: records and target logits.  probs: e, with a known logsumexp or not.  only_again: nothing
