@@ -418,12 +418,13 @@ epic_status epic_distill_step(const void* d_logits, int32_t dtype, int32_t B, in
  * states [B][n][d] (element c of position i of sequence b at b * stride_b + i *
  * stride_n + c, strides >= 0 in elements, rows may start at any multiple of the
  * element size) and the weights [V][d] of the output layer, a row of which is at
- * v * head_stride.  (Rows that start at no multiple of 16 bytes may be read from the 16
- * bytes that they begin in to those that they end in.)  They allocate nothing, are asynchronous on `cuda_stream`, may be
- * captured in a CUDA graph, and may overlap on different streams with workspaces of
- * their own.  A workspace is device memory of the caller's, aligned to 256 bytes, of at
- * least the size that the call's *_workspace function gives for the same sizes and
- * head; its contents do not matter and nothing is kept in it from call to call.
+ * v * head_stride.  (Rows of a head may be read from the aligned 16 bytes that they begin
+ * in to those that they end in; what is beside a row there does not matter.)  They
+ * allocate nothing, are asynchronous on `cuda_stream`, may be captured in a CUDA graph,
+ * and may overlap on different streams with workspaces of their own.  A workspace is
+ * device memory of the caller's, aligned to 256 bytes, of at least the size that the
+ * call's *_workspace function gives for the same sizes and head; its contents do not
+ * matter and nothing is kept in it from call to call.
  * Waits inside the kernels on the tensor units (none in a sound run) end after
  * EPIC_HEAD_WAIT_MS [4000]; the status of the call is EPIC_OK by then.  NaN stands for
  * what was not made so: logits of some tokens, losses and gradients of positions with
