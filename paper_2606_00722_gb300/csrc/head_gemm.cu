@@ -7,10 +7,11 @@
 // tokens and by hidden dimensions.
 //
 // A step of a tile takes the tensor units 512 clocks and 64 bytes a clock and SM from L2, about what L2 gives: a CTA's own
-// tile of 128 x 256 would need 96.  Of 4,096 rows through 32,768 x 2,048 the tensor pipe is active 91 % of the time for logits
-// alone, 82 % with exponentials, 87 % for both gradients (267, 290 and 579 us); of 4,096 through 126,000 x 4,096 they take 2.1,
-// 2.2 and 4.6 ms (1.9 to 2.0 PFLOP/s), at the power limit.  With few rows the head's bytes are the time: 32 through 126,000 x 4,096
-// 185 us (5.6 TB/s) for logits, 400 for the gradients, which read it once and write as much.
+// tile of 128 x 256 would need 96.  Of 4,096 rows through 32,768 x 2,048 the tensor pipe is active 95 % of the time for logits
+// alone, 84 % with exponentials, 88 % for both gradients (261, 289 and 582 us); of 4,096 through 126,000 x 4,096 they take 2.08,
+// 2.22 and 4.64 ms (2.03, 1.90 and 1.82 PFLOP/s) from rest, both calls 9.1 ms, and 10.1 one after another, at the power limit.  With
+// few rows the head's bytes are the time: 32 through 126,000 x 4,096 185 us (5.6 TB/s) for logits, 400 for the gradients, which
+// read it once and write as much.
 #include <cuda.h>
 
 #include <algorithm>

@@ -33,8 +33,11 @@ namespace {
 
 constexpr int kPieceRows = 16384;  // most positions of a piece
 constexpr int kRowsThreads = 256;
-constexpr int kFewRows = 608;   // positions that have a CTA each
-constexpr int kCounted = 1024;  // more positions are counted by a kernel before
+constexpr int kFewRows = 608;   // positions that have a CTA each; see run_head
+// More positions are counted by a kernel before, else by every CTA.  Steps with and without (us): 640 positions through 1,000 x 256
+// 33 and 31, 1,024 33 and 32, 4,096 45 and 45, 8,192 66 and 68; through 8,000 x 2,048 1,024 120 and 120, 4,096 290 and 292, 8,192 558
+// and 564.
+constexpr int kCounted = 1024;
 
 struct RowsArgs {
   HeadPlan p;
@@ -522,8 +525,9 @@ epic_status run_head(const HeadCall& c, const HeadTensors& t, HeadPlan p, cudaSt
     a.loss = t.loss;
     a.lse_out = t.lse;
     a.out = {t.grad_hidden, t.gstride_b, t.gstride_n};
-    // Few positions have a CTA each: a step of 100 x 8,000 x 2,048 takes 53 us so and 63 with a warp a position, of 300 x 4,000 x
-    // 1,024 42 and 45, of 600 x 8,000 x 2,048 89 and 100.
+    // Few positions have a CTA each, which pays by the row's width.  Steps with a CTA and with a warp a position (us): 300 positions
+    // through 1,000 x 256 34 and 33, 608 33 and 31, 1,000 35 and 33, 1,300 39 and 34; through 4,000 x 1,024 300 43 and 45, 608 49 and
+    // 51, 1,000 58 and 60, 1,300 74 and 74; through 8,000 x 2,048 300 70 and 77, 608 89 and 100, 1,000 109 and 119, 1,300 125 and 132.
     const bool few = p.rows <= kFewRows;
     a.per = few ? 1 : 8;
     const bool known = c.form == kBackward, stored = known || (grads && !half);

@@ -11,7 +11,11 @@ namespace epic {
 
 constexpr int kRowTile = 256;   // rows of a workspace come in whole tiles
 constexpr int kRecCols = 128;   // tokens whose exponentials one record sums
-constexpr int kListed = 4;      // (an int4) rows of one target whose gradient at it is kept in 32 bits
+// Rows of one target whose gradient at it is kept in 32 bits for the head's gradient (an int4).  With none, 1, 2 and 4 the head's
+// gradient of a step in bf16 is off by 0.0027, 0.0020, 0.0017 and 0.0017 of itself (500 rows, 1,000 tokens drawn alike), and by
+// 0.0027, 0.0022, 0.0021 and 0.0020 with targets as frequent as words (2,048 rows, 32,768 tokens); a step of 500 x 256 x 1,000 takes
+// 32, 33, 35 and 37 us, large ones the same within 2 %.
+constexpr int kListed = 4;
 constexpr int kMostParts = 64;  // of a gradient's sum
 
 // Few tiles with long sums are cut into parts, whose sums meet in a second kernel: of gradients of hidden states over the
